@@ -44,7 +44,7 @@ typedef enum mtp_status {
                                destroyed */
 } mtp_status;
 
-typedef enum mtp_dtype { MTP_F32 = 0, MTP_BF16 = 1 } mtp_dtype;
+typedef enum mtp_dtype { MTP_F32 = 0, MTP_BF16 = 1, MTP_F16 = 2 } mtp_dtype; /* F16: the paged beam search only */
 
 /* Acceptance of the selected path (Sec. III-C).
  *   MTP_ACCEPT_ALL      the paper's rule: the whole Viterbi path is accepted each
@@ -468,6 +468,117 @@ MTP_API int mtp_attention_noalloc(const mtp_attention_args* args, void* cuda_str
  * alignment), MTP_ERR_CUDA, MTP_ERR_DEVICE (a bounded wait ran out). */
 MTP_API int mtp_gemm_bf16x2(const void* w, const void* a_hi, const void* a_lo, float* out, int n_w, int k, int m,
                             int splits, int accumulate, void* cuda_stream);
+
+/* ---- paged beam search (device pointers, caller's stream) ---------------
+ *
+ * Operators for programs that keep a paged cache of their own, in memory they
+ * own.  The paper has no counterpart: they serve a model next to its codec model,
+ * or a beam search over the codec tokens in place of the Viterbi selection.
+ *
+ * The cache pool is bf16 or fp16 [n_pages][layers][2][n_kv_heads][page_size][head_dim],
+ * index 0 of the "2" axis keys, 1 values (mtp_attention's layout), 16-byte aligned.
+ * A slot is one sequence: its length, and a row of the block table with the pages of
+ * positions 0 .. length - 1, page_size (16, 32, 64 or 128) to a page.  page_refs[p] is
+ * the number of slots whose tables hold page p; 0 = free.  A slot's last page, where it
+ * is partly filled, is in no other table.
+ *
+ * The calls enqueue their kernels on the stream and return: nothing is synchronised,
+ * allocated or copied to the host, and all may be captured in a CUDA graph.  Sizes,
+ * types and pointers are checked on the host (MTP_ERR_INVALID, nothing is queued);
+ * what stands in device memory is checked on the device, and the outcome is in
+ * out_status.  The caller's buffers are on the current device. */
+
+/* Pages, block tables and row plan of the tokens that each slot gets in a step.
+ * Slot s of length kv_lens[s] gets new_lens[s] >= 0 tokens: the pages that positions
+ * kv_lens[s] .. kv_lens[s] + new_lens[s] - 1 lack are taken from the free ones, lowest
+ * number first, in the order of the slots, and entered into its row of the table.
+ *   kv_lens, new_lens  int32 [slots]
+ *   block_table        int32 [slots][bt_stride], new pages are added in place
+ *   page_refs          int32 [n_pages]
+ *   out_kv_lens        int32 [slots]: kv_lens + new_lens (may be kv_lens itself)
+ *   out_page_refs      int32 [n_pages]: page_refs with 1 at the new pages (may be page_refs itself)
+ *   out_cu_rows        int32 [slots + 1]: first row of every slot, then the number of rows
+ *   out_slot_map       int64 [max_rows]: page * page_size + offset of each new token, rows in
+ *                      the order of slots and positions; -1 past the last (and where the
+ *                      table holds no page of the pool)
+ *   out_row_seq, out_row_pos  int32 [max_rows]: slot and position (as mtp_attention takes
+ *                      them); -1 past the last
+ *   out_status         int32 [4]: {mtp_status, rows, pages taken, pages still free}.
+ * Where out_status[0] is MTP_ERR_NO_PAGES (fewer free pages than needed) or MTP_ERR_INVALID
+ * (a negative length, more than bt_stride pages for a slot, more than max_rows rows)
+ * nothing is taken: lengths, counts and table are as they were, and there are no rows.
+ * Limits: slots <= 8192, n_pages <= 2^22, max_rows <= 2^24, bt_stride * page_size <= 2^30.
+ * Errors: MTP_ERR_INVALID, MTP_ERR_CUDA. */
+typedef struct mtp_page_plan_args {
+    int32_t slots, page_size, n_pages, bt_stride, max_rows;
+    const int32_t* kv_lens;
+    const int32_t* new_lens;
+    int32_t* block_table;
+    const int32_t* page_refs;
+    int32_t* out_kv_lens;
+    int32_t* out_page_refs;
+    int32_t* out_cu_rows;
+    int64_t* out_slot_map;
+    int32_t* out_row_seq;
+    int32_t* out_row_pos;
+    int32_t* out_status;
+} mtp_page_plan_args;
+MTP_API int mtp_page_plan(const mtp_page_plan_args* args, void* cuda_stream);
+
+/* New keys and values into one layer of the cache: row r goes to place slot_map[r]
+ * (page * page_size + offset; rows with a place outside the pool, -1 among them, are
+ * left out; no place may occur twice).
+ *   k, v       [rows][n_kv_heads * head_dim] with row strides k_stride, v_stride (elements),
+ *              src_dtype (MTP_F32, or the pool's type: copied bit by bit); fp32 values are
+ *              rounded to nearest even
+ *   slot_map   int64 [rows]
+ *   kv_pool    the pool, pool_dtype MTP_BF16 or MTP_F16
+ * head_dim: a multiple of 8, at most 256.  Errors: MTP_ERR_INVALID, MTP_ERR_CUDA. */
+typedef struct mtp_cache_append_args {
+    int32_t rows, n_kv_heads, head_dim, page_size, layers, layer, n_pages, src_dtype, pool_dtype;
+    int64_t k_stride, v_stride;
+    const void* k;
+    const void* v;
+    const int64_t* slot_map;
+    void* kv_pool;
+} mtp_cache_append_args;
+MTP_API int mtp_cache_append(const mtp_cache_append_args* args, void* cuda_stream);
+
+/* The cache of the beams that a selection kept.  Slots are item * beams + beam; beam j of
+ * item b continues beam parent[b][j] (< 0: the beam ends and its slot becomes empty).
+ * Tables share the parent's pages.  A partly filled last page stays with the first of its
+ * children; each later child gets a free page (lowest number first, in the order of the
+ * slots) into which its filled rows are copied, in all layers.
+ *   parent         int32 [batch][beams]
+ *   block_table    int32 [batch * beams][bt_stride]; kv_lens int32 [batch * beams]
+ *   page_refs      int32 [n_pages]
+ *   kv_pool        the pool; only the pages taken are written
+ *   out_block_table, out_kv_lens  as block_table and kv_lens, in buffers of their own; table
+ *                  entries past a slot's last page are -1
+ *   out_page_refs  int32 [n_pages] (may be page_refs itself): pages that no kept beam holds
+ *                  drop to 0
+ *   out_status     int32 [4]: {mtp_status, pages copied, pages free afterwards, 0}.
+ * Where out_status[0] is MTP_ERR_NO_PAGES or MTP_ERR_INVALID (a parent past the beams, a length
+ * outside the table, a held page outside the pool or with a count below 1) the outputs
+ * repeat the inputs and no page is written.
+ *   workspace      mtp_beam_reorder_workspace_bytes(args) bytes, 16-byte aligned
+ * Limits: beams <= 64, batch * beams <= 8192, n_pages <= 2^22, bt_stride * page_size <= 2^30,
+ * head_dim a multiple of 8, at most 256.  Errors: MTP_ERR_INVALID, MTP_ERR_CUDA. */
+typedef struct mtp_beam_reorder_args {
+    int32_t batch, beams, page_size, n_pages, bt_stride, layers, n_kv_heads, head_dim, pool_dtype;
+    const int32_t* parent;
+    const int32_t* block_table;
+    const int32_t* kv_lens;
+    const int32_t* page_refs;
+    void* kv_pool;
+    int32_t* out_block_table;
+    int32_t* out_kv_lens;
+    int32_t* out_page_refs;
+    int32_t* out_status;
+} mtp_beam_reorder_args;
+MTP_API size_t mtp_beam_reorder_workspace_bytes(const mtp_beam_reorder_args* args);
+MTP_API int mtp_beam_reorder(const mtp_beam_reorder_args* args, void* workspace, size_t workspace_bytes,
+                             void* cuda_stream);
 
 #ifdef __cplusplus
 }

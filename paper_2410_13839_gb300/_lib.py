@@ -19,6 +19,7 @@ MTP_ERR_WEIGHTS = -4
 MTP_ERR_DEVICE = -5
 MTP_F32 = 0
 MTP_BF16 = 1
+MTP_F16 = 2
 MTP_ACCEPT_ALL = 0
 MTP_VERIFY_GREEDY = 1
 MTP_OPT_GRAPHS = 0
@@ -50,6 +51,24 @@ class MtpAttentionArgs(ctypes.Structure):
         "rows", "rows_per_group", "n_heads", "page_size", "layers", "layer", "bt_stride",
         "max_keys")] + [(name, ctypes.c_void_p) for name in (
             "q", "kv_pool", "block_table", "row_seq", "row_pos", "out")]
+
+
+def _struct(name: str, ints: str, strides: str, pointers: str):
+    """An argument block: int32 fields, then int64 fields, then pointers, as the header declares them."""
+    fields = [(n, ctypes.c_int32) for n in ints.split()] + [(n, ctypes.c_int64) for n in strides.split()]
+    return type(name, (ctypes.Structure,), {"_fields_": fields + [(n, ctypes.c_void_p) for n in pointers.split()]})
+
+
+MtpPagePlanArgs = _struct(
+    "MtpPagePlanArgs", "slots page_size n_pages bt_stride max_rows", "",
+    "kv_lens new_lens block_table page_refs out_kv_lens out_page_refs out_cu_rows out_slot_map out_row_seq "
+    "out_row_pos out_status")
+MtpCacheAppendArgs = _struct(
+    "MtpCacheAppendArgs", "rows n_kv_heads head_dim page_size layers layer n_pages src_dtype pool_dtype",
+    "k_stride v_stride", "k v slot_map kv_pool")
+MtpBeamReorderArgs = _struct(
+    "MtpBeamReorderArgs", "batch beams page_size n_pages bt_stride layers n_kv_heads head_dim pool_dtype", "",
+    "parent block_table kv_lens page_refs kv_pool out_block_table out_kv_lens out_page_refs out_status")
 
 
 class MTPError(RuntimeError):
@@ -94,6 +113,10 @@ def _load() -> ctypes.CDLL:
         "mtp_attention_tc_workspace_bytes": (sz, [ctypes.POINTER(MtpAttentionArgs)]),
         "mtp_attention_tc": (i32, [ctypes.POINTER(MtpAttentionArgs), vp, sz, vp]),
         "mtp_gemm_bf16x2": (i32, [vp, vp, vp, vp, i32, i32, i32, i32, i32, vp]),
+        "mtp_page_plan": (i32, [ctypes.POINTER(MtpPagePlanArgs), vp]),
+        "mtp_cache_append": (i32, [ctypes.POINTER(MtpCacheAppendArgs), vp]),
+        "mtp_beam_reorder_workspace_bytes": (sz, [ctypes.POINTER(MtpBeamReorderArgs)]),
+        "mtp_beam_reorder": (i32, [ctypes.POINTER(MtpBeamReorderArgs), vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)

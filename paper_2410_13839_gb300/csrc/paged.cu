@@ -1,0 +1,581 @@
+// paged.cu -- the paged cache's bookkeeping on the GPU: pages, block tables and
+// slot maps of a step's new tokens (mtp_page_plan), the new keys and values into
+// the cache (mtp_cache_append), and the cache of the beams that a selection keeps
+// (mtp_beam_reorder).
+//
+// A page is free where its count is zero.  Pages are taken lowest number first,
+// in the order of the requests, so the outcome does not depend on how the work is
+// spread: with f_0 < f_1 < ... the free pages and need(s) the pages that request s
+// lacks, request s takes f_{N(s)} .. f_{N(s) + need(s) - 1}, N(s) = sum_{s' < s} need(s').
+// Both sides are prefix sums: over the requests (every CTA makes the whole one, in
+// shared memory), and over the counts, of which each of the cluster's CTAs reads a
+// part once and keeps a bit per page; CTA totals go over distributed shared memory.
+// A free page then finds its request by a binary search of its rank.
+//
+// One cluster of eight CTAs does it in one launch: the steps need a barrier between
+// them (the ranks before the tables, the tables before the rows that look pages up),
+// and a cluster barrier is a fraction of a launch.  The plan's rows, of which a prompt
+// batch has hundreds of thousands, are written by the whole GPU in a second launch
+// where they are many.
+#include <climits>
+
+#include "serving.cuh"
+
+namespace mtp {
+namespace {
+
+constexpr int PG_CTAS = 8, PG_THREADS = 1024, PG_WARPS = PG_THREADS / 32;
+constexpr int PG_MAX_SLOTS = 8192;
+constexpr int PG_MAX_PAGES = 1 << 22;
+constexpr int PG_MAX_ROWS = 1 << 24;
+
+struct FreeBits {
+    uint32_t* bits;       // shared memory: a bit per page of this CTA's part, set where it is free
+    int first, words;     // the part: words [first, first + words) of 32 pages
+    int per;              // words of a thread, consecutive
+    long long before;     // free pages of the CTA before this thread's
+};
+
+__host__ __device__ inline int free_words(int n_pages) {  // words of a CTA's part
+    return ((n_pages + 31) / 32 + PG_CTAS - 1) / PG_CTAS;
+}
+
+// Reads this CTA's part of the counts once (and copies it, where they go to another
+// array); leaves the part's free pages in *total.
+__device__ __forceinline__ FreeBits find_free(const int* refs, int* out_refs, int n_pages, int rank, uint32_t* bits,
+                                              long long (*part)[2], int* total) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    FreeBits f;
+    const int all = (n_pages + 31) / 32, cap = free_words(n_pages);
+    f.bits = bits;
+    f.first = rank * cap;
+    f.words = max(0, min(cap, all - f.first));
+    const bool copy = out_refs != refs;
+    for (int w0 = warp; w0 < f.words; w0 += PG_WARPS * 4) {
+        int r[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int w = w0 + u * PG_WARPS, i = (f.first + w) * 32 + lane;
+            r[u] = w < f.words && i < n_pages ? refs[i] : 1;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int w = w0 + u * PG_WARPS, i = (f.first + w) * 32 + lane;
+            const unsigned b = __ballot_sync(FULL_MASK, r[u] == 0);
+            if (w < f.words) {
+                if (copy && i < n_pages) out_refs[i] = r[u];
+                if (lane == 0) bits[w] = b;
+            }
+        }
+    }
+    __syncthreads();
+    f.per = (f.words + PG_THREADS - 1) / PG_THREADS;
+    long long n = 0, unused = 0, sum, none;
+    for (int i = 0; i < f.per; ++i) {
+        const int w = tid * f.per + i;
+        if (w < f.words) n += __popc(bits[w]);
+    }
+    block_scan2<PG_WARPS>(n, unused, part, sum, none);
+    f.before = n;
+    if (tid == 0) *total = (int)sum;
+    return f;
+}
+
+// take(page, rank) for every free page of this thread's words whose rank among all is below `want`
+template <class F>
+__device__ __forceinline__ void take_free(const FreeBits& f, long long base, long long want, F take) {
+    long long rank = base + f.before;
+    for (int i = 0; i < f.per && rank < want; ++i) {
+        const int w = threadIdx.x * f.per + i;
+        if (w >= f.words) break;
+        for (uint32_t b = f.bits[w]; b && rank < want; b &= b - 1, ++rank)
+            take((f.first + w) * 32 + __ffs(b) - 1, (int)rank);
+    }
+}
+
+__device__ __forceinline__ int ld_dsmem_int(const int* p, int rank) {
+    int v;
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(dsmem_addr(p, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_barrier() {
+    cluster_arrive_release();
+    cluster_wait();
+}
+
+// largest s in [0, n) with before[s] <= x (before ascending, before[0] = 0 <= x)
+__device__ __forceinline__ int owner_of(const int* before, int n, int x) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (before[mid] <= x) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ int pages_of(int tokens, int shift) { return (tokens + (1 << shift) - 1) >> shift; }
+
+struct PlanRow {
+    int64_t at;
+    int seq, pos;
+};
+// Row r of the plan: its slot, position and place; none (-1) past the last.
+__device__ __forceinline__ PlanRow plan_row(int r, int rows, const int* before, const int* lens, int slots,
+                                            const int* table, int stride, int n_pages, int shift) {
+    PlanRow o{-1, -1, -1};
+    if (r >= rows) return o;
+    o.seq = owner_of(before, slots, r);
+    o.pos = lens[o.seq] + r - before[o.seq];
+    const int page = __ldcg(table + (size_t)o.seq * stride + (o.pos >> shift));
+    if (page >= 0 && page < n_pages) o.at = ((int64_t)page << shift) + (o.pos & ((1 << shift) - 1));
+    return o;
+}
+
+struct PlanArgs {
+    mtp_page_plan_args a;
+    int shift;      // page_size = 1 << shift
+    int rows_here;  // write the rows in this launch
+};
+
+__global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS, 1) page_plan_kernel(const PlanArgs p) {
+    extern __shared__ int pg_sm[];
+    __shared__ long long part[PG_WARPS][2];
+    __shared__ int s_free;
+    const mtp_page_plan_args& a = p.a;
+    const int tid = threadIdx.x, rank = blockIdx.x, slots = a.slots;
+    int* rows_before = pg_sm;                  // [slots + 1]
+    int* pages_before = rows_before + slots + 1;  // [slots + 1]
+    int* lens = pages_before + slots + 1;      // [slots]
+    uint32_t* bits = reinterpret_cast<uint32_t*>(lens + slots);
+
+    // the requests: every CTA makes the whole prefix sums
+    long long rows = 0, want = 0;
+    bool bad = false;
+    for (int s0 = 0; s0 < slots; s0 += PG_THREADS) {
+        const int s = s0 + tid;
+        long long x = 0, y = 0, sx, sy;
+        if (s < slots) {
+            const int len = a.kv_lens[s], add = a.new_lens[s];
+            const bool wrong = len < 0 || add < 0 || (long long)len + add > (long long)a.bt_stride << p.shift;
+            bad |= wrong;
+            lens[s] = len;
+            if (!wrong) {
+                x = add;
+                y = pages_of(len + add, p.shift) - pages_of(len, p.shift);
+            }
+        }
+        block_scan2<PG_WARPS>(x, y, part, sx, sy);
+        if (s < slots) {  // (sums past 31 bits are refused below)
+            rows_before[s] = (int)min(rows + x, (long long)INT_MAX);
+            pages_before[s] = (int)min(want + y, (long long)INT_MAX);
+        }
+        rows += sx;
+        want += sy;
+    }
+    if (tid == 0) {
+        rows_before[slots] = (int)min(rows, (long long)INT_MAX);
+        pages_before[slots] = (int)min(want, (long long)INT_MAX);
+    }
+    int code = __syncthreads_or(bad) || rows > a.max_rows ? MTP_ERR_INVALID : MTP_OK;
+
+    // the free pages
+    const FreeBits f = find_free(a.page_refs, a.out_page_refs, a.n_pages, rank, bits, part, &s_free);
+    cluster_barrier();
+    long long base = 0, free_all = 0;
+#pragma unroll
+    for (int c = 0; c < PG_CTAS; ++c) {
+        const int n = ld_dsmem_int(&s_free, c);
+        if (c < rank) base += n;
+        free_all += n;
+    }
+    if (code == MTP_OK && want > free_all) code = MTP_ERR_NO_PAGES;
+    if (code != MTP_OK) rows = want = 0;
+    take_free(f, base, want, [&](int page, int n) {
+        const int s = owner_of(pages_before, slots, n);
+        a.block_table[(size_t)s * a.bt_stride + pages_of(lens[s], p.shift) + n - pages_before[s]] = page;
+        a.out_page_refs[page] = 1;
+    });
+    cluster_barrier();  // the tables are written
+
+    const int gid = rank * PG_THREADS + tid;
+    for (int s = gid; s <= slots; s += PG_CTAS * PG_THREADS) {
+        const int before = code == MTP_OK ? rows_before[s] : 0;
+        a.out_cu_rows[s] = before;
+        if (s < slots) a.out_kv_lens[s] = code == MTP_OK ? lens[s] + rows_before[s + 1] - before : lens[s];
+    }
+    if (gid == 0) {
+        a.out_status[0] = code;
+        a.out_status[1] = (int)rows;
+        a.out_status[2] = (int)want;
+        a.out_status[3] = (int)(free_all - want);
+    }
+    if (!p.rows_here) return;
+    for (int r = gid; r < a.max_rows; r += PG_CTAS * PG_THREADS) {
+        const PlanRow o = plan_row(r, (int)rows, rows_before, lens, slots, a.block_table, a.bt_stride, a.n_pages, p.shift);
+        a.out_slot_map[r] = o.at;
+        a.out_row_seq[r] = o.seq;
+        a.out_row_pos[r] = o.pos;
+    }
+}
+
+// ---- append ----
+
+struct AppendArgs {
+    mtp_cache_append_args a;
+    int shift;
+    unsigned vecs;   // 8-element pieces of a row's keys
+    unsigned total;  // rows * 2 * vecs
+};
+
+constexpr int AP_THREADS = 256, AP_UNROLL = 4;
+
+template <class DST, int SRC, bool VECTOR>
+__device__ __forceinline__ uint4 load8(const void* base, int64_t at) {
+    if constexpr (SRC == MTP_F32) {
+        const float* p = static_cast<const float*>(base) + at;
+        float x[8];
+        if constexpr (VECTOR) {
+            const float4 u = __ldg(reinterpret_cast<const float4*>(p)), v = __ldg(reinterpret_cast<const float4*>(p) + 1);
+            x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
+            x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __ldg(p + i);
+        }
+        return make_uint4(DST::pack(x[0], x[1]), DST::pack(x[2], x[3]), DST::pack(x[4], x[5]), DST::pack(x[6], x[7]));
+    } else {  // the pool's own type: copied bit by bit
+        const uint16_t* p = static_cast<const uint16_t*>(base) + at;
+        if constexpr (VECTOR) return __ldg(reinterpret_cast<const uint4*>(p));
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (uint32_t)__ldg(p + 2 * i) | (uint32_t)__ldg(p + 2 * i + 1) << 16;
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// A thread moves AP_UNROLL pieces of eight elements, all loaded before any is stored.
+// Bound by memory: each element is read once and written once.
+template <class DST, int SRC, bool VECTOR>
+__global__ void __launch_bounds__(AP_THREADS) cache_append_kernel(const AppendArgs p) {
+    const mtp_cache_append_args& a = p.a;
+    const unsigned first = blockIdx.x * (AP_THREADS * AP_UNROLL) + threadIdx.x, hv = a.head_dim / 8;
+    uint16_t* pool = static_cast<uint16_t*>(a.kv_pool);
+    uint4 x[AP_UNROLL];
+    uint16_t* to[AP_UNROLL];
+#pragma unroll
+    for (int u = 0; u < AP_UNROLL; ++u) {
+        const unsigned i = first + u * AP_THREADS;
+        to[u] = nullptr;
+        if (i >= p.total) continue;
+        const unsigned row = i / (2 * p.vecs), rest = i - row * 2 * p.vecs, kv = rest >= p.vecs, vec = rest - kv * p.vecs;
+        const int64_t slot = __ldg(a.slot_map + row), page = slot >> p.shift;
+        if (slot < 0 || page >= a.n_pages) continue;
+        const unsigned head = vec / hv, c = vec - head * hv;
+        const int64_t block = ((page * a.layers + a.layer) * 2 + kv) * a.n_kv_heads + head;
+        to[u] = pool + ((block << p.shift) + (slot & ((1 << p.shift) - 1))) * a.head_dim + c * 8;
+        x[u] = load8<DST, SRC, VECTOR>(kv ? a.v : a.k, (int64_t)row * (kv ? a.v_stride : a.k_stride) + vec * 8);
+    }
+#pragma unroll
+    for (int u = 0; u < AP_UNROLL; ++u)
+        if (to[u]) *reinterpret_cast<uint4*>(to[u]) = x[u];
+}
+
+template <class DST>
+cudaError_t launch_append(const AppendArgs& p, bool vector, cudaStream_t s) {
+    const unsigned grid = (p.total + AP_THREADS * AP_UNROLL - 1) / (AP_THREADS * AP_UNROLL);
+    if (p.a.src_dtype == MTP_F32) {
+        if (vector) cache_append_kernel<DST, MTP_F32, true><<<grid, AP_THREADS, 0, s>>>(p);
+        else cache_append_kernel<DST, MTP_F32, false><<<grid, AP_THREADS, 0, s>>>(p);
+    } else {
+        if (vector) cache_append_kernel<DST, MTP_BF16, true><<<grid, AP_THREADS, 0, s>>>(p);
+        else cache_append_kernel<DST, MTP_BF16, false><<<grid, AP_THREADS, 0, s>>>(p);
+    }
+    return cudaGetLastError();
+}
+
+// ---- reorder ----
+
+struct ReorderArgs {
+    mtp_beam_reorder_args a;
+    int shift;
+    int rows;      // batch * beams
+    int* count;    // workspace: pages to copy
+    int4* copies;  // workspace: {from, to, tokens, -}
+};
+
+// One launch of a cluster: checks, new tables, lengths and counts, and the list of copies.
+// A page's count is the number of tables that hold it, so the new count is the old one,
+// plus the kept beams' holdings, minus the old beams'.  A beam that is its own parent and
+// copies nothing adds and takes the same, and is left out.  The additions come first: a
+// count passes zero only where no table holds the page any more.
+__global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS, 1)
+    beam_reorder_kernel(const ReorderArgs p) {
+    extern __shared__ int pg_sm[];
+    __shared__ long long part[PG_WARPS][2];
+    __shared__ int s_free, s_bad, s_freed;
+    const mtp_beam_reorder_args& a = p.a;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, rank = blockIdx.x, rows = p.rows, W = a.beams;
+    int* copies_before = pg_sm;                    // [rows + 1]
+    int* from = copies_before + rows + 1;          // [rows]: the parent's row, -1 = none
+    int* lens = from + rows;                       // [rows]: the parent's length
+    uint32_t* bits = reinterpret_cast<uint32_t*>(lens + rows);
+    const long long cap = (long long)a.bt_stride << p.shift;
+    const int part_mask = (1 << p.shift) - 1;
+
+    long long want = 0;
+    bool bad = false;
+    if (tid == 0) s_freed = 0;
+    for (int r0 = 0; r0 < rows; r0 += PG_THREADS) {
+        const int r = r0 + tid;
+        long long x = 0, y = 0, sx, sy;
+        if (r < rows) {
+            const int item = r / W, j = r - item * W, parent = a.parent[r];
+            int n = a.kv_lens[r], src = -1;
+            bad |= parent >= W || n < 0 || n > cap;
+            n = 0;
+            if (parent >= 0 && parent < W) {
+                src = item * W + parent;
+                n = a.kv_lens[src];
+                if (n < 0 || n > cap) n = 0;  // (refused)
+                bool again = false;
+                for (int i = 0; i < j; ++i) again |= a.parent[item * W + i] == parent;
+                x = again && (n & part_mask);
+            }
+            from[r] = src;
+            lens[r] = n;
+        }
+        block_scan2<PG_WARPS>(x, y, part, sx, sy);
+        if (r < rows) copies_before[r] = (int)(want + x);
+        want += sx;
+    }
+    if (tid == 0) copies_before[rows] = (int)want;
+    bad = __syncthreads_or(bad) != 0;
+    // every page that a table holds is one, and is counted
+    if (!bad)
+        for (int r = rank * PG_WARPS + warp; r < rows; r += PG_CTAS * PG_WARPS)
+            for (int c = lane; c < pages_of(a.kv_lens[r], p.shift); c += 32) {
+                const int page = a.block_table[(size_t)r * a.bt_stride + c];
+                bad |= page < 0 || page >= a.n_pages || a.page_refs[page] < 1;
+            }
+    bad = __syncthreads_or(bad) != 0;
+    if (tid == 0) s_bad = bad;
+    const FreeBits f = find_free(a.page_refs, a.out_page_refs, a.n_pages, rank, bits, part, &s_free);
+    cluster_barrier();  // counts copied, totals there
+    long long base = 0, free_all = 0;
+#pragma unroll
+    for (int c = 0; c < PG_CTAS; ++c) {
+        const int n = ld_dsmem_int(&s_free, c);
+        if (c < rank) base += n;
+        free_all += n;
+        bad |= ld_dsmem_int(&s_bad, c) != 0;
+    }
+    const int code = bad ? MTP_ERR_INVALID : want > free_all ? MTP_ERR_NO_PAGES : MTP_OK;
+    if (code != MTP_OK) {  // everything stays
+        for (int r = rank * PG_WARPS + warp; r < rows; r += PG_CTAS * PG_WARPS)
+            for (int c = lane; c < a.bt_stride; c += 32)
+                a.out_block_table[(size_t)r * a.bt_stride + c] = a.block_table[(size_t)r * a.bt_stride + c];
+        for (int r = rank * PG_THREADS + tid; r < rows; r += PG_CTAS * PG_THREADS) a.out_kv_lens[r] = a.kv_lens[r];
+        if (rank == 0 && tid == 0) {
+            *p.count = 0;
+            a.out_status[0] = code;
+            a.out_status[1] = 0;
+            a.out_status[2] = (int)free_all;
+            a.out_status[3] = 0;
+        }
+        cluster_barrier();  // no peer still reads this CTA's shared memory
+        return;
+    }
+    take_free(f, base, want, [&](int page, int n) {
+        const int r = owner_of(copies_before, rows + 1, n), tokens = lens[r];
+        p.copies[n] = make_int4(a.block_table[(size_t)from[r] * a.bt_stride + (tokens >> p.shift)], page,
+                                tokens & part_mask, 0);
+        a.out_page_refs[page] = 1;
+    });
+    cluster_barrier();  // the copies' pages are known
+    auto itself = [&](int r) { return from[r] == r && copies_before[r + 1] == copies_before[r]; };
+    for (int r = rank * PG_WARPS + warp; r < rows; r += PG_CTAS * PG_WARPS) {
+        const bool fresh = copies_before[r + 1] != copies_before[r], same = itself(r);
+        const int used = pages_of(lens[r], p.shift);
+        for (int c = lane; c < a.bt_stride; c += 32) {
+            int page = -1;
+            if (c < used) {
+                if (fresh && c == used - 1) {
+                    page = __ldcg(&p.copies[copies_before[r]].y);
+                } else {
+                    page = a.block_table[(size_t)from[r] * a.bt_stride + c];
+                    if (!same) atomicAdd(a.out_page_refs + page, 1);
+                }
+            }
+            a.out_block_table[(size_t)r * a.bt_stride + c] = page;
+        }
+    }
+    cluster_barrier();
+    int freed = 0;
+    for (int r = rank * PG_WARPS + warp; r < rows; r += PG_CTAS * PG_WARPS)
+        if (!itself(r))
+            for (int c = lane; c < pages_of(a.kv_lens[r], p.shift); c += 32)
+                freed += atomicSub(a.out_page_refs + a.block_table[(size_t)r * a.bt_stride + c], 1) == 1;
+    if (freed) atomicAdd(&s_freed, freed);
+    cluster_barrier();
+    for (int r = rank * PG_THREADS + tid; r < rows; r += PG_CTAS * PG_THREADS) a.out_kv_lens[r] = lens[r];
+    if (rank == 0 && tid == 0) {
+        long long all = free_all - want;
+        for (int c = 0; c < PG_CTAS; ++c) all += ld_dsmem_int(&s_freed, c);
+        *p.count = (int)want;
+        a.out_status[0] = MTP_OK;
+        a.out_status[1] = (int)want;
+        a.out_status[2] = (int)all;
+        a.out_status[3] = 0;
+    }
+    cluster_barrier();  // no peer still reads this CTA's shared memory
+}
+
+constexpr int CP_THREADS = 256, CP_UNROLL = 4;
+
+// The filled rows of every copied page: for each (layer, keys | values, head) one run of
+// tokens * head_dim elements.  A warp takes a run; CP_UNROLL loads are in flight per lane.
+// Bound by memory: each row is read once and written once.
+__global__ void __launch_bounds__(CP_THREADS) page_copy_kernel(const ReorderArgs p, int runs) {
+    const int n = *p.count, lane = threadIdx.x & 31;
+    const long long total = (long long)n * runs, stride = (long long)gridDim.x * (CP_THREADS / 32);
+    const size_t block = (size_t)p.a.head_dim << p.shift >> 3;  // 16-byte pieces of a (page, layer, K | V, head) block
+    uint4* pool = static_cast<uint4*>(p.a.kv_pool);
+    for (long long w = (long long)blockIdx.x * (CP_THREADS / 32) + (threadIdx.x >> 5); w < total; w += stride) {
+        const int i = (int)(w / runs), run = (int)(w - (long long)i * runs);
+        const int4 c = __ldg(p.copies + i);
+        const uint4* src = pool + ((size_t)c.x * runs + run) * block;
+        uint4* dst = pool + ((size_t)c.y * runs + run) * block;
+        const int pieces = c.z * (p.a.head_dim >> 3);
+        for (int q0 = lane; q0 < pieces; q0 += 32 * CP_UNROLL) {
+            uint4 v[CP_UNROLL];
+#pragma unroll
+            for (int u = 0; u < CP_UNROLL; ++u)
+                if (q0 + u * 32 < pieces) v[u] = src[q0 + u * 32];
+#pragma unroll
+            for (int u = 0; u < CP_UNROLL; ++u)
+                if (q0 + u * 32 < pieces) dst[q0 + u * 32] = v[u];
+        }
+    }
+}
+
+int log2_of(int page_size) { return page_size == 16 ? 4 : page_size == 32 ? 5 : page_size == 64 ? 6 : 7; }
+
+int check_pool(const char* what, int n_pages, int layers, int layer, int n_kv_heads, int head_dim, int page_size) {
+    if (n_pages < 1 || n_pages > PG_MAX_PAGES || layers < 1 || layer < 0 || layer >= layers || n_kv_heads < 1 ||
+        n_kv_heads > 1024 || head_dim < 8 || head_dim > 256 || head_dim % 8 || !page_size_ok(page_size))
+        return invalid("%s: invalid pool (pages %d, layers %d, layer %d, heads %d, head_dim %d, page_size %d)", what,
+                       n_pages, layers, layer, n_kv_heads, head_dim, page_size);
+    return MTP_OK;
+}
+
+size_t reorder_workspace(int rows) { return 16 + (size_t)rows * sizeof(int4); }
+
+}  // namespace
+}  // namespace mtp
+
+using namespace mtp;
+
+extern "C" {
+
+MTP_API int mtp_page_plan(const mtp_page_plan_args* a, void* cuda_stream) {
+    return guarded([&]() -> int {
+        if (!a || a->slots < 1 || a->slots > PG_MAX_SLOTS || a->n_pages < 1 || a->n_pages > PG_MAX_PAGES ||
+            !page_size_ok(a->page_size) || a->bt_stride < 1 || a->max_rows < 0 || a->max_rows > PG_MAX_ROWS)
+            return invalid("page_plan: invalid sizes");
+        if ((long long)a->bt_stride * a->page_size > (1 << 30)) return invalid("page_plan: bt_stride %d", a->bt_stride);
+        if (!a->kv_lens || !a->new_lens || !a->block_table || !a->page_refs || !a->out_kv_lens || !a->out_page_refs ||
+            !a->out_cu_rows || !a->out_status ||
+            (a->max_rows > 0 && (!a->out_slot_map || !a->out_row_seq || !a->out_row_pos)))
+            return invalid("page_plan: null pointer");
+        PlanArgs p{*a, log2_of(a->page_size), 1};
+        const size_t smem = (size_t)(3 * a->slots + 2 + free_words(a->n_pages)) * 4;
+        const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+        cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(page_plan_kernel), smem);
+        if (e == cudaSuccess) {
+            page_plan_kernel<<<PG_CTAS, PG_THREADS, smem, s>>>(p);
+            e = cudaGetLastError();
+        }
+        return cuda_status(e, "page_plan");
+    });
+}
+
+MTP_API int mtp_cache_append(const mtp_cache_append_args* a, void* cuda_stream) {
+    return guarded([&]() -> int {
+        if (!a) return invalid("cache_append: null arguments");
+        if (const int r = check_pool("cache_append", a->n_pages, a->layers, a->layer, a->n_kv_heads, a->head_dim,
+                                     a->page_size))
+            return r;
+        if (a->rows < 0) return invalid("cache_append: rows %d", a->rows);
+        if ((a->pool_dtype != MTP_BF16 && a->pool_dtype != MTP_F16) ||
+            (a->src_dtype != MTP_F32 && a->src_dtype != a->pool_dtype))
+            return invalid("cache_append: src_dtype %d, pool_dtype %d", a->src_dtype, a->pool_dtype);
+        const int width = a->n_kv_heads * a->head_dim;
+        if (a->k_stride < width || a->v_stride < width)
+            return invalid("cache_append: row strides %lld, %lld below %d", (long long)a->k_stride,
+                           (long long)a->v_stride, width);
+        const unsigned vecs = width / 8;
+        if ((long long)a->rows * 2 * vecs > INT_MAX) return invalid("cache_append: rows %d", a->rows);
+        if (a->rows == 0) return MTP_OK;
+        if (!a->k || !a->v || !a->slot_map || !a->kv_pool) return invalid("cache_append: null pointer");
+        if (!aligned16(a->kv_pool)) return invalid("cache_append: kv_pool must be 16-byte aligned");
+        const int size = a->src_dtype == MTP_F32 ? 4 : 2;
+        if (reinterpret_cast<uintptr_t>(a->k) % size || reinterpret_cast<uintptr_t>(a->v) % size)
+            return invalid("cache_append: k and v must be aligned to their elements");
+        AppendArgs p{*a, log2_of(a->page_size), vecs, (unsigned)a->rows * 2 * vecs};
+        const bool vector = aligned16(a->k) && aligned16(a->v) && a->k_stride * size % 16 == 0 && a->v_stride * size % 16 == 0;
+        const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+        return cuda_status(a->pool_dtype == MTP_BF16 ? launch_append<Bf16>(p, vector, s) : launch_append<F16>(p, vector, s),
+                           "cache_append");
+    });
+}
+
+MTP_API size_t mtp_beam_reorder_workspace_bytes(const mtp_beam_reorder_args* a) {
+    if (!a || a->batch < 1 || a->beams < 1 || (long long)a->batch * a->beams > PG_MAX_SLOTS) return 0;
+    return reorder_workspace(a->batch * a->beams);
+}
+
+MTP_API int mtp_beam_reorder(const mtp_beam_reorder_args* a, void* workspace, size_t workspace_bytes,
+                             void* cuda_stream) {
+    return guarded([&]() -> int {
+        if (!a) return invalid("beam_reorder: null arguments");
+        if (const int r = check_pool("beam_reorder", a->n_pages, a->layers, 0, a->n_kv_heads, a->head_dim, a->page_size))
+            return r;
+        if (a->batch < 1 || a->beams < 1 || a->beams > 64 || (long long)a->batch * a->beams > PG_MAX_SLOTS ||
+            a->bt_stride < 1 || (long long)a->bt_stride * a->page_size > (1 << 30))
+            return invalid("beam_reorder: invalid sizes (batch %d, beams %d, bt_stride %d)", a->batch, a->beams,
+                           a->bt_stride);
+        if (a->pool_dtype != MTP_BF16 && a->pool_dtype != MTP_F16)
+            return invalid("beam_reorder: pool_dtype %d", a->pool_dtype);
+        if (!a->parent || !a->block_table || !a->kv_lens || !a->page_refs || !a->kv_pool || !a->out_block_table ||
+            !a->out_kv_lens || !a->out_page_refs || !a->out_status)
+            return invalid("beam_reorder: null pointer");
+        if (a->out_block_table == a->block_table || a->out_kv_lens == a->kv_lens)
+            return invalid("beam_reorder: the new tables and lengths need buffers of their own");
+        if (!aligned16(a->kv_pool)) return invalid("beam_reorder: kv_pool must be 16-byte aligned");
+        const int rows = a->batch * a->beams;
+        if (!workspace || !aligned16(workspace) || workspace_bytes < reorder_workspace(rows))
+            return invalid("beam_reorder: workspace %zu bytes, need %zu, 16-byte aligned", workspace_bytes,
+                           reorder_workspace(rows));
+        ReorderArgs p{*a, log2_of(a->page_size), rows, static_cast<int*>(workspace),
+                      reinterpret_cast<int4*>(static_cast<char*>(workspace) + 16)};
+        const size_t smem = (size_t)(3 * rows + 1 + free_words(a->n_pages)) * 4;
+        const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+        cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(beam_reorder_kernel), smem);
+        if (e == cudaSuccess) {
+            beam_reorder_kernel<<<PG_CTAS, PG_THREADS, smem, s>>>(p);
+            e = cudaGetLastError();
+        }
+        if (e == cudaSuccess && a->beams > 1) {  // (one beam has nothing to copy)
+            int dev = 0, sms = 0;
+            e = cudaGetDevice(&dev);
+            if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+            if (e == cudaSuccess) {
+                page_copy_kernel<<<sms * 8, CP_THREADS, 0, s>>>(p, a->layers * 2 * a->n_kv_heads);
+                e = cudaGetLastError();
+            }
+        }
+        return cuda_status(e, "beam_reorder");
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,101 @@
+// serving.cuh -- what the paged beam-search operators (paged.cu, beam.cu,
+// chunk_attention*.cu) share: argument errors, element types, the cache pool's
+// layout and block-wide prefix sums.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <cstdarg>
+#include <cstdint>
+#include <cstdio>
+
+#include "common.cuh"
+#include "kernels.cuh"
+#include "mtp.h"
+
+namespace mtp {
+
+inline int invalid(const char* fmt, ...) {
+    char msg[256];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(msg, sizeof(msg), fmt, ap);
+    va_end(ap);
+    return report_error(MTP_ERR_INVALID, msg);
+}
+inline int cuda_status(cudaError_t e, const char* what) {
+    if (e == cudaSuccess) return MTP_OK;
+    char msg[256];
+    snprintf(msg, sizeof(msg), "%s: %s", what, cudaGetErrorString(e));
+    return report_error(MTP_ERR_CUDA, msg);
+}
+// The body of a C entry point: no C++ exception leaves it.
+template <class F>
+int guarded(F body) noexcept {
+    try {
+        clear_error();
+        return body();
+    } catch (...) {
+        return MTP_ERR_CUDA;
+    }
+}
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+inline bool page_size_ok(int p) { return p == 16 || p == 32 || p == 64 || p == 128; }
+
+// Element types of two bytes as raw bits: to and from fp32, rounded to nearest even.
+struct Bf16 {
+    static __device__ __forceinline__ float to_float(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) {
+        const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&p);
+    }
+};
+struct F16 {
+    static __device__ __forceinline__ float to_float(uint16_t x) { return __half2float(__ushort_as_half(x)); }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) {
+        const __half2 p = __floats2half2_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&p);
+    }
+};
+
+// Exclusive prefix sums of x and y over the threads of a block of WARPS warps, and
+// their totals.  `part` is shared memory; the call synchronises the block.
+template <int WARPS>
+__device__ __forceinline__ void block_scan2(long long& x, long long& y, long long (*part)[2], long long& sum_x,
+                                            long long& sum_y) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    long long ix = x, iy = y;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long ux = __shfl_up_sync(FULL_MASK, ix, o), uy = __shfl_up_sync(FULL_MASK, iy, o);
+        if (lane >= o) {
+            ix += ux;
+            iy += uy;
+        }
+    }
+    __syncthreads();  // `part` may still be read from an earlier call
+    if (lane == 31) {
+        part[warp][0] = ix;
+        part[warp][1] = iy;
+    }
+    __syncthreads();
+    long long bx = lane < WARPS ? part[lane][0] : 0, by = lane < WARPS ? part[lane][1] : 0;
+    const long long tx = bx, ty = by;
+#pragma unroll
+    for (int o = 1; o < WARPS; o <<= 1) {
+        const long long ux = __shfl_up_sync(FULL_MASK, bx, o), uy = __shfl_up_sync(FULL_MASK, by, o);
+        if (lane >= o) {
+            bx += ux;
+            by += uy;
+        }
+    }
+    sum_x = __shfl_sync(FULL_MASK, bx, WARPS - 1);
+    sum_y = __shfl_sync(FULL_MASK, by, WARPS - 1);
+    bx = __shfl_sync(FULL_MASK, bx - tx, warp);
+    by = __shfl_sync(FULL_MASK, by - ty, warp);
+    x = bx + ix - x;
+    y = by + iy - y;
+}
+
+}  // namespace mtp

@@ -12,7 +12,8 @@ import struct
 import numpy as np
 
 from . import _lib
-from ._lib import MTP_OPT_BATCHED, MTPError, MtpAttentionArgs, MtpConfig, check, lib  # noqa: F401
+from ._lib import (MTP_OPT_BATCHED, MTPError, MtpAttentionArgs, MtpBeamReorderArgs,  # noqa: F401
+                   MtpCacheAppendArgs, MtpConfig, MtpPagePlanArgs, check, lib)
 
 BLOB_MAGIC = b"MTPWGT01"
 
@@ -243,6 +244,126 @@ def mtp_gemm_bf16x2(w, a_hi, a_lo, out, n_w, k, m, splits=1, accumulate=0, strea
                               _stream_handle(stream)))
 
 
+# ---- paged beam search ------------------------------------------------------
+# The *_args functions read sizes, strides and types off the tensors and refuse
+# what the operators cannot take.  An argument block holds addresses: keep its
+# tensors alive, and pass it again for every step on the same buffers.
+
+_DTYPES = {"torch.float32": _lib.MTP_F32, "torch.bfloat16": _lib.MTP_BF16, "torch.float16": _lib.MTP_F16}
+
+
+def _buf(name, x, dtype, shape=None):
+    """Address of a contiguous CUDA tensor of a type and shape (None in a shape: any size there)."""
+    if str(x.dtype) != "torch." + dtype:
+        raise TypeError(f"{name}: {dtype} wanted, got {x.dtype}")
+    if not x.is_cuda or not x.is_contiguous():
+        raise ValueError(f"{name}: a contiguous tensor on the GPU is wanted")
+    if shape is not None and (x.dim() != len(shape) or any(s not in (None, n) for s, n in zip(shape, x.shape))):
+        raise ValueError(f"{name}: shape {tuple(shape)} wanted, got {tuple(x.shape)}")
+    return x.data_ptr()
+
+
+def _rows(name, x, shape):
+    """Address and row stride (elements) of a CUDA tensor whose rows are contiguous, the rows themselves strided."""
+    if not x.is_cuda:
+        raise ValueError(f"{name}: a tensor on the GPU is wanted")
+    if x.dim() != len(shape) or any(s not in (None, n) for s, n in zip(shape, x.shape)):
+        raise ValueError(f"{name}: shape {tuple(shape)} wanted, got {tuple(x.shape)}")
+    inner = 1
+    for n, s in zip(reversed(x.shape[1:]), reversed(x.stride()[1:])):
+        if n != 1 and s != inner:
+            raise ValueError(f"{name}: the elements of a row have to be contiguous")
+        inner *= n
+    return x.data_ptr(), max(x.stride(0), inner)
+
+
+def _dtype(name, x, allowed):
+    code = _DTYPES.get(str(x.dtype))
+    if code not in allowed:
+        raise TypeError(f"{name}: unsupported type {x.dtype}")
+    return code
+
+
+def _pool(kv_pool):
+    """Fields that an argument block takes from the cache pool [n_pages, layers, 2, kv heads, page_size, head_dim]."""
+    dtype = _dtype("kv_pool", kv_pool, (_lib.MTP_BF16, _lib.MTP_F16))
+    ptr = _buf("kv_pool", kv_pool, str(kv_pool.dtype)[6:], (None, None, 2, None, None, None))
+    n_pages, layers, _, heads, page, dim = kv_pool.shape
+    return dict(kv_pool=ptr, n_pages=n_pages, layers=layers, n_kv_heads=heads, page_size=page, head_dim=dim), dtype
+
+
+def page_plan_args(kv_lens, new_lens, block_table, page_refs, out_kv_lens, out_page_refs, out_cu_rows, out_slot_map,
+                   out_row_seq, out_row_pos, out_status, page_size, slots=None, n_pages=None, bt_stride=None,
+                   max_rows=None) -> MtpPagePlanArgs:
+    """Argument block of mtp_page_plan; sizes not given are the tensors'."""
+    slots = kv_lens.shape[0] if slots is None else slots
+    n_pages = page_refs.shape[0] if n_pages is None else n_pages
+    bt_stride = block_table.shape[1] if bt_stride is None else bt_stride
+    max_rows = out_slot_map.shape[0] if max_rows is None else max_rows
+    return MtpPagePlanArgs(
+        slots=slots, page_size=page_size, n_pages=n_pages, bt_stride=bt_stride, max_rows=max_rows,
+        kv_lens=_buf("kv_lens", kv_lens, "int32", (slots,)), new_lens=_buf("new_lens", new_lens, "int32", (slots,)),
+        block_table=_buf("block_table", block_table, "int32", (slots, bt_stride)),
+        page_refs=_buf("page_refs", page_refs, "int32", (n_pages,)),
+        out_kv_lens=_buf("out_kv_lens", out_kv_lens, "int32", (slots,)),
+        out_page_refs=_buf("out_page_refs", out_page_refs, "int32", (n_pages,)),
+        out_cu_rows=_buf("out_cu_rows", out_cu_rows, "int32", (slots + 1,)),
+        out_slot_map=_buf("out_slot_map", out_slot_map, "int64", (max_rows,)),
+        out_row_seq=_buf("out_row_seq", out_row_seq, "int32", (max_rows,)),
+        out_row_pos=_buf("out_row_pos", out_row_pos, "int32", (max_rows,)),
+        out_status=_buf("out_status", out_status, "int32", (4,)))
+
+
+def mtp_page_plan(args: MtpPagePlanArgs, stream=None) -> None:
+    """Pages, block tables and row plan of the tokens that each slot gets in a step."""
+    check(lib.mtp_page_plan(ctypes.byref(args), _stream_handle(stream)))
+
+
+def cache_append_args(k, v, slot_map, kv_pool, layer) -> MtpCacheAppendArgs:
+    """Argument block of mtp_cache_append: k, v [rows, kv heads, head_dim], their rows possibly strided."""
+    pool, dtype = _pool(kv_pool)
+    rows = k.shape[0]
+    shape = (rows, pool["n_kv_heads"], pool["head_dim"])
+    (kp, ks), (vp, vs) = _rows("k", k, shape), _rows("v", v, shape)
+    src = _dtype("k", k, (_lib.MTP_F32, dtype))
+    if v.dtype != k.dtype:
+        raise TypeError(f"v: {k.dtype} wanted, got {v.dtype}")
+    return MtpCacheAppendArgs(rows=rows, layer=layer, src_dtype=src, pool_dtype=dtype, k_stride=ks, v_stride=vs, k=kp,
+                              v=vp, slot_map=_buf("slot_map", slot_map, "int64", (rows,)), **pool)
+
+
+def mtp_cache_append(args: MtpCacheAppendArgs, stream=None) -> None:
+    """New keys and values into one layer of the cache, by slot map."""
+    check(lib.mtp_cache_append(ctypes.byref(args), _stream_handle(stream)))
+
+
+def beam_reorder_args(parent, block_table, kv_lens, page_refs, kv_pool, out_block_table, out_kv_lens, out_page_refs,
+                      out_status) -> MtpBeamReorderArgs:
+    """Argument block of mtp_beam_reorder: parent [batch, beams]."""
+    pool, dtype = _pool(kv_pool)
+    batch, beams = parent.shape
+    rows, stride, n_pages = batch * beams, block_table.shape[1], pool["n_pages"]
+    return MtpBeamReorderArgs(
+        batch=batch, beams=beams, bt_stride=stride, pool_dtype=dtype,
+        parent=_buf("parent", parent, "int32", (batch, beams)),
+        block_table=_buf("block_table", block_table, "int32", (rows, stride)),
+        kv_lens=_buf("kv_lens", kv_lens, "int32", (rows,)),
+        page_refs=_buf("page_refs", page_refs, "int32", (n_pages,)),
+        out_block_table=_buf("out_block_table", out_block_table, "int32", (rows, stride)),
+        out_kv_lens=_buf("out_kv_lens", out_kv_lens, "int32", (rows,)),
+        out_page_refs=_buf("out_page_refs", out_page_refs, "int32", (n_pages,)),
+        out_status=_buf("out_status", out_status, "int32", (4,)), **pool)
+
+
+def mtp_beam_reorder_workspace_bytes(args: MtpBeamReorderArgs) -> int:
+    return int(lib.mtp_beam_reorder_workspace_bytes(ctypes.byref(args)))
+
+
+def mtp_beam_reorder(args: MtpBeamReorderArgs, workspace, workspace_bytes: int, stream=None) -> None:
+    """Block tables, lengths and page counts of the kept beams; copies of their partly filled last pages."""
+    check(lib.mtp_beam_reorder(ctypes.byref(args), _ptr(workspace), workspace_bytes, _stream_handle(stream)))
+
+
 def _as_i32(x):
     if x is None:
         return None
@@ -324,4 +445,5 @@ class MTPDecoder:
 
 
 __all__ = [n for n in dir() if n.startswith("mtp_")] + ["MTPDecoder", "MTPError", "pack_weights",
-                                                         "make_config", "attention_args"]
+                                                         "make_config", "attention_args", "page_plan_args",
+                                                         "cache_append_args", "beam_reorder_args"]

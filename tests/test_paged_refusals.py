@@ -1,0 +1,88 @@
+"""What the paged operators refuse on the host, before anything is queued: no GPU is needed.  The addresses are
+never followed."""
+import pytest
+
+from test_lib_cpu import libpath  # noqa: F401
+
+A = 1 << 20  # an aligned address that nothing follows
+
+
+def _plan(**kw):
+    from paper_2410_13839_gb300._lib import MtpPagePlanArgs
+    d = dict(slots=4, page_size=16, n_pages=8, bt_stride=4, max_rows=9)
+    d.update({n: A for n, t in MtpPagePlanArgs._fields_[5:]})
+    return MtpPagePlanArgs(**{**d, **kw})
+
+
+def _append(**kw):
+    from paper_2410_13839_gb300._lib import MtpCacheAppendArgs
+    d = dict(rows=4, n_kv_heads=2, head_dim=64, page_size=16, layers=2, layer=1, n_pages=8, src_dtype=0, pool_dtype=1,
+             k_stride=128, v_stride=128, k=A, v=A, slot_map=A, kv_pool=A)
+    return MtpCacheAppendArgs(**{**d, **kw})
+
+
+def _reorder(**kw):
+    from paper_2410_13839_gb300._lib import MtpBeamReorderArgs
+    d = dict(batch=2, beams=4, page_size=16, n_pages=8, bt_stride=4, layers=2, n_kv_heads=2, head_dim=64, pool_dtype=1)
+    d.update({n: A * (i + 1) for i, (n, t) in enumerate(MtpBeamReorderArgs._fields_[9:])})
+    return MtpBeamReorderArgs(**{**d, **kw})
+
+
+def _refused(call):
+    from paper_2410_13839_gb300 import mtp
+    with pytest.raises(mtp.MTPError) as e:
+        call(mtp)
+    assert e.value.code == -1 and str(e.value)
+
+
+@pytest.mark.parametrize("kw", [dict(slots=0), dict(slots=8193), dict(page_size=24), dict(page_size=256), dict(n_pages=0),
+                                dict(n_pages=(1 << 22) + 1), dict(bt_stride=0), dict(bt_stride=(1 << 26) + 1),
+                                dict(max_rows=-1), dict(max_rows=(1 << 24) + 1), dict(kv_lens=None),
+                                dict(block_table=None), dict(out_slot_map=None), dict(out_status=None)])
+def test_page_plan(libpath, kw):  # noqa: F811
+    _refused(lambda mtp: mtp.mtp_page_plan(_plan(**kw)))
+
+
+@pytest.mark.parametrize("kw", [dict(rows=-1), dict(rows=1 << 28), dict(n_kv_heads=0), dict(head_dim=60),
+                                dict(head_dim=264), dict(page_size=8), dict(layer=2), dict(layer=-1), dict(n_pages=0),
+                                dict(src_dtype=2), dict(src_dtype=7), dict(pool_dtype=0), dict(k_stride=127),
+                                dict(v_stride=0), dict(k=None), dict(v=None), dict(slot_map=None), dict(kv_pool=None),
+                                dict(kv_pool=A + 8), dict(k=A + 2)])
+def test_cache_append(libpath, kw):  # noqa: F811
+    _refused(lambda mtp: mtp.mtp_cache_append(_append(**kw)))
+
+
+@pytest.mark.parametrize("kw", [dict(batch=0), dict(beams=0), dict(beams=65), dict(batch=4096), dict(page_size=20),
+                                dict(n_pages=0), dict(bt_stride=0), dict(layers=0), dict(n_kv_heads=0),
+                                dict(head_dim=12), dict(pool_dtype=0), dict(parent=None), dict(kv_pool=None),
+                                dict(out_status=None), dict(kv_pool=A + 4), dict(out_block_table=A * 2),
+                                dict(out_kv_lens=A * 3)])
+def test_beam_reorder(libpath, kw):  # noqa: F811
+    _refused(lambda mtp: mtp.mtp_beam_reorder(_reorder(**kw), A, 1 << 20))
+
+
+def test_beam_reorder_workspace(libpath):  # noqa: F811
+    from paper_2410_13839_gb300 import mtp
+    need = mtp.mtp_beam_reorder_workspace_bytes(_reorder())
+    assert need > 0
+    for ws, n in ((None, need), (A, need - 1), (A + 8, need)):
+        _refused(lambda m: m.mtp_beam_reorder(_reorder(), ws, n))
+
+
+def test_null_argument_blocks(libpath):  # noqa: F811
+    from paper_2410_13839_gb300 import _lib
+    for call in (lambda: _lib.lib.mtp_page_plan(None, None), lambda: _lib.lib.mtp_cache_append(None, None),
+                 lambda: _lib.lib.mtp_beam_reorder(None, None, 0, None)):
+        assert call() == -1
+    assert _lib.lib.mtp_beam_reorder_workspace_bytes(None) == 0
+
+
+def test_argument_blocks_refuse_tensors_they_cannot_describe(libpath):  # noqa: F811
+    torch = pytest.importorskip("torch")
+    from paper_2410_13839_gb300 import mtp
+    pool = torch.zeros(2, 1, 2, 2, 16, 64, dtype=torch.bfloat16)
+    k, places = torch.zeros(3, 2, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int64)
+    with pytest.raises(ValueError):  # host memory
+        mtp.cache_append_args(k=k, v=k, slot_map=places, kv_pool=pool, layer=0)
+    with pytest.raises(TypeError):
+        mtp.cache_append_args(k=k, v=k, slot_map=places, kv_pool=pool.float(), layer=0)
