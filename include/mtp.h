@@ -544,6 +544,44 @@ typedef struct mtp_cache_append_args {
 } mtp_cache_append_args;
 MTP_API int mtp_cache_append(const mtp_cache_append_args* args, void* cuda_stream);
 
+/* Beam search's selection: of each item's beams * vocab continuations the k best,
+ *   score(b, t) = scores[b] + (logits[b][t] - lse[b]),
+ * each operation one fp32 operation, by descending score; equal scores by ascending beam,
+ * then token.  A NaN score counts as -inf.  A finished beam (done != 0) has the one
+ * continuation eos_id, at the score it has; its other scores are -inf.
+ *   logits      [batch * beams] rows of vocab, row stride logits_stride (elements), of
+ *               logits_dtype (MTP_F32, MTP_BF16, MTP_F16)
+ *   lse         float [batch][beams]: the rows' log-sum-exp, as mtp_heads_topk gives it; NULL:
+ *               computed (NaN, so that no continuation of the beam counts, where a row has
+ *               NaN or +inf)
+ *   scores      float [batch][beams]: the beams' scores so far; -inf leaves a beam out
+ *   done        int32 [batch][beams] or NULL (needs an eos_id)
+ *   eos_id      the end's token, -1 = none
+ *   out_scores  float [batch][k]; out_parent, out_token int32 [batch][k]: beam and token
+ *   out_done    int32 [batch][k] or NULL: 1 where the token is eos_id or the parent is finished
+ *   out_lse     float [batch][beams] or NULL: the log-sum-exp used
+ *   workspace   mtp_beam_select_workspace_bytes(args) bytes, 16-byte aligned (0: may be NULL).  Its
+ *               counters must be zero on the first call and are left zero; their place is the
+ *               same for calls of all sizes.  Calls that overlap need workspaces of their own.
+ * Limits: batch <= 4096, beams <= 64, k <= 64, k <= beams * vocab <= 2^30.
+ * Errors: MTP_ERR_INVALID, MTP_ERR_CUDA. */
+typedef struct mtp_beam_select_args {
+    int32_t batch, beams, vocab, k, eos_id, logits_dtype;
+    int64_t logits_stride;
+    const void* logits;
+    const float* lse;
+    const float* scores;
+    const int32_t* done;
+    float* out_scores;
+    int32_t* out_parent;
+    int32_t* out_token;
+    int32_t* out_done;
+    float* out_lse;
+} mtp_beam_select_args;
+MTP_API size_t mtp_beam_select_workspace_bytes(const mtp_beam_select_args* args);
+MTP_API int mtp_beam_select(const mtp_beam_select_args* args, void* workspace, size_t workspace_bytes,
+                            void* cuda_stream);
+
 /* The cache of the beams that a selection kept.  Slots are item * beams + beam; beam j of
  * item b continues beam parent[b][j] (< 0: the beam ends and its slot becomes empty).
  * Tables share the parent's pages.  A partly filled last page stays with the first of its

@@ -66,6 +66,9 @@ MtpPagePlanArgs = _struct(
 MtpCacheAppendArgs = _struct(
     "MtpCacheAppendArgs", "rows n_kv_heads head_dim page_size layers layer n_pages src_dtype pool_dtype",
     "k_stride v_stride", "k v slot_map kv_pool")
+MtpBeamSelectArgs = _struct(
+    "MtpBeamSelectArgs", "batch beams vocab k eos_id logits_dtype", "logits_stride",
+    "logits lse scores done out_scores out_parent out_token out_done out_lse")
 MtpBeamReorderArgs = _struct(
     "MtpBeamReorderArgs", "batch beams page_size n_pages bt_stride layers n_kv_heads head_dim pool_dtype", "",
     "parent block_table kv_lens page_refs kv_pool out_block_table out_kv_lens out_page_refs out_status")
@@ -115,6 +118,8 @@ def _load() -> ctypes.CDLL:
         "mtp_gemm_bf16x2": (i32, [vp, vp, vp, vp, i32, i32, i32, i32, i32, vp]),
         "mtp_page_plan": (i32, [ctypes.POINTER(MtpPagePlanArgs), vp]),
         "mtp_cache_append": (i32, [ctypes.POINTER(MtpCacheAppendArgs), vp]),
+        "mtp_beam_select_workspace_bytes": (sz, [ctypes.POINTER(MtpBeamSelectArgs)]),
+        "mtp_beam_select": (i32, [ctypes.POINTER(MtpBeamSelectArgs), vp, sz, vp]),
         "mtp_beam_reorder_workspace_bytes": (sz, [ctypes.POINTER(MtpBeamReorderArgs)]),
         "mtp_beam_reorder": (i32, [ctypes.POINTER(MtpBeamReorderArgs), vp, sz, vp]),
     }

@@ -1,0 +1,425 @@
+// beam.cu -- beam search's selection (mtp_beam_select): of an item's beams * vocab
+// continuations the k best,
+//   score(b, t) = beam_score[b] + (logit[b][t] - lse[b]),
+// each operation one fp32 operation, by descending score and, where scores are equal,
+// ascending b * vocab + t.  A finished beam has one continuation, its end, at its own
+// score.
+//
+// A continuation is a 64-bit key, the score's bits in an order-preserving form above the
+// complement of its number: keys are distinct, so the k largest are one set, whatever
+// order they are looked at in, and no tie is a special case.
+//
+// The best of n keys in shared memory (best_of): 128 groups of threads give a maximum
+// each; the k-th largest of these maxima is a bound that at least k keys reach, and hardly
+// more do (for k = 8 about 8.3 are expected, for k = 64 about 89); those are gathered and
+// ranked by counting.  Where more than CAND_MAX reach it (runs of equal scores that one
+// group holds), the keys are taken out one by one instead.
+//
+// A CTA holds up to SEG scores in shared memory.  Items of more are cut into segments; each
+// leaves its k best keys in the workspace, and the item's CTA that finishes last (an atomic
+// counter, reset by it) selects among these.  The log-sum-exp, where it is not given, is
+// taken from shared memory in the same launch if the item is one segment, else by a kernel
+// before it, whose reading leaves the logits in L2.
+#include <float.h>
+
+#include "serving.cuh"
+
+namespace mtp {
+namespace {
+
+constexpr int BS_THREADS = 512, BS_WARPS = BS_THREADS / 32;
+constexpr int SEG = 16384;        // scores of a CTA: 64 KB, three CTAs to an SM
+constexpr int GROUPS = 128;       // groups of four threads, each with a maximum
+constexpr int CAND_MAX = 1024;
+constexpr int BS_MAX_K = 64, BS_MAX_BEAMS = 64, BS_MAX_BATCH = 4096;
+constexpr int LSE_THREADS = 512;
+
+struct SelectArgsB {
+    mtp_beam_select_args a;
+    int segments, seg_len;        // segments of an item, scores of a segment
+    int lse_here;                 // the log-sum-exp is taken in this kernel (one segment)
+    const float* lse;             // given, or a kernel's before this one
+    unsigned long long* keys;     // [batch][segments][k]
+    int* count;                   // [batch]
+};
+
+__device__ __forceinline__ unsigned long long make_key(float score, uint32_t number) {
+    if (isnan(score)) score = -INFINITY;
+    uint32_t u = __float_as_uint(score + 0.f);  // (-0 is 0)
+    u ^= (u >> 31) ? 0xffffffffu : 0x80000000u;
+    return (unsigned long long)u << 32 | (0xffffffffu - number);
+}
+__device__ __forceinline__ float key_score(unsigned long long key) {
+    const uint32_t u = (uint32_t)(key >> 32);
+    return __uint_as_float(u ^ ((u >> 31) ? 0x80000000u : 0xffffffffu));
+}
+__device__ __forceinline__ unsigned long long warp_max64(unsigned long long v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(FULL_MASK, v, o));
+    return v;
+}
+
+struct Best {
+    unsigned long long thread_max[BS_THREADS];
+    unsigned long long group_max[GROUPS];
+    unsigned long long cand[CAND_MAX];
+    unsigned long long best[BS_MAX_K];
+    unsigned long long bound, warp_best[BS_WARPS];
+    int n;
+};
+
+// The k largest of key(0) .. key(n - 1) into b.best, descending; 0 past the last.
+// The whole block calls it, with the keys visible to all; b.best is visible afterwards.
+template <class KEY>
+__device__ __forceinline__ void best_of(Best& b, int n, int k, KEY key) {
+    const int tid = threadIdx.x;
+    unsigned long long most = 0;
+#pragma unroll 8
+    for (int i = tid; i < n; i += BS_THREADS) most = max(most, key(i));
+    b.thread_max[tid] = most;
+    if (tid == 0) {
+        b.bound = 1;  // fewer than k groups with a key: all keys
+        b.n = 0;
+    }
+    if (tid < BS_MAX_K) b.best[tid] = 0;
+    __syncthreads();
+    unsigned long long mine = 0;
+    if (tid < GROUPS) {
+#pragma unroll
+        for (int u = 0; u < BS_THREADS / GROUPS; ++u) mine = max(mine, b.thread_max[tid + u * GROUPS]);
+        b.group_max[tid] = mine;
+    }
+    __syncthreads();
+    if (tid < GROUPS) {
+        int larger = 0;
+#pragma unroll 16
+        for (int i = 0; i < GROUPS; ++i) larger += b.group_max[i] > mine;
+        if (larger == k - 1 && mine) b.bound = mine;
+    }
+    __syncthreads();
+    const unsigned long long bound = b.bound;
+    if (most >= bound)
+        for (int i = tid; i < n; i += BS_THREADS) {
+            const unsigned long long x = key(i);
+            if (x >= bound) {
+                const int at = atomicAdd(&b.n, 1);
+                if (at < CAND_MAX) b.cand[at] = x;
+            }
+        }
+    __syncthreads();
+    const int found = b.n;
+    if (found <= CAND_MAX) {
+        for (int i = tid; i < found; i += BS_THREADS) {
+            const unsigned long long x = b.cand[i];
+            int larger = 0;
+            for (int j = 0; j < found; ++j) larger += b.cand[j] > x;
+            if (larger < k) b.best[larger] = x;
+        }
+        __syncthreads();
+        return;
+    }
+    unsigned long long last = ~0ull;
+    for (int r = 0; r < k && last; ++r) {
+        unsigned long long x = 0;
+        for (int i = tid; i < n; i += BS_THREADS) {
+            const unsigned long long y = key(i);
+            if (y < last) x = max(x, y);
+        }
+        x = warp_max64(x);
+        if ((tid & 31) == 0) b.warp_best[tid >> 5] = x;
+        __syncthreads();
+        x = 0;
+#pragma unroll
+        for (int w = 0; w < BS_WARPS; ++w) x = max(x, b.warp_best[w]);
+        if (tid == 0) b.best[r] = x;
+        last = x;
+        __syncthreads();
+    }
+}
+
+struct F32T {
+    using elem = float;
+    static constexpr int PER = 4;
+    static __device__ __forceinline__ float one(const void* p, int64_t i) { return __ldg(static_cast<const float*>(p) + i); }
+    static __device__ __forceinline__ void unpack(uint4 v, float* x) {
+        x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+    }
+};
+template <class T>
+struct Half {
+    using elem = uint16_t;
+    static constexpr int PER = 8;
+    static __device__ __forceinline__ float one(const void* p, int64_t i) {
+        return T::to_float(__ldg(static_cast<const uint16_t*>(p) + i));
+    }
+    static __device__ __forceinline__ void unpack(uint4 v, float* x) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = T::to_float((uint16_t)w[i]);
+            x[2 * i + 1] = T::to_float((uint16_t)(w[i] >> 16));
+        }
+    }
+};
+
+// use(i, x) for the elements [0, n) at p + first, by the block: single ones up to the first
+// 16-byte boundary, 16 bytes at a time with UNROLL loads in flight, single ones at the end.
+template <class T, int THREADS, int UNROLL, class F>
+__device__ __forceinline__ void for_row(const void* base, int64_t first, int n, F use) {
+    using E = typename T::elem;
+    const E* p = static_cast<const E*>(base) + first;
+    const int tid = threadIdx.x;
+    const int head = min(n, (int)(((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / sizeof(E)));
+    const int vecs = (n - head) / T::PER;
+    if (tid < head) use(tid, T::one(p, tid));
+    const uint4* v = reinterpret_cast<const uint4*>(p + head);
+    for (int i0 = tid; i0 < vecs; i0 += THREADS * UNROLL) {
+        uint4 raw[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u)
+            if (i0 + u * THREADS < vecs) raw[u] = __ldg(v + i0 + u * THREADS);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int i = i0 + u * THREADS;
+            if (i < vecs) {
+                float x[T::PER];
+                T::unpack(raw[u], x);
+#pragma unroll
+                for (int e = 0; e < T::PER; ++e) use(head + i * T::PER + e, x[e]);
+            }
+        }
+    }
+    const int rest = head + vecs * T::PER + tid;
+    if (rest < n) use(rest, T::one(p, rest));
+}
+
+// (maximum, sum of exp(x - maximum)) of two sets, as one
+__device__ __forceinline__ void join_sums(float& m, float& s, float m2, float s2) {
+    const float top = fmaxf(m, m2);
+    if (top == -INFINITY) return;  // neither has a value
+    s = s * __expf(m - top) + s2 * __expf(m2 - top);
+    m = top;
+}
+__device__ __forceinline__ float warp_lse(float m, float s) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        join_sums(m, s, __shfl_xor_sync(FULL_MASK, m, o), __shfl_xor_sync(FULL_MASK, s, o));
+    return s != s ? NAN : m + logf(s);  // (nothing but -inf: -inf)
+}
+
+// log-sum-exp of a row, one CTA each: a running maximum and sum per thread.  Bound by memory.
+template <class T>
+__global__ void __launch_bounds__(LSE_THREADS) row_lse_kernel(const void* logits, int64_t stride, int vocab,
+                                                              float* out) {
+    __shared__ float2 part[LSE_THREADS / 32];
+    const int row = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    pdl_launch_dependents();
+    float m = -INFINITY, s = 0.f;
+    for_row<T, LSE_THREADS, 4>(logits, row * stride, vocab, [&](int, float x) {
+        if (x > m) {
+            s *= __expf(m - x);  // (the first value: 0)
+            m = x;
+        }
+        s += x == -INFINITY ? 0.f : __expf(x - m);
+    });
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        join_sums(m, s, __shfl_xor_sync(FULL_MASK, m, o), __shfl_xor_sync(FULL_MASK, s, o));
+    if (lane == 0) part[warp] = make_float2(m, s);
+    __syncthreads();
+    if (warp == 0) {
+        const float2 q = lane < LSE_THREADS / 32 ? part[lane] : make_float2(-INFINITY, 0.f);
+        const float lse = warp_lse(q.x, q.y);
+        if (lane == 0) out[row] = lse;
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(BS_THREADS) beam_select_kernel(const SelectArgsB p) {
+    extern __shared__ float bs_score[];  // [seg_len]; the item's keys when they are joined
+    __shared__ Best b;
+    __shared__ float s_lse[BS_MAX_BEAMS], s_beam[BS_MAX_BEAMS];
+    __shared__ int s_done[BS_MAX_BEAMS], s_last;
+    const mtp_beam_select_args& a = p.a;
+    const int item = blockIdx.y, seg = blockIdx.x, W = a.beams, V = a.vocab, tid = threadIdx.x;
+    const int first = seg * p.seg_len, n = min(p.seg_len, W * V - first);
+    pdl_wait();
+    if (tid < W) {
+        s_beam[tid] = a.scores[item * W + tid];
+        s_done[tid] = a.done ? a.done[item * W + tid] : 0;
+        if (!p.lse_here) s_lse[tid] = p.lse[item * W + tid];
+    }
+    __syncthreads();
+    // the segment's logits, beam by beam, as scores (as they are where their log-sum-exp is still to come)
+    const int beam0 = first / V, beam1 = (first + n - 1) / V;
+    for (int w = beam0; w <= beam1; ++w) {
+        const int c0 = max(0, first - w * V), c1 = min(V, first + n - w * V);
+        float* to = bs_score + (w * V + c0 - first);
+        const float cum = s_beam[w], lse = p.lse_here ? 0.f : s_lse[w];
+        if (s_done[w] && !p.lse_here) {
+            for (int i = tid; i < c1 - c0; i += BS_THREADS) to[i] = c0 + i == a.eos_id ? cum : -INFINITY;
+        } else {
+            const bool raw = p.lse_here;
+            for_row<T, BS_THREADS, 4>(a.logits, ((int64_t)item * W + w) * a.logits_stride + c0, c1 - c0,
+                                      [&](int i, float x) { to[i] = raw ? x : cum + (x - lse); });
+        }
+    }
+    __syncthreads();
+    if (p.lse_here) {
+        for (int w = tid >> 5; w < W; w += BS_WARPS) {
+            const float* x = bs_score + w * V;
+            float m = -INFINITY, s = 0.f;
+            for (int i = tid & 31; i < V; i += 32) m = fmaxf(m, x[i]);
+            m = warp_max(m);
+            for (int i = tid & 31; i < V; i += 32) s += x[i] == -INFINITY ? 0.f : __expf(x[i] - m);
+            s = warp_sum(s);
+            if ((tid & 31) == 0) s_lse[w] = m + logf(s);
+        }
+        __syncthreads();
+        for (int i = tid; i < n; i += BS_THREADS) {
+            const int w = i / V;
+            bs_score[i] = !s_done[w] ? s_beam[w] + (bs_score[i] - s_lse[w]) : i - w * V == a.eos_id ? s_beam[w] : -INFINITY;
+        }
+        __syncthreads();
+    }
+    if (seg == 0 && a.out_lse && tid < W) a.out_lse[item * W + tid] = s_lse[tid];
+    best_of(b, n, a.k, [&](int i) { return make_key(bs_score[i], (uint32_t)(first + i)); });
+
+    if (p.segments > 1) {
+        unsigned long long* keys = p.keys + (size_t)item * p.segments * a.k;
+        if (tid < a.k) __stcg(keys + (size_t)seg * a.k + tid, b.best[tid]);
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) s_last = atomicAdd(p.count + item, 1) == p.segments - 1;
+        __syncthreads();
+        if (!s_last) return;
+        __threadfence();
+        if (tid == 0) p.count[item] = 0;
+        // the k best of all segments' keys, as many at a time as shared memory holds beside the best so far
+        unsigned long long* held = reinterpret_cast<unsigned long long*>(bs_score);
+        const int room = p.seg_len / 2, total = p.segments * a.k;
+        int have = 0;
+        for (int at = 0; at < total;) {
+            const int take = min(room - have, total - at);
+            for (int i = tid; i < take; i += BS_THREADS) held[have + i] = __ldcg(keys + at + i);
+            __syncthreads();
+            best_of(b, have + take, a.k, [&](int i) { return held[i]; });
+            at += take;
+            have = a.k;
+            if (at < total) {
+                if (tid < a.k) held[tid] = b.best[tid];
+                __syncthreads();
+            }
+        }
+    }
+    if (tid < a.k) {
+        const unsigned long long key = b.best[tid];
+        const uint32_t number = 0xffffffffu - (uint32_t)key;
+        const int parent = (int)(number / (uint32_t)V), token = (int)(number - (uint32_t)parent * V);
+        const size_t at = (size_t)item * a.k + tid;
+        a.out_scores[at] = key_score(key);
+        a.out_parent[at] = parent;
+        a.out_token[at] = token;
+        if (a.out_done) a.out_done[at] = token == a.eos_id || s_done[parent];
+    }
+}
+
+struct SelectPlan {
+    int segments, seg_len;
+    bool lse_here, lse_before;
+    size_t count_bytes, key_bytes, need;
+};
+
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+int select_plan(const mtp_beam_select_args* a, SelectPlan* p) {
+    if (!a || a->batch < 1 || a->batch > BS_MAX_BATCH || a->beams < 1 || a->beams > BS_MAX_BEAMS || a->vocab < 1 ||
+        (long long)a->beams * a->vocab > (1 << 30) || a->k < 1 || a->k > BS_MAX_K ||
+        (long long)a->k > (long long)a->beams * a->vocab)
+        return invalid("beam_select: invalid sizes");
+    if (a->logits_dtype != MTP_F32 && a->logits_dtype != MTP_BF16 && a->logits_dtype != MTP_F16)
+        return invalid("beam_select: logits_dtype %d", a->logits_dtype);
+    const int all = a->beams * a->vocab;
+    p->segments = (all + SEG - 1) / SEG;
+    p->seg_len = ((all + p->segments - 1) / p->segments + 7) & ~7;  // even segments
+    p->segments = (all + p->seg_len - 1) / p->seg_len;
+    p->lse_here = !a->lse && p->segments == 1;
+    p->lse_before = !a->lse && p->segments > 1;
+    // the counters' place is the same for all calls, and they are left zero
+    p->count_bytes = p->segments > 1 || p->lse_before ? BS_MAX_BATCH * sizeof(int) : 0;
+    p->key_bytes = p->segments > 1 ? align256((size_t)a->batch * p->segments * a->k * 8) : 0;
+    p->need = p->count_bytes + p->key_bytes +
+              (p->lse_before && !a->out_lse ? align256((size_t)a->batch * a->beams * sizeof(float)) : 0);
+    return MTP_OK;
+}
+
+template <class T>
+cudaError_t launch_select(const mtp_beam_select_args* a, const SelectPlan& pl, char* ws, cudaStream_t s) {
+    SelectArgsB p{*a, pl.segments, pl.seg_len, pl.lse_here, a->lse, reinterpret_cast<unsigned long long*>(ws + pl.count_bytes),
+                  reinterpret_cast<int*>(ws)};
+    if (pl.lse_before) {
+        float* lse = a->out_lse ? a->out_lse : reinterpret_cast<float*>(ws + pl.count_bytes + pl.key_bytes);
+        p.lse = lse;
+        p.a.out_lse = nullptr;  // written already
+        row_lse_kernel<T><<<a->batch * a->beams, LSE_THREADS, 0, s>>>(a->logits, a->logits_stride, a->vocab, lse);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+    }
+    const size_t smem = (size_t)pl.seg_len * sizeof(float);
+    const void* kern = reinterpret_cast<const void*>(beam_select_kernel<T>);
+    cudaError_t e = ensure_kernel_smem(kern, smem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(pl.segments, a->batch);
+    cfg.blockDim = dim3(BS_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = pl.lse_before ? 1 : 0;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, beam_select_kernel<T>, p);
+}
+
+}  // namespace
+}  // namespace mtp
+
+using namespace mtp;
+
+extern "C" {
+
+MTP_API size_t mtp_beam_select_workspace_bytes(const mtp_beam_select_args* a) {
+    SelectPlan p;
+    size_t need = 0;
+    guarded([&]() -> int {
+        const int r = select_plan(a, &p);
+        need = r == MTP_OK ? p.need : 0;
+        return r;
+    });
+    return need;
+}
+
+MTP_API int mtp_beam_select(const mtp_beam_select_args* a, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    return guarded([&]() -> int {
+        SelectPlan p;
+        if (const int r = select_plan(a, &p)) return r;
+        if (!a->logits || !a->scores || !a->out_scores || !a->out_parent || !a->out_token)
+            return invalid("beam_select: null pointer");
+        if (a->logits_stride < a->vocab) return invalid("beam_select: logits_stride %lld below the vocabulary", (long long)a->logits_stride);
+        if (a->eos_id >= a->vocab) return invalid("beam_select: eos_id %d", a->eos_id);
+        if (a->done && a->eos_id < 0) return invalid("beam_select: finished beams need an eos_id");
+        if (reinterpret_cast<uintptr_t>(a->logits) % (a->logits_dtype == MTP_F32 ? 4 : 2))
+            return invalid("beam_select: logits must be aligned to their elements");
+        if (p.need && (!workspace || !aligned16(workspace) || workspace_bytes < p.need))
+            return invalid("beam_select: workspace %zu bytes, need %zu, 16-byte aligned", workspace_bytes, p.need);
+        const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+        char* ws = static_cast<char*>(workspace);
+        const cudaError_t e = a->logits_dtype == MTP_F32    ? launch_select<F32T>(a, p, ws, s)
+                              : a->logits_dtype == MTP_BF16 ? launch_select<Half<Bf16>>(a, p, ws, s)
+                                                            : launch_select<Half<F16>>(a, p, ws, s);
+        return cuda_status(e, "beam_select");
+    });
+}
+
+}  // extern "C"

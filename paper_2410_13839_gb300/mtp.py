@@ -13,7 +13,7 @@ import numpy as np
 
 from . import _lib
 from ._lib import (MTP_OPT_BATCHED, MTPError, MtpAttentionArgs, MtpBeamReorderArgs,  # noqa: F401
-                   MtpCacheAppendArgs, MtpConfig, MtpPagePlanArgs, check, lib)
+                   MtpBeamSelectArgs, MtpCacheAppendArgs, MtpConfig, MtpPagePlanArgs, check, lib)
 
 BLOB_MAGIC = b"MTPWGT01"
 
@@ -337,6 +337,37 @@ def mtp_cache_append(args: MtpCacheAppendArgs, stream=None) -> None:
     check(lib.mtp_cache_append(ctypes.byref(args), _stream_handle(stream)))
 
 
+def beam_select_args(logits, scores, k, out_scores, out_parent, out_token, lse=None, done=None, eos_id=-1,
+                     out_done=None, out_lse=None) -> MtpBeamSelectArgs:
+    """Argument block of mtp_beam_select: logits [batch, beams, vocab], the rows of all beams at one stride."""
+    batch, beams, vocab = logits.shape
+    code = _dtype("logits", logits, (_lib.MTP_F32, _lib.MTP_BF16, _lib.MTP_F16))
+    if not logits.is_cuda or (vocab != 1 and logits.stride(2) != 1) or (
+            batch != 1 and beams != 1 and logits.stride(0) != beams * logits.stride(1)):
+        raise ValueError("logits: rows on the GPU, contiguous and at one stride, are wanted")
+    stride = logits.stride(1) if beams != 1 else logits.stride(0) if batch != 1 else vocab
+
+    def opt(name, x, dtype, shape):
+        return None if x is None else _buf(name, x, dtype, shape)
+    return MtpBeamSelectArgs(
+        batch=batch, beams=beams, vocab=vocab, k=k, eos_id=eos_id, logits_dtype=code, logits_stride=stride,
+        logits=logits.data_ptr(), lse=opt("lse", lse, "float32", (batch, beams)),
+        scores=_buf("scores", scores, "float32", (batch, beams)), done=opt("done", done, "int32", (batch, beams)),
+        out_scores=_buf("out_scores", out_scores, "float32", (batch, k)),
+        out_parent=_buf("out_parent", out_parent, "int32", (batch, k)),
+        out_token=_buf("out_token", out_token, "int32", (batch, k)),
+        out_done=opt("out_done", out_done, "int32", (batch, k)), out_lse=opt("out_lse", out_lse, "float32", (batch, beams)))
+
+
+def mtp_beam_select_workspace_bytes(args: MtpBeamSelectArgs) -> int:
+    return int(lib.mtp_beam_select_workspace_bytes(ctypes.byref(args)))
+
+
+def mtp_beam_select(args: MtpBeamSelectArgs, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    """The k best continuations of each item over its beams and the vocabulary."""
+    check(lib.mtp_beam_select(ctypes.byref(args), _ptr(workspace), workspace_bytes, _stream_handle(stream)))
+
+
 def beam_reorder_args(parent, block_table, kv_lens, page_refs, kv_pool, out_block_table, out_kv_lens, out_page_refs,
                       out_status) -> MtpBeamReorderArgs:
     """Argument block of mtp_beam_reorder: parent [batch, beams]."""
@@ -446,4 +477,4 @@ class MTPDecoder:
 
 __all__ = [n for n in dir() if n.startswith("mtp_")] + ["MTPDecoder", "MTPError", "pack_weights",
                                                          "make_config", "attention_args", "page_plan_args",
-                                                         "cache_append_args", "beam_reorder_args"]
+                                                         "cache_append_args", "beam_select_args", "beam_reorder_args"]

@@ -28,6 +28,13 @@ def _reorder(**kw):
     return MtpBeamReorderArgs(**{**d, **kw})
 
 
+def _select(**kw):
+    from paper_2410_13839_gb300._lib import MtpBeamSelectArgs
+    d = dict(batch=2, beams=4, vocab=1025, k=8, eos_id=1024, logits_dtype=0, logits_stride=1025)
+    d.update({n: A * (i + 1) for i, (n, t) in enumerate(MtpBeamSelectArgs._fields_[7:])})
+    return MtpBeamSelectArgs(**{**d, **kw})
+
+
 def _refused(call):
     from paper_2410_13839_gb300 import mtp
     with pytest.raises(mtp.MTPError) as e:
@@ -69,10 +76,29 @@ def test_beam_reorder_workspace(libpath):  # noqa: F811
         _refused(lambda m: m.mtp_beam_reorder(_reorder(), ws, n))
 
 
+@pytest.mark.parametrize("kw", [dict(batch=0), dict(batch=4097), dict(beams=0), dict(beams=65), dict(vocab=0), dict(k=0),
+                                dict(k=65), dict(vocab=1, logits_stride=1, k=5, eos_id=0), dict(vocab=1 << 29),
+                                dict(eos_id=1025), dict(eos_id=-1), dict(logits_dtype=3), dict(logits_stride=1024),
+                                dict(logits=None), dict(scores=None), dict(out_scores=None), dict(out_parent=None),
+                                dict(out_token=None), dict(logits=A + 2)])
+def test_beam_select(libpath, kw):  # noqa: F811
+    _refused(lambda mtp: mtp.mtp_beam_select(_select(**kw), A, 1 << 30))
+
+
+def test_beam_select_workspace(libpath):  # noqa: F811
+    from paper_2410_13839_gb300 import mtp
+    assert mtp.mtp_beam_select_workspace_bytes(_select()) == 0  # an item of one segment needs none
+    big = dict(vocab=100000, logits_stride=100000, eos_id=5)
+    need = mtp.mtp_beam_select_workspace_bytes(_select(**big))
+    assert need > 0 and mtp.mtp_beam_select_workspace_bytes(_select(vocab=-1)) == 0
+    for ws, n in ((None, need), (A, need - 1), (A + 8, need)):
+        _refused(lambda m: m.mtp_beam_select(_select(**big), ws, n))
+
+
 def test_null_argument_blocks(libpath):  # noqa: F811
     from paper_2410_13839_gb300 import _lib
     for call in (lambda: _lib.lib.mtp_page_plan(None, None), lambda: _lib.lib.mtp_cache_append(None, None),
-                 lambda: _lib.lib.mtp_beam_reorder(None, None, 0, None)):
+                 lambda: _lib.lib.mtp_beam_select(None, None, 0, None), lambda: _lib.lib.mtp_beam_reorder(None, None, 0, None)):
         assert call() == -1
     assert _lib.lib.mtp_beam_reorder_workspace_bytes(None) == 0
 
