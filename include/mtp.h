@@ -544,6 +544,48 @@ typedef struct mtp_cache_append_args {
 } mtp_cache_append_args;
 MTP_API int mtp_cache_append(const mtp_cache_append_args* args, void* cuda_stream);
 
+/* Causal attention of a chunk of new tokens per slot over one layer of the cache, whose
+ * keys and values (the new tokens' too) are there: decoding steps, drafts to verify,
+ * chunked prefill, mixed batches.  Slot s has the rows cu_rows[s] .. cu_rows[s + 1] - 1, its
+ * last n = cu_rows[s + 1] - cu_rows[s] tokens: row i of them is position
+ * kv_lens[s] - n + i and sees the keys up to its own, the last `window` of them where
+ * window > 0.  A row that sees no key (a position below 0) gives 0, with lse -inf.
+ * Query head h uses key head h / (n_heads / n_kv_heads).
+ *   q, out       [rows][n_heads * head_dim] of dtype (MTP_BF16 or MTP_F16, the pool's type) with
+ *                row strides q_stride, out_stride (elements); head_dim 64 or 128
+ *   scale        factor of the products q . k, > 0 (head_dim ^ -0.5 as a rule)
+ *   block_table  int32 [slots][bt_stride]; of a slot the pages of the keys that its rows see are
+ *                used (keys on pages outside the pool count as zeros)
+ *   cu_rows      int32 [slots + 1], ascending; rows past the last are left as they are
+ *   kv_lens      int32 [slots]
+ *   out_lse      float [rows][n_heads] or NULL: natural log of the sum of exp(scale q . k)
+ *   max_new, max_keys  host-known upper bounds of a slot's new tokens and length: max_new
+ *                chooses the kernel, max_keys the number of CTAs
+ *   err_word     int32 on the device or NULL: MTP_DEVICE_ERR_* bits are ORed in
+ *   workspace    mtp_chunk_attention_workspace_bytes(args) bytes, 16-byte aligned, of any content;
+ *                calls that overlap need workspaces of their own
+ * What the cache holds past a slot's length, or before every row's window, may be anything,
+ * NaN too; a non-finite value inside can reach every row of the slot.
+ * Limits: slots <= 4096, n_heads <= 1024, n_heads / n_kv_heads <= 64, bt_stride * page_size <=
+ * 2^24, 8192 tiles (of 16 rows and more).  Errors: MTP_ERR_INVALID, MTP_ERR_CUDA. */
+typedef struct mtp_chunk_attention_args {
+    int32_t slots, rows, n_heads, n_kv_heads, head_dim, page_size, layers, layer, n_pages, bt_stride, dtype, window,
+        max_new, max_keys;
+    float scale;
+    int64_t q_stride, out_stride;
+    const void* q;
+    const void* kv_pool;
+    const int32_t* block_table;
+    const int32_t* cu_rows;
+    const int32_t* kv_lens;
+    void* out;
+    float* out_lse;
+    int32_t* err_word;
+} mtp_chunk_attention_args;
+MTP_API size_t mtp_chunk_attention_workspace_bytes(const mtp_chunk_attention_args* args);
+MTP_API int mtp_chunk_attention(const mtp_chunk_attention_args* args, void* workspace, size_t workspace_bytes,
+                                void* cuda_stream);
+
 /* Beam search's selection: of each item's beams * vocab continuations the k best,
  *   score(b, t) = scores[b] + (logits[b][t] - lse[b]),
  * each operation one fp32 operation, by descending score; equal scores by ascending beam,

@@ -53,9 +53,10 @@ class MtpAttentionArgs(ctypes.Structure):
             "q", "kv_pool", "block_table", "row_seq", "row_pos", "out")]
 
 
-def _struct(name: str, ints: str, strides: str, pointers: str):
-    """An argument block: int32 fields, then int64 fields, then pointers, as the header declares them."""
-    fields = [(n, ctypes.c_int32) for n in ints.split()] + [(n, ctypes.c_int64) for n in strides.split()]
+def _struct(name: str, ints: str, strides: str, pointers: str, floats: str = ""):
+    """An argument block: int32 fields, floats, int64 fields, then pointers, as the header declares them."""
+    fields = [(n, ctypes.c_int32) for n in ints.split()] + [(n, ctypes.c_float) for n in floats.split()]
+    fields += [(n, ctypes.c_int64) for n in strides.split()]
     return type(name, (ctypes.Structure,), {"_fields_": fields + [(n, ctypes.c_void_p) for n in pointers.split()]})
 
 
@@ -66,6 +67,10 @@ MtpPagePlanArgs = _struct(
 MtpCacheAppendArgs = _struct(
     "MtpCacheAppendArgs", "rows n_kv_heads head_dim page_size layers layer n_pages src_dtype pool_dtype",
     "k_stride v_stride", "k v slot_map kv_pool")
+MtpChunkAttentionArgs = _struct(
+    "MtpChunkAttentionArgs",
+    "slots rows n_heads n_kv_heads head_dim page_size layers layer n_pages bt_stride dtype window max_new max_keys",
+    "q_stride out_stride", "q kv_pool block_table cu_rows kv_lens out out_lse err_word", "scale")
 MtpBeamSelectArgs = _struct(
     "MtpBeamSelectArgs", "batch beams vocab k eos_id logits_dtype", "logits_stride",
     "logits lse scores done out_scores out_parent out_token out_done out_lse")
@@ -118,6 +123,8 @@ def _load() -> ctypes.CDLL:
         "mtp_gemm_bf16x2": (i32, [vp, vp, vp, vp, i32, i32, i32, i32, i32, vp]),
         "mtp_page_plan": (i32, [ctypes.POINTER(MtpPagePlanArgs), vp]),
         "mtp_cache_append": (i32, [ctypes.POINTER(MtpCacheAppendArgs), vp]),
+        "mtp_chunk_attention_workspace_bytes": (sz, [ctypes.POINTER(MtpChunkAttentionArgs)]),
+        "mtp_chunk_attention": (i32, [ctypes.POINTER(MtpChunkAttentionArgs), vp, sz, vp]),
         "mtp_beam_select_workspace_bytes": (sz, [ctypes.POINTER(MtpBeamSelectArgs)]),
         "mtp_beam_select": (i32, [ctypes.POINTER(MtpBeamSelectArgs), vp, sz, vp]),
         "mtp_beam_reorder_workspace_bytes": (sz, [ctypes.POINTER(MtpBeamReorderArgs)]),

@@ -1,0 +1,623 @@
+// chunk_attention.cu -- attention of a chunk of new tokens per slot over the paged
+// cache (mtp_chunk_attention): its entry point, the kernel of few rows per slot and key
+// head (decoding steps, drafts), and the merge of shared items.
+//
+//   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = 2^(s_ij - m_i),  s_ij = scale log2(e) q_i . k_j,
+//   lse_i = ln 2 (m_i + log2 sum_j p_ij),  j over the keys that token i sees,
+//
+// in one pass over the keys with a running maximum m_i (fp32, as the sums and outputs).
+//
+// Few rows: the keys are read once and used by few rows, so memory bounds it.  A CTA's
+// share of the unit stream (chunk.cuh) runs through a ring of stages of 64 keys; the fifth
+// warp fills them, a lane per page piece, with TMA copies that lay the rows out in the
+// 128-byte swizzle that ldmatrix reads without bank conflicts.  Each of the four other
+// warps takes 16 of a stage's keys: S = Q K^T and O += P V by mma.sync (16 rows of a tile
+// as M; tcgen05's 128 rows would be empty for most), with a maximum, sum and output of its
+// own, which the four join at the item's end.
+//
+// Q enters as it is (16 bits).  P enters as a pair hi + lo of the type, its rounding
+// residue with it: a bound memory leaves the second product free, and the outputs then
+// err by their own rounding alone (P rounded once would add as much again).
+#include <algorithm>
+
+#include "chunk.cuh"
+#include "frag.cuh"
+
+namespace mtp {
+
+int tc_encode_cache(CUtensorMap* map, const void* pool, int dtype, int head_dim, int page_size, uint64_t blocks,
+                    int box_rows);
+
+namespace {
+
+constexpr int FR_KEYS = 64, FR_WARPS = 5, FR_THREADS = FR_WARPS * 32, FR_CONSUMERS = 128;
+constexpr int CH_MIN_UNITS = 4;
+constexpr float LN2 = 0.69314718055994531f;
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void tma_cache(void* dst, const CUtensorMap* map, int x, int row, int block, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+            smem_addr(dst)),
+        "l"(map), "r"(x), "r"(row), "r"(block), "r"(smem_addr(bar))
+        : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;" ::"n"(FR_CONSUMERS) : "memory"); }
+
+template <class T>
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma16<Bf16>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma16<F16>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <class T>
+__device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t& lo) {
+    hi = T::pack(x, y);
+    lo = T::pack(x - T::to_float((uint16_t)hi), y - T::to_float((uint16_t)(hi >> 16)));
+}
+
+// Shared memory of the few-rows kernel, from a 1024-byte boundary: ring stages (K then V, each
+// HD / 64 tiles of 64 rows of 128 bytes), Q (HD / 64 tiles of TR rows), a join buffer of TR x HD
+// floats, per-warp maxima and sums, the map.
+template <int HD, int MT>
+struct FrLayout {
+    static constexpr int TR = 16 * MT;
+    static constexpr int STAGES = HD == 64 ? 4 : MT == 1 ? 3 : 2;
+    static constexpr uint32_t TILE = FR_KEYS * 128, KV = TILE * (HD / 64), STAGE = 2 * KV;
+    static constexpr uint32_t Q = STAGES * STAGE, JOIN = Q + TR * HD * 2, ML = JOIN + TR * HD * 4, MAP = ML + 2 * 4 * TR * 4;
+    static size_t bytes(int slots, int tiles) { return 1024 + MAP + chunk_map_bytes(slots, tiles); }
+};
+
+template <class T, int HD, int MT>
+__global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
+    chunk_rows_kernel(const ChunkArgs a, const __grid_constant__ CUtensorMap map) {
+    using L = FrLayout<HD, MT>;
+    constexpr int TR = L::TR, ST = L::STAGES;
+    extern __shared__ unsigned char fr_raw[];
+    __shared__ uint64_t full[ST], empty[ST];
+    __shared__ long long scan_part[FR_WARPS][2];
+    unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(fr_raw) + 1023) & ~(uintptr_t)1023);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
+    if (tid == 0) {
+        for (int i = 0; i < ST; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 4);
+        }
+        fence_barrier_init();
+    }
+    const ChunkMap m = chunk_map<FR_WARPS, TR, FR_KEYS>(a, sm + L::MAP, scan_part);  // (synchronises)
+    pdl_launch_dependents();
+    const long long u0 = m.units ? chunk_border(a, m, cta) : 0, u1 = m.units ? chunk_border(a, m, cta + 1) : 0;
+    if (tid == 0) a.desc[cta * CH_DESC] = 0;
+    if (cta >= m.ctas || u0 >= u1) return;
+    const ChunkItem start = chunk_item(a, m, u0);
+
+    if (warp == 4) {  // ---- the ring's filler ----
+        const int P = 1 << a.page_shift, box = min(P, FR_KEYS), per = FR_KEYS / box;
+        // this lane's piece of a stage: rows [sub * box, + box) of half `half` of K (0) or V (1)
+        const int sub = lane % per, half = lane / per % (HD / 64), kv = lane / per / (HD / 64);
+        const bool mine = kv < 2;
+        const uint32_t to = kv * L::KV + half * L::TILE + sub * box * 128;
+        ChunkItem it = start;
+        int k = (int)(u0 - it.first);
+        ChunkTile t = chunk_tile<TR, FR_KEYS>(a, chunk_slot_of(a, m, it.tile), it.tile - m.slot_first[chunk_slot_of(a, m, it.tile)]);
+        // the piece's page, -1 outside the pool (its rows are then zeros), -2 where no row sees a key of it
+        auto page_of = [&]() {
+            const int key = t.key0 + k * FR_KEYS + sub * box;
+            if (!mine || key >= t.hi || key + box <= t.lo) return -2;
+            const int page = __ldg(a.block_table + (size_t)t.slot * a.bt_stride + (key >> a.page_shift));
+            return page >= 0 && page < a.n_pages ? page : -1;
+        };
+        int page = page_of();
+        bool ok = true;
+        int issued = 0;
+        for (long long u = u0; u < u1; ++u, ++issued) {
+            const int st = issued % ST;
+            if (issued >= ST) {
+                ok = __all_sync(FULL_MASK, lane != 0 || mbar_wait(&empty[st], (uint32_t)(issued / ST - 1) & 1, a.err));
+                if (!ok) break;
+            }
+            const unsigned have = __ballot_sync(FULL_MASK, page != -2);
+            if (lane == 0) mbar_arrive_expect_tx(&full[st], __popc(have) * box * 128);
+            __syncwarp();
+            if (page != -2) {
+                const int row = (t.key0 + k * FR_KEYS + sub * box) & (P - 1);
+                const int block = page < 0 ? -1 : page * a.page_blocks + a.layer_block + kv * a.kv_heads + it.head;
+                tma_cache(sm + st * L::STAGE + to, &map, half * 64, row, block, &full[st]);
+            }
+            if (++k == it.units) {
+                const int tile = it.tile;
+                it = chunk_next(a, m, it);
+                k = 0;
+                if (it.tile != tile && u + 1 < u1) {
+                    const int s = chunk_slot_of(a, m, it.tile);
+                    t = chunk_tile<TR, FR_KEYS>(a, s, it.tile - m.slot_first[s]);
+                }
+            }
+            if (u + 1 < u1) page = page_of();
+        }
+        // after a failed wait: what is in flight lands before the CTA leaves
+        if (!ok && lane == 0)
+            for (int i = max(0, issued - ST); i < issued; ++i) mbar_wait(&full[i % ST], (uint32_t)(i / ST) & 1, nullptr);
+        return;
+    }
+
+    // ---- the rows ----
+    const int r0 = lane >> 2, c0 = (lane & 3) * 2;  // this lane's rows r0, r0 + 8 of 16, columns c0, c0 + 1 of 8
+    const uint32_t q_base = smem_addr(sm + L::Q);
+    float* join = reinterpret_cast<float*>(sm + L::JOIN);
+    float* ml = reinterpret_cast<float*>(sm + L::ML);  // [4 warps][TR] maxima, then sums
+    ChunkItem it = start;
+    int k = (int)(u0 - it.first), stage = 0;
+    bool alive = true;
+    for (long long u = u0; u < u1;) {
+        const int slot = chunk_slot_of(a, m, it.tile);
+        const ChunkTile t = chunk_tile<TR, FR_KEYS>(a, slot, it.tile - m.slot_first[slot]);
+        const int k1 = (int)min((long long)it.units, k + (u1 - u));
+        const bool begins = k == 0, ends = k1 == it.units;
+        // Q: 16 bytes a thread and step, rows past the tile zero
+        for (int i = tid; i < TR * (HD / 8); i += FR_CONSUMERS) {
+            const int r = i / (HD / 8), c = i % (HD / 8), p = t.p0 + r;
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (r < t.rows) {
+                const uint16_t* src = a.q + (t.row0 + p / a.group) * a.q_stride + (it.head * a.group + p % a.group) * HD + c * 8;
+                if (a.q_vec) {
+                    v = __ldg(reinterpret_cast<const uint4*>(src));
+                } else {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = (uint32_t)__ldg(src + 2 * e) | (uint32_t)__ldg(src + 2 * e + 1) << 16;
+                    v = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+            *reinterpret_cast<uint4*>(sm + L::Q + (c >> 3) * (TR * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
+        }
+        consumer_sync();
+        float o[MT][HD / 8][4], mx[MT][2], sum[MT][2];
+        int pos[MT][2];  // the rows' positions
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+            for (int d = 0; d < HD / 8; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[i][d][e] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                mx[i][e] = -INFINITY;
+                sum[i][e] = 0.f;
+                const int r = i * 16 + r0 + e * 8;
+                pos[i][e] = r < t.rows ? t.len - t.n + (t.p0 + r) / a.group : -1;
+            }
+        }
+        const int pos_first = t.len - t.n + t.p0 / a.group, pos_last = t.hi - 1;
+        for (; k < k1; ++k, ++u) {
+            const int st = stage % ST;
+            if (alive) alive = __all_sync(FULL_MASK, lane != 0 || mbar_wait(&full[st], (uint32_t)(stage / ST) & 1, a.err));
+            const int key0 = t.key0 + k * FR_KEYS + warp * 16;  // this warp's keys
+            if (alive && key0 < t.hi && key0 + 16 > t.lo) {
+                unsigned char* kb = sm + st * L::STAGE;
+                // a unit that every row sees in full needs no mask; its keys are all copied
+                const bool inner = key0 + 15 <= pos_first && (a.window <= 0 || key0 > pos_last - a.window) && t.rows == TR;
+                const bool edge = key0 + 16 > t.hi || key0 < t.lo;  // keys that no row sees: their values may be anything
+                if (edge) {
+                    const int r = lane >> 1, key = key0 + r;
+                    if (key >= t.hi || key < t.lo)
+                        for (int c = lane & 1; c < HD / 8; c += 2)
+                            *reinterpret_cast<uint4*>(kb + L::KV + (c >> 3) * L::TILE + (warp * 16 + r) * 128 + (c & 7) * 16) =
+                                make_uint4(0u, 0u, 0u, 0u);
+                    fence_proxy_async();  // (the stage is copied into again)
+                    __syncwarp();
+                }
+                const uint32_t kr = smem_addr(kb), vr = kr + L::KV;
+                float s[MT][2][4];
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[i][j][e] = 0.f;
+#pragma unroll
+                for (int d = 0; d < HD / 16; ++d) {
+                    uint32_t kf[4];
+                    const int key = warp * 16 + ((lane >> 4) << 3) + (lane & 7), c = 2 * d + ((lane >> 3) & 1);
+                    frag::ldsm_x4(kf, kr + (c >> 3) * L::TILE + key * 128 + (((c & 7) ^ (key & 7)) << 4));
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        uint32_t qf[4];
+                        const int row = i * 16 + (lane & 15), cq = 2 * d + (lane >> 4);
+                        frag::ldsm_x4(qf, q_base + (cq >> 3) * (TR * 128) + row * 128 + (((cq & 7) ^ (row & 7)) << 4));
+                        mma16<T>(s[i][0], qf, kf[0], kf[1]);
+                        mma16<T>(s[i][1], qf, kf[2], kf[3]);
+                    }
+                }
+                uint32_t hi[MT][4], lo[MT][4];
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    if (!inner) {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int key = key0 + j * 8 + c0 + (e & 1), p = pos[i][e >> 1];
+                                if (key > p || (a.window > 0 && key <= p - a.window)) s[i][j][e] = -INFINITY;
+                            }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float top = fmaxf(fmaxf(s[i][0][2 * e], s[i][0][2 * e + 1]), fmaxf(s[i][1][2 * e], s[i][1][2 * e + 1]));
+                        top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, 1));
+                        top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, 2));
+                        const float now = fmaxf(mx[i][e], top * a.scale_log2);
+                        if (__any_sync(FULL_MASK, now > mx[i][e])) {
+                            const float f = mx[i][e] == -INFINITY ? 0.f : ex2(mx[i][e] - now);
+                            sum[i][e] *= f;
+#pragma unroll
+                            for (int d = 0; d < HD / 8; ++d) {
+                                o[i][d][2 * e] *= f;
+                                o[i][d][2 * e + 1] *= f;
+                            }
+                            mx[i][e] = now;
+                        }
+                        const float ref = now == -INFINITY ? 0.f : now;  // a row that has seen no key: every weight 0
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const float x = ex2(fmaf(s[i][j][2 * e], a.scale_log2, -ref)),
+                                        y = ex2(fmaf(s[i][j][2 * e + 1], a.scale_log2, -ref));
+                            sum[i][e] += x + y;
+                            split2<T>(x, y, hi[i][2 * j + e], lo[i][2 * j + e]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int d = 0; d < HD / 16; ++d) {
+                    uint32_t vf[4];
+                    const int key = warp * 16 + (lane & 15), c = 2 * d + (lane >> 4);
+                    frag::ldsm_x4_t(vf, vr + (c >> 3) * L::TILE + key * 128 + (((c & 7) ^ (key & 7)) << 4));
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        mma16<T>(o[i][2 * d], hi[i], vf[0], vf[1]);
+                        mma16<T>(o[i][2 * d + 1], hi[i], vf[2], vf[3]);
+                        mma16<T>(o[i][2 * d], lo[i], vf[0], vf[1]);
+                        mma16<T>(o[i][2 * d + 1], lo[i], vf[2], vf[3]);
+                    }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&empty[st]);
+            ++stage;
+        }
+        // ---- the four warps' maxima, sums and outputs as one ----
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                sum[i][e] += __shfl_xor_sync(FULL_MASK, sum[i][e], 1);
+                sum[i][e] += __shfl_xor_sync(FULL_MASK, sum[i][e], 2);
+                if ((lane & 3) == 0) {
+                    const int r = i * 16 + r0 + e * 8;
+                    ml[warp * TR + r] = mx[i][e];
+                    ml[(4 + warp) * TR + r] = sum[i][e];
+                }
+            }
+        consumer_sync();
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = i * 16 + r0 + e * 8;
+                float top = -INFINITY, all = 0.f;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * TR + r]);
+                const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) all = fmaf(ml[(4 + w) * TR + r], ex2(ml[w * TR + r] - ref), all);
+                const float f = ex2(mx[i][e] - ref);
+#pragma unroll
+                for (int d = 0; d < HD / 8; ++d) {
+                    o[i][d][2 * e] *= f;
+                    o[i][d][2 * e + 1] *= f;
+                }
+                mx[i][e] = top;
+                sum[i][e] = all;
+            }
+#pragma unroll
+        for (int w = 3; w >= 0; --w) {  // warp 3 leaves its outputs, 2 and 1 add theirs, 0 takes the sum
+            if (warp == w) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int d = 0; d < HD / 8; ++d) {
+                        float4* at = reinterpret_cast<float4*>(join) + (i * (HD / 8) + d) * 32 + lane;
+                        float4 v = make_float4(o[i][d][0], o[i][d][1], o[i][d][2], o[i][d][3]);
+                        if (w < 3) {
+                            const float4 x = *at;
+                            v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+                        }
+                        if (w > 0) *at = v;
+                        o[i][d][0] = v.x; o[i][d][1] = v.y; o[i][d][2] = v.z; o[i][d][3] = v.w;
+                    }
+            }
+            if (w > 0) consumer_sync();
+        }
+        if (warp == 0 && alive) {
+            if (begins && ends) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int r = i * 16 + r0 + e * 8, p = t.p0 + r;
+                        if (r >= t.rows) continue;
+                        const long long row = t.row0 + p / a.group;
+                        const int head = it.head * a.group + p % a.group;
+                        const float f = sum[i][e] == 0.f ? 0.f : 1.f / sum[i][e];  // (no key: 0)
+                        uint16_t* to = a.out + row * a.out_stride + head * HD + c0;
+#pragma unroll
+                        for (int d = 0; d < HD / 8; ++d) {
+                            const uint32_t v = T::pack(o[i][d][2 * e] * f, o[i][d][2 * e + 1] * f);
+                            if (a.out_vec) {
+                                *reinterpret_cast<uint32_t*>(to + d * 8) = v;
+                            } else {
+                                to[d * 8] = (uint16_t)v;
+                                to[d * 8 + 1] = (uint16_t)(v >> 16);
+                            }
+                        }
+                        if (a.lse && (lane & 3) == 0)
+                            a.lse[row * (a.kv_heads * a.group) + head] =
+                                sum[i][e] == 0.f ? -INFINITY : LN2 * (mx[i][e] + log2f(sum[i][e]));
+                    }
+            } else {
+                float* part = a.part + ((size_t)cta * 2 + begins) * TR * (HD + 2);
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int r = i * 16 + r0 + e * 8;
+#pragma unroll
+                        for (int d = 0; d < HD / 8; ++d)
+                            *reinterpret_cast<float2*>(part + r * HD + d * 8 + c0) = make_float2(o[i][d][2 * e], o[i][d][2 * e + 1]);
+                        if ((lane & 3) == 0)
+                            *reinterpret_cast<float2*>(part + TR * HD + 2 * r) = make_float2(mx[i][e], sum[i][e]);
+                    }
+                if (begins && lane == 0) {
+                    int* d = a.desc + cta * CH_DESC;
+                    d[0] = chunk_cta_of(m, it.first + it.units - 1) - cta;
+                    d[1] = t.p0;
+                    d[2] = t.rows;
+                    d[3] = t.row0;
+                    d[4] = it.head;
+                }
+            }
+        }
+        k = 0;
+        it = chunk_next(a, m, it);
+    }
+}
+
+// ---- merge ----
+// Grid (CTA of the kernel before, groups of four rows); a warp takes a row of the item that
+// begins in that CTA's share and goes on in the next ones': out = sum_c 2^(m_c - M) o_c / L,
+// L = sum_c 2^(m_c - M) l_c, M = max m_c, in the CTAs' order.
+template <class T, int HD, int TR>
+__global__ void __launch_bounds__(128) chunk_merge_kernel(const ChunkArgs a) {
+    const int cta = blockIdx.x, r = blockIdx.y * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    constexpr int PER = HD / 32;
+    pdl_wait();
+    const int* d = a.desc + cta * CH_DESC;
+    const int more = d[0];
+    if (more <= 0 || r >= d[2]) return;
+    constexpr size_t STEP = (size_t)TR * (HD + 2);
+    // parts: 1 of `cta` (the item begins there), then 0 of the CTAs after it
+    const float* first = a.part + ((size_t)cta * 2 + 1) * STEP;
+    const float* rest = a.part + ((size_t)cta + 1) * 2 * STEP;
+    auto part = [&](int i) { return i == 0 ? first : rest + (size_t)(i - 1) * 2 * STEP; };
+    float top = -INFINITY;
+    for (int i = lane; i <= more; i += 32) top = fmaxf(top, part(i)[TR * HD + 2 * r]);
+    top = warp_max(top);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float sum = 0.f, o[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) o[e] = 0.f;
+#pragma unroll 4
+    for (int i = 0; i <= more; ++i) {
+        const float* p = part(i);
+        const float2 x = *reinterpret_cast<const float2*>(p + TR * HD + 2 * r);
+        const float f = ex2(x.x - ref);
+        sum = fmaf(f, x.y, sum);
+#pragma unroll
+        for (int e = 0; e < PER; e += 2) {
+            const float2 v = *reinterpret_cast<const float2*>(p + r * HD + lane * PER + e);
+            o[e] = fmaf(f, v.x, o[e]);
+            o[e + 1] = fmaf(f, v.y, o[e + 1]);
+        }
+    }
+    const int p = d[1] + r, head = d[4] * a.group + p % a.group;
+    const long long row = d[3] + p / a.group;
+    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    uint16_t* to = a.out + row * a.out_stride + head * HD + lane * PER;
+#pragma unroll
+    for (int e = 0; e < PER; e += 2) {
+        const uint32_t v = T::pack(o[e] * f, o[e + 1] * f);
+        if (a.out_vec) {
+            *reinterpret_cast<uint32_t*>(to + e) = v;
+        } else {
+            to[e] = (uint16_t)v;
+            to[e + 1] = (uint16_t)(v >> 16);
+        }
+    }
+    if (a.lse && lane == 0)
+        a.lse[row * (a.kv_heads * a.group) + head] = sum == 0.f ? -INFINITY : LN2 * (top + log2f(sum));
+}
+
+template <class... P>
+cudaError_t launch_ex(void (*kern)(P...), dim3 grid, int threads, size_t smem, bool pdl, cudaStream_t s, P... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = pdl ? 1 : 0;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
+template <class T, int HD>
+cudaError_t merge_hd(const ChunkArgs& a, int tile_rows, int ctas, cudaStream_t s) {
+    const dim3 grid(ctas, tile_rows / 4);
+    switch (tile_rows) {
+        case 16: return launch_ex(chunk_merge_kernel<T, HD, 16>, grid, 128, 0, true, s, a);
+        case 32: return launch_ex(chunk_merge_kernel<T, HD, 32>, grid, 128, 0, true, s, a);
+        default: return launch_ex(chunk_merge_kernel<T, HD, 256>, grid, 128, 0, true, s, a);
+    }
+}
+
+// How a call runs: tile rows, CTAs, workspace.
+struct ChunkPlan {
+    int tile_rows, ctas, max_tiles;
+    size_t desc_bytes, need;
+};
+
+template <int HD, int MT>
+constexpr int fr_per_sm() { return HD == 64 && MT == 1 ? 3 : 2; }
+
+int chunk_plan(const mtp_chunk_attention_args* a, ChunkPlan* p) {
+    if (!a || a->slots < 1 || a->slots > CH_MAX_SLOTS || a->rows < 0 || a->n_heads < 1 || a->n_kv_heads < 1 ||
+        a->n_heads % a->n_kv_heads || a->n_heads / a->n_kv_heads > 64 || a->n_heads > 1024)
+        return invalid("chunk_attention: invalid sizes (slots, rows or heads)");
+    if (a->head_dim != 64 && a->head_dim != 128) return invalid("chunk_attention: head_dim %d: 64 or 128", a->head_dim);
+    if (!page_size_ok(a->page_size) || a->layers < 1 || a->layer < 0 || a->layer >= a->layers || a->n_pages < 1 ||
+        a->bt_stride < 1 || (long long)a->bt_stride * a->page_size > (1 << 24) ||
+        (long long)a->n_pages * a->layers * 2 * a->n_kv_heads > 0x7fffffffLL)
+        return invalid("chunk_attention: invalid cache (page_size %d, layers %d, layer %d, pages %d, bt_stride %d)",
+                       a->page_size, a->layers, a->layer, a->n_pages, a->bt_stride);
+    if (a->dtype != MTP_BF16 && a->dtype != MTP_F16) return invalid("chunk_attention: dtype %d", a->dtype);
+    if (a->window < 0 || a->max_new < 0 || a->max_keys < 0 || !(a->scale > 0.f) || !(a->scale < 1e30f))
+        return invalid("chunk_attention: window %d, max_new %d, max_keys %d, scale %g", a->window, a->max_new, a->max_keys,
+                       (double)a->scale);
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        cudaGetLastError();
+        return report_error(MTP_ERR_CUDA, "chunk_attention: no usable CUDA device");
+    }
+    const int group = a->n_heads / a->n_kv_heads;
+    const long long packed = (long long)std::min(a->max_new, a->rows) * group;  // rows of a slot and key head
+    p->tile_rows = packed <= 16 ? 16 : 32;
+    const long long tiles = std::min((long long)a->slots * ((packed + p->tile_rows - 1) / p->tile_rows),
+                                     (long long)a->rows * group / p->tile_rows + a->slots);
+    if (tiles > CH_MAX_TILES) return invalid("chunk_attention: %lld tiles of %d rows, at most %d", tiles, p->tile_rows, CH_MAX_TILES);
+    p->max_tiles = (int)tiles;
+    const int per_sm = a->head_dim == 64 && p->tile_rows == 16 ? 3 : 2;
+    const long long units = tiles * a->n_kv_heads * std::max(1, (a->max_keys + FR_KEYS - 1) / FR_KEYS + 1);
+    p->ctas = (int)std::max(1ll, std::min((long long)sms * per_sm, (units + CH_MIN_UNITS - 1) / CH_MIN_UNITS));
+    p->desc_bytes = ((size_t)p->ctas * CH_DESC * sizeof(int) + 255) & ~(size_t)255;
+    p->need = p->desc_bytes + (size_t)p->ctas * 2 * p->tile_rows * (a->head_dim + 2) * sizeof(float);
+    return MTP_OK;
+}
+
+template <class T, int HD, int MT>
+cudaError_t launch_rows(const ChunkArgs& a, const CUtensorMap& map, int ctas, cudaStream_t s) {
+    const size_t smem = FrLayout<HD, MT>::bytes(a.slots, a.max_tiles);
+    const auto kern = chunk_rows_kernel<T, HD, MT>;
+    const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem, true);
+    if (e != cudaSuccess) return e;
+    return launch_ex(kern, dim3(ctas), FR_THREADS, smem, false, s, a, map);
+}
+template <class T>
+cudaError_t launch_rows_of(const ChunkArgs& a, const CUtensorMap& map, int head_dim, const ChunkPlan& p, cudaStream_t s) {
+    if (head_dim == 64)
+        return p.tile_rows == 16 ? launch_rows<T, 64, 1>(a, map, p.ctas, s) : launch_rows<T, 64, 2>(a, map, p.ctas, s);
+    return p.tile_rows == 16 ? launch_rows<T, 128, 1>(a, map, p.ctas, s) : launch_rows<T, 128, 2>(a, map, p.ctas, s);
+}
+
+}  // namespace
+
+cudaError_t launch_chunk_merge(const ChunkArgs& a, int head_dim, int tile_rows, int dtype, int ctas, cudaStream_t s) {
+    if (dtype == MTP_BF16) return head_dim == 64 ? merge_hd<Bf16, 64>(a, tile_rows, ctas, s) : merge_hd<Bf16, 128>(a, tile_rows, ctas, s);
+    return head_dim == 64 ? merge_hd<F16, 64>(a, tile_rows, ctas, s) : merge_hd<F16, 128>(a, tile_rows, ctas, s);
+}
+
+}  // namespace mtp
+
+using namespace mtp;
+
+extern "C" {
+
+MTP_API size_t mtp_chunk_attention_workspace_bytes(const mtp_chunk_attention_args* a) {
+    size_t need = 0;
+    guarded([&]() -> int {
+        ChunkPlan p;
+        const int r = chunk_plan(a, &p);
+        need = r == MTP_OK ? p.need : 0;
+        return r;
+    });
+    return need;
+}
+
+MTP_API int mtp_chunk_attention(const mtp_chunk_attention_args* a, void* workspace, size_t workspace_bytes,
+                                void* cuda_stream) {
+    return guarded([&]() -> int {
+        ChunkPlan p;
+        if (const int r = chunk_plan(a, &p)) return r;
+        const int group = a->n_heads / a->n_kv_heads, width = a->n_heads * a->head_dim;
+        if (a->q_stride < width || a->out_stride < width)
+            return invalid("chunk_attention: row strides %lld, %lld below %d", (long long)a->q_stride,
+                           (long long)a->out_stride, width);
+        if (a->rows == 0 || a->max_new == 0) return MTP_OK;  // no new tokens
+        if (!a->q || !a->kv_pool || !a->block_table || !a->cu_rows || !a->kv_lens || !a->out)
+            return invalid("chunk_attention: null pointer");
+        if (!aligned16(a->kv_pool)) return invalid("chunk_attention: kv_pool must be 16-byte aligned");
+        if ((reinterpret_cast<uintptr_t>(a->q) | reinterpret_cast<uintptr_t>(a->out)) & 1)
+            return invalid("chunk_attention: q and out must be aligned to their elements");
+        if (!workspace || !aligned16(workspace) || workspace_bytes < p.need)
+            return invalid("chunk_attention: workspace %zu bytes, need %zu, 16-byte aligned", workspace_bytes, p.need);
+        ChunkArgs c;
+        c.q = static_cast<const uint16_t*>(a->q);
+        c.out = static_cast<uint16_t*>(a->out);
+        c.lse = a->out_lse;
+        c.block_table = a->block_table; c.cu_rows = a->cu_rows; c.kv_lens = a->kv_lens;
+        c.q_stride = a->q_stride; c.out_stride = a->out_stride;
+        c.slots = a->slots; c.rows = a->rows; c.kv_heads = a->n_kv_heads; c.group = group;
+        c.page_shift = a->page_size == 16 ? 4 : a->page_size == 32 ? 5 : a->page_size == 64 ? 6 : 7;
+        c.bt_stride = a->bt_stride; c.n_pages = a->n_pages;
+        c.page_blocks = a->layers * 2 * a->n_kv_heads;
+        c.layer_block = a->layer * 2 * a->n_kv_heads;
+        c.window = a->window; c.max_tiles = p.max_tiles; c.min_units = CH_MIN_UNITS; c.snap = 0;
+        c.q_vec = aligned16(a->q) && a->q_stride % 8 == 0;
+        c.out_vec = aligned16(a->out) && a->out_stride % 8 == 0;
+        c.scale_log2 = a->scale * 1.4426950408889634f;
+        c.desc = static_cast<int*>(workspace);
+        c.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.desc_bytes);
+        c.err = a->err_word;
+        const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+        CUtensorMap map;
+        if (tc_encode_cache(&map, a->kv_pool, a->dtype, a->head_dim, a->page_size,
+                            (uint64_t)a->n_pages * c.page_blocks, std::min(a->page_size, FR_KEYS)) != 0)
+            return report_error(MTP_ERR_CUDA, "chunk_attention: cuTensorMapEncodeTiled failed");
+        cudaError_t e = a->dtype == MTP_BF16 ? launch_rows_of<Bf16>(c, map, a->head_dim, p, s)
+                                             : launch_rows_of<F16>(c, map, a->head_dim, p, s);
+        if (e == cudaSuccess) e = launch_chunk_merge(c, a->head_dim, p.tile_rows, a->dtype, p.ctas, s);
+        return cuda_status(e, "chunk_attention");
+    });
+}
+
+}  // extern "C"

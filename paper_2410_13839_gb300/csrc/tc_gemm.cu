@@ -425,6 +425,21 @@ int tc_encode_rows(CUtensorMap* map, const void* base, uint64_t rows_per_block, 
     return r == CUDA_SUCCESS ? 0 : -3;
 }
 
+// A cache pool [blocks][page_size][head_dim] of 16-bit elements: boxes of 64 x box_rows of one block, laid out
+// with the 128-byte swizzle; blocks outside the pool read as zeros.
+int tc_encode_cache(CUtensorMap* map, const void* pool, int dtype, int head_dim, int page_size, uint64_t blocks,
+                    int box_rows) {
+    EncodeTiled fn = encode_fn();
+    if (!fn) return -1;
+    const cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)page_size, blocks};
+    const cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)head_dim * 2 * page_size};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, estr[3] = {1, 1, 1};
+    const CUresult r = fn(map, dtype == MTP_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                          const_cast<void*>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? 0 : -3;
+}
+
 int tc_tile_rows(int m) { return m <= 32 ? 32 : (m <= 64 ? 64 : 128); }
 
 cudaError_t launch_tc_gemm(const TcGemm& g, cudaStream_t s, bool pdl) {

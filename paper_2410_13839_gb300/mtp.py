@@ -13,7 +13,7 @@ import numpy as np
 
 from . import _lib
 from ._lib import (MTP_OPT_BATCHED, MTPError, MtpAttentionArgs, MtpBeamReorderArgs,  # noqa: F401
-                   MtpBeamSelectArgs, MtpCacheAppendArgs, MtpConfig, MtpPagePlanArgs, check, lib)
+                   MtpBeamSelectArgs, MtpCacheAppendArgs, MtpChunkAttentionArgs, MtpConfig, MtpPagePlanArgs, check, lib)
 
 BLOB_MAGIC = b"MTPWGT01"
 
@@ -337,6 +337,34 @@ def mtp_cache_append(args: MtpCacheAppendArgs, stream=None) -> None:
     check(lib.mtp_cache_append(ctypes.byref(args), _stream_handle(stream)))
 
 
+def chunk_attention_args(q, kv_pool, layer, block_table, cu_rows, kv_lens, out, scale, max_new, max_keys, window=0,
+                         out_lse=None, err_word=None) -> MtpChunkAttentionArgs:
+    """Argument block of mtp_chunk_attention: q, out [rows, heads, head_dim], their rows possibly strided."""
+    pool, dtype = _pool(kv_pool)
+    rows, heads, dim = q.shape
+    slots, stride = block_table.shape
+    if dim != pool["head_dim"] or q.dtype != kv_pool.dtype or out.dtype != kv_pool.dtype:
+        raise ValueError(f"q {tuple(q.shape)} {q.dtype}, out {out.dtype} and kv_pool {tuple(kv_pool.shape)} "
+                         f"{kv_pool.dtype} do not go together")
+    (qp, qs), (op, os_) = _rows("q", q, (rows, heads, dim)), _rows("out", out, (rows, heads, dim))
+    return MtpChunkAttentionArgs(
+        slots=slots, rows=rows, n_heads=heads, layer=layer, bt_stride=stride, dtype=dtype, window=window, max_new=max_new,
+        max_keys=max_keys, scale=scale, q_stride=qs, out_stride=os_, q=qp, out=op,
+        block_table=_buf("block_table", block_table, "int32", (slots, stride)),
+        cu_rows=_buf("cu_rows", cu_rows, "int32", (slots + 1,)), kv_lens=_buf("kv_lens", kv_lens, "int32", (slots,)),
+        out_lse=None if out_lse is None else _buf("out_lse", out_lse, "float32", (rows, heads)),
+        err_word=None if err_word is None else _buf("err_word", err_word, "int32"), **pool)
+
+
+def mtp_chunk_attention_workspace_bytes(args: MtpChunkAttentionArgs) -> int:
+    return int(lib.mtp_chunk_attention_workspace_bytes(ctypes.byref(args)))
+
+
+def mtp_chunk_attention(args: MtpChunkAttentionArgs, workspace, workspace_bytes: int, stream=None) -> None:
+    """Causal attention of a chunk of new tokens per slot over one layer of the paged cache."""
+    check(lib.mtp_chunk_attention(ctypes.byref(args), _ptr(workspace), workspace_bytes, _stream_handle(stream)))
+
+
 def beam_select_args(logits, scores, k, out_scores, out_parent, out_token, lse=None, done=None, eos_id=-1,
                      out_done=None, out_lse=None) -> MtpBeamSelectArgs:
     """Argument block of mtp_beam_select: logits [batch, beams, vocab], the rows of all beams at one stride."""
@@ -477,4 +505,4 @@ class MTPDecoder:
 
 __all__ = [n for n in dir() if n.startswith("mtp_")] + ["MTPDecoder", "MTPError", "pack_weights",
                                                          "make_config", "attention_args", "page_plan_args",
-                                                         "cache_append_args", "beam_select_args", "beam_reorder_args"]
+                                                         "cache_append_args", "chunk_attention_args", "beam_select_args", "beam_reorder_args"]

@@ -1,0 +1,246 @@
+"""mtp_chunk_attention against 64 bits.
+
+Bounds, element by element, with u half a unit of the output's type (2^-9 bf16, 2^-12 fp16), p a row's weights and
+A = sum_j p_j |v_j|: the output's rounding gives u |out|; weights rounded once to the type would give u A at most; scores
+of up to 128 products summed in fp32, exp2's approximation and sums in fp32 stay below 2^-14 A; fp16 weights below 2^-14
+of the largest are rounded to multiples of 2^-24, which gives 2^-25 sum_j |v_j| over the keys.  The log-sum-exp errs as
+one score does, and by its own rounding: 4e-5 + 2^-22 |lse|."""
+import pytest
+
+from gpu_util import lib_module
+
+pytestmark = pytest.mark.gpu
+
+NAN = float("nan")
+
+
+def reference(torch, q, pool, layer, table, new, lens, scale, window):
+    """(out, lse, A, sum |v|) in 64 bits, rows packed; rows without a key 0 and -inf."""
+    rows, heads, dim = q.shape
+    page, kv_heads = pool.shape[4], pool.shape[3]
+    out = torch.zeros(rows, heads, dim, dtype=torch.float64, device="cuda")
+    size, total = out.clone(), out.clone()
+    lse = torch.full((rows, heads), -float("inf"), dtype=torch.float64, device="cuda")
+    row = 0
+    for s, (n, length) in enumerate(zip(new, lens)):
+        pos = length - n + torch.arange(n, device="cuda")
+        key = torch.arange(length, device="cuda")
+        if n and length:
+            pages = torch.tensor([p if 0 <= p < len(pool) else 0 for p in table[s][:-(-length // page)]], device="cuda")
+            k, v = (pool[pages, layer, i].transpose(1, 2).flatten(0, 1)[:length].double().repeat_interleave(heads // kv_heads, 1)
+                    for i in (0, 1))
+            sees = key <= pos[:, None]
+            if window:
+                sees &= key > pos[:, None] - window
+            unseen = ~sees.any(0)
+            k[unseen], v[unseen] = 0.0, 0.0
+            for h in range(heads):
+                x = (q[row:row + n, h].double() @ k[:, h].T * scale).masked_fill(~sees, -float("inf"))
+                some = sees.any(1)
+                p = torch.where(some[:, None], torch.softmax(x, -1), 0.0).nan_to_num(0.0)
+                out[row:row + n, h] = p @ v[:, h]
+                size[row:row + n, h] = p @ v[:, h].abs()
+                total[row:row + n, h] = sees.double() @ v[:, h].abs()
+                lse[row:row + n, h] = torch.logsumexp(x, -1)
+        row += n
+    return out, lse, size, total
+
+
+def check(new, lens, heads, kv_heads, dim, page, dtype="bfloat16", window=0, layout="own", layers=2, layer=1, seed=0,
+          spread=2.0, rows_past=3, stream=None, workspace=None, hints=None, scale=None):
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    dt = getattr(torch, dtype)
+    gen = torch.Generator(device="cuda").manual_seed(seed + sum(lens))
+    counts = [-(-n // page) for n in lens]
+    n_pages, stride = sum(counts) + 2, max(counts + [1]) + 1
+    order = torch.randperm(n_pages, device="cuda", generator=gen).tolist()
+    bad = order.pop()  # a page of NaN, which no slot holds
+    pool = torch.randn(n_pages, layers, 2, kv_heads, page, dim, device="cuda", generator=gen).to(dt)
+    pool[bad] = NAN
+    table, it = [], iter(order)
+    for n, c in zip(lens, counts):
+        mine = [next(it) for _ in range(c)]
+        if n % page:
+            pool[mine[-1], :, :, :, n % page:] = NAN  # past the length: anything
+        table.append(mine + [bad] * (stride - c))
+    if window:  # what lies before every row's window: NaN, or pages given away
+        for s, (n, length) in enumerate(zip(new, lens)):
+            first = max(0, length - n - window + 1)
+            for c in range(first // page):
+                pool[table[s][c]] = NAN
+                table[s][c] = [bad, -1, 1 << 30][c % 3]
+            if first % page and first < length:
+                pool[table[s][first // page], :, :, :, :first % page] = NAN
+    pool[:, [i for i in range(layers) if i != layer]] = NAN
+    live, rows = sum(new), sum(new) + rows_past
+    pad = {"own": 0, "fused": 2 * kv_heads * dim, "odd": 1, "shifted": 3}[layout]
+    at = 1 if layout == "shifted" else 0
+
+    def buffer():
+        return torch.full((rows, heads * dim + pad), -7.0, device="cuda").to(dt)[:, at:at + heads * dim].unflatten(1, (heads, dim))
+    q, out = buffer(), buffer()
+    q.copy_((spread * torch.randn(rows, heads, dim, device="cuda", generator=gen)).to(dt))
+    lse = torch.full((rows, heads), -7.0, device="cuda")
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    d_table, cu, d_lens, err = ints(table), ints([sum(new[:i]) for i in range(len(new) + 1)]), ints(lens), ints([0])
+    scale = dim ** -0.5 if scale is None else scale
+    max_new, max_keys = hints or (max(new), max(lens))
+    args = mtp.chunk_attention_args(q=q, kv_pool=pool, layer=layer, block_table=d_table, cu_rows=cu, kv_lens=d_lens, out=out,
+                                    out_lse=lse, scale=scale, window=window, max_new=max_new, max_keys=max_keys, err_word=err)
+    nbytes = mtp.mtp_chunk_attention_workspace_bytes(args)
+    if workspace is None:
+        workspace = torch.full((max(16, nbytes),), 255, dtype=torch.uint8, device="cuda")  # any content (here NaN)
+    torch.cuda.synchronize()
+    mtp.mtp_chunk_attention(args, workspace, nbytes, stream or torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    assert int(err) == 0
+    ref, want_lse, size, total = reference(torch, q[:live], pool, layer, table, new, lens, scale, window)
+    u = 2.0 ** -9 if dtype == "bfloat16" else 2.0 ** -12
+    bound = u * ref.abs() + (u + 2.0 ** -14) * size + (2.0 ** -25 * total + 2.0 ** -25 if dtype == "float16" else 1e-30)
+    off = (out[:live].double() - ref).abs()
+    assert bool(out[:live].isfinite().all())
+    assert bool((off <= bound).all()), f"{(off - bound).max().item()} over its bound, {int((off > bound).sum())} values"
+    none = want_lse == -float("inf")
+    assert torch.equal(lse[:live] == -float("inf"), none)
+    assert bool((out[:live][none] == 0).all())
+    off = (lse[:live].double() - want_lse)[~none].abs()
+    assert bool((off <= 4e-5 + 2.0 ** -22 * want_lse[~none].abs()).all()), off.max().item()
+    assert bool((out[live:] == -7).all()) and bool((lse[live:] == -7).all())
+    return out, lse
+
+
+SHAPES = [(1, 1, 64), (16, 16, 64), (4, 1, 128), (8, 2, 64), (5, 1, 128), (32, 8, 128), (16, 1, 64)]
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("heads,kv_heads,dim", SHAPES)
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+def test_decoding_steps(heads, kv_heads, dim, page, dtype):
+    """One token a slot: lengths of one, around pages and units, and long ones."""
+    check([1] * 12, [1, 2, 15, 16, 17, 63, 64, 65, 127, 129, 1000, 5000], heads, kv_heads, dim, page, dtype)
+
+
+@pytest.mark.parametrize("new", [1, 2, 3, 5, 8, 17])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(2, 2, 64), (8, 2, 128), (6, 2, 64)])
+def test_drafts(heads, kv_heads, dim, new):
+    """A few new tokens a slot: the causal edge inside a unit, slots without tokens, a slot that holds nothing else."""
+    for lens in ([new, 64 + new, 63 + new, 129, 700, 64], [new] * 6):
+        tokens = [new, new, 0, max(1, new - 1), new, new] if new <= 64 else [new] * 6
+        check(tokens, lens, heads, kv_heads, dim, 16, seed=new)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(2, 2, 64), (4, 1, 128), (16, 2, 64), (3, 1, 128)])
+@pytest.mark.parametrize("page", [16, 64, 128])
+def test_chunks(heads, kv_heads, dim, page, dtype):
+    """Prompts from nothing and chunks behind cached tokens, of ragged sizes around tiles and units."""
+    check([33, 1, 127, 128, 129, 256, 257, 0, 500], [33, 300, 127, 700, 129, 256, 1257, 40, 513], heads, kv_heads, dim, page, dtype)
+
+
+def test_a_long_chunk_and_a_long_context():
+    check([2500], [2500], 4, 2, 128, 64)
+    check([700, 1, 90], [9000, 12000, 90], 8, 2, 64, 32, "float16")
+
+
+@pytest.mark.parametrize("window", [1, 2, 16, 63, 64, 65, 200, 4000])
+@pytest.mark.parametrize("new,lens", [([1, 1, 1, 4], [1, 300, 64, 2000]), ([300, 40, 1], [300, 500, 1500])])
+def test_windows(window, new, lens):
+    check(new, lens, 4, 2, 64, 16, window=window)
+    check(new, lens, 4, 1, 128, 64, "float16", window=window)
+
+
+def test_rows_that_see_no_key():
+    """More rows than the slot has tokens: the first of them are at positions below 0."""
+    check([5, 3, 1], [2, 3, 0], 4, 2, 64, 16)
+    check([300, 5], [100, 0], 2, 1, 128, 16)
+
+
+@pytest.mark.parametrize("layout", ["fused", "odd", "shifted"])
+@pytest.mark.parametrize("new", [1, 4, 150])
+def test_rows_at_any_stride_and_alignment(layout, new):
+    check([new, new], [200, 333], 4, 2, 64, 16, layout=layout)
+    check([new, new], [200, 333], 4, 4, 128, 32, layout=layout, dtype="float16")
+
+
+@pytest.mark.parametrize("new", [1, 200])
+def test_peaked_and_flat_scores(new):
+    for spread in (0.0, 30.0):
+        check([new], [1500], 4, 4, 64, 64, spread=spread)
+    check([new], [1500], 4, 4, 64, 64, scale=1e-3)
+
+
+def test_many_slots():
+    check([1] * 700, [1 + 7 * i % 400 for i in range(700)], 2, 1, 64, 16)
+    check([1 + i % 9 for i in range(300)], [10 + 13 * i % 300 for i in range(300)], 4, 1, 64, 32)
+
+
+def test_hints_may_be_generous():
+    for hints in ((1, 100000), (8, 300), (64, 20000), (1000, 1 << 20)):
+        check([1, 1, 1], [300, 20, 299], 4, 2, 64, 16, hints=hints, rows_past=1200)
+
+
+@pytest.mark.parametrize("new", [1, 300])
+def test_the_same_call_gives_the_same_bits(new):
+    torch = pytest.importorskip("torch")
+    a = check([new] * 5, [3000, 2500, 400, 1000, 301], 8, 2, 64, 16)
+    for _ in range(3):
+        b = check([new] * 5, [3000, 2500, 400, 1000, 301], 8, 2, 64, 16)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_another_stream_and_one_workspace():
+    torch = pytest.importorskip("torch")
+    stream = torch.cuda.Stream()
+    ws = torch.full((128 << 20,), 255, dtype=torch.uint8, device="cuda")
+    for new, lens in (([1, 1], [900, 4000]), ([400], [600]), ([3] * 40, [500] * 40), ([1], [1])):
+        check(new, lens, 8, 2, 128, 64, stream=stream, workspace=ws)
+
+
+@pytest.mark.parametrize("new", [1, 140])
+def test_a_cache_past_32_bits(new):
+    """Element offsets above 2^32: a pool of 8 GB whose last pages are used."""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    pool = torch.zeros(4200, 8, 2, 8, 128, 64, dtype=torch.bfloat16, device="cuda")
+    assert pool.numel() > 1 << 32
+    torch.manual_seed(1)
+    kv = torch.randn(3, 2, 8, 128, 64, device="cuda").bfloat16()
+    pages = [4199, 4100, 4198]
+    pool[pages, 7] = kv
+    q = torch.randn(new, 8, 64, device="cuda").bfloat16()
+    out, lse = torch.zeros_like(q), torch.zeros(new, 8, device="cuda")
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    table, cu, lens = ints([pages]), ints([0, new]), ints([300])
+    args = mtp.chunk_attention_args(q=q, kv_pool=pool, layer=7, block_table=table, cu_rows=cu, kv_lens=lens, out=out,
+                                    out_lse=lse, scale=0.125, max_new=new, max_keys=300)
+    n = mtp.mtp_chunk_attention_workspace_bytes(args)
+    mtp.mtp_chunk_attention(args, torch.empty(n, dtype=torch.uint8, device="cuda"), n, torch.cuda.current_stream())
+    k, v = (kv[:, i].transpose(0, 1).flatten(1, 2)[:, :300].double() for i in (0, 1))
+    x = torch.einsum("rhd,hkd->hrk", q.double(), k) * 0.125
+    x = x.masked_fill(torch.arange(300, device="cuda") > 300 - new + torch.arange(new, device="cuda")[:, None], -float("inf"))
+    ref = torch.einsum("hrk,hkd->rhd", torch.softmax(x, -1), v)
+    assert bool(((out.double() - ref).abs() <= 2.0 ** -9 * ref.abs() + (2.0 ** -9 + 2.0 ** -14) * 5).all())
+    assert bool(((lse.double() - torch.logsumexp(x, -1).T).abs() <= 4e-5).all())
+    assert float((out.double() - ref).norm() / ref.norm()) < 2.0 ** -8
+
+
+@pytest.mark.parametrize("kw", [dict(q=None), dict(kv_pool=None), dict(block_table=None), dict(cu_rows=None), dict(kv_lens=None),
+                                dict(out=None), dict(kv_pool=(1 << 20) + 8), dict(q=(1 << 20) + 1), dict(out=(1 << 20) + 1),
+                                dict(q_stride=255), dict(out_stride=0), dict(slots=4000, rows=1 << 20, max_new=300)])
+def test_refusals_behind_the_device_query(kw):
+    """Checked once the number of SMs is known; the addresses are never followed."""
+    from test_paged_refusals import A, _chunk, _refused
+    lib_module()
+    _refused(lambda mtp: mtp.mtp_chunk_attention(_chunk(**kw), A, 1 << 40))
+
+
+def test_workspace_and_empty_calls():
+    from test_paged_refusals import A, _chunk, _refused
+    mtp = lib_module()
+    need = mtp.mtp_chunk_attention_workspace_bytes(_chunk())
+    assert need > 0
+    for ws, n in ((None, need), (A, need - 1), (A + 8, need)):
+        _refused(lambda m: m.mtp_chunk_attention(_chunk(), ws, n))
+    mtp.mtp_chunk_attention(_chunk(rows=0), None, 0)
+    mtp.mtp_chunk_attention(_chunk(max_new=0), None, 0)

@@ -35,6 +35,14 @@ def _select(**kw):
     return MtpBeamSelectArgs(**{**d, **kw})
 
 
+def _chunk(**kw):
+    from paper_2410_13839_gb300._lib import MtpChunkAttentionArgs
+    d = dict(slots=2, rows=4, n_heads=4, n_kv_heads=2, head_dim=64, page_size=16, layers=2, layer=1, n_pages=8, bt_stride=4,
+             dtype=1, window=0, max_new=2, max_keys=64, scale=0.125, q_stride=256, out_stride=256, q=A, kv_pool=A, block_table=A,
+             cu_rows=A, kv_lens=A, out=A, out_lse=A)
+    return MtpChunkAttentionArgs(**{**d, **kw})
+
+
 def _refused(call):
     from paper_2410_13839_gb300 import mtp
     with pytest.raises(mtp.MTPError) as e:
@@ -76,6 +84,17 @@ def test_beam_reorder_workspace(libpath):  # noqa: F811
         _refused(lambda m: m.mtp_beam_reorder(_reorder(), ws, n))
 
 
+@pytest.mark.parametrize("kw", [dict(slots=0), dict(slots=4097), dict(rows=-1), dict(n_heads=3), dict(n_kv_heads=0),
+                                dict(n_heads=130), dict(n_heads=1026), dict(head_dim=96), dict(page_size=48), dict(layer=2),
+                                dict(layers=0), dict(n_pages=0), dict(n_pages=1 << 29), dict(bt_stride=0),
+                                dict(bt_stride=(1 << 20) + 1), dict(dtype=0), dict(window=-1), dict(max_new=-1),
+                                dict(max_keys=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan"))])
+def test_chunk_attention(libpath, kw):  # noqa: F811
+    from paper_2410_13839_gb300 import mtp
+    _refused(lambda m: m.mtp_chunk_attention(_chunk(**kw), A, 1 << 40))
+    assert mtp.mtp_chunk_attention_workspace_bytes(_chunk(**kw)) == 0
+
+
 @pytest.mark.parametrize("kw", [dict(batch=0), dict(batch=4097), dict(beams=0), dict(beams=65), dict(vocab=0), dict(k=0),
                                 dict(k=65), dict(vocab=1, logits_stride=1, k=5, eos_id=0), dict(vocab=1 << 29),
                                 dict(eos_id=1025), dict(eos_id=-1), dict(logits_dtype=3), dict(logits_stride=1024),
@@ -98,6 +117,7 @@ def test_beam_select_workspace(libpath):  # noqa: F811
 def test_null_argument_blocks(libpath):  # noqa: F811
     from paper_2410_13839_gb300 import _lib
     for call in (lambda: _lib.lib.mtp_page_plan(None, None), lambda: _lib.lib.mtp_cache_append(None, None),
+                 lambda: _lib.lib.mtp_chunk_attention(None, None, 0, None),
                  lambda: _lib.lib.mtp_beam_select(None, None, 0, None), lambda: _lib.lib.mtp_beam_reorder(None, None, 0, None)):
         assert call() == -1
     assert _lib.lib.mtp_beam_reorder_workspace_bytes(None) == 0
