@@ -26,7 +26,8 @@ struct ChunkArgs {
     long long q_stride, out_stride;
     int slots, rows, kv_heads, group, page_shift, bt_stride, n_pages;
     int page_blocks, layer_block;  // (layer, K | V, head) blocks of a page; the layer's first
-    int window, max_tiles, min_units, snap;
+    int window, max_tiles, min_units;
+    int snap;                      // items of at most 1 / snap of a share are not cut (0: all are)
     bool q_vec, out_vec;           // rows 16-byte aligned
     float scale_log2;              // scale * log2 e: scores in log2 units
     float* part;                   // [ctas][2][TR][dim + 2]
@@ -68,7 +69,7 @@ __device__ __forceinline__ ChunkTile chunk_tile(const ChunkArgs& a, int slot, in
 struct ChunkMap {
     int* slot_first;       // [slots + 1]: first tile of every slot
     uint32_t* unit_first;  // [tiles + 1]: first unit of every tile, counted for one key head
-    int tiles, ctas;
+    int tiles, ctas, snap;
     long long units;       // of all key heads
 };
 __host__ __device__ inline size_t chunk_map_bytes(int slots, int max_tiles) { return (size_t)(slots + max_tiles + 2) * 4; }
@@ -122,6 +123,7 @@ __device__ __forceinline__ ChunkMap chunk_map(const ChunkArgs& a, void* space, l
     __syncthreads();
     m.units = base * a.kv_heads;
     m.ctas = (int)min((long long)gridDim.x, max(1ll, (m.units + a.min_units - 1) / a.min_units));
+    m.snap = a.snap ? (int)min(m.units / m.ctas / a.snap, 1ll << 30) : 0;
     return m;
 }
 
@@ -151,22 +153,23 @@ __device__ __forceinline__ ChunkItem chunk_next(const ChunkArgs& a, const ChunkM
 __device__ __forceinline__ int chunk_slot_of(const ChunkArgs& a, const ChunkMap& m, int tile) {
     return chunk_owner(m.slot_first, a.slots, tile);
 }
-// First unit of CTA c's share.  Items of at most `snap` units are not cut: the border goes to
+// First unit of CTA c's share.  Items of at most m.snap units are not cut: the border goes to
 // their nearer end.
 __device__ __forceinline__ long long chunk_border(const ChunkArgs& a, const ChunkMap& m, int c) {
     const long long u = c >= m.ctas ? m.units : m.units * c / m.ctas;
-    if (u >= m.units || a.snap == 0) return u;
+    if (u >= m.units || m.snap == 0) return u;
     const ChunkItem x = chunk_item(a, m, u);
-    if (x.units > a.snap) return u;
+    if (x.units > m.snap) return u;
     return u - x.first <= x.units / 2 ? x.first : x.first + x.units;
 }
-// The CTA in whose share a unit of an uncut-able item lies (items above `snap` are cut at the plain borders)
+// The CTA in whose share a unit of an item above m.snap units lies (such items are cut at the plain borders)
 __device__ __forceinline__ int chunk_cta_of(const ChunkMap& m, long long unit) {
     return (int)(((unit + 1) * m.ctas - 1) / m.units);
 }
 
 constexpr int CH_DESC = 8;  // {CTAs after this one, first packed row, rows, first row of the slot, key head, -, -, -}
 
+cudaError_t launch_chunk_tc(const ChunkArgs& a, const CUtensorMap& map, int head_dim, int dtype, int ctas, cudaStream_t s);
 cudaError_t launch_chunk_merge(const ChunkArgs& a, int head_dim, int tile_rows, int dtype, int ctas, cudaStream_t s);
 
 }  // namespace mtp

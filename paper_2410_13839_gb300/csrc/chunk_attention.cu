@@ -31,7 +31,8 @@ int tc_encode_cache(CUtensorMap* map, const void* pool, int dtype, int head_dim,
 namespace {
 
 constexpr int FR_KEYS = 64, FR_WARPS = 5, FR_THREADS = FR_WARPS * 32, FR_CONSUMERS = 128;
-constexpr int CH_MIN_UNITS = 4;
+constexpr int FR_MIN_UNITS = 4, CT_MIN_UNITS = 2, CT_SNAP = 3;  // fewest units of a CTA
+constexpr int FR_MAX_ROWS = 32, CT_TILE_ROWS = 256, CT_UNIT_KEYS = 128;
 constexpr float LN2 = 0.69314718055994531f;
 
 __device__ __forceinline__ float ex2(float x) {
@@ -492,12 +493,9 @@ cudaError_t merge_hd(const ChunkArgs& a, int tile_rows, int ctas, cudaStream_t s
 
 // How a call runs: tile rows, CTAs, workspace.
 struct ChunkPlan {
-    int tile_rows, ctas, max_tiles;
+    int tile_rows, ctas, max_tiles, min_units;
     size_t desc_bytes, need;
 };
-
-template <int HD, int MT>
-constexpr int fr_per_sm() { return HD == 64 && MT == 1 ? 3 : 2; }
 
 int chunk_plan(const mtp_chunk_attention_args* a, ChunkPlan* p) {
     if (!a || a->slots < 1 || a->slots > CH_MAX_SLOTS || a->rows < 0 || a->n_heads < 1 || a->n_kv_heads < 1 ||
@@ -521,14 +519,17 @@ int chunk_plan(const mtp_chunk_attention_args* a, ChunkPlan* p) {
     }
     const int group = a->n_heads / a->n_kv_heads;
     const long long packed = (long long)std::min(a->max_new, a->rows) * group;  // rows of a slot and key head
-    p->tile_rows = packed <= 16 ? 16 : 32;
+    p->tile_rows = packed <= 16 ? 16 : packed <= FR_MAX_ROWS ? 32 : CT_TILE_ROWS;
+    const bool few = p->tile_rows != CT_TILE_ROWS;
     const long long tiles = std::min((long long)a->slots * ((packed + p->tile_rows - 1) / p->tile_rows),
                                      (long long)a->rows * group / p->tile_rows + a->slots);
-    if (tiles > CH_MAX_TILES) return invalid("chunk_attention: %lld tiles of %d rows, at most %d", tiles, p->tile_rows, CH_MAX_TILES);
+    if (tiles + a->slots > CH_MAX_TILES)
+        return invalid("chunk_attention: %lld tiles of %d rows in %d slots, at most %d together", tiles, p->tile_rows, a->slots, CH_MAX_TILES);
     p->max_tiles = (int)tiles;
-    const int per_sm = a->head_dim == 64 && p->tile_rows == 16 ? 3 : 2;
-    const long long units = tiles * a->n_kv_heads * std::max(1, (a->max_keys + FR_KEYS - 1) / FR_KEYS + 1);
-    p->ctas = (int)std::max(1ll, std::min((long long)sms * per_sm, (units + CH_MIN_UNITS - 1) / CH_MIN_UNITS));
+    const int per_sm = !few ? 1 : a->head_dim == 64 && p->tile_rows == 16 ? 3 : 2, keys = few ? FR_KEYS : CT_UNIT_KEYS;
+    p->min_units = few ? FR_MIN_UNITS : CT_MIN_UNITS;
+    const long long units = tiles * a->n_kv_heads * (a->max_keys / keys + 2);
+    p->ctas = (int)std::max(1ll, std::min((long long)sms * per_sm, (units + p->min_units - 1) / p->min_units));
     p->desc_bytes = ((size_t)p->ctas * CH_DESC * sizeof(int) + 255) & ~(size_t)255;
     p->need = p->desc_bytes + (size_t)p->ctas * 2 * p->tile_rows * (a->head_dim + 2) * sizeof(float);
     return MTP_OK;
@@ -601,7 +602,9 @@ MTP_API int mtp_chunk_attention(const mtp_chunk_attention_args* a, void* workspa
         c.bt_stride = a->bt_stride; c.n_pages = a->n_pages;
         c.page_blocks = a->layers * 2 * a->n_kv_heads;
         c.layer_block = a->layer * 2 * a->n_kv_heads;
-        c.window = a->window; c.max_tiles = p.max_tiles; c.min_units = CH_MIN_UNITS; c.snap = 0;
+        c.window = a->window; c.max_tiles = p.max_tiles; c.min_units = p.min_units;
+        const bool few = p.tile_rows != CT_TILE_ROWS;
+        c.snap = few ? 0 : CT_SNAP;
         c.q_vec = aligned16(a->q) && a->q_stride % 8 == 0;
         c.out_vec = aligned16(a->out) && a->out_stride % 8 == 0;
         c.scale_log2 = a->scale * 1.4426950408889634f;
@@ -611,10 +614,11 @@ MTP_API int mtp_chunk_attention(const mtp_chunk_attention_args* a, void* workspa
         const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
         CUtensorMap map;
         if (tc_encode_cache(&map, a->kv_pool, a->dtype, a->head_dim, a->page_size,
-                            (uint64_t)a->n_pages * c.page_blocks, std::min(a->page_size, FR_KEYS)) != 0)
+                            (uint64_t)a->n_pages * c.page_blocks, std::min(a->page_size, few ? FR_KEYS : CT_UNIT_KEYS)) != 0)
             return report_error(MTP_ERR_CUDA, "chunk_attention: cuTensorMapEncodeTiled failed");
-        cudaError_t e = a->dtype == MTP_BF16 ? launch_rows_of<Bf16>(c, map, a->head_dim, p, s)
-                                             : launch_rows_of<F16>(c, map, a->head_dim, p, s);
+        cudaError_t e = !few                    ? launch_chunk_tc(c, map, a->head_dim, a->dtype, p.ctas, s)
+                        : a->dtype == MTP_BF16 ? launch_rows_of<Bf16>(c, map, a->head_dim, p, s)
+                                               : launch_rows_of<F16>(c, map, a->head_dim, p, s);
         if (e == cudaSuccess) e = launch_chunk_merge(c, a->head_dim, p.tile_rows, a->dtype, p.ctas, s);
         return cuda_status(e, "chunk_attention");
     });

@@ -1,0 +1,527 @@
+// chunk_attention_tc.cu -- the kernel of mtp_chunk_attention for many rows per slot and key
+// head (prompts, chunks): tcgen05, one CTA per SM, shares of the unit stream (chunk.cuh) of
+// 256 packed rows by 128 keys.
+//
+//   S = Q K^T          128 x 128 fp32 in TMEM per tile of 128 rows, Q and K in shared memory
+//   P = 2^(c S - m)    a row per thread, written over S as 16-bit values (c = scale log2 e)
+//   O += P V           P read from TMEM, V as an MN-major operand, 128 x head_dim fp32 in TMEM
+//
+// A CTA has two tiles, A and B, of an item: while one's scores are in the hands of its four
+// softmax warps, the tensor cores work for the other.  The issuing warp's order is
+// PV_A(j) S_A(j+1) PV_B(j) S_B(j+1); it runs over the items of the share without a stop, as
+// does the ring of keys and values that the tenth warp fills with TMA copies, a lane per
+// page piece.  A tile skips the units of which its rows see no key.
+//
+// m is a row's reference, not its maximum: it moves only where the maximum passes it by more
+// than 8 (log2 units), so P stays below 2^8 and the output in TMEM is rescaled a few times per
+// row instead of once per unit.  The sum takes the weights before they are rounded, in fp32.
+// P is rounded once to the type: a second product with its residues would cost half as much
+// tensor time again, and the error (as large as the output's own rounding to 16 bits) is
+// within the type.  Q, K and V enter as they are.
+#include <algorithm>
+#include <type_traits>
+
+#include "chunk.cuh"
+#include "tcgen05.cuh"
+
+namespace mtp {
+namespace {
+
+constexpr int CT_ROWS = 256, CT_TILE = 128, CT_KEYS = 128;
+constexpr int CT_WARPS = 10, CT_THREADS = CT_WARPS * 32;  // two softmax groups of four, MMA, copies
+constexpr uint32_t CT_SUB = 128 * 128;                    // 128 rows of 128 bytes
+constexpr uint32_t TM_S = 0, TM_O = 256, TM_COLS = 512;   // tile t: S at 128 t, O at 256 + 128 t
+constexpr float LAG = 8.f;
+constexpr float LN2 = 0.69314718055994531f;
+
+template <int HD>
+struct CtLayout {
+    static constexpr int STAGES = HD == 64 ? 4 : 2;
+    static constexpr uint32_t OPER = CT_SUB * (HD / 64);  // a tile of Q, K or V
+    static constexpr uint32_t K = 2 * OPER, V = K + STAGES * OPER, MAP = V + STAGES * OPER;
+    static size_t bytes(int slots, int tiles) { return 1024 + MAP + chunk_map_bytes(slots, tiles); }
+};
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void tma_cache(void* dst, const CUtensorMap* map, int x, int row, int block, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+            smem_addr(dst)),
+        "l"(map), "r"(x), "r"(row), "r"(block), "r"(smem_addr(bar))
+        : "memory");
+}
+// D = A B (+ D), A (16-bit, K-major) in TMEM: lane = row, two K elements per column
+__device__ __forceinline__ void tc_mma_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(acc)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+        "%15, %16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// V's 128-byte-swizzled rows as an MN-major operand of HD columns: 64-column atoms CT_SUB apart
+__device__ __forceinline__ uint64_t v_desc(uint32_t saddr) {
+    uint64_t d = (uint64_t)((saddr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(CT_SUB >> 4) << 16;  // between 64-column atoms
+    d |= (uint64_t)(1024 >> 4) << 32;    // between groups of 8 keys
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+template <class T>
+constexpr uint32_t ct_idesc(int n, bool b_mn) {  // f16_idesc's types are bf16; fp16's codes are 0
+    return std::is_same<T, Bf16>::value ? f16_idesc(CT_TILE, n, b_mn) : f16_idesc(CT_TILE, n, b_mn) & ~((1u << 7) | (1u << 10));
+}
+
+// What a tile (0 or 1) of an item does in this CTA: its rows, and the units [from, to) of the
+// item, of those in [k0, k1), of which its rows see a key.
+struct CtTile {
+    int p0, rows, from, to;
+};
+__device__ __forceinline__ CtTile ct_tile(const ChunkArgs& a, const ChunkTile& t, int tile, int k0, int k1) {
+    CtTile x;
+    x.p0 = t.p0 + tile * CT_TILE;
+    x.rows = max(0, min(CT_TILE, t.rows - tile * CT_TILE));
+    x.from = x.to = k0;
+    if (x.rows == 0) return x;
+    const int first = t.len - t.n + x.p0 / a.group, last = t.len - t.n + (x.p0 + x.rows - 1) / a.group;
+    const int hi = max(0, last + 1), lo = a.window > 0 ? max(0, first - a.window + 1) : 0;
+    if (hi <= lo) return x;
+    x.from = max(k0, (lo - t.key0) / CT_KEYS);
+    x.to = max(x.from, min(k1, (hi - t.key0 + CT_KEYS - 1) / CT_KEYS));
+    return x;
+}
+
+// A walk over the units of a share.
+struct CtWalk {
+    ChunkItem it;
+    ChunkTile t;
+    int k0, k1;     // the item's units in the share
+    CtTile x[2];
+    __device__ __forceinline__ void load(const ChunkArgs& a, const ChunkMap& m, long long left) {
+        const int s = chunk_slot_of(a, m, it.tile);
+        t = chunk_tile<CT_ROWS, CT_KEYS>(a, s, it.tile - m.slot_first[s]);
+        k1 = (int)min((long long)it.units, k0 + left);
+        x[0] = ct_tile(a, t, 0, k0, k1);
+        x[1] = ct_tile(a, t, 1, k0, k1);
+    }
+    __device__ __forceinline__ bool active(int tile, int k) const { return k >= x[tile].from && k < x[tile].to; }
+};
+
+template <class T, int HD>
+__global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const ChunkArgs a, const __grid_constant__ CUtensorMap map) {
+    using L = CtLayout<HD>;
+    constexpr int ST = L::STAGES;
+    extern __shared__ unsigned char ct_raw[];
+    __shared__ uint64_t q_full[2], s_full[2], p_full[2], o_full[2], k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], drain;
+    __shared__ long long scan_part[CT_WARPS][2];
+    __shared__ uint32_t tmem_base;
+    unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(ct_raw) + 1023) & ~(uintptr_t)1023);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
+    if (warp == 8) {
+        tmem_alloc(&tmem_base, TM_COLS);
+        tmem_relinquish();
+    }
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&q_full[i], 4);
+            mbar_init(&s_full[i], 1);
+            mbar_init(&p_full[i], 4);
+            mbar_init(&o_full[i], 1);
+        }
+        for (int i = 0; i < ST; ++i) {
+            mbar_init(&k_full[i], 1);
+            mbar_init(&k_empty[i], 1);
+            mbar_init(&v_full[i], 1);
+            mbar_init(&v_empty[i], 1);
+        }
+        mbar_init(&drain, 1);
+        fence_barrier_init();
+        a.desc[cta * CH_DESC] = 0;
+    }
+    const ChunkMap m = chunk_map<CT_WARPS, CT_ROWS, CT_KEYS>(a, sm + L::MAP, scan_part);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_base;
+    pdl_launch_dependents();
+    const long long u0 = m.units && cta < m.ctas ? chunk_border(a, m, cta) : 0;
+    const long long u1 = m.units && cta < m.ctas ? chunk_border(a, m, cta + 1) : 0;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {  // one lane polls
+        return __all_sync(FULL_MASK, lane != 0 || mbar_wait(bar, parity & 1, a.err)) != 0;
+    };
+
+    if (u0 < u1) {
+        CtWalk w;
+        w.it = chunk_item(a, m, u0);
+        w.k0 = (int)(u0 - w.it.first);
+        w.load(a, m, u1 - u0);
+        if (warp == 9) {
+            // ---- copies: a lane per piece of a unit's keys (kv 0) and values (kv 1) ----
+            const int P = 1 << a.page_shift, box = min(P, CT_KEYS), per = CT_KEYS / box;
+            const int sub = lane % per, half = lane / per % (HD / 64), kv = lane / per / (HD / 64);
+            const uint32_t to = half * CT_SUB + sub * box * 128;
+            int k = w.k0, n = 0;
+            bool ok = true;
+            auto page_of = [&]() {  // -1 outside the pool (zeros), -2 where no row sees a key of it
+                const int key = w.t.key0 + k * CT_KEYS + sub * box;
+                if (kv > 1 || key >= w.t.hi || key + box <= w.t.lo) return -2;
+                const int page = __ldg(a.block_table + (size_t)w.t.slot * a.bt_stride + (key >> a.page_shift));
+                return page >= 0 && page < a.n_pages ? page : -1;
+            };
+            int page = page_of(), k_sent = 0, v_sent = 0;
+            for (long long u = u0; u < u1; ++u, ++n) {
+                const int st = n % ST, block = page < 0 ? -1 : page * a.page_blocks + a.layer_block + kv * a.kv_heads + w.it.head;
+                const unsigned have = __ballot_sync(FULL_MASK, page >= -1 && kv == 0);  // (the values' pieces are as many)
+                const uint32_t bytes = __popc(have) * box * 128;
+                if (n >= ST && !(ok = wait(&k_empty[st], n / ST - 1))) break;
+                if (lane == 0) mbar_arrive_expect_tx(&k_full[st], bytes);
+                __syncwarp();
+                if (kv == 0 && page >= -1) tma_cache(sm + L::K + st * L::OPER + to, &map, half * 64, 0, block, &k_full[st]);
+                ++k_sent;
+                if (n >= ST && !(ok = wait(&v_empty[st], n / ST - 1))) break;
+                if (lane == 0) mbar_arrive_expect_tx(&v_full[st], bytes);
+                __syncwarp();
+                if (kv == 1 && page >= -1) tma_cache(sm + L::V + st * L::OPER + to, &map, half * 64, 0, block, &v_full[st]);
+                ++v_sent;
+                if (++k == w.k1) {
+                    w.it = chunk_next(a, m, w.it);
+                    k = w.k0 = 0;
+                    if (u + 1 < u1) w.load(a, m, u1 - u - 1);
+                }
+                if (u + 1 < u1) page = page_of();
+            }
+            if (!ok && lane == 0) {  // what is in flight lands before the CTA leaves
+                for (int i = max(0, k_sent - ST); i < k_sent; ++i) mbar_wait(&k_full[i % ST], (uint32_t)(i / ST) & 1, nullptr);
+                for (int i = max(0, v_sent - ST); i < v_sent; ++i) mbar_wait(&v_full[i % ST], (uint32_t)(i / ST) & 1, nullptr);
+            }
+            __syncwarp();
+        } else if (warp == 8) {
+            // ---- MMAs ----
+            constexpr uint32_t IDESC_S = ct_idesc<T>(CT_KEYS, false), IDESC_O = ct_idesc<T>(HD, true);
+            int items[2] = {0, 0}, scores[2] = {0, 0};  // q_full and p_full phases waited for
+            bool ok = true;
+            auto issue_s = [&](int tile, int st) {
+                if (lane == 0) {
+                    const uint32_t q = smem_addr(sm + tile * L::OPER), kb = smem_addr(sm + L::K + st * L::OPER);
+#pragma unroll
+                    for (int d = 0; d < HD / 16; ++d) {
+                        const uint32_t at = (d >> 2) * CT_SUB + (d & 3) * 32;
+                        tc_mma(tmem + TM_S + tile * 128, sw128_desc(q + at), sw128_desc(kb + at), IDESC_S, d != 0);
+                    }
+                    tc_commit(&s_full[tile]);
+                }
+                __syncwarp();
+            };
+            // S of unit k of the walk (the n-th of the share), where the tile has it
+            auto scores_of = [&](int tile, int k, int n) {
+                if (!w.active(tile, k)) return;
+                if (k == w.x[tile].from) ok = ok && wait(&q_full[tile], items[tile]++);
+                ok = ok && wait(&k_full[n % ST], n / ST);
+                if (!ok) return;
+                tc_fence_after();
+                issue_s(tile, n % ST);
+            };
+            auto k_done = [&](int n) {
+                // (a unit of which no tile has a key is released all the same)
+                ok = ok && wait(&k_full[n % ST], n / ST);
+                if (ok && lane == 0) tc_commit(&k_empty[n % ST]);
+                __syncwarp();
+            };
+            int k = w.k0, n = 0;
+            scores_of(0, k, 0);
+            scores_of(1, k, 0);
+            k_done(0);
+            for (long long u = u0; ok && u < u1; ++u, ++n) {
+                const int st = n % ST;
+                const bool has[2] = {w.active(0, k), w.active(1, k)};
+                const bool first[2] = {k == w.x[0].from, k == w.x[1].from}, last[2] = {k + 1 == w.x[0].to, k + 1 == w.x[1].to};
+                // the walk goes on: what follows is the next unit's
+                if (++k == w.k1) {
+                    w.it = chunk_next(a, m, w.it);
+                    k = w.k0 = 0;
+                    if (u + 1 < u1) w.load(a, m, u1 - u - 1);
+                }
+#pragma unroll
+                for (int tile = 0; tile < 2; ++tile) {
+                    if (ok && has[tile]) {
+                        ok = wait(&p_full[tile], scores[tile]++) && wait(&v_full[st], n / ST);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (lane == 0) {
+                            const uint32_t vb = smem_addr(sm + L::V + st * L::OPER);
+#pragma unroll
+                            for (int d = 0; d < CT_KEYS / 16; ++d)
+                                tc_mma_ta(tmem + TM_O + tile * 128, tmem + TM_S + tile * 128 + d * 8, v_desc(vb + d * 2048), IDESC_O,
+                                          !(first[tile] && d == 0));
+                            if (last[tile]) tc_commit(&o_full[tile]);
+                        }
+                        __syncwarp();
+                    }
+                    if (tile == 1) {  // both tiles' products of this unit are on their way
+                        ok = ok && wait(&v_full[st], n / ST);
+                        if (ok && lane == 0) tc_commit(&v_empty[st]);
+                        __syncwarp();
+                    }
+                    if (ok && u + 1 < u1) scores_of(tile, k, n + 1);
+                }
+                if (ok && u + 1 < u1) k_done(n + 1);
+            }
+            if (lane == 0) {  // every MMA has ended before TMEM is given back
+                tc_commit(&drain);
+                mbar_wait(&drain, 0, a.err);
+            }
+            __syncwarp();
+        } else {
+            // ---- softmax: group g has tile g, a row per thread ----
+            const int g = warp >> 2, r = tid & 127;
+            const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), ts = lanes + TM_S + g * 128, to = lanes + TM_O + g * 128;
+            unsigned char* qs = sm + g * L::OPER;
+            const int heads = a.kv_heads * a.group;
+            int n = 0, s_seen = 0, o_seen = 0;
+            bool ok = true;
+            // Q of an item on its way into shared memory: 16 bytes a thread and step, rows past the tile zero
+            auto load_q = [&](const CtWalk& x) {
+                for (int i = r; i < CT_TILE * (HD / 8); i += 128) {
+                    const int row = i / (HD / 8), c = i % (HD / 8), p = x.x[g].p0 + row;
+                    unsigned char* dst = qs + (c >> 3) * CT_SUB + row * 128 + (((c & 7) ^ (row & 7)) << 4);
+                    const bool live = row < x.x[g].rows;
+                    const uint16_t* src = live ? a.q + (x.t.row0 + p / a.group) * a.q_stride + (x.it.head * a.group + p % a.group) * HD + c * 8 : a.q;
+                    if (a.q_vec) {
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(dst)), "l"(src), "r"(live ? 16 : 0) : "memory");
+                    } else {
+                        uint32_t v[4] = {0u, 0u, 0u, 0u};
+                        if (live)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) v[e] = (uint32_t)__ldg(src + 2 * e) | (uint32_t)__ldg(src + 2 * e + 1) << 16;
+                        *reinterpret_cast<uint4*>(dst) = make_uint4(v[0], v[1], v[2], v[3]);
+                    }
+                }
+            };
+            auto q_there = [&]() {
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&q_full[g]);
+            };
+            if (w.x[g].from < w.x[g].to) {
+                load_q(w);
+                q_there();
+            }
+            for (long long u = u0; u < u1;) {
+                const int len = w.k1 - w.k0;
+                const CtTile x = w.x[g];
+                const int pos = r < x.rows ? w.t.len - w.t.n + (x.p0 + r) / a.group : -1;
+                float ref = -INFINITY, sum = 0.f;
+                const bool more = u + len < u1;  // the share has an item after this one
+                bool q_next = false;             // whose Q this group has asked for
+                auto ask_q = [&]() {
+                    CtWalk next;
+                    next.it = chunk_next(a, m, w.it);
+                    next.k0 = 0;
+                    next.load(a, m, u1 - u - len);
+                    q_next = next.x[g].from < next.x[g].to;
+                    if (q_next) load_q(next);
+                };
+                for (int k = x.from; k < x.to; ++k) {
+                    const int key0 = w.t.key0 + k * CT_KEYS;
+                    if (ok) ok = wait(&s_full[g], s_seen);
+                    ++s_seen;
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (k + 1 == x.to && more) ask_q();  // the tile's last S is there: Q's space is free
+                    __syncwarp();
+                    float s[128];
+#pragma unroll
+                    for (int c = 0; c < 128; c += 32) tmem_ld_issue<32>(ts + c, *reinterpret_cast<float(*)[32]>(&s[c]));
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int c = 0; c < 128; c += 32) tmem_ld_done(*reinterpret_cast<float(*)[32]>(&s[c]));
+                    // columns (lowest, highest] of the unit are the keys that this row sees
+                    const int highest = pos - key0, lowest = a.window > 0 ? pos - a.window - key0 : -1;
+                    if (!__all_sync(FULL_MASK, highest >= CT_KEYS - 1 && lowest < 0)) {
+#pragma unroll
+                        for (int c = 0; c < 128; ++c) s[c] = c <= highest && c > lowest ? s[c] : -INFINITY;
+                    }
+                    float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+                    for (int c = 4; c < 128; ++c) mx[c & 3] = fmaxf(mx[c & 3], s[c]);
+                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
+                    const bool moves = top > ref + LAG;  // (from -inf: any value)
+                    if (__any_sync(FULL_MASK, moves)) {
+                        const float f = moves ? ex2(ref - top) : 1.f;
+                        if (moves) {
+                            ref = top;
+                            sum *= f;
+                        }
+                        __syncwarp();
+                        if (k > x.from) {  // the products so far are complete: this unit's S came after them
+#pragma unroll
+                            for (int c = 0; c < HD; c += 16) {
+                                float v[16];
+                                tmem_ld<16>(to + c, v);
+                                uint32_t y[16];
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(v[e] * f);
+                                tmem_st16(to + c, y);
+                            }
+                        }
+                    }
+                    const float base = ref == -INFINITY ? 0.f : ref;  // a row that has seen no key: every weight 0
+                    float2 acc[2] = {{0.f, 0.f}, {0.f, 0.f}};
+#pragma unroll
+                    for (int c = 0; c < 128; c += 32) {
+                        uint32_t y[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const float2 z = fma2(make_float2(s[c + 2 * e], s[c + 2 * e + 1]), make_float2(a.scale_log2, a.scale_log2),
+                                                  make_float2(-base, -base));
+                            const float2 p = make_float2(ex2(z.x), ex2(z.y));
+                            acc[e & 1] = add2(acc[e & 1], p);
+                            y[e] = T::pack(p.x, p.y);
+                        }
+                        tmem_st16(ts + c / 2, y);
+                    }
+                    sum += (acc[0].x + acc[0].y) + (acc[1].x + acc[1].y);
+                    // keys of the unit that no row of the item sees: whatever their values are, zeros in their place.  The
+                    // first tile that has the unit sees to it (the other's product comes after it).
+                    if ((g == 0 || !w.active(0, k)) && (key0 + CT_KEYS > w.t.hi || key0 < w.t.lo)) {
+                        ok = wait(&v_full[(n + k - w.k0) % ST], (n + k - w.k0) / ST);
+                        if (!ok) break;
+                        const int key = key0 + r;
+                        if (key >= w.t.hi || key < w.t.lo) {
+                            unsigned char* v = sm + L::V + (uint32_t)((n + k - w.k0) % ST) * L::OPER + r * 128;
+#pragma unroll
+                            for (int c = 0; c < HD / 8; ++c) *reinterpret_cast<uint4*>(v + (c >> 3) * CT_SUB + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        }
+                        fence_proxy_async();
+                    }
+                    __syncwarp();
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_full[g]);
+                }
+                if (!ok) break;
+                if (x.from >= x.to && more) ask_q();  // (nothing here: Q's space was free already)
+                if (q_next) q_there();
+                // ---- the item's rows ----
+                const bool any = x.from < x.to;
+                if (any) {
+                    ok = wait(&o_full[g], o_seen++);
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                const bool begins = w.k0 == 0, ends = w.k1 == w.it.units, whole = begins && ends;
+                const int p = x.p0 + r, head = w.it.head * a.group + p % a.group;
+                const long long row = w.t.row0 + p / a.group;
+                const bool live = r < x.rows;
+                const float f = sum == 0.f ? 0.f : 1.f / sum;  // (no key: 0)
+                float* part = a.part + ((size_t)cta * 2 + begins) * CT_ROWS * (HD + 2);
+#pragma unroll 1
+                for (int c = 0; c < HD; c += 32) {
+                    float v[32];
+                    __syncwarp();
+                    if (any) {
+                        tmem_ld32(to + c, v);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = 0.f;
+                    }
+                    if (!live) continue;
+                    if (whole) {
+                        uint16_t* dst = a.out + row * a.out_stride + head * HD + c;
+                        uint32_t y[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) y[e] = T::pack(sum == 0.f ? 0.f : v[2 * e] * f, sum == 0.f ? 0.f : v[2 * e + 1] * f);
+                        if (a.out_vec) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(dst)[e] = make_uint4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                dst[2 * e] = (uint16_t)y[e];
+                                dst[2 * e + 1] = (uint16_t)(y[e] >> 16);
+                            }
+                        }
+                    } else {
+                        float4* dst = reinterpret_cast<float4*>(part + (g * CT_TILE + r) * HD + c);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) dst[e] = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                    }
+                }
+                if (live && whole && a.lse) a.lse[row * heads + head] = sum == 0.f ? -INFINITY : LN2 * (ref + log2f(sum));
+                if (live && !whole) *reinterpret_cast<float2*>(part + CT_ROWS * HD + 2 * (g * CT_TILE + r)) = make_float2(ref, sum);
+                if (tid == 0 && begins && !ends) {
+                    int* d = a.desc + cta * CH_DESC;
+                    d[0] = chunk_cta_of(m, w.it.first + w.it.units - 1) - cta;
+                    d[1] = w.t.p0;
+                    d[2] = w.t.rows;
+                    d[3] = w.t.row0;
+                    d[4] = w.it.head;
+                }
+                tc_fence_before();  // O is read before the next item's product overwrites it
+                u += len;
+                n += len;
+                if (more) {
+                    w.it = chunk_next(a, m, w.it);
+                    w.k0 = 0;
+                    w.load(a, m, u1 - u);
+                }
+            }
+        }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) tmem_dealloc(tmem, TM_COLS);
+}
+
+template <class T, int HD>
+cudaError_t launch_tc(const ChunkArgs& a, const CUtensorMap& map, int ctas, cudaStream_t s) {
+    const size_t smem = CtLayout<HD>::bytes(a.slots, a.max_tiles);
+    const auto kern = chunk_tc_kernel<T, HD>;
+    const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem);
+    if (e != cudaSuccess) return e;
+    kern<<<ctas, CT_THREADS, smem, s>>>(a, map);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_chunk_tc(const ChunkArgs& a, const CUtensorMap& map, int head_dim, int dtype, int ctas, cudaStream_t s) {
+    if (dtype == MTP_BF16) return head_dim == 64 ? launch_tc<Bf16, 64>(a, map, ctas, s) : launch_tc<Bf16, 128>(a, map, ctas, s);
+    return head_dim == 64 ? launch_tc<F16, 64>(a, map, ctas, s) : launch_tc<F16, 128>(a, map, ctas, s);
+}
+
+}  // namespace mtp
