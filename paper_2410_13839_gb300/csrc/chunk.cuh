@@ -25,6 +25,7 @@ struct ChunkArgs {
     const int *block_table, *cu_rows, *kv_lens;
     long long q_stride, out_stride;
     int slots, rows, kv_heads, group, page_shift, bt_stride, n_pages;
+    uint32_t group_inv;            // ceil(2^32 / group)
     int page_blocks, layer_block;  // (layer, K | V, head) blocks of a page; the layer's first
     int window, max_tiles, min_units;
     int snap;                      // items of at most 1 / snap of a share are not cut (0: all are)
@@ -34,6 +35,21 @@ struct ChunkArgs {
     int* desc;                     // [ctas][8]
     int* err;
 };
+
+// Token of packed row p: p / group (p < 2^26: the product with the rounded-up inverse has the exact quotient)
+__device__ __forceinline__ int chunk_token(const ChunkArgs& a, int p) {
+    return a.group == 1 ? p : (int)__umulhi((uint32_t)p, a.group_inv);
+}
+
+// Bounded wait for a barrier's phase, as mbar_wait; one short loop, for kernels whose code has to stay
+// in the instruction cache.
+__device__ __forceinline__ bool chunk_wait(uint64_t* bar, uint32_t parity, int* err) {
+#pragma unroll 1
+    for (uint32_t i = 0; i < MBAR_MAX_POLLS; ++i)
+        if (mbar_try_wait(bar, parity & 1)) return true;
+    if (err) atomicOr(err, ERR_WAIT_TIMEOUT);
+    return false;
+}
 
 struct ChunkTile {
     int slot, row0, n, len;  // the slot, its first row, its new tokens, its length with them
@@ -58,7 +74,7 @@ __device__ __forceinline__ ChunkTile chunk_tile(const ChunkArgs& a, int slot, in
     x.len = max(0, min(a.kv_lens[slot], a.bt_stride << a.page_shift));
     x.p0 = t * TR;
     x.rows = min(x.n * a.group - x.p0, TR);
-    const int first = x.len - x.n + x.p0 / a.group, last = x.len - x.n + (x.p0 + x.rows - 1) / a.group;  // positions
+    const int first = x.len - x.n + chunk_token(a, x.p0), last = x.len - x.n + chunk_token(a, x.p0 + x.rows - 1);  // positions
     x.hi = max(0, last + 1);
     x.lo = a.window > 0 ? min(x.hi, max(0, first - a.window + 1)) : 0;
     x.key0 = x.lo / KT * KT;
@@ -132,7 +148,7 @@ struct ChunkItem {
     long long first;  // its first unit
     int units;
 };
-__device__ __forceinline__ ChunkItem chunk_item(const ChunkArgs& a, const ChunkMap& m, long long unit) {
+static __device__ __noinline__ ChunkItem chunk_item(const ChunkArgs& a, const ChunkMap& m, long long unit) {
     // unit < m.units: unit / kv_heads is a unit of one head
     ChunkItem x;
     x.tile = chunk_owner(m.unit_first, m.tiles, (uint32_t)(unit / a.kv_heads));
@@ -155,7 +171,7 @@ __device__ __forceinline__ int chunk_slot_of(const ChunkArgs& a, const ChunkMap&
 }
 // First unit of CTA c's share.  Items of at most m.snap units are not cut: the border goes to
 // their nearer end.
-__device__ __forceinline__ long long chunk_border(const ChunkArgs& a, const ChunkMap& m, int c) {
+static __device__ __noinline__ long long chunk_border(const ChunkArgs& a, const ChunkMap& m, int c) {
     const long long u = c >= m.ctas ? m.units : m.units * c / m.ctas;
     if (u >= m.units || m.snap == 0) return u;
     const ChunkItem x = chunk_item(a, m, u);

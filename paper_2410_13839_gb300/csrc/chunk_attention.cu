@@ -88,7 +88,7 @@ struct FrLayout {
 
 template <class T, int HD, int MT>
 __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
-    chunk_rows_kernel(const ChunkArgs a, const __grid_constant__ CUtensorMap map) {
+    chunk_rows_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ CUtensorMap map) {
     using L = FrLayout<HD, MT>;
     constexpr int TR = L::TR, ST = L::STAGES;
     extern __shared__ unsigned char fr_raw[];
@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
         for (long long u = u0; u < u1; ++u, ++issued) {
             const int st = issued % ST;
             if (issued >= ST) {
-                ok = __all_sync(FULL_MASK, lane != 0 || mbar_wait(&empty[st], (uint32_t)(issued / ST - 1) & 1, a.err));
+                ok = __all_sync(FULL_MASK, lane != 0 || chunk_wait(&empty[st], (uint32_t)(issued / ST - 1) & 1, a.err));
                 if (!ok) break;
             }
             const unsigned have = __ballot_sync(FULL_MASK, page != -2);
@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
         }
         // after a failed wait: what is in flight lands before the CTA leaves
         if (!ok && lane == 0)
-            for (int i = max(0, issued - ST); i < issued; ++i) mbar_wait(&full[i % ST], (uint32_t)(i / ST) & 1, nullptr);
+            for (int i = max(0, issued - ST); i < issued; ++i) chunk_wait(&full[i % ST], (uint32_t)(i / ST) & 1, nullptr);
         return;
     }
 
@@ -178,7 +178,8 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
             const int r = i / (HD / 8), c = i % (HD / 8), p = t.p0 + r;
             uint4 v = make_uint4(0u, 0u, 0u, 0u);
             if (r < t.rows) {
-                const uint16_t* src = a.q + (t.row0 + p / a.group) * a.q_stride + (it.head * a.group + p % a.group) * HD + c * 8;
+                const int token = chunk_token(a, p);
+                const uint16_t* src = a.q + (t.row0 + token) * a.q_stride + (it.head * a.group + p - token * a.group) * HD + c * 8;
                 if (a.q_vec) {
                     v = __ldg(reinterpret_cast<const uint4*>(src));
                 } else {
@@ -204,13 +205,13 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
                 mx[i][e] = -INFINITY;
                 sum[i][e] = 0.f;
                 const int r = i * 16 + r0 + e * 8;
-                pos[i][e] = r < t.rows ? t.len - t.n + (t.p0 + r) / a.group : -1;
+                pos[i][e] = r < t.rows ? t.len - t.n + chunk_token(a, t.p0 + r) : -1;
             }
         }
-        const int pos_first = t.len - t.n + t.p0 / a.group, pos_last = t.hi - 1;
+        const int pos_first = t.len - t.n + chunk_token(a, t.p0), pos_last = t.hi - 1;
         for (; k < k1; ++k, ++u) {
             const int st = stage % ST;
-            if (alive) alive = __all_sync(FULL_MASK, lane != 0 || mbar_wait(&full[st], (uint32_t)(stage / ST) & 1, a.err));
+            if (alive) alive = __all_sync(FULL_MASK, lane != 0 || chunk_wait(&full[st], (uint32_t)(stage / ST) & 1, a.err));
             const int key0 = t.key0 + k * FR_KEYS + warp * 16;  // this warp's keys
             if (alive && key0 < t.hi && key0 + 16 > t.lo) {
                 unsigned char* kb = sm + st * L::STAGE;
@@ -365,8 +366,8 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
                     for (int e = 0; e < 2; ++e) {
                         const int r = i * 16 + r0 + e * 8, p = t.p0 + r;
                         if (r >= t.rows) continue;
-                        const long long row = t.row0 + p / a.group;
-                        const int head = it.head * a.group + p % a.group;
+                        const int token = chunk_token(a, p), head = it.head * a.group + p - token * a.group;
+                        const long long row = t.row0 + token;
                         const float f = sum[i][e] == 0.f ? 0.f : 1.f / sum[i][e];  // (no key: 0)
                         uint16_t* to = a.out + row * a.out_stride + head * HD + c0;
 #pragma unroll
@@ -448,8 +449,8 @@ __global__ void __launch_bounds__(128) chunk_merge_kernel(const ChunkArgs a) {
             o[e + 1] = fmaf(f, v.y, o[e + 1]);
         }
     }
-    const int p = d[1] + r, head = d[4] * a.group + p % a.group;
-    const long long row = d[3] + p / a.group;
+    const int p = d[1] + r, token = chunk_token(a, p), head = d[4] * a.group + p - token * a.group;
+    const long long row = d[3] + token;
     const float f = sum == 0.f ? 0.f : 1.f / sum;
     uint16_t* to = a.out + row * a.out_stride + head * HD + lane * PER;
 #pragma unroll
@@ -598,6 +599,7 @@ MTP_API int mtp_chunk_attention(const mtp_chunk_attention_args* a, void* workspa
         c.block_table = a->block_table; c.cu_rows = a->cu_rows; c.kv_lens = a->kv_lens;
         c.q_stride = a->q_stride; c.out_stride = a->out_stride;
         c.slots = a->slots; c.rows = a->rows; c.kv_heads = a->n_kv_heads; c.group = group;
+        c.group_inv = group == 1 ? 0u : (uint32_t)(((1ull << 32) + group - 1) / group);
         c.page_shift = a->page_size == 16 ? 4 : a->page_size == 32 ? 5 : a->page_size == 64 ? 6 : 7;
         c.bt_stride = a->bt_stride; c.n_pages = a->n_pages;
         c.page_blocks = a->layers * 2 * a->n_kv_heads;

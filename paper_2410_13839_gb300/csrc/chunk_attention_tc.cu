@@ -30,7 +30,7 @@ namespace {
 constexpr int CT_ROWS = 256, CT_TILE = 128, CT_KEYS = 128;
 constexpr int CT_WARPS = 10, CT_THREADS = CT_WARPS * 32;  // two softmax groups of four, MMA, copies
 constexpr uint32_t CT_SUB = 128 * 128;                    // 128 rows of 128 bytes
-constexpr uint32_t TM_S = 0, TM_O = 256, TM_COLS = 512;   // tile t: S at 128 t, O at 256 + 128 t
+constexpr uint32_t TM_S = 0, TM_P = 64, TM_O = 256, TM_COLS = 512;  // tile t: S at 128 t, P in its upper half, O at 256 + 128 t
 constexpr float LAG = 8.f;
 constexpr float LN2 = 0.69314718055994531f;
 
@@ -72,6 +72,12 @@ __device__ __forceinline__ void tma_cache(void* dst, const CUtensorMap* map, int
         "l"(map), "r"(x), "r"(row), "r"(block), "r"(smem_addr(bar))
         : "memory");
 }
+// One thread of the (whole) warp, the same at every call.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
 // D = A B (+ D), A (16-bit, K-major) in TMEM: lane = row, two K elements per column
 __device__ __forceinline__ void tc_mma_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
     asm volatile(
@@ -108,13 +114,13 @@ constexpr uint32_t ct_idesc(int n, bool b_mn) {  // f16_idesc's types are bf16; 
 struct CtTile {
     int p0, rows, from, to;
 };
-__device__ __forceinline__ CtTile ct_tile(const ChunkArgs& a, const ChunkTile& t, int tile, int k0, int k1) {
+__device__ __noinline__ CtTile ct_tile(const ChunkArgs& a, const ChunkTile& t, int tile, int k0, int k1) {
     CtTile x;
     x.p0 = t.p0 + tile * CT_TILE;
     x.rows = max(0, min(CT_TILE, t.rows - tile * CT_TILE));
     x.from = x.to = k0;
     if (x.rows == 0) return x;
-    const int first = t.len - t.n + x.p0 / a.group, last = t.len - t.n + (x.p0 + x.rows - 1) / a.group;
+    const int first = t.len - t.n + chunk_token(a, x.p0), last = t.len - t.n + chunk_token(a, x.p0 + x.rows - 1);
     const int hi = max(0, last + 1), lo = a.window > 0 ? max(0, first - a.window + 1) : 0;
     if (hi <= lo) return x;
     x.from = max(k0, (lo - t.key0) / CT_KEYS);
@@ -122,24 +128,31 @@ __device__ __forceinline__ CtTile ct_tile(const ChunkArgs& a, const ChunkTile& t
     return x;
 }
 
-// A walk over the units of a share.
+// A walk over the items of a share: the item, and its units [k0, k1) in the share.
 struct CtWalk {
     ChunkItem it;
     ChunkTile t;
-    int k0, k1;     // the item's units in the share
-    CtTile x[2];
-    __device__ __forceinline__ void load(const ChunkArgs& a, const ChunkMap& m, long long left) {
+    int k0, k1;
+    __device__ __forceinline__ CtWalk(const ChunkArgs& a, const ChunkMap& m, long long u0, long long u1) {
+        it = chunk_item(a, m, u0);
+        k0 = (int)(u0 - it.first);
+        load(a, m, u1 - u0);
+    }
+    __device__ __noinline__ void load(const ChunkArgs& a, const ChunkMap& m, long long left) {
         const int s = chunk_slot_of(a, m, it.tile);
         t = chunk_tile<CT_ROWS, CT_KEYS>(a, s, it.tile - m.slot_first[s]);
         k1 = (int)min((long long)it.units, k0 + left);
-        x[0] = ct_tile(a, t, 0, k0, k1);
-        x[1] = ct_tile(a, t, 1, k0, k1);
     }
-    __device__ __forceinline__ bool active(int tile, int k) const { return k >= x[tile].from && k < x[tile].to; }
+    __device__ __forceinline__ void next(const ChunkArgs& a, const ChunkMap& m, long long left) {
+        it = chunk_next(a, m, it);
+        k0 = 0;
+        if (left > 0) load(a, m, left);
+    }
+    __device__ __forceinline__ CtTile tile(const ChunkArgs& a, int g) const { return ct_tile(a, t, g, k0, k1); }
 };
 
 template <class T, int HD>
-__global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const ChunkArgs a, const __grid_constant__ CUtensorMap map) {
+__global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ CUtensorMap map) {
     using L = CtLayout<HD>;
     constexpr int ST = L::STAGES;
     extern __shared__ unsigned char ct_raw[];
@@ -178,15 +191,12 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const ChunkArgs
     const long long u0 = m.units && cta < m.ctas ? chunk_border(a, m, cta) : 0;
     const long long u1 = m.units && cta < m.ctas ? chunk_border(a, m, cta + 1) : 0;
     auto wait = [&](uint64_t* bar, uint32_t parity) {  // one lane polls
-        return __all_sync(FULL_MASK, lane != 0 || mbar_wait(bar, parity & 1, a.err)) != 0;
+        return __all_sync(FULL_MASK, lane != 0 || chunk_wait(bar, parity, a.err)) != 0;
     };
 
     if (u0 < u1) {
-        CtWalk w;
-        w.it = chunk_item(a, m, u0);
-        w.k0 = (int)(u0 - w.it.first);
-        w.load(a, m, u1 - u0);
         if (warp == 9) {
+            CtWalk w(a, m, u0, u1);
             // ---- copies: a lane per piece of a unit's keys (kv 0) and values (kv 1) ----
             const int P = 1 << a.page_shift, box = min(P, CT_KEYS), per = CT_KEYS / box;
             const int sub = lane % per, half = lane / per % (HD / 64), kv = lane / per / (HD / 64);
@@ -215,108 +225,111 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const ChunkArgs
                 if (kv == 1 && page >= -1) tma_cache(sm + L::V + st * L::OPER + to, &map, half * 64, 0, block, &v_full[st]);
                 ++v_sent;
                 if (++k == w.k1) {
-                    w.it = chunk_next(a, m, w.it);
-                    k = w.k0 = 0;
-                    if (u + 1 < u1) w.load(a, m, u1 - u - 1);
+                    w.next(a, m, u1 - u - 1);
+                    k = 0;
                 }
                 if (u + 1 < u1) page = page_of();
             }
             if (!ok && lane == 0) {  // what is in flight lands before the CTA leaves
-                for (int i = max(0, k_sent - ST); i < k_sent; ++i) mbar_wait(&k_full[i % ST], (uint32_t)(i / ST) & 1, nullptr);
-                for (int i = max(0, v_sent - ST); i < v_sent; ++i) mbar_wait(&v_full[i % ST], (uint32_t)(i / ST) & 1, nullptr);
+                for (int i = max(0, k_sent - ST); i < k_sent; ++i) chunk_wait(&k_full[i % ST], i / ST, nullptr);
+                for (int i = max(0, v_sent - ST); i < v_sent; ++i) chunk_wait(&v_full[i % ST], i / ST, nullptr);
             }
             __syncwarp();
         } else if (warp == 8) {
-            // ---- MMAs ----
-            constexpr uint32_t IDESC_S = ct_idesc<T>(CT_KEYS, false), IDESC_O = ct_idesc<T>(HD, true);
-            int items[2] = {0, 0}, scores[2] = {0, 0};  // q_full and p_full phases waited for
-            bool ok = true;
-            auto issue_s = [&](int tile, int st) {
-                if (lane == 0) {
-                    const uint32_t q = smem_addr(sm + tile * L::OPER), kb = smem_addr(sm + L::K + st * L::OPER);
+            // ---- MMAs, all by one thread ----
+            if (elect_one()) {
+                constexpr uint32_t IDESC_S = ct_idesc<T>(CT_KEYS, false), IDESC_O = ct_idesc<T>(HD, true);
+                CtWalk w(a, m, u0, u1);
+                CtTile x0 = w.tile(a, 0), x1 = w.tile(a, 1);
+                int items0 = 0, items1 = 0, scores0 = 0, scores1 = 0;  // q_full and p_full phases waited for
+                bool ok = true;
+                auto await = [&](uint64_t* bar, uint32_t phase) { ok = ok && chunk_wait(bar, phase, a.err); };
+                // S of unit k of the walk, whose keys are in stage st, where the tile has it
+                auto scores_of = [&](int tile, const CtTile& x, int& items, int k, int st) {
+                    if (k < x.from || k >= x.to) return;
+                    if (k == x.from) await(&q_full[tile], items++);
+                    if (!ok) return;
+                    tc_fence_after();
+                    const uint64_t q = sw128_desc(smem_addr(sm + tile * L::OPER)), kd = sw128_desc(smem_addr(sm + L::K + st * L::OPER));
 #pragma unroll
                     for (int d = 0; d < HD / 16; ++d) {
-                        const uint32_t at = (d >> 2) * CT_SUB + (d & 3) * 32;
-                        tc_mma(tmem + TM_S + tile * 128, sw128_desc(q + at), sw128_desc(kb + at), IDESC_S, d != 0);
+                        const uint32_t at = ((d >> 2) * CT_SUB + (d & 3) * 32) >> 4;
+                        tc_mma(tmem + TM_S + tile * 128, q + at, kd + at, IDESC_S, d != 0);
                     }
                     tc_commit(&s_full[tile]);
-                }
-                __syncwarp();
-            };
-            // S of unit k of the walk (the n-th of the share), where the tile has it
-            auto scores_of = [&](int tile, int k, int n) {
-                if (!w.active(tile, k)) return;
-                if (k == w.x[tile].from) ok = ok && wait(&q_full[tile], items[tile]++);
-                ok = ok && wait(&k_full[n % ST], n / ST);
-                if (!ok) return;
-                tc_fence_after();
-                issue_s(tile, n % ST);
-            };
-            auto k_done = [&](int n) {
-                // (a unit of which no tile has a key is released all the same)
-                ok = ok && wait(&k_full[n % ST], n / ST);
-                if (ok && lane == 0) tc_commit(&k_empty[n % ST]);
-                __syncwarp();
-            };
-            int k = w.k0, n = 0;
-            scores_of(0, k, 0);
-            scores_of(1, k, 0);
-            k_done(0);
-            for (long long u = u0; ok && u < u1; ++u, ++n) {
-                const int st = n % ST;
-                const bool has[2] = {w.active(0, k), w.active(1, k)};
-                const bool first[2] = {k == w.x[0].from, k == w.x[1].from}, last[2] = {k + 1 == w.x[0].to, k + 1 == w.x[1].to};
-                // the walk goes on: what follows is the next unit's
-                if (++k == w.k1) {
-                    w.it = chunk_next(a, m, w.it);
-                    k = w.k0 = 0;
-                    if (u + 1 < u1) w.load(a, m, u1 - u - 1);
-                }
+                };
+                // O += P V of the unit whose values are in stage st
+                auto product = [&](int tile, const CtTile& x, int& scores, int k, int st) {
+                    if (k < x.from || k >= x.to) return;
+                    await(&p_full[tile], scores++);
+                    if (!ok) return;
+                    tc_fence_after();
+                    const uint64_t v = v_desc(smem_addr(sm + L::V + st * L::OPER));
 #pragma unroll
-                for (int tile = 0; tile < 2; ++tile) {
-                    if (ok && has[tile]) {
-                        ok = wait(&p_full[tile], scores[tile]++) && wait(&v_full[st], n / ST);
-                        if (!ok) break;
-                        tc_fence_after();
-                        if (lane == 0) {
-                            const uint32_t vb = smem_addr(sm + L::V + st * L::OPER);
-#pragma unroll
-                            for (int d = 0; d < CT_KEYS / 16; ++d)
-                                tc_mma_ta(tmem + TM_O + tile * 128, tmem + TM_S + tile * 128 + d * 8, v_desc(vb + d * 2048), IDESC_O,
-                                          !(first[tile] && d == 0));
-                            if (last[tile]) tc_commit(&o_full[tile]);
+                    for (int d = 0; d < CT_KEYS / 16; ++d)
+                        tc_mma_ta(tmem + TM_O + tile * 128, tmem + TM_S + tile * 128 + TM_P + d * 8, v + d * (2048 >> 4), IDESC_O,
+                                  d != 0 || k != x.from);
+                    if (k + 1 == x.to) tc_commit(&o_full[tile]);
+                };
+                int k = w.k0;
+                CtTile y0 = x0, y1 = x1;  // the unit before's
+                // step n: the products of unit n - 1, between them the scores of unit n
+                for (int n = 0, units = (int)(u1 - u0); ok && n <= units; ++n) {
+                    const int st = n % ST, before = (n + ST - 1) % ST, last = k - 1;
+                    const bool more = n < units;
+                    int at = last;  // the unit before, in its item
+                    if (n > 0 && k == w.k1) {
+                        at = w.k1 - 1;
+                        w.next(a, m, units - n);
+                        k = 0;
+                        if (more) {
+                            x0 = w.tile(a, 0);
+                            x1 = w.tile(a, 1);
                         }
-                        __syncwarp();
                     }
-                    if (tile == 1) {  // both tiles' products of this unit are on their way
-                        ok = ok && wait(&v_full[st], n / ST);
-                        if (ok && lane == 0) tc_commit(&v_empty[st]);
-                        __syncwarp();
+                    if (n > 0) {
+                        await(&v_full[before], (n - 1) / ST);
+                        product(0, y0, scores0, at, before);
                     }
-                    if (ok && u + 1 < u1) scores_of(tile, k, n + 1);
+                    if (more) {
+                        await(&k_full[st], n / ST);
+                        scores_of(0, x0, items0, k, st);
+                    }
+                    if (n > 0) {
+                        product(1, y1, scores1, at, before);
+                        if (ok) tc_commit(&v_empty[before]);
+                    }
+                    if (more) {
+                        scores_of(1, x1, items1, k, st);
+                        if (ok) tc_commit(&k_empty[st]);
+                    }
+                    y0 = x0;
+                    y1 = x1;
+                    ++k;
                 }
-                if (ok && u + 1 < u1) k_done(n + 1);
-            }
-            if (lane == 0) {  // every MMA has ended before TMEM is given back
-                tc_commit(&drain);
-                mbar_wait(&drain, 0, a.err);
+                tc_commit(&drain);  // every MMA has ended before TMEM is given back
+                chunk_wait(&drain, 0, a.err);
             }
             __syncwarp();
-        } else {
+        } else if (warp < 8) {
             // ---- softmax: group g has tile g, a row per thread ----
             const int g = warp >> 2, r = tid & 127;
             const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), ts = lanes + TM_S + g * 128, to = lanes + TM_O + g * 128;
             unsigned char* qs = sm + g * L::OPER;
             const int heads = a.kv_heads * a.group;
+            CtWalk w(a, m, u0, u1);
+            CtTile x = w.tile(a, g);
             int n = 0, s_seen = 0, o_seen = 0;
             bool ok = true;
             // Q of an item on its way into shared memory: 16 bytes a thread and step, rows past the tile zero
-            auto load_q = [&](const CtWalk& x) {
+            auto load_q = [&](const CtWalk& w, const CtTile& x) {
+#pragma unroll 1
                 for (int i = r; i < CT_TILE * (HD / 8); i += 128) {
-                    const int row = i / (HD / 8), c = i % (HD / 8), p = x.x[g].p0 + row;
+                    const int row = i / (HD / 8), c = i % (HD / 8), p = x.p0 + row;
                     unsigned char* dst = qs + (c >> 3) * CT_SUB + row * 128 + (((c & 7) ^ (row & 7)) << 4);
-                    const bool live = row < x.x[g].rows;
-                    const uint16_t* src = live ? a.q + (x.t.row0 + p / a.group) * a.q_stride + (x.it.head * a.group + p % a.group) * HD + c * 8 : a.q;
+                    const bool live = row < x.rows;
+                    const int token = chunk_token(a, p);
+                    const uint16_t* src = live ? a.q + (w.t.row0 + token) * a.q_stride + (w.it.head * a.group + p - token * a.group) * HD + c * 8 : a.q;
                     if (a.q_vec) {
                         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(dst)), "l"(src), "r"(live ? 16 : 0) : "memory");
                     } else {
@@ -334,24 +347,26 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const ChunkArgs
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&q_full[g]);
             };
-            if (w.x[g].from < w.x[g].to) {
-                load_q(w);
+            if (x.from < x.to) {
+                load_q(w, x);
                 q_there();
             }
             for (long long u = u0; u < u1;) {
                 const int len = w.k1 - w.k0;
-                const CtTile x = w.x[g];
-                const int pos = r < x.rows ? w.t.len - w.t.n + (x.p0 + r) / a.group : -1;
+                const int pos = r < x.rows ? w.t.len - w.t.n + chunk_token(a, x.p0 + r) : -1;
                 float ref = -INFINITY, sum = 0.f;
                 const bool more = u + len < u1;  // the share has an item after this one
                 bool q_next = false;             // whose Q this group has asked for
+                auto first_has = [&](int k) {  // the first tile has unit k too
+                    const CtTile y = w.tile(a, 0);
+                    return k >= y.from && k < y.to;
+                };
                 auto ask_q = [&]() {
-                    CtWalk next;
-                    next.it = chunk_next(a, m, w.it);
-                    next.k0 = 0;
-                    next.load(a, m, u1 - u - len);
-                    q_next = next.x[g].from < next.x[g].to;
-                    if (q_next) load_q(next);
+                    CtWalk next = w;
+                    next.next(a, m, u1 - u - len);
+                    const CtTile y = next.tile(a, g);
+                    q_next = y.from < y.to;
+                    if (q_next) load_q(next, y);
                 };
                 for (int k = x.from; k < x.to; ++k) {
                     const int key0 = w.t.key0 + k * CT_KEYS;
@@ -361,21 +376,34 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const ChunkArgs
                     tc_fence_after();
                     if (k + 1 == x.to && more) ask_q();  // the tile's last S is there: Q's space is free
                     __syncwarp();
-                    float s[128];
-#pragma unroll
-                    for (int c = 0; c < 128; c += 32) tmem_ld_issue<32>(ts + c, *reinterpret_cast<float(*)[32]>(&s[c]));
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int c = 0; c < 128; c += 32) tmem_ld_done(*reinterpret_cast<float(*)[32]>(&s[c]));
                     // columns (lowest, highest] of the unit are the keys that this row sees
                     const int highest = pos - key0, lowest = a.window > 0 ? pos - a.window - key0 : -1;
-                    if (!__all_sync(FULL_MASK, highest >= CT_KEYS - 1 && lowest < 0)) {
+                    const bool inner = __all_sync(FULL_MASK, highest >= CT_KEYS - 1 && lowest < 0);
+                    // 32 scores at a time, for the maximum and then for the weights: the upper half stays in registers, the
+                    // lower is read again while the upper's weights are made
+                    float s0[32], s1[32];
+                    auto mask = [&](float (&x)[32], int c0) {
+                        if (!inner) {
 #pragma unroll
-                        for (int c = 0; c < 128; ++c) s[c] = c <= highest && c > lowest ? s[c] : -INFINITY;
+                            for (int c = 0; c < 32; ++c) x[c] = c0 + c <= highest && c0 + c > lowest ? x[c] : -INFINITY;
+                        }
+                    };
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    auto peak = [&](float (&x)[32], int c0) {
+                        mask(x, c0);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], x[e]);
+                    };
+#pragma unroll 1
+                    for (int c = 0; c < 128; c += 64) {
+                        tmem_ld_issue<32>(ts + c, s0);
+                        tmem_ld_issue<32>(ts + c + 32, s1);
+                        tmem_ld_wait();
+                        tmem_ld_done(s0);
+                        tmem_ld_done(s1);
+                        peak(s0, c);
+                        peak(s1, c + 32);
                     }
-                    float mx[4] = {s[0], s[1], s[2], s[3]};
-#pragma unroll
-                    for (int c = 4; c < 128; ++c) mx[c & 3] = fmaxf(mx[c & 3], s[c]);
                     const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
                     const bool moves = top > ref + LAG;  // (from -inf: any value)
                     if (__any_sync(FULL_MASK, moves)) {
@@ -386,7 +414,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const ChunkArgs
                         }
                         __syncwarp();
                         if (k > x.from) {  // the products so far are complete: this unit's S came after them
-#pragma unroll
+#pragma unroll 1
                             for (int c = 0; c < HD; c += 16) {
                                 float v[16];
                                 tmem_ld<16>(to + c, v);
@@ -399,23 +427,37 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const ChunkArgs
                     }
                     const float base = ref == -INFINITY ? 0.f : ref;  // a row that has seen no key: every weight 0
                     float2 acc[2] = {{0.f, 0.f}, {0.f, 0.f}};
-#pragma unroll
-                    for (int c = 0; c < 128; c += 32) {
+                    auto weights = [&](float (&x)[32], int c0) {
                         uint32_t y[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            const float2 z = fma2(make_float2(s[c + 2 * e], s[c + 2 * e + 1]), make_float2(a.scale_log2, a.scale_log2),
+                            const float2 z = fma2(make_float2(x[2 * e], x[2 * e + 1]), make_float2(a.scale_log2, a.scale_log2),
                                                   make_float2(-base, -base));
                             const float2 p = make_float2(ex2(z.x), ex2(z.y));
                             acc[e & 1] = add2(acc[e & 1], p);
                             y[e] = T::pack(p.x, p.y);
                         }
-                        tmem_st16(ts + c / 2, y);
+                        tmem_st16(ts + TM_P + c0 / 2, y);
+                    };
+                    // upper half, then lower (P lies over the upper half's scores, which are all in registers)
+#pragma unroll 1
+                    for (int c = 64; c >= 0; c -= 64) {
+                        weights(s0, c);
+                        if (c) tmem_ld_issue<32>(ts, s0);
+                        weights(s1, c + 32);
+                        if (c) {
+                            tmem_ld_issue<32>(ts + 32, s1);
+                            tmem_ld_wait();
+                            tmem_ld_done(s0);
+                            tmem_ld_done(s1);
+                            mask(s0, 0);
+                            mask(s1, 32);
+                        }
                     }
                     sum += (acc[0].x + acc[0].y) + (acc[1].x + acc[1].y);
                     // keys of the unit that no row of the item sees: whatever their values are, zeros in their place.  The
                     // first tile that has the unit sees to it (the other's product comes after it).
-                    if ((g == 0 || !w.active(0, k)) && (key0 + CT_KEYS > w.t.hi || key0 < w.t.lo)) {
+                    if ((key0 + CT_KEYS > w.t.hi || key0 < w.t.lo) && (g == 0 || !first_has(k))) {
                         ok = wait(&v_full[(n + k - w.k0) % ST], (n + k - w.k0) / ST);
                         if (!ok) break;
                         const int key = key0 + r;
@@ -443,8 +485,8 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const ChunkArgs
                     tc_fence_after();
                 }
                 const bool begins = w.k0 == 0, ends = w.k1 == w.it.units, whole = begins && ends;
-                const int p = x.p0 + r, head = w.it.head * a.group + p % a.group;
-                const long long row = w.t.row0 + p / a.group;
+                const int p = x.p0 + r, token = chunk_token(a, p), head = w.it.head * a.group + p - token * a.group;
+                const long long row = w.t.row0 + token;
                 const bool live = r < x.rows;
                 const float f = sum == 0.f ? 0.f : 1.f / sum;  // (no key: 0)
                 float* part = a.part + ((size_t)cta * 2 + begins) * CT_ROWS * (HD + 2);
@@ -493,11 +535,8 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const ChunkArgs
                 tc_fence_before();  // O is read before the next item's product overwrites it
                 u += len;
                 n += len;
-                if (more) {
-                    w.it = chunk_next(a, m, w.it);
-                    w.k0 = 0;
-                    w.load(a, m, u1 - u);
-                }
+                w.next(a, m, u1 - u);
+                if (more) x = w.tile(a, g);
             }
         }
     }
