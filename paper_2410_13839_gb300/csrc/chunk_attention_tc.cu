@@ -2,15 +2,21 @@
 // head (prompts, chunks): tcgen05, one CTA per SM, shares of the unit stream (chunk.cuh) of
 // 256 packed rows by 128 keys.
 //
-//   S = Q K^T          128 x 128 fp32 in TMEM per tile of 128 rows, Q and K in shared memory
+//   S = Q K^T          128 x 64 fp32 in TMEM per tile of 128 rows and step of 64 keys
 //   P = 2^(c S - m)    a row per thread, written over S as 16-bit values (c = scale log2 e)
 //   O += P V           P read from TMEM, V as an MN-major operand, 128 x head_dim fp32 in TMEM
 //
-// A CTA has two tiles, A and B, of an item: while one's scores are in the hands of its four
-// softmax warps, the tensor cores work for the other.  The issuing warp's order is
-// PV_A(j) S_A(j+1) PV_B(j) S_B(j+1); it runs over the items of the share without a stop, as
-// does the ring of keys and values that the tenth warp fills with TMA copies, a lane per
-// page piece.  A tile skips the units of which its rows see no key.
+// A CTA has two tiles, A and B, of an item, each with four softmax warps and two places for S:
+// while a step's scores are in the hands of the softmax, the tensor cores make the next
+// step's and work for the other tile, so that the softmax warps go from step to step without
+// waiting.  (With one place of 128 keys a tile's softmax and MMAs took turns: 4500 cycles per
+// 128 keys, of which the MMAs fill 2048.  The price of N = 64 is its Q, read per 64 keys:
+// 45 cycles per MMA where 32 would do.)  One thread issues all MMAs; it runs over the items of
+// the share without a stop, as does the ring of keys and values that the tenth warp fills
+// with TMA copies, a lane per page piece.  A tile skips the steps of which its rows see no key.
+//
+// Code size matters: with everything unrolled and inlined (190 KB) the warps waited for
+// instructions, 10,000 cycles per 128 keys.
 //
 // m is a row's reference, not its maximum: it moves only where the maximum passes it by more
 // than 8 (log2 units), so P stays below 2^8 and the output in TMEM is rescaled a few times per
@@ -30,7 +36,8 @@ namespace {
 constexpr int CT_ROWS = 256, CT_TILE = 128, CT_KEYS = 128;
 constexpr int CT_WARPS = 10, CT_THREADS = CT_WARPS * 32;  // two softmax groups of four, MMA, copies
 constexpr uint32_t CT_SUB = 128 * 128;                    // 128 rows of 128 bytes
-constexpr uint32_t TM_S = 0, TM_P = 64, TM_O = 256, TM_COLS = 512;  // tile t: S at 128 t, P in its upper half, O at 256 + 128 t
+constexpr int CT_STEP = 64;  // keys of a step: the scores that a thread holds
+constexpr uint32_t TM_S = 0, TM_O = 256, TM_COLS = 512;  // tile t, step s: S at 128 t + 64 (s & 1), O at 256 + 128 t
 constexpr float LAG = 8.f;
 constexpr float LN2 = 0.69314718055994531f;
 
@@ -109,8 +116,8 @@ constexpr uint32_t ct_idesc(int n, bool b_mn) {  // f16_idesc's types are bf16; 
     return std::is_same<T, Bf16>::value ? f16_idesc(CT_TILE, n, b_mn) : f16_idesc(CT_TILE, n, b_mn) & ~((1u << 7) | (1u << 10));
 }
 
-// What a tile (0 or 1) of an item does in this CTA: its rows, and the units [from, to) of the
-// item, of those in [k0, k1), of which its rows see a key.
+// What a tile (0 or 1) of an item does in this CTA: its rows, and the steps [from, to) of the
+// item (two to a unit), of those of units [k0, k1), of which its rows see a key.
 struct CtTile {
     int p0, rows, from, to;
 };
@@ -118,13 +125,13 @@ __device__ __noinline__ CtTile ct_tile(const ChunkArgs& a, const ChunkTile& t, i
     CtTile x;
     x.p0 = t.p0 + tile * CT_TILE;
     x.rows = max(0, min(CT_TILE, t.rows - tile * CT_TILE));
-    x.from = x.to = k0;
+    x.from = x.to = 2 * k0;
     if (x.rows == 0) return x;
     const int first = t.len - t.n + chunk_token(a, x.p0), last = t.len - t.n + chunk_token(a, x.p0 + x.rows - 1);
     const int hi = max(0, last + 1), lo = a.window > 0 ? max(0, first - a.window + 1) : 0;
     if (hi <= lo) return x;
-    x.from = max(k0, (lo - t.key0) / CT_KEYS);
-    x.to = max(x.from, min(k1, (hi - t.key0 + CT_KEYS - 1) / CT_KEYS));
+    x.from = max(2 * k0, (lo - t.key0) / CT_STEP);
+    x.to = max(x.from, min(2 * k1, (hi - t.key0 + CT_STEP - 1) / CT_STEP));
     return x;
 }
 
@@ -156,7 +163,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
     using L = CtLayout<HD>;
     constexpr int ST = L::STAGES;
     extern __shared__ unsigned char ct_raw[];
-    __shared__ uint64_t q_full[2], s_full[2], p_full[2], o_full[2], k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], drain;
+    __shared__ uint64_t q_full[2], s_full[2][2], p_full[2][2], pv_done[2][2], k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], drain;
     __shared__ long long scan_part[CT_WARPS][2];
     __shared__ uint32_t tmem_base;
     unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(ct_raw) + 1023) & ~(uintptr_t)1023);
@@ -168,9 +175,11 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(&q_full[i], 4);
-            mbar_init(&s_full[i], 1);
-            mbar_init(&p_full[i], 4);
-            mbar_init(&o_full[i], 1);
+            for (int h = 0; h < 2; ++h) {
+                mbar_init(&s_full[i][h], 1);
+                mbar_init(&p_full[i][h], 4);
+                mbar_init(&pv_done[i][h], 1);
+            }
         }
         for (int i = 0; i < ST; ++i) {
             mbar_init(&k_full[i], 1);
@@ -238,48 +247,48 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
         } else if (warp == 8) {
             // ---- MMAs, all by one thread ----
             if (elect_one()) {
-                constexpr uint32_t IDESC_S = ct_idesc<T>(CT_KEYS, false), IDESC_O = ct_idesc<T>(HD, true);
+                constexpr uint32_t IDESC_S = ct_idesc<T>(CT_STEP, false), IDESC_O = ct_idesc<T>(HD, true);
                 CtWalk w(a, m, u0, u1);
                 CtTile x0 = w.tile(a, 0), x1 = w.tile(a, 1);
-                int items0 = 0, items1 = 0, scores0 = 0, scores1 = 0;  // q_full and p_full phases waited for
+                int items[2] = {0, 0}, weights[2][2] = {{0, 0}, {0, 0}};  // q_full and p_full phases waited for
                 bool ok = true;
                 auto await = [&](uint64_t* bar, uint32_t phase) { ok = ok && chunk_wait(bar, phase, a.err); };
-                // S of unit k of the walk, whose keys are in stage st, where the tile has it
-                auto scores_of = [&](int tile, const CtTile& x, int& items, int k, int st) {
-                    if (k < x.from || k >= x.to) return;
-                    if (k == x.from) await(&q_full[tile], items++);
+                // S of a step (number `step` of the item), whose keys are in stage st, where the tile has it
+                auto scores_of = [&](int tile, int half, const CtTile& x, int step, int st) {
+                    if (step < x.from || step >= x.to) return;
+                    if (step == x.from) await(&q_full[tile], items[tile]++);
                     if (!ok) return;
                     tc_fence_after();
-                    const uint64_t q = sw128_desc(smem_addr(sm + tile * L::OPER)), kd = sw128_desc(smem_addr(sm + L::K + st * L::OPER));
+                    const uint64_t q = sw128_desc(smem_addr(sm + tile * L::OPER));
+                    const uint64_t kd = sw128_desc(smem_addr(sm + L::K + st * L::OPER + half * (CT_STEP * 128)));
 #pragma unroll
                     for (int d = 0; d < HD / 16; ++d) {
                         const uint32_t at = ((d >> 2) * CT_SUB + (d & 3) * 32) >> 4;
-                        tc_mma(tmem + TM_S + tile * 128, q + at, kd + at, IDESC_S, d != 0);
+                        tc_mma(tmem + TM_S + tile * 128 + half * 64, q + at, kd + at, IDESC_S, d != 0);
                     }
-                    tc_commit(&s_full[tile]);
+                    tc_commit(&s_full[tile][half]);
                 };
-                // O += P V of the unit whose values are in stage st
-                auto product = [&](int tile, const CtTile& x, int& scores, int k, int st) {
-                    if (k < x.from || k >= x.to) return;
-                    await(&p_full[tile], scores++);
+                // O += P V of a step whose values are in stage st
+                auto product = [&](int tile, int half, const CtTile& x, int step, int st) {
+                    if (step < x.from || step >= x.to) return;
+                    await(&p_full[tile][half], weights[tile][half]++);
                     if (!ok) return;
                     tc_fence_after();
-                    const uint64_t v = v_desc(smem_addr(sm + L::V + st * L::OPER));
+                    const uint64_t v = v_desc(smem_addr(sm + L::V + st * L::OPER + half * (CT_STEP * 128)));
 #pragma unroll
-                    for (int d = 0; d < CT_KEYS / 16; ++d)
-                        tc_mma_ta(tmem + TM_O + tile * 128, tmem + TM_S + tile * 128 + TM_P + d * 8, v + d * (2048 >> 4), IDESC_O,
-                                  d != 0 || k != x.from);
-                    if (k + 1 == x.to) tc_commit(&o_full[tile]);
+                    for (int d = 0; d < CT_STEP / 16; ++d)
+                        tc_mma_ta(tmem + TM_O + tile * 128, tmem + TM_S + tile * 128 + half * 64 + d * 8, v + d * (2048 >> 4), IDESC_O,
+                                  d != 0 || step != x.from);
+                    tc_commit(&pv_done[tile][half]);
                 };
                 int k = w.k0;
                 CtTile y0 = x0, y1 = x1;  // the unit before's
-                // step n: the products of unit n - 1, between them the scores of unit n
+                // the products of unit n - 1, between them the scores of unit n: a tile's S of a step comes after its
+                // P V of two steps before, in whose place it goes, and its softmax has the step between to work on
                 for (int n = 0, units = (int)(u1 - u0); ok && n <= units; ++n) {
-                    const int st = n % ST, before = (n + ST - 1) % ST, last = k - 1;
+                    const int st = n % ST, before = (n + ST - 1) % ST, at = k - 1;
                     const bool more = n < units;
-                    int at = last;  // the unit before, in its item
                     if (n > 0 && k == w.k1) {
-                        at = w.k1 - 1;
                         w.next(a, m, units - n);
                         k = 0;
                         if (more) {
@@ -287,22 +296,17 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                             x1 = w.tile(a, 1);
                         }
                     }
-                    if (n > 0) {
-                        await(&v_full[before], (n - 1) / ST);
-                        product(0, y0, scores0, at, before);
+                    if (n > 0) await(&v_full[before], (n - 1) / ST);
+                    if (more) await(&k_full[st], n / ST);
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        if (n > 0) product(0, half, y0, 2 * at + half, before);
+                        if (more) scores_of(0, half, x0, 2 * k + half, st);
+                        if (n > 0) product(1, half, y1, 2 * at + half, before);
+                        if (more) scores_of(1, half, x1, 2 * k + half, st);
                     }
-                    if (more) {
-                        await(&k_full[st], n / ST);
-                        scores_of(0, x0, items0, k, st);
-                    }
-                    if (n > 0) {
-                        product(1, y1, scores1, at, before);
-                        if (ok) tc_commit(&v_empty[before]);
-                    }
-                    if (more) {
-                        scores_of(1, x1, items1, k, st);
-                        if (ok) tc_commit(&k_empty[st]);
-                    }
+                    if (ok && n > 0) tc_commit(&v_empty[before]);
+                    if (ok && more) tc_commit(&k_empty[st]);
                     y0 = x0;
                     y1 = x1;
                     ++k;
@@ -319,7 +323,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
             const int heads = a.kv_heads * a.group;
             CtWalk w(a, m, u0, u1);
             CtTile x = w.tile(a, g);
-            int n = 0, s_seen = 0, o_seen = 0;
+            int n = 0, seen[2] = {0, 0};  // steps of either half, which s_full and pv_done count too
             bool ok = true;
             // Q of an item on its way into shared memory: 16 bytes a thread and step, rows past the tile zero
             auto load_q = [&](const CtWalk& w, const CtTile& x) {
@@ -357,9 +361,9 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                 float ref = -INFINITY, sum = 0.f;
                 const bool more = u + len < u1;  // the share has an item after this one
                 bool q_next = false;             // whose Q this group has asked for
-                auto first_has = [&](int k) {  // the first tile has unit k too
+                auto first_has = [&](int step) {  // the first tile has the step too
                     const CtTile y = w.tile(a, 0);
-                    return k >= y.from && k < y.to;
+                    return step >= y.from && step < y.to;
                 };
                 auto ask_q = [&]() {
                     CtWalk next = w;
@@ -368,41 +372,38 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                     q_next = y.from < y.to;
                     if (q_next) load_q(next, y);
                 };
-                for (int k = x.from; k < x.to; ++k) {
-                    const int key0 = w.t.key0 + k * CT_KEYS;
-                    if (ok) ok = wait(&s_full[g], s_seen);
-                    ++s_seen;
+#pragma unroll 1
+                for (int step = x.from; step < x.to; ++step) {
+                    const int key0 = w.t.key0 + step * CT_STEP, half = step & 1;
+                    const uint32_t tsh = ts + half * 64;
+                    if (ok) ok = wait(&s_full[g][half], half ? seen[1]++ : seen[0]++);
                     if (!ok) break;
                     tc_fence_after();
-                    if (k + 1 == x.to && more) ask_q();  // the tile's last S is there: Q's space is free
-                    __syncwarp();
-                    // columns (lowest, highest] of the unit are the keys that this row sees
-                    const int highest = pos - key0, lowest = a.window > 0 ? pos - a.window - key0 : -1;
-                    const bool inner = __all_sync(FULL_MASK, highest >= CT_KEYS - 1 && lowest < 0);
-                    // 32 scores at a time, for the maximum and then for the weights: the upper half stays in registers, the
-                    // lower is read again while the upper's weights are made
                     float s0[32], s1[32];
-                    auto mask = [&](float (&x)[32], int c0) {
-                        if (!inner) {
+                    tmem_ld_issue<32>(tsh, s0);
+                    tmem_ld_issue<32>(tsh + 32, s1);
+                    if (step + 1 == x.to && more) ask_q();  // the tile's last S is there: Q's space is free
+                    __syncwarp();
+                    // columns (lowest, highest] of the step are the keys that this row sees
+                    const int highest = pos - key0, lowest = a.window > 0 ? pos - a.window - key0 : -1;
+                    const bool inner = __all_sync(FULL_MASK, highest >= CT_STEP - 1 && lowest < 0);
+                    tmem_ld_wait();
+                    tmem_ld_done(s0);
+                    tmem_ld_done(s1);
+                    if (!inner) {
 #pragma unroll
-                            for (int c = 0; c < 32; ++c) x[c] = c0 + c <= highest && c0 + c > lowest ? x[c] : -INFINITY;
+                        for (int c = 0; c < 32; ++c) {
+                            s0[c] = c <= highest && c > lowest ? s0[c] : -INFINITY;
+                            s1[c] = c + 32 <= highest && c + 32 > lowest ? s1[c] : -INFINITY;
                         }
-                    };
+                    }
                     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                    auto peak = [&](float (&x)[32], int c0) {
-                        mask(x, c0);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], x[e]);
-                    };
-#pragma unroll 1
-                    for (int c = 0; c < 128; c += 64) {
-                        tmem_ld_issue<32>(ts + c, s0);
-                        tmem_ld_issue<32>(ts + c + 32, s1);
-                        tmem_ld_wait();
-                        tmem_ld_done(s0);
-                        tmem_ld_done(s1);
-                        peak(s0, c);
-                        peak(s1, c + 32);
+                    for (int c = 0; c < 32; c += 2) {
+                        mx[0] = fmaxf(mx[0], s0[c]);
+                        mx[1] = fmaxf(mx[1], s0[c + 1]);
+                        mx[2] = fmaxf(mx[2], s1[c]);
+                        mx[3] = fmaxf(mx[3], s1[c + 1]);
                     }
                     const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
                     const bool moves = top > ref + LAG;  // (from -inf: any value)
@@ -413,7 +414,10 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                             sum *= f;
                         }
                         __syncwarp();
-                        if (k > x.from) {  // the products so far are complete: this unit's S came after them
+                        if (step > x.from) {  // the product before is complete, the next one waits for this step's weights
+                            ok = wait(&pv_done[g][half ^ 1], (half ? seen[0] : seen[1]) - 1);
+                            if (!ok) break;
+                            tc_fence_after();
 #pragma unroll 1
                             for (int c = 0; c < HD; c += 16) {
                                 float v[16];
@@ -427,7 +431,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                     }
                     const float base = ref == -INFINITY ? 0.f : ref;  // a row that has seen no key: every weight 0
                     float2 acc[2] = {{0.f, 0.f}, {0.f, 0.f}};
-                    auto weights = [&](float (&x)[32], int c0) {
+                    auto weights = [&](const float (&x)[32], uint32_t at) {  // over S, which is all in registers
                         uint32_t y[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
@@ -437,34 +441,22 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                             acc[e & 1] = add2(acc[e & 1], p);
                             y[e] = T::pack(p.x, p.y);
                         }
-                        tmem_st16(ts + TM_P + c0 / 2, y);
+                        tmem_st16(at, y);
                     };
-                    // upper half, then lower (P lies over the upper half's scores, which are all in registers)
-#pragma unroll 1
-                    for (int c = 64; c >= 0; c -= 64) {
-                        weights(s0, c);
-                        if (c) tmem_ld_issue<32>(ts, s0);
-                        weights(s1, c + 32);
-                        if (c) {
-                            tmem_ld_issue<32>(ts + 32, s1);
-                            tmem_ld_wait();
-                            tmem_ld_done(s0);
-                            tmem_ld_done(s1);
-                            mask(s0, 0);
-                            mask(s1, 32);
-                        }
-                    }
+                    weights(s0, tsh);
+                    weights(s1, tsh + 16);
                     sum += (acc[0].x + acc[0].y) + (acc[1].x + acc[1].y);
-                    // keys of the unit that no row of the item sees: whatever their values are, zeros in their place.  The
-                    // first tile that has the unit sees to it (the other's product comes after it).
-                    if ((key0 + CT_KEYS > w.t.hi || key0 < w.t.lo) && (g == 0 || !first_has(k))) {
-                        ok = wait(&v_full[(n + k - w.k0) % ST], (n + k - w.k0) / ST);
+                    // keys of the step that no row of the item sees: whatever their values are, zeros in their place.  The
+                    // first tile that has the step sees to it (the other's product comes after it).
+                    if ((key0 + CT_STEP > w.t.hi || key0 < w.t.lo) && (g == 0 || !first_has(step))) {
+                        const int unit = n + (step >> 1) - w.k0;
+                        ok = wait(&v_full[unit % ST], unit / ST);
                         if (!ok) break;
-                        const int key = key0 + r;
+                        const int row = r & (CT_STEP - 1), key = key0 + row;
                         if (key >= w.t.hi || key < w.t.lo) {
-                            unsigned char* v = sm + L::V + (uint32_t)((n + k - w.k0) % ST) * L::OPER + r * 128;
-#pragma unroll
-                            for (int c = 0; c < HD / 8; ++c) *reinterpret_cast<uint4*>(v + (c >> 3) * CT_SUB + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                            unsigned char* v = sm + L::V + (uint32_t)(unit % ST) * L::OPER + (half * CT_STEP + row) * 128;
+                            for (int c = r / CT_STEP; c < HD / 8; c += 128 / CT_STEP)
+                                *reinterpret_cast<uint4*>(v + (c >> 3) * CT_SUB + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                         }
                         fence_proxy_async();
                     }
@@ -472,7 +464,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                     tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&p_full[g]);
+                    if (lane == 0) mbar_arrive(&p_full[g][half]);
                 }
                 if (!ok) break;
                 if (x.from >= x.to && more) ask_q();  // (nothing here: Q's space was free already)
@@ -480,7 +472,8 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                 // ---- the item's rows ----
                 const bool any = x.from < x.to;
                 if (any) {
-                    ok = wait(&o_full[g], o_seen++);
+                    const int half = (x.to - 1) & 1;
+                    ok = wait(&pv_done[g][half], (half ? seen[1] : seen[0]) - 1);
                     if (!ok) break;
                     tc_fence_after();
                 }
