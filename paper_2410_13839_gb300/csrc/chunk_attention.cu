@@ -616,7 +616,7 @@ MTP_API int mtp_chunk_attention(const mtp_chunk_attention_args* a, void* workspa
         const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
         CUtensorMap map;
         if (tc_encode_cache(&map, a->kv_pool, a->dtype, a->head_dim, a->page_size,
-                            (uint64_t)a->n_pages * c.page_blocks, std::min(a->page_size, few ? FR_KEYS : CT_UNIT_KEYS)) != 0)
+                            (uint64_t)a->n_pages * c.page_blocks, std::min(a->page_size, FR_KEYS)) != 0)
             return report_error(MTP_ERR_CUDA, "chunk_attention: cuTensorMapEncodeTiled failed");
         cudaError_t e = !few                    ? launch_chunk_tc(c, map, a->head_dim, a->dtype, p.ctas, s)
                         : a->dtype == MTP_BF16 ? launch_rows_of<Bf16>(c, map, a->head_dim, p, s)

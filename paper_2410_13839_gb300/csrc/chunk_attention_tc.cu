@@ -11,9 +11,11 @@
 // step's and work for the other tile, so that the softmax warps go from step to step without
 // waiting.  (With one place of 128 keys a tile's softmax and MMAs took turns: 4500 cycles per
 // 128 keys, of which the MMAs fill 2048.  The price of N = 64 is its Q, read per 64 keys:
-// 45 cycles per MMA where 32 would do.)  One thread issues all MMAs; it runs over the items of
-// the share without a stop, as does the ring of keys and values that the tenth warp fills
-// with TMA copies, a lane per page piece.  A tile skips the steps of which its rows see no key.
+// 45 cycles per MMA where 32 would do.)  A tile's MMAs are issued by a thread of its own: one
+// for both spent more time on its waits and branches (about 175 cycles for a barrier that is
+// complete) than the MMAs took.  The issuing threads run over the items of the share without
+// a stop, as does the ring of keys and values that the tenth warp fills with TMA copies, a
+// lane per page piece.  A tile skips the steps of which its rows see no key.
 //
 // Code size matters: with everything unrolled and inlined (190 KB) the warps waited for
 // instructions, 10,000 cycles per 128 keys.
@@ -34,7 +36,7 @@ namespace mtp {
 namespace {
 
 constexpr int CT_ROWS = 256, CT_TILE = 128, CT_KEYS = 128;
-constexpr int CT_WARPS = 10, CT_THREADS = CT_WARPS * 32;  // two softmax groups of four, MMA, copies
+constexpr int CT_WARPS = 12, CT_THREADS = CT_WARPS * 32;  // two softmax groups of four, MMAs of A, copies, MMAs of B, -
 constexpr uint32_t CT_SUB = 128 * 128;                    // 128 rows of 128 bytes
 constexpr int CT_STEP = 64;  // keys of a step: the scores that a thread holds
 constexpr uint32_t TM_S = 0, TM_O = 256, TM_COLS = 512;  // tile t, step s: S at 128 t + 64 (s & 1), O at 256 + 128 t
@@ -43,9 +45,10 @@ constexpr float LN2 = 0.69314718055994531f;
 
 template <int HD>
 struct CtLayout {
-    static constexpr int STAGES = HD == 64 ? 4 : 2;
-    static constexpr uint32_t OPER = CT_SUB * (HD / 64);  // a tile of Q, K or V
-    static constexpr uint32_t K = 2 * OPER, V = K + STAGES * OPER, MAP = V + STAGES * OPER;
+    static constexpr int STAGES = HD == 64 ? 8 : 4;       // of K and of V, 64 keys each
+    static constexpr uint32_t OPER = CT_SUB * (HD / 64);  // a tile of Q
+    static constexpr uint32_t ATOM = CT_STEP * 128, STEP = ATOM * (HD / 64);  // 64 columns of a stage; a stage
+    static constexpr uint32_t K = 2 * OPER, V = K + STAGES * STEP, MAP = V + STAGES * STEP;
     static size_t bytes(int slots, int tiles) { return 1024 + MAP + chunk_map_bytes(slots, tiles); }
 };
 
@@ -102,10 +105,10 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// V's 128-byte-swizzled rows as an MN-major operand of HD columns: 64-column atoms CT_SUB apart
-__device__ __forceinline__ uint64_t v_desc(uint32_t saddr) {
+// V's 128-byte-swizzled rows as an MN-major operand: 64-column atoms `atom` bytes apart
+__device__ __forceinline__ uint64_t v_desc(uint32_t saddr, uint32_t atom) {
     uint64_t d = (uint64_t)((saddr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)(CT_SUB >> 4) << 16;  // between 64-column atoms
+    d |= (uint64_t)(atom >> 4) << 16;    // between 64-column atoms
     d |= (uint64_t)(1024 >> 4) << 32;    // between groups of 8 keys
     d |= (uint64_t)1 << 46;
     d |= (uint64_t)2 << 61;
@@ -163,7 +166,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
     using L = CtLayout<HD>;
     constexpr int ST = L::STAGES;
     extern __shared__ unsigned char ct_raw[];
-    __shared__ uint64_t q_full[2], s_full[2][2], p_full[2][2], pv_done[2][2], k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], drain;
+    __shared__ uint64_t q_full[2], s_full[2][2], p_full[2][2], pv_done[2][2], k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], drain[2];
     __shared__ long long scan_part[CT_WARPS][2];
     __shared__ uint32_t tmem_base;
     unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(ct_raw) + 1023) & ~(uintptr_t)1023);
@@ -174,6 +177,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
     }
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
+            mbar_init(&drain[i], 1);
             mbar_init(&q_full[i], 4);
             for (int h = 0; h < 2; ++h) {
                 mbar_init(&s_full[i][h], 1);
@@ -183,11 +187,10 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
         }
         for (int i = 0; i < ST; ++i) {
             mbar_init(&k_full[i], 1);
-            mbar_init(&k_empty[i], 1);
+            mbar_init(&k_empty[i], 2);  // both tiles' MMAs
             mbar_init(&v_full[i], 1);
-            mbar_init(&v_empty[i], 1);
+            mbar_init(&v_empty[i], 2);
         }
-        mbar_init(&drain, 1);
         fence_barrier_init();
         a.desc[cta * CH_DESC] = 0;
     }
@@ -207,112 +210,108 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
         if (warp == 9) {
             CtWalk w(a, m, u0, u1);
             // ---- copies: a lane per piece of a unit's keys (kv 0) and values (kv 1) ----
-            const int P = 1 << a.page_shift, box = min(P, CT_KEYS), per = CT_KEYS / box;
+            const int P = 1 << a.page_shift, box = min(P, CT_STEP), per = CT_STEP / box;
             const int sub = lane % per, half = lane / per % (HD / 64), kv = lane / per / (HD / 64);
-            const uint32_t to = half * CT_SUB + sub * box * 128;
-            int k = w.k0, n = 0;
+            const uint32_t to = half * L::ATOM + sub * box * 128;
+            int step = 2 * w.k0, n = 0;
             bool ok = true;
             auto page_of = [&]() {  // -1 outside the pool (zeros), -2 where no row sees a key of it
-                const int key = w.t.key0 + k * CT_KEYS + sub * box;
+                const int key = w.t.key0 + step * CT_STEP + sub * box;
                 if (kv > 1 || key >= w.t.hi || key + box <= w.t.lo) return -2;
                 const int page = __ldg(a.block_table + (size_t)w.t.slot * a.bt_stride + (key >> a.page_shift));
                 return page >= 0 && page < a.n_pages ? page : -1;
             };
             int page = page_of(), k_sent = 0, v_sent = 0;
-            for (long long u = u0; u < u1; ++u, ++n) {
+            for (const int steps = 2 * (int)(u1 - u0); n < steps; ++n) {
                 const int st = n % ST, block = page < 0 ? -1 : page * a.page_blocks + a.layer_block + kv * a.kv_heads + w.it.head;
+                const int row = (w.t.key0 + step * CT_STEP + sub * box) & (P - 1);
                 const unsigned have = __ballot_sync(FULL_MASK, page >= -1 && kv == 0);  // (the values' pieces are as many)
                 const uint32_t bytes = __popc(have) * box * 128;
                 if (n >= ST && !(ok = wait(&k_empty[st], n / ST - 1))) break;
                 if (lane == 0) mbar_arrive_expect_tx(&k_full[st], bytes);
                 __syncwarp();
-                if (kv == 0 && page >= -1) tma_cache(sm + L::K + st * L::OPER + to, &map, half * 64, 0, block, &k_full[st]);
+                if (kv == 0 && page >= -1) tma_cache(sm + L::K + st * L::STEP + to, &map, half * 64, row, block, &k_full[st]);
                 ++k_sent;
                 if (n >= ST && !(ok = wait(&v_empty[st], n / ST - 1))) break;
                 if (lane == 0) mbar_arrive_expect_tx(&v_full[st], bytes);
                 __syncwarp();
-                if (kv == 1 && page >= -1) tma_cache(sm + L::V + st * L::OPER + to, &map, half * 64, 0, block, &v_full[st]);
+                if (kv == 1 && page >= -1) tma_cache(sm + L::V + st * L::STEP + to, &map, half * 64, row, block, &v_full[st]);
                 ++v_sent;
-                if (++k == w.k1) {
-                    w.next(a, m, u1 - u - 1);
-                    k = 0;
+                if (++step == 2 * w.k1) {
+                    w.next(a, m, u1 - u0 - (n + 1) / 2);
+                    step = 0;
                 }
-                if (u + 1 < u1) page = page_of();
+                if (n + 1 < steps) page = page_of();
             }
             if (!ok && lane == 0) {  // what is in flight lands before the CTA leaves
                 for (int i = max(0, k_sent - ST); i < k_sent; ++i) chunk_wait(&k_full[i % ST], i / ST, nullptr);
                 for (int i = max(0, v_sent - ST); i < v_sent; ++i) chunk_wait(&v_full[i % ST], i / ST, nullptr);
             }
             __syncwarp();
-        } else if (warp == 8) {
-            // ---- MMAs, all by one thread ----
+        } else if (warp == 8 || warp == 10) {
+            // ---- MMAs of a tile, by one thread ----
             if (elect_one()) {
                 constexpr uint32_t IDESC_S = ct_idesc<T>(CT_STEP, false), IDESC_O = ct_idesc<T>(HD, true);
+                const int tile = warp == 10;
                 CtWalk w(a, m, u0, u1);
-                CtTile x0 = w.tile(a, 0), x1 = w.tile(a, 1);
-                int items[2] = {0, 0}, weights[2][2] = {{0, 0}, {0, 0}};  // q_full and p_full phases waited for
+                CtTile x = w.tile(a, tile), y = x;  // y: the unit before's
+                const uint64_t q = sw128_desc(smem_addr(sm + tile * L::OPER)), k0 = sw128_desc(smem_addr(sm + L::K)),
+                               v0 = v_desc(smem_addr(sm + L::V), L::ATOM);
+                const uint32_t s_tmem = tmem + TM_S + tile * 128, o_tmem = tmem + TM_O + tile * 128;
+                uint32_t q_phase = 0, p_phase[2] = {0, 0};
                 bool ok = true;
                 auto await = [&](uint64_t* bar, uint32_t phase) { ok = ok && chunk_wait(bar, phase, a.err); };
-                // S of a step (number `step` of the item), whose keys are in stage st, where the tile has it
-                auto scores_of = [&](int tile, int half, const CtTile& x, int step, int st) {
-                    if (step < x.from || step >= x.to) return;
-                    if (step == x.from) await(&q_full[tile], items[tile]++);
-                    if (!ok) return;
-                    tc_fence_after();
-                    const uint64_t q = sw128_desc(smem_addr(sm + tile * L::OPER));
-                    const uint64_t kd = sw128_desc(smem_addr(sm + L::K + st * L::OPER + half * (CT_STEP * 128)));
-#pragma unroll
-                    for (int d = 0; d < HD / 16; ++d) {
-                        const uint32_t at = ((d >> 2) * CT_SUB + (d & 3) * 32) >> 4;
-                        tc_mma(tmem + TM_S + tile * 128 + half * 64, q + at, kd + at, IDESC_S, d != 0);
-                    }
-                    tc_commit(&s_full[tile][half]);
-                };
-                // O += P V of a step whose values are in stage st
-                auto product = [&](int tile, int half, const CtTile& x, int step, int st) {
-                    if (step < x.from || step >= x.to) return;
-                    await(&p_full[tile][half], weights[tile][half]++);
-                    if (!ok) return;
-                    tc_fence_after();
-                    const uint64_t v = v_desc(smem_addr(sm + L::V + st * L::OPER + half * (CT_STEP * 128)));
-#pragma unroll
-                    for (int d = 0; d < CT_STEP / 16; ++d)
-                        tc_mma_ta(tmem + TM_O + tile * 128, tmem + TM_S + tile * 128 + half * 64 + d * 8, v + d * (2048 >> 4), IDESC_O,
-                                  d != 0 || step != x.from);
-                    tc_commit(&pv_done[tile][half]);
-                };
                 int k = w.k0;
-                CtTile y0 = x0, y1 = x1;  // the unit before's
-                // the products of unit n - 1, between them the scores of unit n: a tile's S of a step comes after its
-                // P V of two steps before, in whose place it goes, and its softmax has the step between to work on
+                // the products of the steps of unit n - 1, between them the scores of unit n's: S of a step comes after
+                // the P V of two steps before, in whose place it goes, and the softmax has the step between to work on
                 for (int n = 0, units = (int)(u1 - u0); ok && n <= units; ++n) {
-                    const int st = n % ST, before = (n + ST - 1) % ST, at = k - 1;
+                    const int at = k - 1;
                     const bool more = n < units;
                     if (n > 0 && k == w.k1) {
                         w.next(a, m, units - n);
                         k = 0;
-                        if (more) {
-                            x0 = w.tile(a, 0);
-                            x1 = w.tile(a, 1);
-                        }
+                        if (more) x = w.tile(a, tile);
                     }
-                    if (n > 0) await(&v_full[before], (n - 1) / ST);
-                    if (more) await(&k_full[st], n / ST);
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        if (n > 0) product(0, half, y0, 2 * at + half, before);
-                        if (more) scores_of(0, half, x0, 2 * k + half, st);
-                        if (n > 0) product(1, half, y1, 2 * at + half, before);
-                        if (more) scores_of(1, half, x1, 2 * k + half, st);
+                        const int i = 2 * n + half, st = i % ST, before = (i + ST - 2) % ST;
+                        if (n > 0) {
+                            const int step = 2 * at + half;
+                            await(&v_full[before], (i - 2) / ST);
+                            if (step >= y.from && step < y.to) {  // O += P V
+                                await(&p_full[tile][half], p_phase[half]++);
+                                if (!ok) break;
+                                tc_fence_after();
+                                const uint64_t v = v0 + before * (L::STEP >> 4);
+#pragma unroll
+                                for (int d = 0; d < CT_STEP / 16; ++d)
+                                    tc_mma_ta(o_tmem, s_tmem + half * 64 + d * 8, v + d * (2048 >> 4), IDESC_O, d != 0 || step != y.from);
+                                tc_commit(&pv_done[tile][half]);
+                            }
+                            tc_commit(&v_empty[before]);
+                        }
+                        if (more) {
+                            const int step = 2 * k + half;
+                            await(&k_full[st], i / ST);
+                            if (step >= x.from && step < x.to) {  // S = Q K^T
+                                if (step == x.from) await(&q_full[tile], q_phase++);
+                                if (!ok) break;
+                                tc_fence_after();
+                                const uint64_t kd = k0 + st * (L::STEP >> 4);
+#pragma unroll
+                                for (int d = 0; d < HD / 16; ++d)
+                                    tc_mma(s_tmem + half * 64, q + (((d >> 2) * CT_SUB + (d & 3) * 32) >> 4),
+                                           kd + (((d >> 2) * L::ATOM + (d & 3) * 32) >> 4), IDESC_S, d != 0);
+                                tc_commit(&s_full[tile][half]);
+                            }
+                            tc_commit(&k_empty[st]);
+                        }
                     }
-                    if (ok && n > 0) tc_commit(&v_empty[before]);
-                    if (ok && more) tc_commit(&k_empty[st]);
-                    y0 = x0;
-                    y1 = x1;
+                    y = x;
                     ++k;
                 }
-                tc_commit(&drain);  // every MMA has ended before TMEM is given back
-                chunk_wait(&drain, 0, a.err);
+                tc_commit(&drain[tile]);  // every MMA has ended before TMEM is given back
+                chunk_wait(&drain[tile], 0, a.err);
             }
             __syncwarp();
         } else if (warp < 8) {
@@ -361,10 +360,6 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                 float ref = -INFINITY, sum = 0.f;
                 const bool more = u + len < u1;  // the share has an item after this one
                 bool q_next = false;             // whose Q this group has asked for
-                auto first_has = [&](int step) {  // the first tile has the step too
-                    const CtTile y = w.tile(a, 0);
-                    return step >= y.from && step < y.to;
-                };
                 auto ask_q = [&]() {
                     CtWalk next = w;
                     next.next(a, m, u1 - u - len);
@@ -446,17 +441,17 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                     weights(s0, tsh);
                     weights(s1, tsh + 16);
                     sum += (acc[0].x + acc[0].y) + (acc[1].x + acc[1].y);
-                    // keys of the step that no row of the item sees: whatever their values are, zeros in their place.  The
-                    // first tile that has the step sees to it (the other's product comes after it).
-                    if ((key0 + CT_STEP > w.t.hi || key0 < w.t.lo) && (g == 0 || !first_has(step))) {
-                        const int unit = n + (step >> 1) - w.k0;
-                        ok = wait(&v_full[unit % ST], unit / ST);
+                    // keys of the step that no row of the item sees: whatever their values are, zeros in their place (both
+                    // groups write them, each before its own product)
+                    if (key0 + CT_STEP > w.t.hi || key0 < w.t.lo) {
+                        const int i = 2 * (n - w.k0) + step;  // of the share's steps
+                        ok = wait(&v_full[i % ST], i / ST);
                         if (!ok) break;
                         const int row = r & (CT_STEP - 1), key = key0 + row;
                         if (key >= w.t.hi || key < w.t.lo) {
-                            unsigned char* v = sm + L::V + (uint32_t)(unit % ST) * L::OPER + (half * CT_STEP + row) * 128;
+                            unsigned char* v = sm + L::V + (uint32_t)(i % ST) * L::STEP + row * 128;
                             for (int c = r / CT_STEP; c < HD / 8; c += 128 / CT_STEP)
-                                *reinterpret_cast<uint4*>(v + (c >> 3) * CT_SUB + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                                *reinterpret_cast<uint4*>(v + (c >> 3) * L::ATOM + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                         }
                         fence_proxy_async();
                     }
