@@ -36,7 +36,7 @@ namespace mtp {
 namespace {
 
 constexpr int CT_ROWS = 256, CT_TILE = 128, CT_KEYS = 128;
-constexpr int CT_WARPS = 12, CT_THREADS = CT_WARPS * 32;  // two softmax groups of four, MMAs of A, copies, MMAs of B, -
+constexpr int CT_WARPS = 12, CT_THREADS = CT_WARPS * 32;  // two softmax groups of four, MMAs of A, copies of K, MMAs of B, copies of V
 constexpr uint32_t CT_SUB = 128 * 128;                    // 128 rows of 128 bytes
 constexpr int CT_STEP = 64;  // keys of a step: the scores that a thread holds
 constexpr uint32_t TM_S = 0, TM_O = 256, TM_COLS = 512;  // tile t, step s: S at 128 t + 64 (s & 1), O at 256 + 128 t
@@ -202,51 +202,56 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
     pdl_launch_dependents();
     const long long u0 = m.units && cta < m.ctas ? chunk_border(a, m, cta) : 0;
     const long long u1 = m.units && cta < m.ctas ? chunk_border(a, m, cta + 1) : 0;
-    auto wait = [&](uint64_t* bar, uint32_t parity) {  // one lane polls
-        return __all_sync(FULL_MASK, lane != 0 || chunk_wait(bar, parity, a.err)) != 0;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+        return __all_sync(FULL_MASK, mbar_try_wait(bar, parity & 1) || chunk_wait(bar, parity, a.err)) != 0;
     };
 
     if (u0 < u1) {
-        if (warp == 9) {
+        if (warp == 9 || warp == 11) {
+            // ---- copies of the keys (warp 9) or values (warp 11): a lane per piece of a step ----
+            const int kv = warp == 11, P = 1 << a.page_shift, box = min(P, CT_STEP), per = CT_STEP / box;
+            const int sub = lane % per, half = lane / per;
+            const bool mine = half < HD / 64;
+            unsigned char* ring = sm + (kv ? L::V : L::K) + half * L::ATOM + sub * box * 128;
+            uint64_t *full = kv ? v_full : k_full, *empty = kv ? v_empty : k_empty;
             CtWalk w(a, m, u0, u1);
-            // ---- copies: a lane per piece of a unit's keys (kv 0) and values (kv 1) ----
-            const int P = 1 << a.page_shift, box = min(P, CT_STEP), per = CT_STEP / box;
-            const int sub = lane % per, half = lane / per % (HD / 64), kv = lane / per / (HD / 64);
-            const uint32_t to = half * L::ATOM + sub * box * 128;
             int step = 2 * w.k0, n = 0;
             bool ok = true;
-            auto page_of = [&]() {  // -1 outside the pool (zeros), -2 where no row sees a key of it
-                const int key = w.t.key0 + step * CT_STEP + sub * box;
-                if (kv > 1 || key >= w.t.hi || key + box <= w.t.lo) return -2;
-                const int page = __ldg(a.block_table + (size_t)w.t.slot * a.bt_stride + (key >> a.page_shift));
-                return page >= 0 && page < a.n_pages ? page : -1;
+            // pages [base, base + 32) of the slot, one per lane, and the 32 after them
+            int base = 0, pages = 0, ahead = 0;
+            const int* table = nullptr;
+            auto lookup = [&](int first) { return first + lane < a.bt_stride ? __ldg(table + first + lane) : -1; };
+            auto enter = [&]() {  // an item's first step
+                table = a.block_table + (size_t)w.t.slot * a.bt_stride;
+                base = (w.t.key0 + step * CT_STEP) >> a.page_shift & ~31;
+                pages = lookup(base);
+                ahead = lookup(base + 32);
             };
-            int page = page_of(), k_sent = 0, v_sent = 0;
+            enter();
             for (const int steps = 2 * (int)(u1 - u0); n < steps; ++n) {
-                const int st = n % ST, block = page < 0 ? -1 : page * a.page_blocks + a.layer_block + kv * a.kv_heads + w.it.head;
-                const int row = (w.t.key0 + step * CT_STEP + sub * box) & (P - 1);
-                const unsigned have = __ballot_sync(FULL_MASK, page >= -1 && kv == 0);  // (the values' pieces are as many)
-                const uint32_t bytes = __popc(have) * box * 128;
-                if (n >= ST && !(ok = wait(&k_empty[st], n / ST - 1))) break;
-                if (lane == 0) mbar_arrive_expect_tx(&k_full[st], bytes);
+                const int st = n % ST, key = w.t.key0 + step * CT_STEP + sub * box, index = key >> a.page_shift;
+                if (index - base >= 32) {  // (the same in all lanes: a step's pages lie in one aligned group)
+                    base += 32;
+                    pages = ahead;
+                    ahead = lookup(base + 32);
+                }
+                int page = __shfl_sync(FULL_MASK, pages, (index - base) & 31);
+                page = page >= 0 && page < a.n_pages ? page : -1;  // -1: outside the pool, zeros
+                const int block = page < 0 ? -1 : page * a.page_blocks + a.layer_block + kv * a.kv_heads + w.it.head;
+                const bool wanted = mine && key < w.t.hi && key + box > w.t.lo;  // some row sees a key of the piece
+                const uint32_t bytes = __popc(__ballot_sync(FULL_MASK, wanted)) * box * 128;
+                if (n >= ST && !(ok = wait(&empty[st], n / ST - 1))) break;
+                if (lane == 0) mbar_arrive_expect_tx(&full[st], bytes);
                 __syncwarp();
-                if (kv == 0 && page >= -1) tma_cache(sm + L::K + st * L::STEP + to, &map, half * 64, row, block, &k_full[st]);
-                ++k_sent;
-                if (n >= ST && !(ok = wait(&v_empty[st], n / ST - 1))) break;
-                if (lane == 0) mbar_arrive_expect_tx(&v_full[st], bytes);
-                __syncwarp();
-                if (kv == 1 && page >= -1) tma_cache(sm + L::V + st * L::STEP + to, &map, half * 64, row, block, &v_full[st]);
-                ++v_sent;
-                if (++step == 2 * w.k1) {
+                if (wanted) tma_cache(ring + st * L::STEP, &map, half * 64, key & (P - 1), block, &full[st]);
+                if (++step == 2 * w.k1 && n + 1 < steps) {
                     w.next(a, m, u1 - u0 - (n + 1) / 2);
                     step = 0;
+                    enter();
                 }
-                if (n + 1 < steps) page = page_of();
             }
-            if (!ok && lane == 0) {  // what is in flight lands before the CTA leaves
-                for (int i = max(0, k_sent - ST); i < k_sent; ++i) chunk_wait(&k_full[i % ST], i / ST, nullptr);
-                for (int i = max(0, v_sent - ST); i < v_sent; ++i) chunk_wait(&v_full[i % ST], i / ST, nullptr);
-            }
+            if (!ok && lane == 0)  // what is in flight lands before the CTA leaves
+                for (int i = max(0, n - ST); i < n; ++i) chunk_wait(&full[i % ST], i / ST, nullptr);
             __syncwarp();
         } else if (warp == 8 || warp == 10) {
             // ---- MMAs of a tile, by one thread ----
@@ -260,7 +265,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                 const uint32_t s_tmem = tmem + TM_S + tile * 128, o_tmem = tmem + TM_O + tile * 128;
                 uint32_t q_phase = 0, p_phase[2] = {0, 0};
                 bool ok = true;
-                auto await = [&](uint64_t* bar, uint32_t phase) { ok = ok && chunk_wait(bar, phase, a.err); };
+                auto await = [&](bool there, uint64_t* bar, uint32_t phase) { ok = ok && (there || chunk_wait(bar, phase, a.err)); };
                 int k = w.k0;
                 // the products of the steps of unit n - 1, between them the scores of unit n's: S of a step comes after
                 // the P V of two steps before, in whose place it goes, and the softmax has the step between to work on
@@ -275,28 +280,34 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const int i = 2 * n + half, st = i % ST, before = (i + ST - 2) % ST;
-                        if (n > 0) {
-                            const int step = 2 * at + half;
-                            await(&v_full[before], (i - 2) / ST);
-                            if (step >= y.from && step < y.to) {  // O += P V
-                                await(&p_full[tile][half], p_phase[half]++);
-                                if (!ok) break;
-                                tc_fence_after();
-                                const uint64_t v = v0 + before * (L::STEP >> 4);
+                        const int p_step = 2 * at + half, s_step = 2 * k + half;
+                        const bool p_on = n > 0 && p_step >= y.from && p_step < y.to, s_on = more && s_step >= x.from && s_step < x.to;
+                        const bool s_first = s_on && s_step == x.from;
+                        // all barriers are asked at once: an answer takes 126 cycles
+                        const bool k_there = !more || mbar_try_wait(&k_full[st], (i / ST) & 1);
+                        const bool v_there = n == 0 || mbar_try_wait(&v_full[before], ((i - 2) / ST) & 1);
+                        const bool p_there = !p_on || mbar_try_wait(&p_full[tile][half], p_phase[half] & 1);
+                        await(k_there, &k_full[st], i / ST);
+                        await(v_there, &v_full[before], (i - 2) / ST);
+                        await(p_there, &p_full[tile][half], p_phase[half]);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (p_on) {  // O += P V
+                            p_phase[half]++;
+                            const uint64_t v = v0 + before * (L::STEP >> 4);
 #pragma unroll
-                                for (int d = 0; d < CT_STEP / 16; ++d)
-                                    tc_mma_ta(o_tmem, s_tmem + half * 64 + d * 8, v + d * (2048 >> 4), IDESC_O, d != 0 || step != y.from);
-                                tc_commit(&pv_done[tile][half]);
-                            }
-                            tc_commit(&v_empty[before]);
+                            for (int d = 0; d < CT_STEP / 16; ++d)
+                                tc_mma_ta(o_tmem, s_tmem + half * 64 + d * 8, v + d * (2048 >> 4), IDESC_O, d != 0 || p_step != y.from);
+                            tc_commit(&pv_done[tile][half]);
+                        }
+                        if (n > 0) tc_commit(&v_empty[before]);
+                        if (s_first) {
+                            await(false, &q_full[tile], q_phase++);
+                            if (!ok) break;
+                            tc_fence_after();
                         }
                         if (more) {
-                            const int step = 2 * k + half;
-                            await(&k_full[st], i / ST);
-                            if (step >= x.from && step < x.to) {  // S = Q K^T
-                                if (step == x.from) await(&q_full[tile], q_phase++);
-                                if (!ok) break;
-                                tc_fence_after();
+                            if (s_on) {  // S = Q K^T
                                 const uint64_t kd = k0 + st * (L::STEP >> 4);
 #pragma unroll
                                 for (int d = 0; d < HD / 16; ++d)
