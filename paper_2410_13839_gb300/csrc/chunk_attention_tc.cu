@@ -27,6 +27,7 @@
 // tensor time again, and the error (as large as the output's own rounding to 16 bits) is
 // within the type.  Q, K and V enter as they are.
 #include <algorithm>
+#include <climits>
 #include <type_traits>
 
 #include "chunk.cuh"
@@ -81,6 +82,16 @@ __device__ __forceinline__ void tma_cache(void* dst, const CUtensorMap* map, int
             smem_addr(dst)),
         "l"(map), "r"(x), "r"(row), "r"(block), "r"(smem_addr(bar))
         : "memory");
+}
+// Whether a barrier's phase is complete, without waiting (try_wait suspends the thread for a while where it is not).
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(smem_addr(bar)), "r"(parity)
+        : "memory");
+    return done != 0;
 }
 // One thread of the (whole) warp, the same at every call.
 __device__ __forceinline__ bool elect_one() {
@@ -218,18 +229,23 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
             int step = 2 * w.k0, n = 0;
             bool ok = true;
             // pages [base, base + 32) of the slot, one per lane, and the 32 after them
-            int base = 0, pages = 0, ahead = 0;
+            int base = 0, pages = 0, ahead = 0, key_first = 0, hi = 0, lo = 0, last = 0, head_block = 0;
             const int* table = nullptr;
             auto lookup = [&](int first) { return first + lane < a.bt_stride ? __ldg(table + first + lane) : -1; };
             auto enter = [&]() {  // an item's first step
                 table = a.block_table + (size_t)w.t.slot * a.bt_stride;
-                base = (w.t.key0 + step * CT_STEP) >> a.page_shift & ~31;
+                key_first = w.t.key0;
+                hi = w.t.hi;
+                lo = w.t.lo;
+                last = 2 * w.k1;
+                head_block = a.layer_block + kv * a.kv_heads + w.it.head;
+                base = (key_first + step * CT_STEP) >> a.page_shift & ~31;
                 pages = lookup(base);
                 ahead = lookup(base + 32);
             };
             enter();
             for (const int steps = 2 * (int)(u1 - u0); n < steps; ++n) {
-                const int st = n % ST, key = w.t.key0 + step * CT_STEP + sub * box, index = key >> a.page_shift;
+                const int st = n % ST, key = key_first + step * CT_STEP + sub * box, index = key >> a.page_shift;
                 if (index - base >= 32) {  // (the same in all lanes: a step's pages lie in one aligned group)
                     base += 32;
                     pages = ahead;
@@ -237,14 +253,14 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                 }
                 int page = __shfl_sync(FULL_MASK, pages, (index - base) & 31);
                 page = page >= 0 && page < a.n_pages ? page : -1;  // -1: outside the pool, zeros
-                const int block = page < 0 ? -1 : page * a.page_blocks + a.layer_block + kv * a.kv_heads + w.it.head;
-                const bool wanted = mine && key < w.t.hi && key + box > w.t.lo;  // some row sees a key of the piece
+                const int block = page < 0 ? -1 : page * a.page_blocks + head_block;
+                const bool wanted = mine && key < hi && key + box > lo;  // some row sees a key of the piece
                 const uint32_t bytes = __popc(__ballot_sync(FULL_MASK, wanted)) * box * 128;
                 if (n >= ST && !(ok = wait(&empty[st], n / ST - 1))) break;
                 if (lane == 0) mbar_arrive_expect_tx(&full[st], bytes);
                 __syncwarp();
                 if (wanted) tma_cache(ring + st * L::STEP, &map, half * 64, key & (P - 1), block, &full[st]);
-                if (++step == 2 * w.k1 && n + 1 < steps) {
+                if (++step == last && n + 1 < steps) {
                     w.next(a, m, u1 - u0 - (n + 1) / 2);
                     step = 0;
                     enter();
@@ -266,15 +282,16 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                 uint32_t q_phase = 0, p_phase[2] = {0, 0};
                 bool ok = true;
                 auto await = [&](bool there, uint64_t* bar, uint32_t phase) { ok = ok && (there || chunk_wait(bar, phase, a.err)); };
-                int k = w.k0;
+                int k = w.k0, k1 = w.k1;
                 // the products of the steps of unit n - 1, between them the scores of unit n's: S of a step comes after
                 // the P V of two steps before, in whose place it goes, and the softmax has the step between to work on
                 for (int n = 0, units = (int)(u1 - u0); ok && n <= units; ++n) {
                     const int at = k - 1;
                     const bool more = n < units;
-                    if (n > 0 && k == w.k1) {
+                    if (n > 0 && k == k1) {
                         w.next(a, m, units - n);
                         k = 0;
+                        k1 = w.k1;
                         if (more) x = w.tile(a, tile);
                     }
 #pragma unroll
@@ -367,7 +384,16 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
             }
             for (long long u = u0; u < u1;) {
                 const int len = w.k1 - w.k0;
-                const int pos = r < x.rows ? w.t.len - w.t.n + chunk_token(a, x.p0 + r) : -1;
+                // (rows past the tile's are not looked at: as if they saw every key)
+                const int pos = r < x.rows ? w.t.len - w.t.n + chunk_token(a, x.p0 + r) : INT_MAX;
+                const int window = a.window > 0 && r < x.rows ? a.window : INT_MAX;
+                // steps [inner_from, inner_to): every row of the warp sees all of their keys (and some row of the item does,
+                // where the warp has none)
+                const int key_first = w.t.key0, hi = w.t.hi, lo = w.t.lo, share = 2 * (n - w.k0);
+                const int pos0 = __reduce_min_sync(FULL_MASK, pos), pos1 = __reduce_max_sync(FULL_MASK, r < x.rows ? pos : INT_MIN);
+                int inner_to = (hi - key_first) / CT_STEP, inner_from = (lo - key_first + CT_STEP - 1) / CT_STEP;
+                if (pos0 < hi) inner_to = pos0 < key_first ? 0 : min(inner_to, (pos0 + 1 - key_first) / CT_STEP);
+                if (a.window > 0 && pos1 >= a.window + key_first) inner_from = max(inner_from, (pos1 - a.window - key_first) / CT_STEP + 1);
                 float ref = -INFINITY, sum = 0.f;
                 const bool more = u + len < u1;  // the share has an item after this one
                 bool q_next = false;             // whose Q this group has asked for
@@ -378,25 +404,28 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                     q_next = y.from < y.to;
                     if (q_next) load_q(next, y);
                 };
+                bool there = false;  // the step's scores are known to be there
 #pragma unroll 1
                 for (int step = x.from; step < x.to; ++step) {
-                    const int key0 = w.t.key0 + step * CT_STEP, half = step & 1;
+                    const int half = step & 1;
                     const uint32_t tsh = ts + half * 64;
-                    if (ok) ok = wait(&s_full[g][half], half ? seen[1]++ : seen[0]++);
+                    const bool inner = step >= inner_from && step < inner_to, onward = step + 1 < x.to;
+                    ok = __all_sync(FULL_MASK, there || chunk_wait(&s_full[g][half], half ? seen[1] : seen[0], a.err)) != 0;
                     if (!ok) break;
                     tc_fence_after();
                     float s0[32], s1[32];
                     tmem_ld_issue<32>(tsh, s0);
                     tmem_ld_issue<32>(tsh + 32, s1);
-                    if (step + 1 == x.to && more) ask_q();  // the tile's last S is there: Q's space is free
+                    if (half) ++seen[1]; else ++seen[0];
+                    const uint32_t next_phase = half ? seen[0] : seen[1];
+                    if (!onward && more) ask_q();  // the tile's last S is there: Q's space is free
                     __syncwarp();
-                    // columns (lowest, highest] of the step are the keys that this row sees
-                    const int highest = pos - key0, lowest = a.window > 0 ? pos - a.window - key0 : -1;
-                    const bool inner = __all_sync(FULL_MASK, highest >= CT_STEP - 1 && lowest < 0);
                     tmem_ld_wait();
                     tmem_ld_done(s0);
                     tmem_ld_done(s1);
                     if (!inner) {
+                        // columns (lowest, highest] of the step are the keys that this row sees
+                        const int key0 = key_first + step * CT_STEP, highest = pos - key0, lowest = pos - key0 >= window ? pos - key0 - window : -1;
 #pragma unroll
                         for (int c = 0; c < 32; ++c) {
                             s0[c] = c <= highest && c > lowest ? s0[c] : -INFINITY;
@@ -421,7 +450,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                         }
                         __syncwarp();
                         if (step > x.from) {  // the product before is complete, the next one waits for this step's weights
-                            ok = wait(&pv_done[g][half ^ 1], (half ? seen[0] : seen[1]) - 1);
+                            ok = wait(&pv_done[g][half ^ 1], next_phase - 1);
                             if (!ok) break;
                             tc_fence_after();
 #pragma unroll 1
@@ -449,22 +478,27 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                         }
                         tmem_st16(at, y);
                     };
+                    // (asked here: the answer is there when it is needed)
+                    there = onward && mbar_test(&s_full[g][half ^ 1], next_phase & 1);
                     weights(s0, tsh);
                     weights(s1, tsh + 16);
                     sum += (acc[0].x + acc[0].y) + (acc[1].x + acc[1].y);
-                    // keys of the step that no row of the item sees: whatever their values are, zeros in their place (both
-                    // groups write them, each before its own product)
-                    if (key0 + CT_STEP > w.t.hi || key0 < w.t.lo) {
-                        const int i = 2 * (n - w.k0) + step;  // of the share's steps
-                        ok = wait(&v_full[i % ST], i / ST);
-                        if (!ok) break;
-                        const int row = r & (CT_STEP - 1), key = key0 + row;
-                        if (key >= w.t.hi || key < w.t.lo) {
-                            unsigned char* v = sm + L::V + (uint32_t)(i % ST) * L::STEP + row * 128;
-                            for (int c = r / CT_STEP; c < HD / 8; c += 128 / CT_STEP)
-                                *reinterpret_cast<uint4*>(v + (c >> 3) * L::ATOM + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    if (!inner) {
+                        // keys of the step that no row of the item sees: whatever their values are, zeros in their place (both
+                        // groups write them, each before its own product)
+                        const int key0 = key_first + step * CT_STEP;
+                        if (key0 + CT_STEP > hi || key0 < lo) {
+                            const int i = share + step;  // of the share's steps
+                            ok = wait(&v_full[i % ST], i / ST);
+                            if (!ok) break;
+                            const int row = r & (CT_STEP - 1), key = key0 + row;
+                            if (key >= hi || key < lo) {
+                                unsigned char* v = sm + L::V + (uint32_t)(i % ST) * L::STEP + row * 128;
+                                for (int c = r / CT_STEP; c < HD / 8; c += 128 / CT_STEP)
+                                    *reinterpret_cast<uint4*>(v + (c >> 3) * L::ATOM + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                            }
+                            fence_proxy_async();
                         }
-                        fence_proxy_async();
                     }
                     __syncwarp();
                     tmem_st_wait();
