@@ -20,9 +20,12 @@
 // Code size matters: with everything unrolled and inlined (190 KB) the warps waited for
 // instructions, 10,000 cycles per 128 keys.
 //
-// m is a row's reference, not its maximum: it moves only where the maximum passes it by more
-// than 8 (log2 units), so P stays below 2^8 and the output in TMEM is rescaled a few times per
-// row instead of once per unit.  The sum takes the weights before they are rounded, in fp32.
+// m is a row's reference, not its maximum: the weights are made with the one that is there, and
+// only where a step's weights add up to more than 2^15 (or a row has none yet) is the maximum
+// looked for, the reference moved and the output in TMEM rescaled.  After a row's first steps
+// that is rare, and 64 maxima per row and step are saved.  16-bit weights have the same
+// relative precision whatever the reference is.  The sum takes the weights before they are
+// rounded, in fp32.
 // P is rounded once to the type: a second product with its residues would cost half as much
 // tensor time again, and the error (as large as the output's own rounding to 16 bits) is
 // within the type.  Q, K and V enter as they are.
@@ -41,7 +44,8 @@ constexpr int CT_WARPS = 12, CT_THREADS = CT_WARPS * 32;  // two softmax groups 
 constexpr uint32_t CT_SUB = 128 * 128;                    // 128 rows of 128 bytes
 constexpr int CT_STEP = 64;  // keys of a step: the scores that a thread holds
 constexpr uint32_t TM_S = 0, TM_O = 256, TM_COLS = 512;  // tile t, step s: S at 128 t + 64 (s & 1), O at 256 + 128 t
-constexpr float LAG = 8.f;
+constexpr int CT_HANDOVER = 2;  // MMAs of S before whose end the other tile may go on
+constexpr float LAG = 8.f, LIMIT = 32768.f;
 constexpr float LN2 = 0.69314718055994531f;
 
 template <int HD>
@@ -177,7 +181,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
     using L = CtLayout<HD>;
     constexpr int ST = L::STAGES;
     extern __shared__ unsigned char ct_raw[];
-    __shared__ uint64_t q_full[2], s_full[2][2], p_full[2][2], pv_done[2][2], k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], drain[2];
+    __shared__ uint64_t q_full[2], s_full[2][2], p_full[2][2], pv_done[2][2], k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], turn[2], drain[2];
     __shared__ long long scan_part[CT_WARPS][2];
     __shared__ uint32_t tmem_base;
     unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(ct_raw) + 1023) & ~(uintptr_t)1023);
@@ -189,6 +193,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(&drain[i], 1);
+            mbar_init(&turn[i], 1);
             mbar_init(&q_full[i], 4);
             for (int h = 0; h < 2; ++h) {
                 mbar_init(&s_full[i][h], 1);
@@ -304,9 +309,15 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                         const bool k_there = !more || mbar_try_wait(&k_full[st], (i / ST) & 1);
                         const bool v_there = n == 0 || mbar_try_wait(&v_full[before], ((i - 2) / ST) & 1);
                         const bool p_there = !p_on || mbar_try_wait(&p_full[tile][half], p_phase[half] & 1);
+                        // The tiles take turns, so that a tile's MMAs run in one piece and their results come half a step apart:
+                        // mixed, both tiles' scores would be ready late, and both softmax groups wait for them.
+                        const bool my_turn = tile == 0 && i == 0;
+                        const uint32_t turn_phase = i - 1 + tile;
+                        const bool turn_there = my_turn || mbar_try_wait(&turn[tile], turn_phase & 1);
                         await(k_there, &k_full[st], i / ST);
                         await(v_there, &v_full[before], (i - 2) / ST);
                         await(p_there, &p_full[tile][half], p_phase[half]);
+                        await(turn_there, &turn[tile], turn_phase);
                         if (!ok) break;
                         tc_fence_after();
                         if (p_on) {  // O += P V
@@ -323,13 +334,16 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                             if (!ok) break;
                             tc_fence_after();
                         }
+                        if (!s_on) mbar_arrive(&turn[tile ^ 1]);
                         if (more) {
                             if (s_on) {  // S = Q K^T
                                 const uint64_t kd = k0 + st * (L::STEP >> 4);
 #pragma unroll
-                                for (int d = 0; d < HD / 16; ++d)
+                                for (int d = 0; d < HD / 16; ++d) {
+                                    if (d == HD / 16 - CT_HANDOVER) mbar_arrive(&turn[tile ^ 1]);  // (seen by the time that S is through)
                                     tc_mma(s_tmem + half * 64, q + (((d >> 2) * CT_SUB + (d & 3) * 32) >> 4),
                                            kd + (((d >> 2) * L::ATOM + (d & 3) * 32) >> 4), IDESC_S, d != 0);
+                                }
                                 tc_commit(&s_full[tile][half]);
                             }
                             tc_commit(&k_empty[st]);
@@ -405,6 +419,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                     if (q_next) load_q(next, y);
                 };
                 bool there = false;  // the step's scores are known to be there
+                float s0[32], s1[32];
 #pragma unroll 1
                 for (int step = x.from; step < x.to; ++step) {
                     const int half = step & 1;
@@ -413,7 +428,6 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                     ok = __all_sync(FULL_MASK, there || chunk_wait(&s_full[g][half], half ? seen[1] : seen[0], a.err)) != 0;
                     if (!ok) break;
                     tc_fence_after();
-                    float s0[32], s1[32];
                     tmem_ld_issue<32>(tsh, s0);
                     tmem_ld_issue<32>(tsh + 32, s1);
                     if (half) ++seen[1]; else ++seen[0];
@@ -432,22 +446,47 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                             s1[c] = c + 32 <= highest && c + 32 > lowest ? s1[c] : -INFINITY;
                         }
                     }
-                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    // (asked here: the answer is there when it is needed)
+                    there = onward && mbar_test(&s_full[g][half ^ 1], next_phase & 1);
+                    float2 acc[2];
+                    auto weights32 = [&](const float (&x)[32], uint32_t at) {  // over S, which is all in registers
+                        uint32_t y[16];
 #pragma unroll
-                    for (int c = 0; c < 32; c += 2) {
-                        mx[0] = fmaxf(mx[0], s0[c]);
-                        mx[1] = fmaxf(mx[1], s0[c + 1]);
-                        mx[2] = fmaxf(mx[2], s1[c]);
-                        mx[3] = fmaxf(mx[3], s1[c + 1]);
-                    }
-                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
-                    const bool moves = top > ref + LAG;  // (from -inf: any value)
-                    if (__any_sync(FULL_MASK, moves)) {
-                        const float f = moves ? ex2(ref - top) : 1.f;
-                        if (moves) {
-                            ref = top;
-                            sum *= f;
+                        for (int e = 0; e < 16; ++e) {
+                            const float2 z = fma2(make_float2(x[2 * e], x[2 * e + 1]), make_float2(a.scale_log2, a.scale_log2),
+                                                  make_float2(-ref, -ref));
+                            const float2 p = make_float2(ex2(z.x), ex2(z.y));
+                            acc[e & 1] = add2(acc[e & 1], p);
+                            y[e] = T::pack(p.x, p.y);
                         }
+                        tmem_st16(at, y);
+                    };
+                    auto weights = [&]() {  // their sum
+                        acc[0] = acc[1] = make_float2(0.f, 0.f);
+                        weights32(s0, tsh);
+                        weights32(s1, tsh + 16);
+                        return (acc[0].x + acc[0].y) + (acc[1].x + acc[1].y);
+                    };
+                    float part = 0.f;
+                    bool fits = __all_sync(FULL_MASK, ref != -INFINITY);  // every row has a reference
+                    if (fits) {
+                        part = weights();
+                        fits = __all_sync(FULL_MASK, part <= LIMIT);
+                    }
+                    if (!fits) {
+                        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                        for (int c = 0; c < 32; c += 2) {
+                            mx[0] = fmaxf(mx[0], s0[c]);
+                            mx[1] = fmaxf(mx[1], s0[c + 1]);
+                            mx[2] = fmaxf(mx[2], s1[c]);
+                            mx[3] = fmaxf(mx[3], s1[c + 1]);
+                        }
+                        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
+                        const bool moves = top > ref + LAG;  // (from -inf: any value)
+                        const float f = moves ? ex2(ref - top) : 1.f;
+                        if (moves) ref = top;
+                        sum *= f;
                         __syncwarp();
                         if (step > x.from) {  // the product before is complete, the next one waits for this step's weights
                             ok = wait(&pv_done[g][half ^ 1], next_phase - 1);
@@ -463,26 +502,12 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                                 tmem_st16(to + c, y);
                             }
                         }
+                        const float kept = ref;
+                        if (ref == -INFINITY) ref = 0.f;  // a row that has seen no key: every weight 0
+                        part = weights();
+                        ref = kept;
                     }
-                    const float base = ref == -INFINITY ? 0.f : ref;  // a row that has seen no key: every weight 0
-                    float2 acc[2] = {{0.f, 0.f}, {0.f, 0.f}};
-                    auto weights = [&](const float (&x)[32], uint32_t at) {  // over S, which is all in registers
-                        uint32_t y[16];
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const float2 z = fma2(make_float2(x[2 * e], x[2 * e + 1]), make_float2(a.scale_log2, a.scale_log2),
-                                                  make_float2(-base, -base));
-                            const float2 p = make_float2(ex2(z.x), ex2(z.y));
-                            acc[e & 1] = add2(acc[e & 1], p);
-                            y[e] = T::pack(p.x, p.y);
-                        }
-                        tmem_st16(at, y);
-                    };
-                    // (asked here: the answer is there when it is needed)
-                    there = onward && mbar_test(&s_full[g][half ^ 1], next_phase & 1);
-                    weights(s0, tsh);
-                    weights(s1, tsh + 16);
-                    sum += (acc[0].x + acc[0].y) + (acc[1].x + acc[1].y);
+                    sum += part;
                     if (!inner) {
                         // keys of the step that no row of the item sees: whatever their values are, zeros in their place (both
                         // groups write them, each before its own product)
