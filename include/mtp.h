@@ -567,7 +567,7 @@ MTP_API int mtp_cache_append(const mtp_cache_append_args* args, void* cuda_strea
  * What the cache holds past a slot's length, or before every row's window, may be anything,
  * NaN too; a non-finite value inside can reach every row of the slot.
  * Limits: slots <= 4096, n_heads <= 1024, G = n_heads / n_kv_heads <= 64, bt_stride * page_size <=
- * 2^24, 2 slots + rows * G / 256 <= 8192.  Errors: MTP_ERR_INVALID, MTP_ERR_CUDA. */
+ * 2^24, rows * G < 2^21.  Errors: MTP_ERR_INVALID, MTP_ERR_CUDA. */
 typedef struct mtp_chunk_attention_args {
     int32_t slots, rows, n_heads, n_kv_heads, head_dim, page_size, layers, layer, n_pages, bt_stride, dtype, window,
         max_new, max_keys;

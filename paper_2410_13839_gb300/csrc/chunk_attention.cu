@@ -76,14 +76,14 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t&
 
 // Shared memory of the few-rows kernel, from a 1024-byte boundary: ring stages (K then V, each
 // HD / 64 tiles of 64 rows of 128 bytes), Q (HD / 64 tiles of TR rows), a join buffer of TR x HD
-// floats, per-warp maxima and sums, the map.
+// floats, per-warp maxima and sums.
 template <int HD, int MT>
 struct FrLayout {
     static constexpr int TR = 16 * MT;
     static constexpr int STAGES = HD == 64 ? 4 : MT == 1 ? 3 : 2;
     static constexpr uint32_t TILE = FR_KEYS * 128, KV = TILE * (HD / 64), STAGE = 2 * KV;
-    static constexpr uint32_t Q = STAGES * STAGE, JOIN = Q + TR * HD * 2, ML = JOIN + TR * HD * 4, MAP = ML + 2 * 4 * TR * 4;
-    static size_t bytes(int slots, int tiles) { return 1024 + MAP + chunk_map_bytes(slots, tiles); }
+    static constexpr uint32_t Q = STAGES * STAGE, JOIN = Q + TR * HD * 2, ML = JOIN + TR * HD * 4;
+    static constexpr size_t BYTES = 1024 + ML + 2 * 4 * TR * 4;
 };
 
 template <class T, int HD, int MT>
@@ -93,7 +93,6 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
     constexpr int TR = L::TR, ST = L::STAGES;
     extern __shared__ unsigned char fr_raw[];
     __shared__ uint64_t full[ST], empty[ST];
-    __shared__ long long scan_part[FR_WARPS][2];
     unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(fr_raw) + 1023) & ~(uintptr_t)1023);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
     if (tid == 0) {
@@ -103,60 +102,60 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
         }
         fence_barrier_init();
     }
-    const ChunkMap m = chunk_map<FR_WARPS, TR, FR_KEYS>(a, sm + L::MAP, scan_part);  // (synchronises)
+    __syncthreads();
     pdl_launch_dependents();
-    const long long u0 = m.units ? chunk_border(a, m, cta) : 0, u1 = m.units ? chunk_border(a, m, cta + 1) : 0;
-    if (tid == 0) a.desc[cta * CH_DESC] = 0;
-    if (cta >= m.ctas || u0 >= u1) return;
-    const ChunkItem start = chunk_item(a, m, u0);
+    pdl_wait();  // the plan
+    const int4 start = a.start[cta];
+    const int units = start.w;
+    if (units == 0) return;
 
     if (warp == 4) {  // ---- the ring's filler ----
         const int P = 1 << a.page_shift, box = min(P, FR_KEYS), per = FR_KEYS / box;
         // this lane's piece of a stage: rows [sub * box, + box) of half `half` of K (0) or V (1)
         const int sub = lane % per, half = lane / per % (HD / 64), kv = lane / per / (HD / 64);
         const bool mine = kv < 2;
-        const uint32_t to = kv * L::KV + half * L::TILE + sub * box * 128;
-        ChunkItem it = start;
-        int k = (int)(u0 - it.first);
-        ChunkTile t = chunk_tile<TR, FR_KEYS>(a, chunk_slot_of(a, m, it.tile), it.tile - m.slot_first[chunk_slot_of(a, m, it.tile)]);
-        // the piece's page, -1 outside the pool (its rows are then zeros), -2 where no row sees a key of it
-        auto page_of = [&]() {
-            const int key = t.key0 + k * FR_KEYS + sub * box;
-            if (!mine || key >= t.hi || key + box <= t.lo) return -2;
-            const int page = __ldg(a.block_table + (size_t)t.slot * a.bt_stride + (key >> a.page_shift));
-            return page >= 0 && page < a.n_pages ? page : -1;
-        };
-        int page = page_of();
+        unsigned char* ring = sm + kv * L::KV + half * L::TILE + sub * box * 128;
+        ChunkWalk w(a, start);
+        int k = w.k0, issued = 0, base = 0, pages = 0, ahead = 0;
         bool ok = true;
-        int issued = 0;
-        for (long long u = u0; u < u1; ++u, ++issued) {
-            const int st = issued % ST;
+        // pages [base, base + 32) of the slot, one per lane, and the 32 after them
+        auto lookup = [&](int first) {
+            return first + lane < a.bt_stride ? __ldg(a.block_table + (size_t)w.t.slot * a.bt_stride + first + lane) : -1;
+        };
+        auto enter = [&]() {
+            base = (w.key0<FR_KEYS>() + k * FR_KEYS) >> a.page_shift & ~31;
+            pages = lookup(base);
+            ahead = lookup(base + 32);
+        };
+        enter();
+        for (; issued < units; ++issued) {
+            const int st = issued % ST, key = w.key0<FR_KEYS>() + k * FR_KEYS + sub * box, index = key >> a.page_shift;
+            if (index - base >= 32) {  // (the same in all lanes: a unit's pages lie in one aligned group)
+                base += 32;
+                pages = ahead;
+                ahead = lookup(base + 32);
+            }
+            int page = __shfl_sync(FULL_MASK, pages, (index - base) & 31);
+            page = page >= 0 && page < a.n_pages ? page : -1;  // -1: outside the pool, zeros
+            const int block = page < 0 ? -1 : page * a.page_blocks + a.layer_block + kv * a.kv_heads + w.head;
+            const bool wanted = mine && key < w.t.hi && key + box > w.t.lo;  // some row sees a key of the piece
+            const unsigned have = __ballot_sync(FULL_MASK, wanted);
             if (issued >= ST) {
-                ok = __all_sync(FULL_MASK, lane != 0 || chunk_wait(&empty[st], (uint32_t)(issued / ST - 1) & 1, a.err));
+                ok = __all_sync(FULL_MASK, lane != 0 || chunk_wait(&empty[st], issued / ST - 1, a.err));
                 if (!ok) break;
             }
-            const unsigned have = __ballot_sync(FULL_MASK, page != -2);
             if (lane == 0) mbar_arrive_expect_tx(&full[st], __popc(have) * box * 128);
             __syncwarp();
-            if (page != -2) {
-                const int row = (t.key0 + k * FR_KEYS + sub * box) & (P - 1);
-                const int block = page < 0 ? -1 : page * a.page_blocks + a.layer_block + kv * a.kv_heads + it.head;
-                tma_cache(sm + st * L::STAGE + to, &map, half * 64, row, block, &full[st]);
-            }
-            if (++k == it.units) {
-                const int tile = it.tile;
-                it = chunk_next(a, m, it);
+            if (wanted) tma_cache(ring + st * L::STAGE, &map, half * 64, key & (P - 1), block, &full[st]);
+            if (++k == w.k1 && issued + 1 < units) {
+                w.next(a);
                 k = 0;
-                if (it.tile != tile && u + 1 < u1) {
-                    const int s = chunk_slot_of(a, m, it.tile);
-                    t = chunk_tile<TR, FR_KEYS>(a, s, it.tile - m.slot_first[s]);
-                }
+                enter();
             }
-            if (u + 1 < u1) page = page_of();
         }
         // after a failed wait: what is in flight lands before the CTA leaves
         if (!ok && lane == 0)
-            for (int i = max(0, issued - ST); i < issued; ++i) chunk_wait(&full[i % ST], (uint32_t)(i / ST) & 1, nullptr);
+            for (int i = max(0, issued - ST); i < issued; ++i) chunk_wait(&full[i % ST], i / ST, nullptr);
         return;
     }
 
@@ -165,21 +164,20 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
     const uint32_t q_base = smem_addr(sm + L::Q);
     float* join = reinterpret_cast<float*>(sm + L::JOIN);
     float* ml = reinterpret_cast<float*>(sm + L::ML);  // [4 warps][TR] maxima, then sums
-    ChunkItem it = start;
-    int k = (int)(u0 - it.first), stage = 0;
+    int stage = 0;
     bool alive = true;
-    for (long long u = u0; u < u1;) {
-        const int slot = chunk_slot_of(a, m, it.tile);
-        const ChunkTile t = chunk_tile<TR, FR_KEYS>(a, slot, it.tile - m.slot_first[slot]);
-        const int k1 = (int)min((long long)it.units, k + (u1 - u));
-        const bool begins = k == 0, ends = k1 == it.units;
+    ChunkWalk w(a, start);
+    for (; w.left > 0; w.next(a)) {
+        const ChunkTile& t = w.t;
+        const int key_first = w.key0<FR_KEYS>();
+        const bool begins = w.begins(), ends = w.ends();
         // Q: 16 bytes a thread and step, rows past the tile zero
         for (int i = tid; i < TR * (HD / 8); i += FR_CONSUMERS) {
             const int r = i / (HD / 8), c = i % (HD / 8), p = t.p0 + r;
             uint4 v = make_uint4(0u, 0u, 0u, 0u);
             if (r < t.rows) {
                 const int token = chunk_token(a, p);
-                const uint16_t* src = a.q + (t.row0 + token) * a.q_stride + (it.head * a.group + p - token * a.group) * HD + c * 8;
+                const uint16_t* src = a.q + (t.row0 + token) * a.q_stride + (w.head * a.group + p - token * a.group) * HD + c * 8;
                 if (a.q_vec) {
                     v = __ldg(reinterpret_cast<const uint4*>(src));
                 } else {
@@ -205,14 +203,14 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
                 mx[i][e] = -INFINITY;
                 sum[i][e] = 0.f;
                 const int r = i * 16 + r0 + e * 8;
-                pos[i][e] = r < t.rows ? t.len - t.n + chunk_token(a, t.p0 + r) : -1;
+                pos[i][e] = r < t.rows ? t.base + chunk_token(a, t.p0 + r) : -1;
             }
         }
-        const int pos_first = t.len - t.n + chunk_token(a, t.p0), pos_last = t.hi - 1;
-        for (; k < k1; ++k, ++u) {
+        const int pos_first = t.base + chunk_token(a, t.p0), pos_last = t.hi - 1;
+        for (int k = w.k0; k < w.k1; ++k) {
             const int st = stage % ST;
-            if (alive) alive = __all_sync(FULL_MASK, lane != 0 || chunk_wait(&full[st], (uint32_t)(stage / ST) & 1, a.err));
-            const int key0 = t.key0 + k * FR_KEYS + warp * 16;  // this warp's keys
+            if (alive) alive = __all_sync(FULL_MASK, lane != 0 || chunk_wait(&full[st], stage / ST, a.err));
+            const int key0 = key_first + k * FR_KEYS + warp * 16;  // this warp's keys
             if (alive && key0 < t.hi && key0 + 16 > t.lo) {
                 unsigned char* kb = sm + st * L::STAGE;
                 // a unit that every row sees in full needs no mask; its keys are all copied
@@ -366,7 +364,7 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
                     for (int e = 0; e < 2; ++e) {
                         const int r = i * 16 + r0 + e * 8, p = t.p0 + r;
                         if (r >= t.rows) continue;
-                        const int token = chunk_token(a, p), head = it.head * a.group + p - token * a.group;
+                        const int token = chunk_token(a, p), head = w.head * a.group + p - token * a.group;
                         const long long row = t.row0 + token;
                         const float f = sum[i][e] == 0.f ? 0.f : 1.f / sum[i][e];  // (no key: 0)
                         uint16_t* to = a.out + row * a.out_stride + head * HD + c0;
@@ -397,18 +395,8 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
                         if ((lane & 3) == 0)
                             *reinterpret_cast<float2*>(part + TR * HD + 2 * r) = make_float2(mx[i][e], sum[i][e]);
                     }
-                if (begins && lane == 0) {
-                    int* d = a.desc + cta * CH_DESC;
-                    d[0] = chunk_cta_of(m, it.first + it.units - 1) - cta;
-                    d[1] = t.p0;
-                    d[2] = t.rows;
-                    d[3] = t.row0;
-                    d[4] = it.head;
-                }
             }
         }
-        k = 0;
-        it = chunk_next(a, m, it);
     }
 }
 
@@ -467,24 +455,9 @@ __global__ void __launch_bounds__(128) chunk_merge_kernel(const ChunkArgs a) {
         a.lse[row * (a.kv_heads * a.group) + head] = sum == 0.f ? -INFINITY : LN2 * (top + log2f(sum));
 }
 
-template <class... P>
-cudaError_t launch_ex(void (*kern)(P...), dim3 grid, int threads, size_t smem, bool pdl, cudaStream_t s, P... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = pdl ? 1 : 0;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, args...);
-}
-
 template <class T, int HD>
-cudaError_t merge_hd(const ChunkArgs& a, int tile_rows, int ctas, cudaStream_t s) {
-    const dim3 grid(ctas, tile_rows / 4);
+cudaError_t merge_hd(const ChunkArgs& a, int tile_rows, cudaStream_t s) {
+    const dim3 grid(a.ctas, tile_rows / 4);
     switch (tile_rows) {
         case 16: return launch_ex(chunk_merge_kernel<T, HD, 16>, grid, 128, 0, true, s, a);
         case 32: return launch_ex(chunk_merge_kernel<T, HD, 32>, grid, 128, 0, true, s, a);
@@ -495,7 +468,7 @@ cudaError_t merge_hd(const ChunkArgs& a, int tile_rows, int ctas, cudaStream_t s
 // How a call runs: tile rows, CTAs, workspace.
 struct ChunkPlan {
     int tile_rows, ctas, max_tiles, min_units;
-    size_t desc_bytes, need;
+    size_t start, desc, tiles, part, need;  // places in the workspace, its bytes
 };
 
 int chunk_plan(const mtp_chunk_attention_args* a, ChunkPlan* p) {
@@ -524,39 +497,49 @@ int chunk_plan(const mtp_chunk_attention_args* a, ChunkPlan* p) {
     const bool few = p->tile_rows != CT_TILE_ROWS;
     const long long tiles = std::min((long long)a->slots * ((packed + p->tile_rows - 1) / p->tile_rows),
                                      (long long)a->rows * group / p->tile_rows + a->slots);
-    if (tiles + a->slots > CH_MAX_TILES)
-        return invalid("chunk_attention: %lld tiles of %d rows in %d slots, at most %d together", tiles, p->tile_rows, a->slots, CH_MAX_TILES);
+    if ((long long)a->rows * group >= CH_MAX_PACKED)
+        return invalid("chunk_attention: %d rows of %d query heads per key head: below %d together", a->rows, group, CH_MAX_PACKED);
     p->max_tiles = (int)tiles;
     const int per_sm = !few ? 1 : a->head_dim == 64 && p->tile_rows == 16 ? 3 : 2, keys = few ? FR_KEYS : CT_UNIT_KEYS;
     p->min_units = few ? FR_MIN_UNITS : CT_MIN_UNITS;
     const long long units = tiles * a->n_kv_heads * (a->max_keys / keys + 2);
     p->ctas = (int)std::max(1ll, std::min((long long)sms * per_sm, (units + p->min_units - 1) / p->min_units));
-    p->desc_bytes = ((size_t)p->ctas * CH_DESC * sizeof(int) + 255) & ~(size_t)255;
-    p->need = p->desc_bytes + (size_t)p->ctas * 2 * p->tile_rows * (a->head_dim + 2) * sizeof(float);
+    auto place = [&](size_t bytes) {
+        const size_t at = p->need;
+        p->need += (bytes + 255) & ~(size_t)255;
+        return at;
+    };
+    p->need = 0;
+    p->start = place((size_t)p->ctas * sizeof(int4));
+    p->desc = place((size_t)p->ctas * CH_DESC * sizeof(int));
+    p->tiles = place((size_t)p->max_tiles * sizeof(ChunkTile));
+    p->part = place((size_t)p->ctas * 2 * p->tile_rows * (a->head_dim + 2) * sizeof(float));
     return MTP_OK;
 }
 
 template <class T, int HD, int MT>
-cudaError_t launch_rows(const ChunkArgs& a, const CUtensorMap& map, int ctas, cudaStream_t s) {
-    const size_t smem = FrLayout<HD, MT>::bytes(a.slots, a.max_tiles);
+cudaError_t launch_rows(const ChunkArgs& a, const CUtensorMap& map, cudaStream_t s) {
+    const size_t smem = FrLayout<HD, MT>::BYTES;
     const auto kern = chunk_rows_kernel<T, HD, MT>;
     const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem, true);
     if (e != cudaSuccess) return e;
-    return launch_ex(kern, dim3(ctas), FR_THREADS, smem, false, s, a, map);
+    return launch_ex(kern, dim3(a.ctas), FR_THREADS, smem, true, s, a, map);
 }
 template <class T>
-cudaError_t launch_rows_of(const ChunkArgs& a, const CUtensorMap& map, int head_dim, const ChunkPlan& p, cudaStream_t s) {
-    if (head_dim == 64)
-        return p.tile_rows == 16 ? launch_rows<T, 64, 1>(a, map, p.ctas, s) : launch_rows<T, 64, 2>(a, map, p.ctas, s);
-    return p.tile_rows == 16 ? launch_rows<T, 128, 1>(a, map, p.ctas, s) : launch_rows<T, 128, 2>(a, map, p.ctas, s);
+cudaError_t launch_kernels(const ChunkArgs& a, const CUtensorMap& map, int head_dim, int dtype, int tile_rows, cudaStream_t s) {
+    cudaError_t e = launch_chunk_plan(a, tile_rows, s);
+    if (e != cudaSuccess) return e;
+    if (tile_rows == CT_TILE_ROWS)
+        e = launch_chunk_tc(a, map, head_dim, dtype, s);
+    else if (head_dim == 64)
+        e = tile_rows == 16 ? launch_rows<T, 64, 1>(a, map, s) : launch_rows<T, 64, 2>(a, map, s);
+    else
+        e = tile_rows == 16 ? launch_rows<T, 128, 1>(a, map, s) : launch_rows<T, 128, 2>(a, map, s);
+    if (e != cudaSuccess) return e;
+    return head_dim == 64 ? merge_hd<T, 64>(a, tile_rows, s) : merge_hd<T, 128>(a, tile_rows, s);
 }
 
 }  // namespace
-
-cudaError_t launch_chunk_merge(const ChunkArgs& a, int head_dim, int tile_rows, int dtype, int ctas, cudaStream_t s) {
-    if (dtype == MTP_BF16) return head_dim == 64 ? merge_hd<Bf16, 64>(a, tile_rows, ctas, s) : merge_hd<Bf16, 128>(a, tile_rows, ctas, s);
-    return head_dim == 64 ? merge_hd<F16, 64>(a, tile_rows, ctas, s) : merge_hd<F16, 128>(a, tile_rows, ctas, s);
-}
 
 }  // namespace mtp
 
@@ -610,18 +593,20 @@ MTP_API int mtp_chunk_attention(const mtp_chunk_attention_args* a, void* workspa
         c.q_vec = aligned16(a->q) && a->q_stride % 8 == 0;
         c.out_vec = aligned16(a->out) && a->out_stride % 8 == 0;
         c.scale_log2 = a->scale * 1.4426950408889634f;
-        c.desc = static_cast<int*>(workspace);
-        c.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.desc_bytes);
+        char* ws = static_cast<char*>(workspace);
+        c.ctas = p.ctas;
+        c.start = reinterpret_cast<int4*>(ws + p.start);
+        c.desc = reinterpret_cast<int*>(ws + p.desc);
+        c.tiles = reinterpret_cast<ChunkTile*>(ws + p.tiles);
+        c.part = reinterpret_cast<float*>(ws + p.part);
         c.err = a->err_word;
         const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
         CUtensorMap map;
         if (tc_encode_cache(&map, a->kv_pool, a->dtype, a->head_dim, a->page_size,
                             (uint64_t)a->n_pages * c.page_blocks, std::min(a->page_size, FR_KEYS)) != 0)
             return report_error(MTP_ERR_CUDA, "chunk_attention: cuTensorMapEncodeTiled failed");
-        cudaError_t e = !few                    ? launch_chunk_tc(c, map, a->head_dim, a->dtype, p.ctas, s)
-                        : a->dtype == MTP_BF16 ? launch_rows_of<Bf16>(c, map, a->head_dim, p, s)
-                                               : launch_rows_of<F16>(c, map, a->head_dim, p, s);
-        if (e == cudaSuccess) e = launch_chunk_merge(c, a->head_dim, p.tile_rows, a->dtype, p.ctas, s);
+        const cudaError_t e = a->dtype == MTP_BF16 ? launch_kernels<Bf16>(c, map, a->head_dim, a->dtype, p.tile_rows, s)
+                                                   : launch_kernels<F16>(c, map, a->head_dim, a->dtype, p.tile_rows, s);
         return cuda_status(e, "chunk_attention");
     });
 }

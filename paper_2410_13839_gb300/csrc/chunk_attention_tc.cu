@@ -53,8 +53,8 @@ struct CtLayout {
     static constexpr int STAGES = HD == 64 ? 8 : 4;       // of K and of V, 64 keys each
     static constexpr uint32_t OPER = CT_SUB * (HD / 64);  // a tile of Q
     static constexpr uint32_t ATOM = CT_STEP * 128, STEP = ATOM * (HD / 64);  // 64 columns of a stage; a stage
-    static constexpr uint32_t K = 2 * OPER, V = K + STAGES * STEP, MAP = V + STAGES * STEP;
-    static size_t bytes(int slots, int tiles) { return 1024 + MAP + chunk_map_bytes(slots, tiles); }
+    static constexpr uint32_t K = 2 * OPER, V = K + STAGES * STEP;
+    static constexpr size_t BYTES = 1024 + V + STAGES * STEP;
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -135,45 +135,15 @@ constexpr uint32_t ct_idesc(int n, bool b_mn) {  // f16_idesc's types are bf16; 
 }
 
 // What a tile (0 or 1) of an item does in this CTA: its rows, and the steps [from, to) of the
-// item (two to a unit), of those of units [k0, k1), of which its rows see a key.
+// item (two to a unit), of the share's, of which its rows see a key.
 struct CtTile {
     int p0, rows, from, to;
-};
-__device__ __noinline__ CtTile ct_tile(const ChunkArgs& a, const ChunkTile& t, int tile, int k0, int k1) {
-    CtTile x;
-    x.p0 = t.p0 + tile * CT_TILE;
-    x.rows = max(0, min(CT_TILE, t.rows - tile * CT_TILE));
-    x.from = x.to = 2 * k0;
-    if (x.rows == 0) return x;
-    const int first = t.len - t.n + chunk_token(a, x.p0), last = t.len - t.n + chunk_token(a, x.p0 + x.rows - 1);
-    const int hi = max(0, last + 1), lo = a.window > 0 ? max(0, first - a.window + 1) : 0;
-    if (hi <= lo) return x;
-    x.from = max(2 * k0, (lo - t.key0) / CT_STEP);
-    x.to = max(x.from, min(2 * k1, (hi - t.key0 + CT_STEP - 1) / CT_STEP));
-    return x;
-}
-
-// A walk over the items of a share: the item, and its units [k0, k1) in the share.
-struct CtWalk {
-    ChunkItem it;
-    ChunkTile t;
-    int k0, k1;
-    __device__ __forceinline__ CtWalk(const ChunkArgs& a, const ChunkMap& m, long long u0, long long u1) {
-        it = chunk_item(a, m, u0);
-        k0 = (int)(u0 - it.first);
-        load(a, m, u1 - u0);
+    __device__ __forceinline__ CtTile(const ChunkWalk& w, int tile) {
+        p0 = w.t.p0 + tile * CT_TILE;
+        rows = max(0, min(CT_TILE, w.t.rows - tile * CT_TILE));
+        from = max(2 * w.k0, tile ? w.t.steps.z : w.t.steps.x);
+        to = max(from, min(2 * w.k1, tile ? w.t.steps.w : w.t.steps.y));
     }
-    __device__ __noinline__ void load(const ChunkArgs& a, const ChunkMap& m, long long left) {
-        const int s = chunk_slot_of(a, m, it.tile);
-        t = chunk_tile<CT_ROWS, CT_KEYS>(a, s, it.tile - m.slot_first[s]);
-        k1 = (int)min((long long)it.units, k0 + left);
-    }
-    __device__ __forceinline__ void next(const ChunkArgs& a, const ChunkMap& m, long long left) {
-        it = chunk_next(a, m, it);
-        k0 = 0;
-        if (left > 0) load(a, m, left);
-    }
-    __device__ __forceinline__ CtTile tile(const ChunkArgs& a, int g) const { return ct_tile(a, t, g, k0, k1); }
 };
 
 template <class T, int HD>
@@ -182,7 +152,6 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
     constexpr int ST = L::STAGES;
     extern __shared__ unsigned char ct_raw[];
     __shared__ uint64_t q_full[2], s_full[2][2], p_full[2][2], pv_done[2][2], k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], turn[2], drain[2];
-    __shared__ long long scan_part[CT_WARPS][2];
     __shared__ uint32_t tmem_base;
     unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(ct_raw) + 1023) & ~(uintptr_t)1023);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
@@ -208,21 +177,20 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
             mbar_init(&v_empty[i], 2);
         }
         fence_barrier_init();
-        a.desc[cta * CH_DESC] = 0;
     }
-    const ChunkMap m = chunk_map<CT_WARPS, CT_ROWS, CT_KEYS>(a, sm + L::MAP, scan_part);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_base;
     pdl_launch_dependents();
-    const long long u0 = m.units && cta < m.ctas ? chunk_border(a, m, cta) : 0;
-    const long long u1 = m.units && cta < m.ctas ? chunk_border(a, m, cta + 1) : 0;
+    pdl_wait();  // the plan
+    const int4 start = a.start[cta];
+    const int units = start.w;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
         return __all_sync(FULL_MASK, mbar_try_wait(bar, parity & 1) || chunk_wait(bar, parity, a.err)) != 0;
     };
 
-    if (u0 < u1) {
+    if (units > 0) {
         if (warp == 9 || warp == 11) {
             // ---- copies of the keys (warp 9) or values (warp 11): a lane per piece of a step ----
             const int kv = warp == 11, P = 1 << a.page_shift, box = min(P, CT_STEP), per = CT_STEP / box;
@@ -230,7 +198,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
             const bool mine = half < HD / 64;
             unsigned char* ring = sm + (kv ? L::V : L::K) + half * L::ATOM + sub * box * 128;
             uint64_t *full = kv ? v_full : k_full, *empty = kv ? v_empty : k_empty;
-            CtWalk w(a, m, u0, u1);
+            ChunkWalk w(a, start);
             int step = 2 * w.k0, n = 0;
             bool ok = true;
             // pages [base, base + 32) of the slot, one per lane, and the 32 after them
@@ -239,17 +207,17 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
             auto lookup = [&](int first) { return first + lane < a.bt_stride ? __ldg(table + first + lane) : -1; };
             auto enter = [&]() {  // an item's first step
                 table = a.block_table + (size_t)w.t.slot * a.bt_stride;
-                key_first = w.t.key0;
+                key_first = w.key0<CT_KEYS>();
                 hi = w.t.hi;
                 lo = w.t.lo;
                 last = 2 * w.k1;
-                head_block = a.layer_block + kv * a.kv_heads + w.it.head;
+                head_block = a.layer_block + kv * a.kv_heads + w.head;
                 base = (key_first + step * CT_STEP) >> a.page_shift & ~31;
                 pages = lookup(base);
                 ahead = lookup(base + 32);
             };
             enter();
-            for (const int steps = 2 * (int)(u1 - u0); n < steps; ++n) {
+            for (const int steps = 2 * units; n < steps; ++n) {
                 const int st = n % ST, key = key_first + step * CT_STEP + sub * box, index = key >> a.page_shift;
                 if (index - base >= 32) {  // (the same in all lanes: a step's pages lie in one aligned group)
                     base += 32;
@@ -266,7 +234,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                 __syncwarp();
                 if (wanted) tma_cache(ring + st * L::STEP, &map, half * 64, key & (P - 1), block, &full[st]);
                 if (++step == last && n + 1 < steps) {
-                    w.next(a, m, u1 - u0 - (n + 1) / 2);
+                    w.next(a);
                     step = 0;
                     enter();
                 }
@@ -279,8 +247,8 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
             if (elect_one()) {
                 constexpr uint32_t IDESC_S = ct_idesc<T>(CT_STEP, false), IDESC_O = ct_idesc<T>(HD, true);
                 const int tile = warp == 10;
-                CtWalk w(a, m, u0, u1);
-                CtTile x = w.tile(a, tile), y = x;  // y: the unit before's
+                ChunkWalk w(a, start);
+                CtTile x(w, tile), y = x;  // y: the unit before's
                 const uint64_t q = sw128_desc(smem_addr(sm + tile * L::OPER)), k0 = sw128_desc(smem_addr(sm + L::K)),
                                v0 = v_desc(smem_addr(sm + L::V), L::ATOM);
                 const uint32_t s_tmem = tmem + TM_S + tile * 128, o_tmem = tmem + TM_O + tile * 128;
@@ -290,14 +258,14 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                 int k = w.k0, k1 = w.k1;
                 // the products of the steps of unit n - 1, between them the scores of unit n's: S of a step comes after
                 // the P V of two steps before, in whose place it goes, and the softmax has the step between to work on
-                for (int n = 0, units = (int)(u1 - u0); ok && n <= units; ++n) {
+                for (int n = 0; ok && n <= units; ++n) {
                     const int at = k - 1;
                     const bool more = n < units;
                     if (n > 0 && k == k1) {
-                        w.next(a, m, units - n);
+                        w.next(a);
                         k = 0;
                         k1 = w.k1;
-                        if (more) x = w.tile(a, tile);
+                        x = CtTile(w, tile);
                     }
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
@@ -362,19 +330,30 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
             const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), ts = lanes + TM_S + g * 128, to = lanes + TM_O + g * 128;
             unsigned char* qs = sm + g * L::OPER;
             const int heads = a.kv_heads * a.group;
-            CtWalk w(a, m, u0, u1);
-            CtTile x = w.tile(a, g);
+            ChunkWalk w(a, start);
+            CtTile x(w, g);
             int n = 0, seen[2] = {0, 0};  // steps of either half, which s_full and pv_done count too
             bool ok = true;
-            // Q of an item on its way into shared memory: 16 bytes a thread and step, rows past the tile zero
-            auto load_q = [&](const CtWalk& w, const CtTile& x) {
-#pragma unroll 1
-                for (int i = r; i < CT_TILE * (HD / 8); i += 128) {
-                    const int row = i / (HD / 8), c = i % (HD / 8), p = x.p0 + row;
-                    unsigned char* dst = qs + (c >> 3) * CT_SUB + row * 128 + (((c & 7) ^ (row & 7)) << 4);
-                    const bool live = row < x.rows;
-                    const int token = chunk_token(a, p);
-                    const uint16_t* src = live ? a.q + (w.t.row0 + token) * a.q_stride + (w.it.head * a.group + p - token * a.group) * HD + c * 8 : a.q;
+            // a row's place in q and out, without the strides
+            auto place = [&](const ChunkWalk& w, int p, int& head) {
+                const int token = chunk_token(a, p);
+                head = w.head * a.group + p - token * a.group;
+                return (long long)w.t.row0 + token;
+            };
+            // Q of an item on its way into shared memory: a warp brings its own 32 rows, 16 bytes a thread and step,
+            // HD / 8 threads to a row; rows past the tile are zeros
+            auto load_q = [&](const ChunkWalk& w, const CtTile& x) {
+                constexpr int PER = HD / 8, ROWS = 32 / PER;
+                int head;
+                const long long row = place(w, x.p0 + min(r, max(x.rows - 1, 0)), head);
+                const long long mine = row * a.q_stride + head * HD;
+                const int c = lane % PER;
+#pragma unroll 4
+                for (int i = 0; i < 32; i += ROWS) {
+                    const int from = i + lane / PER, at = (r & ~31) + from;
+                    const uint16_t* src = a.q + __shfl_sync(FULL_MASK, mine, from) + c * 8;
+                    unsigned char* dst = qs + (c >> 3) * CT_SUB + at * 128 + (((c & 7) ^ (at & 7)) << 4);
+                    const bool live = at < x.rows;
                     if (a.q_vec) {
                         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(dst)), "l"(src), "r"(live ? 16 : 0) : "memory");
                     } else {
@@ -396,28 +375,23 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                 load_q(w, x);
                 q_there();
             }
-            for (long long u = u0; u < u1;) {
+            for (;;) {
                 const int len = w.k1 - w.k0;
                 // (rows past the tile's are not looked at: as if they saw every key)
-                const int pos = r < x.rows ? w.t.len - w.t.n + chunk_token(a, x.p0 + r) : INT_MAX;
+                const int pos = r < x.rows ? w.t.base + chunk_token(a, x.p0 + r) : INT_MAX;
                 const int window = a.window > 0 && r < x.rows ? a.window : INT_MAX;
                 // steps [inner_from, inner_to): every row of the warp sees all of their keys (and some row of the item does,
                 // where the warp has none)
-                const int key_first = w.t.key0, hi = w.t.hi, lo = w.t.lo, share = 2 * (n - w.k0);
+                const int key_first = w.key0<CT_KEYS>(), hi = w.t.hi, lo = w.t.lo, share = 2 * (n - w.k0);
                 const int pos0 = __reduce_min_sync(FULL_MASK, pos), pos1 = __reduce_max_sync(FULL_MASK, r < x.rows ? pos : INT_MIN);
                 int inner_to = (hi - key_first) / CT_STEP, inner_from = (lo - key_first + CT_STEP - 1) / CT_STEP;
                 if (pos0 < hi) inner_to = pos0 < key_first ? 0 : min(inner_to, (pos0 + 1 - key_first) / CT_STEP);
                 if (a.window > 0 && pos1 >= a.window + key_first) inner_from = max(inner_from, (pos1 - a.window - key_first) / CT_STEP + 1);
                 float ref = -INFINITY, sum = 0.f;
-                const bool more = u + len < u1;  // the share has an item after this one
-                bool q_next = false;             // whose Q this group has asked for
-                auto ask_q = [&]() {
-                    CtWalk next = w;
-                    next.next(a, m, u1 - u - len);
-                    const CtTile y = next.tile(a, g);
-                    q_next = y.from < y.to;
-                    if (q_next) load_q(next, y);
-                };
+                ChunkWalk next = w;
+                next.next(a);
+                const CtTile y(next, g);
+                const bool more = next.left > 0, q_next = more && y.from < y.to;  // an item after this one; one with Q
                 bool there = false;  // the step's scores are known to be there
                 float s0[32], s1[32];
 #pragma unroll 1
@@ -432,7 +406,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                     tmem_ld_issue<32>(tsh + 32, s1);
                     if (half) ++seen[1]; else ++seen[0];
                     const uint32_t next_phase = half ? seen[0] : seen[1];
-                    if (!onward && more) ask_q();  // the tile's last S is there: Q's space is free
+                    if (!onward && q_next) load_q(next, y);  // the tile's last S is there: Q's space is free
                     __syncwarp();
                     tmem_ld_wait();
                     tmem_ld_done(s0);
@@ -532,8 +506,10 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                     if (lane == 0) mbar_arrive(&p_full[g][half]);
                 }
                 if (!ok) break;
-                if (x.from >= x.to && more) ask_q();  // (nothing here: Q's space was free already)
-                if (q_next) q_there();
+                if (q_next) {
+                    if (x.from >= x.to) load_q(next, y);  // (nothing here: Q's space was free already)
+                    q_there();
+                }
                 // ---- the item's rows ----
                 const bool any = x.from < x.to;
                 if (any) {
@@ -542,9 +518,9 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                     if (!ok) break;
                     tc_fence_after();
                 }
-                const bool begins = w.k0 == 0, ends = w.k1 == w.it.units, whole = begins && ends;
-                const int p = x.p0 + r, token = chunk_token(a, p), head = w.it.head * a.group + p - token * a.group;
-                const long long row = w.t.row0 + token;
+                const bool begins = w.begins(), whole = begins && w.ends();
+                int head;
+                const long long row = place(w, x.p0 + r, head);
                 const bool live = r < x.rows;
                 const float f = sum == 0.f ? 0.f : 1.f / sum;  // (no key: 0)
                 float* part = a.part + ((size_t)cta * 2 + begins) * CT_ROWS * (HD + 2);
@@ -582,19 +558,11 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                 }
                 if (live && whole && a.lse) a.lse[row * heads + head] = sum == 0.f ? -INFINITY : LN2 * (ref + log2f(sum));
                 if (live && !whole) *reinterpret_cast<float2*>(part + CT_ROWS * HD + 2 * (g * CT_TILE + r)) = make_float2(ref, sum);
-                if (tid == 0 && begins && !ends) {
-                    int* d = a.desc + cta * CH_DESC;
-                    d[0] = chunk_cta_of(m, w.it.first + w.it.units - 1) - cta;
-                    d[1] = w.t.p0;
-                    d[2] = w.t.rows;
-                    d[3] = w.t.row0;
-                    d[4] = w.it.head;
-                }
                 tc_fence_before();  // O is read before the next item's product overwrites it
-                u += len;
+                if (!more) break;
                 n += len;
-                w.next(a, m, u1 - u);
-                if (more) x = w.tile(a, g);
+                w = next;
+                x = y;
             }
         }
     }
@@ -605,20 +573,17 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
 }
 
 template <class T, int HD>
-cudaError_t launch_tc(const ChunkArgs& a, const CUtensorMap& map, int ctas, cudaStream_t s) {
-    const size_t smem = CtLayout<HD>::bytes(a.slots, a.max_tiles);
+cudaError_t launch_tc(const ChunkArgs& a, const CUtensorMap& map, cudaStream_t s) {
     const auto kern = chunk_tc_kernel<T, HD>;
-    const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem);
-    if (e != cudaSuccess) return e;
-    kern<<<ctas, CT_THREADS, smem, s>>>(a, map);
-    return cudaGetLastError();
+    const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), CtLayout<HD>::BYTES);
+    return e == cudaSuccess ? launch_ex(kern, dim3(a.ctas), CT_THREADS, CtLayout<HD>::BYTES, true, s, a, map) : e;
 }
 
 }  // namespace
 
-cudaError_t launch_chunk_tc(const ChunkArgs& a, const CUtensorMap& map, int head_dim, int dtype, int ctas, cudaStream_t s) {
-    if (dtype == MTP_BF16) return head_dim == 64 ? launch_tc<Bf16, 64>(a, map, ctas, s) : launch_tc<Bf16, 128>(a, map, ctas, s);
-    return head_dim == 64 ? launch_tc<F16, 64>(a, map, ctas, s) : launch_tc<F16, 128>(a, map, ctas, s);
+cudaError_t launch_chunk_tc(const ChunkArgs& a, const CUtensorMap& map, int head_dim, int dtype, cudaStream_t s) {
+    if (dtype == MTP_BF16) return head_dim == 64 ? launch_tc<Bf16, 64>(a, map, s) : launch_tc<Bf16, 128>(a, map, s);
+    return head_dim == 64 ? launch_tc<F16, 64>(a, map, s) : launch_tc<F16, 128>(a, map, s);
 }
 
 }  // namespace mtp
