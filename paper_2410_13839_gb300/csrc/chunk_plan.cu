@@ -9,24 +9,28 @@ namespace {
 
 constexpr int PL_THREADS = 1024, PL_WARPS = PL_THREADS / 32;
 
-// rows of slot s, as far as they lie in the row buffers
-__device__ __forceinline__ void slot_rows(const ChunkArgs& a, int s, int& row0, int& n) {
-    row0 = a.cu_rows[s];
-    n = a.cu_rows[s + 1] - row0;
-    if (row0 < 0 || row0 > a.rows || n < 0) n = 0;
-    n = min(n, a.rows - row0);
+// A slot in shared memory: its first row, new tokens (as far as they lie in the row buffers), length.
+struct Slot {
+    int row0, n, len;
+};
+__device__ __forceinline__ Slot load_slot(const ChunkArgs& a, int s) {
+    Slot x;
+    x.row0 = a.cu_rows[s];
+    x.n = a.cu_rows[s + 1] - x.row0;
+    x.len = max(0, min(a.kv_lens[s], a.bt_stride << a.page_shift));
+    if (x.row0 < 0 || x.row0 > a.rows || x.n < 0) x.n = 0;
+    x.n = min(x.n, a.rows - x.row0);
+    return x;
 }
 
 template <int TR, int KT>
-__device__ __forceinline__ ChunkTile make_tile(const ChunkArgs& a, int slot, int t) {
+__device__ __forceinline__ ChunkTile make_tile(const ChunkArgs& a, int slot, const Slot& y, int t) {
     ChunkTile x;
-    int n;
     x.slot = slot;
-    slot_rows(a, slot, x.row0, n);
-    const int len = max(0, min(a.kv_lens[slot], a.bt_stride << a.page_shift));
+    x.row0 = y.row0;
     x.p0 = t * TR;
-    x.rows = min(n * a.group - x.p0, TR);
-    x.base = len - n;
+    x.rows = min(y.n * a.group - x.p0, TR);
+    x.base = y.len - y.n;
     const int first = x.base + chunk_token(a, x.p0), last = x.base + chunk_token(a, x.p0 + x.rows - 1);  // positions
     x.hi = max(0, last + 1);
     x.lo = a.window > 0 ? min(x.hi, max(0, first - a.window + 1)) : 0;
@@ -43,6 +47,23 @@ __device__ __forceinline__ ChunkTile make_tile(const ChunkArgs& a, int slot, int
     return x;
 }
 
+// Exclusive prefix sum of x over the block, and the total.
+__device__ __forceinline__ uint32_t scan(uint32_t x, uint32_t* part, uint32_t& sum) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t y = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t u = __shfl_up_sync(FULL_MASK, y, o);
+        if (lane >= o) y += u;
+    }
+    __syncthreads();  // `part` may still be read from an earlier call
+    if (lane == 31) part[warp] = y;
+    __syncthreads();
+    const uint32_t mine = lane < PL_WARPS ? part[lane] : 0;
+    sum = __reduce_add_sync(FULL_MASK, mine);
+    return __reduce_add_sync(FULL_MASK, lane < warp ? mine : 0) + y - x;
+}
+
 template <class T>
 __device__ __forceinline__ int owner(const T* first, int n, T x) {  // largest i in [0, n) with first[i] <= x
     int lo = 0, hi = n;
@@ -56,94 +77,51 @@ __device__ __forceinline__ int owner(const T* first, int n, T x) {  // largest i
 struct Map {
     const uint32_t* unit_first;  // [tiles + 1]: first unit of every tile, counted for one key head
     int tiles, ctas, snap;
-    long long units;             // of all key heads
 };
+template <class U>
 struct Item {
     int tile, head, units;
-    long long first;  // its first unit
+    U first;  // its first unit
 };
-__device__ __forceinline__ Item item_of(const ChunkArgs& a, const Map& m, long long unit) {
-    Item x;
-    x.tile = owner(m.unit_first, m.tiles, (uint32_t)(unit / a.kv_heads));
-    const long long first = (long long)m.unit_first[x.tile] * a.kv_heads;
+template <class U>
+__device__ __forceinline__ Item<U> item_of(const ChunkArgs& a, const Map& m, U unit) {
+    Item<U> x;
+    x.tile = owner(m.unit_first, m.tiles, (uint32_t)(unit / (U)a.kv_heads));
+    const U first = (U)m.unit_first[x.tile] * (U)a.kv_heads;
     x.units = (int)(m.unit_first[x.tile + 1] - m.unit_first[x.tile]);
     x.head = (int)((uint32_t)(unit - first) / (uint32_t)x.units);  // (an item's units and heads: below 2^32 together)
-    x.first = first + (long long)x.head * x.units;
+    x.first = first + (U)x.head * (U)x.units;
     return x;
 }
-// First unit of CTA c's share.  Items of at most m.snap units are not cut: the border goes to
-// their nearer end.
-__device__ __forceinline__ long long border(const ChunkArgs& a, const Map& m, int c) {
-    const long long u = c >= m.ctas ? m.units : m.units * c / m.ctas;
-    if (u >= m.units || m.snap == 0) return u;
-    const Item x = item_of(a, m, u);
-    if (x.units > m.snap) return u;
-    return u - x.first <= x.units / 2 ? x.first : x.first + x.units;
-}
 
-template <int TR, int KT>
-__global__ void __launch_bounds__(PL_THREADS) chunk_plan_kernel(const __grid_constant__ ChunkArgs a) {
-    extern __shared__ int pl_sm[];
-    __shared__ long long part[PL_WARPS][2];
-    int* slot_first = pl_sm;                                              // [slots + 1]: first tile of every slot
-    uint32_t* unit_first = reinterpret_cast<uint32_t*>(pl_sm + a.slots + 1);  // [tiles + 1]
-    const int tid = threadIdx.x;
-    pdl_launch_dependents();
-    long long base = 0, unused = 0, sum, none;
-    for (int s0 = 0; s0 < a.slots; s0 += PL_THREADS) {
-        const int s = s0 + tid;
-        long long x = 0;
-        if (s < a.slots) {
-            int row0, n;
-            slot_rows(a, s, row0, n);
-            x = ((long long)n * a.group + TR - 1) / TR;
+// Shares and merges, in 32 bits where the units times the CTAs fit (64-bit divisions were most of
+// the plan's time).  CTA c's share begins at c / ctas of the units; items of at most m.snap
+// units are not cut: the border goes to their nearer end.
+template <class U>
+__device__ __forceinline__ void share_out(const ChunkArgs& a, const Map& m, U units, U* borders) {
+    for (int c = threadIdx.x; c <= a.ctas; c += PL_THREADS) {
+        U u = c >= m.ctas ? units : units * (U)c / (U)m.ctas;
+        if (u < units && m.snap > 0) {
+            const Item<U> x = item_of<U>(a, m, u);
+            if (x.units <= m.snap) u = u - x.first <= (U)(x.units / 2) ? x.first : x.first + (U)x.units;
         }
-        block_scan2<PL_WARPS>(x, unused, part, sum, none);
-        if (s < a.slots) slot_first[s] = (int)min(base + x, (long long)a.max_tiles);
-        base += sum;
+        borders[c] = u;
     }
-    Map m;
-    m.unit_first = unit_first;
-    m.tiles = (int)min(base, (long long)a.max_tiles);
-    if (tid == 0) slot_first[a.slots] = m.tiles;
     __syncthreads();
-    base = 0;
-    for (int j0 = 0; j0 < m.tiles; j0 += PL_THREADS) {
-        const int j = j0 + tid;
-        long long x = 0;
-        if (j < m.tiles) {
-            const int s = owner(slot_first, a.slots, j);
-            const ChunkTile t = make_tile<TR, KT>(a, s, j - slot_first[s]);
-            const int4* from = reinterpret_cast<const int4*>(&t);
-            int4* to = reinterpret_cast<int4*>(a.tiles + j);
-            to[0] = from[0];
-            to[1] = from[1];
-            to[2] = from[2];
-            x = t.units;
-        }
-        block_scan2<PL_WARPS>(x, unused, part, sum, none);
-        if (j < m.tiles) unit_first[j] = (uint32_t)(base + x);
-        base += sum;
-    }
-    if (tid == 0) unit_first[m.tiles] = (uint32_t)base;
-    __syncthreads();
-    m.units = base * a.kv_heads;
-    m.ctas = (int)min((long long)a.ctas, max(1ll, (m.units + a.min_units - 1) / a.min_units));
-    m.snap = a.snap ? (int)min(m.units / m.ctas / a.snap, 1ll << 30) : 0;
-    for (int c = tid; c < a.ctas; c += PL_THREADS) {
-        const long long u0 = border(a, m, c), u1 = border(a, m, c + 1);
+    for (int c = threadIdx.x; c < a.ctas; c += PL_THREADS) {
+        const U u0 = borders[c], u1 = borders[c + 1];
         int4 start = make_int4(0, 0, 0, 0);
         int more = 0;
         if (u0 < u1) {
-            const Item x = item_of(a, m, u0);
+            const Item<U> x = item_of<U>(a, m, u0);
             start = make_int4(x.tile, x.head, (int)(u0 - x.first), (int)(u1 - u0));
-            if (u1 < m.units) {
-                const Item y = item_of(a, m, u1);
-                if (y.first < u1 && y.first >= u0) {  // begins here and goes on: up to the CTA with its last unit
-                    const long long last = y.first + y.units - 1;
-                    more = (int)(((last + 1) * m.ctas - 1) / m.units) - c;
-                    int* d = a.desc + c * CH_DESC;
+            if (u1 < units) {
+                const Item<U> y = item_of<U>(a, m, u1);
+                if (y.first < u1 && y.first >= u0) {  // begins here and goes on, up to the CTA with its last unit
+                    more = 1;
+                    while (borders[c + 1 + more] < y.first + (U)y.units) ++more;
                     const ChunkTile& t = a.tiles[y.tile];
+                    int* d = a.desc + c * CH_DESC;
                     d[1] = t.p0;
                     d[2] = t.rows;
                     d[3] = t.row0;
@@ -156,9 +134,73 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan_kernel(const __grid_con
     }
 }
 
+// Shared memory: borders (8 bytes each), slots, first tile of every slot, first unit of every tile.
+size_t plan_smem(const ChunkArgs& a) {
+    return (size_t)(a.ctas + 1) * 8 + (size_t)a.slots * sizeof(Slot) + (size_t)(a.slots + a.max_tiles + 2) * 4;
+}
+
+template <int TR, int KT>
+__global__ void __launch_bounds__(PL_THREADS) chunk_plan_kernel(const __grid_constant__ ChunkArgs a) {
+    extern __shared__ __align__(8) unsigned char pl_sm[];
+    __shared__ uint32_t part[PL_WARPS];
+    Slot* slots = reinterpret_cast<Slot*>(pl_sm + (size_t)(a.ctas + 1) * 8);
+    uint32_t* slot_first = reinterpret_cast<uint32_t*>(slots + a.slots);  // [slots + 1]
+    uint32_t* unit_first = slot_first + a.slots + 1;                      // [tiles + 1]
+    const int tid = threadIdx.x;
+    pdl_launch_dependents();
+    uint32_t base = 0, sum;  // (tiles: the kept rows of all slots lie in the buffers; a caller's wrong row starts: cut below)
+    for (int s0 = 0; s0 < a.slots; s0 += PL_THREADS) {
+        const int s = s0 + tid;
+        uint32_t x = 0;
+        if (s < a.slots) {
+            const Slot y = load_slot(a, s);
+            slots[s] = y;
+            x = ((uint32_t)y.n * a.group + TR - 1) / TR;
+        }
+        x = scan(x, part, sum);
+        if (s < a.slots) slot_first[s] = min(base + x, (uint32_t)a.max_tiles);
+        base = min(base + sum, (uint32_t)a.max_tiles);
+    }
+    Map m;
+    m.unit_first = unit_first;
+    m.tiles = (int)base;
+    if (tid == 0) slot_first[a.slots] = base;
+    __syncthreads();
+    base = 0;
+    for (int j0 = 0; j0 < m.tiles; j0 += PL_THREADS) {
+        const int j = j0 + tid;
+        uint32_t x = 0;
+        if (j < m.tiles) {
+            const int s = owner(slot_first, a.slots, (uint32_t)j);
+            const ChunkTile t = make_tile<TR, KT>(a, s, slots[s], j - (int)slot_first[s]);
+            const int4* from = reinterpret_cast<const int4*>(&t);
+            int4* to = reinterpret_cast<int4*>(a.tiles + j);
+            to[0] = from[0];
+            to[1] = from[1];
+            to[2] = from[2];
+            x = t.units;
+        }
+        x = scan(x, part, sum);
+        if (j < m.tiles) unit_first[j] = base + x;
+        base += sum;
+    }
+    if (tid == 0) unit_first[m.tiles] = base;
+    __syncthreads();
+    const unsigned long long units = (unsigned long long)base * a.kv_heads;
+    const bool narrow = units * a.ctas < 1ull << 32;
+    m.ctas = (int)min((unsigned long long)a.ctas,
+                      max(1ull, narrow ? (unsigned long long)(((uint32_t)units + a.min_units - 1) / a.min_units)
+                                       : (units + a.min_units - 1) / a.min_units));
+    m.snap = !a.snap ? 0 : narrow ? (int)((uint32_t)units / m.ctas / a.snap) : (int)min(units / m.ctas / a.snap, 1ull << 30);
+    if (narrow)
+        share_out<uint32_t>(a, m, (uint32_t)units, reinterpret_cast<uint32_t*>(pl_sm));
+    else
+        share_out<unsigned long long>(a, m, units, reinterpret_cast<unsigned long long*>(pl_sm));
+}
+
 template <int TR, int KT>
 cudaError_t launch(const ChunkArgs& a, cudaStream_t s) {
-    const size_t smem = (size_t)(a.slots + a.max_tiles + 2) * 4;
+    const size_t smem = plan_smem(a);
     const auto kern = chunk_plan_kernel<TR, KT>;
     const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem);
     return e == cudaSuccess ? launch_ex(kern, dim3(1), PL_THREADS, smem, false, s, a) : e;
