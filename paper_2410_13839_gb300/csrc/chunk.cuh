@@ -19,7 +19,7 @@
 
 namespace mtp {
 
-constexpr int CH_MAX_TILES = 16384, CH_MAX_SLOTS = 4096, CH_MAX_PACKED = 1 << 21;
+constexpr int CH_MAX_SLOTS = 4096, CH_MAX_PACKED = 1 << 21;
 constexpr int CH_STEP = 64;  // keys of a step of the many-rows kernel
 
 // A tile in the workspace: three 16-byte pieces.
@@ -29,6 +29,11 @@ struct ChunkTile {
     int4 steps;                // steps of CH_STEP keys [x, y) of which the first 128 rows see a key, [z, w) the others
 };
 static_assert(sizeof(ChunkTile) == 48, "three pieces");
+
+// Tiles of 128 rows of a CTA of the many-rows kernel, and CTAs of an SM (they fill TMEM).  One tile of 64
+// dims and two CTAs: bound by the softmax, they need no shared keys, and a tile's start and
+// end lie behind the other CTA's work.  128 dims: two tiles, for half the key and value copies.
+constexpr int chunk_tc_tiles(int head_dim) { return head_dim == 64 ? 1 : 2; }
 
 struct ChunkArgs {
     const uint16_t* q;
@@ -98,7 +103,7 @@ struct ChunkWalk {
     __device__ __forceinline__ bool ends() const { return k1 == t.units; }
 };
 
-cudaError_t launch_chunk_plan(const ChunkArgs& a, int tile_rows, cudaStream_t s);
+cudaError_t launch_chunk_plan(const ChunkArgs& a, int tile_rows, cudaStream_t s);  // 16, 32; 128, 256: many rows
 cudaError_t launch_chunk_tc(const ChunkArgs& a, const CUtensorMap& map, int head_dim, int dtype, cudaStream_t s);
 
 template <class... P>

@@ -32,7 +32,7 @@ namespace {
 
 constexpr int FR_KEYS = 64, FR_WARPS = 5, FR_THREADS = FR_WARPS * 32, FR_CONSUMERS = 128;
 constexpr int FR_MIN_UNITS = 4, CT_MIN_UNITS = 2, CT_SNAP = 3;  // fewest units of a CTA
-constexpr int FR_MAX_ROWS = 32, CT_TILE_ROWS = 256, CT_UNIT_KEYS = 128;
+constexpr int FR_MAX_ROWS = 32, CT_UNIT_KEYS = 128;
 constexpr float LN2 = 0.69314718055994531f;
 
 __device__ __forceinline__ float ex2(float x) {
@@ -461,7 +461,7 @@ cudaError_t merge_hd(const ChunkArgs& a, int tile_rows, cudaStream_t s) {
     switch (tile_rows) {
         case 16: return launch_ex(chunk_merge_kernel<T, HD, 16>, grid, 128, 0, true, s, a);
         case 32: return launch_ex(chunk_merge_kernel<T, HD, 32>, grid, 128, 0, true, s, a);
-        default: return launch_ex(chunk_merge_kernel<T, HD, 256>, grid, 128, 0, true, s, a);
+        default: return launch_ex(chunk_merge_kernel<T, HD, 128 * chunk_tc_tiles(HD)>, grid, 128, 0, true, s, a);
     }
 }
 
@@ -493,14 +493,14 @@ int chunk_plan(const mtp_chunk_attention_args* a, ChunkPlan* p) {
     }
     const int group = a->n_heads / a->n_kv_heads;
     const long long packed = (long long)std::min(a->max_new, a->rows) * group;  // rows of a slot and key head
-    p->tile_rows = packed <= 16 ? 16 : packed <= FR_MAX_ROWS ? 32 : CT_TILE_ROWS;
-    const bool few = p->tile_rows != CT_TILE_ROWS;
+    p->tile_rows = packed <= 16 ? 16 : packed <= FR_MAX_ROWS ? 32 : 128 * chunk_tc_tiles(a->head_dim);
+    const bool few = p->tile_rows <= FR_MAX_ROWS;
     const long long tiles = std::min((long long)a->slots * ((packed + p->tile_rows - 1) / p->tile_rows),
                                      (long long)a->rows * group / p->tile_rows + a->slots);
     if ((long long)a->rows * group >= CH_MAX_PACKED)
         return invalid("chunk_attention: %d rows of %d query heads per key head: below %d together", a->rows, group, CH_MAX_PACKED);
     p->max_tiles = (int)tiles;
-    const int per_sm = !few ? 1 : a->head_dim == 64 && p->tile_rows == 16 ? 3 : 2, keys = few ? FR_KEYS : CT_UNIT_KEYS;
+    const int per_sm = !few ? 3 - chunk_tc_tiles(a->head_dim) : a->head_dim == 64 && p->tile_rows == 16 ? 3 : 2, keys = few ? FR_KEYS : CT_UNIT_KEYS;
     p->min_units = few ? FR_MIN_UNITS : CT_MIN_UNITS;
     const long long units = tiles * a->n_kv_heads * (a->max_keys / keys + 2);
     p->ctas = (int)std::max(1ll, std::min((long long)sms * per_sm, (units + p->min_units - 1) / p->min_units));
@@ -529,7 +529,7 @@ template <class T>
 cudaError_t launch_kernels(const ChunkArgs& a, const CUtensorMap& map, int head_dim, int dtype, int tile_rows, cudaStream_t s) {
     cudaError_t e = launch_chunk_plan(a, tile_rows, s);
     if (e != cudaSuccess) return e;
-    if (tile_rows == CT_TILE_ROWS)
+    if (tile_rows > FR_MAX_ROWS)
         e = launch_chunk_tc(a, map, head_dim, dtype, s);
     else if (head_dim == 64)
         e = tile_rows == 16 ? launch_rows<T, 64, 1>(a, map, s) : launch_rows<T, 64, 2>(a, map, s);
@@ -588,7 +588,7 @@ MTP_API int mtp_chunk_attention(const mtp_chunk_attention_args* a, void* workspa
         c.page_blocks = a->layers * 2 * a->n_kv_heads;
         c.layer_block = a->layer * 2 * a->n_kv_heads;
         c.window = a->window; c.max_tiles = p.max_tiles; c.min_units = p.min_units;
-        const bool few = p.tile_rows != CT_TILE_ROWS;
+        const bool few = p.tile_rows <= FR_MAX_ROWS;
         c.snap = few ? 0 : CT_SNAP;
         c.q_vec = aligned16(a->q) && a->q_stride % 8 == 0;
         c.out_vec = aligned16(a->out) && a->out_stride % 8 == 0;

@@ -39,21 +39,24 @@
 namespace mtp {
 namespace {
 
-constexpr int CT_ROWS = 256, CT_TILE = 128, CT_KEYS = 128;
-constexpr int CT_WARPS = 12, CT_THREADS = CT_WARPS * 32;  // two softmax groups of four, MMAs of A, copies of K, MMAs of B, copies of V
-constexpr uint32_t CT_SUB = 128 * 128;                    // 128 rows of 128 bytes
-constexpr int CT_STEP = 64;  // keys of a step: the scores that a thread holds
-constexpr uint32_t TM_S = 0, TM_O = 256, TM_COLS = 512;  // tile t, step s: S at 128 t + 64 (s & 1), O at 256 + 128 t
+constexpr int CT_TILE = 128, CT_KEYS = 128;
+constexpr int CT_STEP = CH_STEP;        // keys of a step: the scores that a thread holds
+constexpr uint32_t CT_SUB = 128 * 128;  // 128 rows of 128 bytes
 constexpr int CT_HANDOVER = 2;  // MMAs of S before whose end the other tile may go on
 constexpr float LAG = 8.f, LIMIT = 32768.f;
 constexpr float LN2 = 0.69314718055994531f;
 
+// Tiles, warps and shared memory of a CTA.
 template <int HD>
 struct CtLayout {
-    static constexpr int STAGES = HD == 64 ? 8 : 4;       // of K and of V, 64 keys each
+    static constexpr int TILES = chunk_tc_tiles(HD), STAGES = 4;  // stages: of K and of V, 64 keys each
+    static constexpr int MMA = 4 * TILES, COPY_K = 5 * TILES, COPY_V = COPY_K + 1;  // the first MMA warp, the copying warps
+    static constexpr int WARPS = (COPY_V + 4) / 4 * 4, THREADS = WARPS * 32;
+    // TMEM: tile t, step s: S at 128 t + 64 (s & 1), O after the tiles' S
+    static constexpr uint32_t TM_S = 0, TM_O = 128 * TILES, TM_O_TILE = 128, TM_COLS = TILES == 1 ? 256 : 512;
     static constexpr uint32_t OPER = CT_SUB * (HD / 64);  // a tile of Q
     static constexpr uint32_t ATOM = CT_STEP * 128, STEP = ATOM * (HD / 64);  // 64 columns of a stage; a stage
-    static constexpr uint32_t K = 2 * OPER, V = K + STAGES * STEP;
+    static constexpr uint32_t K = TILES * OPER, V = K + STAGES * STEP;
     static constexpr size_t BYTES = 1024 + V + STAGES * STEP;
 };
 
@@ -147,20 +150,21 @@ struct CtTile {
 };
 
 template <class T, int HD>
-__global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ CUtensorMap map) {
+__global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES) chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ CUtensorMap map) {
     using L = CtLayout<HD>;
-    constexpr int ST = L::STAGES;
+    constexpr int ST = L::STAGES, TILES = L::TILES;
+    constexpr uint32_t TM_S = L::TM_S, TM_O = L::TM_O;
     extern __shared__ unsigned char ct_raw[];
-    __shared__ uint64_t q_full[2], s_full[2][2], p_full[2][2], pv_done[2][2], k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], turn[2], drain[2];
+    __shared__ uint64_t q_full[TILES], s_full[TILES][2], p_full[TILES][2], pv_done[TILES][2], k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], turn[TILES], drain[TILES];
     __shared__ uint32_t tmem_base;
     unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(ct_raw) + 1023) & ~(uintptr_t)1023);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
-    if (warp == 8) {
-        tmem_alloc(&tmem_base, TM_COLS);
+    if (warp == L::MMA) {
+        tmem_alloc(&tmem_base, L::TM_COLS);
         tmem_relinquish();
     }
     if (tid == 0) {
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < TILES; ++i) {
             mbar_init(&drain[i], 1);
             mbar_init(&turn[i], 1);
             mbar_init(&q_full[i], 4);
@@ -172,9 +176,9 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
         }
         for (int i = 0; i < ST; ++i) {
             mbar_init(&k_full[i], 1);
-            mbar_init(&k_empty[i], 2);  // both tiles' MMAs
+            mbar_init(&k_empty[i], TILES);  // every tile's MMAs
             mbar_init(&v_full[i], 1);
-            mbar_init(&v_empty[i], 2);
+            mbar_init(&v_empty[i], TILES);
         }
         fence_barrier_init();
     }
@@ -191,9 +195,9 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
     };
 
     if (units > 0) {
-        if (warp == 9 || warp == 11) {
-            // ---- copies of the keys (warp 9) or values (warp 11): a lane per piece of a step ----
-            const int kv = warp == 11, P = 1 << a.page_shift, box = min(P, CT_STEP), per = CT_STEP / box;
+        if (warp == L::COPY_K || warp == L::COPY_V) {
+            // ---- copies of the keys or the values: a lane per piece of a step ----
+            const int kv = warp == L::COPY_V, P = 1 << a.page_shift, box = min(P, CT_STEP), per = CT_STEP / box;
             const int sub = lane % per, half = lane / per;
             const bool mine = half < HD / 64;
             unsigned char* ring = sm + (kv ? L::V : L::K) + half * L::ATOM + sub * box * 128;
@@ -242,16 +246,16 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
             if (!ok && lane == 0)  // what is in flight lands before the CTA leaves
                 for (int i = max(0, n - ST); i < n; ++i) chunk_wait(&full[i % ST], i / ST, nullptr);
             __syncwarp();
-        } else if (warp == 8 || warp == 10) {
+        } else if (warp >= L::MMA && warp < L::MMA + TILES) {
             // ---- MMAs of a tile, by one thread ----
             if (elect_one()) {
                 constexpr uint32_t IDESC_S = ct_idesc<T>(CT_STEP, false), IDESC_O = ct_idesc<T>(HD, true);
-                const int tile = warp == 10;
+                const int tile = warp - L::MMA;
                 ChunkWalk w(a, start);
                 CtTile x(w, tile), y = x;  // y: the unit before's
                 const uint64_t q = sw128_desc(smem_addr(sm + tile * L::OPER)), k0 = sw128_desc(smem_addr(sm + L::K)),
                                v0 = v_desc(smem_addr(sm + L::V), L::ATOM);
-                const uint32_t s_tmem = tmem + TM_S + tile * 128, o_tmem = tmem + TM_O + tile * 128;
+                const uint32_t s_tmem = tmem + TM_S + tile * 128, o_tmem = tmem + TM_O + tile * L::TM_O_TILE;
                 uint32_t q_phase = 0, p_phase[2] = {0, 0};
                 bool ok = true;
                 auto await = [&](bool there, uint64_t* bar, uint32_t phase) { ok = ok && (there || chunk_wait(bar, phase, a.err)); };
@@ -279,7 +283,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                         const bool p_there = !p_on || mbar_try_wait(&p_full[tile][half], p_phase[half] & 1);
                         // The tiles take turns, so that a tile's MMAs run in one piece and their results come half a step apart:
                         // mixed, both tiles' scores would be ready late, and both softmax groups wait for them.
-                        const bool my_turn = tile == 0 && i == 0;
+                        const bool my_turn = TILES == 1 || (tile == 0 && i == 0);
                         const uint32_t turn_phase = i - 1 + tile;
                         const bool turn_there = my_turn || mbar_try_wait(&turn[tile], turn_phase & 1);
                         await(k_there, &k_full[st], i / ST);
@@ -302,13 +306,13 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                             if (!ok) break;
                             tc_fence_after();
                         }
-                        if (!s_on) mbar_arrive(&turn[tile ^ 1]);
+                        if (TILES == 2 && !s_on) mbar_arrive(&turn[tile ^ 1]);
                         if (more) {
                             if (s_on) {  // S = Q K^T
                                 const uint64_t kd = k0 + st * (L::STEP >> 4);
 #pragma unroll
                                 for (int d = 0; d < HD / 16; ++d) {
-                                    if (d == HD / 16 - CT_HANDOVER) mbar_arrive(&turn[tile ^ 1]);  // (seen by the time that S is through)
+                                    if (TILES == 2 && d == HD / 16 - CT_HANDOVER) mbar_arrive(&turn[tile ^ 1]);  // (seen by the time that S is through)
                                     tc_mma(s_tmem + half * 64, q + (((d >> 2) * CT_SUB + (d & 3) * 32) >> 4),
                                            kd + (((d >> 2) * L::ATOM + (d & 3) * 32) >> 4), IDESC_S, d != 0);
                                 }
@@ -324,10 +328,10 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                 chunk_wait(&drain[tile], 0, a.err);
             }
             __syncwarp();
-        } else if (warp < 8) {
+        } else if (warp < 4 * TILES) {
             // ---- softmax: group g has tile g, a row per thread ----
             const int g = warp >> 2, r = tid & 127;
-            const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), ts = lanes + TM_S + g * 128, to = lanes + TM_O + g * 128;
+            const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), ts = lanes + TM_S + g * 128, to = lanes + TM_O + g * L::TM_O_TILE;
             unsigned char* qs = sm + g * L::OPER;
             const int heads = a.kv_heads * a.group;
             ChunkWalk w(a, start);
@@ -523,7 +527,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                 const long long row = place(w, x.p0 + r, head);
                 const bool live = r < x.rows;
                 const float f = sum == 0.f ? 0.f : 1.f / sum;  // (no key: 0)
-                float* part = a.part + ((size_t)cta * 2 + begins) * CT_ROWS * (HD + 2);
+                float* part = a.part + ((size_t)cta * 2 + begins) * (CT_TILE * TILES) * (HD + 2);
 #pragma unroll 1
                 for (int c = 0; c < HD; c += 32) {
                     float v[32];
@@ -557,7 +561,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
                     }
                 }
                 if (live && whole && a.lse) a.lse[row * heads + head] = sum == 0.f ? -INFINITY : LN2 * (ref + log2f(sum));
-                if (live && !whole) *reinterpret_cast<float2*>(part + CT_ROWS * HD + 2 * (g * CT_TILE + r)) = make_float2(ref, sum);
+                if (live && !whole) *reinterpret_cast<float2*>(part + (CT_TILE * TILES) * HD + 2 * (g * CT_TILE + r)) = make_float2(ref, sum);
                 tc_fence_before();  // O is read before the next item's product overwrites it
                 if (!more) break;
                 n += len;
@@ -569,14 +573,14 @@ __global__ void __launch_bounds__(CT_THREADS, 1) chunk_tc_kernel(const __grid_co
     asm volatile("cp.async.wait_all;" ::: "memory");
     tc_fence_before();
     __syncthreads();
-    if (warp == 8) tmem_dealloc(tmem, TM_COLS);
+    if (warp == L::MMA) tmem_dealloc(tmem, L::TM_COLS);
 }
 
 template <class T, int HD>
 cudaError_t launch_tc(const ChunkArgs& a, const CUtensorMap& map, cudaStream_t s) {
     const auto kern = chunk_tc_kernel<T, HD>;
     const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), CtLayout<HD>::BYTES);
-    return e == cudaSuccess ? launch_ex(kern, dim3(a.ctas), CT_THREADS, CtLayout<HD>::BYTES, true, s, a, map) : e;
+    return e == cudaSuccess ? launch_ex(kern, dim3(a.ctas), CtLayout<HD>::THREADS, CtLayout<HD>::BYTES, true, s, a, map) : e;
 }
 
 }  // namespace
