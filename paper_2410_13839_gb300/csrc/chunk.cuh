@@ -47,6 +47,7 @@ struct ChunkArgs {
     int window, max_tiles, min_units, ctas;
     int snap;                      // items of at most 1 / snap of a share are not cut (0: all are)
     bool q_vec, out_vec;           // rows 16-byte aligned
+    bool q_tma;                    // many rows: Q's tiles are copied by a tensor map
     float scale_log2;              // scale * log2 e: scores in log2 units
     int4* start;                   // [ctas]: first tile, key head, unit in the item, units of the share
     int* desc;                     // [ctas][CH_DESC]: merges
@@ -104,7 +105,8 @@ struct ChunkWalk {
 };
 
 cudaError_t launch_chunk_plan(const ChunkArgs& a, int tile_rows, cudaStream_t s);  // 16, 32; 128, 256: many rows
-cudaError_t launch_chunk_tc(const ChunkArgs& a, const CUtensorMap& map, int head_dim, int dtype, cudaStream_t s);
+cudaError_t launch_chunk_tc(const ChunkArgs& a, const CUtensorMap& map, const CUtensorMap& q_map, int head_dim, int dtype,
+                            cudaStream_t s);
 
 template <class... P>
 cudaError_t launch_ex(void (*kern)(P...), dim3 grid, int threads, size_t smem, bool pdl, cudaStream_t s, P... args) {

@@ -27,6 +27,8 @@ namespace mtp {
 
 int tc_encode_cache(CUtensorMap* map, const void* pool, int dtype, int head_dim, int page_size, uint64_t blocks,
                     int box_rows);
+int tc_encode_queries(CUtensorMap* map, const void* q, int dtype, int head_dim, int heads, uint64_t rows, uint64_t stride,
+                      int group);
 
 namespace {
 
@@ -526,11 +528,11 @@ cudaError_t launch_rows(const ChunkArgs& a, const CUtensorMap& map, cudaStream_t
     return launch_ex(kern, dim3(a.ctas), FR_THREADS, smem, true, s, a, map);
 }
 template <class T>
-cudaError_t launch_kernels(const ChunkArgs& a, const CUtensorMap& map, int head_dim, int dtype, int tile_rows, cudaStream_t s) {
+cudaError_t launch_kernels(const ChunkArgs& a, const CUtensorMap& map, const CUtensorMap& q_map, int head_dim, int dtype, int tile_rows, cudaStream_t s) {
     cudaError_t e = launch_chunk_plan(a, tile_rows, s);
     if (e != cudaSuccess) return e;
     if (tile_rows > FR_MAX_ROWS)
-        e = launch_chunk_tc(a, map, head_dim, dtype, s);
+        e = launch_chunk_tc(a, map, q_map, head_dim, dtype, s);
     else if (head_dim == 64)
         e = tile_rows == 16 ? launch_rows<T, 64, 1>(a, map, s) : launch_rows<T, 64, 2>(a, map, s);
     else
@@ -601,12 +603,15 @@ MTP_API int mtp_chunk_attention(const mtp_chunk_attention_args* a, void* workspa
         c.part = reinterpret_cast<float*>(ws + p.part);
         c.err = a->err_word;
         const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-        CUtensorMap map;
+        CUtensorMap map, q_map = {};
         if (tc_encode_cache(&map, a->kv_pool, a->dtype, a->head_dim, a->page_size,
                             (uint64_t)a->n_pages * c.page_blocks, std::min(a->page_size, FR_KEYS)) != 0)
             return report_error(MTP_ERR_CUDA, "chunk_attention: cuTensorMapEncodeTiled failed");
-        const cudaError_t e = a->dtype == MTP_BF16 ? launch_kernels<Bf16>(c, map, a->head_dim, a->dtype, p.tile_rows, s)
-                                                   : launch_kernels<F16>(c, map, a->head_dim, a->dtype, p.tile_rows, s);
+        // a tile's 128 packed rows are a box of the query rows where the heads of a key head divide 128
+        c.q_tma = !few && c.q_vec && 128 % group == 0 && a->q_stride < (1ll << 38) &&
+                  tc_encode_queries(&q_map, a->q, a->dtype, a->head_dim, a->n_heads, a->rows, a->q_stride, group) == 0;
+        const cudaError_t e = a->dtype == MTP_BF16 ? launch_kernels<Bf16>(c, map, q_map, a->head_dim, a->dtype, p.tile_rows, s)
+                                                   : launch_kernels<F16>(c, map, q_map, a->head_dim, a->dtype, p.tile_rows, s);
         return cuda_status(e, "chunk_attention");
     });
 }

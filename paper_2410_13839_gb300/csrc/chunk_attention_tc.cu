@@ -56,8 +56,8 @@ struct CtLayout {
     static constexpr uint32_t TM_S = 0, TM_O = 128 * TILES, TM_O_TILE = 128, TM_COLS = TILES == 1 ? 256 : 512;
     static constexpr uint32_t OPER = CT_SUB * (HD / 64);  // a tile of Q
     static constexpr uint32_t ATOM = CT_STEP * 128, STEP = ATOM * (HD / 64);  // 64 columns of a stage; a stage
-    static constexpr uint32_t K = TILES * OPER, V = K + STAGES * STEP;
-    static constexpr size_t BYTES = 1024 + V + STAGES * STEP;
+    static constexpr uint32_t K = TILES * OPER, V = K + STAGES * STEP, OUT = V + STAGES * STEP;  // OUT: 64 columns of a tile's rows
+    static constexpr size_t BYTES = 1024 + OUT + TILES * CT_SUB;
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -150,12 +150,12 @@ struct CtTile {
 };
 
 template <class T, int HD>
-__global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES) chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ CUtensorMap map) {
+__global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES) chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map) {
     using L = CtLayout<HD>;
     constexpr int ST = L::STAGES, TILES = L::TILES;
     constexpr uint32_t TM_S = L::TM_S, TM_O = L::TM_O;
     extern __shared__ unsigned char ct_raw[];
-    __shared__ uint64_t q_full[TILES], s_full[TILES][2], p_full[TILES][2], pv_done[TILES][2], k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], turn[TILES], drain[TILES];
+    __shared__ uint64_t q_full[TILES], q_empty[TILES], s_full[TILES][2], p_full[TILES][2], pv_done[TILES][2], k_full[ST], k_empty[ST], v_full[ST], v_empty[ST], turn[TILES], drain[TILES];
     __shared__ uint32_t tmem_base;
     unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(ct_raw) + 1023) & ~(uintptr_t)1023);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
@@ -167,7 +167,8 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
         for (int i = 0; i < TILES; ++i) {
             mbar_init(&drain[i], 1);
             mbar_init(&turn[i], 1);
-            mbar_init(&q_full[i], 4);
+            mbar_init(&q_full[i], a.q_tma ? 1 : 4);
+            mbar_init(&q_empty[i], 1);
             for (int h = 0; h < 2; ++h) {
                 mbar_init(&s_full[i][h], 1);
                 mbar_init(&p_full[i][h], 4);
@@ -209,7 +210,22 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
             int base = 0, pages = 0, ahead = 0, key_first = 0, hi = 0, lo = 0, last = 0, head_block = 0;
             const int* table = nullptr;
             auto lookup = [&](int first) { return first + lane < a.bt_stride ? __ldg(table + first + lane) : -1; };
+            int queries[TILES] = {};  // tiles of Q copied so far
             auto enter = [&]() {  // an item's first step
+                if (kv && a.q_tma)  // the values' warp, which is behind the keys', copies Q too
+#pragma unroll
+                    for (int tile = 0; tile < TILES; ++tile) {
+                        const CtTile x(w, tile);
+                        if (x.from >= x.to) continue;
+                        if (queries[tile] > 0) ok = ok && wait(&q_empty[tile], queries[tile] - 1);
+                        ++queries[tile];
+                        if (ok && lane == 0) {
+                            mbar_arrive_expect_tx(&q_full[tile], L::OPER);
+                            for (int h = 0; h < HD / 64; ++h)
+                                tma_cache(sm + tile * L::OPER + h * CT_SUB, &q_map, h * 64, w.head * a.group,
+                                          w.t.row0 + chunk_token(a, x.p0), &q_full[tile]);
+                        }
+                    }
                 table = a.block_table + (size_t)w.t.slot * a.bt_stride;
                 key_first = w.key0<CT_KEYS>();
                 hi = w.t.hi;
@@ -221,7 +237,7 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
                 ahead = lookup(base + 32);
             };
             enter();
-            for (const int steps = 2 * units; n < steps; ++n) {
+            for (const int steps = 2 * units; ok && n < steps; ++n) {
                 const int st = n % ST, key = key_first + step * CT_STEP + sub * box, index = key >> a.page_shift;
                 if (index - base >= 32) {  // (the same in all lanes: a step's pages lie in one aligned group)
                     base += 32;
@@ -245,6 +261,9 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
             }
             if (!ok && lane == 0)  // what is in flight lands before the CTA leaves
                 for (int i = max(0, n - ST); i < n; ++i) chunk_wait(&full[i % ST], i / ST, nullptr);
+            if (!ok && lane == 0 && kv && a.q_tma)
+                for (int tile = 0; tile < TILES; ++tile)
+                    if (queries[tile] > 0) chunk_wait(&q_full[tile], queries[tile] - 1, nullptr);
             __syncwarp();
         } else if (warp >= L::MMA && warp < L::MMA + TILES) {
             // ---- MMAs of a tile, by one thread ----
@@ -271,12 +290,37 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
                         k1 = w.k1;
                         x = CtTile(w, tile);
                     }
+                    // S of a step, whose keys are there; `hand`: the turn goes to the other tile under it
+                    auto scores = [&](int half, int st, bool hand) {
+                        const int step = 2 * k + half;
+                        if (step >= x.from && step < x.to) {  // S = Q K^T
+                            if (step == x.from) {
+                                await(false, &q_full[tile], q_phase++);
+                                if (!ok) return;
+                                tc_fence_after();
+                            }
+                            const uint64_t kd = k0 + st * (L::STEP >> 4);
+#pragma unroll
+                            for (int d = 0; d < HD / 16; ++d) {
+                                if (hand && d == HD / 16 - CT_HANDOVER) mbar_arrive(&turn[tile ^ 1]);  // (seen by the time that S is through)
+                                tc_mma(s_tmem + half * 64, q + (((d >> 2) * CT_SUB + (d & 3) * 32) >> 4),
+                                       kd + (((d >> 2) * L::ATOM + (d & 3) * 32) >> 4), IDESC_S, d != 0);
+                            }
+                            tc_commit(&s_full[tile][half]);
+                            if (step + 1 == x.to) tc_commit(&q_empty[tile]);
+                        } else if (hand) {
+                            mbar_arrive(&turn[tile ^ 1]);
+                        }
+                        tc_commit(&k_empty[st]);
+                    };
+                    // at an item's first unit both products come first: its Q may still be on its way, and the item before
+                    // waits for its last product
+                    const bool entering = n > 0 && k == 0;
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const int i = 2 * n + half, st = i % ST, before = (i + ST - 2) % ST;
-                        const int p_step = 2 * at + half, s_step = 2 * k + half;
-                        const bool p_on = n > 0 && p_step >= y.from && p_step < y.to, s_on = more && s_step >= x.from && s_step < x.to;
-                        const bool s_first = s_on && s_step == x.from;
+                        const int p_step = 2 * at + half;
+                        const bool p_on = n > 0 && p_step >= y.from && p_step < y.to;
                         // all barriers are asked at once: an answer takes 126 cycles
                         const bool k_there = !more || mbar_try_wait(&k_full[st], (i / ST) & 1);
                         const bool v_there = n == 0 || mbar_try_wait(&v_full[before], ((i - 2) / ST) & 1);
@@ -301,26 +345,14 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
                             tc_commit(&pv_done[tile][half]);
                         }
                         if (n > 0) tc_commit(&v_empty[before]);
-                        if (s_first) {
-                            await(false, &q_full[tile], q_phase++);
-                            if (!ok) break;
-                            tc_fence_after();
-                        }
-                        if (TILES == 2 && !s_on) mbar_arrive(&turn[tile ^ 1]);
-                        if (more) {
-                            if (s_on) {  // S = Q K^T
-                                const uint64_t kd = k0 + st * (L::STEP >> 4);
-#pragma unroll
-                                for (int d = 0; d < HD / 16; ++d) {
-                                    if (TILES == 2 && d == HD / 16 - CT_HANDOVER) mbar_arrive(&turn[tile ^ 1]);  // (seen by the time that S is through)
-                                    tc_mma(s_tmem + half * 64, q + (((d >> 2) * CT_SUB + (d & 3) * 32) >> 4),
-                                           kd + (((d >> 2) * L::ATOM + (d & 3) * 32) >> 4), IDESC_S, d != 0);
-                                }
-                                tc_commit(&s_full[tile][half]);
-                            }
-                            tc_commit(&k_empty[st]);
-                        }
+                        if (more && !entering)
+                            scores(half, st, TILES == 2);
+                        else if (TILES == 2)
+                            mbar_arrive(&turn[tile ^ 1]);
                     }
+                    if (ok && more && entering)
+#pragma unroll 1
+                        for (int half = 0; half < 2; ++half) scores(half, (2 * n + half) % ST, false);
                     y = x;
                     ++k;
                 }
@@ -375,7 +407,8 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&q_full[g]);
             };
-            if (x.from < x.to) {
+            const bool bring_q = !a.q_tma;  // rows that a tensor map cannot describe
+            if (bring_q && x.from < x.to) {
                 load_q(w, x);
                 q_there();
             }
@@ -395,7 +428,7 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
                 ChunkWalk next = w;
                 next.next(a);
                 const CtTile y(next, g);
-                const bool more = next.left > 0, q_next = more && y.from < y.to;  // an item after this one; one with Q
+                const bool more = next.left > 0, q_next = bring_q && more && y.from < y.to;  // an item after this one; whose Q is to be brought
                 bool there = false;  // the step's scores are known to be there
                 float s0[32], s1[32];
 #pragma unroll 1
@@ -527,37 +560,60 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
                 const long long row = place(w, x.p0 + r, head);
                 const bool live = r < x.rows;
                 const float f = sum == 0.f ? 0.f : 1.f / sum;  // (no key: 0)
+                const long long mine = row * a.out_stride + head * HD;
                 float* part = a.part + ((size_t)cta * 2 + begins) * (CT_TILE * TILES) * (HD + 2);
 #pragma unroll 1
-                for (int c = 0; c < HD; c += 32) {
-                    float v[32];
+                for (int c = 0; c < HD; c += 64) {
+                    float v[2][32];
                     __syncwarp();
                     if (any) {
-                        tmem_ld32(to + c, v);
+                        tmem_ld_issue<32>(to + c, v[0]);
+                        tmem_ld_issue<32>(to + c + 32, v[1]);
+                        tmem_ld_wait();
+                        tmem_ld_done(v[0]);
+                        tmem_ld_done(v[1]);
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) v[e] = 0.f;
+                        for (int e = 0; e < 32; ++e) v[0][e] = v[1][e] = 0.f;
                     }
-                    if (!live) continue;
                     if (whole) {
-                        uint16_t* dst = a.out + row * a.out_stride + head * HD + c;
-                        uint32_t y[16];
+                        // through shared memory, a warp its own 32 rows: eight threads write a row's 128 bytes
+                        unsigned char* stage = sm + L::OUT + g * CT_SUB;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) y[e] = T::pack(sum == 0.f ? 0.f : v[2 * e] * f, sum == 0.f ? 0.f : v[2 * e + 1] * f);
-                        if (a.out_vec) {
+                        for (int e = 0; e < 8; ++e) {
+                            const float* z = v[e >> 2] + (e & 3) * 8;
+                            uint4 y;
+                            y.x = T::pack(z[0] * f, z[1] * f);
+                            y.y = T::pack(z[2] * f, z[3] * f);
+                            y.z = T::pack(z[4] * f, z[5] * f);
+                            y.w = T::pack(z[6] * f, z[7] * f);
+                            *reinterpret_cast<uint4*>(stage + r * 128 + ((e ^ (r & 7)) << 4)) = y;
+                        }
+                        __syncwarp();
+#pragma unroll 4
+                        for (int i = 0; i < 32; i += 4) {
+                            const int from = i + (lane >> 3), at = (r & ~31) + from;
+                            uint16_t* dst = a.out + __shfl_sync(FULL_MASK, mine, from) + c + (lane & 7) * 8;
+                            const uint4 y = *reinterpret_cast<const uint4*>(stage + at * 128 + (((lane & 7) ^ (at & 7)) << 4));
+                            if (at >= x.rows) continue;
+                            if (a.out_vec) {
+                                *reinterpret_cast<uint4*>(dst) = y;
+                            } else {
+                                const uint32_t z[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(dst)[e] = make_uint4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                dst[2 * e] = (uint16_t)y[e];
-                                dst[2 * e + 1] = (uint16_t)(y[e] >> 16);
+                                for (int e = 0; e < 4; ++e) {
+                                    dst[2 * e] = (uint16_t)z[e];
+                                    dst[2 * e + 1] = (uint16_t)(z[e] >> 16);
+                                }
                             }
                         }
-                    } else {
+                    } else if (live) {
                         float4* dst = reinterpret_cast<float4*>(part + (g * CT_TILE + r) * HD + c);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) dst[e] = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                        for (int e = 0; e < 16; ++e) {
+                            const float* z = v[e >> 3] + (e & 7) * 4;
+                            dst[e] = make_float4(z[0], z[1], z[2], z[3]);
+                        }
                     }
                 }
                 if (live && whole && a.lse) a.lse[row * heads + head] = sum == 0.f ? -INFINITY : LN2 * (ref + log2f(sum));
@@ -577,17 +633,18 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
 }
 
 template <class T, int HD>
-cudaError_t launch_tc(const ChunkArgs& a, const CUtensorMap& map, cudaStream_t s) {
+cudaError_t launch_tc(const ChunkArgs& a, const CUtensorMap& map, const CUtensorMap& q_map, cudaStream_t s) {
     const auto kern = chunk_tc_kernel<T, HD>;
     const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), CtLayout<HD>::BYTES);
-    return e == cudaSuccess ? launch_ex(kern, dim3(a.ctas), CtLayout<HD>::THREADS, CtLayout<HD>::BYTES, true, s, a, map) : e;
+    return e == cudaSuccess ? launch_ex(kern, dim3(a.ctas), CtLayout<HD>::THREADS, CtLayout<HD>::BYTES, true, s, a, map, q_map) : e;
 }
 
 }  // namespace
 
-cudaError_t launch_chunk_tc(const ChunkArgs& a, const CUtensorMap& map, int head_dim, int dtype, cudaStream_t s) {
-    if (dtype == MTP_BF16) return head_dim == 64 ? launch_tc<Bf16, 64>(a, map, s) : launch_tc<Bf16, 128>(a, map, s);
-    return head_dim == 64 ? launch_tc<F16, 64>(a, map, s) : launch_tc<F16, 128>(a, map, s);
+cudaError_t launch_chunk_tc(const ChunkArgs& a, const CUtensorMap& map, const CUtensorMap& q_map, int head_dim, int dtype,
+                            cudaStream_t s) {
+    if (dtype == MTP_BF16) return head_dim == 64 ? launch_tc<Bf16, 64>(a, map, q_map, s) : launch_tc<Bf16, 128>(a, map, q_map, s);
+    return head_dim == 64 ? launch_tc<F16, 64>(a, map, q_map, s) : launch_tc<F16, 128>(a, map, q_map, s);
 }
 
 }  // namespace mtp

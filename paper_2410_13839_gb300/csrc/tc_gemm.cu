@@ -440,6 +440,21 @@ int tc_encode_cache(CUtensorMap* map, const void* pool, int dtype, int head_dim,
     return r == CUDA_SUCCESS ? 0 : -3;
 }
 
+// Query rows [rows][heads][head_dim] of 16-bit elements at a row stride (elements): boxes of 64 columns of
+// `group` heads of 128 / group rows; rows past the last read as zeros.
+int tc_encode_queries(CUtensorMap* map, const void* q, int dtype, int head_dim, int heads, uint64_t rows, uint64_t stride,
+                      int group) {
+    EncodeTiled fn = encode_fn();
+    if (!fn) return -1;
+    const cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads, rows};
+    const cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)group, (cuuint32_t)(128 / group)}, estr[3] = {1, 1, 1};
+    const CUresult r = fn(map, dtype == MTP_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                          const_cast<void*>(q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? 0 : -3;
+}
+
 int tc_tile_rows(int m) { return m <= 32 ? 32 : (m <= 64 ? 64 : 128); }
 
 cudaError_t launch_tc_gemm(const TcGemm& g, cudaStream_t s, bool pdl) {
