@@ -45,6 +45,7 @@ struct ChunkArgs {
     uint32_t group_inv;            // ceil(2^32 / group)
     int page_blocks, layer_block;  // (layer, K | V, head) blocks of a page; the layer's first
     int window, max_tiles, min_units, ctas;
+    int item_cost;                 // an item's start and end, in units
     int snap;                      // items of at most 1 / snap of a share are not cut (0: all are)
     bool q_vec, out_vec;           // rows 16-byte aligned
     bool q_tma;                    // many rows: Q's tiles are copied by a tensor map

@@ -34,6 +34,7 @@ namespace {
 
 constexpr int FR_KEYS = 64, FR_WARPS = 5, FR_THREADS = FR_WARPS * 32, FR_CONSUMERS = 128;
 constexpr int FR_MIN_UNITS = 4, CT_MIN_UNITS = 2, CT_SNAP = 3;  // fewest units of a CTA
+constexpr int FR_ITEM_COST = 2, CT_ITEM_COST = 2;
 constexpr int FR_MAX_ROWS = 32, CT_UNIT_KEYS = 128;
 constexpr float LN2 = 0.69314718055994531f;
 
@@ -592,6 +593,7 @@ MTP_API int mtp_chunk_attention(const mtp_chunk_attention_args* a, void* workspa
         c.window = a->window; c.max_tiles = p.max_tiles; c.min_units = p.min_units;
         const bool few = p.tile_rows <= FR_MAX_ROWS;
         c.snap = few ? 0 : CT_SNAP;
+        c.item_cost = few ? FR_ITEM_COST : CT_ITEM_COST;
         c.q_vec = aligned16(a->q) && a->q_stride % 8 == 0;
         c.out_vec = aligned16(a->out) && a->out_stride % 8 == 0;
         c.scale_log2 = a->scale * 1.4426950408889634f;

@@ -64,46 +64,58 @@ __device__ __forceinline__ uint32_t scan(uint32_t x, uint32_t* part, uint32_t& s
     return __reduce_add_sync(FULL_MASK, lane < warp ? mine : 0) + y - x;
 }
 
+// largest i in [0, n) with first[i] + i * extra <= x
 template <class T>
-__device__ __forceinline__ int owner(const T* first, int n, T x) {  // largest i in [0, n) with first[i] <= x
+__device__ __forceinline__ int owner(const T* first, int n, T x, T extra = 0) {
     int lo = 0, hi = n;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (first[mid] <= x) lo = mid; else hi = mid;
+        if (first[mid] + mid * extra <= x) lo = mid; else hi = mid;
     }
     return lo;
 }
 
+// The stream in cost: an item costs its units and a.item_cost for its start and end, which come first.
 struct Map {
     const uint32_t* unit_first;  // [tiles + 1]: first unit of every tile, counted for one key head
     int tiles, ctas, snap;
 };
 template <class U>
-struct Item {
-    int tile, head, units;
-    U first;  // its first unit
+struct Place {
+    int tile, head, units, k;  // k: the unit of the item that this place stands before
+    U first, cost;             // the item's place and cost
+    U unit;                    // units before this place
 };
 template <class U>
-__device__ __forceinline__ Item<U> item_of(const ChunkArgs& a, const Map& m, U unit) {
-    Item<U> x;
-    x.tile = owner(m.unit_first, m.tiles, (uint32_t)(unit / (U)a.kv_heads));
-    const U first = (U)m.unit_first[x.tile] * (U)a.kv_heads;
-    x.units = (int)(m.unit_first[x.tile + 1] - m.unit_first[x.tile]);
-    x.head = (int)((uint32_t)(unit - first) / (uint32_t)x.units);  // (an item's units and heads: below 2^32 together)
-    x.first = first + (U)x.head * (U)x.units;
+__device__ __forceinline__ Place<U> place_of(const ChunkArgs& a, const Map& m, U at) {
+    Place<U> x;
+    const uint32_t c = a.item_cost;
+    x.tile = owner(m.unit_first, m.tiles, (uint32_t)(at / (U)a.kv_heads), c);
+    const uint32_t unit0 = m.unit_first[x.tile];
+    const U first = ((U)unit0 + (U)x.tile * c) * (U)a.kv_heads;
+    x.units = (int)(m.unit_first[x.tile + 1] - unit0);
+    x.cost = (U)x.units + c;
+    x.head = (int)((uint32_t)(at - first) / (uint32_t)x.cost);  // (an item's cost and heads: below 2^32 together)
+    x.first = first + (U)x.head * x.cost;
+    x.k = (int)(at - x.first) - (int)c;
+    if (x.k < 0) x.k = 0;
+    x.unit = (U)unit0 * (U)a.kv_heads + (U)x.head * (U)x.units + (U)x.k;
     return x;
 }
 
-// Shares and merges, in 32 bits where the units times the CTAs fit (64-bit divisions were most of
-// the plan's time).  CTA c's share begins at c / ctas of the units; items of at most m.snap
-// units are not cut: the border goes to their nearer end.
+// Shares and merges, in 32 bits where the cost times the CTAs fits (64-bit divisions were most of
+// the plan's time).  CTA c's share begins at c / ctas of the cost; items of at most m.snap units
+// are not cut: the border goes to their nearer end.
 template <class U>
-__device__ __forceinline__ void share_out(const ChunkArgs& a, const Map& m, U units, U* borders) {
+__device__ __forceinline__ void share_out(const ChunkArgs& a, const Map& m, U cost, U units, U* borders) {
     for (int c = threadIdx.x; c <= a.ctas; c += PL_THREADS) {
-        U u = c >= m.ctas ? units : units * (U)c / (U)m.ctas;
-        if (u < units && m.snap > 0) {
-            const Item<U> x = item_of<U>(a, m, u);
-            if (x.units <= m.snap) u = u - x.first <= (U)(x.units / 2) ? x.first : x.first + (U)x.units;
+        U u = c >= m.ctas ? cost : cost * (U)c / (U)m.ctas;
+        if (u < cost) {
+            const Place<U> x = place_of<U>(a, m, u);
+            if (x.units <= m.snap)
+                u = u - x.first <= x.cost / 2 ? x.first : x.first + x.cost;
+            else if (x.k == 0)
+                u = x.first;
         }
         borders[c] = u;
     }
@@ -113,13 +125,14 @@ __device__ __forceinline__ void share_out(const ChunkArgs& a, const Map& m, U un
         int4 start = make_int4(0, 0, 0, 0);
         int more = 0;
         if (u0 < u1) {
-            const Item<U> x = item_of<U>(a, m, u0);
-            start = make_int4(x.tile, x.head, (int)(u0 - x.first), (int)(u1 - u0));
-            if (u1 < units) {
-                const Item<U> y = item_of<U>(a, m, u1);
-                if (y.first < u1 && y.first >= u0) {  // begins here and goes on, up to the CTA with its last unit
+            const Place<U> x = place_of<U>(a, m, u0);
+            U end = units;
+            if (u1 < cost) {
+                const Place<U> y = place_of<U>(a, m, u1);
+                end = y.unit;
+                if (y.k > 0 && y.first >= u0) {  // begins here and goes on, up to the CTA with its last unit
                     more = 1;
-                    while (borders[c + 1 + more] < y.first + (U)y.units) ++more;
+                    while (borders[c + 1 + more] < y.first + y.cost) ++more;
                     const ChunkTile& t = a.tiles[y.tile];
                     int* d = a.desc + c * CH_DESC;
                     d[1] = t.p0;
@@ -128,6 +141,7 @@ __device__ __forceinline__ void share_out(const ChunkArgs& a, const Map& m, U un
                     d[4] = y.head;
                 }
             }
+            start = make_int4(x.tile, x.head, x.k, (int)(end - x.unit));
         }
         a.start[c] = start;
         a.desc[c * CH_DESC] = more;
@@ -187,15 +201,16 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan_kernel(const __grid_con
     if (tid == 0) unit_first[m.tiles] = base;
     __syncthreads();
     const unsigned long long units = (unsigned long long)base * a.kv_heads;
-    const bool narrow = units * a.ctas < 1ull << 32;
+    const unsigned long long cost = ((unsigned long long)base + (unsigned long long)m.tiles * a.item_cost) * a.kv_heads;
+    const bool narrow = cost * a.ctas < 1ull << 32;
     m.ctas = (int)min((unsigned long long)a.ctas,
                       max(1ull, narrow ? (unsigned long long)(((uint32_t)units + a.min_units - 1) / a.min_units)
                                        : (units + a.min_units - 1) / a.min_units));
     m.snap = !a.snap ? 0 : narrow ? (int)((uint32_t)units / m.ctas / a.snap) : (int)min(units / m.ctas / a.snap, 1ull << 30);
     if (narrow)
-        share_out<uint32_t>(a, m, (uint32_t)units, reinterpret_cast<uint32_t*>(pl_sm));
+        share_out<uint32_t>(a, m, (uint32_t)cost, (uint32_t)units, reinterpret_cast<uint32_t*>(pl_sm));
     else
-        share_out<unsigned long long>(a, m, units, reinterpret_cast<unsigned long long*>(pl_sm));
+        share_out<unsigned long long>(a, m, cost, units, reinterpret_cast<unsigned long long*>(pl_sm));
 }
 
 template <int TR, int KT>
