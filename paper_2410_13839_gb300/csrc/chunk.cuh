@@ -30,6 +30,13 @@ struct ChunkTile {
 };
 static_assert(sizeof(ChunkTile) == 48, "three pieces");
 
+// Where a CTA's share begins: tile (a copy of it, for one look-up less), key head, unit of the item; units of the share.
+struct ChunkStart {
+    int tile, head, k, units;
+    ChunkTile t;
+};
+static_assert(sizeof(ChunkStart) == 64, "four pieces");
+
 // Tiles of 128 rows of a CTA of the many-rows kernel, and CTAs of an SM (they fill TMEM).  One tile of 64
 // dims and two CTAs: bound by the softmax, they need no shared keys, and a tile's start and
 // end lie behind the other CTA's work.  128 dims: two tiles, for half the key and value copies.
@@ -50,7 +57,7 @@ struct ChunkArgs {
     bool q_vec, out_vec;           // rows 16-byte aligned
     bool q_tma;                    // many rows: Q's tiles are copied by a tensor map
     float scale_log2;              // scale * log2 e: scores in log2 units
-    int4* start;                   // [ctas]: first tile, key head, unit in the item, units of the share
+    ChunkStart* start;             // [ctas]
     int* desc;                     // [ctas][CH_DESC]: merges
     ChunkTile* tiles;              // [max_tiles]
     float* part;                   // [ctas][2][TR][dim + 2]
@@ -84,8 +91,7 @@ struct ChunkWalk {
         to[1] = p[1];
         to[2] = p[2];
     }
-    __device__ __forceinline__ ChunkWalk(const ChunkArgs& a, int4 start) : tile(start.x), head(start.y), k0(start.z), left(start.w) {
-        if (left > 0) load(a);
+    __device__ __forceinline__ ChunkWalk(const ChunkStart& s) : tile(s.tile), head(s.head), k0(s.k), left(s.units), t(s.t) {
         k1 = left > 0 ? min(t.units, k0 + left) : k0;
     }
     __device__ __forceinline__ void next(const ChunkArgs& a) {  // the item after this one (left 0: there is none)

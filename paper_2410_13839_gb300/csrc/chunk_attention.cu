@@ -108,8 +108,8 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
     __syncthreads();
     pdl_launch_dependents();
     pdl_wait();  // the plan
-    const int4 start = a.start[cta];
-    const int units = start.w;
+    const ChunkStart start = a.start[cta];
+    const int units = start.units;
     if (units == 0) return;
 
     if (warp == 4) {  // ---- the ring's filler ----
@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
         const int sub = lane % per, half = lane / per % (HD / 64), kv = lane / per / (HD / 64);
         const bool mine = kv < 2;
         unsigned char* ring = sm + kv * L::KV + half * L::TILE + sub * box * 128;
-        ChunkWalk w(a, start);
+        ChunkWalk w(start);
         int k = w.k0, issued = 0, base = 0, pages = 0, ahead = 0;
         bool ok = true;
         // pages [base, base + 32) of the slot, one per lane, and the 32 after them
@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
     float* ml = reinterpret_cast<float*>(sm + L::ML);  // [4 warps][TR] maxima, then sums
     int stage = 0;
     bool alive = true;
-    ChunkWalk w(a, start);
+    ChunkWalk w(start);
     for (; w.left > 0; w.next(a)) {
         const ChunkTile& t = w.t;
         const int key_first = w.key0<FR_KEYS>();
@@ -513,7 +513,7 @@ int chunk_plan(const mtp_chunk_attention_args* a, ChunkPlan* p) {
         return at;
     };
     p->need = 0;
-    p->start = place((size_t)p->ctas * sizeof(int4));
+    p->start = place((size_t)p->ctas * sizeof(ChunkStart));
     p->desc = place((size_t)p->ctas * CH_DESC * sizeof(int));
     p->tiles = place((size_t)p->max_tiles * sizeof(ChunkTile));
     p->part = place((size_t)p->ctas * 2 * p->tile_rows * (a->head_dim + 2) * sizeof(float));
@@ -599,7 +599,7 @@ MTP_API int mtp_chunk_attention(const mtp_chunk_attention_args* a, void* workspa
         c.scale_log2 = a->scale * 1.4426950408889634f;
         char* ws = static_cast<char*>(workspace);
         c.ctas = p.ctas;
-        c.start = reinterpret_cast<int4*>(ws + p.start);
+        c.start = reinterpret_cast<ChunkStart*>(ws + p.start);
         c.desc = reinterpret_cast<int*>(ws + p.desc);
         c.tiles = reinterpret_cast<ChunkTile*>(ws + p.tiles);
         c.part = reinterpret_cast<float*>(ws + p.part);

@@ -189,8 +189,8 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
     const uint32_t tmem = tmem_base;
     pdl_launch_dependents();
     pdl_wait();  // the plan
-    const int4 start = a.start[cta];
-    const int units = start.w;
+    const ChunkStart start = a.start[cta];
+    const int units = start.units;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
         return __all_sync(FULL_MASK, mbar_try_wait(bar, parity & 1) || chunk_wait(bar, parity, a.err)) != 0;
     };
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
             const bool mine = half < HD / 64;
             unsigned char* ring = sm + (kv ? L::V : L::K) + half * L::ATOM + sub * box * 128;
             uint64_t *full = kv ? v_full : k_full, *empty = kv ? v_empty : k_empty;
-            ChunkWalk w(a, start);
+            ChunkWalk w(start);
             int step = 2 * w.k0, n = 0;
             bool ok = true;
             // pages [base, base + 32) of the slot, one per lane, and the 32 after them
@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
             if (elect_one()) {
                 constexpr uint32_t IDESC_S = ct_idesc<T>(CT_STEP, false), IDESC_O = ct_idesc<T>(HD, true);
                 const int tile = warp - L::MMA;
-                ChunkWalk w(a, start);
+                ChunkWalk w(start);
                 CtTile x(w, tile), y = x;  // y: the unit before's
                 const uint64_t q = sw128_desc(smem_addr(sm + tile * L::OPER)), k0 = sw128_desc(smem_addr(sm + L::K)),
                                v0 = v_desc(smem_addr(sm + L::V), L::ATOM);
@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
             const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), ts = lanes + TM_S + g * 128, to = lanes + TM_O + g * L::TM_O_TILE;
             unsigned char* qs = sm + g * L::OPER;
             const int heads = a.kv_heads * a.group;
-            ChunkWalk w(a, start);
+            ChunkWalk w(start);
             CtTile x(w, g);
             int n = 0, seen[2] = {0, 0};  // steps of either half, which s_full and pv_done count too
             bool ok = true;
@@ -451,14 +451,15 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
                     if (!inner) {
                         // columns (lowest, highest] of the step are the keys that this row sees
                         const int key0 = key_first + step * CT_STEP, highest = pos - key0, lowest = pos - key0 >= window ? pos - key0 - window : -1;
+                        auto below = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };  // columns [0, n)
+                        const unsigned long long sees = below(highest + 1) & ~below(lowest + 1);
+                        const uint32_t m0 = (uint32_t)sees, m1 = (uint32_t)(sees >> 32);
 #pragma unroll
                         for (int c = 0; c < 32; ++c) {
-                            s0[c] = c <= highest && c > lowest ? s0[c] : -INFINITY;
-                            s1[c] = c + 32 <= highest && c + 32 > lowest ? s1[c] : -INFINITY;
+                            s0[c] = m0 >> c & 1 ? s0[c] : -INFINITY;
+                            s1[c] = m1 >> c & 1 ? s1[c] : -INFINITY;
                         }
                     }
-                    // (asked here: the answer is there when it is needed)
-                    there = onward && mbar_test(&s_full[g][half ^ 1], next_phase & 1);
                     float2 acc[2];
                     auto weights32 = [&](const float (&x)[32], uint32_t at) {  // over S, which is all in registers
                         uint32_t y[16];
@@ -519,6 +520,7 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
                         ref = kept;
                     }
                     sum += part;
+                    there = onward && mbar_test(&s_full[g][half ^ 1], next_phase & 1);  // (the answer is there when it is needed)
                     if (!inner) {
                         // keys of the step that no row of the item sees: whatever their values are, zeros in their place (both
                         // groups write them, each before its own product)

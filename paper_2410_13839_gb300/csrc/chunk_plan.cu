@@ -123,6 +123,7 @@ __device__ __forceinline__ void share_out(const ChunkArgs& a, const Map& m, U co
     for (int c = threadIdx.x; c < a.ctas; c += PL_THREADS) {
         const U u0 = borders[c], u1 = borders[c + 1];
         int4 start = make_int4(0, 0, 0, 0);
+        int4* to = reinterpret_cast<int4*>(a.start + c);
         int more = 0;
         if (u0 < u1) {
             const Place<U> x = place_of<U>(a, m, u0);
@@ -142,8 +143,12 @@ __device__ __forceinline__ void share_out(const ChunkArgs& a, const Map& m, U co
                 }
             }
             start = make_int4(x.tile, x.head, x.k, (int)(end - x.unit));
+            const int4* from = reinterpret_cast<const int4*>(a.tiles + x.tile);
+            to[1] = from[0];
+            to[2] = from[1];
+            to[3] = from[2];
         }
-        a.start[c] = start;
+        to[0] = start;
         a.desc[c * CH_DESC] = more;
     }
 }
