@@ -12,11 +12,13 @@
 // part once and keeps a bit per page; CTA totals go over distributed shared memory.
 // A free page then finds its request by a binary search of its rank.
 //
-// One cluster of eight CTAs does it in one launch: the steps need a barrier between
-// them (the ranks before the tables, the tables before the rows that look pages up),
-// and a cluster barrier is a fraction of a launch.  The plan's rows, of which a prompt
-// batch has hundreds of thousands, are written by the whole GPU in a second launch
-// where they are many.
+// What bounds them is latency: a handful of dependent steps with a barrier between them (the
+// ranks before the tables, the tables before the rows that look pages up).  One CTA does a
+// serving step's work; where there are more pages, requests or tables than its threads
+// get through in a step, a cluster of eight (a barrier of the cluster takes about a
+// microsecond, one of a CTA a few dozen cycles, a second launch more than either).  The plan's
+// rows, of which a prompt batch has hundreds of thousands, are then written by the whole
+// GPU in a launch of their own.
 #include <climits>
 
 #include "serving.cuh"
@@ -24,7 +26,9 @@
 namespace mtp {
 namespace {
 
-constexpr int PG_CTAS = 8, PG_THREADS = 1024, PG_WARPS = PG_THREADS / 32;
+constexpr int PG_CLUSTER = 8, PG_THREADS = 1024, PG_WARPS = PG_THREADS / 32;
+// one CTA up to these (32 slots and 2048 pages, one CTA against eight: 6.9 and 8.2 us a plan; 16384 pages: level)
+constexpr int PG_ONE_PAGES = 16384, PG_ONE_SLOTS = 1024, PG_ONE_ROWS = 8192, PG_ONE_BEAMS = 128;
 constexpr int PG_MAX_SLOTS = 8192;
 constexpr int PG_MAX_PAGES = 1 << 22;
 constexpr int PG_MAX_ROWS = 1 << 24;
@@ -36,47 +40,64 @@ struct FreeBits {
     long long before;     // free pages of the CTA before this thread's
 };
 
-__host__ __device__ inline int free_words(int n_pages) {  // words of a CTA's part
-    return ((n_pages + 31) / 32 + PG_CTAS - 1) / PG_CTAS;
+__host__ __device__ inline int free_words(int n_pages, int ctas) {  // words of a CTA's part
+    return ((n_pages + 31) / 32 + ctas - 1) / ctas;
+}
+
+// Exclusive prefix sum of x over the block and the total, both below 2^32.  Synchronises the block.
+__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* part, uint32_t& sum) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t y = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t u = __shfl_up_sync(FULL_MASK, y, o);
+        if (lane >= o) y += u;
+    }
+    __syncthreads();  // `part` may still be read from an earlier call
+    if (lane == 31) part[warp] = y;
+    __syncthreads();
+    const uint32_t mine = part[lane];
+    sum = __reduce_add_sync(FULL_MASK, mine);
+    return __reduce_add_sync(FULL_MASK, lane < warp ? mine : 0) + y - x;
 }
 
 // Reads this CTA's part of the counts once (and copies it, where they go to another
 // array); leaves the part's free pages in *total.
+template <int CTAS>
 __device__ __forceinline__ FreeBits find_free(const int* refs, int* out_refs, int n_pages, int rank, uint32_t* bits,
-                                              long long (*part)[2], int* total) {
+                                              uint32_t* part, int* total) {
+    constexpr int UNROLL = 8;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     FreeBits f;
-    const int all = (n_pages + 31) / 32, cap = free_words(n_pages);
+    const int all = (n_pages + 31) / 32, cap = free_words(n_pages, CTAS);
     f.bits = bits;
     f.first = rank * cap;
     f.words = max(0, min(cap, all - f.first));
     const bool copy = out_refs != refs;
-    for (int w0 = warp; w0 < f.words; w0 += PG_WARPS * 4) {
-        int r[4];
+    for (int w0 = warp; w0 < f.words; w0 += PG_WARPS * UNROLL) {
+        int r[UNROLL];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < UNROLL; ++u) {
             const int w = w0 + u * PG_WARPS, i = (f.first + w) * 32 + lane;
             r[u] = w < f.words && i < n_pages ? refs[i] : 1;
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < UNROLL; ++u) {
             const int w = w0 + u * PG_WARPS, i = (f.first + w) * 32 + lane;
+            if (w >= f.words) break;
             const unsigned b = __ballot_sync(FULL_MASK, r[u] == 0);
-            if (w < f.words) {
-                if (copy && i < n_pages) out_refs[i] = r[u];
-                if (lane == 0) bits[w] = b;
-            }
+            if (copy && i < n_pages) out_refs[i] = r[u];
+            if (lane == 0) bits[w] = b;
         }
     }
     __syncthreads();
     f.per = (f.words + PG_THREADS - 1) / PG_THREADS;
-    long long n = 0, unused = 0, sum, none;
+    uint32_t n = 0, sum;
     for (int i = 0; i < f.per; ++i) {
         const int w = tid * f.per + i;
         if (w < f.words) n += __popc(bits[w]);
     }
-    block_scan2<PG_WARPS>(n, unused, part, sum, none);
-    f.before = n;
+    f.before = block_scan(n, part, sum);
     if (tid == 0) *total = (int)sum;
     return f;
 }
@@ -98,9 +119,28 @@ __device__ __forceinline__ int ld_dsmem_int(const int* p, int rank) {
     asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(dsmem_addr(p, rank)) : "memory");
     return v;
 }
-__device__ __forceinline__ void cluster_barrier() {
-    cluster_arrive_release();
-    cluster_wait();
+// A barrier of the CTAs that work together, after which they see each other's writes.
+template <int CTAS>
+__device__ __forceinline__ void team_barrier() {
+    if constexpr (CTAS == 1) {
+        __syncthreads();
+    } else {
+        cluster_arrive_release();
+        cluster_wait();
+    }
+}
+// Sum of a shared-memory word of every CTA; *before: of those below `rank`.
+template <int CTAS>
+__device__ __forceinline__ long long team_sum(const int* word, int rank, long long* before) {
+    long long all = 0, low = 0;
+#pragma unroll
+    for (int c = 0; c < CTAS; ++c) {
+        const int n = CTAS == 1 ? *word : ld_dsmem_int(word, c);
+        if (c < rank) low += n;
+        all += n;
+    }
+    if (before) *before = low;
+    return all;
 }
 
 // largest s in [0, n) with before[s] <= x (before ascending, before[0] = 0 <= x)
@@ -137,26 +177,28 @@ struct PlanArgs {
     int rows_here;  // write the rows in this launch
 };
 
-__global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS, 1) page_plan_kernel(const PlanArgs p) {
+template <int CTAS>
+__global__ void __launch_bounds__(PG_THREADS, 1) page_plan_kernel(const __grid_constant__ PlanArgs p) {
     extern __shared__ int pg_sm[];
-    __shared__ long long part[PG_WARPS][2];
+    __shared__ uint32_t part[PG_WARPS];
     __shared__ int s_free;
     const mtp_page_plan_args& a = p.a;
-    const int tid = threadIdx.x, rank = blockIdx.x, slots = a.slots;
-    int* rows_before = pg_sm;                  // [slots + 1]
+    const int tid = threadIdx.x, rank = CTAS == 1 ? 0 : blockIdx.x, slots = a.slots;
+    int* rows_before = pg_sm;                     // [slots + 1]
     int* pages_before = rows_before + slots + 1;  // [slots + 1]
-    int* lens = pages_before + slots + 1;      // [slots]
+    int* lens = pages_before + slots + 1;         // [slots]
     uint32_t* bits = reinterpret_cast<uint32_t*>(lens + slots);
+    pdl_launch_dependents();
 
     // the requests: every CTA makes the whole prefix sums
-    long long rows = 0, want = 0;
+    uint32_t rows32 = 0, want = 0, mine = 0;
     bool bad = false;
     for (int s0 = 0; s0 < slots; s0 += PG_THREADS) {
         const int s = s0 + tid;
-        long long x = 0, y = 0, sx, sy;
+        uint32_t x = 0, y = 0, sx, sy;
         if (s < slots) {
             const int len = a.kv_lens[s], add = a.new_lens[s];
-            const bool wrong = len < 0 || add < 0 || (long long)len + add > (long long)a.bt_stride << p.shift;
+            const bool wrong = len < 0 || add < 0 || add > a.max_rows || (long long)len + add > (long long)a.bt_stride << p.shift;
             bad |= wrong;
             lens[s] = len;
             if (!wrong) {
@@ -164,30 +206,32 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS, 1)
                 y = pages_of(len + add, p.shift) - pages_of(len, p.shift);
             }
         }
-        block_scan2<PG_WARPS>(x, y, part, sx, sy);
-        if (s < slots) {  // (sums past 31 bits are refused below)
-            rows_before[s] = (int)min(rows + x, (long long)INT_MAX);
-            pages_before[s] = (int)min(want + y, (long long)INT_MAX);
+        mine += x;
+        x = block_scan(x, part, sx);
+        y = block_scan(y, part, sy);
+        if (s < slots) {  // (more rows than 32 bits hold: nothing of this is used)
+            rows_before[s] = (int)(rows32 + x);
+            pages_before[s] = (int)(want + y);
         }
-        rows += sx;
+        rows32 += sx;
         want += sy;
     }
+    // 8192 requests of 2^24 rows at most: the low and the high halves of the threads' sums, apart
+    uint32_t low, high;
+    block_scan(mine & 0xffff, part, low);
+    block_scan(mine >> 16, part, high);
+    long long rows = ((long long)high << 16) + low;
     if (tid == 0) {
-        rows_before[slots] = (int)min(rows, (long long)INT_MAX);
-        pages_before[slots] = (int)min(want, (long long)INT_MAX);
+        rows_before[slots] = (int)rows;
+        pages_before[slots] = (int)want;
     }
     int code = __syncthreads_or(bad) || rows > a.max_rows ? MTP_ERR_INVALID : MTP_OK;
 
     // the free pages
-    const FreeBits f = find_free(a.page_refs, a.out_page_refs, a.n_pages, rank, bits, part, &s_free);
-    cluster_barrier();
-    long long base = 0, free_all = 0;
-#pragma unroll
-    for (int c = 0; c < PG_CTAS; ++c) {
-        const int n = ld_dsmem_int(&s_free, c);
-        if (c < rank) base += n;
-        free_all += n;
-    }
+    const FreeBits f = find_free<CTAS>(a.page_refs, a.out_page_refs, a.n_pages, rank, bits, part, &s_free);
+    team_barrier<CTAS>();
+    long long base;
+    const long long free_all = team_sum<CTAS>(&s_free, rank, &base);
     if (code == MTP_OK && want > free_all) code = MTP_ERR_NO_PAGES;
     if (code != MTP_OK) rows = want = 0;
     take_free(f, base, want, [&](int page, int n) {
@@ -195,10 +239,10 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS, 1)
         a.block_table[(size_t)s * a.bt_stride + pages_of(lens[s], p.shift) + n - pages_before[s]] = page;
         a.out_page_refs[page] = 1;
     });
-    cluster_barrier();  // the tables are written
+    team_barrier<CTAS>();  // the tables are written
 
     const int gid = rank * PG_THREADS + tid;
-    for (int s = gid; s <= slots; s += PG_CTAS * PG_THREADS) {
+    for (int s = gid; s <= slots; s += CTAS * PG_THREADS) {
         const int before = code == MTP_OK ? rows_before[s] : 0;
         a.out_cu_rows[s] = before;
         if (s < slots) a.out_kv_lens[s] = code == MTP_OK ? lens[s] + rows_before[s + 1] - before : lens[s];
@@ -210,8 +254,34 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS, 1)
         a.out_status[3] = (int)(free_all - want);
     }
     if (!p.rows_here) return;
-    for (int r = gid; r < a.max_rows; r += PG_CTAS * PG_THREADS) {
+    for (int r = gid; r < a.max_rows; r += CTAS * PG_THREADS) {
         const PlanRow o = plan_row(r, (int)rows, rows_before, lens, slots, a.block_table, a.bt_stride, a.n_pages, p.shift);
+        a.out_slot_map[r] = o.at;
+        a.out_row_seq[r] = o.seq;
+        a.out_row_pos[r] = o.pos;
+    }
+}
+
+// The rows of a large plan: a CTA takes ROWS of them, finds the slots in shared memory.
+constexpr int RW_THREADS = 256, RW_ROWS = 1024;
+__global__ void __launch_bounds__(RW_THREADS) plan_rows_kernel(const __grid_constant__ PlanArgs p) {
+    extern __shared__ int pg_sm[];  // [slots + 1] rows before each slot, [slots] lengths before the step
+    const mtp_page_plan_args& a = p.a;
+    const int slots = a.slots, first = blockIdx.x * RW_ROWS;
+    int *before = pg_sm, *lens = pg_sm + slots + 1;
+    pdl_wait();
+    const int rows = a.out_status[1];
+    if (first < rows) {
+        for (int s = threadIdx.x; s <= slots; s += RW_THREADS) before[s] = a.out_cu_rows[s];
+        __syncthreads();
+        for (int s = threadIdx.x; s < slots; s += RW_THREADS) lens[s] = a.out_kv_lens[s] - (before[s + 1] - before[s]);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int u = 0; u < RW_ROWS / RW_THREADS; ++u) {
+        const int r = first + u * RW_THREADS + threadIdx.x;
+        if (r >= a.max_rows) break;
+        const PlanRow o = plan_row(r, rows, before, lens, slots, a.block_table, a.bt_stride, a.n_pages, p.shift);
         a.out_slot_map[r] = o.at;
         a.out_row_seq[r] = o.seq;
         a.out_row_pos[r] = o.pos;
@@ -308,13 +378,13 @@ struct ReorderArgs {
 // plus the kept beams' holdings, minus the old beams'.  A beam that is its own parent and
 // copies nothing adds and takes the same, and is left out.  The additions come first: a
 // count passes zero only where no table holds the page any more.
-__global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS, 1)
-    beam_reorder_kernel(const ReorderArgs p) {
+template <int CTAS>
+__global__ void __launch_bounds__(PG_THREADS, 1) beam_reorder_kernel(const __grid_constant__ ReorderArgs p) {
     extern __shared__ int pg_sm[];
-    __shared__ long long part[PG_WARPS][2];
+    __shared__ uint32_t part[PG_WARPS];
     __shared__ int s_free, s_bad, s_freed;
     const mtp_beam_reorder_args& a = p.a;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, rank = blockIdx.x, rows = p.rows, W = a.beams;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, rank = CTAS == 1 ? 0 : blockIdx.x, rows = p.rows, W = a.beams;
     int* copies_before = pg_sm;                    // [rows + 1]
     int* from = copies_before + rows + 1;          // [rows]: the parent's row, -1 = none
     int* lens = from + rows;                       // [rows]: the parent's length
@@ -322,12 +392,13 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS, 1)
     const long long cap = (long long)a.bt_stride << p.shift;
     const int part_mask = (1 << p.shift) - 1;
 
-    long long want = 0;
+    pdl_launch_dependents();
+    uint32_t want = 0;
     bool bad = false;
     if (tid == 0) s_freed = 0;
     for (int r0 = 0; r0 < rows; r0 += PG_THREADS) {
         const int r = r0 + tid;
-        long long x = 0, y = 0, sx, sy;
+        uint32_t x = 0, sx;
         if (r < rows) {
             const int item = r / W, j = r - item * W, parent = a.parent[r];
             int n = a.kv_lens[r], src = -1;
@@ -344,7 +415,7 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS, 1)
             from[r] = src;
             lens[r] = n;
         }
-        block_scan2<PG_WARPS>(x, y, part, sx, sy);
+        x = block_scan(x, part, sx);
         if (r < rows) copies_before[r] = (int)(want + x);
         want += sx;
     }
@@ -352,29 +423,24 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS, 1)
     bad = __syncthreads_or(bad) != 0;
     // every page that a table holds is one, and is counted
     if (!bad)
-        for (int r = rank * PG_WARPS + warp; r < rows; r += PG_CTAS * PG_WARPS)
+        for (int r = rank * PG_WARPS + warp; r < rows; r += CTAS * PG_WARPS)
             for (int c = lane; c < pages_of(a.kv_lens[r], p.shift); c += 32) {
                 const int page = a.block_table[(size_t)r * a.bt_stride + c];
                 bad |= page < 0 || page >= a.n_pages || a.page_refs[page] < 1;
             }
     bad = __syncthreads_or(bad) != 0;
     if (tid == 0) s_bad = bad;
-    const FreeBits f = find_free(a.page_refs, a.out_page_refs, a.n_pages, rank, bits, part, &s_free);
-    cluster_barrier();  // counts copied, totals there
-    long long base = 0, free_all = 0;
-#pragma unroll
-    for (int c = 0; c < PG_CTAS; ++c) {
-        const int n = ld_dsmem_int(&s_free, c);
-        if (c < rank) base += n;
-        free_all += n;
-        bad |= ld_dsmem_int(&s_bad, c) != 0;
-    }
+    const FreeBits f = find_free<CTAS>(a.page_refs, a.out_page_refs, a.n_pages, rank, bits, part, &s_free);
+    team_barrier<CTAS>();  // counts copied, totals there
+    long long base;
+    const long long free_all = team_sum<CTAS>(&s_free, rank, &base);
+    bad = team_sum<CTAS>(&s_bad, rank, nullptr) != 0;
     const int code = bad ? MTP_ERR_INVALID : want > free_all ? MTP_ERR_NO_PAGES : MTP_OK;
     if (code != MTP_OK) {  // everything stays
-        for (int r = rank * PG_WARPS + warp; r < rows; r += PG_CTAS * PG_WARPS)
+        for (int r = rank * PG_WARPS + warp; r < rows; r += CTAS * PG_WARPS)
             for (int c = lane; c < a.bt_stride; c += 32)
                 a.out_block_table[(size_t)r * a.bt_stride + c] = a.block_table[(size_t)r * a.bt_stride + c];
-        for (int r = rank * PG_THREADS + tid; r < rows; r += PG_CTAS * PG_THREADS) a.out_kv_lens[r] = a.kv_lens[r];
+        for (int r = rank * PG_THREADS + tid; r < rows; r += CTAS * PG_THREADS) a.out_kv_lens[r] = a.kv_lens[r];
         if (rank == 0 && tid == 0) {
             *p.count = 0;
             a.out_status[0] = code;
@@ -382,7 +448,7 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS, 1)
             a.out_status[2] = (int)free_all;
             a.out_status[3] = 0;
         }
-        cluster_barrier();  // no peer still reads this CTA's shared memory
+        if (CTAS > 1) team_barrier<CTAS>();  // no peer still reads this CTA's shared memory
         return;
     }
     take_free(f, base, want, [&](int page, int n) {
@@ -391,9 +457,9 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS, 1)
                                 tokens & part_mask, 0);
         a.out_page_refs[page] = 1;
     });
-    cluster_barrier();  // the copies' pages are known
+    team_barrier<CTAS>();  // the copies' pages are known
     auto itself = [&](int r) { return from[r] == r && copies_before[r + 1] == copies_before[r]; };
-    for (int r = rank * PG_WARPS + warp; r < rows; r += PG_CTAS * PG_WARPS) {
+    for (int r = rank * PG_WARPS + warp; r < rows; r += CTAS * PG_WARPS) {
         const bool fresh = copies_before[r + 1] != copies_before[r], same = itself(r);
         const int used = pages_of(lens[r], p.shift);
         for (int c = lane; c < a.bt_stride; c += 32) {
@@ -409,25 +475,24 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS, 1)
             a.out_block_table[(size_t)r * a.bt_stride + c] = page;
         }
     }
-    cluster_barrier();
+    team_barrier<CTAS>();
     int freed = 0;
-    for (int r = rank * PG_WARPS + warp; r < rows; r += PG_CTAS * PG_WARPS)
+    for (int r = rank * PG_WARPS + warp; r < rows; r += CTAS * PG_WARPS)
         if (!itself(r))
             for (int c = lane; c < pages_of(a.kv_lens[r], p.shift); c += 32)
                 freed += atomicSub(a.out_page_refs + a.block_table[(size_t)r * a.bt_stride + c], 1) == 1;
     if (freed) atomicAdd(&s_freed, freed);
-    cluster_barrier();
-    for (int r = rank * PG_THREADS + tid; r < rows; r += PG_CTAS * PG_THREADS) a.out_kv_lens[r] = lens[r];
+    team_barrier<CTAS>();
+    for (int r = rank * PG_THREADS + tid; r < rows; r += CTAS * PG_THREADS) a.out_kv_lens[r] = lens[r];
     if (rank == 0 && tid == 0) {
-        long long all = free_all - want;
-        for (int c = 0; c < PG_CTAS; ++c) all += ld_dsmem_int(&s_freed, c);
+        const long long all = free_all - want + team_sum<CTAS>(&s_freed, rank, nullptr);
         *p.count = (int)want;
         a.out_status[0] = MTP_OK;
         a.out_status[1] = (int)want;
         a.out_status[2] = (int)all;
         a.out_status[3] = 0;
     }
-    cluster_barrier();  // no peer still reads this CTA's shared memory
+    if (CTAS > 1) team_barrier<CTAS>();  // no peer still reads this CTA's shared memory
 }
 
 constexpr int CP_THREADS = 256, CP_UNROLL = 4;
@@ -435,14 +500,15 @@ constexpr int CP_THREADS = 256, CP_UNROLL = 4;
 // The filled rows of every copied page: for each (layer, keys | values, head) one run of
 // tokens * head_dim elements.  A warp takes a run; CP_UNROLL loads are in flight per lane.
 // Bound by memory: each row is read once and written once.
-__global__ void __launch_bounds__(CP_THREADS) page_copy_kernel(const ReorderArgs p, int runs) {
+__global__ void __launch_bounds__(CP_THREADS) page_copy_kernel(const __grid_constant__ ReorderArgs p, int runs) {
+    pdl_wait();
     const int n = *p.count, lane = threadIdx.x & 31;
     const long long total = (long long)n * runs, stride = (long long)gridDim.x * (CP_THREADS / 32);
     const size_t block = (size_t)p.a.head_dim << p.shift >> 3;  // 16-byte pieces of a (page, layer, K | V, head) block
     uint4* pool = static_cast<uint4*>(p.a.kv_pool);
     for (long long w = (long long)blockIdx.x * (CP_THREADS / 32) + (threadIdx.x >> 5); w < total; w += stride) {
         const int i = (int)(w / runs), run = (int)(w - (long long)i * runs);
-        const int4 c = __ldg(p.copies + i);
+        const int4 c = p.copies[i];
         const uint4* src = pool + ((size_t)c.x * runs + run) * block;
         uint4* dst = pool + ((size_t)c.y * runs + run) * block;
         const int pieces = c.z * (p.a.head_dim >> 3);
@@ -468,6 +534,28 @@ int check_pool(const char* what, int n_pages, int layers, int layer, int n_kv_he
     return MTP_OK;
 }
 
+// Enqueue a kernel; clusters of `cluster` CTAs; `pdl`: it may start while the kernel before it runs.
+template <class... P>
+cudaError_t launch(void (*kern)(P...), int grid, int threads, size_t smem, int cluster, bool pdl, cudaStream_t s, P... args) {
+    cudaError_t e = smem > 48 * 1024 ? ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem) : cudaSuccess;
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = pdl ? 1 : 0;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
 size_t reorder_workspace(int rows) { return 16 + (size_t)rows * sizeof(int4); }
 
 }  // namespace
@@ -487,14 +575,14 @@ MTP_API int mtp_page_plan(const mtp_page_plan_args* a, void* cuda_stream) {
             !a->out_cu_rows || !a->out_status ||
             (a->max_rows > 0 && (!a->out_slot_map || !a->out_row_seq || !a->out_row_pos)))
             return invalid("page_plan: null pointer");
-        PlanArgs p{*a, log2_of(a->page_size), 1};
-        const size_t smem = (size_t)(3 * a->slots + 2 + free_words(a->n_pages)) * 4;
+        const bool one = a->n_pages <= PG_ONE_PAGES && a->slots <= PG_ONE_SLOTS;
+        const PlanArgs p{*a, log2_of(a->page_size), a->max_rows <= PG_ONE_ROWS};
+        const size_t smem = (size_t)(3 * a->slots + 2 + free_words(a->n_pages, one ? 1 : PG_CLUSTER)) * 4;
         const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-        cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(page_plan_kernel), smem);
-        if (e == cudaSuccess) {
-            page_plan_kernel<<<PG_CTAS, PG_THREADS, smem, s>>>(p);
-            e = cudaGetLastError();
-        }
+        cudaError_t e = one ? launch(page_plan_kernel<1>, 1, PG_THREADS, smem, 1, false, s, p)
+                            : launch(page_plan_kernel<PG_CLUSTER>, PG_CLUSTER, PG_THREADS, smem, PG_CLUSTER, false, s, p);
+        if (e == cudaSuccess && !p.rows_here)
+            e = launch(plan_rows_kernel, (a->max_rows + RW_ROWS - 1) / RW_ROWS, RW_THREADS, (size_t)(2 * a->slots + 1) * 4, 1, true, s, p);
         return cuda_status(e, "page_plan");
     });
 }
@@ -558,21 +646,17 @@ MTP_API int mtp_beam_reorder(const mtp_beam_reorder_args* a, void* workspace, si
                            reorder_workspace(rows));
         ReorderArgs p{*a, log2_of(a->page_size), rows, static_cast<int*>(workspace),
                       reinterpret_cast<int4*>(static_cast<char*>(workspace) + 16)};
-        const size_t smem = (size_t)(3 * rows + 1 + free_words(a->n_pages)) * 4;
+        const bool one = a->n_pages <= PG_ONE_PAGES && rows <= PG_ONE_BEAMS;
+        const size_t smem = (size_t)(3 * rows + 1 + free_words(a->n_pages, one ? 1 : PG_CLUSTER)) * 4;
         const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-        cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(beam_reorder_kernel), smem);
-        if (e == cudaSuccess) {
-            beam_reorder_kernel<<<PG_CTAS, PG_THREADS, smem, s>>>(p);
-            e = cudaGetLastError();
-        }
+        cudaError_t e = one ? launch(beam_reorder_kernel<1>, 1, PG_THREADS, smem, 1, false, s, p)
+                            : launch(beam_reorder_kernel<PG_CLUSTER>, PG_CLUSTER, PG_THREADS, smem, PG_CLUSTER, false, s, p);
         if (e == cudaSuccess && a->beams > 1) {  // (one beam has nothing to copy)
             int dev = 0, sms = 0;
             e = cudaGetDevice(&dev);
             if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-            if (e == cudaSuccess) {
-                page_copy_kernel<<<sms * 8, CP_THREADS, 0, s>>>(p, a->layers * 2 * a->n_kv_heads);
-                e = cudaGetLastError();
-            }
+            if (e == cudaSuccess)
+                e = launch(page_copy_kernel, sms * 8, CP_THREADS, 0, 1, true, s, p, a->layers * 2 * a->n_kv_heads);
         }
         return cuda_status(e, "beam_reorder");
     });
