@@ -642,7 +642,8 @@ MTP_API int mtp_beam_select(const mtp_beam_select_args* args, void* workspace, s
  * outside the table, a held page outside the pool or with a count below 1) the outputs
  * repeat the inputs and no page is written.
  *   workspace      mtp_beam_reorder_workspace_bytes(args) bytes, 16-byte aligned
- * Limits: beams <= 64, batch * beams <= 8192, n_pages <= 2^22, bt_stride * page_size <= 2^30,
+ * Limits: beams <= 64, batch * beams <= 8192, n_pages <= 2^22, bt_stride * page_size and
+ * batch * beams * bt_stride <= 2^30,
  * head_dim a multiple of 8, at most 256.  Errors: MTP_ERR_INVALID, MTP_ERR_CUDA. */
 typedef struct mtp_beam_reorder_args {
     int32_t batch, beams, page_size, n_pages, bt_stride, layers, n_kv_heads, head_dim, pool_dtype;

@@ -28,16 +28,15 @@ namespace {
 
 constexpr int PG_CLUSTER = 8, PG_THREADS = 1024, PG_WARPS = PG_THREADS / 32;
 // one CTA up to these (32 slots and 2048 pages, one CTA against eight: 6.9 and 8.2 us a plan; 16384 pages: level)
-constexpr int PG_ONE_PAGES = 16384, PG_ONE_SLOTS = 1024, PG_ONE_ROWS = 8192, PG_ONE_BEAMS = 128;
+constexpr int PG_ONE_PAGES = 16384, PG_ONE_SLOTS = 1024, PG_ONE_ROWS = 8192, PG_ONE_BEAMS = 512, PG_KEPT = 16384;
 constexpr int PG_MAX_SLOTS = 8192;
 constexpr int PG_MAX_PAGES = 1 << 22;
 constexpr int PG_MAX_ROWS = 1 << 24;
 
 struct FreeBits {
     uint32_t* bits;       // shared memory: a bit per page of this CTA's part, set where it is free
+    uint32_t* before;     // [words] free pages of the part before each word
     int first, words;     // the part: words [first, first + words) of 32 pages
-    int per;              // words of a thread, consecutive
-    long long before;     // free pages of the CTA before this thread's
 };
 
 __host__ __device__ inline int free_words(int n_pages, int ctas) {  // words of a CTA's part
@@ -71,6 +70,7 @@ __device__ __forceinline__ FreeBits find_free(const int* refs, int* out_refs, in
     FreeBits f;
     const int all = (n_pages + 31) / 32, cap = free_words(n_pages, CTAS);
     f.bits = bits;
+    f.before = bits + cap;
     f.first = rank * cap;
     f.words = max(0, min(cap, all - f.first));
     const bool copy = out_refs != refs;
@@ -91,26 +91,29 @@ __device__ __forceinline__ FreeBits find_free(const int* refs, int* out_refs, in
         }
     }
     __syncthreads();
-    f.per = (f.words + PG_THREADS - 1) / PG_THREADS;
+    const int per = (f.words + PG_THREADS - 1) / PG_THREADS;  // words of a thread, consecutive
     uint32_t n = 0, sum;
-    for (int i = 0; i < f.per; ++i) {
-        const int w = tid * f.per + i;
-        if (w < f.words) n += __popc(bits[w]);
+    for (int w = tid * per; w < min((tid + 1) * per, f.words); ++w) n += __popc(bits[w]);
+    n = block_scan(n, part, sum);
+    for (int w = tid * per; w < min((tid + 1) * per, f.words); ++w) {
+        f.before[w] = n;
+        n += __popc(bits[w]);
     }
-    f.before = block_scan(n, part, sum);
     if (tid == 0) *total = (int)sum;
     return f;
 }
 
-// take(page, rank) for every free page of this thread's words whose rank among all is below `want`
+// take(page, rank) for the free pages of this CTA's part whose rank among all is below `want`: a
+// warp takes a word of the bits at a time, a lane a page.
 template <class F>
 __device__ __forceinline__ void take_free(const FreeBits& f, long long base, long long want, F take) {
-    long long rank = base + f.before;
-    for (int i = 0; i < f.per && rank < want; ++i) {
-        const int w = threadIdx.x * f.per + i;
-        if (w >= f.words) break;
-        for (uint32_t b = f.bits[w]; b && rank < want; b &= b - 1, ++rank)
-            take((f.first + w) * 32 + __ffs(b) - 1, (int)rank);
+    const int lane = threadIdx.x & 31;
+    for (int w = threadIdx.x >> 5; w < f.words; w += PG_WARPS) {
+        const long long first = base + f.before[w];
+        if (first >= want) break;
+        const uint32_t b = f.bits[w];
+        const long long rank = first + __popc(b & ((1u << lane) - 1));
+        if ((b >> lane & 1) && rank < want) take((f.first + w) * 32 + lane, (int)rank);
     }
 }
 
@@ -369,6 +372,7 @@ struct ReorderArgs {
     mtp_beam_reorder_args a;
     int shift;
     int rows;      // batch * beams
+    int kept;      // table entries that shared memory holds
     int* count;    // workspace: pages to copy
     int4* copies;  // workspace: {from, to, tokens, -}
 };
@@ -387,8 +391,9 @@ __global__ void __launch_bounds__(PG_THREADS, 1) beam_reorder_kernel(const __gri
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, rank = CTAS == 1 ? 0 : blockIdx.x, rows = p.rows, W = a.beams;
     int* copies_before = pg_sm;                    // [rows + 1]
     int* from = copies_before + rows + 1;          // [rows]: the parent's row, -1 = none
-    int* lens = from + rows;                       // [rows]: the parent's length
-    uint32_t* bits = reinterpret_cast<uint32_t*>(lens + rows);
+    int* old = from + rows;                        // [rows]: the length before
+    uint32_t* bits = reinterpret_cast<uint32_t*>(old + rows);
+    auto lens = [&](int r) { return from[r] < 0 ? 0 : old[from[r]]; };  // the parent's
     const long long cap = (long long)a.bt_stride << p.shift;
     const int part_mask = (1 << p.shift) - 1;
 
@@ -402,6 +407,7 @@ __global__ void __launch_bounds__(PG_THREADS, 1) beam_reorder_kernel(const __gri
         if (r < rows) {
             const int item = r / W, j = r - item * W, parent = a.parent[r];
             int n = a.kv_lens[r], src = -1;
+            old[r] = n;
             bad |= parent >= W || n < 0 || n > cap;
             n = 0;
             if (parent >= 0 && parent < W) {
@@ -409,11 +415,11 @@ __global__ void __launch_bounds__(PG_THREADS, 1) beam_reorder_kernel(const __gri
                 n = a.kv_lens[src];
                 if (n < 0 || n > cap) n = 0;  // (refused)
                 bool again = false;
+#pragma unroll 4
                 for (int i = 0; i < j; ++i) again |= a.parent[item * W + i] == parent;
                 x = again && (n & part_mask);
             }
             from[r] = src;
-            lens[r] = n;
         }
         x = block_scan(x, part, sx);
         if (r < rows) copies_before[r] = (int)(want + x);
@@ -421,13 +427,22 @@ __global__ void __launch_bounds__(PG_THREADS, 1) beam_reorder_kernel(const __gri
     }
     if (tid == 0) copies_before[rows] = (int)want;
     bad = __syncthreads_or(bad) != 0;
-    // every page that a table holds is one, and is counted
+    // every page that a table holds is one, and is counted (an entry per thread; the old tables stay in shared memory
+    // where they fit, for the steps below)
+    const unsigned stride = a.bt_stride, first = rank * PG_THREADS + tid, step = CTAS * PG_THREADS, entries = rows * stride;
+    const bool keep = CTAS == 1 && entries <= (unsigned)p.kept;
+    int* kept = reinterpret_cast<int*>(bits + 2 * free_words(a.n_pages, CTAS));
     if (!bad)
-        for (int r = rank * PG_WARPS + warp; r < rows; r += CTAS * PG_WARPS)
-            for (int c = lane; c < pages_of(a.kv_lens[r], p.shift); c += 32) {
-                const int page = a.block_table[(size_t)r * a.bt_stride + c];
+#pragma unroll 4
+        for (unsigned e = first; e < entries; e += step) {
+            const int r = e / stride, c = e - r * stride;
+            int page = -1;
+            if (c < pages_of(old[r], p.shift)) {
+                page = a.block_table[e];
                 bad |= page < 0 || page >= a.n_pages || a.page_refs[page] < 1;
             }
+            if (keep) kept[e] = page;
+        }
     bad = __syncthreads_or(bad) != 0;
     if (tid == 0) s_bad = bad;
     const FreeBits f = find_free<CTAS>(a.page_refs, a.out_page_refs, a.n_pages, rank, bits, part, &s_free);
@@ -452,38 +467,39 @@ __global__ void __launch_bounds__(PG_THREADS, 1) beam_reorder_kernel(const __gri
         return;
     }
     take_free(f, base, want, [&](int page, int n) {
-        const int r = owner_of(copies_before, rows + 1, n), tokens = lens[r];
+        const int r = owner_of(copies_before, rows + 1, n), tokens = lens(r);
         p.copies[n] = make_int4(a.block_table[(size_t)from[r] * a.bt_stride + (tokens >> p.shift)], page,
                                 tokens & part_mask, 0);
         a.out_page_refs[page] = 1;
     });
     team_barrier<CTAS>();  // the copies' pages are known
     auto itself = [&](int r) { return from[r] == r && copies_before[r + 1] == copies_before[r]; };
-    for (int r = rank * PG_WARPS + warp; r < rows; r += CTAS * PG_WARPS) {
-        const bool fresh = copies_before[r + 1] != copies_before[r], same = itself(r);
-        const int used = pages_of(lens[r], p.shift);
-        for (int c = lane; c < a.bt_stride; c += 32) {
-            int page = -1;
-            if (c < used) {
-                if (fresh && c == used - 1) {
-                    page = __ldcg(&p.copies[copies_before[r]].y);
-                } else {
-                    page = a.block_table[(size_t)from[r] * a.bt_stride + c];
-                    if (!same) atomicAdd(a.out_page_refs + page, 1);
-                }
+#pragma unroll 4
+    for (unsigned e = first; e < entries; e += step) {
+        const int r = e / stride, c = e - r * stride, used = pages_of(lens(r), p.shift);
+        int page = -1;
+        if (c < used) {
+            if (c == used - 1 && copies_before[r + 1] != copies_before[r]) {
+                page = __ldcg(&p.copies[copies_before[r]].y);
+            } else {
+                const unsigned at = from[r] * stride + c;
+                page = keep ? kept[at] : a.block_table[at];
+                if (!itself(r)) atomicAdd(a.out_page_refs + page, 1);
             }
-            a.out_block_table[(size_t)r * a.bt_stride + c] = page;
         }
+        a.out_block_table[e] = page;
     }
     team_barrier<CTAS>();
     int freed = 0;
-    for (int r = rank * PG_WARPS + warp; r < rows; r += CTAS * PG_WARPS)
-        if (!itself(r))
-            for (int c = lane; c < pages_of(a.kv_lens[r], p.shift); c += 32)
-                freed += atomicSub(a.out_page_refs + a.block_table[(size_t)r * a.bt_stride + c], 1) == 1;
+#pragma unroll 4
+    for (unsigned e = first; e < entries; e += step) {
+        const int r = e / stride, c = e - r * stride;
+        if (c < pages_of(old[r], p.shift) && !itself(r))
+            freed += atomicSub(a.out_page_refs + (keep ? kept[e] : a.block_table[e]), 1) == 1;
+    }
     if (freed) atomicAdd(&s_freed, freed);
     team_barrier<CTAS>();
-    for (int r = rank * PG_THREADS + tid; r < rows; r += CTAS * PG_THREADS) a.out_kv_lens[r] = lens[r];
+    for (int r = rank * PG_THREADS + tid; r < rows; r += CTAS * PG_THREADS) a.out_kv_lens[r] = lens(r);
     if (rank == 0 && tid == 0) {
         const long long all = free_all - want + team_sum<CTAS>(&s_freed, rank, nullptr);
         *p.count = (int)want;
@@ -577,7 +593,7 @@ MTP_API int mtp_page_plan(const mtp_page_plan_args* a, void* cuda_stream) {
             return invalid("page_plan: null pointer");
         const bool one = a->n_pages <= PG_ONE_PAGES && a->slots <= PG_ONE_SLOTS;
         const PlanArgs p{*a, log2_of(a->page_size), a->max_rows <= PG_ONE_ROWS};
-        const size_t smem = (size_t)(3 * a->slots + 2 + free_words(a->n_pages, one ? 1 : PG_CLUSTER)) * 4;
+        const size_t smem = (size_t)(3 * a->slots + 2 + 2 * free_words(a->n_pages, one ? 1 : PG_CLUSTER)) * 4;
         const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
         cudaError_t e = one ? launch(page_plan_kernel<1>, 1, PG_THREADS, smem, 1, false, s, p)
                             : launch(page_plan_kernel<PG_CLUSTER>, PG_CLUSTER, PG_THREADS, smem, PG_CLUSTER, false, s, p);
@@ -629,7 +645,8 @@ MTP_API int mtp_beam_reorder(const mtp_beam_reorder_args* a, void* workspace, si
         if (const int r = check_pool("beam_reorder", a->n_pages, a->layers, 0, a->n_kv_heads, a->head_dim, a->page_size))
             return r;
         if (a->batch < 1 || a->beams < 1 || a->beams > 64 || (long long)a->batch * a->beams > PG_MAX_SLOTS ||
-            a->bt_stride < 1 || (long long)a->bt_stride * a->page_size > (1 << 30))
+            a->bt_stride < 1 || (long long)a->bt_stride * a->page_size > (1 << 30) ||
+            (long long)a->batch * a->beams * a->bt_stride > (1 << 30))
             return invalid("beam_reorder: invalid sizes (batch %d, beams %d, bt_stride %d)", a->batch, a->beams,
                            a->bt_stride);
         if (a->pool_dtype != MTP_BF16 && a->pool_dtype != MTP_F16)
@@ -644,10 +661,12 @@ MTP_API int mtp_beam_reorder(const mtp_beam_reorder_args* a, void* workspace, si
         if (!workspace || !aligned16(workspace) || workspace_bytes < reorder_workspace(rows))
             return invalid("beam_reorder: workspace %zu bytes, need %zu, 16-byte aligned", workspace_bytes,
                            reorder_workspace(rows));
-        ReorderArgs p{*a, log2_of(a->page_size), rows, static_cast<int*>(workspace),
-                      reinterpret_cast<int4*>(static_cast<char*>(workspace) + 16)};
         const bool one = a->n_pages <= PG_ONE_PAGES && rows <= PG_ONE_BEAMS;
-        const size_t smem = (size_t)(3 * rows + 1 + free_words(a->n_pages, one ? 1 : PG_CLUSTER)) * 4;
+        const long long entries = (long long)rows * a->bt_stride;
+        const int kept = one && entries <= PG_KEPT ? (int)entries : 0;
+        const ReorderArgs p{*a, log2_of(a->page_size), rows, kept, static_cast<int*>(workspace),
+                            reinterpret_cast<int4*>(static_cast<char*>(workspace) + 16)};
+        const size_t smem = (size_t)(3 * rows + 1 + 2 * free_words(a->n_pages, one ? 1 : PG_CLUSTER) + kept) * 4;
         const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
         cudaError_t e = one ? launch(beam_reorder_kernel<1>, 1, PG_THREADS, smem, 1, false, s, p)
                             : launch(beam_reorder_kernel<PG_CLUSTER>, PG_CLUSTER, PG_THREADS, smem, PG_CLUSTER, false, s, p);
