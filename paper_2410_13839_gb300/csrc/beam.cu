@@ -22,13 +22,15 @@
 // before it, whose reading leaves the logits in L2.
 #include <float.h>
 
+#include <algorithm>
+
 #include "serving.cuh"
 
 namespace mtp {
 namespace {
 
 constexpr int BS_THREADS = 512, BS_WARPS = BS_THREADS / 32;
-constexpr int SEG = 16384;        // scores of a CTA: 64 KB, three CTAs to an SM
+constexpr int SEG = 14336, LEAST = 2048;  // most scores of a CTA (56 KB, three CTAs to an SM) and fewest
 constexpr int GROUPS = 128;       // groups of four threads, each with a maximum
 constexpr int CAND_MAX = 1024;
 constexpr int BS_MAX_K = 64, BS_MAX_BEAMS = 64, BS_MAX_BATCH = 4096;
@@ -43,9 +45,10 @@ struct SelectArgsB {
     int* count;                   // [batch]
 };
 
+// A score as it is ranked: NaN is -inf, -0 is 0.
+__device__ __forceinline__ float ranked(float score) { return isnan(score) ? -INFINITY : score + 0.f; }
 __device__ __forceinline__ unsigned long long make_key(float score, uint32_t number) {
-    if (isnan(score)) score = -INFINITY;
-    uint32_t u = __float_as_uint(score + 0.f);  // (-0 is 0)
+    uint32_t u = __float_as_uint(score);
     u ^= (u >> 31) ? 0xffffffffu : 0x80000000u;
     return (unsigned long long)u << 32 | (0xffffffffu - number);
 }
@@ -70,12 +73,10 @@ struct Best {
 
 // The k largest of key(0) .. key(n - 1) into b.best, descending; 0 past the last.
 // The whole block calls it, with the keys visible to all; b.best is visible afterwards.
+// `most`: the largest of this thread's keys, those of tid, tid + BS_THREADS, ...
 template <class KEY>
-__device__ __forceinline__ void best_of(Best& b, int n, int k, KEY key) {
+__device__ __forceinline__ void best_of(Best& b, int n, int k, unsigned long long most, KEY key) {
     const int tid = threadIdx.x;
-    unsigned long long most = 0;
-#pragma unroll 8
-    for (int i = tid; i < n; i += BS_THREADS) most = max(most, key(i));
     b.thread_max[tid] = most;
     if (tid == 0) {
         b.bound = 1;  // fewer than k groups with a key: all keys
@@ -162,25 +163,29 @@ struct Half {
     }
 };
 
-// use(i, x) for the elements [0, n) at p + first, by the block: single ones up to the first
-// 16-byte boundary, 16 bytes at a time with UNROLL loads in flight, single ones at the end.
-template <class T, int THREADS, int UNROLL, class F>
-__device__ __forceinline__ void for_row(const void* base, int64_t first, int n, F use) {
+// use(i, x) for the elements [0, n) at p + first, by `warps` warps of which this is number `warp`: 16 bytes at a
+// time, UNROLL loads in flight, each warp a stretch of 32 UNROLL pieces; the single elements before the
+// first and after the last 16-byte boundary by warp 0.  Returns the stretches there are.
+template <class T, int UNROLL, class F>
+__device__ __forceinline__ int for_row(const void* base, int64_t first, int n, int warp, int warps, F use) {
     using E = typename T::elem;
     const E* p = static_cast<const E*>(base) + first;
-    const int tid = threadIdx.x;
+    const int lane = threadIdx.x & 31;
     const int head = min(n, (int)(((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / sizeof(E)));
-    const int vecs = (n - head) / T::PER;
-    if (tid < head) use(tid, T::one(p, tid));
+    const int vecs = (n - head) / T::PER, rest = head + vecs * T::PER + lane;
+    if (warp == 0) {
+        if (lane < head) use(lane, T::one(p, lane));
+        if (rest < n) use(rest, T::one(p, rest));
+    }
     const uint4* v = reinterpret_cast<const uint4*>(p + head);
-    for (int i0 = tid; i0 < vecs; i0 += THREADS * UNROLL) {
+    for (int i0 = warp * (32 * UNROLL) + lane; i0 - lane < vecs; i0 += warps * (32 * UNROLL)) {
         uint4 raw[UNROLL];
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u)
-            if (i0 + u * THREADS < vecs) raw[u] = __ldg(v + i0 + u * THREADS);
+            if (i0 + u * 32 < vecs) raw[u] = __ldg(v + i0 + u * 32);
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            const int i = i0 + u * THREADS;
+            const int i = i0 + u * 32;
             if (i < vecs) {
                 float x[T::PER];
                 T::unpack(raw[u], x);
@@ -189,8 +194,7 @@ __device__ __forceinline__ void for_row(const void* base, int64_t first, int n, 
             }
         }
     }
-    const int rest = head + vecs * T::PER + tid;
-    if (rest < n) use(rest, T::one(p, rest));
+    return max(1, (vecs + 32 * UNROLL - 1) / (32 * UNROLL));
 }
 
 // (maximum, sum of exp(x - maximum)) of two sets, as one
@@ -215,7 +219,7 @@ __global__ void __launch_bounds__(LSE_THREADS) row_lse_kernel(const void* logits
     const int row = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_launch_dependents();
     float m = -INFINITY, s = 0.f;
-    for_row<T, LSE_THREADS, 4>(logits, row * stride, vocab, [&](int, float x) {
+    for_row<T, 4>(logits, row * stride, vocab, warp, LSE_THREADS / 32, [&](int, float x) {
         if (x > m) {
             s *= __expf(m - x);  // (the first value: 0)
             m = x;
@@ -250,40 +254,55 @@ __global__ void __launch_bounds__(BS_THREADS) beam_select_kernel(const SelectArg
         if (!p.lse_here) s_lse[tid] = p.lse[item * W + tid];
     }
     __syncthreads();
-    // the segment's logits, beam by beam, as scores (as they are where their log-sum-exp is still to come)
-    const int beam0 = first / V, beam1 = (first + n - 1) / V;
+    // the segment's logits, beam by beam, as scores (as they are where their log-sum-exp is still to come); the
+    // beams' stretches go round the warps, so that short rows are on their way together
+    const int beam0 = first / V, beam1 = (first + n - 1) / V, warp = tid >> 5, lane = tid & 31;
+    int turn = warp;
     for (int w = beam0; w <= beam1; ++w) {
         const int c0 = max(0, first - w * V), c1 = min(V, first + n - w * V);
         float* to = bs_score + (w * V + c0 - first);
         const float cum = s_beam[w], lse = p.lse_here ? 0.f : s_lse[w];
         if (s_done[w] && !p.lse_here) {
-            for (int i = tid; i < c1 - c0; i += BS_THREADS) to[i] = c0 + i == a.eos_id ? cum : -INFINITY;
+            for (int i = tid; i < c1 - c0; i += BS_THREADS) to[i] = c0 + i == a.eos_id ? ranked(cum) : -INFINITY;
         } else {
             const bool raw = p.lse_here;
-            for_row<T, BS_THREADS, 4>(a.logits, ((int64_t)item * W + w) * a.logits_stride + c0, c1 - c0,
-                                      [&](int i, float x) { to[i] = raw ? x : cum + (x - lse); });
+            const int used = for_row<T, 4>(a.logits, ((int64_t)item * W + w) * a.logits_stride + c0, c1 - c0, turn, BS_WARPS,
+                                           [&](int i, float x) { to[i] = raw ? x : ranked(cum + (x - lse)); });
+            turn = (turn + BS_WARPS - used % BS_WARPS) % BS_WARPS;
         }
     }
     __syncthreads();
-    if (p.lse_here) {
-        for (int w = tid >> 5; w < W; w += BS_WARPS) {
-            const float* x = bs_score + w * V;
+    if (p.lse_here) {  // a warp per beam
+        for (int w = warp; w < W; w += BS_WARPS) {
+            float* x = bs_score + w * V;
             float m = -INFINITY, s = 0.f;
-            for (int i = tid & 31; i < V; i += 32) m = fmaxf(m, x[i]);
+#pragma unroll 8
+            for (int i = lane; i < V; i += 32) m = fmaxf(m, x[i]);
             m = warp_max(m);
-            for (int i = tid & 31; i < V; i += 32) s += x[i] == -INFINITY ? 0.f : __expf(x[i] - m);
+            const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll 8
+            for (int i = lane; i < V; i += 32) s += __expf(x[i] - ref);
             s = warp_sum(s);
-            if ((tid & 31) == 0) s_lse[w] = m + logf(s);
-        }
-        __syncthreads();
-        for (int i = tid; i < n; i += BS_THREADS) {
-            const int w = i / V;
-            bs_score[i] = !s_done[w] ? s_beam[w] + (bs_score[i] - s_lse[w]) : i - w * V == a.eos_id ? s_beam[w] : -INFINITY;
+            const float lse = m + logf(s), cum = s_beam[w];
+            if (lane == 0) s_lse[w] = lse;
+            const bool done = s_done[w];
+#pragma unroll 8
+            for (int i = lane; i < V; i += 32) x[i] = ranked(!done ? cum + (x[i] - lse) : i == a.eos_id ? cum : -INFINITY);
         }
         __syncthreads();
     }
     if (seg == 0 && a.out_lse && tid < W) a.out_lse[item * W + tid] = s_lse[tid];
-    best_of(b, n, a.k, [&](int i) { return make_key(bs_score[i], (uint32_t)(first + i)); });
+    // this thread's largest score, the first of equal ones
+    float most = -INFINITY;
+    int at_most = tid;
+#pragma unroll 8
+    for (int i = tid; i < n; i += BS_THREADS)
+        if (bs_score[i] > most) {
+            most = bs_score[i];
+            at_most = i;
+        }
+    best_of(b, n, a.k, tid < n ? make_key(most, (uint32_t)(first + at_most)) : 0ull,
+            [&](int i) { return make_key(bs_score[i], (uint32_t)(first + i)); });
 
     if (p.segments > 1) {
         unsigned long long* keys = p.keys + (size_t)item * p.segments * a.k;
@@ -303,7 +322,9 @@ __global__ void __launch_bounds__(BS_THREADS) beam_select_kernel(const SelectArg
             const int take = min(room - have, total - at);
             for (int i = tid; i < take; i += BS_THREADS) held[have + i] = __ldcg(keys + at + i);
             __syncthreads();
-            best_of(b, have + take, a.k, [&](int i) { return held[i]; });
+            unsigned long long most = 0;
+            for (int i = tid; i < have + take; i += BS_THREADS) most = max(most, held[i]);
+            best_of(b, have + take, a.k, most, [&](int i) { return held[i]; });
             at += take;
             have = a.k;
             if (at < total) {
@@ -340,7 +361,16 @@ int select_plan(const mtp_beam_select_args* a, SelectPlan* p) {
     if (a->logits_dtype != MTP_F32 && a->logits_dtype != MTP_BF16 && a->logits_dtype != MTP_F16)
         return invalid("beam_select: logits_dtype %d", a->logits_dtype);
     const int all = a->beams * a->vocab;
-    p->segments = (all + SEG - 1) / SEG;
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        cudaGetLastError();
+        sms = 152;  // (the sizes are checked all the same; a launch will say what is wrong)
+    }
+    // as many segments as fill one wave of three CTAs per SM, none shorter than LEAST (an item of up to SEG scores
+    // and no log-sum-exp stays one: nothing to join) and none longer than shared memory holds
+    const int most = (all + LEAST - 1) / LEAST, least = (all + SEG - 1) / SEG;
+    p->segments = least == 1 && (!a->lse || all <= 4 * LEAST) ? 1 : std::max(least, std::min(most, std::max(1, 3 * sms / a->batch)));
     p->seg_len = ((all + p->segments - 1) / p->segments + 7) & ~7;  // even segments
     p->segments = (all + p->seg_len - 1) / p->seg_len;
     p->lse_here = !a->lse && p->segments == 1;
