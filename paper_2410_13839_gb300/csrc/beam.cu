@@ -9,17 +9,20 @@
 // complement of its number: keys are distinct, so the k largest are one set, whatever
 // order they are looked at in, and no tie is a special case.
 //
-// The best of n keys in shared memory (best_of): 128 groups of threads give a maximum
-// each; the k-th largest of these maxima is a bound that at least k keys reach, and hardly
-// more do (for k = 8 about 8.3 are expected, for k = 64 about 89); those are gathered and
-// ranked by counting.  Where more than CAND_MAX reach it (runs of equal scores that one
-// group holds), the keys are taken out one by one instead.
+// The best keys of a CTA (best_of): a thread goes through its own keys once for their maximum;
+// 128 groups of threads give a maximum each; the k-th largest of these is a bound that at least
+// k keys reach, and hardly more do (for k = 8 about 8.3 are expected, for k = 64 about 89).  The
+// few threads with a key that reaches it go through theirs again, and what they find is ranked
+// by counting.  Where more than CAND_MAX keys reach it (runs of equal scores that one group
+// holds), the keys are taken out one by one instead.
 //
-// A CTA holds up to SEG scores in shared memory.  Items of more are cut into segments; each
-// leaves its k best keys in the workspace, and the item's CTA that finishes last (an atomic
-// counter, reset by it) selects among these.  The log-sum-exp, where it is not given, is
-// taken from shared memory in the same launch if the item is one segment, else by a kernel
-// before it, whose reading leaves the logits in L2.
+// The logits of a long item are not stored anywhere: the second look is L2's.  (Kept in shared
+// memory as scores, 32 x 4 beams of 48001 took 21 us: the stores of 16-byte pieces conflict.)  An item
+// is cut into segments that make one wave of CTAs; each leaves its k best keys in the workspace,
+// and the item's CTA that finishes last (an atomic counter, reset by it) selects among these.
+// Short items are one segment; where their log-sum-exp is not given they are held in shared
+// memory, and it is taken in the same launch.  Longer items have a kernel for it before, whose
+// reading leaves the logits in L2.
 #include <float.h>
 
 #include <algorithm>
@@ -30,16 +33,17 @@ namespace mtp {
 namespace {
 
 constexpr int BS_THREADS = 512, BS_WARPS = BS_THREADS / 32;
-constexpr int SEG = 14336, LEAST = 2048;  // most scores of a CTA (56 KB, three CTAs to an SM) and fewest
+constexpr int HELD = 14336, LEAST = 2048;  // most scores of an item held in shared memory; fewest of a segment
+constexpr int WHOLE = 10240;                // scores of an item that is not cut
+constexpr int SEL_PER_SM = 2;              // CTAs of a wave
 constexpr int GROUPS = 128;       // groups of four threads, each with a maximum
-constexpr int CAND_MAX = 1024;
+constexpr int CAND_MAX = 1024, HELD_KEYS = 1024;
 constexpr int BS_MAX_K = 64, BS_MAX_BEAMS = 64, BS_MAX_BATCH = 4096;
 constexpr int LSE_THREADS = 512;
 
 struct SelectArgsB {
     mtp_beam_select_args a;
     int segments, seg_len;        // segments of an item, scores of a segment
-    int lse_here;                 // the log-sum-exp is taken in this kernel (one segment)
     const float* lse;             // given, or a kernel's before this one
     unsigned long long* keys;     // [batch][segments][k]
     int* count;                   // [batch]
@@ -67,15 +71,16 @@ struct Best {
     unsigned long long group_max[GROUPS];
     unsigned long long cand[CAND_MAX];
     unsigned long long best[BS_MAX_K];
+    unsigned long long held[HELD_KEYS];  // the segments' keys, when they are joined
     unsigned long long bound, warp_best[BS_WARPS];
     int n;
 };
 
-// The k largest of key(0) .. key(n - 1) into b.best, descending; 0 past the last.
-// The whole block calls it, with the keys visible to all; b.best is visible afterwards.
-// `most`: the largest of this thread's keys, those of tid, tid + BS_THREADS, ...
-template <class KEY>
-__device__ __forceinline__ void best_of(Best& b, int n, int k, unsigned long long most, KEY key) {
+// The k largest of the block's keys into b.best, descending; 0 past the last.  each(f) calls f with
+// every key of this thread; `most`: their largest (0: none).  The whole block calls it; b.best is
+// visible afterwards.
+template <class EACH>
+__device__ __forceinline__ void best_of(Best& b, int k, unsigned long long most, EACH each) {
     const int tid = threadIdx.x;
     b.thread_max[tid] = most;
     if (tid == 0) {
@@ -100,19 +105,19 @@ __device__ __forceinline__ void best_of(Best& b, int n, int k, unsigned long lon
     __syncthreads();
     const unsigned long long bound = b.bound;
     if (most >= bound)
-        for (int i = tid; i < n; i += BS_THREADS) {
-            const unsigned long long x = key(i);
+        each([&](unsigned long long x) {
             if (x >= bound) {
                 const int at = atomicAdd(&b.n, 1);
                 if (at < CAND_MAX) b.cand[at] = x;
             }
-        }
+        });
     __syncthreads();
     const int found = b.n;
     if (found <= CAND_MAX) {
         for (int i = tid; i < found; i += BS_THREADS) {
             const unsigned long long x = b.cand[i];
             int larger = 0;
+#pragma unroll 4
             for (int j = 0; j < found; ++j) larger += b.cand[j] > x;
             if (larger < k) b.best[larger] = x;
         }
@@ -122,10 +127,10 @@ __device__ __forceinline__ void best_of(Best& b, int n, int k, unsigned long lon
     unsigned long long last = ~0ull;
     for (int r = 0; r < k && last; ++r) {
         unsigned long long x = 0;
-        for (int i = tid; i < n; i += BS_THREADS) {
-            const unsigned long long y = key(i);
+        each([&](unsigned long long y) {
             if (y < last) x = max(x, y);
-        }
+        });
+        __syncwarp();
         x = warp_max64(x);
         if ((tid & 31) == 0) b.warp_best[tid >> 5] = x;
         __syncthreads();
@@ -173,10 +178,7 @@ __device__ __forceinline__ int for_row(const void* base, int64_t first, int n, i
     const int lane = threadIdx.x & 31;
     const int head = min(n, (int)(((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / sizeof(E)));
     const int vecs = (n - head) / T::PER, rest = head + vecs * T::PER + lane;
-    if (warp == 0) {
-        if (lane < head) use(lane, T::one(p, lane));
-        if (rest < n) use(rest, T::one(p, rest));
-    }
+    if (warp == 0 && lane < head) use(lane, T::one(p, lane));
     const uint4* v = reinterpret_cast<const uint4*>(p + head);
     for (int i0 = warp * (32 * UNROLL) + lane; i0 - lane < vecs; i0 += warps * (32 * UNROLL)) {
         uint4 raw[UNROLL];
@@ -194,6 +196,7 @@ __device__ __forceinline__ int for_row(const void* base, int64_t first, int n, i
             }
         }
     }
+    if (warp == 0 && rest < n) use(rest, T::one(p, rest));
     return max(1, (vecs + 32 * UNROLL - 1) / (32 * UNROLL));
 }
 
@@ -238,41 +241,41 @@ __global__ void __launch_bounds__(LSE_THREADS) row_lse_kernel(const void* logits
     }
 }
 
-template <class T>
-__global__ void __launch_bounds__(BS_THREADS) beam_select_kernel(const SelectArgsB p) {
-    extern __shared__ float bs_score[];  // [seg_len]; the item's keys when they are joined
+template <class T, bool HOLD>
+__global__ void __launch_bounds__(BS_THREADS) beam_select_kernel(const __grid_constant__ SelectArgsB p) {
+    extern __shared__ float bs_score[];  // HOLD: the item's scores
     __shared__ Best b;
     __shared__ float s_lse[BS_MAX_BEAMS], s_beam[BS_MAX_BEAMS];
     __shared__ int s_done[BS_MAX_BEAMS], s_last;
     const mtp_beam_select_args& a = p.a;
-    const int item = blockIdx.y, seg = blockIdx.x, W = a.beams, V = a.vocab, tid = threadIdx.x;
+    const int item = blockIdx.y, seg = blockIdx.x, W = a.beams, V = a.vocab, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int first = seg * p.seg_len, n = min(p.seg_len, W * V - first);
     pdl_wait();
     if (tid < W) {
         s_beam[tid] = a.scores[item * W + tid];
         s_done[tid] = a.done ? a.done[item * W + tid] : 0;
-        if (!p.lse_here) s_lse[tid] = p.lse[item * W + tid];
+        if (!HOLD) s_lse[tid] = p.lse[item * W + tid];
     }
     __syncthreads();
-    // the segment's logits, beam by beam, as scores (as they are where their log-sum-exp is still to come); the
-    // beams' stretches go round the warps, so that short rows are on their way together
-    const int beam0 = first / V, beam1 = (first + n - 1) / V, warp = tid >> 5, lane = tid & 31;
-    int turn = warp;
-    for (int w = beam0; w <= beam1; ++w) {
-        const int c0 = max(0, first - w * V), c1 = min(V, first + n - w * V);
-        float* to = bs_score + (w * V + c0 - first);
-        const float cum = s_beam[w], lse = p.lse_here ? 0.f : s_lse[w];
-        if (s_done[w] && !p.lse_here) {
-            for (int i = tid; i < c1 - c0; i += BS_THREADS) to[i] = c0 + i == a.eos_id ? ranked(cum) : -INFINITY;
-        } else {
-            const bool raw = p.lse_here;
-            const int used = for_row<T, 4>(a.logits, ((int64_t)item * W + w) * a.logits_stride + c0, c1 - c0, turn, BS_WARPS,
-                                           [&](int i, float x) { to[i] = raw ? x : ranked(cum + (x - lse)); });
-            turn = (turn + BS_WARPS - used % BS_WARPS) % BS_WARPS;
+    // use(beam, column, logit) for this thread's logits of the segment; the beams' stretches go round the warps, so
+    // that short rows are on their way together.  A finished beam has its end alone.
+    auto logits = [&](auto use) {
+        const int beam0 = first / V, beam1 = (first + n - 1) / V;
+        int turn = warp;
+        for (int w = beam0; w <= beam1; ++w) {
+            const int c0 = max(0, first - w * V), c1 = min(V, first + n - w * V);
+            if (s_done[w] && !HOLD) {
+                for (int c = c0 + tid; c < c1; c += BS_THREADS) use(w, c, c == a.eos_id ? 0.f : -INFINITY);
+            } else {
+                const int used = for_row<T, 4>(a.logits, ((int64_t)item * W + w) * a.logits_stride + c0, c1 - c0, turn, BS_WARPS,
+                                               [&](int i, float x) { use(w, c0 + i, x); });
+                turn = (turn + BS_WARPS - used % BS_WARPS) % BS_WARPS;
+            }
         }
-    }
-    __syncthreads();
-    if (p.lse_here) {  // a warp per beam
+    };
+    if constexpr (HOLD) {  // a warp per beam: its log-sum-exp, then its scores
+        logits([&](int w, int c, float x) { bs_score[w * V + c] = x; });
+        __syncthreads();
         for (int w = warp; w < W; w += BS_WARPS) {
             float* x = bs_score + w * V;
             float m = -INFINITY, s = 0.f;
@@ -294,15 +297,34 @@ __global__ void __launch_bounds__(BS_THREADS) beam_select_kernel(const SelectArg
     if (seg == 0 && a.out_lse && tid < W) a.out_lse[item * W + tid] = s_lse[tid];
     // this thread's largest score, the first of equal ones
     float most = -INFINITY;
-    int at_most = tid;
-#pragma unroll 8
-    for (int i = tid; i < n; i += BS_THREADS)
-        if (bs_score[i] > most) {
-            most = bs_score[i];
-            at_most = i;
+    uint32_t at_most = 0xffffffffu;
+    auto larger = [&](uint32_t number, float x) {
+        if (x > most || (x == most && number < at_most)) {
+            most = x;
+            at_most = number;
         }
-    best_of(b, n, a.k, tid < n ? make_key(most, (uint32_t)(first + at_most)) : 0ull,
-            [&](int i) { return make_key(bs_score[i], (uint32_t)(first + i)); });
+    };
+    auto each = [&](auto f) {  // f(number, score)
+        if constexpr (HOLD) {
+#pragma unroll 8
+            for (int i = tid; i < n; i += BS_THREADS) f((uint32_t)i, bs_score[i]);
+        } else {
+            int beam = -1;  // (a finished beam's end comes as 0, its score is the beam's own)
+            float cum = 0.f, lse = 0.f;
+            logits([&](int w, int c, float x) {
+                if (w != beam) {
+                    beam = w;
+                    cum = s_beam[w];
+                    lse = s_done[w] ? 0.f : s_lse[w];
+                }
+                f((uint32_t)(w * V + c), ranked(cum + (x - lse)));
+            });
+        }
+    };
+    each(larger);
+    __syncwarp();
+    best_of(b, a.k, at_most != 0xffffffffu ? make_key(most, at_most) : 0ull,
+            [&](auto f) { each([&](uint32_t number, float x) { f(make_key(x, number)); }); });
 
     if (p.segments > 1) {
         unsigned long long* keys = p.keys + (size_t)item * p.segments * a.k;
@@ -315,8 +337,8 @@ __global__ void __launch_bounds__(BS_THREADS) beam_select_kernel(const SelectArg
         __threadfence();
         if (tid == 0) p.count[item] = 0;
         // the k best of all segments' keys, as many at a time as shared memory holds beside the best so far
-        unsigned long long* held = reinterpret_cast<unsigned long long*>(bs_score);
-        const int room = p.seg_len / 2, total = p.segments * a.k;
+        unsigned long long* held = b.held;
+        const int room = HELD_KEYS, total = p.segments * a.k;
         int have = 0;
         for (int at = 0; at < total;) {
             const int take = min(room - have, total - at);
@@ -324,7 +346,9 @@ __global__ void __launch_bounds__(BS_THREADS) beam_select_kernel(const SelectArg
             __syncthreads();
             unsigned long long most = 0;
             for (int i = tid; i < have + take; i += BS_THREADS) most = max(most, held[i]);
-            best_of(b, have + take, a.k, most, [&](int i) { return held[i]; });
+            best_of(b, a.k, most, [&](auto f) {
+                for (int i = tid; i < have + take; i += BS_THREADS) f(held[i]);
+            });
             at += take;
             have = a.k;
             if (at < total) {
@@ -367,14 +391,13 @@ int select_plan(const mtp_beam_select_args* a, SelectPlan* p) {
         cudaGetLastError();
         sms = 152;  // (the sizes are checked all the same; a launch will say what is wrong)
     }
-    // as many segments as fill one wave of three CTAs per SM, none shorter than LEAST (an item of up to SEG scores
-    // and no log-sum-exp stays one: nothing to join) and none longer than shared memory holds
-    const int most = (all + LEAST - 1) / LEAST, least = (all + SEG - 1) / SEG;
-    p->segments = least == 1 && (!a->lse || all <= 4 * LEAST) ? 1 : std::max(least, std::min(most, std::max(1, 3 * sms / a->batch)));
+    // as many segments as make one wave, none shorter than LEAST; short items are one (joining segments takes about
+    // 5 us, a CTA reads 10240 scores in 2)
+    p->lse_here = !a->lse && all <= HELD;
+    p->segments = p->lse_here || all <= WHOLE ? 1 : std::max(1, std::min((all + LEAST - 1) / LEAST, SEL_PER_SM * sms / a->batch));
     p->seg_len = ((all + p->segments - 1) / p->segments + 7) & ~7;  // even segments
     p->segments = (all + p->seg_len - 1) / p->seg_len;
-    p->lse_here = !a->lse && p->segments == 1;
-    p->lse_before = !a->lse && p->segments > 1;
+    p->lse_before = !a->lse && !p->lse_here;
     // the counters' place is the same for all calls, and they are left zero
     p->count_bytes = p->segments > 1 || p->lse_before ? BS_MAX_BATCH * sizeof(int) : 0;
     p->key_bytes = p->segments > 1 ? align256((size_t)a->batch * p->segments * a->k * 8) : 0;
@@ -385,7 +408,7 @@ int select_plan(const mtp_beam_select_args* a, SelectPlan* p) {
 
 template <class T>
 cudaError_t launch_select(const mtp_beam_select_args* a, const SelectPlan& pl, char* ws, cudaStream_t s) {
-    SelectArgsB p{*a, pl.segments, pl.seg_len, pl.lse_here, a->lse, reinterpret_cast<unsigned long long*>(ws + pl.count_bytes),
+    SelectArgsB p{*a, pl.segments, pl.seg_len, a->lse, reinterpret_cast<unsigned long long*>(ws + pl.count_bytes),
                   reinterpret_cast<int*>(ws)};
     if (pl.lse_before) {
         float* lse = a->out_lse ? a->out_lse : reinterpret_cast<float*>(ws + pl.count_bytes + pl.key_bytes);
@@ -395,9 +418,9 @@ cudaError_t launch_select(const mtp_beam_select_args* a, const SelectPlan& pl, c
         const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }
-    const size_t smem = (size_t)pl.seg_len * sizeof(float);
-    const void* kern = reinterpret_cast<const void*>(beam_select_kernel<T>);
-    cudaError_t e = ensure_kernel_smem(kern, smem);
+    const size_t smem = pl.lse_here ? (size_t)pl.seg_len * sizeof(float) : 0;
+    const auto kern = pl.lse_here ? beam_select_kernel<T, true> : beam_select_kernel<T, false>;
+    const cudaError_t e = pl.lse_here ? ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem) : cudaSuccess;
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(pl.segments, a->batch);
@@ -409,7 +432,7 @@ cudaError_t launch_select(const mtp_beam_select_args* a, const SelectPlan& pl, c
     attr[0].val.programmaticStreamSerializationAllowed = pl.lse_before ? 1 : 0;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, beam_select_kernel<T>, p);
+    return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
 }  // namespace
