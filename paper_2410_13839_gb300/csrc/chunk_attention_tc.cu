@@ -425,10 +425,15 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
                 if (pos0 < hi) inner_to = pos0 < key_first ? 0 : min(inner_to, (pos0 + 1 - key_first) / CT_STEP);
                 if (a.window > 0 && pos1 >= a.window + key_first) inner_from = max(inner_from, (pos1 - a.window - key_first) / CT_STEP + 1);
                 float ref = -INFINITY, sum = 0.f;
-                ChunkWalk next = w;
-                next.next(a);
-                const CtTile y(next, g);
-                const bool more = next.left > 0, q_next = bring_q && more && y.from < y.to;  // an item after this one; whose Q is to be brought
+                bool asked = false;  // Q of the item after this one is on its way
+                auto ask_q = [&]() {
+                    ChunkWalk next = w;
+                    next.next(a);
+                    if (next.left <= 0) return;
+                    const CtTile y(next, g);
+                    asked = y.from < y.to;
+                    if (asked) load_q(next, y);
+                };
                 bool there = false;  // the step's scores are known to be there
                 float s0[32], s1[32];
 #pragma unroll 1
@@ -443,7 +448,7 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
                     tmem_ld_issue<32>(tsh + 32, s1);
                     if (half) ++seen[1]; else ++seen[0];
                     const uint32_t next_phase = half ? seen[0] : seen[1];
-                    if (!onward && q_next) load_q(next, y);  // the tile's last S is there: Q's space is free
+                    if (!onward && bring_q) ask_q();  // the tile's last S is there: Q's space is free
                     __syncwarp();
                     tmem_ld_wait();
                     tmem_ld_done(s0);
@@ -545,9 +550,9 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
                     if (lane == 0) mbar_arrive(&p_full[g][half]);
                 }
                 if (!ok) break;
-                if (q_next) {
-                    if (x.from >= x.to) load_q(next, y);  // (nothing here: Q's space was free already)
-                    q_there();
+                if (bring_q) {
+                    if (x.from >= x.to) ask_q();  // (nothing here: Q's space was free already)
+                    if (asked) q_there();
                 }
                 // ---- the item's rows ----
                 const bool any = x.from < x.to;
@@ -621,10 +626,10 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
                 if (live && whole && a.lse) a.lse[row * heads + head] = sum == 0.f ? -INFINITY : LN2 * (ref + log2f(sum));
                 if (live && !whole) *reinterpret_cast<float2*>(part + (CT_TILE * TILES) * HD + 2 * (g * CT_TILE + r)) = make_float2(ref, sum);
                 tc_fence_before();  // O is read before the next item's product overwrites it
-                if (!more) break;
                 n += len;
-                w = next;
-                x = y;
+                w.next(a);
+                if (w.left <= 0) break;
+                x = CtTile(w, g);
             }
         }
     }
