@@ -424,7 +424,8 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
                 int inner_to = (hi - key_first) / CT_STEP, inner_from = (lo - key_first + CT_STEP - 1) / CT_STEP;
                 if (pos0 < hi) inner_to = pos0 < key_first ? 0 : min(inner_to, (pos0 + 1 - key_first) / CT_STEP);
                 if (a.window > 0 && pos1 >= a.window + key_first) inner_from = max(inner_from, (pos1 - a.window - key_first) / CT_STEP + 1);
-                float ref = -INFINITY, sum = 0.f;
+                const bool own = r < x.rows;  // (what stands in Q's other rows, NaN perhaps, is no reason to look for a reference)
+                float ref = own ? -INFINITY : 0.f, sum = 0.f;
                 bool asked = false;  // Q of the item after this one is on its way
                 auto ask_q = [&]() {
                     ChunkWalk next = w;
@@ -488,7 +489,7 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
                     bool fits = __all_sync(FULL_MASK, ref != -INFINITY);  // every row has a reference
                     if (fits) {
                         part = weights();
-                        fits = __all_sync(FULL_MASK, part <= LIMIT);
+                        fits = __all_sync(FULL_MASK, part <= LIMIT || !own);
                     }
                     if (!fits) {
                         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};

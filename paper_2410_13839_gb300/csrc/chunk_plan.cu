@@ -80,89 +80,102 @@ struct Map {
     const uint32_t* unit_first;  // [tiles + 1]: first unit of every tile, counted for one key head
     int tiles, ctas, snap;
 };
+// A border between shares: a place in the cost, the item that begins or goes on there, the unit of the item that
+// it stands before, the units before it.
 template <class U>
-struct Place {
-    int tile, head, units, k;  // k: the unit of the item that this place stands before
-    U first, cost;             // the item's place and cost
-    U unit;                    // units before this place
+struct Border {
+    U at, unit, item_end;  // item_end: where the item ends in the cost
+    int tile, head, k;
 };
-template <class U>
-__device__ __forceinline__ Place<U> place_of(const ChunkArgs& a, const Map& m, U at) {
-    Place<U> x;
-    const uint32_t c = a.item_cost;
-    x.tile = owner(m.unit_first, m.tiles, (uint32_t)(at / (U)a.kv_heads), c);
-    const uint32_t unit0 = m.unit_first[x.tile];
-    const U first = ((U)unit0 + (U)x.tile * c) * (U)a.kv_heads;
-    x.units = (int)(m.unit_first[x.tile + 1] - unit0);
-    x.cost = (U)x.units + c;
-    x.head = (int)((uint32_t)(at - first) / (uint32_t)x.cost);  // (an item's cost and heads: below 2^32 together)
-    x.first = first + (U)x.head * x.cost;
-    x.k = (int)(at - x.first) - (int)c;
-    if (x.k < 0) x.k = 0;
-    x.unit = (U)unit0 * (U)a.kv_heads + (U)x.head * (U)x.units + (U)x.k;
-    return x;
-}
 
 // Shares and merges, in 32 bits where the cost times the CTAs fits (64-bit divisions were most of
 // the plan's time).  CTA c's share begins at c / ctas of the cost; items of at most m.snap units
 // are not cut: the border goes to their nearer end.
 template <class U>
-__device__ __forceinline__ void share_out(const ChunkArgs& a, const Map& m, U cost, U units, U* borders) {
-    for (int c = threadIdx.x; c <= a.ctas; c += PL_THREADS) {
-        U u = c >= m.ctas ? cost : cost * (U)c / (U)m.ctas;
-        if (u < cost) {
-            const Place<U> x = place_of<U>(a, m, u);
-            if (x.units <= m.snap)
-                u = u - x.first <= x.cost / 2 ? x.first : x.first + x.cost;
-            else if (x.k == 0)
-                u = x.first;
+__device__ __forceinline__ Border<U> border(const ChunkArgs& a, const Map& m, U cost, U units, int c) {
+    Border<U> x;
+    x.at = x.item_end = cost;
+    x.unit = units;
+    x.tile = m.tiles;
+    x.head = x.k = 0;
+    if (c >= m.ctas) return x;
+    const U u = cost * (U)c / (U)m.ctas;
+    if (u >= cost) return x;
+    const uint32_t extra = a.item_cost;
+    x.tile = owner(m.unit_first, m.tiles, (uint32_t)(u / (U)a.kv_heads), extra);
+    const uint32_t unit0 = m.unit_first[x.tile], n = m.unit_first[x.tile + 1] - unit0;
+    const U first = ((U)unit0 + (U)x.tile * extra) * (U)a.kv_heads, item = (U)n + extra;
+    x.head = (int)((uint32_t)(u - first) / (uint32_t)item);  // (an item's cost and heads: below 2^32 together)
+    x.at = first + (U)x.head * item;
+    x.unit = (U)unit0 * (U)a.kv_heads + (U)x.head * (U)n;
+    x.item_end = x.at + item;
+    const uint32_t in = (uint32_t)(u - x.at);
+    if (n <= (uint32_t)m.snap) {
+        if (in > (n + extra) / 2) {  // the next item's start
+            x.at += item;
+            x.unit += n;
+            if (++x.head == a.kv_heads) {
+                x.head = 0;
+                ++x.tile;
+            }
+            const uint32_t next = x.tile < m.tiles ? m.unit_first[x.tile + 1] - m.unit_first[x.tile] : 0;
+            x.item_end = x.at + (U)next + extra;
         }
-        borders[c] = u;
+    } else if (in > extra) {
+        x.k = (int)(in - extra);
+        x.unit += (U)x.k;
+        x.at = u;
     }
+    return x;
+}
+
+template <class U>
+__device__ __forceinline__ void share_out(const ChunkArgs& a, const Map& m, U cost, U units, const ChunkTile* tiles,
+                                          Border<U>* borders) {
+    for (int c = threadIdx.x; c <= a.ctas; c += PL_THREADS) borders[c] = border<U>(a, m, cost, units, c);
     __syncthreads();
     for (int c = threadIdx.x; c < a.ctas; c += PL_THREADS) {
-        const U u0 = borders[c], u1 = borders[c + 1];
+        const Border<U> x = borders[c], y = borders[c + 1];
         int4 start = make_int4(0, 0, 0, 0);
-        int4* to = reinterpret_cast<int4*>(a.start + c);
         int more = 0;
-        if (u0 < u1) {
-            const Place<U> x = place_of<U>(a, m, u0);
-            U end = units;
-            if (u1 < cost) {
-                const Place<U> y = place_of<U>(a, m, u1);
-                end = y.unit;
-                if (y.k > 0 && y.first >= u0) {  // begins here and goes on, up to the CTA with its last unit
-                    more = 1;
-                    while (borders[c + 1 + more] < y.first + y.cost) ++more;
-                    const ChunkTile& t = a.tiles[y.tile];
-                    int* d = a.desc + c * CH_DESC;
-                    d[1] = t.p0;
-                    d[2] = t.rows;
-                    d[3] = t.row0;
-                    d[4] = y.head;
-                }
-            }
-            start = make_int4(x.tile, x.head, x.k, (int)(end - x.unit));
-            const int4* from = reinterpret_cast<const int4*>(a.tiles + x.tile);
+        int4* to = reinterpret_cast<int4*>(a.start + c);
+        if (x.at < y.at) {
+            start = make_int4(x.tile, x.head, x.k, (int)(y.unit - x.unit));
+            const int4* from = reinterpret_cast<const int4*>(tiles + x.tile);
             to[1] = from[0];
             to[2] = from[1];
             to[3] = from[2];
+            // the item that this share ends in, where it begins in the share and goes on, up to the CTA with its last unit
+            if (y.k > 0 && (x.tile != y.tile || x.head != y.head || x.k == 0)) {
+                more = 1;
+                while (borders[c + 1 + more].at < y.item_end) ++more;
+                const ChunkTile& t = tiles[y.tile];
+                int* d = a.desc + c * CH_DESC;
+                d[1] = t.p0;
+                d[2] = t.rows;
+                d[3] = t.row0;
+                d[4] = y.head;
+            }
         }
         to[0] = start;
         a.desc[c * CH_DESC] = more;
     }
 }
 
-// Shared memory: borders (8 bytes each), slots, first tile of every slot, first unit of every tile.
+// Shared memory: borders, the tiles where they are few, slots, first tile of every slot, first unit of every tile.
+constexpr int PL_KEPT = 512;
+__host__ __device__ inline size_t border_bytes(int ctas) { return ((size_t)(ctas + 1) * sizeof(Border<unsigned long long>) + 15) & ~(size_t)15; }
 size_t plan_smem(const ChunkArgs& a) {
-    return (size_t)(a.ctas + 1) * 8 + (size_t)a.slots * sizeof(Slot) + (size_t)(a.slots + a.max_tiles + 2) * 4;
+    return border_bytes(a.ctas) + (a.max_tiles <= PL_KEPT ? a.max_tiles * sizeof(ChunkTile) : 0) + (size_t)a.slots * sizeof(Slot) + (size_t)(a.slots + a.max_tiles + 2) * 4;
 }
 
 template <int TR, int KT>
 __global__ void __launch_bounds__(PL_THREADS) chunk_plan_kernel(const __grid_constant__ ChunkArgs a) {
-    extern __shared__ __align__(8) unsigned char pl_sm[];
+    extern __shared__ __align__(16) unsigned char pl_sm[];
     __shared__ uint32_t part[PL_WARPS];
-    Slot* slots = reinterpret_cast<Slot*>(pl_sm + (size_t)(a.ctas + 1) * 8);
+    const bool keep = a.max_tiles <= PL_KEPT;
+    ChunkTile* kept = reinterpret_cast<ChunkTile*>(pl_sm + border_bytes(a.ctas));
+    Slot* slots = reinterpret_cast<Slot*>(kept + (keep ? a.max_tiles : 0));
     uint32_t* slot_first = reinterpret_cast<uint32_t*>(slots + a.slots);  // [slots + 1]
     uint32_t* unit_first = slot_first + a.slots + 1;                      // [tiles + 1]
     const int tid = threadIdx.x;
@@ -197,6 +210,7 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan_kernel(const __grid_con
             to[0] = from[0];
             to[1] = from[1];
             to[2] = from[2];
+            if (keep) kept[j] = t;
             x = t.units;
         }
         x = scan(x, part, sum);
@@ -212,10 +226,11 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan_kernel(const __grid_con
                       max(1ull, narrow ? (unsigned long long)(((uint32_t)units + a.min_units - 1) / a.min_units)
                                        : (units + a.min_units - 1) / a.min_units));
     m.snap = !a.snap ? 0 : narrow ? (int)((uint32_t)units / m.ctas / a.snap) : (int)min(units / m.ctas / a.snap, 1ull << 30);
+    const ChunkTile* tiles = keep ? kept : a.tiles;
     if (narrow)
-        share_out<uint32_t>(a, m, (uint32_t)cost, (uint32_t)units, reinterpret_cast<uint32_t*>(pl_sm));
+        share_out<uint32_t>(a, m, (uint32_t)cost, (uint32_t)units, tiles, reinterpret_cast<Border<uint32_t>*>(pl_sm));
     else
-        share_out<unsigned long long>(a, m, cost, units, reinterpret_cast<unsigned long long*>(pl_sm));
+        share_out<unsigned long long>(a, m, cost, units, tiles, reinterpret_cast<Border<unsigned long long>*>(pl_sm));
 }
 
 template <int TR, int KT>

@@ -255,3 +255,84 @@ def test_workspace_and_empty_calls():
         _refused(lambda m: m.mtp_chunk_attention(_chunk(), ws, n))
     mtp.mtp_chunk_attention(_chunk(rows=0), None, 0)
     mtp.mtp_chunk_attention(_chunk(max_new=0), None, 0)
+
+
+@pytest.mark.parametrize("new,lens", [([1, 3], [700, 900]), ([150, 40], [300, 2000])])
+def test_captured_in_a_graph(new, lens):
+    """A plan, an append and the attention of a step as one graph: replays follow the buffers' contents."""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    heads, kv_heads, dim, page, slots = 4, 2, 64, 16, len(new)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    stride, rows = -(-max(lens) // page), sum(new)
+    n_pages = slots * stride + 5
+    i32 = dict(dtype=torch.int32, device="cuda")
+    pool = torch.randn(n_pages, 1, 2, kv_heads, page, dim, device="cuda", generator=gen).bfloat16()
+    before = [n - a for n, a in zip(lens, new)]
+    pages = torch.randperm(n_pages).tolist()
+    table = [[pages.pop() for _ in range(-(-n // page))] for n in before]
+    refs = torch.zeros(n_pages, **i32)
+    refs[[p for t in table for p in t]] = 1
+    d_table = torch.tensor([t + [-1] * (stride - len(t)) for t in table], **i32)
+    d_new, d_before = torch.tensor(new, **i32), torch.tensor(before, **i32)
+    cu, d_lens, out_refs, status = torch.zeros(slots + 1, **i32), torch.zeros(slots, **i32), torch.zeros(n_pages, **i32), torch.zeros(4, **i32)
+    seq, pos, places = torch.zeros(rows, **i32), torch.zeros(rows, **i32), torch.zeros(rows, dtype=torch.int64, device="cuda")
+    x = torch.randn(rows, heads + 2 * kv_heads, dim, device="cuda", generator=gen).bfloat16()
+    q, k, v = x[:, :heads], x[:, heads:heads + kv_heads], x[:, heads + kv_heads:]
+    out, lse = torch.zeros(rows, heads, dim, dtype=torch.bfloat16, device="cuda"), torch.zeros(rows, heads, device="cuda")
+    plan = mtp.page_plan_args(kv_lens=d_before, new_lens=d_new, block_table=d_table, page_refs=refs, out_kv_lens=d_lens,
+                              out_page_refs=out_refs, out_cu_rows=cu, out_slot_map=places, out_row_seq=seq, out_row_pos=pos,
+                              out_status=status, page_size=page)
+    append = mtp.cache_append_args(k=k, v=v, slot_map=places, kv_pool=pool, layer=0)
+    attend = mtp.chunk_attention_args(q=q, kv_pool=pool, layer=0, block_table=d_table, cu_rows=cu, kv_lens=d_lens, out=out,
+                                      out_lse=lse, scale=0.125, max_new=max(new), max_keys=max(lens))
+    n = mtp.mtp_chunk_attention_workspace_bytes(attend)
+    ws = torch.zeros(n, dtype=torch.uint8, device="cuda")
+
+    def step():
+        stream = torch.cuda.current_stream()
+        mtp.mtp_page_plan(plan, stream)
+        mtp.mtp_cache_append(append, stream)
+        mtp.mtp_chunk_attention(attend, ws, n, stream)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        x.normal_(generator=gen)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert status[0] == 0 and d_lens.tolist() == lens
+        ref, want, size, total = reference(torch, q, pool, 0, d_table.tolist(), new, lens, 0.125, 0)
+        assert bool(((out.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2.0 ** -14) * size).all())
+        assert bool(((lse.double() - want).abs() <= 4e-5 + 2.0 ** -22 * want.abs()).all())
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(4, 2, 64), (5, 1, 128), (8, 2, 128)])
+def test_query_rows_past_the_last_may_be_anything(heads, kv_heads, dim):
+    """Rows of the buffer that belong to no slot, NaN here, share tiles with the last slot's: they leave no trace."""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    page, n, length, rows = 16, 70, 200, 90
+    i32 = dict(dtype=torch.int32, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    pool = torch.randn(20, 1, 2, kv_heads, page, dim, device="cuda", generator=gen).bfloat16()
+    q = torch.randn(rows, heads, dim, device="cuda", generator=gen).bfloat16()
+    q[n:] = NAN
+    out, lse = torch.full_like(q, -7.0), torch.full((rows, heads), -7.0, device="cuda")
+    args = mtp.chunk_attention_args(q=q, kv_pool=pool, layer=0, block_table=torch.arange(13, **i32)[None].contiguous(),
+                                    cu_rows=torch.tensor([0, n], **i32), kv_lens=torch.tensor([length], **i32), out=out,
+                                    out_lse=lse, scale=dim ** -0.5, max_new=n, max_keys=length)
+    nbytes = mtp.mtp_chunk_attention_workspace_bytes(args)
+    mtp.mtp_chunk_attention(args, torch.zeros(nbytes, dtype=torch.uint8, device="cuda"), nbytes, torch.cuda.current_stream())
+    ref, want, size, _ = reference(torch, q[:n], pool, 0, [list(range(13))], [n], [length], dim ** -0.5, 0)
+    assert bool(((out[:n].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2.0 ** -14) * size).all())
+    assert bool(((lse[:n].double() - want).abs() <= 4e-5 + 2.0 ** -22 * want.abs()).all())
+    assert bool((out[n:] == -7).all()) and bool((lse[n:] == -7).all())
+
+
+def test_tokens_of_one_slot_in_every_size():
+    """One to 300 tokens behind a short context: every filling of a tile, both kernels, both tiles of a CTA."""
+    for n in list(range(1, 40)) + list(range(60, 70)) + list(range(120, 136)) + list(range(250, 262)) + [300]:
+        check([n], [n + 5], 2, 1, 128 if n % 2 else 64, 16, seed=n)
