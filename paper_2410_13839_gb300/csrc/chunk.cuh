@@ -55,6 +55,7 @@ struct ChunkArgs {
     int item_cost;                 // an item's start and end, in units
     int snap;                      // items of at most 1 / snap of a share are not cut (0: all are)
     bool q_vec, out_vec;           // rows 16-byte aligned
+    bool residues;                 // the weights enter with their rounding residues
     bool q_tma;                    // many rows: Q's tiles are copied by a tensor map
     float scale_log2;              // scale * log2 e: scores in log2 units
     ChunkStart* start;             // [ctas]
@@ -111,7 +112,7 @@ struct ChunkWalk {
     __device__ __forceinline__ bool ends() const { return k1 == t.units; }
 };
 
-cudaError_t launch_chunk_plan(const ChunkArgs& a, int tile_rows, cudaStream_t s);  // 16, 32; 128, 256: many rows
+cudaError_t launch_chunk_plan(const ChunkArgs& a, int tile_rows, cudaStream_t s);  // 16; 128, 256: many rows
 cudaError_t launch_chunk_tc(const ChunkArgs& a, const CUtensorMap& map, const CUtensorMap& q_map, int head_dim, int dtype,
                             cudaStream_t s);
 

@@ -35,7 +35,8 @@ namespace {
 constexpr int FR_KEYS = 64, FR_WARPS = 5, FR_THREADS = FR_WARPS * 32, FR_CONSUMERS = 128;
 constexpr int FR_MIN_UNITS = 4, CT_MIN_UNITS = 2, CT_SNAP = 3;  // fewest units of a CTA
 constexpr int FR_ITEM_COST = 2, CT_ITEM_COST = 2;
-constexpr int FR_MAX_ROWS = 32, CT_UNIT_KEYS = 128;
+constexpr int FR_ROWS = 16, CT_UNIT_KEYS = 128;  // a tile of few rows
+constexpr int RESIDUE_ROWS = 32;  // rows of a slot and key head up to which the weights' residues are kept
 constexpr float LN2 = 0.69314718055994531f;
 
 __device__ __forceinline__ float ex2(float x) {
@@ -80,19 +81,19 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t&
 // Shared memory of the few-rows kernel, from a 1024-byte boundary: ring stages (K then V, each
 // HD / 64 tiles of 64 rows of 128 bytes), Q (HD / 64 tiles of TR rows), a join buffer of TR x HD
 // floats, per-warp maxima and sums.
-template <int HD, int MT>
+template <int HD>
 struct FrLayout {
-    static constexpr int TR = 16 * MT;
-    static constexpr int STAGES = HD == 64 ? 4 : MT == 1 ? 3 : 2;
+    static constexpr int TR = FR_ROWS;
+    static constexpr int STAGES = HD == 64 ? 4 : 3;
     static constexpr uint32_t TILE = FR_KEYS * 128, KV = TILE * (HD / 64), STAGE = 2 * KV;
     static constexpr uint32_t Q = STAGES * STAGE, JOIN = Q + TR * HD * 2, ML = JOIN + TR * HD * 4;
     static constexpr size_t BYTES = 1024 + ML + 2 * 4 * TR * 4;
 };
 
-template <class T, int HD, int MT>
-__global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
+template <class T, int HD>
+__global__ void __launch_bounds__(FR_THREADS, HD == 64 ? 3 : 2)
     chunk_rows_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ CUtensorMap map) {
-    using L = FrLayout<HD, MT>;
+    using L = FrLayout<HD>;
     constexpr int TR = L::TR, ST = L::STAGES;
     extern __shared__ unsigned char fr_raw[];
     __shared__ uint64_t full[ST], empty[ST];
@@ -193,21 +194,18 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
             *reinterpret_cast<uint4*>(sm + L::Q + (c >> 3) * (TR * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
         }
         consumer_sync();
-        float o[MT][HD / 8][4], mx[MT][2], sum[MT][2];
-        int pos[MT][2];  // the rows' positions
+        float o[HD / 8][4], mx[2], sum[2];
+        int pos[2];  // the rows' positions
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
+        for (int d = 0; d < HD / 8; ++d)
 #pragma unroll
-            for (int d = 0; d < HD / 8; ++d)
+            for (int e = 0; e < 4; ++e) o[d][e] = 0.f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[i][d][e] = 0.f;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                mx[i][e] = -INFINITY;
-                sum[i][e] = 0.f;
-                const int r = i * 16 + r0 + e * 8;
-                pos[i][e] = r < t.rows ? t.base + chunk_token(a, t.p0 + r) : -1;
-            }
+        for (int e = 0; e < 2; ++e) {
+            mx[e] = -INFINITY;
+            sum[e] = 0.f;
+            const int r = r0 + e * 8;
+            pos[e] = r < t.rows ? t.base + chunk_token(a, t.p0 + r) : -1;
         }
         const int pos_first = t.base + chunk_token(a, t.p0), pos_last = t.hi - 1;
         for (int k = w.k0; k < w.k1; ++k) {
@@ -229,63 +227,55 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
                     __syncwarp();
                 }
                 const uint32_t kr = smem_addr(kb), vr = kr + L::KV;
-                float s[MT][2][4];
+                float s[2][4];
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+                for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) s[i][j][e] = 0.f;
+                    for (int e = 0; e < 4; ++e) s[j][e] = 0.f;
 #pragma unroll
                 for (int d = 0; d < HD / 16; ++d) {
                     uint32_t kf[4];
                     const int key = warp * 16 + ((lane >> 4) << 3) + (lane & 7), c = 2 * d + ((lane >> 3) & 1);
                     frag::ldsm_x4(kf, kr + (c >> 3) * L::TILE + key * 128 + (((c & 7) ^ (key & 7)) << 4));
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        uint32_t qf[4];
-                        const int row = i * 16 + (lane & 15), cq = 2 * d + (lane >> 4);
-                        frag::ldsm_x4(qf, q_base + (cq >> 3) * (TR * 128) + row * 128 + (((cq & 7) ^ (row & 7)) << 4));
-                        mma16<T>(s[i][0], qf, kf[0], kf[1]);
-                        mma16<T>(s[i][1], qf, kf[2], kf[3]);
-                    }
+                    uint32_t qf[4];
+                    const int row = lane & 15, cq = 2 * d + (lane >> 4);
+                    frag::ldsm_x4(qf, q_base + (cq >> 3) * (TR * 128) + row * 128 + (((cq & 7) ^ (row & 7)) << 4));
+                    mma16<T>(s[0], qf, kf[0], kf[1]);
+                    mma16<T>(s[1], qf, kf[2], kf[3]);
                 }
-                uint32_t hi[MT][4], lo[MT][4];
+                uint32_t hi[4], lo[4];
+                if (!inner) {
 #pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    if (!inner) {
+                    for (int j = 0; j < 2; ++j)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j)
+                        for (int e = 0; e < 4; ++e) {
+                            const int key = key0 + j * 8 + c0 + (e & 1), p = pos[e >> 1];
+                            if (key > p || (a.window > 0 && key <= p - a.window)) s[j][e] = -INFINITY;
+                        }
+                }
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const int key = key0 + j * 8 + c0 + (e & 1), p = pos[i][e >> 1];
-                                if (key > p || (a.window > 0 && key <= p - a.window)) s[i][j][e] = -INFINITY;
-                            }
+                for (int e = 0; e < 2; ++e) {
+                    float top = fmaxf(fmaxf(s[0][2 * e], s[0][2 * e + 1]), fmaxf(s[1][2 * e], s[1][2 * e + 1]));
+                    top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, 1));
+                    top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, 2));
+                    const float now = fmaxf(mx[e], top * a.scale_log2);
+                    if (__any_sync(FULL_MASK, now > mx[e])) {
+                        const float f = mx[e] == -INFINITY ? 0.f : ex2(mx[e] - now);
+                        sum[e] *= f;
+#pragma unroll
+                        for (int d = 0; d < HD / 8; ++d) {
+                            o[d][2 * e] *= f;
+                            o[d][2 * e + 1] *= f;
+                        }
+                        mx[e] = now;
                     }
+                    const float ref = now == -INFINITY ? 0.f : now;  // a row that has seen no key: every weight 0
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float top = fmaxf(fmaxf(s[i][0][2 * e], s[i][0][2 * e + 1]), fmaxf(s[i][1][2 * e], s[i][1][2 * e + 1]));
-                        top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, 1));
-                        top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, 2));
-                        const float now = fmaxf(mx[i][e], top * a.scale_log2);
-                        if (__any_sync(FULL_MASK, now > mx[i][e])) {
-                            const float f = mx[i][e] == -INFINITY ? 0.f : ex2(mx[i][e] - now);
-                            sum[i][e] *= f;
-#pragma unroll
-                            for (int d = 0; d < HD / 8; ++d) {
-                                o[i][d][2 * e] *= f;
-                                o[i][d][2 * e + 1] *= f;
-                            }
-                            mx[i][e] = now;
-                        }
-                        const float ref = now == -INFINITY ? 0.f : now;  // a row that has seen no key: every weight 0
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const float x = ex2(fmaf(s[i][j][2 * e], a.scale_log2, -ref)),
-                                        y = ex2(fmaf(s[i][j][2 * e + 1], a.scale_log2, -ref));
-                            sum[i][e] += x + y;
-                            split2<T>(x, y, hi[i][2 * j + e], lo[i][2 * j + e]);
-                        }
+                    for (int j = 0; j < 2; ++j) {
+                        const float x = ex2(fmaf(s[j][2 * e], a.scale_log2, -ref)),
+                                    y = ex2(fmaf(s[j][2 * e + 1], a.scale_log2, -ref));
+                        sum[e] += x + y;
+                        split2<T>(x, y, hi[2 * j + e], lo[2 * j + e]);
                     }
                 }
 #pragma unroll
@@ -293,13 +283,10 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
                     uint32_t vf[4];
                     const int key = warp * 16 + (lane & 15), c = 2 * d + (lane >> 4);
                     frag::ldsm_x4_t(vf, vr + (c >> 3) * L::TILE + key * 128 + (((c & 7) ^ (key & 7)) << 4));
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        mma16<T>(o[i][2 * d], hi[i], vf[0], vf[1]);
-                        mma16<T>(o[i][2 * d + 1], hi[i], vf[2], vf[3]);
-                        mma16<T>(o[i][2 * d], lo[i], vf[0], vf[1]);
-                        mma16<T>(o[i][2 * d + 1], lo[i], vf[2], vf[3]);
-                    }
+                    mma16<T>(o[2 * d], hi, vf[0], vf[1]);
+                    mma16<T>(o[2 * d + 1], hi, vf[2], vf[3]);
+                    mma16<T>(o[2 * d], lo, vf[0], vf[1]);
+                    mma16<T>(o[2 * d + 1], lo, vf[2], vf[3]);
                 }
             }
             __syncwarp();
@@ -308,96 +295,86 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 && MT == 1 ? 3 : 2)
         }
         // ---- the four warps' maxima, sums and outputs as one ----
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                sum[i][e] += __shfl_xor_sync(FULL_MASK, sum[i][e], 1);
-                sum[i][e] += __shfl_xor_sync(FULL_MASK, sum[i][e], 2);
-                if ((lane & 3) == 0) {
-                    const int r = i * 16 + r0 + e * 8;
-                    ml[warp * TR + r] = mx[i][e];
-                    ml[(4 + warp) * TR + r] = sum[i][e];
-                }
+        for (int e = 0; e < 2; ++e) {
+            sum[e] += __shfl_xor_sync(FULL_MASK, sum[e], 1);
+            sum[e] += __shfl_xor_sync(FULL_MASK, sum[e], 2);
+            if ((lane & 3) == 0) {
+                const int r = r0 + e * 8;
+                ml[warp * TR + r] = mx[e];
+                ml[(4 + warp) * TR + r] = sum[e];
             }
+        }
         consumer_sync();
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int e = 0; e < 2; ++e) {
+            const int r = r0 + e * 8;
+            float top = -INFINITY, all = 0.f;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int r = i * 16 + r0 + e * 8;
-                float top = -INFINITY, all = 0.f;
+            for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * TR + r]);
+            const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * TR + r]);
-                const float ref = top == -INFINITY ? 0.f : top;
+            for (int w = 0; w < 4; ++w) all = fmaf(ml[(4 + w) * TR + r], ex2(ml[w * TR + r] - ref), all);
+            const float f = ex2(mx[e] - ref);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) all = fmaf(ml[(4 + w) * TR + r], ex2(ml[w * TR + r] - ref), all);
-                const float f = ex2(mx[i][e] - ref);
-#pragma unroll
-                for (int d = 0; d < HD / 8; ++d) {
-                    o[i][d][2 * e] *= f;
-                    o[i][d][2 * e + 1] *= f;
-                }
-                mx[i][e] = top;
-                sum[i][e] = all;
+            for (int d = 0; d < HD / 8; ++d) {
+                o[d][2 * e] *= f;
+                o[d][2 * e + 1] *= f;
             }
+            mx[e] = top;
+            sum[e] = all;
+        }
 #pragma unroll
         for (int w = 3; w >= 0; --w) {  // warp 3 leaves its outputs, 2 and 1 add theirs, 0 takes the sum
             if (warp == w) {
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int d = 0; d < HD / 8; ++d) {
-                        float4* at = reinterpret_cast<float4*>(join) + (i * (HD / 8) + d) * 32 + lane;
-                        float4 v = make_float4(o[i][d][0], o[i][d][1], o[i][d][2], o[i][d][3]);
-                        if (w < 3) {
-                            const float4 x = *at;
-                            v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
-                        }
-                        if (w > 0) *at = v;
-                        o[i][d][0] = v.x; o[i][d][1] = v.y; o[i][d][2] = v.z; o[i][d][3] = v.w;
+                for (int d = 0; d < HD / 8; ++d) {
+                    float4* at = reinterpret_cast<float4*>(join) + d * 32 + lane;
+                    float4 v = make_float4(o[d][0], o[d][1], o[d][2], o[d][3]);
+                    if (w < 3) {
+                        const float4 x = *at;
+                        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
                     }
+                    if (w > 0) *at = v;
+                    o[d][0] = v.x; o[d][1] = v.y; o[d][2] = v.z; o[d][3] = v.w;
+                }
             }
             if (w > 0) consumer_sync();
         }
         if (warp == 0 && alive) {
             if (begins && ends) {
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+                for (int e = 0; e < 2; ++e) {
+                    const int r = r0 + e * 8, p = t.p0 + r;
+                    if (r >= t.rows) continue;
+                    const int token = chunk_token(a, p), head = w.head * a.group + p - token * a.group;
+                    const long long row = t.row0 + token;
+                    const float f = sum[e] == 0.f ? 0.f : 1.f / sum[e];  // (no key: 0)
+                    uint16_t* to = a.out + row * a.out_stride + head * HD + c0;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int r = i * 16 + r0 + e * 8, p = t.p0 + r;
-                        if (r >= t.rows) continue;
-                        const int token = chunk_token(a, p), head = w.head * a.group + p - token * a.group;
-                        const long long row = t.row0 + token;
-                        const float f = sum[i][e] == 0.f ? 0.f : 1.f / sum[i][e];  // (no key: 0)
-                        uint16_t* to = a.out + row * a.out_stride + head * HD + c0;
-#pragma unroll
-                        for (int d = 0; d < HD / 8; ++d) {
-                            const uint32_t v = T::pack(o[i][d][2 * e] * f, o[i][d][2 * e + 1] * f);
-                            if (a.out_vec) {
-                                *reinterpret_cast<uint32_t*>(to + d * 8) = v;
-                            } else {
-                                to[d * 8] = (uint16_t)v;
-                                to[d * 8 + 1] = (uint16_t)(v >> 16);
-                            }
+                    for (int d = 0; d < HD / 8; ++d) {
+                        const uint32_t v = T::pack(o[d][2 * e] * f, o[d][2 * e + 1] * f);
+                        if (a.out_vec) {
+                            *reinterpret_cast<uint32_t*>(to + d * 8) = v;
+                        } else {
+                            to[d * 8] = (uint16_t)v;
+                            to[d * 8 + 1] = (uint16_t)(v >> 16);
                         }
-                        if (a.lse && (lane & 3) == 0)
-                            a.lse[row * (a.kv_heads * a.group) + head] =
-                                sum[i][e] == 0.f ? -INFINITY : LN2 * (mx[i][e] + log2f(sum[i][e]));
                     }
+                    if (a.lse && (lane & 3) == 0)
+                        a.lse[row * (a.kv_heads * a.group) + head] =
+                            sum[e] == 0.f ? -INFINITY : LN2 * (mx[e] + log2f(sum[e]));
+                }
             } else {
                 float* part = a.part + ((size_t)cta * 2 + begins) * TR * (HD + 2);
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+                for (int e = 0; e < 2; ++e) {
+                    const int r = r0 + e * 8;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int r = i * 16 + r0 + e * 8;
-#pragma unroll
-                        for (int d = 0; d < HD / 8; ++d)
-                            *reinterpret_cast<float2*>(part + r * HD + d * 8 + c0) = make_float2(o[i][d][2 * e], o[i][d][2 * e + 1]);
-                        if ((lane & 3) == 0)
-                            *reinterpret_cast<float2*>(part + TR * HD + 2 * r) = make_float2(mx[i][e], sum[i][e]);
-                    }
+                    for (int d = 0; d < HD / 8; ++d)
+                        *reinterpret_cast<float2*>(part + r * HD + d * 8 + c0) = make_float2(o[d][2 * e], o[d][2 * e + 1]);
+                    if ((lane & 3) == 0)
+                        *reinterpret_cast<float2*>(part + TR * HD + 2 * r) = make_float2(mx[e], sum[e]);
+                }
             }
         }
     }
@@ -462,8 +439,7 @@ template <class T, int HD>
 cudaError_t merge_hd(const ChunkArgs& a, int tile_rows, cudaStream_t s) {
     const dim3 grid(a.ctas, tile_rows / 4);
     switch (tile_rows) {
-        case 16: return launch_ex(chunk_merge_kernel<T, HD, 16>, grid, 128, 0, true, s, a);
-        case 32: return launch_ex(chunk_merge_kernel<T, HD, 32>, grid, 128, 0, true, s, a);
+        case FR_ROWS: return launch_ex(chunk_merge_kernel<T, HD, FR_ROWS>, grid, 128, 0, true, s, a);
         default: return launch_ex(chunk_merge_kernel<T, HD, 128 * chunk_tc_tiles(HD)>, grid, 128, 0, true, s, a);
     }
 }
@@ -471,6 +447,7 @@ cudaError_t merge_hd(const ChunkArgs& a, int tile_rows, cudaStream_t s) {
 // How a call runs: tile rows, CTAs, workspace.
 struct ChunkPlan {
     int tile_rows, ctas, max_tiles, min_units;
+    bool residues;
     size_t start, desc, tiles, part, need;  // places in the workspace, its bytes
 };
 
@@ -496,14 +473,15 @@ int chunk_plan(const mtp_chunk_attention_args* a, ChunkPlan* p) {
     }
     const int group = a->n_heads / a->n_kv_heads;
     const long long packed = (long long)std::min(a->max_new, a->rows) * group;  // rows of a slot and key head
-    p->tile_rows = packed <= 16 ? 16 : packed <= FR_MAX_ROWS ? 32 : 128 * chunk_tc_tiles(a->head_dim);
-    const bool few = p->tile_rows <= FR_MAX_ROWS;
+    p->tile_rows = packed <= FR_ROWS ? FR_ROWS : 128 * chunk_tc_tiles(a->head_dim);
+    p->residues = packed <= RESIDUE_ROWS;
+    const bool few = p->tile_rows == FR_ROWS;
     const long long tiles = std::min((long long)a->slots * ((packed + p->tile_rows - 1) / p->tile_rows),
                                      (long long)a->rows * group / p->tile_rows + a->slots);
     if ((long long)a->rows * group >= CH_MAX_PACKED)
         return invalid("chunk_attention: %d rows of %d query heads per key head: below %d together", a->rows, group, CH_MAX_PACKED);
     p->max_tiles = (int)tiles;
-    const int per_sm = !few ? 3 - chunk_tc_tiles(a->head_dim) : a->head_dim == 64 && p->tile_rows == 16 ? 3 : 2, keys = few ? FR_KEYS : CT_UNIT_KEYS;
+    const int per_sm = !few ? 3 - chunk_tc_tiles(a->head_dim) : a->head_dim == 64 ? 3 : 2, keys = few ? FR_KEYS : CT_UNIT_KEYS;
     p->min_units = few ? FR_MIN_UNITS : CT_MIN_UNITS;
     const long long units = tiles * a->n_kv_heads * (a->max_keys / keys + 2);
     p->ctas = (int)std::max(1ll, std::min((long long)sms * per_sm, (units + p->min_units - 1) / p->min_units));
@@ -520,10 +498,10 @@ int chunk_plan(const mtp_chunk_attention_args* a, ChunkPlan* p) {
     return MTP_OK;
 }
 
-template <class T, int HD, int MT>
+template <class T, int HD>
 cudaError_t launch_rows(const ChunkArgs& a, const CUtensorMap& map, cudaStream_t s) {
-    const size_t smem = FrLayout<HD, MT>::BYTES;
-    const auto kern = chunk_rows_kernel<T, HD, MT>;
+    const size_t smem = FrLayout<HD>::BYTES;
+    const auto kern = chunk_rows_kernel<T, HD>;
     const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem, true);
     if (e != cudaSuccess) return e;
     return launch_ex(kern, dim3(a.ctas), FR_THREADS, smem, true, s, a, map);
@@ -532,12 +510,10 @@ template <class T>
 cudaError_t launch_kernels(const ChunkArgs& a, const CUtensorMap& map, const CUtensorMap& q_map, int head_dim, int dtype, int tile_rows, cudaStream_t s) {
     cudaError_t e = launch_chunk_plan(a, tile_rows, s);
     if (e != cudaSuccess) return e;
-    if (tile_rows > FR_MAX_ROWS)
+    if (tile_rows > FR_ROWS)
         e = launch_chunk_tc(a, map, q_map, head_dim, dtype, s);
-    else if (head_dim == 64)
-        e = tile_rows == 16 ? launch_rows<T, 64, 1>(a, map, s) : launch_rows<T, 64, 2>(a, map, s);
     else
-        e = tile_rows == 16 ? launch_rows<T, 128, 1>(a, map, s) : launch_rows<T, 128, 2>(a, map, s);
+        e = head_dim == 64 ? launch_rows<T, 64>(a, map, s) : launch_rows<T, 128>(a, map, s);
     if (e != cudaSuccess) return e;
     return head_dim == 64 ? merge_hd<T, 64>(a, tile_rows, s) : merge_hd<T, 128>(a, tile_rows, s);
 }
@@ -591,7 +567,8 @@ MTP_API int mtp_chunk_attention(const mtp_chunk_attention_args* a, void* workspa
         c.page_blocks = a->layers * 2 * a->n_kv_heads;
         c.layer_block = a->layer * 2 * a->n_kv_heads;
         c.window = a->window; c.max_tiles = p.max_tiles; c.min_units = p.min_units;
-        const bool few = p.tile_rows <= FR_MAX_ROWS;
+        const bool few = p.tile_rows == FR_ROWS;
+        c.residues = p.residues;
         c.snap = few ? 0 : CT_SNAP;
         c.item_cost = few ? FR_ITEM_COST : CT_ITEM_COST;
         c.q_vec = aligned16(a->q) && a->q_stride % 8 == 0;

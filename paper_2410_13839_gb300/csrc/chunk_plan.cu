@@ -246,7 +246,6 @@ cudaError_t launch(const ChunkArgs& a, cudaStream_t s) {
 cudaError_t launch_chunk_plan(const ChunkArgs& a, int tile_rows, cudaStream_t s) {
     switch (tile_rows) {
         case 16: return launch<16, 64>(a, s);
-        case 32: return launch<32, 64>(a, s);
         case 128: return launch<128, 128>(a, s);
         default: return launch<256, 128>(a, s);
     }
