@@ -33,7 +33,7 @@ int tc_encode_queries(CUtensorMap* map, const void* q, int dtype, int head_dim, 
 namespace {
 
 constexpr int FR_KEYS = 64, FR_WARPS = 5, FR_THREADS = FR_WARPS * 32, FR_CONSUMERS = 128;
-constexpr int FR_MIN_UNITS = 4, CT_MIN_UNITS = 2, CT_SNAP = 3;  // fewest units of a CTA
+constexpr int FR_MIN_UNITS = 4, CT_MIN_UNITS = 1, CT_SNAP = 12;  // fewest units of a CTA
 constexpr int FR_ITEM_COST = 2, CT_ITEM_COST = 2;
 constexpr int FR_ROWS = 16, CT_UNIT_KEYS = 128;  // a tile of few rows
 constexpr int RESIDUE_ROWS = 32;  // rows of a slot and key head up to which the weights' residues are kept

@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan_kernel(const __grid_con
     m.ctas = (int)min((unsigned long long)a.ctas,
                       max(1ull, narrow ? (unsigned long long)(((uint32_t)units + a.min_units - 1) / a.min_units)
                                        : (units + a.min_units - 1) / a.min_units));
-    m.snap = !a.snap ? 0 : narrow ? (int)((uint32_t)units / m.ctas / a.snap) : (int)min(units / m.ctas / a.snap, 1ull << 30);
+    m.snap = a.snap > 0 ? (int)min((unsigned long long)a.snap, narrow ? (uint32_t)units / m.ctas / 3 : units / m.ctas / 3) : 0;
     const ChunkTile* tiles = keep ? kept : a.tiles;
     if (narrow)
         share_out<uint32_t>(a, m, (uint32_t)cost, (uint32_t)units, tiles, reinterpret_cast<Border<uint32_t>*>(pl_sm));
