@@ -53,7 +53,8 @@ struct ChunkArgs {
     int page_blocks, layer_block;  // (layer, K | V, head) blocks of a page; the layer's first
     int window, max_tiles, min_units, ctas;
     int item_cost;                 // an item's start and end, in units
-    int snap;                      // items of at most 1 / snap of a share are not cut (0: all are)
+    int snap;                      // items of at most so many units (and a third of a share) are not cut
+    bool plan_here;                // few rows, few slots: every CTA makes its share itself
     bool q_vec, out_vec;           // rows 16-byte aligned
     bool residues;                 // the weights enter with their rounding residues
     bool q_tma;                    // many rows: Q's tiles are copied by a tensor map
@@ -82,17 +83,24 @@ __device__ __forceinline__ bool chunk_wait(uint64_t* bar, uint32_t parity, int* 
 }
 
 // A CTA's walk over the items of its share: the item, and its units [k0, k1) in the share.
-struct ChunkWalk {
-    int tile, head, k0, k1, left;  // left: units of the share from this item on
-    ChunkTile t;
-    __device__ __forceinline__ void load(const ChunkArgs& a) {
+struct PlannedTiles {  // the plan kernel's
+    __device__ __forceinline__ ChunkTile operator()(const ChunkArgs& a, int tile) const {
+        ChunkTile t;
         const int4* p = reinterpret_cast<const int4*>(a.tiles + tile);
         int4* to = reinterpret_cast<int4*>(&t);
         to[0] = p[0];
         to[1] = p[1];
         to[2] = p[2];
+        return t;
     }
-    __device__ __forceinline__ ChunkWalk(const ChunkStart& s) : tile(s.tile), head(s.head), k0(s.k), left(s.units), t(s.t) {
+};
+template <class TILES>
+struct ChunkWalkOf {
+    TILES tiles;
+    int tile, head, k0, k1, left;  // left: units of the share from this item on
+    ChunkTile t;
+    __device__ __forceinline__ ChunkWalkOf(const ChunkStart& s, TILES from = TILES())
+        : tiles(from), tile(s.tile), head(s.head), k0(s.k), left(s.units), t(s.t) {
         k1 = left > 0 ? min(t.units, k0 + left) : k0;
     }
     __device__ __forceinline__ void next(const ChunkArgs& a) {  // the item after this one (left 0: there is none)
@@ -102,7 +110,7 @@ struct ChunkWalk {
         if (++head == a.kv_heads) {
             head = 0;
             ++tile;
-            load(a);
+            t = tiles(a, tile);
         }
         k1 = min(t.units, left);
     }
@@ -111,6 +119,115 @@ struct ChunkWalk {
     __device__ __forceinline__ bool begins() const { return k0 == 0; }
     __device__ __forceinline__ bool ends() const { return k1 == t.units; }
 };
+using ChunkWalk = ChunkWalkOf<PlannedTiles>;
+
+// A slot: its first row, new tokens (as far as they lie in the row buffers), length.
+struct Slot {
+    int row0, n, len;
+};
+__device__ __forceinline__ Slot load_slot(const ChunkArgs& a, int s) {
+    Slot x;
+    x.row0 = a.cu_rows[s];
+    x.n = a.cu_rows[s + 1] - x.row0;
+    x.len = max(0, min(a.kv_lens[s], a.bt_stride << a.page_shift));
+    if (x.row0 < 0 || x.row0 > a.rows || x.n < 0) x.n = 0;
+    x.n = min(x.n, a.rows - x.row0);
+    return x;
+}
+
+template <int TR, int KT>
+__device__ __forceinline__ ChunkTile make_tile(const ChunkArgs& a, int slot, const Slot& y, int t) {
+    ChunkTile x;
+    x.slot = slot;
+    x.row0 = y.row0;
+    x.p0 = t * TR;
+    x.rows = min(y.n * a.group - x.p0, TR);
+    x.base = y.len - y.n;
+    const int first = x.base + chunk_token(a, x.p0), last = x.base + chunk_token(a, x.p0 + x.rows - 1);  // positions
+    x.hi = max(0, last + 1);
+    x.lo = a.window > 0 ? min(x.hi, max(0, first - a.window + 1)) : 0;
+    const int key0 = x.lo & ~(KT - 1);
+    x.units = max(1, (x.hi - key0 + KT - 1) / KT);
+    auto steps = [&](int p0, int rows) {  // of the keys that packed rows [p0, p0 + rows) see
+        if (rows <= 0) return make_int2(0, 0);
+        const int f = x.base + chunk_token(a, p0), l = x.base + chunk_token(a, p0 + rows - 1);
+        const int hi = max(0, l + 1), lo = a.window > 0 ? max(0, f - a.window + 1) : 0;
+        return hi <= lo ? make_int2(0, 0) : make_int2((lo - key0) / CH_STEP, (hi - key0 + CH_STEP - 1) / CH_STEP);
+    };
+    const int2 u = steps(x.p0, min(x.rows, 128)), v = steps(x.p0 + 128, x.rows - 128);
+    x.steps = make_int4(u.x, u.y, v.x, v.y);
+    return x;
+}
+
+// largest i in [0, n) with first[i] + i * extra <= x
+template <class T>
+__device__ __forceinline__ int owner(const T* first, int n, T x, T extra = 0) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first[mid] + mid * extra <= x) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// The stream in cost: an item costs its units and a.item_cost for its start and end, which come first.
+struct Map {
+    const uint32_t* unit_first;  // [tiles + 1]: first unit of every tile, counted for one key head
+    int tiles, ctas, snap;
+};
+// A border between shares: a place in the cost, the item that begins or goes on there, the unit of the item that
+// it stands before, the units before it.
+template <class U>
+struct Border {
+    U at, unit, item_end;  // item_end: where the item ends in the cost
+    int tile, head, k;
+};
+
+// CTA c's share begins at c / ctas of the cost; items of at most m.snap units are not cut: the border
+// goes to their nearer end.  In 32 bits where the cost times the CTAs fits (64-bit divisions were most of the plan's time).
+template <class U>
+__device__ __forceinline__ Border<U> border(const ChunkArgs& a, const Map& m, U cost, U units, int c) {
+    Border<U> x;
+    x.at = x.item_end = cost;
+    x.unit = units;
+    x.tile = m.tiles;
+    x.head = x.k = 0;
+    if (c >= m.ctas) return x;
+    const U u = cost * (U)c / (U)m.ctas;
+    if (u >= cost) return x;
+    const uint32_t extra = a.item_cost;
+    x.tile = owner(m.unit_first, m.tiles, (uint32_t)(u / (U)a.kv_heads), extra);
+    const uint32_t unit0 = m.unit_first[x.tile], n = m.unit_first[x.tile + 1] - unit0;
+    const U first = ((U)unit0 + (U)x.tile * extra) * (U)a.kv_heads, item = (U)n + extra;
+    x.head = (int)((uint32_t)(u - first) / (uint32_t)item);  // (an item's cost and heads: below 2^32 together)
+    x.at = first + (U)x.head * item;
+    x.unit = (U)unit0 * (U)a.kv_heads + (U)x.head * (U)n;
+    x.item_end = x.at + item;
+    const uint32_t in = (uint32_t)(u - x.at);
+    if (n <= (uint32_t)m.snap) {
+        if (in > (n + extra) / 2) {  // the next item's start
+            x.at += item;
+            x.unit += n;
+            if (++x.head == a.kv_heads) {
+                x.head = 0;
+                ++x.tile;
+            }
+            const uint32_t next = x.tile < m.tiles ? m.unit_first[x.tile + 1] - m.unit_first[x.tile] : 0;
+            x.item_end = x.at + (U)next + extra;
+        }
+    } else if (in > extra) {
+        x.k = (int)(in - extra);
+        x.unit += (U)x.k;
+        x.at = u;
+    }
+    return x;
+}
+
+// CTAs after c whose shares begin in the item that x cuts: floor(cost * i / ctas) < item_end
+template <class U>
+__device__ __forceinline__ int shares_after(const Border<U>& x, U cost, int ctas, int c) {
+    return (int)((x.item_end * (U)ctas - 1) / cost) - c;
+}
 
 cudaError_t launch_chunk_plan(const ChunkArgs& a, int tile_rows, cudaStream_t s);  // 16; 128, 256: many rows
 cudaError_t launch_chunk_tc(const ChunkArgs& a, const CUtensorMap& map, const CUtensorMap& q_map, int head_dim, int dtype,

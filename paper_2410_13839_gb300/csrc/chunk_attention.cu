@@ -36,6 +36,7 @@ constexpr int FR_KEYS = 64, FR_WARPS = 5, FR_THREADS = FR_WARPS * 32, FR_CONSUME
 constexpr int FR_MIN_UNITS = 4, CT_MIN_UNITS = 1, CT_SNAP = 12;  // fewest units of a CTA
 constexpr int FR_ITEM_COST = 2, CT_ITEM_COST = 2;
 constexpr int FR_ROWS = 16, CT_UNIT_KEYS = 128;  // a tile of few rows
+constexpr int FR_SLOTS = 128;                   // slots whose plan every CTA makes for itself
 constexpr int RESIDUE_ROWS = 32;  // rows of a slot and key head up to which the weights' residues are kept
 constexpr float LN2 = 0.69314718055994531f;
 
@@ -90,6 +91,90 @@ struct FrLayout {
     static constexpr size_t BYTES = 1024 + ML + 2 * 4 * TR * 4;
 };
 
+// Few slots: a tile each (those without new tokens have none), with the first unit of each, in shared memory.
+struct FewSlots {
+    Slot slot[FR_SLOTS];
+    int number[FR_SLOTS];
+    uint32_t first[FR_SLOTS + 1], warp_units[4], warp_tiles[4];
+    Border<uint32_t> border[2];
+};
+struct FewTiles {
+    const FewSlots* f;
+    __device__ __forceinline__ ChunkTile operator()(const ChunkArgs& a, int tile) const {
+        return a.plan_here ? make_tile<FR_ROWS, FR_KEYS>(a, f->number[tile], f->slot[tile], 0) : PlannedTiles()(a, tile);
+    }
+};
+// The plan's work for one CTA: where its share begins, and its merge.  The whole CTA calls it.
+__device__ __forceinline__ ChunkStart plan_share(const ChunkArgs& a, FewSlots& f) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
+    Slot y{0, 0, 0};
+    uint32_t units = 0;
+    if (tid < a.slots) {
+        y = load_slot(a, tid);
+        if (y.n > 0) units = make_tile<FR_ROWS, FR_KEYS>(a, tid, y, 0).units;
+    }
+    const unsigned live = __ballot_sync(FULL_MASK, units > 0);
+    uint32_t x = units;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t u = __shfl_up_sync(FULL_MASK, x, o);
+        if (lane >= o) x += u;
+    }
+    if (lane == 31 && warp < 4) {
+        f.warp_units[warp] = x;
+        f.warp_tiles[warp] = __popc(live);
+    }
+    __syncthreads();
+    uint32_t all = 0, tiles = 0, j = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (w == warp) {
+            x += all;
+            j = tiles;
+        }
+        all += f.warp_units[w];
+        tiles += f.warp_tiles[w];
+    }
+    if (units > 0) {
+        j += __popc(live & ((1u << lane) - 1));
+        f.slot[j] = y;
+        f.number[j] = tid;
+        f.first[j] = x - units;
+    }
+    if (tid == 0) f.first[tiles] = all;
+    __syncthreads();
+    Map m;
+    m.unit_first = f.first;
+    m.tiles = (int)tiles;
+    m.snap = 0;
+    const uint32_t sum = all * a.kv_heads, cost = sum + tiles * a.item_cost * a.kv_heads;
+    m.ctas = min(a.ctas, max(1, (int)((sum + a.min_units - 1) / a.min_units)));
+    if (lane == 0 && warp < 2) f.border[warp] = border<uint32_t>(a, m, cost, sum, cta + warp);
+    __syncthreads();
+    const Border<uint32_t> at = f.border[0], end = f.border[1];
+    ChunkStart s;
+    s.tile = s.head = s.k = s.units = 0;
+    int more = 0;
+    if (at.at < end.at) {
+        s.tile = at.tile;
+        s.head = at.head;
+        s.k = at.k;
+        s.units = (int)(end.unit - at.unit);
+        s.t = make_tile<FR_ROWS, FR_KEYS>(a, f.number[at.tile], f.slot[at.tile], 0);
+        if (tid == 0 && end.k > 0 && (at.tile != end.tile || at.head != end.head || at.k == 0)) {
+            more = shares_after(end, cost, m.ctas, cta);
+            const Slot& z = f.slot[end.tile];
+            int* d = a.desc + cta * CH_DESC;
+            d[1] = 0;
+            d[2] = min(z.n * a.group, FR_ROWS);
+            d[3] = z.row0;
+            d[4] = end.head;
+        }
+    }
+    if (tid == 0) a.desc[cta * CH_DESC] = more;
+    return s;
+}
+
 template <class T, int HD>
 __global__ void __launch_bounds__(FR_THREADS, HD == 64 ? 3 : 2)
     chunk_rows_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ CUtensorMap map) {
@@ -97,6 +182,7 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 ? 3 : 2)
     constexpr int TR = L::TR, ST = L::STAGES;
     extern __shared__ unsigned char fr_raw[];
     __shared__ uint64_t full[ST], empty[ST];
+    __shared__ FewSlots few;
     unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(fr_raw) + 1023) & ~(uintptr_t)1023);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
     if (tid == 0) {
@@ -109,7 +195,7 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 ? 3 : 2)
     __syncthreads();
     pdl_launch_dependents();
     pdl_wait();  // the plan
-    const ChunkStart start = a.start[cta];
+    const ChunkStart start = a.plan_here ? plan_share(a, few) : a.start[cta];
     const int units = start.units;
     if (units == 0) return;
 
@@ -119,7 +205,7 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 ? 3 : 2)
         const int sub = lane % per, half = lane / per % (HD / 64), kv = lane / per / (HD / 64);
         const bool mine = kv < 2;
         unsigned char* ring = sm + kv * L::KV + half * L::TILE + sub * box * 128;
-        ChunkWalk w(start);
+        ChunkWalkOf<FewTiles> w(start, FewTiles{&few});
         int k = w.k0, issued = 0, base = 0, pages = 0, ahead = 0;
         bool ok = true;
         // pages [base, base + 32) of the slot, one per lane, and the 32 after them
@@ -170,7 +256,7 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 ? 3 : 2)
     float* ml = reinterpret_cast<float*>(sm + L::ML);  // [4 warps][TR] maxima, then sums
     int stage = 0;
     bool alive = true;
-    ChunkWalk w(start);
+    ChunkWalkOf<FewTiles> w(start, FewTiles{&few});
     for (; w.left > 0; w.next(a)) {
         const ChunkTile& t = w.t;
         const int key_first = w.key0<FR_KEYS>();
@@ -447,7 +533,7 @@ cudaError_t merge_hd(const ChunkArgs& a, int tile_rows, cudaStream_t s) {
 // How a call runs: tile rows, CTAs, workspace.
 struct ChunkPlan {
     int tile_rows, ctas, max_tiles, min_units;
-    bool residues;
+    bool residues, plan_here;
     size_t start, desc, tiles, part, need;  // places in the workspace, its bytes
 };
 
@@ -485,6 +571,9 @@ int chunk_plan(const mtp_chunk_attention_args* a, ChunkPlan* p) {
     p->min_units = few ? FR_MIN_UNITS : CT_MIN_UNITS;
     const long long units = tiles * a->n_kv_heads * (a->max_keys / keys + 2);
     p->ctas = (int)std::max(1ll, std::min((long long)sms * per_sm, (units + p->min_units - 1) / p->min_units));
+    // what a slot can cost at most, in a table of its width, has to fit the plan's 32 bits
+    const long long slot_cost = (long long)a->bt_stride * a->page_size / FR_KEYS + 1 + FR_ITEM_COST;
+    p->plan_here = few && a->slots <= FR_SLOTS && a->slots * slot_cost * a->n_kv_heads * p->ctas < 1ll << 32;
     auto place = [&](size_t bytes) {
         const size_t at = p->need;
         p->need += (bytes + 255) & ~(size_t)255;
@@ -504,11 +593,11 @@ cudaError_t launch_rows(const ChunkArgs& a, const CUtensorMap& map, cudaStream_t
     const auto kern = chunk_rows_kernel<T, HD>;
     const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem, true);
     if (e != cudaSuccess) return e;
-    return launch_ex(kern, dim3(a.ctas), FR_THREADS, smem, true, s, a, map);
+    return launch_ex(kern, dim3(a.ctas), FR_THREADS, smem, !a.plan_here, s, a, map);
 }
 template <class T>
 cudaError_t launch_kernels(const ChunkArgs& a, const CUtensorMap& map, const CUtensorMap& q_map, int head_dim, int dtype, int tile_rows, cudaStream_t s) {
-    cudaError_t e = launch_chunk_plan(a, tile_rows, s);
+    cudaError_t e = a.plan_here ? cudaSuccess : launch_chunk_plan(a, tile_rows, s);
     if (e != cudaSuccess) return e;
     if (tile_rows > FR_ROWS)
         e = launch_chunk_tc(a, map, q_map, head_dim, dtype, s);
@@ -570,6 +659,7 @@ MTP_API int mtp_chunk_attention(const mtp_chunk_attention_args* a, void* workspa
         const bool few = p.tile_rows == FR_ROWS;
         c.residues = p.residues;
         c.snap = few ? 0 : CT_SNAP;
+        c.plan_here = p.plan_here;
         c.item_cost = few ? FR_ITEM_COST : CT_ITEM_COST;
         c.q_vec = aligned16(a->q) && a->q_stride % 8 == 0;
         c.out_vec = aligned16(a->out) && a->out_stride % 8 == 0;

@@ -9,44 +9,6 @@ namespace {
 
 constexpr int PL_THREADS = 1024, PL_WARPS = PL_THREADS / 32;
 
-// A slot in shared memory: its first row, new tokens (as far as they lie in the row buffers), length.
-struct Slot {
-    int row0, n, len;
-};
-__device__ __forceinline__ Slot load_slot(const ChunkArgs& a, int s) {
-    Slot x;
-    x.row0 = a.cu_rows[s];
-    x.n = a.cu_rows[s + 1] - x.row0;
-    x.len = max(0, min(a.kv_lens[s], a.bt_stride << a.page_shift));
-    if (x.row0 < 0 || x.row0 > a.rows || x.n < 0) x.n = 0;
-    x.n = min(x.n, a.rows - x.row0);
-    return x;
-}
-
-template <int TR, int KT>
-__device__ __forceinline__ ChunkTile make_tile(const ChunkArgs& a, int slot, const Slot& y, int t) {
-    ChunkTile x;
-    x.slot = slot;
-    x.row0 = y.row0;
-    x.p0 = t * TR;
-    x.rows = min(y.n * a.group - x.p0, TR);
-    x.base = y.len - y.n;
-    const int first = x.base + chunk_token(a, x.p0), last = x.base + chunk_token(a, x.p0 + x.rows - 1);  // positions
-    x.hi = max(0, last + 1);
-    x.lo = a.window > 0 ? min(x.hi, max(0, first - a.window + 1)) : 0;
-    const int key0 = x.lo & ~(KT - 1);
-    x.units = max(1, (x.hi - key0 + KT - 1) / KT);
-    auto steps = [&](int p0, int rows) {  // of the keys that packed rows [p0, p0 + rows) see
-        if (rows <= 0) return make_int2(0, 0);
-        const int f = x.base + chunk_token(a, p0), l = x.base + chunk_token(a, p0 + rows - 1);
-        const int hi = max(0, l + 1), lo = a.window > 0 ? max(0, f - a.window + 1) : 0;
-        return hi <= lo ? make_int2(0, 0) : make_int2((lo - key0) / CH_STEP, (hi - key0 + CH_STEP - 1) / CH_STEP);
-    };
-    const int2 u = steps(x.p0, min(x.rows, 128)), v = steps(x.p0 + 128, x.rows - 128);
-    x.steps = make_int4(u.x, u.y, v.x, v.y);
-    return x;
-}
-
 // Exclusive prefix sum of x over the block, and the total.
 __device__ __forceinline__ uint32_t scan(uint32_t x, uint32_t* part, uint32_t& sum) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -62,71 +24,6 @@ __device__ __forceinline__ uint32_t scan(uint32_t x, uint32_t* part, uint32_t& s
     const uint32_t mine = lane < PL_WARPS ? part[lane] : 0;
     sum = __reduce_add_sync(FULL_MASK, mine);
     return __reduce_add_sync(FULL_MASK, lane < warp ? mine : 0) + y - x;
-}
-
-// largest i in [0, n) with first[i] + i * extra <= x
-template <class T>
-__device__ __forceinline__ int owner(const T* first, int n, T x, T extra = 0) {
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (first[mid] + mid * extra <= x) lo = mid; else hi = mid;
-    }
-    return lo;
-}
-
-// The stream in cost: an item costs its units and a.item_cost for its start and end, which come first.
-struct Map {
-    const uint32_t* unit_first;  // [tiles + 1]: first unit of every tile, counted for one key head
-    int tiles, ctas, snap;
-};
-// A border between shares: a place in the cost, the item that begins or goes on there, the unit of the item that
-// it stands before, the units before it.
-template <class U>
-struct Border {
-    U at, unit, item_end;  // item_end: where the item ends in the cost
-    int tile, head, k;
-};
-
-// Shares and merges, in 32 bits where the cost times the CTAs fits (64-bit divisions were most of
-// the plan's time).  CTA c's share begins at c / ctas of the cost; items of at most m.snap units
-// are not cut: the border goes to their nearer end.
-template <class U>
-__device__ __forceinline__ Border<U> border(const ChunkArgs& a, const Map& m, U cost, U units, int c) {
-    Border<U> x;
-    x.at = x.item_end = cost;
-    x.unit = units;
-    x.tile = m.tiles;
-    x.head = x.k = 0;
-    if (c >= m.ctas) return x;
-    const U u = cost * (U)c / (U)m.ctas;
-    if (u >= cost) return x;
-    const uint32_t extra = a.item_cost;
-    x.tile = owner(m.unit_first, m.tiles, (uint32_t)(u / (U)a.kv_heads), extra);
-    const uint32_t unit0 = m.unit_first[x.tile], n = m.unit_first[x.tile + 1] - unit0;
-    const U first = ((U)unit0 + (U)x.tile * extra) * (U)a.kv_heads, item = (U)n + extra;
-    x.head = (int)((uint32_t)(u - first) / (uint32_t)item);  // (an item's cost and heads: below 2^32 together)
-    x.at = first + (U)x.head * item;
-    x.unit = (U)unit0 * (U)a.kv_heads + (U)x.head * (U)n;
-    x.item_end = x.at + item;
-    const uint32_t in = (uint32_t)(u - x.at);
-    if (n <= (uint32_t)m.snap) {
-        if (in > (n + extra) / 2) {  // the next item's start
-            x.at += item;
-            x.unit += n;
-            if (++x.head == a.kv_heads) {
-                x.head = 0;
-                ++x.tile;
-            }
-            const uint32_t next = x.tile < m.tiles ? m.unit_first[x.tile + 1] - m.unit_first[x.tile] : 0;
-            x.item_end = x.at + (U)next + extra;
-        }
-    } else if (in > extra) {
-        x.k = (int)(in - extra);
-        x.unit += (U)x.k;
-        x.at = u;
-    }
-    return x;
 }
 
 template <class U>
@@ -147,8 +44,7 @@ __device__ __forceinline__ void share_out(const ChunkArgs& a, const Map& m, U co
             to[3] = from[2];
             // the item that this share ends in, where it begins in the share and goes on, up to the CTA with its last unit
             if (y.k > 0 && (x.tile != y.tile || x.head != y.head || x.k == 0)) {
-                more = 1;
-                while (borders[c + 1 + more].at < y.item_end) ++more;
+                more = shares_after(y, cost, m.ctas, c);
                 const ChunkTile& t = tiles[y.tile];
                 int* d = a.desc + c * CH_DESC;
                 d[1] = t.p0;
