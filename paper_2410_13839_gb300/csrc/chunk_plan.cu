@@ -27,8 +27,7 @@ __device__ __forceinline__ uint32_t scan(uint32_t x, uint32_t* part, uint32_t& s
 }
 
 template <class U>
-__device__ __forceinline__ void share_out(const ChunkArgs& a, const Map& m, U cost, U units, const ChunkTile* tiles,
-                                          Border<U>* borders) {
+__device__ __forceinline__ void share_out(const ChunkArgs& a, const Map& m, U cost, U units, Border<U>* borders) {
     for (int c = threadIdx.x; c <= a.ctas; c += PL_THREADS) borders[c] = border<U>(a, m, cost, units, c);
     __syncthreads();
     for (int c = threadIdx.x; c < a.ctas; c += PL_THREADS) {
@@ -38,14 +37,14 @@ __device__ __forceinline__ void share_out(const ChunkArgs& a, const Map& m, U co
         int4* to = reinterpret_cast<int4*>(a.start + c);
         if (x.at < y.at) {
             start = make_int4(x.tile, x.head, x.k, (int)(y.unit - x.unit));
-            const int4* from = reinterpret_cast<const int4*>(tiles + x.tile);
+            const int4* from = reinterpret_cast<const int4*>(a.tiles + x.tile);
             to[1] = from[0];
             to[2] = from[1];
             to[3] = from[2];
             // the item that this share ends in, where it begins in the share and goes on, up to the CTA with its last unit
             if (y.k > 0 && (x.tile != y.tile || x.head != y.head || x.k == 0)) {
                 more = shares_after(y, cost, m.ctas, c);
-                const ChunkTile& t = tiles[y.tile];
+                const ChunkTile& t = a.tiles[y.tile];
                 int* d = a.desc + c * CH_DESC;
                 d[1] = t.p0;
                 d[2] = t.rows;
@@ -58,20 +57,17 @@ __device__ __forceinline__ void share_out(const ChunkArgs& a, const Map& m, U co
     }
 }
 
-// Shared memory: borders, the tiles where they are few, slots, first tile of every slot, first unit of every tile.
-constexpr int PL_KEPT = 512;
+// Shared memory: borders, slots, first tile of every slot, first unit of every tile.
 __host__ __device__ inline size_t border_bytes(int ctas) { return ((size_t)(ctas + 1) * sizeof(Border<unsigned long long>) + 15) & ~(size_t)15; }
 size_t plan_smem(const ChunkArgs& a) {
-    return border_bytes(a.ctas) + (a.max_tiles <= PL_KEPT ? a.max_tiles * sizeof(ChunkTile) : 0) + (size_t)a.slots * sizeof(Slot) + (size_t)(a.slots + a.max_tiles + 2) * 4;
+    return border_bytes(a.ctas) + (size_t)a.slots * sizeof(Slot) + (size_t)(a.slots + a.max_tiles + 2) * 4;
 }
 
 template <int TR, int KT>
 __global__ void __launch_bounds__(PL_THREADS) chunk_plan_kernel(const __grid_constant__ ChunkArgs a) {
     extern __shared__ __align__(16) unsigned char pl_sm[];
     __shared__ uint32_t part[PL_WARPS];
-    const bool keep = a.max_tiles <= PL_KEPT;
-    ChunkTile* kept = reinterpret_cast<ChunkTile*>(pl_sm + border_bytes(a.ctas));
-    Slot* slots = reinterpret_cast<Slot*>(kept + (keep ? a.max_tiles : 0));
+    Slot* slots = reinterpret_cast<Slot*>(pl_sm + border_bytes(a.ctas));
     uint32_t* slot_first = reinterpret_cast<uint32_t*>(slots + a.slots);  // [slots + 1]
     uint32_t* unit_first = slot_first + a.slots + 1;                      // [tiles + 1]
     const int tid = threadIdx.x;
@@ -106,7 +102,6 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan_kernel(const __grid_con
             to[0] = from[0];
             to[1] = from[1];
             to[2] = from[2];
-            if (keep) kept[j] = t;
             x = t.units;
         }
         x = scan(x, part, sum);
@@ -122,11 +117,10 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan_kernel(const __grid_con
                       max(1ull, narrow ? (unsigned long long)(((uint32_t)units + a.min_units - 1) / a.min_units)
                                        : (units + a.min_units - 1) / a.min_units));
     m.snap = a.snap > 0 ? (int)min((unsigned long long)a.snap, narrow ? (uint32_t)units / m.ctas / 3 : units / m.ctas / 3) : 0;
-    const ChunkTile* tiles = keep ? kept : a.tiles;
     if (narrow)
-        share_out<uint32_t>(a, m, (uint32_t)cost, (uint32_t)units, tiles, reinterpret_cast<Border<uint32_t>*>(pl_sm));
+        share_out<uint32_t>(a, m, (uint32_t)cost, (uint32_t)units, reinterpret_cast<Border<uint32_t>*>(pl_sm));
     else
-        share_out<unsigned long long>(a, m, cost, units, tiles, reinterpret_cast<Border<unsigned long long>*>(pl_sm));
+        share_out<unsigned long long>(a, m, cost, units, reinterpret_cast<Border<unsigned long long>*>(pl_sm));
 }
 
 template <int TR, int KT>
