@@ -27,8 +27,10 @@ namespace mtp {
 namespace {
 
 constexpr int PG_CLUSTER = 8, PG_THREADS = 1024, PG_WARPS = PG_THREADS / 32;
-// one CTA up to these (32 slots and 2048 pages, one CTA against eight: 6.9 and 8.2 us a plan; 16384 pages: level)
-constexpr int PG_ONE_PAGES = 16384, PG_ONE_SLOTS = 1024, PG_ONE_ROWS = 8192, PG_ONE_BEAMS = 512, PG_KEPT = 16384;
+// One CTA up to these.  One CTA against eight, us a call: plan of 32 slots and 2048 pages 6.3 and 8.3, 32768 pages 10.4 and
+// 8.3; of 1024 slots and 34,000 pages 12.4 and 10.4; reordering of 96 beams 12.5 and 14.5, of 256 beams 16.5 and 15.8, of
+// 512 21.0 and 16.5.  Rows written by the plan's own launch against one of theirs: 4096 rows 10.4 and 12.4, 8192 14.5 and 12.4.
+constexpr int PG_ONE_PAGES = 16384, PG_ONE_SLOTS = 1024, PG_ONE_ROWS = 4096, PG_ONE_BEAMS = 192;
 constexpr int PG_MAX_SLOTS = 8192;
 constexpr int PG_MAX_PAGES = 1 << 22;
 constexpr int PG_MAX_ROWS = 1 << 24;
@@ -372,7 +374,6 @@ struct ReorderArgs {
     mtp_beam_reorder_args a;
     int shift;
     int rows;      // batch * beams
-    int kept;      // table entries that shared memory holds
     int* count;    // workspace: pages to copy
     int4* copies;  // workspace: {from, to, tokens, -}
 };
@@ -427,21 +428,16 @@ __global__ void __launch_bounds__(PG_THREADS, 1) beam_reorder_kernel(const __gri
     }
     if (tid == 0) copies_before[rows] = (int)want;
     bad = __syncthreads_or(bad) != 0;
-    // every page that a table holds is one, and is counted (an entry per thread; the old tables stay in shared memory
-    // where they fit, for the steps below)
+    // every page that a table holds is one, and is counted (an entry per thread)
     const unsigned stride = a.bt_stride, first = rank * PG_THREADS + tid, step = CTAS * PG_THREADS, entries = rows * stride;
-    const bool keep = CTAS == 1 && entries <= (unsigned)p.kept;
-    int* kept = reinterpret_cast<int*>(bits + 2 * free_words(a.n_pages, CTAS));
     if (!bad)
 #pragma unroll 4
         for (unsigned e = first; e < entries; e += step) {
             const int r = e / stride, c = e - r * stride;
-            int page = -1;
             if (c < pages_of(old[r], p.shift)) {
-                page = a.block_table[e];
+                const int page = a.block_table[e];
                 bad |= page < 0 || page >= a.n_pages || a.page_refs[page] < 1;
             }
-            if (keep) kept[e] = page;
         }
     bad = __syncthreads_or(bad) != 0;
     if (tid == 0) s_bad = bad;
@@ -482,8 +478,7 @@ __global__ void __launch_bounds__(PG_THREADS, 1) beam_reorder_kernel(const __gri
             if (c == used - 1 && copies_before[r + 1] != copies_before[r]) {
                 page = __ldcg(&p.copies[copies_before[r]].y);
             } else {
-                const unsigned at = from[r] * stride + c;
-                page = keep ? kept[at] : a.block_table[at];
+                page = a.block_table[from[r] * stride + c];
                 if (!itself(r)) atomicAdd(a.out_page_refs + page, 1);
             }
         }
@@ -495,7 +490,7 @@ __global__ void __launch_bounds__(PG_THREADS, 1) beam_reorder_kernel(const __gri
     for (unsigned e = first; e < entries; e += step) {
         const int r = e / stride, c = e - r * stride;
         if (c < pages_of(old[r], p.shift) && !itself(r))
-            freed += atomicSub(a.out_page_refs + (keep ? kept[e] : a.block_table[e]), 1) == 1;
+            freed += atomicSub(a.out_page_refs + a.block_table[e], 1) == 1;
     }
     if (freed) atomicAdd(&s_freed, freed);
     team_barrier<CTAS>();
@@ -662,11 +657,9 @@ MTP_API int mtp_beam_reorder(const mtp_beam_reorder_args* a, void* workspace, si
             return invalid("beam_reorder: workspace %zu bytes, need %zu, 16-byte aligned", workspace_bytes,
                            reorder_workspace(rows));
         const bool one = a->n_pages <= PG_ONE_PAGES && rows <= PG_ONE_BEAMS;
-        const long long entries = (long long)rows * a->bt_stride;
-        const int kept = one && entries <= PG_KEPT ? (int)entries : 0;
-        const ReorderArgs p{*a, log2_of(a->page_size), rows, kept, static_cast<int*>(workspace),
+        const ReorderArgs p{*a, log2_of(a->page_size), rows, static_cast<int*>(workspace),
                             reinterpret_cast<int4*>(static_cast<char*>(workspace) + 16)};
-        const size_t smem = (size_t)(3 * rows + 1 + 2 * free_words(a->n_pages, one ? 1 : PG_CLUSTER) + kept) * 4;
+        const size_t smem = (size_t)(3 * rows + 1 + 2 * free_words(a->n_pages, one ? 1 : PG_CLUSTER)) * 4;
         const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
         cudaError_t e = one ? launch(beam_reorder_kernel<1>, 1, PG_THREADS, smem, 1, false, s, p)
                             : launch(beam_reorder_kernel<PG_CLUSTER>, PG_CLUSTER, PG_THREADS, smem, PG_CLUSTER, false, s, p);

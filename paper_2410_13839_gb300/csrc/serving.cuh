@@ -1,6 +1,5 @@
 // serving.cuh -- what the paged beam-search operators (paged.cu, beam.cu,
-// chunk_attention*.cu) share: argument errors, element types, the cache pool's
-// layout and block-wide prefix sums.
+// chunk_attention*.cu) share: argument errors, element types.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -58,44 +57,5 @@ struct F16 {
         return *reinterpret_cast<const uint32_t*>(&p);
     }
 };
-
-// Exclusive prefix sums of x and y over the threads of a block of WARPS warps, and
-// their totals.  `part` is shared memory; the call synchronises the block.
-template <int WARPS>
-__device__ __forceinline__ void block_scan2(long long& x, long long& y, long long (*part)[2], long long& sum_x,
-                                            long long& sum_y) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    long long ix = x, iy = y;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long ux = __shfl_up_sync(FULL_MASK, ix, o), uy = __shfl_up_sync(FULL_MASK, iy, o);
-        if (lane >= o) {
-            ix += ux;
-            iy += uy;
-        }
-    }
-    __syncthreads();  // `part` may still be read from an earlier call
-    if (lane == 31) {
-        part[warp][0] = ix;
-        part[warp][1] = iy;
-    }
-    __syncthreads();
-    long long bx = lane < WARPS ? part[lane][0] : 0, by = lane < WARPS ? part[lane][1] : 0;
-    const long long tx = bx, ty = by;
-#pragma unroll
-    for (int o = 1; o < WARPS; o <<= 1) {
-        const long long ux = __shfl_up_sync(FULL_MASK, bx, o), uy = __shfl_up_sync(FULL_MASK, by, o);
-        if (lane >= o) {
-            bx += ux;
-            by += uy;
-        }
-    }
-    sum_x = __shfl_sync(FULL_MASK, bx, WARPS - 1);
-    sum_y = __shfl_sync(FULL_MASK, by, WARPS - 1);
-    bx = __shfl_sync(FULL_MASK, bx - tx, warp);
-    by = __shfl_sync(FULL_MASK, by - ty, warp);
-    x = bx + ix - x;
-    y = by + iy - y;
-}
 
 }  // namespace mtp
