@@ -344,6 +344,19 @@ __global__ void __launch_bounds__(BS_THREADS) beam_select_kernel(const __grid_co
             const int take = min(room - have, total - at);
             for (int i = tid; i < take; i += BS_THREADS) held[have + i] = __ldcg(keys + at + i);
             __syncthreads();
+            if (total <= BS_THREADS) {  // few: each finds its rank among all
+                if (tid < BS_MAX_K) b.best[tid] = 0;
+                __syncthreads();
+                if (tid < total && held[tid]) {
+                    const unsigned long long x = held[tid];
+                    int larger = 0;
+#pragma unroll 8
+                    for (int j = 0; j < total; ++j) larger += held[j] > x;
+                    if (larger < a.k) b.best[larger] = x;
+                }
+                __syncthreads();
+                break;
+            }
             unsigned long long most = 0;
             for (int i = tid; i < have + take; i += BS_THREADS) most = max(most, held[i]);
             best_of(b, a.k, most, [&](auto f) {
