@@ -473,7 +473,7 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 ? 3 : 2)
 template <class T, int HD, int TR>
 __global__ void __launch_bounds__(128) chunk_merge_kernel(const ChunkArgs a) {
     const int cta = blockIdx.x, r = blockIdx.y * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    constexpr int PER = HD / 32;
+    constexpr int PER = HD / 32, BATCH = TR == FR_ROWS ? 8 : 4;  // (tiles of many rows are shared by few CTAs)
     pdl_wait();
     const int* d = a.desc + cta * CH_DESC;
     const int more = d[0];
@@ -483,24 +483,37 @@ __global__ void __launch_bounds__(128) chunk_merge_kernel(const ChunkArgs a) {
     const float* first = a.part + ((size_t)cta * 2 + 1) * STEP;
     const float* rest = a.part + ((size_t)cta + 1) * 2 * STEP;
     auto part = [&](int i) { return i == 0 ? first : rest + (size_t)(i - 1) * 2 * STEP; };
-    float top = -INFINITY;
-    for (int i = lane; i <= more; i += 32) top = fmaxf(top, part(i)[TR * HD + 2 * r]);
-    top = warp_max(top);
-    const float ref = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, o[PER];
+    float top = -INFINITY, sum = 0.f, o[PER];
 #pragma unroll
     for (int e = 0; e < PER; ++e) o[e] = 0.f;
-#pragma unroll 4
-    for (int i = 0; i <= more; ++i) {
-        const float* p = part(i);
-        const float2 x = *reinterpret_cast<const float2*>(p + TR * HD + 2 * r);
-        const float f = ex2(x.x - ref);
-        sum = fmaf(f, x.y, sum);
+    for (int i0 = 0; i0 <= more; i0 += BATCH) {  // a batch's maxima, sums and outputs are on their way together
+        float2 x[BATCH], v[BATCH][PER / 2];
 #pragma unroll
-        for (int e = 0; e < PER; e += 2) {
-            const float2 v = *reinterpret_cast<const float2*>(p + r * HD + lane * PER + e);
-            o[e] = fmaf(f, v.x, o[e]);
-            o[e + 1] = fmaf(f, v.y, o[e + 1]);
+        for (int i = 0; i < BATCH; ++i) {
+            const bool there = i0 + i <= more;
+            const float* p = part(i0 + i);
+            x[i] = there ? *reinterpret_cast<const float2*>(p + TR * HD + 2 * r) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int e = 0; e < PER / 2; ++e)
+                v[i][e] = there ? *reinterpret_cast<const float2*>(p + r * HD + lane * PER + 2 * e) : make_float2(0.f, 0.f);
+        }
+        float now = top;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) now = fmaxf(now, x[i].x);
+        const float ref = now == -INFINITY ? 0.f : now, back = ex2(top - ref);
+        top = now;
+        sum *= back;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) o[e] *= back;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const float f = ex2(x[i].x - ref);
+            sum = fmaf(f, x[i].y, sum);
+#pragma unroll
+            for (int e = 0; e < PER / 2; ++e) {
+                o[2 * e] = fmaf(f, v[i][e].x, o[2 * e]);
+                o[2 * e + 1] = fmaf(f, v[i][e].y, o[2 * e + 1]);
+            }
         }
     }
     const int p = d[1] + r, token = chunk_token(a, p), head = d[4] * a.group + p - token * a.group;
