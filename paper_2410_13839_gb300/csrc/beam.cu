@@ -23,6 +23,10 @@
 // Short items are one segment; where their log-sum-exp is not given they are held in shared
 // memory, and it is taken in the same launch.  Longer items have a kernel for it before, whose
 // reading leaves the logits in L2.
+//
+// What bounds it is latency: a dozen steps with a barrier between them, and for a cut item the way
+// of the keys through the workspace.  1 x 5 beams of 1025 fp32 logits, log-sum-exp included: 8.3 us
+// a call; 32 x 4 beams of 48001 bf16 logits with theirs given: 16.5 us (12 MB, 1.8 us at 6.8 TB/s).
 #include <float.h>
 
 #include <algorithm>
@@ -33,9 +37,15 @@ namespace mtp {
 namespace {
 
 constexpr int BS_THREADS = 512, BS_WARPS = BS_THREADS / 32;
-constexpr int HELD = 14336, LEAST = 2048;  // most scores of an item held in shared memory; fewest of a segment
-constexpr int WHOLE = 10240;                // scores of an item that is not cut
-constexpr int SEL_PER_SM = 2;              // CTAs of a wave
+// Most scores of an item held in shared memory.  Held, and with a launch of its own for the log-sum-exp, us a call: 5 beams of
+// 1025 8.4 and 12.4, 8 of 1500 12.4 and 14.4.
+constexpr int HELD = 14336;
+// Scores of an item that is not cut.  Whole and cut: 5125 scores 8.4 and 10.4, 10,000 8.4 and 10.4, 12,000 10.4 and 10.4,
+// 40,000 14.5 and 10.4.
+constexpr int WHOLE = 10240;
+// Fewest scores of a segment (1 x 4 beams of 48001, segments of 1024, 2048, 4096 at least: 14.5, 12.5, 12.4 us); CTAs of a wave
+// per SM (32 x 4 beams of 48001, 1 to 4: 21, 20.3, 23, 25 us when it was chosen).
+constexpr int LEAST = 2048, SEL_PER_SM = 2;
 constexpr int GROUPS = 128;       // groups of four threads, each with a maximum
 constexpr int CAND_MAX = 1024, HELD_KEYS = 1024;
 constexpr int BS_MAX_K = 64, BS_MAX_BEAMS = 64, BS_MAX_BATCH = 4096;
@@ -404,8 +414,7 @@ int select_plan(const mtp_beam_select_args* a, SelectPlan* p) {
         cudaGetLastError();
         sms = 152;  // (the sizes are checked all the same; a launch will say what is wrong)
     }
-    // as many segments as make one wave, none shorter than LEAST; short items are one (joining segments takes about
-    // 5 us, a CTA reads 10240 scores in 2)
+    // as many segments as make one wave, none shorter than LEAST; short items are one
     p->lse_here = !a->lse && all <= HELD;
     p->segments = p->lse_here || all <= WHOLE ? 1 : std::max(1, std::min((all + LEAST - 1) / LEAST, SEL_PER_SM * sms / a->batch));
     p->seg_len = ((all + p->segments - 1) / p->segments + 7) & ~7;  // even segments

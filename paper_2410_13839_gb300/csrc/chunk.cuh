@@ -7,13 +7,18 @@
 // first that one of its rows sees to the last, are cut into units of KT keys.  The units
 // of all items, item after item, are one stream, of which CTA c of N takes the c-th N-th:
 // ragged slots, few long ones or many short ones all give CTAs of equal work, at one
-// prologue each.  A plan kernel of one CTA writes the tiles, every CTA's first item and the
-// merges into the workspace; under programmatic launch the kernel after it sets itself up
-// meanwhile.  (Made by every CTA for itself, the plan and the look-ups in it were a third of a
-// prompt batch's time.)  An item that lies in one CTA's share is written by that CTA.  One that
-// several share leaves (maximum, sum, unnormalised output) per row and CTA in the
-// workspace, and a merge kernel after this one joins them by their maxima, in the CTAs'
-// order: nothing depends on which CTA ends first.
+// prologue each.  In that sharing an item counts ITEM_COST units more than it has, for its start
+// and end.  A plan kernel of one CTA writes the tiles, every CTA's first item and the merges into
+// the workspace; under programmatic launch the kernel after it sets itself up meanwhile.  (Made
+// by every CTA for itself, the plan of 25 prompts' tiles cost 85 us a call where the kernel's
+// costs 66.)  A decoding step has one tile per slot: where its slots are at most FR_SLOTS, every CTA
+// makes its own share's plan in shared memory, and the launch and the wait for it are saved (32
+// slots of up to 2000 keys 40.3 us with the plan kernel, 36.7 without; 8 slots 18.5 and 14.5).
+//
+// An item that lies in one CTA's share is written by that CTA.  One that several share leaves
+// (maximum, sum, unnormalised output) per row and CTA in the workspace, and a merge kernel
+// after this one joins them by their maxima, in the CTAs' order: nothing depends on which CTA
+// ends first.
 #pragma once
 #include "serving.cuh"
 
@@ -21,6 +26,8 @@ namespace mtp {
 
 constexpr int CH_MAX_SLOTS = 4096, CH_MAX_PACKED = 1 << 21;
 constexpr int CH_STEP = 64;  // keys of a step of the many-rows kernel
+// An item's start and end, in units.  0, 1, 2, 3: 25 prompts 66, 56, 52, 53 us; a step of 32 slots 47, 43.5, 42.5, 43.
+constexpr int ITEM_COST = 2;
 
 // A tile in the workspace: three 16-byte pieces.
 struct ChunkTile {
@@ -39,7 +46,8 @@ static_assert(sizeof(ChunkStart) == 64, "four pieces");
 
 // Tiles of 128 rows of a CTA of the many-rows kernel, and CTAs of an SM (they fill TMEM).  One tile of 64
 // dims and two CTAs: bound by the softmax, they need no shared keys, and a tile's start and
-// end lie behind the other CTA's work.  128 dims: two tiles, for half the key and value copies.
+// end lie behind the other CTA's work.  128 dims: two tiles, which share the copies of their keys
+// and values (two CTAs' rings would not fit shared memory).
 constexpr int chunk_tc_tiles(int head_dim) { return head_dim == 64 ? 1 : 2; }
 
 struct ChunkArgs {
@@ -52,7 +60,6 @@ struct ChunkArgs {
     uint32_t group_inv;            // ceil(2^32 / group)
     int page_blocks, layer_block;  // (layer, K | V, head) blocks of a page; the layer's first
     int window, max_tiles, min_units, ctas;
-    int item_cost;                 // an item's start and end, in units
     int snap;                      // items of at most so many units (and a third of a share) are not cut
     bool plan_here;                // few rows, few slots: every CTA makes its share itself
     bool q_vec, out_vec;           // rows 16-byte aligned
@@ -170,7 +177,7 @@ __device__ __forceinline__ int owner(const T* first, int n, T x, T extra = 0) {
     return lo;
 }
 
-// The stream in cost: an item costs its units and a.item_cost for its start and end, which come first.
+// The stream in cost: an item costs its units and ITEM_COST for its start and end, which come first.
 struct Map {
     const uint32_t* unit_first;  // [tiles + 1]: first unit of every tile, counted for one key head
     int tiles, ctas, snap;
@@ -195,7 +202,7 @@ __device__ __forceinline__ Border<U> border(const ChunkArgs& a, const Map& m, U 
     if (c >= m.ctas) return x;
     const U u = cost * (U)c / (U)m.ctas;
     if (u >= cost) return x;
-    const uint32_t extra = a.item_cost;
+    constexpr uint32_t extra = ITEM_COST;
     x.tile = owner(m.unit_first, m.tiles, (uint32_t)(u / (U)a.kv_heads), extra);
     const uint32_t unit0 = m.unit_first[x.tile], n = m.unit_first[x.tile + 1] - unit0;
     const U first = ((U)unit0 + (U)x.tile * extra) * (U)a.kv_heads, item = (U)n + extra;

@@ -12,8 +12,16 @@
 // warp fills them, a lane per page piece, with TMA copies that lay the rows out in the
 // 128-byte swizzle that ldmatrix reads without bank conflicts.  Each of the four other
 // warps takes 16 of a stage's keys: S = Q K^T and O += P V by mma.sync (16 rows of a tile
-// as M; tcgen05's 128 rows would be empty for most), with a maximum, sum and output of its
-// own, which the four join at the item's end.
+// as M), with a maximum, sum and output of its own, which the four join at the item's end.
+// From 17 rows on the tensor cores' 128-row tiles are used, mostly empty (chunk_attention_tc.cu):
+// 16 rows on 8 contexts of 4,000 to 30,000 keys, 128 dims fp16, take 86 us here and 96 there, on
+// 32 of up to 2000 keys, 64 dims bf16, 19.6 and 28.9; 32 rows, in tiles of 32 rows made as
+// these are, took 172 and 24.8, there 98 and 26.8, on 128 contexts 62 and 55.
+//
+// A decoding step of 32 slots (180 to 2000 keys, 16 heads of 64, 147 MB) takes 35.1 us a call, of
+// which the memory's part is 21.6 us: the share's plan, the ring's start, an item's joining
+// and the merge are the rest, about 3 us each.  4 drafts of 8 slots of 4,000 to 30,000 keys, 8 key
+// heads of 128 dims (480 MB): 81.7 us, 87 % of 6.8 TB/s.
 //
 // Q enters as it is (16 bits).  P enters as a pair hi + lo of the type, its rounding
 // residue with it: a bound memory leaves the second product free, and the outputs then
@@ -33,8 +41,12 @@ int tc_encode_queries(CUtensorMap* map, const void* q, int dtype, int head_dim, 
 namespace {
 
 constexpr int FR_KEYS = 64, FR_WARPS = 5, FR_THREADS = FR_WARPS * 32, FR_CONSUMERS = 128;
-constexpr int FR_MIN_UNITS = 4, CT_MIN_UNITS = 1, CT_SNAP = 12;  // fewest units of a CTA
-constexpr int FR_ITEM_COST = 2, CT_ITEM_COST = 2;
+// Fewest units of a CTA (few rows, 2, 4, 8: 2 slots 16.5, 16.5, 18.6 us; many rows, 1, 2, 4: 4 prompts 22.7, 24.5, 28.8).
+constexpr int FR_MIN_UNITS = 4, CT_MIN_UNITS = 1;
+// Items of many rows of at most so many units are not cut: a cut costs a tile's parts and their merge, about two units'
+// time.  All cut, 6, 12, 24: windows of 1000 keys 109, 109, 103, 103 us, 25 prompts of 128 dims 76.7, 73.6, 73.5, 73.6.  (Up to a
+// third of a share, however long: chunks of thousands of tokens 486 us instead of 447.)
+constexpr int CT_SNAP = 12;
 constexpr int FR_ROWS = 16, CT_UNIT_KEYS = 128;  // a tile of few rows
 constexpr int FR_SLOTS = 128;                   // slots whose plan every CTA makes for itself
 constexpr int RESIDUE_ROWS = 32;  // rows of a slot and key head up to which the weights' residues are kept
@@ -147,7 +159,7 @@ __device__ __forceinline__ ChunkStart plan_share(const ChunkArgs& a, FewSlots& f
     m.unit_first = f.first;
     m.tiles = (int)tiles;
     m.snap = 0;
-    const uint32_t sum = all * a.kv_heads, cost = sum + tiles * a.item_cost * a.kv_heads;
+    const uint32_t sum = all * a.kv_heads, cost = sum + tiles * ITEM_COST * a.kv_heads;
     m.ctas = min(a.ctas, max(1, (int)((sum + a.min_units - 1) / a.min_units)));
     if (lane == 0 && warp < 2) f.border[warp] = border<uint32_t>(a, m, cost, sum, cta + warp);
     __syncthreads();
@@ -469,7 +481,10 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 ? 3 : 2)
 // ---- merge ----
 // Grid (CTA of the kernel before, groups of four rows); a warp takes a row of the item that
 // begins in that CTA's share and goes on in the next ones': out = sum_c 2^(m_c - M) o_c / L,
-// L = sum_c 2^(m_c - M) l_c, M = max m_c, in the CTAs' order.
+// L = sum_c 2^(m_c - M) l_c, M = max m_c, in the CTAs' order, a batch of parts at a time.  Bound by
+// latency (the item, then its parts) where items are shared by many CTAs: about 3 us after a
+// step; one slot of 32,000 keys and 2 key heads, 125 parts an item, takes 18.5 us a call, 41 with
+// the maxima looked for first and four parts at a time.
 template <class T, int HD, int TR>
 __global__ void __launch_bounds__(128) chunk_merge_kernel(const ChunkArgs a) {
     const int cta = blockIdx.x, r = blockIdx.y * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
@@ -585,7 +600,7 @@ int chunk_plan(const mtp_chunk_attention_args* a, ChunkPlan* p) {
     const long long units = tiles * a->n_kv_heads * (a->max_keys / keys + 2);
     p->ctas = (int)std::max(1ll, std::min((long long)sms * per_sm, (units + p->min_units - 1) / p->min_units));
     // what a slot can cost at most, in a table of its width, has to fit the plan's 32 bits
-    const long long slot_cost = (long long)a->bt_stride * a->page_size / FR_KEYS + 1 + FR_ITEM_COST;
+    const long long slot_cost = (long long)a->bt_stride * a->page_size / FR_KEYS + 1 + ITEM_COST;
     p->plan_here = few && a->slots <= FR_SLOTS && a->slots * slot_cost * a->n_kv_heads * p->ctas < 1ll << 32;
     auto place = [&](size_t bytes) {
         const size_t at = p->need;
@@ -673,7 +688,6 @@ MTP_API int mtp_chunk_attention(const mtp_chunk_attention_args* a, void* workspa
         c.residues = p.residues;
         c.snap = few ? 0 : CT_SNAP;
         c.plan_here = p.plan_here;
-        c.item_cost = few ? FR_ITEM_COST : CT_ITEM_COST;
         c.q_vec = aligned16(a->q) && a->q_stride % 8 == 0;
         c.out_vec = aligned16(a->out) && a->out_stride % 8 == 0;
         c.scale_log2 = a->scale * 1.4426950408889634f;

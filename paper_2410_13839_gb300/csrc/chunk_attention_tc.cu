@@ -1,21 +1,32 @@
-// chunk_attention_tc.cu -- the kernel of mtp_chunk_attention for many rows per slot and key
-// head (prompts, chunks): tcgen05, one CTA per SM, shares of the unit stream (chunk.cuh) of
+// chunk_attention_tc.cu -- the kernel of mtp_chunk_attention for more than 16 rows per slot
+// and key head (prompts, chunks): tcgen05, shares of the unit stream (chunk.cuh) of 128 or
 // 256 packed rows by 128 keys.
 //
 //   S = Q K^T          128 x 64 fp32 in TMEM per tile of 128 rows and step of 64 keys
 //   P = 2^(c S - m)    a row per thread, written over S as 16-bit values (c = scale log2 e)
 //   O += P V           P read from TMEM, V as an MN-major operand, 128 x head_dim fp32 in TMEM
 //
-// A CTA has two tiles, A and B, of an item, each with four softmax warps and two places for S:
-// while a step's scores are in the hands of the softmax, the tensor cores make the next
-// step's and work for the other tile, so that the softmax warps go from step to step without
-// waiting.  (With one place of 128 keys a tile's softmax and MMAs took turns: 4500 cycles per
-// 128 keys, of which the MMAs fill 2048.  The price of N = 64 is its Q, read per 64 keys:
-// 45 cycles per MMA where 32 would do.)  A tile's MMAs are issued by a thread of its own: one
-// for both spent more time on its waits and branches (about 175 cycles for a barrier that is
-// complete) than the MMAs took.  The issuing threads run over the items of the share without
-// a stop, as does the ring of keys and values that the tenth warp fills with TMA copies, a
-// lane per page piece.  A tile skips the steps of which its rows see no key.
+// A tile has four softmax warps and two places for S: while a step's scores are in the hands of
+// the softmax, the tensor cores make the next step's, so that the softmax warps go from step
+// to step without waiting.  (With one place of 128 keys softmax and MMAs took turns: 4500
+// cycles per 128 keys of two tiles, of which the MMAs fill 2048.  The price of N = 64 is its
+// Q, read per 64 keys: 45 cycles per MMA where 32 would do.)  An SM has two tiles: those of one
+// CTA, which take turns at the tensor cores (128 dims), or two CTAs' (64 dims).
+// A tile's MMAs are issued by a thread of its own: one for both spent more time on its waits
+// and branches (126 cycles for a barrier that is complete) than the MMAs took.  The issuing
+// threads run over the items of the share without a stop, as do the rings of keys and of
+// values, which a warp each fills with TMA copies, a lane per page piece; the values' warp brings
+// Q too, by a tensor map, where the heads of a key head divide 128 and rows are aligned to 16 bytes
+// (25 prompts 47.2 us; brought by the softmax warps, as other rows are, 49.8).  A tile skips the
+// steps of which its rows see no key.
+//
+// Two chunks of 2000 to 4000 tokens after 6000 to 9000, 32 heads on 8 of 128 dims (648 GFLOP): 444 us,
+// 1460 TFLOP/s, of the measured peak (cuBLAS, 1922) three quarters; the MMAs of 45 and 64 cycles
+// fill about as much of the time.  64 dims, 16 heads (162 GFLOP): 228 us, 710 TFLOP/s: bound by
+// the softmax, whose 64 exponentials a row and step are as many as with 128 dims; a warp issues in
+// 44 % of the cycles and waits for results of its own the most.  25 prompts of 182 to 578 tokens,
+// 16 heads of 64: 47.2 us, of which the plan is 5, and items of 1 to 5 units with a start and
+// end each the rest.
 //
 // Code size matters: with everything unrolled and inlined (190 KB) the warps waited for
 // instructions, 10,000 cycles per 128 keys.

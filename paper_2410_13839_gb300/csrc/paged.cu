@@ -19,6 +19,10 @@
 // microsecond, one of a CTA a few dozen cycles, a second launch more than either).  The plan's
 // rows, of which a prompt batch has hundreds of thousands, are then written by the whole
 // GPU in a launch of their own.
+// Times of calls, one after another: plan of 32 slots, one token each, 2048 pages 6.3 us; of 1000
+// slots, 300,000 rows, 90,001 pages 24.8 us (5 MB written: the chain of steps, most of all the
+// taking of 10,000 pages by eight CTAs); reordering of 4 beams 10.4 us, of 96 beams 12.5 us with a
+// small cache's copies and 29 with those of 12 layers of 16 heads of 64.
 #include <climits>
 
 #include "serving.cuh"
@@ -329,7 +333,10 @@ __device__ __forceinline__ uint4 load8(const void* base, int64_t at) {
 }
 
 // A thread moves AP_UNROLL pieces of eight elements, all loaded before any is stored.
-// Bound by memory: each element is read once and written once.
+// Bound by memory: each element is read once and written once.  14592 rows of 16 heads of 64, bf16:
+// 120 MB in 17.4 us, 6.9 TB/s (20.9 us a call, one after another); a step's 128 rows are latency,
+// 5 us.  VECTOR: rows on 16-byte boundaries are read 16 bytes at a time; the same rows again and
+// again 18.6 us a call, element by element 23.1 (from fp32 29.4 and 32.9).
 template <class DST, int SRC, bool VECTOR>
 __global__ void __launch_bounds__(AP_THREADS) cache_append_kernel(const AppendArgs p) {
     const mtp_cache_append_args& a = p.a;
@@ -510,7 +517,9 @@ constexpr int CP_THREADS = 256, CP_UNROLL = 4;
 
 // The filled rows of every copied page: for each (layer, keys | values, head) one run of
 // tokens * head_dim elements.  A warp takes a run; CP_UNROLL loads are in flight per lane.
-// Bound by memory: each row is read once and written once.
+// Bound by memory: each row is read once and written once; with few copies by latency (the list, then
+// the rows).  96 beams' copies, 12 layers of 16 heads of 64, 150 MB read and written: 29 us a call,
+// 12 of them the tables'; 22 at 6.8 TB/s.
 __global__ void __launch_bounds__(CP_THREADS) page_copy_kernel(const __grid_constant__ ReorderArgs p, int runs) {
     pdl_wait();
     const int n = *p.count, lane = threadIdx.x & 31;
