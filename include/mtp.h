@@ -486,7 +486,10 @@ MTP_API int mtp_gemm_bf16x2(const void* w, const void* a_hi, const void* a_lo, f
  * allocated or copied to the host, and all may be captured in a CUDA graph.  Sizes,
  * types and pointers are checked on the host (MTP_ERR_INVALID, nothing is queued);
  * what stands in device memory is checked on the device, and the outcome is in
- * out_status.  The caller's buffers are on the current device. */
+ * out_status.  The caller's buffers are on the current device.  The kernels are launched
+ * programmatically: they may be placed while the kernel before them in the stream ends, and
+ * wait for all that it wrote.  A kernel of the caller's that is launched so behind them has to
+ * wait likewise (griddepcontrol.wait); any other launch does. */
 
 /* Pages, block tables and row plan of the tokens that each slot gets in a step.
  * Slot s of length kv_lens[s] gets new_lens[s] >= 0 tokens: the pages that positions

@@ -156,7 +156,7 @@ __device__ __forceinline__ void best_of(Best& b, int k, unsigned long long most,
 struct F32T {
     using elem = float;
     static constexpr int PER = 4;
-    static __device__ __forceinline__ float one(const void* p, int64_t i) { return __ldg(static_cast<const float*>(p) + i); }
+    static __device__ __forceinline__ float one(const void* p, int64_t i) { return *(static_cast<const float*>(p) + i); }
     static __device__ __forceinline__ void unpack(uint4 v, float* x) {
         x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
     }
@@ -166,7 +166,7 @@ struct Half {
     using elem = uint16_t;
     static constexpr int PER = 8;
     static __device__ __forceinline__ float one(const void* p, int64_t i) {
-        return T::to_float(__ldg(static_cast<const uint16_t*>(p) + i));
+        return T::to_float(*(static_cast<const uint16_t*>(p) + i));
     }
     static __device__ __forceinline__ void unpack(uint4 v, float* x) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -194,7 +194,7 @@ __device__ __forceinline__ int for_row(const void* base, int64_t first, int n, i
         uint4 raw[UNROLL];
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u)
-            if (i0 + u * 32 < vecs) raw[u] = __ldg(v + i0 + u * 32);
+            if (i0 + u * 32 < vecs) raw[u] = *(v + i0 + u * 32);
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             const int i = i0 + u * 32;
@@ -231,6 +231,7 @@ __global__ void __launch_bounds__(LSE_THREADS) row_lse_kernel(const void* logits
     __shared__ float2 part[LSE_THREADS / 32];
     const int row = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_launch_dependents();
+    pdl_wait();
     float m = -INFINITY, s = 0.f;
     for_row<T, 4>(logits, row * stride, vocab, warp, LSE_THREADS / 32, [&](int, float x) {
         if (x > m) {
@@ -260,6 +261,7 @@ __global__ void __launch_bounds__(BS_THREADS) beam_select_kernel(const __grid_co
     const mtp_beam_select_args& a = p.a;
     const int item = blockIdx.y, seg = blockIdx.x, W = a.beams, V = a.vocab, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int first = seg * p.seg_len, n = min(p.seg_len, W * V - first);
+    pdl_launch_dependents();
     pdl_wait();
     if (tid < W) {
         s_beam[tid] = a.scores[item * W + tid];
@@ -436,25 +438,15 @@ cudaError_t launch_select(const mtp_beam_select_args* a, const SelectPlan& pl, c
         float* lse = a->out_lse ? a->out_lse : reinterpret_cast<float*>(ws + pl.count_bytes + pl.key_bytes);
         p.lse = lse;
         p.a.out_lse = nullptr;  // written already
-        row_lse_kernel<T><<<a->batch * a->beams, LSE_THREADS, 0, s>>>(a->logits, a->logits_stride, a->vocab, lse);
-        const cudaError_t e = cudaGetLastError();
+        const cudaError_t e = launch_ex(row_lse_kernel<T>, dim3(a->batch * a->beams), LSE_THREADS, 0, s, 1, a->logits,
+                                        a->logits_stride, (int)a->vocab, lse);
         if (e != cudaSuccess) return e;
     }
     const size_t smem = pl.lse_here ? (size_t)pl.seg_len * sizeof(float) : 0;
     const auto kern = pl.lse_here ? beam_select_kernel<T, true> : beam_select_kernel<T, false>;
     const cudaError_t e = pl.lse_here ? ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem) : cudaSuccess;
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(pl.segments, a->batch);
-    cfg.blockDim = dim3(BS_THREADS);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = pl.lse_before ? 1 : 0;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, p);
+    return launch_ex(kern, dim3(pl.segments, a->batch), BS_THREADS, smem, s, 1, p);
 }
 
 }  // namespace

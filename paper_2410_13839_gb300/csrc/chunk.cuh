@@ -240,19 +240,4 @@ cudaError_t launch_chunk_plan(const ChunkArgs& a, int tile_rows, cudaStream_t s)
 cudaError_t launch_chunk_tc(const ChunkArgs& a, const CUtensorMap& map, const CUtensorMap& q_map, int head_dim, int dtype,
                             cudaStream_t s);
 
-template <class... P>
-cudaError_t launch_ex(void (*kern)(P...), dim3 grid, int threads, size_t smem, bool pdl, cudaStream_t s, P... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = pdl ? 1 : 0;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, args...);
-}
-
 }  // namespace mtp

@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 ? 3 : 2)
     }
     __syncthreads();
     pdl_launch_dependents();
-    pdl_wait();  // the plan
+    pdl_wait();  // the plan, or the kernels before this call
     const ChunkStart start = a.plan_here ? plan_share(a, few) : a.start[cta];
     const int units = start.units;
     if (units == 0) return;
@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 ? 3 : 2)
         bool ok = true;
         // pages [base, base + 32) of the slot, one per lane, and the 32 after them
         auto lookup = [&](int first) {
-            return first + lane < a.bt_stride ? __ldg(a.block_table + (size_t)w.t.slot * a.bt_stride + first + lane) : -1;
+            return first + lane < a.bt_stride ? *(a.block_table + (size_t)w.t.slot * a.bt_stride + first + lane) : -1;
         };
         auto enter = [&]() {
             base = (w.key0<FR_KEYS>() + k * FR_KEYS) >> a.page_shift & ~31;
@@ -281,11 +281,11 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 ? 3 : 2)
                 const int token = chunk_token(a, p);
                 const uint16_t* src = a.q + (t.row0 + token) * a.q_stride + (w.head * a.group + p - token * a.group) * HD + c * 8;
                 if (a.q_vec) {
-                    v = __ldg(reinterpret_cast<const uint4*>(src));
+                    v = *reinterpret_cast<const uint4*>(src);
                 } else {
                     uint32_t w[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = (uint32_t)__ldg(src + 2 * e) | (uint32_t)__ldg(src + 2 * e + 1) << 16;
+                    for (int e = 0; e < 4; ++e) w[e] = (uint32_t)*(src + 2 * e) | (uint32_t)*(src + 2 * e + 1) << 16;
                     v = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
@@ -489,6 +489,9 @@ template <class T, int HD, int TR>
 __global__ void __launch_bounds__(128) chunk_merge_kernel(const ChunkArgs a) {
     const int cta = blockIdx.x, r = blockIdx.y * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     constexpr int PER = HD / 32, BATCH = TR == FR_ROWS ? 8 : 4;  // (tiles of many rows are shared by few CTAs)
+    // (After many rows not: the next call's plan, a CTA of 1024 threads, then starts in the merge's way.  25 prompts, one call
+    // after another: 43.7 us, 47.3 with it.)
+    if (TR == FR_ROWS) pdl_launch_dependents();
     pdl_wait();
     const int* d = a.desc + cta * CH_DESC;
     const int more = d[0];
@@ -553,8 +556,8 @@ template <class T, int HD>
 cudaError_t merge_hd(const ChunkArgs& a, int tile_rows, cudaStream_t s) {
     const dim3 grid(a.ctas, tile_rows / 4);
     switch (tile_rows) {
-        case FR_ROWS: return launch_ex(chunk_merge_kernel<T, HD, FR_ROWS>, grid, 128, 0, true, s, a);
-        default: return launch_ex(chunk_merge_kernel<T, HD, 128 * chunk_tc_tiles(HD)>, grid, 128, 0, true, s, a);
+        case FR_ROWS: return launch_ex(chunk_merge_kernel<T, HD, FR_ROWS>, grid, 128, 0, s, 1, a);
+        default: return launch_ex(chunk_merge_kernel<T, HD, 128 * chunk_tc_tiles(HD)>, grid, 128, 0, s, 1, a);
     }
 }
 
@@ -621,7 +624,7 @@ cudaError_t launch_rows(const ChunkArgs& a, const CUtensorMap& map, cudaStream_t
     const auto kern = chunk_rows_kernel<T, HD>;
     const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem, true);
     if (e != cudaSuccess) return e;
-    return launch_ex(kern, dim3(a.ctas), FR_THREADS, smem, !a.plan_here, s, a, map);
+    return launch_ex(kern, dim3(a.ctas), FR_THREADS, smem, s, 1, a, map);
 }
 template <class T>
 cudaError_t launch_kernels(const ChunkArgs& a, const CUtensorMap& map, const CUtensorMap& q_map, int head_dim, int dtype, int tile_rows, cudaStream_t s) {

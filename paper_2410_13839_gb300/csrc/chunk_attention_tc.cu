@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
             // pages [base, base + 32) of the slot, one per lane, and the 32 after them
             int base = 0, pages = 0, ahead = 0, key_first = 0, hi = 0, lo = 0, last = 0, head_block = 0;
             const int* table = nullptr;
-            auto lookup = [&](int first) { return first + lane < a.bt_stride ? __ldg(table + first + lane) : -1; };
+            auto lookup = [&](int first) { return first + lane < a.bt_stride ? *(table + first + lane) : -1; };
             int queries[TILES] = {};  // tiles of Q copied so far
             auto enter = [&]() {  // an item's first step
                 if (kv && a.q_tma)  // the values' warp, which is behind the keys', copies Q too
@@ -420,7 +420,7 @@ __global__ void __launch_bounds__(CtLayout<HD>::THREADS, 3 - CtLayout<HD>::TILES
                         uint32_t v[4] = {0u, 0u, 0u, 0u};
                         if (live)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) v[e] = (uint32_t)__ldg(src + 2 * e) | (uint32_t)__ldg(src + 2 * e + 1) << 16;
+                            for (int e = 0; e < 4; ++e) v[e] = (uint32_t)*(src + 2 * e) | (uint32_t)*(src + 2 * e + 1) << 16;
                         *reinterpret_cast<uint4*>(dst) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
                 }
@@ -674,7 +674,7 @@ template <class T, int HD, bool RES>
 cudaError_t launch_tc(const ChunkArgs& a, const CUtensorMap& map, const CUtensorMap& q_map, cudaStream_t s) {
     const auto kern = chunk_tc_kernel<T, HD, RES>;
     const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), CtLayout<HD>::BYTES);
-    return e == cudaSuccess ? launch_ex(kern, dim3(a.ctas), CtLayout<HD>::THREADS, CtLayout<HD>::BYTES, true, s, a, map, q_map) : e;
+    return e == cudaSuccess ? launch_ex(kern, dim3(a.ctas), CtLayout<HD>::THREADS, CtLayout<HD>::BYTES, s, 1, a, map, q_map) : e;
 }
 
 }  // namespace

@@ -72,6 +72,7 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan_kernel(const __grid_con
     uint32_t* unit_first = slot_first + a.slots + 1;                      // [tiles + 1]
     const int tid = threadIdx.x;
     pdl_launch_dependents();
+    pdl_wait();
     uint32_t base = 0, sum;  // (tiles: the kept rows of all slots lie in the buffers; a caller's wrong row starts: cut below)
     for (int s0 = 0; s0 < a.slots; s0 += PL_THREADS) {
         const int s = s0 + tid;
@@ -128,7 +129,7 @@ cudaError_t launch(const ChunkArgs& a, cudaStream_t s) {
     const size_t smem = plan_smem(a);
     const auto kern = chunk_plan_kernel<TR, KT>;
     const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem);
-    return e == cudaSuccess ? launch_ex(kern, dim3(1), PL_THREADS, smem, false, s, a) : e;
+    return e == cudaSuccess ? launch_ex(kern, dim3(1), PL_THREADS, smem, s, 1, a) : e;
 }
 
 }  // namespace

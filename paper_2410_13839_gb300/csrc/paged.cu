@@ -198,6 +198,7 @@ __global__ void __launch_bounds__(PG_THREADS, 1) page_plan_kernel(const __grid_c
     int* lens = pages_before + slots + 1;         // [slots]
     uint32_t* bits = reinterpret_cast<uint32_t*>(lens + slots);
     pdl_launch_dependents();
+    pdl_wait();
 
     // the requests: every CTA makes the whole prefix sums
     uint32_t rows32 = 0, want = 0, mine = 0;
@@ -278,6 +279,7 @@ __global__ void __launch_bounds__(RW_THREADS) plan_rows_kernel(const __grid_cons
     const mtp_page_plan_args& a = p.a;
     const int slots = a.slots, first = blockIdx.x * RW_ROWS;
     int *before = pg_sm, *lens = pg_sm + slots + 1;
+    pdl_launch_dependents();
     pdl_wait();
     const int rows = a.out_status[1];
     if (first < rows) {
@@ -314,20 +316,20 @@ __device__ __forceinline__ uint4 load8(const void* base, int64_t at) {
         const float* p = static_cast<const float*>(base) + at;
         float x[8];
         if constexpr (VECTOR) {
-            const float4 u = __ldg(reinterpret_cast<const float4*>(p)), v = __ldg(reinterpret_cast<const float4*>(p) + 1);
+            const float4 u = *reinterpret_cast<const float4*>(p), v = *(reinterpret_cast<const float4*>(p) + 1);
             x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
             x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = __ldg(p + i);
+            for (int i = 0; i < 8; ++i) x[i] = *(p + i);
         }
         return make_uint4(DST::pack(x[0], x[1]), DST::pack(x[2], x[3]), DST::pack(x[4], x[5]), DST::pack(x[6], x[7]));
     } else {  // the pool's own type: copied bit by bit
         const uint16_t* p = static_cast<const uint16_t*>(base) + at;
-        if constexpr (VECTOR) return __ldg(reinterpret_cast<const uint4*>(p));
+        if constexpr (VECTOR) return *reinterpret_cast<const uint4*>(p);
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = (uint32_t)__ldg(p + 2 * i) | (uint32_t)__ldg(p + 2 * i + 1) << 16;
+        for (int i = 0; i < 4; ++i) w[i] = (uint32_t)*(p + 2 * i) | (uint32_t)*(p + 2 * i + 1) << 16;
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
@@ -338,19 +340,21 @@ __device__ __forceinline__ uint4 load8(const void* base, int64_t at) {
 // 5 us.  VECTOR: rows on 16-byte boundaries are read 16 bytes at a time; the same rows again and
 // again 18.6 us a call, element by element 23.1 (from fp32 29.4 and 32.9).
 template <class DST, int SRC, bool VECTOR>
-__global__ void __launch_bounds__(AP_THREADS) cache_append_kernel(const AppendArgs p) {
+__global__ void __launch_bounds__(AP_THREADS) cache_append_kernel(const __grid_constant__ AppendArgs p) {
     const mtp_cache_append_args& a = p.a;
     const unsigned first = blockIdx.x * (AP_THREADS * AP_UNROLL) + threadIdx.x, hv = a.head_dim / 8;
     uint16_t* pool = static_cast<uint16_t*>(a.kv_pool);
     uint4 x[AP_UNROLL];
     uint16_t* to[AP_UNROLL];
+    pdl_launch_dependents();
+    pdl_wait();
 #pragma unroll
     for (int u = 0; u < AP_UNROLL; ++u) {
         const unsigned i = first + u * AP_THREADS;
         to[u] = nullptr;
         if (i >= p.total) continue;
         const unsigned row = i / (2 * p.vecs), rest = i - row * 2 * p.vecs, kv = rest >= p.vecs, vec = rest - kv * p.vecs;
-        const int64_t slot = __ldg(a.slot_map + row), page = slot >> p.shift;
+        const int64_t slot = *(a.slot_map + row), page = slot >> p.shift;
         if (slot < 0 || page >= a.n_pages) continue;
         const unsigned head = vec / hv, c = vec - head * hv;
         const int64_t block = ((page * a.layers + a.layer) * 2 + kv) * a.n_kv_heads + head;
@@ -365,14 +369,10 @@ __global__ void __launch_bounds__(AP_THREADS) cache_append_kernel(const AppendAr
 template <class DST>
 cudaError_t launch_append(const AppendArgs& p, bool vector, cudaStream_t s) {
     const unsigned grid = (p.total + AP_THREADS * AP_UNROLL - 1) / (AP_THREADS * AP_UNROLL);
-    if (p.a.src_dtype == MTP_F32) {
-        if (vector) cache_append_kernel<DST, MTP_F32, true><<<grid, AP_THREADS, 0, s>>>(p);
-        else cache_append_kernel<DST, MTP_F32, false><<<grid, AP_THREADS, 0, s>>>(p);
-    } else {
-        if (vector) cache_append_kernel<DST, MTP_BF16, true><<<grid, AP_THREADS, 0, s>>>(p);
-        else cache_append_kernel<DST, MTP_BF16, false><<<grid, AP_THREADS, 0, s>>>(p);
-    }
-    return cudaGetLastError();
+    const auto kern = p.a.src_dtype == MTP_F32 ? vector ? cache_append_kernel<DST, MTP_F32, true> : cache_append_kernel<DST, MTP_F32, false>
+                      : vector                 ? cache_append_kernel<DST, MTP_BF16, true>
+                                               : cache_append_kernel<DST, MTP_BF16, false>;
+    return launch_ex(kern, dim3(grid), AP_THREADS, 0, s, 1, p);
 }
 
 // ---- reorder ----
@@ -406,6 +406,7 @@ __global__ void __launch_bounds__(PG_THREADS, 1) beam_reorder_kernel(const __gri
     const int part_mask = (1 << p.shift) - 1;
 
     pdl_launch_dependents();
+    pdl_wait();
     uint32_t want = 0;
     bool bad = false;
     if (tid == 0) s_freed = 0;
@@ -521,6 +522,7 @@ constexpr int CP_THREADS = 256, CP_UNROLL = 4;
 // the rows).  96 beams' copies, 12 layers of 16 heads of 64, 150 MB read and written: 29 us a call,
 // 12 of them the tables'; 22 at 6.8 TB/s.
 __global__ void __launch_bounds__(CP_THREADS) page_copy_kernel(const __grid_constant__ ReorderArgs p, int runs) {
+    pdl_launch_dependents();
     pdl_wait();
     const int n = *p.count, lane = threadIdx.x & 31;
     const long long total = (long long)n * runs, stride = (long long)gridDim.x * (CP_THREADS / 32);
@@ -554,26 +556,11 @@ int check_pool(const char* what, int n_pages, int layers, int layer, int n_kv_he
     return MTP_OK;
 }
 
-// Enqueue a kernel; clusters of `cluster` CTAs; `pdl`: it may start while the kernel before it runs.
+// Enqueue a kernel, clusters of `cluster` CTAs.
 template <class... P>
-cudaError_t launch(void (*kern)(P...), int grid, int threads, size_t smem, int cluster, bool pdl, cudaStream_t s, P... args) {
-    cudaError_t e = smem > 48 * 1024 ? ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem) : cudaSuccess;
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = pdl ? 1 : 0;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cluster;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kern, args...);
+cudaError_t launch(void (*kern)(P...), int grid, int threads, size_t smem, int cluster, cudaStream_t s, P... args) {
+    const cudaError_t e = smem > 48 * 1024 ? ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem) : cudaSuccess;
+    return e == cudaSuccess ? launch_ex(kern, dim3(grid), threads, smem, s, cluster, args...) : e;
 }
 
 size_t reorder_workspace(int rows) { return 16 + (size_t)rows * sizeof(int4); }
@@ -599,10 +586,10 @@ MTP_API int mtp_page_plan(const mtp_page_plan_args* a, void* cuda_stream) {
         const PlanArgs p{*a, log2_of(a->page_size), a->max_rows <= PG_ONE_ROWS};
         const size_t smem = (size_t)(3 * a->slots + 2 + 2 * free_words(a->n_pages, one ? 1 : PG_CLUSTER)) * 4;
         const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-        cudaError_t e = one ? launch(page_plan_kernel<1>, 1, PG_THREADS, smem, 1, false, s, p)
-                            : launch(page_plan_kernel<PG_CLUSTER>, PG_CLUSTER, PG_THREADS, smem, PG_CLUSTER, false, s, p);
+        cudaError_t e = one ? launch(page_plan_kernel<1>, 1, PG_THREADS, smem, 1, s, p)
+                            : launch(page_plan_kernel<PG_CLUSTER>, PG_CLUSTER, PG_THREADS, smem, PG_CLUSTER, s, p);
         if (e == cudaSuccess && !p.rows_here)
-            e = launch(plan_rows_kernel, (a->max_rows + RW_ROWS - 1) / RW_ROWS, RW_THREADS, (size_t)(2 * a->slots + 1) * 4, 1, true, s, p);
+            e = launch(plan_rows_kernel, (a->max_rows + RW_ROWS - 1) / RW_ROWS, RW_THREADS, (size_t)(2 * a->slots + 1) * 4, 1, s, p);
         return cuda_status(e, "page_plan");
     });
 }
@@ -670,14 +657,14 @@ MTP_API int mtp_beam_reorder(const mtp_beam_reorder_args* a, void* workspace, si
                             reinterpret_cast<int4*>(static_cast<char*>(workspace) + 16)};
         const size_t smem = (size_t)(3 * rows + 1 + 2 * free_words(a->n_pages, one ? 1 : PG_CLUSTER)) * 4;
         const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-        cudaError_t e = one ? launch(beam_reorder_kernel<1>, 1, PG_THREADS, smem, 1, false, s, p)
-                            : launch(beam_reorder_kernel<PG_CLUSTER>, PG_CLUSTER, PG_THREADS, smem, PG_CLUSTER, false, s, p);
+        cudaError_t e = one ? launch(beam_reorder_kernel<1>, 1, PG_THREADS, smem, 1, s, p)
+                            : launch(beam_reorder_kernel<PG_CLUSTER>, PG_CLUSTER, PG_THREADS, smem, PG_CLUSTER, s, p);
         if (e == cudaSuccess && a->beams > 1) {  // (one beam has nothing to copy)
             int dev = 0, sms = 0;
             e = cudaGetDevice(&dev);
             if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
             if (e == cudaSuccess)
-                e = launch(page_copy_kernel, sms * 8, CP_THREADS, 0, 1, true, s, p, a->layers * 2 * a->n_kv_heads);
+                e = launch(page_copy_kernel, sms * 8, CP_THREADS, 0, 1, s, p, a->layers * 2 * a->n_kv_heads);
         }
         return cuda_status(e, "beam_reorder");
     });

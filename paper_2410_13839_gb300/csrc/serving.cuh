@@ -39,6 +39,28 @@ int guarded(F body) noexcept {
     }
 }
 
+// Enqueue a kernel, in clusters of `cluster` CTAs.  All of these operators' kernels are launched programmatically:
+// they may be placed while the kernel before them in the stream ends, and touch global memory only
+// after pdl_wait, by plain loads (one that says its data never change could be moved before it).
+template <class... P>
+cudaError_t launch_ex(void (*kern)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, int cluster, P... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 inline bool page_size_ok(int p) { return p == 16 || p == 32 || p == 64 || p == 128; }
 
