@@ -19,10 +19,10 @@
 // microsecond, one of a CTA a few dozen cycles, a second launch more than either).  The plan's
 // rows, of which a prompt batch has hundreds of thousands, are then written by the whole
 // GPU in a launch of their own.
-// Times of calls, one after another: plan of 32 slots, one token each, 2048 pages 6.3 us; of 1000
-// slots, 300,000 rows, 90,001 pages 24.8 us (5 MB written: the chain of steps, most of all the
-// taking of 10,000 pages by eight CTAs); reordering of 4 beams 10.4 us, of 96 beams 12.5 us with a
-// small cache's copies and 29 with those of 12 layers of 16 heads of 64.
+// Times of calls, one after another: plan of 32 slots, one token each, 2048 pages 3.8 us; of 1000
+// slots, 300,000 rows, 90,001 pages 21.3 us (5 MB written: the chain of steps, most of all the
+// taking of 10,000 pages by eight CTAs); reordering of 4 beams 8.2 us, of 96 beams with the copies
+// of 12 layers of 16 heads of 64 27 us.
 #include <climits>
 
 #include "serving.cuh"
@@ -64,6 +64,38 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* part, uint3
     const uint32_t mine = part[lane];
     sum = __reduce_add_sync(FULL_MASK, mine);
     return __reduce_add_sync(FULL_MASK, lane < warp ? mine : 0) + y - x;
+}
+
+// The same of two numbers, and the sum alone of a third, between the same barriers.
+struct ScanParts {
+    uint32_t x[PG_WARPS], y[PG_WARPS], z[PG_WARPS];
+};
+__device__ __forceinline__ void block_scan3(uint32_t& x, uint32_t& y, uint32_t z, ScanParts& part, uint32_t& sum_x, uint32_t& sum_y,
+                                            uint32_t& sum_z) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t u = x, v = y;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t p = __shfl_up_sync(FULL_MASK, u, o), q = __shfl_up_sync(FULL_MASK, v, o);
+        if (lane >= o) {
+            u += p;
+            v += q;
+        }
+    }
+    z = __reduce_add_sync(FULL_MASK, z);
+    __syncthreads();
+    if (lane == 31) {
+        part.x[warp] = u;
+        part.y[warp] = v;
+        part.z[warp] = z;
+    }
+    __syncthreads();
+    const uint32_t p = part.x[lane], q = part.y[lane];
+    sum_x = __reduce_add_sync(FULL_MASK, p);
+    sum_y = __reduce_add_sync(FULL_MASK, q);
+    sum_z = __reduce_add_sync(FULL_MASK, part.z[lane]);
+    x = __reduce_add_sync(FULL_MASK, lane < warp ? p : 0) + u - x;
+    y = __reduce_add_sync(FULL_MASK, lane < warp ? q : 0) + v - y;
 }
 
 // Reads this CTA's part of the counts once (and copies it, where they go to another
@@ -128,15 +160,19 @@ __device__ __forceinline__ int ld_dsmem_int(const int* p, int rank) {
     asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(dsmem_addr(p, rank)) : "memory");
     return v;
 }
-// A barrier of the CTAs that work together, after which they see each other's writes.
+// A barrier of the CTAs that work together, after which they see each other's writes; with its two halves apart.
+template <int CTAS>
+__device__ __forceinline__ void team_arrive() {
+    if constexpr (CTAS > 1) cluster_arrive_release();
+}
+template <int CTAS>
+__device__ __forceinline__ void team_wait() {
+    if constexpr (CTAS == 1) __syncthreads(); else cluster_wait();
+}
 template <int CTAS>
 __device__ __forceinline__ void team_barrier() {
-    if constexpr (CTAS == 1) {
-        __syncthreads();
-    } else {
-        cluster_arrive_release();
-        cluster_wait();
-    }
+    team_arrive<CTAS>();
+    team_wait<CTAS>();
 }
 // Sum of a shared-memory word of every CTA; *before: of those below `rank`.
 template <int CTAS>
@@ -190,6 +226,7 @@ template <int CTAS>
 __global__ void __launch_bounds__(PG_THREADS, 1) page_plan_kernel(const __grid_constant__ PlanArgs p) {
     extern __shared__ int pg_sm[];
     __shared__ uint32_t part[PG_WARPS];
+    __shared__ ScanParts parts;
     __shared__ int s_free;
     const mtp_page_plan_args& a = p.a;
     const int tid = threadIdx.x, rank = CTAS == 1 ? 0 : blockIdx.x, slots = a.slots;
@@ -200,14 +237,22 @@ __global__ void __launch_bounds__(PG_THREADS, 1) page_plan_kernel(const __grid_c
     pdl_launch_dependents();
     pdl_wait();
 
+    // the first requests are on their way while the free pages are looked for, and CTAs' totals while the requests are summed
+    int len = tid < slots ? a.kv_lens[tid] : 0, add = tid < slots ? a.new_lens[tid] : 0;
+    const FreeBits f = find_free<CTAS>(a.page_refs, a.out_page_refs, a.n_pages, rank, bits, part, &s_free);
+    team_arrive<CTAS>();
+
     // the requests: every CTA makes the whole prefix sums
-    uint32_t rows32 = 0, want = 0, mine = 0;
+    uint32_t rows = 0, want = 0;
     bool bad = false;
     for (int s0 = 0; s0 < slots; s0 += PG_THREADS) {
         const int s = s0 + tid;
-        uint32_t x = 0, y = 0, sx, sy;
+        uint32_t x = 0, y = 0, sx, sy, thousands;
         if (s < slots) {
-            const int len = a.kv_lens[s], add = a.new_lens[s];
+            if (s0 > 0) {
+                len = a.kv_lens[s];
+                add = a.new_lens[s];
+            }
             const bool wrong = len < 0 || add < 0 || add > a.max_rows || (long long)len + add > (long long)a.bt_stride << p.shift;
             bad |= wrong;
             lens[s] = len;
@@ -216,30 +261,23 @@ __global__ void __launch_bounds__(PG_THREADS, 1) page_plan_kernel(const __grid_c
                 y = pages_of(len + add, p.shift) - pages_of(len, p.shift);
             }
         }
-        mine += x;
-        x = block_scan(x, part, sx);
-        y = block_scan(y, part, sy);
+        block_scan3(x, y, x >> 12, parts, sx, sy, thousands);
         if (s < slots) {  // (more rows than 32 bits hold: nothing of this is used)
-            rows_before[s] = (int)(rows32 + x);
+            rows_before[s] = (int)(rows + x);
             pages_before[s] = (int)(want + y);
         }
-        rows32 += sx;
+        // 1024 requests of 2^24 rows at most: where their multiples of 4096 alone are more than 2^24, their sum may have
+        // passed 32 bits, and is too much in any case
+        bad |= thousands > (uint32_t)PG_MAX_ROWS >> 12 || rows + sx > (uint32_t)a.max_rows;
+        rows += sx;
         want += sy;
     }
-    // 8192 requests of 2^24 rows at most: the low and the high halves of the threads' sums, apart
-    uint32_t low, high;
-    block_scan(mine & 0xffff, part, low);
-    block_scan(mine >> 16, part, high);
-    long long rows = ((long long)high << 16) + low;
     if (tid == 0) {
         rows_before[slots] = (int)rows;
         pages_before[slots] = (int)want;
     }
-    int code = __syncthreads_or(bad) || rows > a.max_rows ? MTP_ERR_INVALID : MTP_OK;
-
-    // the free pages
-    const FreeBits f = find_free<CTAS>(a.page_refs, a.out_page_refs, a.n_pages, rank, bits, part, &s_free);
-    team_barrier<CTAS>();
+    int code = __syncthreads_or(bad) ? MTP_ERR_INVALID : MTP_OK;
+    team_wait<CTAS>();
     long long base;
     const long long free_all = team_sum<CTAS>(&s_free, rank, &base);
     if (code == MTP_OK && want > free_all) code = MTP_ERR_NO_PAGES;
