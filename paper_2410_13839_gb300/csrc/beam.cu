@@ -91,6 +91,7 @@ struct Best {
 // visible afterwards.
 template <class EACH>
 __device__ __forceinline__ void best_of(Best& b, int k, unsigned long long most, EACH each) {
+    static_assert(BS_THREADS == 4 * GROUPS, "four threads to a group");
     const int tid = threadIdx.x;
     b.thread_max[tid] = most;
     if (tid == 0) {
@@ -99,19 +100,18 @@ __device__ __forceinline__ void best_of(Best& b, int k, unsigned long long most,
     }
     if (tid < BS_MAX_K) b.best[tid] = 0;
     __syncthreads();
-    unsigned long long mine = 0;
-    if (tid < GROUPS) {
-#pragma unroll
-        for (int u = 0; u < BS_THREADS / GROUPS; ++u) mine = max(mine, b.thread_max[tid + u * GROUPS]);
-        b.group_max[tid] = mine;
-    }
+    // (threads far apart: a short segment's keys are with the first warps)
+    if (tid < GROUPS)
+        b.group_max[tid] = max(max(b.thread_max[tid], b.thread_max[tid + GROUPS]),
+                               max(b.thread_max[tid + 2 * GROUPS], b.thread_max[tid + 3 * GROUPS]));
     __syncthreads();
-    if (tid < GROUPS) {
-        int larger = 0;
-#pragma unroll 16
-        for (int i = 0; i < GROUPS; ++i) larger += b.group_max[i] > mine;
-        if (larger == k - 1 && mine) b.bound = mine;
-    }
+    const unsigned long long mine = b.group_max[tid >> 2];
+    int larger = 0;  // a quarter of the groups to a thread
+#pragma unroll
+    for (int i = tid & 3; i < GROUPS; i += 4) larger += b.group_max[i] > mine;
+    larger += __shfl_xor_sync(FULL_MASK, larger, 1);
+    larger += __shfl_xor_sync(FULL_MASK, larger, 2);
+    if ((tid & 3) == 0 && larger == k - 1 && mine) b.bound = mine;
     __syncthreads();
     const unsigned long long bound = b.bound;
     if (most >= bound)
@@ -263,12 +263,23 @@ __global__ void __launch_bounds__(BS_THREADS) beam_select_kernel(const __grid_co
     const int first = seg * p.seg_len, n = min(p.seg_len, W * V - first);
     pdl_launch_dependents();
     pdl_wait();
+    // (held logits are on their way while the beams' scores are)
+    float beam_score = 0.f, beam_lse = 0.f;
+    int beam_done = 0;
     if (tid < W) {
-        s_beam[tid] = a.scores[item * W + tid];
-        s_done[tid] = a.done ? a.done[item * W + tid] : 0;
-        if (!HOLD) s_lse[tid] = p.lse[item * W + tid];
+        beam_score = a.scores[item * W + tid];
+        beam_done = a.done ? a.done[item * W + tid] : 0;
+        if (!HOLD) beam_lse = p.lse[item * W + tid];
     }
-    __syncthreads();
+    auto beams_there = [&]() {
+        if (tid < W) {
+            s_beam[tid] = beam_score;
+            s_done[tid] = beam_done;
+            if (!HOLD) s_lse[tid] = beam_lse;
+        }
+        __syncthreads();
+    };
+    if constexpr (!HOLD) beams_there();
     // use(beam, column, logit) for this thread's logits of the segment; the beams' stretches go round the warps, so
     // that short rows are on their way together.  A finished beam has its end alone.
     auto logits = [&](auto use) {
@@ -287,7 +298,7 @@ __global__ void __launch_bounds__(BS_THREADS) beam_select_kernel(const __grid_co
     };
     if constexpr (HOLD) {  // a warp per beam: its log-sum-exp, then its scores
         logits([&](int w, int c, float x) { bs_score[w * V + c] = x; });
-        __syncthreads();
+        beams_there();
         for (int w = warp; w < W; w += BS_WARPS) {
             float* x = bs_score + w * V;
             float m = -INFINITY, s = 0.f;
