@@ -9,7 +9,8 @@
 // complement of its number: keys are distinct, so the k largest are one set, whatever
 // order they are looked at in, and no tie is a special case.
 //
-// The best keys of a CTA (best_of): a thread goes through its own keys once for their maximum;
+// The best keys of a CTA (best_of): a thread goes through its own keys once for their maximum (of 16
+// bytes of logits the largest score, then its place);
 // 128 groups of threads give a maximum each; the k-th largest of these is a bound that at least
 // k keys reach, and hardly more do (for k = 8 about 8.3 are expected, for k = 64 about 89).  The
 // few threads with a key that reaches it go through theirs again, and what they find is ranked
@@ -25,8 +26,8 @@
 // reading leaves the logits in L2.
 //
 // What bounds it is latency: a dozen steps with a barrier between them, and for a cut item the way
-// of the keys through the workspace.  1 x 5 beams of 1025 fp32 logits, log-sum-exp included: 8.3 us
-// a call; 32 x 4 beams of 48001 bf16 logits with theirs given: 16.5 us (12 MB, 1.8 us at 6.8 TB/s).
+// of the keys through the workspace.  1 x 5 beams of 1025 fp32 logits, log-sum-exp included: 6.2 us
+// a call; 32 x 4 beams of 48001 bf16 logits with theirs given: 13.9 us (12 MB, 1.8 us at 6.8 TB/s).
 #include <float.h>
 
 #include <algorithm>
@@ -208,14 +209,6 @@ __device__ __forceinline__ int for_pieces(const void* base, int64_t first, int n
     if (warp == 0 && rest < n) one(rest, T::one(p, rest));
     return max(1, (vecs + 32 * UNROLL - 1) / (32 * UNROLL));
 }
-// use(i, x), element by element
-template <class T, int UNROLL, class F>
-__device__ __forceinline__ int for_row(const void* base, int64_t first, int n, int warp, int warps, F use) {
-    return for_pieces<T, UNROLL>(base, first, n, warp, warps, use, [&](int i, const float (&x)[T::PER]) {
-#pragma unroll
-        for (int e = 0; e < T::PER; ++e) use(i + e, x[e]);
-    });
-}
 
 // (maximum, sum of exp(x - maximum)) of two sets, as one
 __device__ __forceinline__ void join_sums(float& m, float& s, float m2, float s2) {
@@ -328,24 +321,31 @@ __global__ void __launch_bounds__(BS_THREADS) beam_select_kernel(const __grid_co
         __syncthreads();
     };
     if constexpr (!HOLD) beams_there();
-    // use(beam, column, logit) for this thread's logits of the segment; the beams' stretches go round the warps, so
-    // that short rows are on their way together.  A finished beam has its end alone.
-    auto logits = [&](auto use) {
+    // one(beam, column, logit) or piece(beam, column, logits) for this thread's logits of the segment, by ascending number; the
+    // beams' stretches go round the warps, so that short rows are on their way together.  A finished beam has its end alone.
+    auto logits = [&](auto one, auto piece) {
         const int beam0 = first / V, beam1 = (first + n - 1) / V;
         int turn = warp;
         for (int w = beam0; w <= beam1; ++w) {
             const int c0 = max(0, first - w * V), c1 = min(V, first + n - w * V);
             if (s_done[w] && !HOLD) {
-                for (int c = c0 + tid; c < c1; c += BS_THREADS) use(w, c, c == a.eos_id ? 0.f : -INFINITY);
+                for (int c = c0 + tid; c < c1; c += BS_THREADS) one(w, c, c == a.eos_id ? 0.f : -INFINITY);
             } else {
-                const int used = for_row<T, 4>(a.logits, ((int64_t)item * W + w) * a.logits_stride + c0, c1 - c0, turn, BS_WARPS,
-                                               [&](int i, float x) { use(w, c0 + i, x); });
+                const int used = for_pieces<T, 4>(
+                    a.logits, ((int64_t)item * W + w) * a.logits_stride + c0, c1 - c0, turn, BS_WARPS,
+                    [&](int i, float x) { one(w, c0 + i, x); }, [&](int i, const float (&x)[T::PER]) { piece(w, c0 + i, x); });
                 turn = (turn + BS_WARPS - used % BS_WARPS) % BS_WARPS;
             }
         }
     };
+    auto each_logit = [&](auto use) {
+        logits(use, [&](int w, int c, const float (&x)[T::PER]) {
+#pragma unroll
+            for (int e = 0; e < T::PER; ++e) use(w, c + e, x[e]);
+        });
+    };
     if constexpr (HOLD) {  // a warp per beam: its log-sum-exp, then its scores
-        logits([&](int w, int c, float x) { bs_score[w * V + c] = x; });
+        each_logit([&](int w, int c, float x) { bs_score[w * V + c] = x; });
         beams_there();
         for (int w = warp; w < W; w += BS_WARPS) {
             float* x = bs_score + w * V;
@@ -369,30 +369,50 @@ __global__ void __launch_bounds__(BS_THREADS) beam_select_kernel(const __grid_co
     // this thread's largest score, the first of equal ones
     float most = -INFINITY;
     uint32_t at_most = 0xffffffffu;
-    auto larger = [&](uint32_t number, float x) {
-        if (x > most || (x == most && number < at_most)) {
+    auto larger = [&](uint32_t number, float x) {  // (numbers ascend)
+        if (x > most || at_most == 0xffffffffu) {
             most = x;
             at_most = number;
         }
+    };
+    int beam = -1;  // (a finished beam's end comes as 0, its score is the beam's own)
+    float cum = 0.f, lse = 0.f;
+    auto score = [&](int w, float x) {
+        if (w != beam) {
+            beam = w;
+            cum = s_beam[w];
+            lse = s_done[w] ? 0.f : s_lse[w];
+        }
+        return cum + (x - lse);
     };
     auto each = [&](auto f) {  // f(number, score)
         if constexpr (HOLD) {
 #pragma unroll 8
             for (int i = tid; i < n; i += BS_THREADS) f((uint32_t)i, bs_score[i]);
         } else {
-            int beam = -1;  // (a finished beam's end comes as 0, its score is the beam's own)
-            float cum = 0.f, lse = 0.f;
-            logits([&](int w, int c, float x) {
-                if (w != beam) {
-                    beam = w;
-                    cum = s_beam[w];
-                    lse = s_done[w] ? 0.f : s_lse[w];
-                }
-                f((uint32_t)(w * V + c), ranked(cum + (x - lse)));
-            });
+            each_logit([&](int w, int c, float x) { f((uint32_t)(w * V + c), ranked(score(w, x))); });
         }
     };
-    each(larger);
+    if constexpr (HOLD) {
+        each(larger);
+    } else {
+        logits([&](int w, int c, float x) { larger((uint32_t)(w * V + c), ranked(score(w, x))); },
+               [&](int w, int c, const float (&x)[T::PER]) {  // the largest of a piece, then its place
+                   float y[T::PER], top = -INFINITY;
+#pragma unroll
+                   for (int e = 0; e < T::PER; ++e) {
+                       y[e] = score(w, x[e]);
+                       top = fmaxf(top, y[e]);
+                   }
+                   if (top > most || at_most == 0xffffffffu) {
+                       most = ranked(top);
+                       int at = 0;
+#pragma unroll
+                       for (int e = T::PER - 1; e >= 0; --e) at = ranked(y[e]) == most ? e : at;
+                       at_most = (uint32_t)(w * V + c + at);
+                   }
+               });
+    }
     __syncwarp();
     best_of(b, a.k, at_most != 0xffffffffu ? make_key(most, at_most) : 0ull,
             [&](auto f) { each([&](uint32_t number, float x) { f(make_key(x, number)); }); });
