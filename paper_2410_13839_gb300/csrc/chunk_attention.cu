@@ -479,18 +479,21 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 ? 3 : 2)
 }
 
 // ---- merge ----
-// Grid (CTA of the kernel before, groups of four rows); a warp takes a row of the item that
+// Grid (CTA of the kernel before, groups of rows); a warp takes a row of the item that
 // begins in that CTA's share and goes on in the next ones': out = sum_c 2^(m_c - M) o_c / L,
 // L = sum_c 2^(m_c - M) l_c, M = max m_c, in the CTAs' order, a batch of parts at a time.  Bound by
 // latency (the item, then its parts) where items are shared by many CTAs: about 3 us after a
 // step; one slot of 32,000 keys and 2 key heads, 125 parts an item, takes 18.5 us a call, 41 with
 // the maxima looked for first and four parts at a time.
+// Rows of a CTA: most CTAs of the grid have nothing to do, as few items are shared, and for tiles of many rows they are so many
+// that they take time (25 prompts, 4, 8, 16, 32 rows: 43.0, 41.6, 41.5, 42.1 us, of 128 dims 70.8, 69.0, 68.2, 69.4); few rows' wait beside the kernel before.
+constexpr int merge_rows(int tile_rows) { return tile_rows == FR_ROWS ? 4 : 16; }
 template <class T, int HD, int TR>
-__global__ void __launch_bounds__(128) chunk_merge_kernel(const ChunkArgs a) {
-    const int cta = blockIdx.x, r = blockIdx.y * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+__global__ void __launch_bounds__(32 * merge_rows(TR)) chunk_merge_kernel(const __grid_constant__ ChunkArgs a) {
+    const int cta = blockIdx.x, r = blockIdx.y * merge_rows(TR) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     constexpr int PER = HD / 32, BATCH = TR == FR_ROWS ? 8 : 4;  // (tiles of many rows are shared by few CTAs)
-    // (After many rows not: the next call's plan, a CTA of 1024 threads, then starts in the merge's way.  25 prompts, one call
-    // after another: 43.7 us, 47.3 with it.)
+    // (After many rows not: the next call's kernels would start in the merge's way.  Two chunks of thousands of tokens, one call after
+    // another: 463 us, 474 with it, 25 prompts 41.5 and 41.8.)
     if (TR == FR_ROWS) pdl_launch_dependents();
     pdl_wait();
     const int* d = a.desc + cta * CH_DESC;
@@ -552,13 +555,13 @@ __global__ void __launch_bounds__(128) chunk_merge_kernel(const ChunkArgs a) {
         a.lse[row * (a.kv_heads * a.group) + head] = sum == 0.f ? -INFINITY : LN2 * (top + log2f(sum));
 }
 
+template <class T, int HD, int TR>
+cudaError_t launch_merge(const ChunkArgs& a, cudaStream_t s) {
+    return launch_ex(chunk_merge_kernel<T, HD, TR>, dim3(a.ctas, TR / merge_rows(TR)), 32 * merge_rows(TR), 0, s, 1, a);
+}
 template <class T, int HD>
 cudaError_t merge_hd(const ChunkArgs& a, int tile_rows, cudaStream_t s) {
-    const dim3 grid(a.ctas, tile_rows / 4);
-    switch (tile_rows) {
-        case FR_ROWS: return launch_ex(chunk_merge_kernel<T, HD, FR_ROWS>, grid, 128, 0, s, 1, a);
-        default: return launch_ex(chunk_merge_kernel<T, HD, 128 * chunk_tc_tiles(HD)>, grid, 128, 0, s, 1, a);
-    }
+    return tile_rows == FR_ROWS ? launch_merge<T, HD, FR_ROWS>(a, s) : launch_merge<T, HD, 128 * chunk_tc_tiles(HD)>(a, s);
 }
 
 // How a call runs: tile rows, CTAs, workspace.

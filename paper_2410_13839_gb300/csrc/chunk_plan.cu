@@ -7,7 +7,7 @@
 namespace mtp {
 namespace {
 
-constexpr int PL_THREADS = 1024, PL_WARPS = PL_THREADS / 32;
+constexpr int PL_THREADS = 512, PL_WARPS = PL_THREADS / 32;
 
 // Exclusive prefix sum of x over the block, and the total.
 __device__ __forceinline__ uint32_t scan(uint32_t x, uint32_t* part, uint32_t& sum) {
