@@ -39,13 +39,13 @@ namespace {
 
 constexpr int BS_THREADS = 512, BS_WARPS = BS_THREADS / 32;
 // Most scores of an item held in shared memory.  Held, and with a launch of its own for the log-sum-exp, us a call: 5 beams of
-// 1025 8.4 and 12.4, 8 of 1500 12.4 and 14.4.
+// 1025 6.2 and 8.9, 8 of 1500 8.7 and 10.8.
 constexpr int HELD = 14336;
-// Scores of an item that is not cut.  Whole and cut: 5125 scores 8.4 and 10.4, 10,000 8.4 and 10.4, 12,000 10.4 and 10.4,
-// 40,000 14.5 and 10.4.
+// Scores of an item that is not cut.  Whole and cut: 5125 scores 6.1 and 7.4, 10,000 6.1 and 6.7, 12,000 8.4 and 7.3,
+// 40,000 12.2 and 8.3.
 constexpr int WHOLE = 10240;
-// Fewest scores of a segment (1 x 4 beams of 48001, segments of 1024, 2048, 4096 at least: 14.5, 12.5, 12.4 us); CTAs of a wave
-// per SM (32 x 4 beams of 48001, 1 to 4: 21, 20.3, 23, 25 us when it was chosen).
+// Fewest scores of a segment (1 x 4 beams of 48001, segments of 1024, 2048, 4096 at least: 11.5, 9.5, 11.1 us); CTAs of a wave
+// per SM (32 x 4 beams of 48001, 1 to 4: 20.8, 14.1, 17.4, 20.3 us).
 constexpr int LEAST = 2048, SEL_PER_SM = 2;
 constexpr int GROUPS = 128;       // groups of four threads, each with a maximum
 constexpr int CAND_MAX = 1024, HELD_KEYS = 1024;

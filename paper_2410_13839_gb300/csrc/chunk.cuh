@@ -13,7 +13,7 @@
 // by every CTA for itself, the plan of 25 prompts' tiles cost 85 us a call where the kernel's
 // costs 66.)  A decoding step has one tile per slot: where its slots are at most FR_SLOTS, every CTA
 // makes its own share's plan in shared memory, and the launch and the wait for it are saved (32
-// slots of up to 2000 keys 40.3 us with the plan kernel, 36.7 without; 8 slots 18.5 and 14.5).
+// slots of up to 2000 keys 36.4 us with the plan kernel, 33.1 without; 8 slots 14.2 and 11.0).
 //
 // An item that lies in one CTA's share is written by that CTA.  One that several share leaves
 // (maximum, sum, unnormalised output) per row and CTA in the workspace, and a merge kernel
@@ -26,7 +26,8 @@ namespace mtp {
 
 constexpr int CH_MAX_SLOTS = 4096, CH_MAX_PACKED = 1 << 21;
 constexpr int CH_STEP = 64;  // keys of a step of the many-rows kernel
-// An item's start and end, in units.  0, 1, 2, 3: 25 prompts 66, 56, 52, 53 us; a step of 32 slots 47, 43.5, 42.5, 43.
+// An item's start and end, in units.  0, 1, 2, 3: 25 prompts 52.4, 43.4, 41.6, 42.3 us; a step of 32 slots 36.4, 34.8,
+// 33.1, 32.6; windows of 1000 keys 104, 97, 97, 103.
 constexpr int ITEM_COST = 2;
 
 // A tile in the workspace: three 16-byte pieces.

@@ -14,14 +14,14 @@
 // warps takes 16 of a stage's keys: S = Q K^T and O += P V by mma.sync (16 rows of a tile
 // as M), with a maximum, sum and output of its own, which the four join at the item's end.
 // From 17 rows on the tensor cores' 128-row tiles are used, mostly empty (chunk_attention_tc.cu):
-// 16 rows on 8 contexts of 4,000 to 30,000 keys, 128 dims fp16, take 86 us here and 96 there, on
-// 32 of up to 2000 keys, 64 dims bf16, 19.6 and 28.9; 32 rows, in tiles of 32 rows made as
-// these are, took 172 and 24.8, there 98 and 26.8, on 128 contexts 62 and 55.
+// 16 rows on 8 contexts of 4,000 to 30,000 keys, 128 dims fp16, take 79.7 us here and 92 there, on
+// 32 of up to 2000 keys, 64 dims bf16, 12.9 and 21.9; 32 rows, in tiles of 32 rows made as
+// these are, took 172 and 24.8, there 93.6 and 22.3, on 128 contexts 62 and 52.
 //
-// A decoding step of 32 slots (180 to 2000 keys, 16 heads of 64, 147 MB) takes 35.1 us a call, of
+// A decoding step of 32 slots (180 to 2000 keys, 16 heads of 64, 147 MB) takes 33 us a call, of
 // which the memory's part is 21.6 us: the share's plan, the ring's start, an item's joining
-// and the merge are the rest, about 3 us each.  4 drafts of 8 slots of 4,000 to 30,000 keys, 8 key
-// heads of 128 dims (480 MB): 81.7 us, 87 % of 6.8 TB/s.
+// and the merge are the rest, 2 to 3 us each.  4 drafts of 8 slots of 4,000 to 30,000 keys, 8 key
+// heads of 128 dims (480 MB): 79.7 us, 89 % of 6.8 TB/s.
 //
 // Q enters as it is (16 bits).  P enters as a pair hi + lo of the type, its rounding
 // residue with it: a bound memory leaves the second product free, and the outputs then
@@ -41,10 +41,11 @@ int tc_encode_queries(CUtensorMap* map, const void* q, int dtype, int head_dim, 
 namespace {
 
 constexpr int FR_KEYS = 64, FR_WARPS = 5, FR_THREADS = FR_WARPS * 32, FR_CONSUMERS = 128;
-// Fewest units of a CTA (few rows, 2, 4, 8: 2 slots 16.5, 16.5, 18.6 us; many rows, 1, 2, 4: 4 prompts 22.7, 24.5, 28.8).
+// Fewest units of a CTA.  Few rows, 2, 4, 8: 2 slots of up to 2000 keys 8.6, 10.2, 13.9 us, one of 32,000 keys and 2 key heads, whose
+// merge grows, 19.3, 16.6, 15.9; many rows, 1, 2, 4: 4 prompts 18.3, 19.4, 22.3.
 constexpr int FR_MIN_UNITS = 4, CT_MIN_UNITS = 1;
 // Items of many rows of at most so many units are not cut: a cut costs a tile's parts and their merge, about two units'
-// time.  All cut, 6, 12, 24: windows of 1000 keys 109, 109, 103, 103 us, 25 prompts of 128 dims 76.7, 73.6, 73.5, 73.6.  (Up to a
+// time.  All cut, 6, 12, 24: windows of 1000 keys 105, 105, 97, 97 us, 25 prompts of 128 dims 72.6, 67.9, 68.1, 67.7.  (Up to a
 // third of a share, however long: chunks of thousands of tokens 486 us instead of 447.)
 constexpr int CT_SNAP = 12;
 constexpr int FR_ROWS = 16, CT_UNIT_KEYS = 128;  // a tile of few rows
@@ -483,7 +484,7 @@ __global__ void __launch_bounds__(FR_THREADS, HD == 64 ? 3 : 2)
 // begins in that CTA's share and goes on in the next ones': out = sum_c 2^(m_c - M) o_c / L,
 // L = sum_c 2^(m_c - M) l_c, M = max m_c, in the CTAs' order, a batch of parts at a time.  Bound by
 // latency (the item, then its parts) where items are shared by many CTAs: about 3 us after a
-// step; one slot of 32,000 keys and 2 key heads, 125 parts an item, takes 18.5 us a call, 41 with
+// step; one slot of 32,000 keys and 2 key heads, 125 parts an item, takes 16.6 us a call, 39 with
 // the maxima looked for first and four parts at a time.
 // Rows of a CTA: most CTAs of the grid have nothing to do, as few items are shared, and for tiles of many rows they are so many
 // that they take time (25 prompts, 4, 8, 16, 32 rows: 43.0, 41.6, 41.5, 42.1 us, of 128 dims 70.8, 69.0, 68.2, 69.4); few rows' wait beside the kernel before.

@@ -17,15 +17,15 @@
 // threads run over the items of the share without a stop, as do the rings of keys and of
 // values, which a warp each fills with TMA copies, a lane per page piece; the values' warp brings
 // Q too, by a tensor map, where the heads of a key head divide 128 and rows are aligned to 16 bytes
-// (25 prompts 47.2 us; brought by the softmax warps, as other rows are, 49.8).  A tile skips the
+// (25 prompts 41.6 us; brought by the softmax warps, as other rows are, 44.7).  A tile skips the
 // steps of which its rows see no key.
 //
-// Two chunks of 2000 to 4000 tokens after 6000 to 9000, 32 heads on 8 of 128 dims (648 GFLOP): 444 us,
-// 1460 TFLOP/s, of the measured peak (cuBLAS, 1922) three quarters; the MMAs of 45 and 64 cycles
-// fill about as much of the time.  64 dims, 16 heads (162 GFLOP): 228 us, 710 TFLOP/s: bound by
+// Two chunks of 2000 to 4000 tokens after 6000 to 9000, 32 heads on 8 of 128 dims (648 GFLOP): 446 us,
+// 1450 TFLOP/s, of the measured peak (cuBLAS, 1922) three quarters; the MMAs of 45 and 64 cycles
+// fill about as much of the time.  64 dims, 16 heads (162 GFLOP): 218 us, 740 TFLOP/s: bound by
 // the softmax, whose 64 exponentials a row and step are as many as with 128 dims; a warp issues in
 // 44 % of the cycles and waits for results of its own the most.  25 prompts of 182 to 578 tokens,
-// 16 heads of 64: 47.2 us, of which the plan is 5, and items of 1 to 5 units with a start and
+// 16 heads of 64: 41.6 us, of which the plan is 4, and items of 1 to 5 units with a start and
 // end each the rest.
 //
 // Code size matters: with everything unrolled and inlined (190 KB) the warps waited for
@@ -42,8 +42,8 @@
 // within the type.  Q, K and V enter as they are.
 // RES: up to 32 rows, where memory leaves the tensor cores time, P enters with its residues,
 // which go to the other half of S's place and have a product of their own.  (8 slots of 4,000
-// to 30,000 keys, 32 rows each, 128 dims fp16: 98 us, 92 without; 32 slots of up to 2000 keys,
-// 64 dims bf16: 26.8 and 24.7.)
+// to 30,000 keys, 32 rows each, 128 dims fp16: 93.6 us, 86.9 without; 32 slots of up to 2000 keys,
+// 64 dims bf16: 22.3 and 19.1.)
 #include <algorithm>
 #include <climits>
 #include <type_traits>

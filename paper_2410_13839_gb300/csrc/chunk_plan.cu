@@ -1,7 +1,7 @@
 // chunk_plan.cu -- the plan of a chunk attention call (chunk.cuh): its tiles, every CTA's
 // first item, and which items several CTAs share.  One CTA; prefix sums over the slots, over
 // the tiles' units, then a thread per border between shares.  What bounds it is latency: two
-// scans and a few dependent loads, 4.7 us with 32 slots.
+// scans and a few dependent loads, about 3 us with 32 slots.
 #include "chunk.cuh"
 
 namespace mtp {

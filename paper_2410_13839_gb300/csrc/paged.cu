@@ -31,10 +31,13 @@ namespace mtp {
 namespace {
 
 constexpr int PG_CLUSTER = 8, PG_THREADS = 1024, PG_WARPS = PG_THREADS / 32;
-// One CTA up to these.  One CTA against eight, us a call: plan of 32 slots and 2048 pages 6.3 and 8.3, 32768 pages 10.4 and
-// 8.3; of 1024 slots and 34,000 pages 12.4 and 10.4; reordering of 96 beams 12.5 and 14.5, of 256 beams 16.5 and 15.8, of
-// 512 21.0 and 16.5.  Rows written by the plan's own launch against one of theirs: 4096 rows 10.4 and 12.4, 8192 14.5 and 12.4.
-constexpr int PG_ONE_PAGES = 16384, PG_ONE_SLOTS = 1024, PG_ONE_ROWS = 4096, PG_ONE_BEAMS = 192;
+// One CTA up to these.  One CTA against eight, us a call: plan of 32 slots and 2048 pages 3.9 and 4.9, 8192 pages 4.4 and 5.0,
+// 16384 pages 5.5 and 5.1, 32768 pages 7.5 and 5.2; of 1024 slots and 34,000 pages 9.6 and 7.2; 2048 rows beside them 6.5 and 5.7;
+// reordering of 96 beams 10.3 and 12.7, of 256 beams 13.7 and 12.8, of 512 19.1 and 14.0.
+constexpr int PG_ONE_PAGES = 8192, PG_ONE_SLOTS = 1024, PG_ONE_ROWS = 1024, PG_ONE_BEAMS = 192;
+// Rows that the plan's own launch writes, more are written by one of theirs: 4096 rows 5.7 and 8.9 us, 8192 5.9 and 9.4, 16384
+// ROWS16 and 8.9.
+constexpr int PG_ROWS_HERE = 16384;
 constexpr int PG_MAX_SLOTS = 8192;
 constexpr int PG_MAX_PAGES = 1 << 22;
 constexpr int PG_MAX_ROWS = 1 << 24;
@@ -374,9 +377,9 @@ __device__ __forceinline__ uint4 load8(const void* base, int64_t at) {
 
 // A thread moves AP_UNROLL pieces of eight elements, all loaded before any is stored.
 // Bound by memory: each element is read once and written once.  14592 rows of 16 heads of 64, bf16:
-// 120 MB in 17.4 us, 6.9 TB/s (20.9 us a call, one after another); a step's 128 rows are latency,
-// 5 us.  VECTOR: rows on 16-byte boundaries are read 16 bytes at a time; the same rows again and
-// again 18.6 us a call, element by element 23.1 (from fp32 29.4 and 32.9).
+// 120 MB in 17.4 us, 6.9 TB/s (19.3 us a call with other rows between); a step's 128 rows are latency,
+// 3.3 us.  VECTOR: rows on 16-byte boundaries are read 16 bytes at a time; the same rows again and
+// again 17.5 us a call, element by element 21.5 (from fp32 27.5 and 30.9).
 template <class DST, int SRC, bool VECTOR>
 __global__ void __launch_bounds__(AP_THREADS) cache_append_kernel(const __grid_constant__ AppendArgs p) {
     const mtp_cache_append_args& a = p.a;
@@ -557,8 +560,8 @@ constexpr int CP_THREADS = 256, CP_UNROLL = 4;
 // The filled rows of every copied page: for each (layer, keys | values, head) one run of
 // tokens * head_dim elements.  A warp takes a run; CP_UNROLL loads are in flight per lane.
 // Bound by memory: each row is read once and written once; with few copies by latency (the list, then
-// the rows).  96 beams' copies, 12 layers of 16 heads of 64, 150 MB read and written: 29 us a call,
-// 12 of them the tables'; 22 at 6.8 TB/s.
+// the rows).  96 beams' copies, 12 layers of 16 heads of 64, 150 MB read and written: 27 us a call,
+// 8 of them the tables'; 22 at 6.8 TB/s.
 __global__ void __launch_bounds__(CP_THREADS) page_copy_kernel(const __grid_constant__ ReorderArgs p, int runs) {
     pdl_launch_dependents();
     pdl_wait();
@@ -620,8 +623,8 @@ MTP_API int mtp_page_plan(const mtp_page_plan_args* a, void* cuda_stream) {
             !a->out_cu_rows || !a->out_status ||
             (a->max_rows > 0 && (!a->out_slot_map || !a->out_row_seq || !a->out_row_pos)))
             return invalid("page_plan: null pointer");
-        const bool one = a->n_pages <= PG_ONE_PAGES && a->slots <= PG_ONE_SLOTS;
-        const PlanArgs p{*a, log2_of(a->page_size), a->max_rows <= PG_ONE_ROWS};
+        const bool one = a->n_pages <= PG_ONE_PAGES && a->slots <= PG_ONE_SLOTS && a->max_rows <= PG_ONE_ROWS;
+        const PlanArgs p{*a, log2_of(a->page_size), a->max_rows <= PG_ROWS_HERE};
         const size_t smem = (size_t)(3 * a->slots + 2 + 2 * free_words(a->n_pages, one ? 1 : PG_CLUSTER)) * 4;
         const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
         cudaError_t e = one ? launch(page_plan_kernel<1>, 1, PG_THREADS, smem, 1, s, p)
