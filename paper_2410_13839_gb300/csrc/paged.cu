@@ -36,7 +36,7 @@ constexpr int PG_CLUSTER = 8, PG_THREADS = 1024, PG_WARPS = PG_THREADS / 32;
 // reordering of 96 beams 10.3 and 12.7, of 256 beams 13.7 and 12.8, of 512 19.1 and 14.0.
 constexpr int PG_ONE_PAGES = 8192, PG_ONE_SLOTS = 1024, PG_ONE_ROWS = 1024, PG_ONE_BEAMS = 192;
 // Rows that the plan's own launch writes, more are written by one of theirs: 4096 rows 5.7 and 8.9 us, 8192 5.9 and 9.4, 16384
-// ROWS16 and 8.9.
+// 6.5 and 8.9.
 constexpr int PG_ROWS_HERE = 16384;
 constexpr int PG_MAX_SLOTS = 8192;
 constexpr int PG_MAX_PAGES = 1 << 22;
