@@ -274,7 +274,9 @@ def _rows(name, x, shape):
         if n != 1 and s != inner:
             raise ValueError(f"{name}: the elements of a row have to be contiguous")
         inner *= n
-    return x.data_ptr(), max(x.stride(0), inner)
+    if x.shape[0] > 1 and x.stride(0) < inner:
+        raise ValueError(f"{name}: rows of {inner} elements overlap at a stride of {x.stride(0)}")
+    return x.data_ptr(), max(x.stride(0), inner)  # (a single row's stride may say anything)
 
 
 def _dtype(name, x, allowed):

@@ -132,3 +132,52 @@ def test_argument_blocks_refuse_tensors_they_cannot_describe(libpath):  # noqa: 
         mtp.cache_append_args(k=k, v=k, slot_map=places, kv_pool=pool, layer=0)
     with pytest.raises(TypeError):
         mtp.cache_append_args(k=k, v=k, slot_map=places, kv_pool=pool.float(), layer=0)
+
+
+class _OnGpu:
+    """A CPU tensor that says it is on the GPU: argument blocks are built from it, nothing is launched."""
+    is_cuda = True
+
+    def __init__(self, x):
+        self._x = x
+
+    def __getattr__(self, name):
+        return getattr(self._x, name)
+
+
+@pytest.mark.parametrize("rows,stride", [(1000, 0), (2, 0), (3, 64), (3, 127)])
+@pytest.mark.parametrize("which", ["k", "v", "q", "out"])
+def test_rows_that_overlap(libpath, which, rows, stride):  # noqa: F811
+    """Expanded or overlapping rows of 128 elements are refused: read at a stride of a row's width, as if they were
+    packed, they would end past their buffer."""
+    torch = pytest.importorskip("torch")
+    from paper_2410_13839_gb300 import mtp
+    i32 = dict(dtype=torch.int32)
+    pool = _OnGpu(torch.zeros(2, 1, 2, 2, 16, 64, dtype=torch.bfloat16))
+    overlapping = _OnGpu(torch.zeros((rows - 1) * stride + 128, dtype=torch.bfloat16).as_strided((rows, 2, 64), (stride, 64, 1)))
+    good = _OnGpu(torch.zeros(rows, 2, 64, dtype=torch.bfloat16))
+    x = {n: overlapping if n == which else good for n in ("k", "v", "q", "out")}
+
+    def append():
+        return mtp.cache_append_args(k=x["k"], v=x["v"], slot_map=_OnGpu(torch.zeros(rows, dtype=torch.int64)), kv_pool=pool,
+                                     layer=0)
+
+    def attend():
+        return mtp.chunk_attention_args(q=x["q"], kv_pool=pool, layer=0, block_table=_OnGpu(torch.zeros(1, 2, **i32)),
+                                        cu_rows=_OnGpu(torch.zeros(2, **i32)), kv_lens=_OnGpu(torch.zeros(1, **i32)),
+                                        out=x["out"], scale=0.125, max_new=rows, max_keys=32)
+    wrong, right = (append, attend) if which in "kv" else (attend, append)
+    with pytest.raises(ValueError, match=which):
+        wrong()
+    right()
+
+
+@pytest.mark.parametrize("rows,stride", [(0, 0), (1, 0), (1, 128), (1, 500), (4, 128), (4, 200)])
+def test_row_strides_that_are_taken(libpath, rows, stride):  # noqa: F811
+    """The stride of several rows is the tensor's; of one row, whatever the tensor says, it is at least a row's width."""
+    torch = pytest.importorskip("torch")
+    from paper_2410_13839_gb300 import mtp
+    pool = _OnGpu(torch.zeros(2, 1, 2, 2, 16, 64, dtype=torch.bfloat16))
+    k = _OnGpu(torch.zeros(4 * 512, dtype=torch.bfloat16).as_strided((rows, 2, 64), (stride, 64, 1)))
+    args = mtp.cache_append_args(k=k, v=k, slot_map=_OnGpu(torch.zeros(rows, dtype=torch.int64)), kv_pool=pool, layer=0)
+    assert args.rows == rows and args.k_stride == args.v_stride == max(stride, 128)
