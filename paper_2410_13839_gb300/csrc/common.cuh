@@ -65,13 +65,18 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, int* e
 // arrive.release makes this thread's earlier writes (shared memory included)
 // visible to threads that return from their wait; arrive.relaxed orders
 // nothing and only signals progress (e.g. "done reading peers' memory").
+// The aligned forms want a warp's threads together, which after a branch only
+// __syncwarp() makes sure of: whole warps call these.
 __device__ __forceinline__ void cluster_arrive_release() {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void cluster_arrive_relaxed() {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void cluster_wait() {
+    __syncwarp();
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 

@@ -106,3 +106,20 @@ def test_steps_in_turn_keep_the_counts():
                 if p >= 0:
                     held[p] += 1
         assert held == refs
+
+
+def test_steps_in_turn_by_eight_ctas():
+    """The same where eight CTAs share the tables, and beams of uneven lengths, some of which end, free their pages."""
+    rng = random.Random(8)
+    batch, beams = 60, 5
+    table, lens, refs = paged_util.beams_state(8, batch, beams, 16, 1, 150, 400)
+    for _ in range(4):
+        parent = [[rng.choice([-1, rng.randrange(beams), rng.randrange(beams), 0]) for _ in range(beams)] for _ in range(batch)]
+        assert _check(parent, table, lens, refs, 16, layers=1, heads=1, dim=8)[0] == 0
+        table, lens, refs, _, _ = paged_util.reorder(parent, table, lens, refs, 16)
+        held = [0] * len(refs)
+        for r in table:
+            for p in r:
+                if p >= 0:
+                    held[p] += 1
+        assert held == refs
