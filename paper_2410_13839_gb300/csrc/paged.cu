@@ -597,10 +597,11 @@ int check_pool(const char* what, int n_pages, int layers, int layer, int n_kv_he
     return MTP_OK;
 }
 
-// Enqueue a kernel, clusters of `cluster` CTAs.
+// Enqueue a kernel, clusters of `cluster` CTAs.  (The 48 KB that a kernel has without asking hold its static shared memory
+// too: any size is asked for.)
 template <class... P>
 cudaError_t launch(void (*kern)(P...), int grid, int threads, size_t smem, int cluster, cudaStream_t s, P... args) {
-    const cudaError_t e = smem > 48 * 1024 ? ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem) : cudaSuccess;
+    const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem);
     return e == cudaSuccess ? launch_ex(kern, dim3(grid), threads, smem, s, cluster, args...) : e;
 }
 
