@@ -210,10 +210,13 @@ __device__ __forceinline__ int for_pieces(const void* base, int64_t first, int n
     return max(1, (vecs + 32 * UNROLL - 1) / (32 * UNROLL));
 }
 
-// (maximum, sum of exp(x - maximum)) of two sets, as one
+// (maximum, sum of exp(x - maximum)) of two sets, as one.  The maximum passes NaN over, the sum keeps it.
 __device__ __forceinline__ void join_sums(float& m, float& s, float m2, float s2) {
     const float top = fmaxf(m, m2);
-    if (top == -INFINITY) return;  // neither has a value
+    if (top == -INFINITY) {  // neither has a value: each sum is 0, or NaN
+        s += s2;
+        return;
+    }
     s = s * __expf(m - top) + s2 * __expf(m2 - top);
     m = top;
 }

@@ -177,3 +177,33 @@ def test_captured_in_a_graph():
         graph.replay()
         want = _expected(torch, x, out["out_lse"], scores, None, -1, 6)
         assert torch.equal(out["out_scores"].cpu(), want[0]) and torch.equal(out["out_token"].cpu(), want[2])
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("batch,beams,vocab", [(64, 8, 1025), (512, 1, 20001), (1, 16, 40001), (1, 16, 5000), (1, 1, 16385)])
+def test_a_nan_in_a_masked_row(dtype, batch, beams, vocab):
+    """Wherever the NaN of a row stands that is masked but for one logit: its log-sum-exp is NaN, none of its
+    continuations counts.  (Held items, rows by a CTA each, rows by clusters.)"""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    rows = batch * beams
+    g = torch.Generator().manual_seed(vocab)
+    # places of a first load's every lane, the last ones, and any others
+    near = list(range(min(vocab, 512))) + list(range(vocab - 40, vocab))
+    for start in range(0, min(len(near), max(4 * rows, 64)), rows):
+        at = torch.tensor((near[start:start + rows] + torch.randint(0, vocab, (rows,), generator=g).tolist())[:rows])
+        allowed = torch.where(at == vocab // 2, at // 2, torch.full_like(at, vocab // 2))
+        x = torch.full((rows, vocab), -float("inf"))
+        x[torch.arange(rows), allowed] = 1.5
+        clean = x.clone()
+        x[torch.arange(rows), at] = float("nan")
+        x[rows // 2] = clean[rows // 2] if rows > 1 else x[0]  # one row without a NaN
+        x = x.view(batch, beams, vocab).cuda().to(getattr(torch, dtype))
+        scores = torch.zeros(batch, beams, device="cuda")
+        out = _run(torch, mtp, x, None, scores, None, -1, 1)
+        lse = out["out_lse"].flatten().cpu()
+        want = torch.full((rows,), float("nan"))
+        if rows > 1:
+            want[rows // 2] = 1.5
+        assert torch.equal(lse.isnan(), want.isnan()), torch.nonzero(lse.isnan() != want.isnan())[:5].tolist()
+        _equal(torch, out, _expected(torch, x, out["out_lse"], scores, None, -1, 1))
