@@ -690,7 +690,9 @@ MTP_API int mtp_chunk_attention(const mtp_chunk_attention_args* a, void* workspa
         c.bt_stride = a->bt_stride; c.n_pages = a->n_pages;
         c.page_blocks = a->layers * 2 * a->n_kv_heads;
         c.layer_block = a->layer * 2 * a->n_kv_heads;
-        c.window = a->window; c.max_tiles = p.max_tiles; c.min_units = p.min_units;
+        // (no position passes the table: a window as long leaves nothing out, and differences with it stay in 32 bits)
+        c.window = a->window < a->bt_stride * a->page_size ? a->window : 0;
+        c.max_tiles = p.max_tiles; c.min_units = p.min_units;
         const bool few = p.tile_rows == FR_ROWS;
         c.residues = p.residues;
         c.snap = few ? 0 : CT_SNAP;

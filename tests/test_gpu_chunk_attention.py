@@ -336,3 +336,11 @@ def test_tokens_of_one_slot_in_every_size():
     """One to 300 tokens behind a short context: every filling of a tile, both kernels, both tiles of a CTA."""
     for n in list(range(1, 40)) + list(range(60, 70)) + list(range(120, 136)) + list(range(250, 262)) + [300]:
         check([n], [n + 5], 2, 1, 128 if n % 2 else 64, 16, seed=n)
+
+
+@pytest.mark.parametrize("window", [(1 << 24) + 1, (1 << 30), (1 << 31) - 3, (1 << 31) - 1])
+def test_windows_longer_than_any_table(window):
+    """Such a window leaves nothing out, at positions below 0 too."""
+    for new, lens in (([5, 3, 1], [2, 3, 0]), ([4, 1], [300, 64]), ([300, 5, 40], [100, 0, 700])):
+        check(new, lens, 4, 2, 64, 16, window=window)
+        check(new, lens, 4, 1, 128, 16, "float16", window=window)
