@@ -337,6 +337,7 @@ MTP_API int mtp_step_bytes(mtp_ctx* ctx, int n_heads, uint64_t* out_bytes);
  *   err_word  int32, device memory
  * Errors: MTP_ERR_INVALID (null), MTP_ERR_CUDA. */
 #define MTP_DEVICE_ERR_WAIT 1
+#define MTP_DEVICE_ERR_BOUNDS 2 /* a kernel met an index outside its buffers, and left out what it stands for */
 MTP_API int mtp_selftest_bounded_wait(int32_t* err_word, void* cuda_stream);
 
 /* Self-test of the persistent step kernel's grid barrier bound: one CTA
@@ -559,7 +560,9 @@ MTP_API int mtp_cache_append(const mtp_cache_append_args* args, void* cuda_strea
  *   scale        factor of the products q . k, > 0 (head_dim ^ -0.5 as a rule)
  *   block_table  int32 [slots][bt_stride]; of a slot the pages of the keys that its rows see are
  *                used (keys on pages outside the pool count as zeros)
- *   cu_rows      int32 [slots + 1], ascending; rows past the last are left as they are
+ *   cu_rows      int32 [slots + 1], ascending; rows past the last are left as they are.  Rows that do not
+ *                lie in the buffers (below 0, from `rows` on, of a slot whose end is before its start) are
+ *                left out, and MTP_DEVICE_ERR_BOUNDS says so in err_word
  *   kv_lens      int32 [slots]
  *   out_lse      float [rows][n_heads] or NULL: natural log of the sum of exp(scale q . k)
  *   max_new, max_keys  host-known upper bounds of a slot's new tokens and length: max_new

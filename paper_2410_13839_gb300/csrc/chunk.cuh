@@ -129,17 +129,20 @@ struct ChunkWalkOf {
 };
 using ChunkWalk = ChunkWalkOf<PlannedTiles>;
 
-// A slot: its first row, new tokens (as far as they lie in the row buffers), length.
+// A slot: its first row, new tokens (as far as they lie in the row buffers), position of the first of them.
 struct Slot {
-    int row0, n, len;
+    int row0, n, base;
 };
-__device__ __forceinline__ Slot load_slot(const ChunkArgs& a, int s) {
+// `cut` is set where rows that cu_rows gives the slot do not lie in the buffers.  Those that do keep their positions.
+__device__ __forceinline__ Slot load_slot(const ChunkArgs& a, int s, bool& cut) {
     Slot x;
     x.row0 = a.cu_rows[s];
-    x.n = a.cu_rows[s + 1] - x.row0;
-    x.len = max(0, min(a.kv_lens[s], a.bt_stride << a.page_shift));
-    if (x.row0 < 0 || x.row0 > a.rows || x.n < 0) x.n = 0;
-    x.n = min(x.n, a.rows - x.row0);
+    const int end = a.cu_rows[s + 1], len = max(0, min(a.kv_lens[s], a.bt_stride << a.page_shift));
+    const bool placed = x.row0 >= 0 && end >= x.row0;
+    x.n = placed ? max(0, min(end, a.rows) - x.row0) : 0;
+    // (fewer than CH_MAX_PACKED rows lie in the buffers: none of them reaches position 0 from further below)
+    x.base = placed ? max(len - (end - x.row0), -CH_MAX_PACKED) : 0;
+    cut |= !placed || end > a.rows;
     return x;
 }
 
@@ -150,7 +153,7 @@ __device__ __forceinline__ ChunkTile make_tile(const ChunkArgs& a, int slot, con
     x.row0 = y.row0;
     x.p0 = t * TR;
     x.rows = min(y.n * a.group - x.p0, TR);
-    x.base = y.len - y.n;
+    x.base = y.base;
     const int first = x.base + chunk_token(a, x.p0), last = x.base + chunk_token(a, x.p0 + x.rows - 1);  // positions
     x.hi = max(0, last + 1);
     x.lo = a.window > 0 ? min(x.hi, max(0, first - a.window + 1)) : 0;

@@ -122,10 +122,12 @@ __device__ __forceinline__ ChunkStart plan_share(const ChunkArgs& a, FewSlots& f
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
     Slot y{0, 0, 0};
     uint32_t units = 0;
+    bool cut = false;
     if (tid < a.slots) {
-        y = load_slot(a, tid);
+        y = load_slot(a, tid, cut);
         if (y.n > 0) units = make_tile<FR_ROWS, FR_KEYS>(a, tid, y, 0).units;
     }
+    if (cut && cta == 0 && a.err) atomicOr(a.err, ERR_BOUNDS);
     const unsigned live = __ballot_sync(FULL_MASK, units > 0);
     uint32_t x = units;
 #pragma unroll

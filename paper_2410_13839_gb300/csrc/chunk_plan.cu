@@ -74,11 +74,12 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan_kernel(const __grid_con
     pdl_launch_dependents();
     pdl_wait();
     uint32_t base = 0, sum;  // (tiles: the kept rows of all slots lie in the buffers; a caller's wrong row starts: cut below)
+    bool cut = false;
     for (int s0 = 0; s0 < a.slots; s0 += PL_THREADS) {
         const int s = s0 + tid;
         uint32_t x = 0;
         if (s < a.slots) {
-            const Slot y = load_slot(a, s);
+            const Slot y = load_slot(a, s, cut);
             slots[s] = y;
             x = ((uint32_t)y.n * a.group + TR - 1) / TR;
         }
@@ -86,6 +87,7 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan_kernel(const __grid_con
         if (s < a.slots) slot_first[s] = min(base + x, (uint32_t)a.max_tiles);
         base = min(base + sum, (uint32_t)a.max_tiles);
     }
+    if (cut && a.err) atomicOr(a.err, ERR_BOUNDS);
     Map m;
     m.unit_first = unit_first;
     m.tiles = (int)base;

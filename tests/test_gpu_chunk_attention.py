@@ -344,3 +344,57 @@ def test_windows_longer_than_any_table(window):
     for new, lens in (([5, 3, 1], [2, 3, 0]), ([4, 1], [300, 64]), ([300, 5, 40], [100, 0, 700])):
         check(new, lens, 4, 2, 64, 16, window=window)
         check(new, lens, 4, 1, 128, 16, "float16", window=window)
+
+
+def _call(torch, mtp, heads, kv_heads, dim, page, new, lens, rows, stride, max_new, window=0, claimed=None):
+    """Attention of `rows` buffer rows of slots with `new` tokens each, whose lengths are given as `claimed`; the inputs, out,
+    lse and the error word."""
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    counts = [-(-n // page) for n in lens]
+    pages = torch.randperm(sum(counts) + 1).tolist()
+    table = [[pages.pop() for _ in range(c)] + [-1] * (stride - c) for c in counts]
+    pool = torch.randn(sum(counts) + 1, 1, 2, kv_heads, page, dim, device="cuda", generator=gen).bfloat16()
+    q = torch.randn(rows, heads, dim, device="cuda", generator=gen).bfloat16()
+    out, lse = torch.full_like(q, -7.0), torch.full((rows, heads), -7.0, device="cuda")
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    err, cu, d_lens, d_table = ints([0]), ints([sum(new[:i]) for i in range(len(new) + 1)]), ints(claimed or lens), ints(table)
+    args = mtp.chunk_attention_args(q=q, kv_pool=pool, layer=0, block_table=d_table, cu_rows=cu, kv_lens=d_lens, out=out, out_lse=lse,
+                                    scale=dim ** -0.5, window=window, max_new=max_new, max_keys=max(lens), err_word=err)
+    n = mtp.mtp_chunk_attention_workspace_bytes(args)
+    mtp.mtp_chunk_attention(args, torch.full((n,), 255, dtype=torch.uint8, device="cuda"), n, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    return q, pool, table, out, lse, int(err)
+
+
+def _right(torch, out, lse, ref):
+    """Within the bounds above, weights rounded once."""
+    want, want_lse, size, _ = ref
+    assert bool(((out.double() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -14) * size).all())
+    none = want_lse == -float("inf")
+    assert torch.equal(lse == -float("inf"), none)
+    assert bool(((lse.double() - want_lse)[~none].abs() <= 4e-5 + 2.0 ** -22 * want_lse[~none].abs()).all())
+
+
+BOUNDS = 2  # MTP_DEVICE_ERR_BOUNDS
+
+
+@pytest.mark.parametrize("window", [0, 9])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(2, 2, 64), (4, 2, 128)])
+@pytest.mark.parametrize("new,lens,rows", [([3, 6], [20, 50], 5), ([3, 6, 4], [20, 50, 4], 5), ([40, 300], [60, 900], 200),
+                                           ([1] * 150 + [7], [5] * 150 + [90], 153),
+                                           ([1] * 200, [9] * 200, 40), ([130] * 5, [200] * 5, 131)])
+def test_rows_past_the_buffers(new, lens, rows, heads, kv_heads, dim, window):
+    """Row starts that pass the buffers' rows: what lies in the buffers keeps its position, and the error word says that
+    rows are missing."""
+    torch = pytest.importorskip("torch")
+    q, pool, table, out, lse, err = _call(torch, lib_module(), heads, kv_heads, dim, 16, new, lens, rows, 60, max(new), window)
+    all_q = torch.cat([q, torch.zeros(sum(new) - rows, heads, dim, device="cuda", dtype=q.dtype)])
+    _right(torch, out, lse, [x[:rows] for x in reference(torch, all_q, pool, 0, table, new, lens, dim ** -0.5, window)])
+    assert err == BOUNDS
+
+
+def test_row_starts_that_descend():
+    torch = pytest.importorskip("torch")
+    q, pool, table, out, lse, err = _call(torch, lib_module(), 2, 1, 64, 16, [4, -2], [30, 20], 4, 4, 4)
+    _right(torch, out, lse, reference(torch, q, pool, 0, table, [4], [30], 0.125, 0))
+    assert err == BOUNDS
