@@ -563,7 +563,8 @@ MTP_API int mtp_cache_append(const mtp_cache_append_args* args, void* cuda_strea
  *   cu_rows      int32 [slots + 1], ascending; rows past the last are left as they are.  Rows that do not
  *                lie in the buffers (below 0, from `rows` on, of a slot whose end is before its start) are
  *                left out, and MTP_DEVICE_ERR_BOUNDS says so in err_word
- *   kv_lens      int32 [slots]
+ *   kv_lens      int32 [slots], 0 to bt_stride * page_size: new tokens of a slot of another length see no
+ *                key, and MTP_DEVICE_ERR_BOUNDS says so
  *   out_lse      float [rows][n_heads] or NULL: natural log of the sum of exp(scale q . k)
  *   max_new, max_keys  host-known upper bounds of a slot's new tokens and length: max_new
  *                chooses the kernel, max_keys the number of CTAs

@@ -133,16 +133,18 @@ using ChunkWalk = ChunkWalkOf<PlannedTiles>;
 struct Slot {
     int row0, n, base;
 };
-// `cut` is set where rows that cu_rows gives the slot do not lie in the buffers.  Those that do keep their positions.
+// `cut` is set where rows that cu_rows gives the slot do not lie in the buffers (those that do keep their positions), and
+// where the length of a slot with new tokens has no place in the table: such a slot has no key.
 __device__ __forceinline__ Slot load_slot(const ChunkArgs& a, int s, bool& cut) {
     Slot x;
     x.row0 = a.cu_rows[s];
-    const int end = a.cu_rows[s + 1], len = max(0, min(a.kv_lens[s], a.bt_stride << a.page_shift));
-    const bool placed = x.row0 >= 0 && end >= x.row0;
+    const int end = a.cu_rows[s + 1], given = a.kv_lens[s];
+    const bool placed = x.row0 >= 0 && end >= x.row0, held = given >= 0 && given <= a.bt_stride << a.page_shift;
+    const int len = held ? given : 0;
     x.n = placed ? max(0, min(end, a.rows) - x.row0) : 0;
     // (fewer than CH_MAX_PACKED rows lie in the buffers: none of them reaches position 0 from further below)
     x.base = placed ? max(len - (end - x.row0), -CH_MAX_PACKED) : 0;
-    cut |= !placed || end > a.rows;
+    cut |= !placed || end > a.rows || (x.n > 0 && !held);
     return x;
 }
 

@@ -393,6 +393,35 @@ def test_rows_past_the_buffers(new, lens, rows, heads, kv_heads, dim, window):
     assert err == BOUNDS
 
 
+@pytest.mark.parametrize("new", [2, 90])
+@pytest.mark.parametrize("wrong", [-1, -(1 << 31), 4 * 16 + 1, (1 << 31) - 1])
+def test_lengths_outside_the_table(wrong, new):
+    """A slot whose length is negative or longer than its table sees no key, and the error word says so; the others are
+    computed."""
+    torch = pytest.importorskip("torch")
+    stride = 4 if new < 60 else 8
+    wrong = wrong + 64 if stride == 8 and wrong == 65 else wrong
+    lens = [stride * 16, stride * 16 - 3, new]
+    q, pool, table, out, lse, err = _call(torch, lib_module(), 2, 1, 64, 16, [new] * 3, lens, 3 * new, stride, new,
+                                          claimed=[lens[0], wrong, lens[2]])
+    ref = reference(torch, q, pool, 0, table, [new] * 3, lens, 0.125, 0)
+    for x in ref[:1] + ref[2:]:
+        x[new:2 * new] = 0.0
+    ref[1][new:2 * new] = -float("inf")
+    _right(torch, out, lse, ref)
+    assert bool((out[new:2 * new] == 0).all()) and err == BOUNDS
+
+
+def test_the_length_of_a_slot_without_new_tokens_may_be_anything():
+    torch = pytest.importorskip("torch")
+    for new in ([3, 0, 2], [2, 0, 90], [1, 0] * 100):
+        lens = [max(1, 3 * n) for n in new]
+        q, pool, table, out, lse, err = _call(torch, lib_module(), 2, 1, 64, 16, new, lens, sum(new), 20, max(new),
+                                              claimed=[n if a else (-5 if i % 4 == 1 else 1 << 30) for i, (n, a) in enumerate(zip(lens, new))])
+        _right(torch, out, lse, reference(torch, q, pool, 0, table, new, lens, 0.125, 0))
+        assert err == 0
+
+
 def test_row_starts_that_descend():
     torch = pytest.importorskip("torch")
     q, pool, table, out, lse, err = _call(torch, lib_module(), 2, 1, 64, 16, [4, -2], [30, 20], 4, 4, 4)
