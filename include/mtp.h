@@ -567,7 +567,8 @@ MTP_API int mtp_cache_append(const mtp_cache_append_args* args, void* cuda_strea
  *                key, and MTP_DEVICE_ERR_BOUNDS says so
  *   out_lse      float [rows][n_heads] or NULL: natural log of the sum of exp(scale q . k)
  *   max_new, max_keys  host-known upper bounds of a slot's new tokens and length: max_new
- *                chooses the kernel, max_keys the number of CTAs
+ *                chooses the kernel, max_keys the number of CTAs.  Where a slot has more than max_new,
+ *                rows may be left out; MTP_DEVICE_ERR_BOUNDS says so
  *   err_word     int32 on the device or NULL: MTP_DEVICE_ERR_* bits are ORed in
  *   workspace    mtp_chunk_attention_workspace_bytes(args) bytes, 16-byte aligned, of any content;
  *                calls that overlap need workspaces of their own

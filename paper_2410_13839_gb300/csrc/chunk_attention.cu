@@ -126,6 +126,7 @@ __device__ __forceinline__ ChunkStart plan_share(const ChunkArgs& a, FewSlots& f
     if (tid < a.slots) {
         y = load_slot(a, tid, cut);
         if (y.n > 0) units = make_tile<FR_ROWS, FR_KEYS>(a, tid, y, 0).units;
+        cut |= y.n * a.group > FR_ROWS;  // rows past the slot's tile: max_new was too small
     }
     if (cut && cta == 0 && a.err) atomicOr(a.err, ERR_BOUNDS);
     const unsigned live = __ballot_sync(FULL_MASK, units > 0);

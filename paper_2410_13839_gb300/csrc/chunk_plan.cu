@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan_kernel(const __grid_con
     const int tid = threadIdx.x;
     pdl_launch_dependents();
     pdl_wait();
-    uint32_t base = 0, sum;  // (tiles: the kept rows of all slots lie in the buffers; a caller's wrong row starts: cut below)
+    uint32_t base = 0, sum;  // (more tiles than the workspace has, by a max_new too small or slots that overlap, are left out)
     bool cut = false;
     for (int s0 = 0; s0 < a.slots; s0 += PL_THREADS) {
         const int s = s0 + tid;
@@ -85,6 +85,7 @@ __global__ void __launch_bounds__(PL_THREADS) chunk_plan_kernel(const __grid_con
         }
         x = scan(x, part, sum);
         if (s < a.slots) slot_first[s] = min(base + x, (uint32_t)a.max_tiles);
+        cut |= base + sum > (uint32_t)a.max_tiles;
         base = min(base + sum, (uint32_t)a.max_tiles);
     }
     if (cut && a.err) atomicOr(a.err, ERR_BOUNDS);

@@ -427,3 +427,10 @@ def test_row_starts_that_descend():
     q, pool, table, out, lse, err = _call(torch, lib_module(), 2, 1, 64, 16, [4, -2], [30, 20], 4, 4, 4)
     _right(torch, out, lse, reference(torch, q, pool, 0, table, [4], [30], 0.125, 0))
     assert err == BOUNDS
+
+
+@pytest.mark.parametrize("new,max_new,slots", [(20, 1, 3), (20, 8, 200), (300, 17, 2)])
+def test_more_tokens_than_the_bound(new, max_new, slots):
+    """Rows that a wrong max_new leaves out are reported."""
+    torch = pytest.importorskip("torch")
+    assert _call(torch, lib_module(), 2, 2, 64, 16, [new] * slots, [new + 1] * slots, new * slots, 20, max_new)[5] == BOUNDS
