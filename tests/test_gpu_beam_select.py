@@ -207,3 +207,65 @@ def test_a_nan_in_a_masked_row(dtype, batch, beams, vocab):
             want[rows // 2] = 1.5
         assert torch.equal(lse.isnan(), want.isnan()), torch.nonzero(lse.isnan() != want.isnan())[:5].tolist()
         _equal(torch, out, _expected(torch, x, out["out_lse"], scores, None, -1, 1))
+
+
+def _one_large(torch, vocab):
+    """Places whose logit a summing kernel may miss: the row's ends, both sides of every 16-byte border near them (of
+    any row start) and of parts of 1 to 8 CTAs."""
+    places = set(range(min(vocab, 24))) | set(range(max(0, vocab - 24), vocab))
+    for ctas in range(1, 9):
+        seg = (-(-vocab // ctas) + 7) // 8 * 8
+        for edge in range(0, vocab + 1, seg):
+            places |= set(range(edge - 10, edge + 10))
+    for step in (32 * 4, 32 * 8, 32 * 4 * 4, 32 * 4 * 8, 512 * 4, 512 * 8, 512 * 4 * 4, 512 * 4 * 8):
+        places |= set(range(step - 9, step + 9)) | set(range(2 * step - 9, 2 * step + 9))
+    return sorted(p for p in places if 0 <= p < vocab)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("vocab,rows,shift", [(1025, 64, 0), (1025, 13, 3), (16385, 320, 0), (16385, 16, 1), (48001, 8, 0), (48001, 16, 5),
+                                              (20003, 320, 7), (33333, 1, 2)])
+def test_every_logit_is_summed(dtype, vocab, rows, shift):
+    """One logit of 20 among zeros, at places that a sum's heads, tails and cuts could miss: without it the log-sum-exp
+    would be log(vocab - 1), with it counted twice 0.69 more."""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    places = _one_large(torch, vocab)
+    if rows < 16:
+        places = places[::3] + places[1::7]
+    stride = vocab + shift % 4
+    value = 20.0
+    want = torch.tensor([value], dtype=torch.float64).exp().add(vocab - 1).log().item()
+    for start in range(0, len(places), rows):
+        at = torch.tensor([places[(start + i) % len(places)] for i in range(rows)], device="cuda")
+        buf = torch.zeros(shift + rows * stride, device="cuda").to(getattr(torch, dtype))
+        x = buf[shift:].view(1, rows, stride)[..., :vocab] if rows <= 64 else buf[shift:].view(rows, 1, stride)[..., :vocab]
+        x.scatter_(2, at.view(x.shape[0], x.shape[1], 1), value)
+        out = _run(torch, mtp, x, None, torch.zeros(x.shape[:2], device="cuda"), None, -1, 1)
+        # (20 + log(1 + 48000 e^-20): a rounding of the sum and of the last addition, exp of 0 exactly 1)
+        assert float((out["out_lse"].double() - want).abs().max()) <= 2.0 ** -18
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("batch,beams,vocab", [(1, 4, 48001), (32, 4, 48001), (7, 5, 16385), (1, 2, 262144), (3, 2, 30003)])
+def test_log_sum_exp_of_long_rows(dtype, batch, beams, vocab):
+    """Rows of more than one item's scores in shared memory, of which a thread of 512 adds few terms.  __expf errs by
+    2 + 1.173 |x| units of 2^-23 at most; over a term's way to the sum these |x| add up to the distance to the row's maximum,
+    and there is one exponential per 16 bytes that a thread reads and one per join (13 levels at most); an addition
+    rounds by 2^-24, as many of them and the 8 of a piece.  Then the logarithm and the last sum."""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    x = (3 * torch.randn(batch, beams, vocab, device="cuda", generator=gen)).to(getattr(torch, dtype))
+    out = _run(torch, mtp, x, None, torch.zeros(batch, beams, device="cuda"), None, -1, 4)
+    y = x.double()
+    want = torch.logsumexp(y, -1)
+    depth = (torch.softmax(y, -1) * (y.amax(-1, keepdim=True) - y)).sum(-1)  # mean distance to the maximum
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    ctas = 1
+    while ctas < 8 and batch * beams * ctas <= sms and vocab // (ctas * 2) >= 4096:
+        ctas *= 2
+    vecs = -(-vocab // ctas) // (4 if dtype == "float32" else 8) + 1
+    pieces = 4 * -(-vecs // 2048) + 2  # four to a stretch of 128 pieces, a stretch per warp in turn; a head's and a tail's element
+    bound = 2.0 ** -23 * (2 * (pieces + 14) + 1.173 * depth) + 2.0 ** -24 * (pieces + 21) + 2.0 ** -22 * want.abs()
+    assert bool(((out["out_lse"].double() - want).abs() <= bound).all()), ((out["out_lse"].double() - want).abs() / bound).max()
