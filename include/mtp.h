@@ -572,6 +572,13 @@ MTP_API int mtp_cache_append(const mtp_cache_append_args* args, void* cuda_strea
  *   err_word     int32 on the device or NULL: MTP_DEVICE_ERR_* bits are ORed in
  *   workspace    mtp_chunk_attention_workspace_bytes(args) bytes, 16-byte aligned, of any content;
  *                calls that overlap need workspaces of their own
+ * Scores, sums and outputs are held in 32 bits; the weights p enter the second product in 16.  Where
+ * min(max_new, rows) * G <= 32 their rounding residues enter too, and an output errs by its own rounding; beyond, p is
+ * rounded once to dtype, which adds u * sum(p |v|) at most (u = 2^-8 bf16, 2^-11 fp16; fp16 weights below 2^-14 of
+ * the row's largest may become multiples of 2^-24 of it).  A generous max_new therefore costs precision where there
+ * are few new tokens.
+ * mtp_attention_tc is the like for fp32 rows, 64-wide heads and a context's cache, whose order of a row's 16-byte
+ * chunks is another: the two do not read each other's pools.
  * What the cache holds past a slot's length, or before every row's window, may be anything,
  * NaN too; a non-finite value inside can reach every row of the slot.
  * Limits: slots <= 4096, n_heads <= 1024, G = n_heads / n_kv_heads <= 64, bt_stride * page_size <=

@@ -45,8 +45,9 @@ constexpr int FR_KEYS = 64, FR_WARPS = 5, FR_THREADS = FR_WARPS * 32, FR_CONSUME
 // merge grows, 19.3, 16.6, 15.9; many rows, 1, 2, 4: 4 prompts 18.3, 19.4, 22.3.
 constexpr int FR_MIN_UNITS = 4, CT_MIN_UNITS = 1;
 // Items of many rows of at most so many units are not cut: a cut costs a tile's parts and their merge, about two units'
-// time.  All cut, 6, 12, 24: windows of 1000 keys 105, 105, 97, 97 us, 25 prompts of 128 dims 72.6, 67.9, 68.1, 67.7.  (Up to a
-// third of a share, however long: chunks of thousands of tokens 486 us instead of 447.)
+// time.  All cut, 6, 12, 24: windows of 1000 keys 105, 105, 97, 97 us, 25 prompts of 128 dims 72.6, 67.9, 68.1, 67.7; items of
+// many slots are better cut: 128 slots of 32 rows, 128 dims, 77.7, 79.5, 84.0, 84.0, 64 dims 51.4, 52.2, 52.2, 52.2.  (Up to a third
+// of a share, however long: chunks of thousands of tokens 486 us instead of 447.)
 constexpr int CT_SNAP = 12;
 constexpr int FR_ROWS = 16, CT_UNIT_KEYS = 128;  // a tile of few rows
 constexpr int FR_SLOTS = 128;                   // slots whose plan every CTA makes for itself

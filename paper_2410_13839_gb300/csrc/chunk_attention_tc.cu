@@ -20,9 +20,9 @@
 // (25 prompts 41.6 us; brought by the softmax warps, as other rows are, 44.7).  A tile skips the
 // steps of which its rows see no key.
 //
-// Two chunks of 2000 to 4000 tokens after 6000 to 9000, 32 heads on 8 of 128 dims (648 GFLOP): 446 us,
-// 1450 TFLOP/s, of the measured peak (cuBLAS, 1922) three quarters; the MMAs of 45 and 64 cycles
-// fill about as much of the time.  64 dims, 16 heads (162 GFLOP): 218 us, 740 TFLOP/s: bound by
+// Two chunks of 2000 to 4000 tokens after 6000 to 9000, 32 heads on 8 of 128 dims (648 GFLOP): 446 to 471 us
+// (boxes differ), 1380 to 1450 TFLOP/s, of the measured peak (cuBLAS, 1922) about three quarters; the MMAs of 45 and 64
+// cycles fill about as much of the time.  64 dims, 16 heads (162 GFLOP): 212 us, 764 TFLOP/s: bound by
 // the softmax, whose 64 exponentials a row and step are as many as with 128 dims; a warp issues in
 // 44 % of the cycles and waits for results of its own the most.  25 prompts of 182 to 578 tokens,
 // 16 heads of 64: 41.6 us, of which the plan is 4, and items of 1 to 5 units with a start and
@@ -34,9 +34,9 @@
 // m is a row's reference, not its maximum: the weights are made with the one that is there, and
 // only where a step's weights add up to more than 2^15 (or a row has none yet) is the maximum
 // looked for, the reference moved and the output in TMEM rescaled.  After a row's first steps
-// that is rare, and 64 maxima per row and step are saved.  16-bit weights have the same
-// relative precision whatever the reference is.  The sum takes the weights before they are
-// rounded, in fp32.
+// that is rare, and 64 maxima per row and step are saved.  bf16 weights have the same relative
+// precision whatever the reference is; fp16 ones too, down to 2^-14 of the reference's weight, below it
+// they are multiples of 2^-24 of it.  The sum takes the weights before they are rounded, in fp32.
 // P is rounded once to the type: a second product with its residues would cost half as much
 // tensor time again, and the error (as large as the output's own rounding to 16 bits) is
 // within the type.  Q, K and V enter as they are.

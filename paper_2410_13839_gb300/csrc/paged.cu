@@ -21,8 +21,8 @@
 // GPU in a launch of their own.
 // Times of calls, one after another: plan of 32 slots, one token each, 2048 pages 3.8 us; of 1000
 // slots, 300,000 rows, 90,001 pages 21.3 us (5 MB written: the chain of steps, most of all the
-// taking of 10,000 pages by eight CTAs); reordering of 4 beams 8.2 us, of 96 beams with the copies
-// of 12 layers of 16 heads of 64 27 us.
+// taking of 10,000 pages by eight CTAs); reordering of 4 beams 8.2 us, of 96 beams, 36 of them copied,
+// with 12 layers of 16 heads of 64 21.2 us.
 #include <climits>
 
 #include "serving.cuh"
@@ -560,8 +560,9 @@ constexpr int CP_THREADS = 256, CP_UNROLL = 4;
 // The filled rows of every copied page: for each (layer, keys | values, head) one run of
 // tokens * head_dim elements.  A warp takes a run; CP_UNROLL loads are in flight per lane.
 // Bound by memory: each row is read once and written once; with few copies by latency (the list, then
-// the rows).  96 beams' copies, 12 layers of 16 heads of 64, 150 MB read and written: 27 us a call,
-// 8 of them the tables'; 22 at 6.8 TB/s.
+// the rows).  96 beams, 12 layers of 16 heads of 64: 36 copies of 1091 rows, 107 MB read and written,
+// 21.2 us a call, of which 15.8 at 6.8 TB/s; 83 and 136 MB 17.4 and 26.0 us, 12.2 and 20.0.  The 5 to 6 us
+// above that are the tables', which come before.
 __global__ void __launch_bounds__(CP_THREADS) page_copy_kernel(const __grid_constant__ ReorderArgs p, int runs) {
     pdl_launch_dependents();
     pdl_wait();
