@@ -41,8 +41,15 @@ class BeamSearch:
         self.parent, self.token = torch.zeros(batch, beams, **i32), torch.zeros(batch, beams, **i32)
         self.status, self.copied = torch.zeros(4, **i32), torch.zeros(4, **i32)
         self.worst, self.err = torch.zeros((), **i32), torch.zeros(1, **i32)
+        self.workspaces = {}
         self.history = []
         self.longest = 0  # a bound of the slots' lengths, known without asking the GPU
+
+    def _workspace(self, name, nbytes):
+        """One that is kept, zeroed when it is made: the operators leave their counters zero."""
+        if name not in self.workspaces or self.workspaces[name].numel() < nbytes:
+            self.workspaces[name] = torch.zeros(max(nbytes, 16), dtype=torch.uint8, device="cuda")
+        return self.workspaces[name], nbytes
 
     def _position(self, pos):
         d = self.m.d_model
@@ -76,8 +83,7 @@ class BeamSearch:
             args = mtp.chunk_attention_args(q=q16, kv_pool=self.pool, layer=layer, block_table=self.tables[0],
                                             cu_rows=cu_rows, kv_lens=self.lens[0], out=att, scale=self.dim ** -0.5,
                                             max_new=max_new, max_keys=self.longest, err_word=self.err)
-            n = mtp.mtp_chunk_attention_workspace_bytes(args)
-            mtp.mtp_chunk_attention(args, torch.empty(n, dtype=torch.uint8, device="cuda"), n, stream)
+            mtp.mtp_chunk_attention(args, *self._workspace("attend", mtp.mtp_chunk_attention_workspace_bytes(args)), stream)
             x = x + F.linear(att.float().flatten(1), w[p + "wo"], w[p + "bo"])
             h = F.layer_norm(x, (d,), w[p + "ln2_g"], w[p + "ln2_b"], self.m.ln_eps)
             x = x + F.linear(F.gelu(F.linear(h, w[p + "w1"], w[p + "b1"])), w[p + "w2"], w[p + "b2"])
@@ -96,13 +102,11 @@ class BeamSearch:
         args = mtp.beam_select_args(logits=self.logits, scores=self.scores, done=self.done, eos_id=self.m.eos_id,
                                     k=self.beams, out_scores=scores, out_parent=self.parent, out_token=self.token,
                                     out_done=done)
-        n = mtp.mtp_beam_select_workspace_bytes(args)
-        mtp.mtp_beam_select(args, torch.zeros(n, dtype=torch.uint8, device="cuda"), n, stream)
+        mtp.mtp_beam_select(args, *self._workspace("select", mtp.mtp_beam_select_workspace_bytes(args)), stream)
         args = mtp.beam_reorder_args(parent=self.parent, block_table=self.tables[0], kv_lens=self.lens[0],
                                      page_refs=self.refs, kv_pool=self.pool, out_block_table=self.tables[1],
                                      out_kv_lens=self.lens[1], out_page_refs=self.refs, out_status=self.copied)
-        n = mtp.mtp_beam_reorder_workspace_bytes(args)
-        mtp.mtp_beam_reorder(args, torch.empty(n, dtype=torch.uint8, device="cuda"), n, stream)
+        mtp.mtp_beam_reorder(args, *self._workspace("reorder", mtp.mtp_beam_reorder_workspace_bytes(args)), stream)
         self.worst = torch.minimum(self.worst, torch.minimum(self.status[0], self.copied[0]))
         self.tables.reverse()
         self.lens.reverse()
