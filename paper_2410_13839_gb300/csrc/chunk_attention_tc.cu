@@ -21,7 +21,7 @@
 // steps of which its rows see no key.
 //
 // Two chunks of 2000 to 4000 tokens after 6000 to 9000, 32 heads on 8 of 128 dims (648 GFLOP): 446 to 471 us
-// (boxes differ), 1380 to 1450 TFLOP/s, of the measured peak (cuBLAS, 1922) about three quarters; the MMAs of 45 and 64
+// (GPUs differ), 1380 to 1450 TFLOP/s, of the measured peak (cuBLAS, 1922) about three quarters; the MMAs of 45 and 64
 // cycles fill about as much of the time.  64 dims, 16 heads (162 GFLOP): 212 us, 764 TFLOP/s: bound by
 // the softmax, whose 64 exponentials a row and step are as many as with 128 dims; a warp issues in
 // 44 % of the cycles and waits for results of its own the most.  25 prompts of 182 to 578 tokens,
