@@ -39,7 +39,6 @@ constexpr int PG_ONE_PAGES = 8192, PG_ONE_SLOTS = 1024, PG_ONE_ROWS = 1024, PG_O
 // 6.5 and 8.9.
 constexpr int PG_ROWS_HERE = 16384;
 constexpr int PG_MAX_SLOTS = 8192;
-constexpr int PG_MAX_PAGES = 1 << 22;
 constexpr int PG_MAX_ROWS = 1 << 24;
 
 struct FreeBits {
@@ -586,24 +585,6 @@ __global__ void __launch_bounds__(CP_THREADS) page_copy_kernel(const __grid_cons
                 if (q0 + u * 32 < pieces) dst[q0 + u * 32] = v[u];
         }
     }
-}
-
-int log2_of(int page_size) { return page_size == 16 ? 4 : page_size == 32 ? 5 : page_size == 64 ? 6 : 7; }
-
-int check_pool(const char* what, int n_pages, int layers, int layer, int n_kv_heads, int head_dim, int page_size) {
-    if (n_pages < 1 || n_pages > PG_MAX_PAGES || layers < 1 || layer < 0 || layer >= layers || n_kv_heads < 1 ||
-        n_kv_heads > 1024 || head_dim < 8 || head_dim > 256 || head_dim % 8 || !page_size_ok(page_size))
-        return invalid("%s: invalid pool (pages %d, layers %d, layer %d, heads %d, head_dim %d, page_size %d)", what,
-                       n_pages, layers, layer, n_kv_heads, head_dim, page_size);
-    return MTP_OK;
-}
-
-// Enqueue a kernel, clusters of `cluster` CTAs.  (The 48 KB that a kernel has without asking hold its static shared memory
-// too: any size is asked for.)
-template <class... P>
-cudaError_t launch(void (*kern)(P...), int grid, int threads, size_t smem, int cluster, cudaStream_t s, P... args) {
-    const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem);
-    return e == cudaSuccess ? launch_ex(kern, dim3(grid), threads, smem, s, cluster, args...) : e;
 }
 
 size_t reorder_workspace(int rows) { return 16 + (size_t)rows * sizeof(int4); }

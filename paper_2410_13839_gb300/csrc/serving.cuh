@@ -1,5 +1,6 @@
-// serving.cuh -- what the paged beam-search operators (paged.cu, beam.cu,
-// chunk_attention*.cu) share: argument errors, element types.
+// serving.cuh -- what the operators of the caller's own paged cache (paged.cu, beam.cu,
+// chunk_attention*.cu, rotary.cu, key_weights*.cu, verify.cu, evict.cu) share: argument
+// errors, launches, element types.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -61,8 +62,26 @@ cudaError_t launch_ex(void (*kern)(P...), dim3 grid, int threads, size_t smem, c
     return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
+// Enqueue a kernel, clusters of `cluster` CTAs.  (The 48 KB that a kernel has without asking hold its static shared memory
+// too: any size is asked for.)
+template <class... P>
+cudaError_t launch(void (*kern)(P...), int grid, int threads, size_t smem, int cluster, cudaStream_t s, P... args) {
+    const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), smem);
+    return e == cudaSuccess ? launch_ex(kern, dim3(grid), threads, smem, s, cluster, args...) : e;
+}
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 inline bool page_size_ok(int p) { return p == 16 || p == 32 || p == 64 || p == 128; }
+constexpr int PG_MAX_PAGES = 1 << 22;
+inline int log2_of(int page_size) { return page_size == 16 ? 4 : page_size == 32 ? 5 : page_size == 64 ? 6 : 7; }
+
+inline int check_pool(const char* what, int n_pages, int layers, int layer, int n_kv_heads, int head_dim, int page_size) {
+    if (n_pages < 1 || n_pages > PG_MAX_PAGES || layers < 1 || layer < 0 || layer >= layers || n_kv_heads < 1 ||
+        n_kv_heads > 1024 || head_dim < 8 || head_dim > 256 || head_dim % 8 || !page_size_ok(page_size))
+        return invalid("%s: invalid pool (pages %d, layers %d, layer %d, heads %d, head_dim %d, page_size %d)", what,
+                       n_pages, layers, layer, n_kv_heads, head_dim, page_size);
+    return MTP_OK;
+}
 
 // Element types of two bytes as raw bits: to and from fp32, rounded to nearest even.
 struct Bf16 {
