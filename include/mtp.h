@@ -676,6 +676,188 @@ MTP_API size_t mtp_beam_reorder_workspace_bytes(const mtp_beam_reorder_args* arg
 MTP_API int mtp_beam_reorder(const mtp_beam_reorder_args* args, void* workspace, size_t workspace_bytes,
                              void* cuda_stream);
 
+/* ---- speculative decoding over long contexts in the paged cache ---------
+ *
+ * What a program that verifies drafts on contexts with rotary positions needs next to the calls
+ * above, on the same pool, tables and counts, with the same conventions (device pointers, nothing
+ * synchronised, allocated or copied to the host, all may be captured in a CUDA graph, launched
+ * programmatically).  In the order of a step: mtp_page_plan, per layer mtp_rotary_append,
+ * mtp_chunk_attention (out_lse) and mtp_key_weights, then mtp_draft_verify, and mtp_cache_evict where
+ * contexts have grown past their budget.  Buffers of one call do not overlap except where that is said. */
+
+typedef enum mtp_rotary_layout { MTP_ROTARY_HALVES = 0, MTP_ROTARY_PAIRS = 1 } mtp_rotary_layout;
+typedef enum mtp_rotary_scaling {
+    MTP_ROTARY_PLAIN = 0,  /* f_i = base ^ (-2 i / rot_dim) radians per position                        */
+    MTP_ROTARY_LINEAR = 1, /* f_i / factor                                                              */
+    MTP_ROTARY_BASE = 2,   /* base * factor ^ (rot_dim / (rot_dim - 2)): the slowest pair is slowed down
+                              by factor, the fastest not at all                                         */
+    MTP_ROTARY_BANDS = 3   /* r_i f_i + (1 - r_i) f_i / factor, r_i = (context f_i / 2 pi - low) / (high - low),
+                              kept in 0..1: pairs of `high` turns and more in the trained context stay, those
+                              of `low` and fewer are slowed down                                        */
+} mtp_rotary_scaling;
+
+/* How far each of the rot_dim / 2 pairs turns per position, as a fraction of 2^64 of a turn, for
+ * mtp_rotary_append's `turns` (which stands in device memory: the caller copies them once).
+ * out_turns: host memory.  rot_dim even, 2 to 256 (4 with MTP_ROTARY_BASE); base > 1; factor >= 1;
+ * context > 0 and low < high with MTP_ROTARY_BANDS.  Errors: MTP_ERR_INVALID. */
+MTP_API int mtp_rotary_turns(int rot_dim, int scaling, double base, double factor, double context, double low,
+                             double high, uint64_t* out_turns);
+
+/* mtp_cache_append with rotary positions: the keys of a step's new tokens are turned and go into
+ * one layer of the cache with their values, the queries are turned into a buffer for
+ * mtp_chunk_attention.  The first rot_dim elements of each head are pairs (a, b), elements i and
+ * i + rot_dim / 2 (MTP_ROTARY_HALVES) or 2 i and 2 i + 1 (MTP_ROTARY_PAIRS), that become
+ * gain * (a cos t - b sin t, a sin t + b cos t) with t = position * turns[i]; the others, and the
+ * values, stay as they are.  Sines and cosines err by 2^-22 at most at any position, products are made in fp32, and
+ * each result is rounded once, to nearest even; elements that are not turned keep their bits where src_dtype is
+ * the pool's.
+ *   q          [rows][n_heads * head_dim], k, v [rows][n_kv_heads * head_dim] with row strides (elements) of
+ *              src_dtype (MTP_F32 or the pool's type); of one wider buffer, as a rule
+ *   positions  int32 [rows], any value
+ *   slot_map   int64 [rows], as mtp_cache_append: the keys and values of rows with a place outside the
+ *              pool are left out (their queries are turned); no place may occur twice
+ *   turns      uint64 [rot_dim / 2], mtp_rotary_turns
+ *   out_q      [rows][n_heads * head_dim] of the pool's type, row stride out_stride; not q itself
+ * head_dim: a multiple of 8, at most 256; rot_dim even, 2 to head_dim.  Errors: MTP_ERR_INVALID, MTP_ERR_CUDA. */
+typedef struct mtp_rotary_append_args {
+    int32_t rows, n_heads, n_kv_heads, head_dim, rot_dim, layout, page_size, layers, layer, n_pages, src_dtype, pool_dtype;
+    float gain;
+    int64_t q_stride, k_stride, v_stride, out_stride;
+    const void* q;
+    const void* k;
+    const void* v;
+    const int32_t* positions;
+    const int64_t* slot_map;
+    const uint64_t* turns;
+    void* kv_pool;
+    void* out_q;
+} mtp_rotary_append_args;
+MTP_API int mtp_rotary_append(const mtp_rotary_append_args* args, void* cuda_stream);
+
+/* The attention weight that each cached key gets from a step's tokens, added up: what
+ * mtp_cache_evict chooses by.  Rows, slots, masks and the cache are mtp_chunk_attention's; key j
+ * of a slot and key head gets the sum over the rows i that see it and the query heads of the key head of
+ *   exp(scale * q_i . k_j - lse_i).
+ * It is added to the weight that the key has; the keys of the new tokens themselves begin at 0.  Weights
+ * of keys that no row sees, and past a slot's length, are left as they are.  (What drafts that are not
+ * kept have added stays.)
+ *   lse       float [rows][n_heads]: mtp_chunk_attention's out_lse
+ *   weights   float [slots][layers][n_kv_heads][bt_stride * page_size], read and written in place
+ *   max_new, max_keys  host-known upper bounds of a slot's new tokens and length; rows and keys
+ *             past them are left out, and MTP_DEVICE_ERR_BOUNDS says so in err_word, as for rows outside the
+ *             buffers and lengths outside the table
+ *   err_word  int32 on the device or NULL: MTP_DEVICE_ERR_* bits are ORed in
+ *   workspace mtp_key_weights_workspace_bytes(args) bytes, 16-byte aligned, of any content (0: may be NULL);
+ *             calls that overlap need workspaces of their own
+ * Products and sums are held in 32 bits and added in an order that the sizes alone decide.  A key or
+ * query that is not finite makes no difference to the weights of other keys and slots, nor do keys past a slot's
+ * length.  Limits as mtp_chunk_attention's.  Errors: MTP_ERR_INVALID, MTP_ERR_CUDA. */
+typedef struct mtp_key_weights_args {
+    int32_t slots, rows, n_heads, n_kv_heads, head_dim, page_size, layers, layer, n_pages, bt_stride, dtype, window,
+        max_new, max_keys;
+    float scale;
+    int64_t q_stride;
+    const void* q;
+    const void* kv_pool;
+    const int32_t* block_table;
+    const int32_t* cu_rows;
+    const int32_t* kv_lens;
+    const float* lse;
+    float* weights;
+    int32_t* err_word;
+} mtp_key_weights_args;
+MTP_API size_t mtp_key_weights_workspace_bytes(const mtp_key_weights_args* args);
+MTP_API int mtp_key_weights(const mtp_key_weights_args* args, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Which of a step's drafted tokens stay, the token after them, and the pages of what does not.
+ * Slot s has the rows cu_rows[s] .. cu_rows[s + 1] - 1, its last n = cu_rows[s + 1] - cu_rows[s] tokens, all cached:
+ * the last token that is certain, then n - 1 drafts; logits[r] are the target's behind row r.  With
+ *   p = softmax(logits / T), q = softmax(draft_logits / T) of the row, or without draft_logits 1 on the draft,
+ * the draft d fed at row r + 1 is kept where the ones before it are and u q(d) < p(d), u = uniforms[r][0].  A kept
+ * draft that is eos_id is the last token.  Else one more is drawn: behind the last kept of all drafts from w = p,
+ * behind a draft that is not kept from w = max(p - q, 0) (where that is nothing, from p): the first token t with
+ * w_0 + .. + w_t > v (w_0 + ..), v = uniforms[r][1] of the row r it is drawn behind.  So drawn, tokens are
+ * distributed as the target's.  T <= 0 (or NaN): the likeliest token, the lowest of equal ones, is all of p;
+ * a draft is kept where it is that one.
+ *   logits       [rows] rows of vocab, row stride logits_stride (elements), of logits_dtype (MTP_F32, MTP_BF16, MTP_F16)
+ *   draft_logits as logits (stride draft_stride), or NULL; of a slot's last row nothing is read
+ *   temperature  float [slots], or NULL: 1
+ *   tokens       int32 [rows]: the token fed at each row; a draft outside the vocabulary is not kept
+ *   uniforms     float [rows][2] in [0, 1) (other values count as the nearest, NaN as 0)
+ *   kv_lens      int32 [slots]: lengths with all n tokens
+ *   eos_id       the end's token, -1 = none
+ *   out_tokens   int32 [slots][max_new]: the kept drafts, the token drawn, then -1
+ *   out_counts   int32 [slots]: tokens of a slot's row of out_tokens
+ *   out_kv_lens  int32 [slots]: kv_lens less the drafts that are not kept (may be kv_lens itself; the token drawn
+ *                is not cached yet)
+ *   out_done     int32 [slots] or NULL: 1 where eos_id is among the tokens
+ *   block_table, page_refs  or both NULL: pages that a slot no longer reaches leave its row of the table
+ *                (-1), and their counts drop by 1
+ *   err_word     int32 on the device or NULL.  A slot without rows gets no token.  Nor does one whose rows do not lie in
+ *                the buffers, or are more than max_new or than its length, or whose length is outside the
+ *                table: it stays as it is, and MTP_DEVICE_ERR_BOUNDS says so, as where a page that is given back
+ *                is not in the pool or has a count below 1
+ * A logit of NaN or -infinity counts as -10^38, infinity as 10^38; T as 10^-30 to 10^30.  Borders between tokens are exact to 2^-36
+ * or so of the sum, and the outcome is the same in every call.
+ * Limits: slots <= 8192, max_new <= 64, vocab <= 2^18, bt_stride * page_size <= 2^30.
+ * Errors: MTP_ERR_INVALID, MTP_ERR_CUDA. */
+typedef struct mtp_draft_verify_args {
+    int32_t slots, rows, vocab, max_new, eos_id, logits_dtype, page_size, bt_stride, n_pages;
+    int64_t logits_stride, draft_stride;
+    const void* logits;
+    const void* draft_logits;
+    const float* temperature;
+    const int32_t* tokens;
+    const float* uniforms;
+    const int32_t* cu_rows;
+    const int32_t* kv_lens;
+    int32_t* block_table;
+    int32_t* page_refs;
+    int32_t* out_tokens;
+    int32_t* out_counts;
+    int32_t* out_kv_lens;
+    int32_t* out_done;
+    int32_t* err_word;
+} mtp_draft_verify_args;
+MTP_API int mtp_draft_verify(const mtp_draft_verify_args* args, void* cuda_stream);
+
+/* Contexts brought down to a budget of keys.  A slot longer than keep[s] keeps that many keys in every layer
+ * and key head, each of which makes its own choice: the first `sinks`, the last `recent` (as far as the budget
+ * goes, sinks first), and of the others those of largest weight, equal ones in their order (NaN above all).
+ * The keys that stay, with their values and weights, move up in their order to places 0 .. keep[s] - 1, in the
+ * slot's first pages; its other pages leave the table, and their counts drop by 1.
+ *   kv_lens, keep    int32 [slots]
+ *   block_table      int32 [slots][bt_stride]; page_refs int32 [n_pages]
+ *   weights          float [slots][layers][n_kv_heads][bt_stride * page_size], as mtp_key_weights makes them
+ *   kv_pool          the pool, all layers; written in place
+ *   out_kv_lens, out_block_table, out_weights  as kv_lens, block_table and weights, in buffers of their own; table
+ *                    entries past a slot's last page are -1, weights past its length are left as they are
+ *   out_page_refs    int32 [n_pages] (may be page_refs itself)
+ *   out_status       int32 [slots]: MTP_OK, or MTP_ERR_INVALID (a length outside the table, a keep below 0, a held
+ *                    page outside the pool or with a count below 1, or one that would be written, from the one
+ *                    behind the sinks on, that other slots hold too): such a slot stays as it is
+ *   workspace        mtp_cache_evict_workspace_bytes(args) bytes, 16-byte aligned, of any content
+ * Slots within their budgets stay as they are.  Positions turned into keys are not changed: the tokens that
+ * follow go on counting from the text's length, not from the cache's.
+ * Limits: slots <= 8192, bt_stride * page_size <= 2^24, head_dim a multiple of 8, at most 256.
+ * Errors: MTP_ERR_INVALID, MTP_ERR_CUDA. */
+typedef struct mtp_cache_evict_args {
+    int32_t slots, page_size, n_pages, bt_stride, layers, n_kv_heads, head_dim, pool_dtype, sinks, recent;
+    const int32_t* kv_lens;
+    const int32_t* keep;
+    const int32_t* block_table;
+    const int32_t* page_refs;
+    const float* weights;
+    void* kv_pool;
+    int32_t* out_kv_lens;
+    int32_t* out_block_table;
+    int32_t* out_page_refs;
+    float* out_weights;
+    int32_t* out_status;
+} mtp_cache_evict_args;
+MTP_API size_t mtp_cache_evict_workspace_bytes(const mtp_cache_evict_args* args);
+MTP_API int mtp_cache_evict(const mtp_cache_evict_args* args, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -35,6 +35,12 @@ MTP_OPT_PERSISTENT = 9
 MTP_OPT_PREFILL_TC = 10
 MTP_OPT_HEADS_FUSED = 11
 MTP_OPT_GEMM_CLUSTER = 12
+MTP_ROTARY_HALVES = 0
+MTP_ROTARY_PAIRS = 1
+MTP_ROTARY_PLAIN = 0
+MTP_ROTARY_LINEAR = 1
+MTP_ROTARY_BASE = 2
+MTP_ROTARY_BANDS = 3
 KERNEL_KINDS = ("embed", "attn_block", "mlp", "heads", "select", "save", "pack", "gemm", "qkv", "attn", "step", "step_attn",
                 "step_mlp", "step_cta", "attn_tc")
 
@@ -77,6 +83,23 @@ MtpBeamSelectArgs = _struct(
 MtpBeamReorderArgs = _struct(
     "MtpBeamReorderArgs", "batch beams page_size n_pages bt_stride layers n_kv_heads head_dim pool_dtype", "",
     "parent block_table kv_lens page_refs kv_pool out_block_table out_kv_lens out_page_refs out_status")
+MtpRotaryAppendArgs = _struct(
+    "MtpRotaryAppendArgs",
+    "rows n_heads n_kv_heads head_dim rot_dim layout page_size layers layer n_pages src_dtype pool_dtype",
+    "q_stride k_stride v_stride out_stride", "q k v positions slot_map turns kv_pool out_q", "gain")
+MtpKeyWeightsArgs = _struct(
+    "MtpKeyWeightsArgs",
+    "slots rows n_heads n_kv_heads head_dim page_size layers layer n_pages bt_stride dtype window max_new max_keys",
+    "q_stride", "q kv_pool block_table cu_rows kv_lens lse weights err_word", "scale")
+MtpDraftVerifyArgs = _struct(
+    "MtpDraftVerifyArgs", "slots rows vocab max_new eos_id logits_dtype page_size bt_stride n_pages",
+    "logits_stride draft_stride",
+    "logits draft_logits temperature tokens uniforms cu_rows kv_lens block_table page_refs out_tokens out_counts "
+    "out_kv_lens out_done err_word")
+MtpCacheEvictArgs = _struct(
+    "MtpCacheEvictArgs", "slots page_size n_pages bt_stride layers n_kv_heads head_dim pool_dtype sinks recent", "",
+    "kv_lens keep block_table page_refs weights kv_pool out_kv_lens out_block_table out_page_refs out_weights "
+    "out_status")
 
 
 class MTPError(RuntimeError):
@@ -129,6 +152,13 @@ def _load() -> ctypes.CDLL:
         "mtp_beam_select": (i32, [ctypes.POINTER(MtpBeamSelectArgs), vp, sz, vp]),
         "mtp_beam_reorder_workspace_bytes": (sz, [ctypes.POINTER(MtpBeamReorderArgs)]),
         "mtp_beam_reorder": (i32, [ctypes.POINTER(MtpBeamReorderArgs), vp, sz, vp]),
+        "mtp_rotary_turns": (i32, [i32, i32] + 5 * [ctypes.c_double] + [vp]),
+        "mtp_rotary_append": (i32, [ctypes.POINTER(MtpRotaryAppendArgs), vp]),
+        "mtp_key_weights_workspace_bytes": (sz, [ctypes.POINTER(MtpKeyWeightsArgs)]),
+        "mtp_key_weights": (i32, [ctypes.POINTER(MtpKeyWeightsArgs), vp, sz, vp]),
+        "mtp_draft_verify": (i32, [ctypes.POINTER(MtpDraftVerifyArgs), vp]),
+        "mtp_cache_evict_workspace_bytes": (sz, [ctypes.POINTER(MtpCacheEvictArgs)]),
+        "mtp_cache_evict": (i32, [ctypes.POINTER(MtpCacheEvictArgs), vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)

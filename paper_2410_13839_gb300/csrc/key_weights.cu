@@ -1,0 +1,310 @@
+// key_weights.cu -- the attention weight that each cached key gets from a step's tokens
+// (mtp_key_weights): its entry point, the kernel of few rows per slot and key head
+// (decoding steps, drafts), and the sum over row segments.
+//
+//   w_j (+)= sum_p 2^(c q_p . k_j - l_p),  c = scale log2 e, l_p = lse_p log2 e,
+//
+// over the rows p (tokens and query heads of the key head) that see key j: one product and one
+// exponential a pair, no maximum and no second pass, as the log-sum-exps are there.
+//
+// Few rows: the keys are read once and memory bounds it.  A warp takes 16 keys at a time as M of
+// mma.sync (rows as N, eight at a time) straight from global memory into registers: the order of
+// the dimensions in a product is free, so a lane's 16 bytes of a key serve two steps of 16, and
+// its 16 bytes of a query row, taken in the same order, the same two.  No shared memory, no
+// barrier; every warp has several tiles' loads in flight.
+#include <algorithm>
+
+#include "weights.cuh"
+
+namespace mtp {
+
+int tc_encode_cache(CUtensorMap* map, const void* pool, int dtype, int head_dim, int page_size, uint64_t blocks,
+                    int box_rows);
+int tc_encode_queries(CUtensorMap* map, const void* q, int dtype, int head_dim, int heads, uint64_t rows, uint64_t stride,
+                      int group);
+
+namespace {
+
+constexpr int KW_THREADS = 128, KW_WARPS = KW_THREADS / 32;
+constexpr int KW_FEW_ROWS = 32;  // packed rows up to which this file's kernel is used
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <class T>
+__device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma16<Bf16>(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma16<F16>(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Grid (chunk of keys and key head, slot).  NT: tiles of eight rows; KT: tiles of 16 keys that a warp has in flight.
+template <class T, int HD, int NT, int KT>
+__global__ void __launch_bounds__(KW_THREADS) key_weights_kernel(const __grid_constant__ WeightsArgs a, int chunk) {
+    constexpr int B = HD / 32;  // 16-byte pieces of a row per lane: dimensions 32 b + 8 (lane % 4) .. + 7
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = blockIdx.x / a.kv_heads, head = blockIdx.x - part * a.kv_heads, slot = blockIdx.y;
+    pdl_launch_dependents();
+    pdl_wait();
+    bool cut;
+    const WeightsSlot s = weights_slot(a, slot, cut);
+    if (cut && a.err && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.err, ERR_BOUNDS);
+    const int rows = s.n * a.group, first = part * chunk, last = min(min(s.len, a.keys), first + chunk);
+    if (rows == 0 || first >= last) return;
+    const int lowest = a.window > 0 ? max(0, s.base - a.window + 1) : 0;  // the first key that some row sees
+    if (last <= lowest) return;
+
+    // the rows: fragments, log-sum-exps and positions of columns 2 (lane % 4), + 1 of every tile
+    uint4 q[NT][B];
+    float l[NT][2];
+    int pos[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int p = t * 8 + (lane >> 2), token = p / a.group;
+        const uint16_t* src = a.q + (long long)(s.row0 + token) * a.q_stride + (head * a.group + p - token * a.group) * HD + (lane & 3) * 8;
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (p < rows) {
+                if (a.q_vec) {
+                    v = *reinterpret_cast<const uint4*>(src + b * 32);
+                } else {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = (uint32_t)src[b * 32 + 2 * e] | (uint32_t)src[b * 32 + 2 * e + 1] << 16;
+                    v = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+            q[t][b] = v;
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int c = t * 8 + (lane & 3) * 2 + e, token = c / a.group;
+            l[t][e] = 0.f;
+            pos[t][e] = -1;
+            if (c < rows) {
+                l[t][e] = a.lse[(long long)(s.row0 + token) * (a.kv_heads * a.group) + head * a.group + c - token * a.group] * LOG2E;
+                pos[t][e] = s.base + token;
+            }
+        }
+    }
+    const int* table = a.block_table + (size_t)slot * a.bt_stride;
+    float* out = a.weights + slot * a.w_slot + (long long)head * a.width;
+    const int r = lane >> 2, end = s.base + s.n;  // this lane's keys r, r + 8 of a tile
+    const int from = max(first, lowest & ~15);
+    for (int key0 = from + warp * 16 * KT; key0 < last; key0 += KW_WARPS * 16 * KT) {
+        uint4 k[KT][2][B];
+        float old[KT];
+#pragma unroll
+        for (int j = 0; j < KT; ++j) {
+            const int key = key0 + j * 16;
+            const int page = key < last ? table[key >> a.page_shift] : -1;
+            const bool there = page >= 0 && page < a.n_pages;
+            const uint16_t* src = a.pool + ((((long long)page * a.page_blocks + a.layer_block + head) << a.page_shift) + (key & ((1 << a.page_shift) - 1)) + r) * HD + (lane & 3) * 8;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int b = 0; b < B; ++b)
+                    k[j][h][b] = there ? *reinterpret_cast<const uint4*>(src + h * 8 * HD + b * 32) : make_uint4(0u, 0u, 0u, 0u);
+            const int mine = key + r + (lane & 1) * 8;
+            old[j] = (lane & 3) < 2 && mine < last && mine < s.base ? out[mine] : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < KT; ++j) {
+            const int key = key0 + j * 16;
+            if (key >= last) break;
+            float sum[2] = {0.f, 0.f};
+            const bool inner = key + 15 <= s.base && (a.window <= 0 || key > end - 1 - a.window) && rows == NT * 8;  // every row sees all
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int b = 0; b < B; ++b) {
+                    const uint4 x = k[j][0][b], y = k[j][1][b], z = q[t][b];
+                    mma16<T>(d, x.x, y.x, x.y, y.y, z.x, z.y);
+                    mma16<T>(d, x.z, y.z, x.w, y.w, z.z, z.w);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float w = ex2(fmaf(d[2 * h + e], a.scale_log2, -l[t][e]));
+                        const int at = key + r + h * 8;
+                        if (!inner && (at > pos[t][e] || (a.window > 0 && at <= pos[t][e] - a.window))) w = 0.f;
+                        sum[h] += w;
+                    }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                sum[h] += __shfl_xor_sync(FULL_MASK, sum[h], 1);
+                sum[h] += __shfl_xor_sync(FULL_MASK, sum[h], 2);
+            }
+            const int mine = key + r + (lane & 1) * 8;
+            if ((lane & 3) < 2 && mine < last && mine >= lowest) out[mine] = old[j] + (lane & 1 ? sum[1] : sum[0]);
+        }
+    }
+}
+
+// The segments' sums, in their order, onto what the keys had.  Grid (keys / 256, key head, slot).
+__global__ void __launch_bounds__(256) key_weights_sum_kernel(const __grid_constant__ WeightsArgs a) {
+    const int key = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y, slot = blockIdx.z;
+    pdl_launch_dependents();
+    pdl_wait();
+    bool cut;
+    const WeightsSlot s = weights_slot(a, slot, cut);
+    const int lowest = a.window > 0 ? max(0, s.base - a.window + 1) : 0;
+    if (s.n == 0 || key >= min(s.len, a.keys) || key < lowest) return;
+    float* out = a.weights + slot * a.w_slot + (long long)head * a.width + key;
+    float w = key < s.base ? *out : 0.f;
+    const size_t step = (size_t)a.slots * a.kv_heads * a.width;
+    const float* part = a.part + ((size_t)slot * a.kv_heads + head) * a.width + key;
+    float sum = 0.f;
+    for (int i = 0; i < a.segments; ++i) sum += part[i * step];
+    *out = w + sum;
+}
+
+// How a call runs.
+struct WeightsPlan {
+    bool few;
+    int group, key_tiles, segments;
+    size_t need;
+};
+constexpr int KW_TILE = 128;
+
+int weights_plan(const mtp_key_weights_args* a, WeightsPlan* p) {
+    if (!a || a->slots < 1 || a->slots > KW_MAX_SLOTS || a->rows < 0 || a->n_heads < 1 || a->n_kv_heads < 1 ||
+        a->n_heads % a->n_kv_heads || a->n_heads / a->n_kv_heads > 64 || a->n_heads > 1024)
+        return invalid("key_weights: invalid sizes (slots, rows or heads)");
+    if (a->head_dim != 64 && a->head_dim != 128) return invalid("key_weights: head_dim %d: 64 or 128", a->head_dim);
+    if (!page_size_ok(a->page_size) || a->layers < 1 || a->layer < 0 || a->layer >= a->layers || a->n_pages < 1 ||
+        a->bt_stride < 1 || (long long)a->bt_stride * a->page_size > (1 << 24) ||
+        (long long)a->n_pages * a->layers * 2 * a->n_kv_heads > 0x7fffffffLL)
+        return invalid("key_weights: invalid cache (page_size %d, layers %d, layer %d, pages %d, bt_stride %d)",
+                       a->page_size, a->layers, a->layer, a->n_pages, a->bt_stride);
+    if (a->dtype != MTP_BF16 && a->dtype != MTP_F16) return invalid("key_weights: dtype %d", a->dtype);
+    if (a->window < 0 || a->max_new < 0 || a->max_keys < 0 || !(a->scale > 0.f) || !(a->scale < 1e30f))
+        return invalid("key_weights: window %d, max_new %d, max_keys %d, scale %g", a->window, a->max_new, a->max_keys,
+                       (double)a->scale);
+    p->group = a->n_heads / a->n_kv_heads;
+    if ((long long)a->rows * p->group >= 1 << 21)
+        return invalid("key_weights: %d rows of %d query heads per key head: below %d together", a->rows, p->group, 1 << 21);
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        cudaGetLastError();
+        return report_error(MTP_ERR_CUDA, "key_weights: no usable CUDA device");
+    }
+    const long long width = (long long)a->bt_stride * a->page_size;
+    const long long packed = (long long)std::min(a->max_new, a->rows) * p->group;  // rows of a slot and key head
+    p->few = packed <= KW_FEW_ROWS;
+    p->key_tiles = (int)((std::min((long long)a->max_keys, width) + KW_TILE - 1) / KW_TILE);
+    p->segments = 1;
+    p->need = 0;
+    if (!p->few) {
+        // few keys and many rows: the rows are cut too, until every SM has tiles enough
+        const long long tiles = std::max(1ll, (long long)a->slots * a->n_kv_heads * p->key_tiles);
+        const long long row_tiles = (packed + KW_TILE - 1) / KW_TILE;
+        p->segments = (int)std::max(1ll, std::min((row_tiles + 3) / 4, 4ll * sms / tiles));
+        if (p->segments > 1) p->need = (size_t)p->segments * a->slots * a->n_kv_heads * width * sizeof(float);
+    }
+    return MTP_OK;
+}
+
+template <class T, int HD>
+cudaError_t launch_few(const WeightsArgs& a, cudaStream_t s) {
+    const int packed = std::min(a.max_new, a.rows) * a.group;
+    constexpr int KT = HD == 64 ? 4 : 2;
+    // a CTA's keys: each warp a few times its tiles
+    const int chunk = KW_WARPS * 16 * KT * 2;
+    const dim3 grid((a.keys + chunk - 1) / chunk * a.kv_heads, a.slots);
+    const auto kern = packed <= 8 ? key_weights_kernel<T, HD, 1, KT> : packed <= 16 ? key_weights_kernel<T, HD, 2, KT> : key_weights_kernel<T, HD, 4, KT>;
+    return launch_ex(kern, grid, KW_THREADS, 0, s, 1, a, chunk);
+}
+
+}  // namespace
+}  // namespace mtp
+
+using namespace mtp;
+
+extern "C" {
+
+MTP_API size_t mtp_key_weights_workspace_bytes(const mtp_key_weights_args* a) {
+    size_t need = 0;
+    guarded([&]() -> int {
+        WeightsPlan p;
+        const int r = weights_plan(a, &p);
+        need = r == MTP_OK ? p.need : 0;
+        return r;
+    });
+    return need;
+}
+
+MTP_API int mtp_key_weights(const mtp_key_weights_args* a, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    return guarded([&]() -> int {
+        WeightsPlan p;
+        if (const int r = weights_plan(a, &p)) return r;
+        if (a->q_stride < a->n_heads * a->head_dim)
+            return invalid("key_weights: row stride %lld below %d", (long long)a->q_stride, a->n_heads * a->head_dim);
+        if (a->rows == 0 || a->max_new == 0 || a->max_keys == 0) return MTP_OK;  // no new tokens
+        if (!a->q || !a->kv_pool || !a->block_table || !a->cu_rows || !a->kv_lens || !a->lse || !a->weights)
+            return invalid("key_weights: null pointer");
+        if (!aligned16(a->kv_pool)) return invalid("key_weights: kv_pool must be 16-byte aligned");
+        if (reinterpret_cast<uintptr_t>(a->q) & 1 || (reinterpret_cast<uintptr_t>(a->lse) | reinterpret_cast<uintptr_t>(a->weights)) & 3)
+            return invalid("key_weights: q, lse and weights must be aligned to their elements");
+        if (p.need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < p.need))
+            return invalid("key_weights: workspace %zu bytes, need %zu, 16-byte aligned", workspace_bytes, p.need);
+        WeightsArgs w;
+        w.q = static_cast<const uint16_t*>(a->q);
+        w.pool = static_cast<const uint16_t*>(a->kv_pool);
+        w.block_table = a->block_table; w.cu_rows = a->cu_rows; w.kv_lens = a->kv_lens; w.lse = a->lse;
+        w.width = a->bt_stride * a->page_size;
+        w.weights = a->weights + (size_t)a->layer * a->n_kv_heads * w.width;
+        w.w_slot = (long long)a->layers * a->n_kv_heads * w.width;
+        w.q_stride = a->q_stride;
+        w.slots = a->slots; w.rows = a->rows; w.kv_heads = a->n_kv_heads; w.group = p.group; w.dim = a->head_dim;
+        w.page_shift = log2_of(a->page_size);
+        w.bt_stride = a->bt_stride; w.n_pages = a->n_pages;
+        w.page_blocks = a->layers * 2 * a->n_kv_heads;
+        w.layer_block = a->layer * 2 * a->n_kv_heads;
+        // (no position passes the table: a window as long leaves nothing out, and sums with it stay in 32 bits)
+        w.window = a->window < w.width ? a->window : 0;
+        w.max_new = a->max_new;
+        w.keys = std::min(a->max_keys, w.width);
+        w.segments = p.segments;
+        w.part = static_cast<float*>(workspace);
+        w.q_vec = aligned16(a->q) && a->q_stride % 8 == 0;
+        w.scale_log2 = a->scale * LOG2E;
+        w.err = a->err_word;
+        const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+        if (p.few) {
+            auto few = [&](auto type) {
+                using T = decltype(type);
+                return a->head_dim == 64 ? launch_few<T, 64>(w, s) : launch_few<T, 128>(w, s);
+            };
+            return cuda_status(a->dtype == MTP_BF16 ? few(Bf16{}) : few(F16{}), "key_weights");
+        }
+        CUtensorMap map, q_map = {};
+        if (tc_encode_cache(&map, a->kv_pool, a->dtype, a->head_dim, a->page_size, (uint64_t)a->n_pages * w.page_blocks,
+                            std::min(a->page_size, KW_TILE)) != 0)
+            return report_error(MTP_ERR_CUDA, "key_weights: cuTensorMapEncodeTiled failed");
+        const bool q_tma = w.q_vec && a->q_stride < (1ll << 38) &&
+                           tc_encode_queries(&q_map, a->q, a->dtype, a->head_dim, a->n_heads, a->rows, a->q_stride, p.group) == 0;
+        cudaError_t e = launch_weights_tc(w, map, q_map, q_tma, a->dtype, p.key_tiles, s);
+        if (e == cudaSuccess && p.segments > 1)
+            e = launch_ex(key_weights_sum_kernel, dim3((w.keys + 255) / 256, w.kv_heads, w.slots), 256, 0, s, 1, w);
+        return cuda_status(e, "key_weights");
+    });
+}
+
+}  // extern "C"

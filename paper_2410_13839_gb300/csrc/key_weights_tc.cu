@@ -1,0 +1,319 @@
+// key_weights_tc.cu -- the kernel of mtp_key_weights for more than 32 rows per slot and key
+// head (prompts, chunks): tcgen05.
+//
+//   S^T = K Q^T        128 keys x up to 128 packed rows, fp32 in TMEM
+//   w_j += sum_p 2^(c S_jp - l_p)   a key per thread
+//
+// A CTA has 128 keys of a slot and key head, which stay in shared memory; the rows that see one
+// of them come by, as many tokens as have 128 rows at a time (all heads of a token together, so
+// that one tensor-map box is a tile for any number of heads per key head).  A thread's TMEM lane is its
+// key: its weights add up in a register, the rows' log-sum-exps are read from shared memory, the
+// same one by all lanes, and what a causal or window mask leaves of a tile is a range of columns.  Two
+// places for S: while one is summed the tensor cores make the next.  A tile's sum starts anew
+// and is added to the key's with compensation, so that thousands of rows cost no precision.
+// Two CTAs an SM (each half of TMEM): one's start and end lie behind the other's work.
+#include <type_traits>
+
+#include "tcgen05.cuh"
+#include "weights.cuh"
+
+namespace mtp {
+namespace {
+
+constexpr int WT_TILE = 128;
+constexpr uint32_t WT_SUB = 128 * 128;  // 128 rows of 128 bytes
+constexpr int WT_MMA = 4, WT_COPY = 5, WT_THREADS = 192;
+
+template <int HD>
+struct WtLayout {
+    static constexpr int STAGES = HD == 64 ? 4 : 2;
+    static constexpr uint32_t OPER = WT_SUB * (HD / 64);
+    static constexpr uint32_t K = 0, Q = OPER, LSE = Q + STAGES * OPER;  // LSE: [4 warps][2][128] floats
+    static constexpr size_t BYTES = 1024 + LSE + 4 * 2 * WT_TILE * 4;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void tma_box(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+            smem_addr(dst)),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_addr(bar))
+        : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
+template <class T>
+__device__ __forceinline__ uint32_t idesc(int n) {  // f16_idesc's types are bf16; fp16's codes are 0
+    const uint32_t d = f16_idesc(WT_TILE, n, false);
+    return std::is_same<T, Bf16>::value ? d : d & ~((1u << 7) | (1u << 10));
+}
+
+// Grid (key tile and key head, slot, row segment).
+template <class T, int HD>
+__global__ void __launch_bounds__(WT_THREADS, 2)
+    key_weights_tc_kernel(const __grid_constant__ WeightsArgs a, const __grid_constant__ CUtensorMap map,
+                          const __grid_constant__ CUtensorMap q_map, int q_tma) {
+    using L = WtLayout<HD>;
+    constexpr int ST = L::STAGES;
+    extern __shared__ unsigned char wt_raw[];
+    __shared__ uint64_t k_full, q_full[ST], q_empty[ST], s_full[2], s_empty[2], drain;
+    __shared__ uint32_t tmem_base;
+    unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(wt_raw) + 1023) & ~(uintptr_t)1023);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tile = blockIdx.x / a.kv_heads, head = blockIdx.x - tile * a.kv_heads, slot = blockIdx.y, seg = blockIdx.z;
+    pdl_launch_dependents();
+    pdl_wait();
+    bool cut;
+    const WeightsSlot s = weights_slot(a, slot, cut);
+    if (cut && a.err && blockIdx.x == 0 && seg == 0 && tid == 0) atomicOr(a.err, ERR_BOUNDS);
+    const int key0 = tile * WT_TILE, key1 = min(min(s.len, a.keys), key0 + WT_TILE);
+    if (s.n == 0 || key0 >= key1) return;
+    // the tokens that see a key of the tile, `per` at a time; this segment's tiles of them
+    const int2 tokens = seeing(a, s, key0, key1);
+    const int per = WT_TILE / a.group, all = (tokens.y - tokens.x + per - 1) / per;
+    const int u0 = (int)((long long)all * seg / a.segments), u1 = (int)((long long)all * (seg + 1) / a.segments);
+    const int lowest = a.window > 0 ? max(0, s.base - a.window + 1) : 0;  // the first key that some row sees
+    const int key = key0 + tid;
+    const bool mine = tid < WT_TILE && key < key1 && key >= lowest;
+    float* part = a.part + (((size_t)seg * a.slots + slot) * a.kv_heads + head) * a.width + key;
+    if (u0 >= u1) {
+        if (a.segments > 1 && mine) *part = 0.f;
+        return;
+    }
+    if (warp == WT_MMA) {
+        tmem_alloc(&tmem_base, 2 * WT_TILE);
+        tmem_relinquish();
+    }
+    if (tid == 0) {
+        mbar_init(&k_full, 1);
+        mbar_init(&drain, 1);
+        for (int i = 0; i < ST; ++i) {
+            mbar_init(&q_full[i], 1);
+            mbar_init(&q_empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s_full[i], 1);
+            mbar_init(&s_empty[i], 4);
+        }
+        fence_barrier_init();
+    }
+    // rows of a tile past the last token's are zeros
+    for (int i = tid; i < (WT_TILE - per * a.group) * 8 * (HD / 64) * ST; i += WT_THREADS) {
+        const int row = per * a.group + i / 8 % (WT_TILE - per * a.group), half = i / 8 / (WT_TILE - per * a.group);
+        *reinterpret_cast<uint4*>(sm + L::Q + half * WT_SUB + row * 128 + (i & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+    }
+    fence_proxy_async();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_base;
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(FULL_MASK, mbar_wait(bar, parity & 1, a.err)) != 0; };
+
+    if (warp == WT_COPY) {
+        // ---- the keys, a lane per page piece, then the rows ----
+        const int P = 1 << a.page_shift, box = min(P, WT_TILE), pieces = WT_TILE / box;
+        const int sub = lane % pieces, half = lane / pieces, at = key0 + sub * box;
+        const bool wanted = half < HD / 64 && at < key1;
+        int block = -1;  // outside the pool: zeros
+        if (wanted) {
+            const int page = a.block_table[(size_t)slot * a.bt_stride + (at >> a.page_shift)];
+            if (page >= 0 && page < a.n_pages) block = page * a.page_blocks + a.layer_block + head;
+        }
+        const unsigned have = __ballot_sync(FULL_MASK, wanted);
+        if (lane == 0) mbar_arrive_expect_tx(&k_full, __popc(have) * box * 128);
+        __syncwarp();
+        if (wanted) tma_box(sm + L::K + half * WT_SUB + sub * box * 128, &map, half * 64, at & (P - 1), block, &k_full);
+        bool ok = true;
+        int n = 0;
+        for (; n < u1 - u0; ++n) {
+            const int st = n % ST, token = tokens.x + (u0 + n) * per, count = min(per, tokens.y - token);
+            if (n >= ST && !(ok = wait(&q_empty[st], n / ST - 1))) break;
+            unsigned char* dst = sm + L::Q + st * L::OPER;
+            if (q_tma) {
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(&q_full[st], per * a.group * 128 * (HD / 64));
+                    for (int h = 0; h < HD / 64; ++h)
+                        tma_box(dst + h * WT_SUB, &q_map, h * 64, head * a.group, s.row0 + token, &q_full[st]);
+                }
+            } else {  // rows that a tensor map cannot describe: a lane 16 bytes of a row
+                for (int i = lane; i < count * a.group * (HD / 8); i += 32) {
+                    const int r = i / (HD / 8), c = i - r * (HD / 8), t = r / a.group;
+                    const uint16_t* src = a.q + (long long)(s.row0 + token + t) * a.q_stride + (head * a.group + r - t * a.group) * HD + c * 8;
+                    uint32_t v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = (uint32_t)src[2 * e] | (uint32_t)src[2 * e + 1] << 16;
+                    *reinterpret_cast<uint4*>(dst + (c >> 3) * WT_SUB + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                }
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&q_full[st]);
+            }
+            __syncwarp();
+        }
+        if (!ok && lane == 0) {  // what is in flight lands before the CTA leaves
+            mbar_wait(&k_full, 0, nullptr);
+            for (int i = max(0, n - ST); i < n; ++i) mbar_wait(&q_full[i % ST], (i / ST) & 1, nullptr);
+        }
+        __syncwarp();
+    } else if (warp == WT_MMA) {
+        if (elect_one()) {
+            const uint64_t k = sw128_desc(smem_addr(sm + L::K));
+            bool ok = mbar_wait(&k_full, 0, a.err);
+            for (int n = 0; ok && n < u1 - u0; ++n) {
+                const int st = n % ST, count = min(per, tokens.y - (tokens.x + (u0 + n) * per)) * a.group;
+                ok = mbar_wait(&q_full[st], (n / ST) & 1, a.err) && (n < 2 || mbar_wait(&s_empty[n & 1], (n / 2 - 1) & 1, a.err));
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t q = sw128_desc(smem_addr(sm + L::Q + st * L::OPER));
+                const uint32_t id = idesc<T>(count == per * a.group ? WT_TILE : (count + 15) & ~15);
+#pragma unroll
+                for (int d = 0; d < HD / 16; ++d)
+                    tc_mma(tmem + (n & 1) * WT_TILE, k + (((d >> 2) * WT_SUB + (d & 3) * 32) >> 4),
+                           q + (((d >> 2) * WT_SUB + (d & 3) * 32) >> 4), id, d != 0);
+                tc_commit(&s_full[n & 1]);
+                tc_commit(&q_empty[st]);
+            }
+            tc_commit(&drain);  // every MMA has ended before TMEM is given back
+            mbar_wait(&drain, 0, a.err);
+        }
+        __syncwarp();
+    } else {
+        // ---- the sums: a key per thread ----
+        float* lse = reinterpret_cast<float*>(sm + L::LSE) + warp * 2 * WT_TILE;
+        const int heads = a.kv_heads * a.group;
+        int col_token[4], col_head[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = lane + 32 * i;
+            col_token[i] = c / a.group;
+            col_head[i] = head * a.group + c - col_token[i] * a.group;
+        }
+        // the negated log-sum-exps of a tile's columns, in log2 units; of columns past the rows -inf: no weight
+        float l[4];
+        auto ask = [&](int n) {
+            const int token = tokens.x + (u0 + n) * per, count = min(per, tokens.y - token);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                l[i] = INFINITY;
+                if (col_token[i] < count) l[i] = a.lse[(long long)(s.row0 + token + col_token[i]) * heads + col_head[i]];
+            }
+        };
+        ask(0);
+        float sum = 0.f, rest = 0.f;  // with compensation
+        const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
+        bool ok = true;
+        for (int n = 0; n < u1 - u0; ++n) {
+            float* lb = lse + (n & 1) * WT_TILE;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) lb[lane + 32 * i] = -l[i] * LOG2E;
+            __syncwarp();
+            if (n + 1 < u1 - u0) ask(n + 1);
+            const int token = tokens.x + (u0 + n) * per, count = min(per, tokens.y - token), cols = count * a.group;
+            // columns [c0, c1) see the key
+            const int i0 = max(0, key - s.base - token), i1 = a.window > 0 ? min(count, key + a.window - s.base - token) : count;
+            const int c0 = min(i0, count) * a.group, c1 = max(i1, 0) * a.group;
+            const bool full = __all_sync(FULL_MASK, c0 == 0 && c1 == per * a.group) != 0;
+            ok = wait(&s_full[n & 1], n / 2);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t ts = lanes + (n & 1) * WT_TILE;
+            const int chunks = full ? 4 : (cols + 31) >> 5;
+            float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            float x[2][32];
+            auto add = [&](const float (&y)[32], int chunk) {
+                const float4* nl = reinterpret_cast<const float4*>(lb + chunk * 32);
+                const float2 c = make_float2(a.scale_log2, a.scale_log2);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float4 z = nl[e];
+                    const float2 u = fma2(make_float2(y[4 * e], y[4 * e + 1]), c, make_float2(z.x, z.y));
+                    const float2 v = fma2(make_float2(y[4 * e + 2], y[4 * e + 3]), c, make_float2(z.z, z.w));
+                    float2 p = make_float2(ex2(u.x), ex2(u.y)), q = make_float2(ex2(v.x), ex2(v.y));
+                    if (!full) {
+                        const unsigned at = chunk * 32 + 4 * e - c0, width = max(c1 - c0, 0);
+                        p.x = at < width ? p.x : 0.f;
+                        p.y = at + 1 < width ? p.y : 0.f;
+                        q.x = at + 2 < width ? q.x : 0.f;
+                        q.y = at + 3 < width ? q.y : 0.f;
+                    }
+                    acc[0] = add2(acc[0], p);
+                    acc[1] = add2(acc[1], q);
+                }
+            };
+            tmem_ld_issue<32>(ts, x[0]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if (c >= chunks) break;
+                tmem_ld_wait();
+                tmem_ld_done(x[c & 1]);
+                if (c + 1 < chunks) {
+                    tmem_ld_issue<32>(ts + (c + 1) * 32, x[(c + 1) & 1]);
+                } else {  // S is in registers
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&s_empty[n & 1]);
+                }
+                add(x[c & 1], c);
+            }
+            const float y = ((acc[0].x + acc[0].y) + (acc[1].x + acc[1].y)) - rest, t = sum + y;
+            rest = (t - sum) - y;
+            sum = t;
+        }
+        if (ok && mine) {
+            if (a.segments > 1) {
+                *part = sum;
+            } else {
+                float* out = a.weights + slot * a.w_slot + (long long)head * a.width + key;
+                *out = key < s.base ? *out + sum : sum;
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == WT_MMA) tmem_dealloc(tmem, 2 * WT_TILE);
+}
+
+template <class T, int HD>
+cudaError_t launch_tc(const WeightsArgs& a, const CUtensorMap& map, const CUtensorMap& q_map, bool q_tma, int key_tiles, cudaStream_t s) {
+    const auto kern = key_weights_tc_kernel<T, HD>;
+    const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), WtLayout<HD>::BYTES);
+    return e == cudaSuccess ? launch_ex(kern, dim3(key_tiles * a.kv_heads, a.slots, a.segments), WT_THREADS, WtLayout<HD>::BYTES, s, 1, a, map,
+                                        q_map, (int)q_tma)
+                            : e;
+}
+
+}  // namespace
+
+cudaError_t launch_weights_tc(const WeightsArgs& a, const CUtensorMap& map, const CUtensorMap& q_map, bool q_tma, int dtype,
+                              int key_tiles, cudaStream_t s) {
+    if (dtype == MTP_BF16)
+        return a.dim == 64 ? launch_tc<Bf16, 64>(a, map, q_map, q_tma, key_tiles, s) : launch_tc<Bf16, 128>(a, map, q_map, q_tma, key_tiles, s);
+    return a.dim == 64 ? launch_tc<F16, 64>(a, map, q_map, q_tma, key_tiles, s) : launch_tc<F16, 128>(a, map, q_map, q_tma, key_tiles, s);
+}
+
+}  // namespace mtp

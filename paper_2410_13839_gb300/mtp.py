@@ -12,8 +12,10 @@ import struct
 import numpy as np
 
 from . import _lib
-from ._lib import (MTP_OPT_BATCHED, MTPError, MtpAttentionArgs, MtpBeamReorderArgs,  # noqa: F401
-                   MtpBeamSelectArgs, MtpCacheAppendArgs, MtpChunkAttentionArgs, MtpConfig, MtpPagePlanArgs, check, lib)
+from ._lib import (MTP_OPT_BATCHED, MTP_ROTARY_BANDS, MTP_ROTARY_BASE, MTP_ROTARY_HALVES,  # noqa: F401
+                   MTP_ROTARY_LINEAR, MTP_ROTARY_PAIRS, MTP_ROTARY_PLAIN, MTPError, MtpAttentionArgs, MtpBeamReorderArgs,
+                   MtpBeamSelectArgs, MtpCacheAppendArgs, MtpCacheEvictArgs, MtpChunkAttentionArgs, MtpConfig,
+                   MtpDraftVerifyArgs, MtpKeyWeightsArgs, MtpPagePlanArgs, MtpRotaryAppendArgs, check, lib)
 
 BLOB_MAGIC = b"MTPWGT01"
 
@@ -425,6 +427,129 @@ def mtp_beam_reorder(args: MtpBeamReorderArgs, workspace, workspace_bytes: int, 
     check(lib.mtp_beam_reorder(ctypes.byref(args), _ptr(workspace), workspace_bytes, _stream_handle(stream)))
 
 
+def mtp_rotary_turns(rot_dim, scaling=MTP_ROTARY_PLAIN, base=10000.0, factor=1.0, context=0.0, low=1.0, high=4.0,
+                     device="cuda"):
+    """The pairs' turns per position for rotary_append_args, int64 [rot_dim / 2] (the bits of the unsigned fractions)."""
+    import torch
+    host = np.zeros(max(0, rot_dim // 2), np.uint64)
+    check(lib.mtp_rotary_turns(rot_dim, scaling, base, factor, context, low, high, host.ctypes.data))
+    return torch.from_numpy(host.view(np.int64)).to(device)
+
+
+def rotary_append_args(q, k, v, positions, slot_map, turns, kv_pool, layer, out_q, layout=MTP_ROTARY_HALVES,
+                       gain=1.0) -> MtpRotaryAppendArgs:
+    """Argument block of mtp_rotary_append: q, out_q [rows, heads, head_dim], k, v [rows, kv heads, head_dim], their rows
+    possibly strided; turns as mtp_rotary_turns makes them."""
+    pool, dtype = _pool(kv_pool)
+    rows, heads, dim = q.shape
+    shape = (rows, pool["n_kv_heads"], pool["head_dim"])
+    src = _dtype("q", q, (_lib.MTP_F32, dtype))
+    for name, x, want in (("k", k, q.dtype), ("v", v, q.dtype), ("out_q", out_q, kv_pool.dtype)):
+        if x.dtype != want:
+            raise TypeError(f"{name}: {want} wanted, got {x.dtype}")
+    (kp, ks), (vp, vs) = _rows("k", k, shape), _rows("v", v, shape)
+    (qp, qs), (op, os_) = (_rows(n, x, (rows, heads, pool["head_dim"])) for n, x in (("q", q), ("out_q", out_q)))
+    return MtpRotaryAppendArgs(
+        rows=rows, n_heads=heads, rot_dim=2 * turns.shape[0], layout=layout, layer=layer, src_dtype=src, pool_dtype=dtype,
+        gain=gain, q_stride=qs, k_stride=ks, v_stride=vs, out_stride=os_, q=qp, k=kp, v=vp, out_q=op,
+        positions=_buf("positions", positions, "int32", (rows,)), slot_map=_buf("slot_map", slot_map, "int64", (rows,)),
+        turns=_buf("turns", turns, "int64", (None,)), **pool)
+
+
+def mtp_rotary_append(args: MtpRotaryAppendArgs, stream=None) -> None:
+    """Rotary positions of new queries and keys; keys and values into one layer of the cache, by slot map."""
+    check(lib.mtp_rotary_append(ctypes.byref(args), _stream_handle(stream)))
+
+
+def key_weights_args(q, kv_pool, layer, block_table, cu_rows, kv_lens, lse, weights, scale, max_new, max_keys, window=0,
+                     err_word=None) -> MtpKeyWeightsArgs:
+    """Argument block of mtp_key_weights: q [rows, heads, head_dim], its rows possibly strided; weights
+    [slots, layers, kv heads, keys of a table's row]."""
+    pool, dtype = _pool(kv_pool)
+    rows, heads, dim = q.shape
+    slots, stride = block_table.shape
+    if dim != pool["head_dim"] or q.dtype != kv_pool.dtype:
+        raise ValueError(f"q {tuple(q.shape)} {q.dtype} and kv_pool {tuple(kv_pool.shape)} {kv_pool.dtype} do not go together")
+    qp, qs = _rows("q", q, (rows, heads, dim))
+    return MtpKeyWeightsArgs(
+        slots=slots, rows=rows, n_heads=heads, layer=layer, bt_stride=stride, dtype=dtype, window=window, max_new=max_new,
+        max_keys=max_keys, scale=scale, q_stride=qs, q=qp,
+        block_table=_buf("block_table", block_table, "int32", (slots, stride)),
+        cu_rows=_buf("cu_rows", cu_rows, "int32", (slots + 1,)), kv_lens=_buf("kv_lens", kv_lens, "int32", (slots,)),
+        lse=_buf("lse", lse, "float32", (rows, heads)),
+        weights=_buf("weights", weights, "float32", (slots, pool["layers"], pool["n_kv_heads"], stride * pool["page_size"])),
+        err_word=None if err_word is None else _buf("err_word", err_word, "int32"), **pool)
+
+
+def mtp_key_weights_workspace_bytes(args: MtpKeyWeightsArgs) -> int:
+    return int(lib.mtp_key_weights_workspace_bytes(ctypes.byref(args)))
+
+
+def mtp_key_weights(args: MtpKeyWeightsArgs, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    """The attention weight that each cached key gets from a step's tokens, added up."""
+    check(lib.mtp_key_weights(ctypes.byref(args), _ptr(workspace), workspace_bytes, _stream_handle(stream)))
+
+
+def draft_verify_args(logits, tokens, uniforms, cu_rows, kv_lens, out_tokens, out_counts, out_kv_lens, max_new,
+                      draft_logits=None, temperature=None, eos_id=-1, out_done=None, block_table=None, page_refs=None,
+                      page_size=0, err_word=None) -> MtpDraftVerifyArgs:
+    """Argument block of mtp_draft_verify: logits, draft_logits [rows, vocab], their rows possibly strided."""
+    rows, vocab = logits.shape
+    slots = kv_lens.shape[0]
+    code = _dtype("logits", logits, (_lib.MTP_F32, _lib.MTP_BF16, _lib.MTP_F16))
+    if draft_logits is not None and draft_logits.dtype != logits.dtype:
+        raise TypeError(f"draft_logits: {logits.dtype} wanted, got {draft_logits.dtype}")
+    lp, ls = _rows("logits", logits, (rows, vocab))
+    dp, ds = (None, 0) if draft_logits is None else _rows("draft_logits", draft_logits, (rows, vocab))
+
+    def opt(name, x, dtype, *shape):
+        return None if x is None else _buf(name, x, dtype, shape)
+    return MtpDraftVerifyArgs(
+        slots=slots, rows=rows, vocab=vocab, max_new=max_new, eos_id=eos_id, logits_dtype=code, page_size=page_size,
+        bt_stride=0 if block_table is None else block_table.shape[1], n_pages=0 if page_refs is None else page_refs.shape[0],
+        logits_stride=ls, draft_stride=ds, logits=lp, draft_logits=dp,
+        temperature=opt("temperature", temperature, "float32", slots), tokens=_buf("tokens", tokens, "int32", (rows,)),
+        uniforms=_buf("uniforms", uniforms, "float32", (rows, 2)), cu_rows=_buf("cu_rows", cu_rows, "int32", (slots + 1,)),
+        kv_lens=_buf("kv_lens", kv_lens, "int32", (slots,)), block_table=opt("block_table", block_table, "int32", slots, None),
+        page_refs=opt("page_refs", page_refs, "int32", None),
+        out_tokens=_buf("out_tokens", out_tokens, "int32", (slots, max_new)),
+        out_counts=_buf("out_counts", out_counts, "int32", (slots,)),
+        out_kv_lens=_buf("out_kv_lens", out_kv_lens, "int32", (slots,)), out_done=opt("out_done", out_done, "int32", slots),
+        err_word=None if err_word is None else _buf("err_word", err_word, "int32"))
+
+
+def mtp_draft_verify(args: MtpDraftVerifyArgs, stream=None) -> None:
+    """Which drafted tokens the target's distribution keeps, the token after them, the pages of the others."""
+    check(lib.mtp_draft_verify(ctypes.byref(args), _stream_handle(stream)))
+
+
+def cache_evict_args(kv_lens, keep, block_table, page_refs, weights, kv_pool, out_kv_lens, out_block_table, out_page_refs,
+                     out_weights, out_status, sinks=0, recent=0) -> MtpCacheEvictArgs:
+    """Argument block of mtp_cache_evict: weights, out_weights [slots, layers, kv heads, keys of a table's row]."""
+    pool, dtype = _pool(kv_pool)
+    (slots, stride), n_pages = block_table.shape, pool["n_pages"]
+    shape = (slots, pool["layers"], pool["n_kv_heads"], stride * pool["page_size"])
+    return MtpCacheEvictArgs(
+        slots=slots, bt_stride=stride, pool_dtype=dtype, sinks=sinks, recent=recent,
+        kv_lens=_buf("kv_lens", kv_lens, "int32", (slots,)), keep=_buf("keep", keep, "int32", (slots,)),
+        block_table=_buf("block_table", block_table, "int32", (slots, stride)),
+        page_refs=_buf("page_refs", page_refs, "int32", (n_pages,)), weights=_buf("weights", weights, "float32", shape),
+        out_kv_lens=_buf("out_kv_lens", out_kv_lens, "int32", (slots,)),
+        out_block_table=_buf("out_block_table", out_block_table, "int32", (slots, stride)),
+        out_page_refs=_buf("out_page_refs", out_page_refs, "int32", (n_pages,)),
+        out_weights=_buf("out_weights", out_weights, "float32", shape),
+        out_status=_buf("out_status", out_status, "int32", (slots,)), **pool)
+
+
+def mtp_cache_evict_workspace_bytes(args: MtpCacheEvictArgs) -> int:
+    return int(lib.mtp_cache_evict_workspace_bytes(ctypes.byref(args)))
+
+
+def mtp_cache_evict(args: MtpCacheEvictArgs, workspace, workspace_bytes: int, stream=None) -> None:
+    """Every slot's keys of largest weight stay, in their order, and the pages behind them become free."""
+    check(lib.mtp_cache_evict(ctypes.byref(args), _ptr(workspace), workspace_bytes, _stream_handle(stream)))
+
+
 def _as_i32(x):
     if x is None:
         return None
@@ -507,4 +632,6 @@ class MTPDecoder:
 
 __all__ = [n for n in dir() if n.startswith("mtp_")] + ["MTPDecoder", "MTPError", "pack_weights",
                                                          "make_config", "attention_args", "page_plan_args",
-                                                         "cache_append_args", "chunk_attention_args", "beam_select_args", "beam_reorder_args"]
+                                                         "cache_append_args", "chunk_attention_args", "beam_select_args", "beam_reorder_args",
+                                                         "rotary_append_args", "key_weights_args", "draft_verify_args",
+                                                         "cache_evict_args"]
