@@ -26,11 +26,12 @@
 namespace mtp {
 namespace {
 
-constexpr int VF_THREADS = 512, VF_WARPS = VF_THREADS / 32;
-constexpr int VF_BLOCK = 256;      // tokens whose weights are summed as one: 8 a lane
+constexpr int VF_THREADS = 256, VF_WARPS = VF_THREADS / 32;
+constexpr int VF_BLOCK = 256;      // tokens that are summed as one: 8 a lane
+constexpr int VF_WINDOW = 24;      // blocks whose weights shared memory holds
 template <int TYPE>
 constexpr int VF_ITEM = TYPE == MTP_F32 ? 2 : 4;  // blocks that a lane reads at once
-constexpr int VF_MAX_NEW = 64, VF_MAX_VOCAB = 1 << 18, VF_MAX_CLUSTER = 8;
+constexpr int VF_MAX_NEW = 64, VF_MAX_VOCAB = 1 << 18, VF_MAX_CLUSTER = 16;
 constexpr float VF_HUGE = 1e38f;   // infinite logits count as this
 constexpr float VF_NEAR = 1e-4f;   // products nearer than this, relatively, are compared in 64 bits
 
@@ -59,49 +60,64 @@ constexpr ExTable make_ex_table() {
 }
 __device__ const ExTable ex_table = make_ex_table();
 
-// A distribution's exponents: z = (x - top) c - l, c = log2 e / T as hi + lo, l = steps / 1024 + l_rest.
+// A distribution's exponents: z = x c - l, c = log2 e / T as hi + lo, l = top c as steps / 1024 + rest.
 struct Exponent {
-    float top;
     float c_hi, c_lo;
-    int l_steps;
-    float l_rest;
+    float low;      // of x: below it nothing of 2^-44 is left
+    int steps;      // with the bits of the constant that rounds to whole steps
+    float rest;
+    float top;      // where products with c are too large for that: subtracted from x first, exactly
+    bool wide;
 };
-// 2^z = a 2^-22 + b 2^-44, a <= 2^22, |b| <= 2^21 + 1: two roundings to fixed steps by adding a constant of the step's size.
-__device__ __forceinline__ void ex_fixed(float x, const Exponent& e, const ExEntry* table, int& a, int& b) {
-    // x - top as d + err, exactly
-    const float d = x - e.top, bb = d - x, err = (x - (d - bb)) + (-e.top - bb);
-    const float p = d * e.c_hi;
-    float rest = fmaf(d, e.c_hi, -p);
-    rest = fmaf(d, e.c_lo, rest);
-    rest = fmaf(err, e.c_hi, rest);
-    constexpr float ROUND = 12582912.f;  // 1.5 * 2^23
-    const float kf = fmaf(p, (float)EX_STEPS, ROUND);
-    const int k = __float_as_int(kf) - __float_as_int(ROUND) - e.l_steps;
-    const float r = fmaf(kf - ROUND, -1.f / EX_STEPS, p) + (rest - e.l_rest);
-    const ExEntry t = table[k & (EX_STEPS - 1)];
-    const float scale = __int_as_float((max(k >> EX_BITS, -126) + 127) << 23);
-    // 2^r - 1, |r| < 2^-10: ln 2 r + (ln 2 r)^2 / 2 + (ln 2 r)^3 / 6
+constexpr float EX_ROUND = 12582912.f;  // 1.5 * 2^23
+__device__ __forceinline__ Exponent make_exponent(float top, bool tamed, float c_hi, float c_lo) {
+    Exponent e;
+    e.c_hi = c_hi;
+    e.c_lo = c_lo;
+    e.top = top;
+    const float p = top * c_hi;
+    e.wide = tamed || !(fabsf(p) < 2000.f);  // (2^21 steps)
+    e.low = (e.wide ? 0.f : top) - 100.f / c_hi;
+    const float kf = fmaf(p, (float)EX_STEPS, EX_ROUND);
+    e.steps = __float_as_int(EX_ROUND);
+    e.rest = 0.f;
+    if (!e.wide) {
+        e.steps = __float_as_int(kf);
+        e.rest = fmaf(kf - EX_ROUND, -1.f / EX_STEPS, p) + fmaf(top, c_lo, fmaf(top, c_hi, -p));
+    }
+    return e;
+}
+__device__ __forceinline__ float tame(float x) { return fminf(fmaxf(x, -VF_HUGE), VF_HUGE); }  // NaN: the lowest
+// 2^z = (u - 3) + v 2^-44, u in steps of 2^-22, v of 1 with EX_ROUND in front: two roundings to fixed steps by adding a
+// constant of the step's size.  Weights add up in the bits of u and v, each a constant too large.
+constexpr int EX_U = 0x40400000, EX_V = 0x4b400000;  // bits of 3 and EX_ROUND
+__device__ __noinline__ float2 ex_widen(float x, float top, float low, float c) {
+    x = tame(x);
+    const float d = x - top, bb = d - x;  // x - top = d + err
+    return make_float2(d, d > low ? ((x - (d - bb)) + (-top - bb)) * c : 0.f);
+}
+// table: its address in shared memory.
+__device__ __forceinline__ void ex_fixed(float x, const Exponent& e, uint32_t table, int& u_bits, int& v_bits) {
+    float err = 0.f;
+    if (e.wide) {
+        const float2 y = ex_widen(x, e.top, e.low, e.c_hi);
+        x = y.x;
+        err = y.y;
+    }
+    x = fmaxf(x, e.low);  // (-inf and NaN, too)
+    const float p = x * e.c_hi;
+    const float kf = fmaf(p, (float)EX_STEPS, EX_ROUND);
+    const int k = __float_as_int(kf) - e.steps;
+    const float r = fmaf(kf - EX_ROUND, -1.f / EX_STEPS, p) + ((fmaf(x, e.c_lo, -e.rest) + err) + fmaf(x, e.c_hi, -p));
+    ExEntry t;
+    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(t.hi), "=f"(t.lo) : "r"(table + (k & (EX_STEPS - 1)) * 8));
+    const float scale = __int_as_float((int)((unsigned)k << (23 - EX_BITS) & 0xff800000u) + (127 << 23));
+    // 2^r - 1, |r| < 2^-9: ln 2 r + (ln 2 r)^2 / 2 + (ln 2 r)^3 / 6
     const float m = r * fmaf(r, fmaf(r, 0.0555041087f, 0.2402265070f), 0.6931471806f);
     const float hi = t.hi * scale, lo = fmaf(t.hi, m, t.lo) * scale;
-    const float u = (hi + lo) + 3.f;  // steps of 2^-22 above 2
-    const float left = (hi - (u - 3.f)) + lo;
-    const float v = fmaf(left, 0x1p44f, ROUND);
-    const bool there = p > -100.f;  // (below nothing is left; -inf gives no number)
-    a = there ? __float_as_int(u) - __float_as_int(3.f) : 0;
-    b = there ? __float_as_int(v) - __float_as_int(ROUND) : 0;
-}
-
-// The same weights divided by their sum, of 2^-44: l = log2 of it, by its nearest entry of the table and the rest's logarithm.
-__device__ __forceinline__ void divide_by(Exponent& e, long long sum, const ExEntry* table) {
-    const int zeros = __clzll(sum);
-    const unsigned long long m = (unsigned long long)sum << zeros;  // in [1, 2) times 2^63
-    const float hi = (float)(uint32_t)(m >> 40) * 0x1p-23f, lo = (float)(uint32_t)(m >> 8) * 0x1p-55f;
-    const int k = __float2int_rn(log2f(hi) * EX_STEPS);
-    const ExEntry t = table[k & (EX_STEPS - 1)];
-    const float two = k >= EX_STEPS ? 2.f : 1.f;
-    const float r = ((hi - two * t.hi) + (lo - two * t.lo)) / (two * t.hi);
-    e.l_steps = (63 - zeros - 44) * EX_STEPS + k;
-    e.l_rest = 1.4426950409f * r * fmaf(-r, fmaf(-r, 0.3333333333f, 0.5f), 1.f);
+    const float u = (hi + lo) + 3.f;
+    u_bits = __float_as_int(u);
+    v_bits = __float_as_int(fmaf((hi - (u - 3.f)) + lo, 0x1p44f, EX_ROUND));
 }
 
 // ---- rows ----
@@ -131,8 +147,60 @@ struct Logit<MTP_F16> {
     static __device__ __forceinline__ float get(const uint16_t* p) { return F16::to_float(*p); }
 };
 __device__ __forceinline__ float unit(float u) { return u > 0.f ? fminf(u, 1.f) : 0.f; }  // NaN: 0
-__device__ __forceinline__ float tame(float x) { return fminf(fmaxf(x, -VF_HUGE), VF_HUGE); }  // NaN: the lowest
 
+// Eight logits as they stand in memory.
+template <int TYPE>
+struct Raw {
+    uint4 v[TYPE == MTP_F32 ? 2 : 1];
+};
+template <int TYPE>
+__device__ __forceinline__ Raw<TYPE> no_logits() {  // -inf
+    constexpr uint32_t NONE = TYPE == MTP_F32 ? 0xff800000u : TYPE == MTP_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+    Raw<TYPE> r;
+    r.v[0] = make_uint4(NONE, NONE, NONE, NONE);
+    if constexpr (TYPE == MTP_F32) r.v[1] = r.v[0];
+    return r;
+}
+// Tokens first .. first + 7 at the row's ends, or at any place, one by one.
+template <int TYPE>
+__device__ __noinline__ Raw<TYPE> fetch_each(const typename Logit<TYPE>::type* x, int first, int vocab) {
+    Raw<TYPE> r;
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const bool in = first + i >= 0 && first + i < vocab;
+        if constexpr (TYPE == MTP_F32)
+            w[i] = in ? __float_as_uint(x[first + i]) : 0xff800000u;
+        else
+            w[i] = in ? (uint32_t)x[first + i] : TYPE == MTP_BF16 ? 0xff80u : 0xfc00u;
+    }
+    if constexpr (TYPE == MTP_F32) {
+        r.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        r.v[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    } else {
+        r.v[0] = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+    }
+    return r;
+}
+template <int TYPE>
+__device__ __forceinline__ void decode(const Raw<TYPE>& r, float (&v)[8]) {
+    const uint32_t w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
+    if constexpr (TYPE == MTP_F32) {
+        const uint32_t y[4] = {r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = __uint_as_float(w[i]);
+            v[4 + i] = __uint_as_float(y[i]);
+        }
+    } else {
+        using H = typename std::conditional<TYPE == MTP_BF16, Bf16, F16>::type;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = H::to_float((uint16_t)w[i]);
+            v[2 * i + 1] = H::to_float((uint16_t)(w[i] >> 16));
+        }
+    }
+}
 // A row of logits.  Its blocks begin at the 16-byte boundary at or before the row: place j is token j - shift.
 template <int TYPE>
 struct Row {
@@ -142,65 +210,16 @@ struct Row {
         x = static_cast<const typename Logit<TYPE>::type*>(base) + row * stride;
         shift = (int)((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(*x));
     }
-    __device__ __forceinline__ float raw(int token) const { return Logit<TYPE>::get(x + token); }
-    __device__ __forceinline__ float at(int token) const { return tame(raw(token)); }
-    // places j .. j + 7 (j a multiple of 8) as they stand in memory; -inf outside the row, no token's
-    struct Raw {
-        uint4 v[TYPE == MTP_F32 ? 2 : 1];
-    };
-    __device__ __forceinline__ Raw fetch(int j) const {
-        Raw r;
-        const int first = j - shift;
-        if (first >= 0 && first + 8 <= vocab) {
-            r.v[0] = *reinterpret_cast<const uint4*>(x + first);
-            if constexpr (TYPE == MTP_F32) r.v[1] = *reinterpret_cast<const uint4*>(x + first + 4);
-        } else if constexpr (TYPE == MTP_F32) {
-            uint32_t w[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = in(first + i) ? __float_as_uint(x[first + i]) : 0xff800000u;
-            r.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
-            r.v[1] = make_uint4(w[4], w[5], w[6], w[7]);
-        } else {
-            constexpr uint32_t NONE = TYPE == MTP_BF16 ? 0xff80u : 0xfc00u;
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                w[i] = (in(first + 2 * i) ? (uint32_t)x[first + 2 * i] : NONE) | (in(first + 2 * i + 1) ? (uint32_t)x[first + 2 * i + 1] : NONE) << 16;
-            r.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-        return r;
-    }
-    static __device__ __forceinline__ Raw none() {
-        constexpr uint32_t NONE = TYPE == MTP_F32 ? 0xff800000u : TYPE == MTP_BF16 ? 0xff80ff80u : 0xfc00fc00u;
-        Raw r;
-        r.v[0] = make_uint4(NONE, NONE, NONE, NONE);
-        if constexpr (TYPE == MTP_F32) r.v[1] = r.v[0];
-        return r;
-    }
-    static __device__ __forceinline__ void decode(const Raw& r, float (&v)[8]) {
-        const uint32_t w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
-        if constexpr (TYPE == MTP_F32) {
-            const uint32_t y[4] = {r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[i] = __uint_as_float(w[i]);
-                v[4 + i] = __uint_as_float(y[i]);
-            }
-        } else {
-            using H = typename std::conditional<TYPE == MTP_BF16, Bf16, F16>::type;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[2 * i] = H::to_float((uint16_t)w[i]);
-                v[2 * i + 1] = H::to_float((uint16_t)(w[i] >> 16));
-            }
-        }
-    }
-    __device__ __forceinline__ void load(int j, float (&v)[8]) const { decode(fetch(j), v); }
     __device__ __forceinline__ bool in(int token) const { return token >= 0 && token < vocab; }
-    // values of places j .. j + 7 that are not finite as those that they count as
-    __device__ __forceinline__ void make_tame(int j, float (&v)[8]) const {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = in(j - shift + i) ? tame(v[i]) : -INFINITY;
+    __device__ __forceinline__ float at(int token) const { return tame(Logit<TYPE>::get(x + token)); }
+    // places j .. j + 7 (j a multiple of 8); -inf outside the row, no token's
+    __device__ __forceinline__ Raw<TYPE> fetch(int j) const {
+        const int first = j - shift;
+        if (!(first >= 0 && first + 8 <= vocab)) return fetch_each<TYPE>(x, first, vocab);
+        Raw<TYPE> r;
+        r.v[0] = *reinterpret_cast<const uint4*>(x + first);
+        if constexpr (TYPE == MTP_F32) r.v[1] = *reinterpret_cast<const uint4*>(x + first + 4);
+        return r;
     }
 };
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
@@ -220,7 +239,7 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
 
 struct alignas(16) Stat {  // of a row's logits: the largest, sum of 2^((x - top) c), lowest token of the largest
     float top, sum;
-    int arg;
+    int arg, tamed;  // tamed: some logit is not finite, or as large
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -234,7 +253,8 @@ __device__ __forceinline__ void push(long long* p, int rank, long long v) {
 }
 __device__ __forceinline__ void push(Stat* p, int rank, const Stat& s) {
     const uint32_t at = dsmem_addr(p, rank);
-    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %3};" ::"r"(at), "r"(__float_as_uint(s.top)), "r"(__float_as_uint(s.sum)), "r"(s.arg) : "memory");
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(__float_as_uint(s.top)), "r"(__float_as_uint(s.sum)), "r"(s.arg), "r"(s.tamed)
+                 : "memory");
 }
 // Of the lanes' rows one: c as Exponent's.
 __device__ __forceinline__ Stat merge(const Stat& s, float c) {
@@ -242,6 +262,7 @@ __device__ __forceinline__ Stat merge(const Stat& s, float c) {
     all.top = warp_max(s.top);
     all.sum = mtp::warp_sum(s.sum * ex2((s.top - all.top) * c));
     all.arg = __reduce_min_sync(FULL_MASK, s.top == all.top ? s.arg : INT_MAX);
+    all.tamed = __any_sync(FULL_MASK, s.tamed);
     return all;
 }
 __device__ __forceinline__ long long warp_scan(long long x) {  // inclusive
@@ -254,56 +275,102 @@ __device__ __forceinline__ long long warp_scan(long long x) {  // inclusive
     return x;
 }
 
+// A lane's part of the places [from, to) of a row, with what values that are not finite count as.
+template <int TYPE>
+__device__ __noinline__ Stat tame_stat(const Row<TYPE>& row, int from, int to, float c) {
+    Stat s{-VF_HUGE, 0.f, INT_MAX, 1};
+#pragma unroll 1
+    for (int j = from + (threadIdx.x & 31); j < to; j += 32) {
+        const int token = j - row.shift;
+        if (!row.in(token)) continue;
+        const float x = row.at(token), top = fmaxf(s.top, x);
+        s.sum = s.sum * ex2((s.top - top) * c) + ex2((x - top) * c);
+        if (x > s.top || s.arg == INT_MAX) s.arg = token;
+        s.top = top;
+    }
+    return s;
+}
+// u q(d) < p(d) in 64 bits: x, y the logits, sums in 2^-44 (of q: 0, all of it is on d).
+__device__ __noinline__ bool near_kept(float u, float x, float top, long long sum, float y, float y_top, long long y_sum, float t) {
+    const double c = 1.4426950408889634 / (double)t;
+    double q = 1.0;
+    if (y_sum > 0) q = exp2(((double)y - (double)y_top) * c) / ((double)y_sum * 0x1p-44);
+    return (double)u * q < exp2(((double)x - (double)top) * c) / ((double)sum * 0x1p-44);
+}
+
+// A window's weights of one distribution in shared memory: 45 bits each, the lowest 13 of them apart.
+struct Held {
+    uint32_t hi, lo;  // addresses: [window] words, [window] halfwords
+    __device__ __forceinline__ void put(int i, long long w) const {
+        asm volatile("st.shared.b32 [%0], %1;" ::"r"(hi + i * 4), "r"((uint32_t)(w >> 13)) : "memory");
+        asm volatile("st.shared.b16 [%0], %1;" ::"r"(lo + i * 2), "h"((uint16_t)(w & 8191)) : "memory");
+    }
+    __device__ __forceinline__ unsigned long long get(int i) const {
+        uint32_t x;
+        uint16_t y;
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(hi + i * 4) : "memory");
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(lo + i * 2) : "memory");
+        return (unsigned long long)x << 13 | y;
+    }
+};
+// Weights of tokens [from, to) of a row; returns this thread's sum.  One body for all calls: inlined at each, the kernel's
+// instructions did not stay in the cache.
+template <int TYPE>
+__device__ __noinline__ long long hold_weights(const Row<TYPE> row, const Exponent e, uint32_t table, const Held held, int from, int to) {
+    long long sum = 0;
+#pragma unroll 1
+    for (int g = ((from + row.shift) >> 3) + threadIdx.x; g * 8 - row.shift < to; g += VF_THREADS) {
+        const int first = g * 8 - row.shift;
+        float x[8];
+        decode<TYPE>(row.fetch(g * 8), x);
+        const bool all = first >= from && first + 8 <= min(to, row.vocab);
+        int su = 0, sv = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            int u, v;
+            ex_fixed(x[i], e, table, u, v);
+            u -= EX_U;
+            v -= EX_V;
+            if (!all) {
+                if (!row.in(first + i)) u = v = 0;  // (-inf, in the places of none, may count as a number)
+                if (first + i < from || first + i >= to) continue;
+            }
+            su += u;
+            sv += v;
+            held.put(first + i - from, ((long long)u << 22) + v);
+        }
+        sum += ((long long)su << 22) + sv;
+    }
+    return sum;
+}
+
 // How the weights of a draw are made.
 enum DrawMode { DRAW_TARGET, DRAW_WITHOUT, DRAW_REST };  // p; p but for the drafted token; max(p - q, 0)
 
-template <int TYPE>
-struct Draw {
-    DrawMode mode;
-    int without;
-    Exponent p, q;
-    // weights of places j .. j + 7 of the target's row
-    __device__ __forceinline__ void weights(const Row<TYPE>& t, const Row<TYPE>& d, const ExEntry* table, int j, long long (&w)[8]) const {
-        float x[8], y[8];
-        const auto raw = t.fetch(j);
-        if (mode == DRAW_REST)  // (all on their way together)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = t.in(j - t.shift + i) ? d.raw(j - t.shift + i) : -INFINITY;
-        Row<TYPE>::decode(raw, x);
-        t.make_tame(j, x);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            int a, b;
-            ex_fixed(x[i], p, table, a, b);
-            w[i] = ((long long)a << 22) + b;
-            const int token = j - t.shift + i;
-            if (mode == DRAW_WITHOUT && token == without) w[i] = 0;
-            if (mode == DRAW_REST) {
-                ex_fixed(t.in(token) ? tame(y[i]) : -INFINITY, q, table, a, b);
-                w[i] -= ((long long)a << 22) + b;
-            }
-            w[i] = w[i] > 0 ? w[i] : 0;
-        }
-    }
-};
-
-// Grid (slots * ctas).  Shared memory: the table, [2 max_new] sums of rows and of their segments, sums of blocks.
+// Grid (slots * ctas).
 template <int TYPE>
 __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __grid_constant__ DraftArgs p) {
     extern __shared__ __align__(16) unsigned char vf_sm[];
-    __shared__ Stat parts[2 * VF_MAX_NEW + VF_WARPS], gather[VF_MAX_CLUSTER][2 * VF_MAX_NEW], stat[2 * VF_MAX_NEW];
-    __shared__ int state[VF_MAX_NEW];
+    __shared__ int state[VF_MAX_NEW], fed[VF_MAX_NEW];  // of each draft: kept (2: near), the token
+    __shared__ float numbers[VF_MAX_NEW];               // the rows' numbers for a draw
     __shared__ long long warp_total[2][VF_WARPS], word[2][2][VF_MAX_CLUSTER];
-    __shared__ int s_block, s_keep;
+    __shared__ int s_block;
     __shared__ long long s_before, s_at;
     const mtp_draft_verify_args& a = p.a;
     ExEntry* table = reinterpret_cast<ExEntry*>(vf_sm);
-    long long* block_sum = reinterpret_cast<long long*>(vf_sm + sizeof(ExTable));
+    Stat* stat = reinterpret_cast<Stat*>(vf_sm + sizeof(ExTable));  // [2 max_new], of rows
+    Stat* parts = stat + 2 * a.max_new;                             // [2 max_new + warps], of the warps' parts of them
+    Stat* gather = parts + 2 * a.max_new + VF_WARPS;                // [ctas][2 max_new]
+    long long* block_sum = reinterpret_cast<long long*>(gather + p.ctas * 2 * a.max_new);  // [blocks]
+    const int window = min(p.blocks, VF_WINDOW) * VF_BLOCK;
+    const uint32_t table_at = smem_addr(table), held_at = smem_addr(block_sum + p.blocks);
+    const Held held_p{held_at, held_at + 8 * window}, held_q{held_at + 4 * window, held_at + 10 * window};
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, C = p.ctas, slot = blockIdx.x / C, rank = blockIdx.x - slot * C;
     constexpr int ITEM = VF_ITEM<TYPE>;
     const int V = a.vocab;
     pdl_launch_dependents();
     if (C > 1) cluster_arrive_relaxed();  // (before the first push every CTA is there)
+#pragma unroll 1
     for (int i = tid; i < EX_STEPS; i += VF_THREADS) table[i] = ex_table.e[i];
     pdl_wait();
     auto team = [&]() {
@@ -315,12 +382,14 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
         }
     };
     const int r0 = a.cu_rows[slot], end = a.cu_rows[slot + 1], n = end - r0, len = a.kv_lens[slot];
+    const float T = a.temperature ? a.temperature[slot] : 1.f;
     const bool bad = r0 < 0 || n < 0 || end > a.rows || n > a.max_new || len < n ||
                      (a.block_table && len > (long long)a.bt_stride << p.shift);
     int* out = a.out_tokens + (long long)slot * a.max_new;
     if (bad || n == 0) {  // (the whole cluster)
         if (C > 1) cluster_wait();
         if (rank == 0) {
+#pragma unroll 1
             for (int i = tid; i < a.max_new; i += VF_THREADS) out[i] = -1;
             if (tid == 0) {
                 a.out_counts[slot] = 0;
@@ -331,12 +400,11 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
         }
         return;
     }
-    const float T = a.temperature ? a.temperature[slot] : 1.f;
     const bool greedy = !(T > 0.f), drafter = a.draft_logits && !greedy;
     // c = log2 e / T as hi + lo.  (All in 32 bits: 64-bit operations of a CTA's threads take microseconds.)
     const float t_tame = fminf(fmaxf(T, 1e-30f), 1e30f), cf = 1.44269502f / t_tame;
     const float c_lo = (fmaf(-cf, t_tame, 1.44269502f) + 1.92596299e-8f) / t_tame;
-    const int b0 = rank * p.blocks;  // this CTA's blocks of every row
+    const int b0 = rank * p.blocks;  // this CTA's blocks of every row (of places there, of tokens below)
 
     // ---- 1: every row's largest logit and sum ----
     const int tasks = n + (drafter ? n - 1 : 0), items = (p.blocks + ITEM - 1) / ITEM, total = tasks * items;
@@ -344,11 +412,11 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
         return task < n ? Row<TYPE>(a.logits, r0 + task, a.logits_stride, V) : Row<TYPE>(a.draft_logits, r0 + task - n, a.draft_stride, V);
     };
     // what the drafts are judged by, on its way
-    const int* drafts = a.tokens + r0 + 1;  // [n - 1]
     int draft = -1;
     float draft_u = 0.f, draft_x = 0.f, draft_y = 0.f;
+    if (tid < n) numbers[tid] = a.uniforms[2 * (r0 + tid) + 1];
     if (tid < n - 1) {
-        draft = drafts[tid];
+        fed[tid] = draft = a.tokens[r0 + 1 + tid];
         draft_u = a.uniforms[2 * (r0 + tid)];
         if (draft >= 0 && draft < V) {
             draft_x = row_of(tid).at(draft);
@@ -356,79 +424,75 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
         }
     }
     auto first_item = [&](int w) { return (int)((long long)total * w / VF_WARPS); };
+#pragma unroll 1
     for (int it = first_item(warp), stop = first_item(warp + 1); it < stop;) {
-        const int task = it / items, from = it, to = min(stop, (task + 1) * items);
+        const int task = it / items, from = it, to = min(stop, (task + 1) * items);  // items [from, to) of a row
         const Row<TYPE> row = row_of(task);
-        Stat s;
-        // values that are not finite show in the sum or the largest: such a row is gone through once more, with what they count as
+        Stat s{-VF_HUGE, 0.f, INT_MAX, 0};
+        Raw<TYPE> raw[ITEM], next[ITEM];
 #pragma unroll 1
-        for (int safe = greedy; safe < 2; ++safe) {
-            s = Stat{-VF_HUGE, 0.f, V};
-            typename Row<TYPE>::Raw raw[ITEM], next[ITEM];
-            auto fetch = [&](int it) {
-                const int block = b0 + (it - task * items) * ITEM, stop_block = it < to ? min(b0 + p.blocks, block + ITEM) : 0;
+        for (int at = from - 1; at < to; ++at) {
+            // the next item's logits are on their way (the first one's: nothing else is there to do)
+            const int block = b0 + (at - task * items) * ITEM, stop_block = at + 1 < to ? min(b0 + p.blocks, block + 2 * ITEM) : 0;
 #pragma unroll
-                for (int k = 0; k < ITEM; ++k) next[k] = block + k < stop_block ? row.fetch((block + k) * VF_BLOCK + lane * 8) : Row<TYPE>::none();
-            };
-            fetch(from);
-#pragma unroll 1
-            for (it = from; it < to; ++it) {
-                const int block = b0 + (it - task * items) * ITEM, stop_block = min(b0 + p.blocks, block + ITEM);
-                float x[ITEM][8];
-                float top = s.top;
+            for (int k = 0; k < ITEM; ++k) {
+                raw[k] = next[k];
+                next[k] = block + ITEM + k < stop_block ? row.fetch((block + ITEM + k) * VF_BLOCK + lane * 8) : no_logits<TYPE>();
+            }
+            if (at < from) continue;
+            float x[ITEM][8], top = s.top;
 #pragma unroll
-                for (int k = 0; k < ITEM; ++k) raw[k] = next[k];
-                fetch(it + 1);
+            for (int k = 0; k < ITEM; ++k) {
+                decode<TYPE>(raw[k], x[k]);
 #pragma unroll
-                for (int k = 0; k < ITEM; ++k) Row<TYPE>::decode(raw[k], x[k]);
-                if (safe)
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, x[k][i]);
+            }
+            if (greedy) {
+                if (top > s.top || s.arg == INT_MAX) {
+                    int arg = INT_MAX;
 #pragma unroll
-                    for (int k = 0; k < ITEM; ++k)
-                        if (block + k < stop_block) row.make_tame((block + k) * VF_BLOCK + lane * 8, x[k]);
+                    for (int k = ITEM - 1; k >= 0; --k)
+#pragma unroll
+                        for (int i = 7; i >= 0; --i) arg = x[k][i] == top ? (k << 8) + i : arg;
+                    if (arg != INT_MAX) s.arg = block * VF_BLOCK + lane * 8 - row.shift + arg;
+                }
+            } else {
+                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
                 for (int k = 0; k < ITEM; ++k)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) top = fmaxf(top, x[k][i]);
-                if (greedy) {
-                    if (top > s.top || s.arg == V) {
-                        int arg = V;
-#pragma unroll
-                        for (int k = ITEM - 1; k >= 0; --k)
-#pragma unroll
-                            for (int i = 7; i >= 0; --i)
-                                if (x[k][i] == top) arg = (block + k) * VF_BLOCK + lane * 8 + i - row.shift;
-                        s.arg = arg;
+                    for (int i = 0; i < 8; i += 2) {
+                        const float2 z = mul2(add2(make_float2(x[k][i], x[k][i + 1]), make_float2(-top, -top)), make_float2(cf, cf));
+                        sum[i >> 1 & 1] = add2(sum[i >> 1 & 1], make_float2(ex2(z.x), ex2(z.y)));
                     }
-                } else {
-                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-                    for (int k = 0; k < ITEM; ++k)
-#pragma unroll
-                        for (int i = 0; i < 8; i += 2) {
-                            const float2 z = mul2(add2(make_float2(x[k][i], x[k][i + 1]), make_float2(-top, -top)), make_float2(cf, cf));
-                            sum[i >> 1 & 1] = add2(sum[i >> 1 & 1], make_float2(ex2(z.x), ex2(z.y)));
-                        }
-                    s.sum = fmaf(s.sum, ex2((s.top - top) * cf), (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
-                }
-                s.top = top;
+                s.sum = fmaf(s.sum, ex2((s.top - top) * cf), (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
             }
-            // (a number that no comparison holds for, too)
-            if (__all_sync(FULL_MASK, s.sum >= 0.f && s.top < VF_HUGE)) break;
+            s.top = top;
         }
+        it = to;
+        // values that are not finite show in the sum or the largest (or in that there is none): the row's part once more, with care
+        const float most = warp_max(s.top);
+        if (!__all_sync(FULL_MASK, s.sum >= 0.f) || !(most < VF_HUGE && most > -VF_HUGE))
+            s = tame_stat<TYPE>(row, (b0 + (from - task * items) * ITEM) * VF_BLOCK, min(b0 + p.blocks, b0 + (to - task * items) * ITEM) * VF_BLOCK, cf);
         s = merge(s, cf);
         if (lane == 0) parts[task + warp] = s;
     }
     __syncthreads();
     if (C > 1) cluster_wait();
+#pragma unroll 1
     for (int task = warp; task < tasks; task += VF_WARPS) {  // a lane per warp's part, then per CTA
         const bool has = lane < VF_WARPS && max(first_item(lane), task * items) < min(first_item(lane + 1), (task + 1) * items);
-        const Stat s = merge(has ? parts[task + lane] : Stat{-VF_HUGE, 0.f, V}, cf);
-        if (lane < C) push(&gather[rank][task], lane, s);
+        const Stat s = merge(has ? parts[task + lane] : Stat{-VF_HUGE, 0.f, INT_MAX, 0}, cf);
+        if (lane < C) push(&gather[rank * 2 * a.max_new + task], lane, s);
     }
     team();
+#pragma unroll 1
     for (int task = warp; task < tasks; task += VF_WARPS) {
-        Stat s = merge(lane < C ? gather[lane][task] : Stat{-VF_HUGE, 0.f, V}, cf);
-        if (!(s.top > -VF_HUGE)) s.sum = (float)V;  // nothing above what -infinity counts as: all alike
+        Stat s = merge(lane < C ? gather[lane * 2 * a.max_new + task] : Stat{-VF_HUGE, 0.f, INT_MAX, 0}, cf);
+        if (!(s.top > -VF_HUGE)) {  // nothing above what -infinity counts as: all alike
+            s.sum = (float)V;
+            s.tamed = 1;
+        }
         if (lane == 0) stat[task] = s;
     }
     __syncthreads();
@@ -451,15 +515,6 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
     }
     __syncthreads();
 
-    auto exponent = [&](int task) {
-        Exponent e;
-        e.top = stat[task].top;
-        e.c_hi = cf;
-        e.c_lo = c_lo;
-        e.l_steps = 0;
-        e.l_rest = 0.f;
-        return e;
-    };
     int turn = 0;  // which of the words the next sum over the CTAs uses
     // sums over the cluster of the warps' totals, and the first one's over the CTAs before this one
     auto all_sums = [&](long long (&all)[2], long long& before) {
@@ -467,7 +522,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
         if (warp < 2) {
             long long t = lane < VF_WARPS ? warp_total[warp][lane] : 0;
 #pragma unroll
-            for (int o = VF_WARPS / 2; o > 0; o >>= 1) t += __shfl_xor_sync(FULL_MASK, t, o);
+            for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(FULL_MASK, t, o);  // (in all lanes: up to 16 push it)
             if (lane < C) push(&word[turn][warp][rank], lane, t);
         }
         team();
@@ -482,151 +537,138 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
         }
         turn ^= 1;
     };
-    int kept = 0;
+    int kept = 0, token = V;  // V: not this CTA's
     bool cut = false;
-    long long sums[2] = {0, 0}, before;  // of the weights of the row after the kept ones, the target's and the drafter's, in 2^-44
-    while (kept < n - 1) {
-        int keep = state[kept];
-        if (keep == 2 || (keep == 0 && drafter)) {
-            // the blocks of both rows, one after another; the next one's on their way
-            const Row<TYPE> rows[2] = {row_of(kept), row_of(drafter ? n + kept : kept)};
-            const Exponent zs[2] = {exponent(kept), exponent(drafter ? n + kept : kept)};
-            const int count = p.blocks * (1 + drafter);
-            auto fetch = [&](int k) {
-                const int e = k >= p.blocks;
-                return k < count ? (e ? rows[1] : rows[0]).fetch((b0 + k - e * p.blocks) * VF_BLOCK + lane * 8) : Row<TYPE>::none();
-            };
-            typename Row<TYPE>::Raw next = fetch(warp);
-            long long sum[2] = {0, 0};
+    if (tid == 0) s_block = -1;
+    const int t0 = b0 * VF_BLOCK, t1 = t0 + p.blocks * VF_BLOCK;  // this CTA's tokens
 #pragma unroll 1
-            for (int k = warp; k < count; k += VF_WARPS) {
-                const bool e = k >= p.blocks;
-                const Row<TYPE> row = e ? rows[1] : rows[0];
-                const Exponent z = e ? zs[1] : zs[0];
-                float x[8];
-                Row<TYPE>::decode(next, x);
-                next = fetch(k + VF_WARPS);
-                row.make_tame((b0 + k - e * p.blocks) * VF_BLOCK + lane * 8, x);
-                int sa = 0, sb = 0;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    int u, v;
-                    ex_fixed(x[i], z, table, u, v);
-                    sa += u;
-                    sb += v;
-                }
-                const long long s = ((long long)sa << 22) + sb;
-                sum[0] += e ? 0 : s;
-                sum[1] += e ? s : 0;
-            }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) sum[e] += __shfl_xor_sync(FULL_MASK, sum[e], o);
-                if (lane == 0) warp_total[e][warp] = sum[e];
-            }
-            all_sums(sums, before);
-        }
-        if (keep == 2) {
-            if (tid == 0) {
-                const int d = drafts[kept];
-                auto probability = [&](int task, long long sum) {
-                    const double z = ((double)row_of(task).at(d) - (double)stat[task].top) * (1.4426950408889634 / (double)t_tame);
-                    return exp2(z) / ((double)sum * 0x1p-44);
-                };
-                s_keep = (double)unit(a.uniforms[2 * (r0 + kept)]) * (drafter ? probability(n + kept, sums[1]) : 1.0) < probability(kept, sums[0]);
-            }
-            __syncthreads();
-            keep = s_keep;
-        }
-        if (!keep) break;
-        ++kept;
-        if (drafts[kept - 1] == a.eos_id) {
-            cut = true;
+    for (bool drawn = false; !drawn;) {
+#pragma unroll 1
+        for (; !cut && kept < n - 1 && state[kept] == 1; ++kept) cut = fed[kept] == a.eos_id;
+        if (cut) break;
+        if (greedy) {
+            if (rank == 0) token = stat[kept].arg;
             break;
         }
-    }
-
-    // ---- 3: the token ----
-    int token = V;  // V: not this CTA's
-    if (!cut && greedy) {
-        token = rank == 0 ? stat[kept].arg : V;
-    } else if (!cut) {
-        Draw<TYPE> draw;
-        const bool refused = kept < n - 1;
-        draw.mode = !refused ? DRAW_TARGET : drafter ? DRAW_REST : DRAW_WITHOUT;
-        draw.without = refused ? drafts[kept] : -1;
-        draw.p = draw.q = exponent(kept);
-        if (draw.mode == DRAW_REST) {  // by the sums: both distributions in the same units
-            draw.q = exponent(n + kept);
-            divide_by(draw.p, sums[0], table);
-            divide_by(draw.q, sums[1], table);
-        }
-        const Row<TYPE> t = row_of(kept), d = draw.mode == DRAW_REST ? row_of(n + kept) : t;
-        if (tid == 0) s_block = -1;
-        const float number = unit(a.uniforms[2 * (r0 + kept) + 1]);
-        // 0: sums of all blocks; 1: where there are none, those of the target alone; 2: the block that the number falls into
+        // ---- 3: the row that a token is drawn behind, or that has to be looked at in 64 bits ----
+        const bool more = kept < n - 1, near = more && state[kept] == 2;
+        const int other = more && drafter ? n + kept : kept;
+        DrawMode mode = !more ? DRAW_TARGET : drafter ? DRAW_REST : DRAW_WITHOUT;
+        const Row<TYPE> t = row_of(kept), d = row_of(other);
+        const Exponent zp = make_exponent(stat[kept].top, stat[kept].tamed, cf, c_lo);
+        const Exponent zq = make_exponent(stat[other].top, stat[other].tamed, cf, c_lo);
+        const int without = more ? fed[kept] : -1;
+        unsigned long long sp = 0, sq = 0;  // sums, shifted up: weights times the other one's are in the same units
+        int held_from = -1;                 // first token of the window that is held
+        auto hold = [&](int from, long long (&sum)[2]) {
+            __syncthreads();  // (another window may still be read)
+            sum[0] += hold_weights<TYPE>(t, zp, table_at, held_p, from, min(from + window, t1));
+            if (mode == DRAW_REST) sum[1] += hold_weights<TYPE>(d, zq, table_at, held_q, from, min(from + window, t1));
+            held_from = from;
+        };
+        auto weight = [&](int i) {  // of token held_from + i
+            long long w = (long long)held_p.get(i);
+            if (mode == DRAW_REST) w = max((long long)__umul64hi(w, sq) - (long long)__umul64hi(held_q.get(i), sp), 0ll);
+            if (mode == DRAW_WITHOUT && held_from + i == without) w = 0;
+            return w;
+        };
+        // 0: both sums, where they are needed; 1: the weights' sums of blocks; 2: the token
         long long at = 0;
 #pragma unroll 1
-        for (int pass = 0; pass < 3; ++pass) {
-            long long total = 0;
-#pragma unroll 1
-            for (int k = pass < 2 ? warp : warp == 0 ? s_block : -1; k >= 0 && k < p.blocks; k += VF_WARPS) {
-                long long w[8], s = 0;
-                const int j = (b0 + k) * VF_BLOCK + lane * 8;
-                draw.weights(t, d, table, j, w);
+        for (int pass = near || mode == DRAW_REST ? 0 : 1; !drawn;) {
+            long long total[2] = {0, 0}, again[2];  // again: of weights that were added up before
+            if (pass == 2) {
+                const int k = s_block;
+                if (k >= 0) {  // (the whole CTA)
+                    const int from = t0 + k / VF_WINDOW * VF_WINDOW * VF_BLOCK, first = t0 + k * VF_BLOCK + lane * 8;
+                    if (held_from != from) hold(from, again);
+                    __syncthreads();
+                    if (warp == 0) {
+                        long long w[8], s = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s += w[i];
-                if (pass < 2) {
+                        for (int i = 0; i < 8; ++i) s += w[i] = weight(first - from + i);
+                        s = warp_scan(s) + s_before - s;
+                        int found = V;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            s += w[i];
+                            if (s > at && found == V) found = first + i;
+                        }
+                        token = __reduce_min_sync(FULL_MASK, found);
+                    }
+                }
+                drawn = true;
+                break;
+            }
+#pragma unroll 1
+            for (int from = t0; from < t1; from += window) {
+                if (pass == 0) {
+                    hold(from, total);
+                    continue;
+                }
+                if (held_from != from) hold(from, again);
+                __syncthreads();
+                const int blocks = (min(from + window, t1) - from) / VF_BLOCK;
+                long long sum = 0;
+#pragma unroll 1
+                for (int k = warp; k < blocks; k += VF_WARPS) {
+                    long long s = 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s += weight(k * VF_BLOCK + i * 32 + lane);
                     // (s < 2^48: two parts whose sums over a warp have 32 bits)
                     const uint32_t lo = __reduce_add_sync(FULL_MASK, (uint32_t)s & ((1u << 26) - 1)), hi = __reduce_add_sync(FULL_MASK, (uint32_t)(s >> 26));
                     s = ((long long)hi << 26) + lo;
-                    if (lane == 0) block_sum[k] = s;
-                    total += s;
-                    continue;
+                    if (lane == 0) block_sum[(from - t0) / VF_BLOCK + k] = s;
+                    sum += s;
                 }
-                long long x = warp_scan(s) + s_before - s;
-                int found = V;
+                total[0] += lane == 0 ? sum : 0;
+            }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x += w[i];
-                    if (x > at && found == V) found = j - t.shift + i;
-                }
-                token = __reduce_min_sync(FULL_MASK, found);
-                break;
+            for (int o = 16; o > 0; o >>= 1) {
+                total[0] += __shfl_xor_sync(FULL_MASK, total[0], o);
+                total[1] += __shfl_xor_sync(FULL_MASK, total[1], o);
             }
-            if (pass == 2) break;
-            __syncthreads();  // (earlier sums are still read)
             if (lane == 0) {
-                warp_total[0][warp] = total;
-                warp_total[1][warp] = 0;
+                warp_total[0][warp] = total[0];
+                warp_total[1][warp] = total[1];
             }
-            long long all[2];
+            long long all[2], before;
             all_sums(all, before);
-            if (all[0] == 0 && pass == 0) {  // nothing is left of p: p
-                draw.mode = DRAW_TARGET;
-                draw.p.l_steps = 0;
-                draw.p.l_rest = 0.f;
-                continue;
-            }
-            // the token's weight covers this place
-            if (tid == 0) s_at = min((long long)((double)number * (double)all[0]), all[0] - 1) - before;
-            __syncthreads();
-            at = s_at;
-            if (warp == 0 && at >= 0) {
-                long long base = 0;
-                for (int k0 = 0; k0 < p.blocks; k0 += 32) {
-                    const int k = k0 + lane;
-                    const long long s = k < p.blocks ? block_sum[k] : 0, x = base + warp_scan(s);
-                    if (x > at && x - s <= at) {
-                        s_block = k;
-                        s_before = x - s;
-                    }
-                    base = __shfl_sync(FULL_MASK, x, 31);
+            if (pass == 0) {
+                if (near) {
+                    if (tid == 0)
+                        state[kept] = near_kept(unit(a.uniforms[2 * (r0 + kept)]), t.at(without), stat[kept].top, all[0],
+                                                d.at(without), stat[other].top, drafter ? all[1] : 0, t_tame);
+                    __syncthreads();
+                    if (state[kept] == 1) break;  // on to the next draft
                 }
-                __syncwarp();
+                const int up = __clzll(max(all[0], all[1]));
+                sp = (unsigned long long)all[0] << up;
+                sq = (unsigned long long)all[1] << up;
+                pass = 1;
+            } else if (all[0] == 0 && mode != DRAW_TARGET) {  // nothing is left of p: p
+                mode = DRAW_TARGET;
+            } else {
+                // the token's weight covers this place
+                if (tid == 0) s_at = min((long long)((double)unit(numbers[kept]) * (double)all[0]), all[0] - 1) - before;
+                __syncthreads();
+                at = s_at;
+                if (warp == 0 && at >= 0) {
+                    long long base = 0;
+#pragma unroll 1
+                    for (int k0 = 0; k0 < p.blocks; k0 += 32) {
+                        const int k = k0 + lane;
+                        const long long s = k < p.blocks ? block_sum[k] : 0, x = base + warp_scan(s);
+                        if (x > at && x - s <= at) {
+                            s_block = k;
+                            s_before = x - s;
+                        }
+                        base = __shfl_sync(FULL_MASK, x, 31);
+                    }
+                }
+                __syncthreads();
+                pass = 2;
             }
-            pass = 1;
         }
     }
     if (tid == 0 && token < V) {  // one thread of the cluster
@@ -637,8 +679,9 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
     // ---- the other outputs; the pages of what is not kept ----
     if (rank == C - 1) {
         const int after = len - (n - 1 - kept);
+#pragma unroll 1
         for (int i = tid; i < a.max_new; i += VF_THREADS)
-            if (i != kept || cut) out[i] = i < kept ? drafts[i] : -1;
+            if (i != kept || cut) out[i] = i < kept ? fed[i] : -1;
         if (tid == 0) {
             a.out_counts[slot] = cut ? kept : kept + 1;
             a.out_kv_lens[slot] = after;
@@ -646,6 +689,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
         }
         if (a.block_table) {
             const int mask = (1 << p.shift) - 1, from = (after + mask) >> p.shift, to = (len + mask) >> p.shift;
+#pragma unroll 1
             for (int i = from + tid; i < to; i += VF_THREADS) {
                 int* entry = a.block_table + (long long)slot * a.bt_stride + i;
                 const int page = *entry;
@@ -659,9 +703,17 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
     }
 }
 
+cudaError_t allow_wide_cluster(const void* kernel) {  // (setting it again changes nothing)
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+}
 template <int TYPE>
 cudaError_t launch_verify(const DraftArgs& p, cudaStream_t s) {
-    const size_t smem = sizeof(ExTable) + (size_t)p.blocks * sizeof(long long);
+    const size_t stats = 2 * p.a.max_new * (2 + p.ctas) + VF_WARPS, window = (size_t)std::min(p.blocks, VF_WINDOW) * VF_BLOCK;
+    const size_t smem = sizeof(ExTable) + stats * sizeof(Stat) + p.blocks * sizeof(long long) + window * 12;
+    if (p.ctas > 8) {
+        const cudaError_t e = allow_wide_cluster(reinterpret_cast<const void*>(draft_verify_kernel<TYPE>));
+        if (e != cudaSuccess) return e;
+    }
     return launch(draft_verify_kernel<TYPE>, p.a.slots * p.ctas, VF_THREADS, smem, p.ctas, s, p);
 }
 
