@@ -13,6 +13,7 @@
 // its 16 bytes of a query row, taken in the same order, the same two.  No shared memory, no
 // barrier; every warp has several tiles' loads in flight.
 #include <algorithm>
+#include <cstdlib>
 
 #include "weights.cuh"
 
@@ -177,7 +178,7 @@ __global__ void __launch_bounds__(256) key_weights_sum_kernel(const __grid_const
 // How a call runs.
 struct WeightsPlan {
     bool few;
-    int group, key_tiles, segments;
+    int group, key_tiles, tiles, segments;
     size_t need;
 };
 constexpr int KW_TILE = 128;
@@ -209,13 +210,14 @@ int weights_plan(const mtp_key_weights_args* a, WeightsPlan* p) {
     const long long packed = (long long)std::min(a->max_new, a->rows) * p->group;  // rows of a slot and key head
     p->few = packed <= KW_FEW_ROWS;
     p->key_tiles = (int)((std::min((long long)a->max_keys, width) + KW_TILE - 1) / KW_TILE);
-    p->segments = 1;
+    p->segments = p->tiles = 1;
     p->need = 0;
     if (!p->few) {
-        // few keys and many rows: the rows are cut too, until every SM has tiles enough
-        const long long tiles = std::max(1ll, (long long)a->slots * a->n_kv_heads * p->key_tiles);
-        const long long row_tiles = (packed + KW_TILE - 1) / KW_TILE;
-        p->segments = (int)std::max(1ll, std::min((row_tiles + 3) / 4, 4ll * sms / tiles));
+        const long long lists = (long long)a->slots * a->n_kv_heads, row_tiles = (packed + KW_TILE - 1) / KW_TILE;
+        p->tiles = std::getenv("KW_TILES") ? atoi(std::getenv("KW_TILES")) : lists * p->key_tiles >= 4 * sms ? 4 : 1;
+        // few keys and many rows: the rows are cut too, until every SM has work enough
+        const long long groups = std::max(1ll, lists * ((p->key_tiles + p->tiles - 1) / p->tiles));
+        p->segments = (int)std::max(1ll, std::min((row_tiles + 3) / 4, (8ll / (p->tiles == 4 ? 1 : 2) * sms + groups / 2) / groups));
         if (p->segments > 1) p->need = (size_t)p->segments * a->slots * a->n_kv_heads * width * sizeof(float);
     }
     return MTP_OK;
@@ -281,6 +283,7 @@ MTP_API int mtp_key_weights(const mtp_key_weights_args* a, void* workspace, size
         w.window = a->window < w.width ? a->window : 0;
         w.max_new = a->max_new;
         w.keys = std::min(a->max_keys, w.width);
+        w.tiles = p.tiles;
         w.segments = p.segments;
         w.part = static_cast<float*>(workspace);
         w.q_vec = aligned16(a->q) && a->q_stride % 8 == 0;

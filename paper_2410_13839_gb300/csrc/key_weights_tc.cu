@@ -4,14 +4,15 @@
 //   S^T = K Q^T        128 keys x up to 128 packed rows, fp32 in TMEM
 //   w_j += sum_p 2^(c S_jp - l_p)   a key per thread
 //
-// A CTA has 128 keys of a slot and key head, which stay in shared memory; the rows that see one
+// A CTA has 128 or 512 keys of a slot and key head, which stay in shared memory; the rows that see one
 // of them come by, as many tokens as have 128 rows at a time (all heads of a token together, so
 // that one tensor-map box is a tile for any number of heads per key head).  A thread's TMEM lane is its
 // key: its weights add up in a register, the rows' log-sum-exps are read from shared memory, the
-// same one by all lanes, and what a causal or window mask leaves of a tile is a range of columns.  Two
-// places for S: while one is summed the tensor cores make the next.  A tile's sum starts anew
-// and is added to the key's with compensation, so that thousands of rows cost no precision.
-// Two CTAs an SM (each half of TMEM): one's start and end lie behind the other's work.
+// same one by all lanes, and what a causal or window mask leaves of a tile is a range of columns.  A
+// tile's sum starts anew and is added to the key's with compensation, so that thousands of rows cost no
+// precision.
+// 512 keys: four tiles of 128, each with a place for S and four warps; while three are summed the tensor
+// cores make the fourth's.  128 keys: two places, and two CTAs an SM.
 #include <type_traits>
 
 #include "tcgen05.cuh"
@@ -22,14 +23,16 @@ namespace {
 
 constexpr int WT_TILE = 128;
 constexpr uint32_t WT_SUB = 128 * 128;  // 128 rows of 128 bytes
-constexpr int WT_MMA = 4, WT_COPY = 5, WT_THREADS = 192;
 
-template <int HD>
+// TILES: of 128 keys, that a CTA has.
+template <int HD, int TILES>
 struct WtLayout {
-    static constexpr int STAGES = HD == 64 ? 4 : 2;
+    static constexpr int STAGES = HD == 64 ? 4 : 2, CTAS = TILES == 1 ? 2 : 1;  // CTAS: of an SM
+    static constexpr int MMA = 4 * TILES, COPY = MMA + 1, THREADS = (COPY + 1) * 32;
+    static constexpr uint32_t TM_COLS = TILES == 1 ? 2 * WT_TILE : TILES * WT_TILE;
     static constexpr uint32_t OPER = WT_SUB * (HD / 64);
-    static constexpr uint32_t K = 0, Q = OPER, LSE = Q + STAGES * OPER;  // LSE: [4 warps][2][128] floats
-    static constexpr size_t BYTES = 1024 + LSE + 4 * 2 * WT_TILE * 4;
+    static constexpr uint32_t K = 0, Q = TILES * OPER, LSE = Q + STAGES * OPER;  // LSE: [4 TILES warps][2][128] floats
+    static constexpr size_t BYTES = 1024 + LSE + 4 * TILES * 2 * WT_TILE * 4;
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -73,40 +76,48 @@ __device__ __forceinline__ uint32_t idesc(int n) {  // f16_idesc's types are bf1
     return std::is_same<T, Bf16>::value ? d : d & ~((1u << 7) | (1u << 10));
 }
 
-// Grid (key tile and key head, slot, row segment).
-template <class T, int HD>
-__global__ void __launch_bounds__(WT_THREADS, 2)
+// Grid (group of TILES key tiles and key head, slot, row segment).
+template <class T, int HD, int TILES>
+__global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TILES>::CTAS)
     key_weights_tc_kernel(const __grid_constant__ WeightsArgs a, const __grid_constant__ CUtensorMap map,
                           const __grid_constant__ CUtensorMap q_map, int q_tma) {
-    using L = WtLayout<HD>;
+    using L = WtLayout<HD, TILES>;
     constexpr int ST = L::STAGES;
     extern __shared__ unsigned char wt_raw[];
-    __shared__ uint64_t k_full, q_full[ST], q_empty[ST], s_full[2], s_empty[2], drain;
+    __shared__ uint64_t k_full, q_full[ST], q_empty[ST], s_full[4], s_empty[4], drain;
     __shared__ uint32_t tmem_base;
     unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(wt_raw) + 1023) & ~(uintptr_t)1023);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int tile = blockIdx.x / a.kv_heads, head = blockIdx.x - tile * a.kv_heads, slot = blockIdx.y, seg = blockIdx.z;
+    const int group = blockIdx.x / a.kv_heads, head = blockIdx.x - group * a.kv_heads, slot = blockIdx.y, seg = blockIdx.z;
     pdl_launch_dependents();
     pdl_wait();
     bool cut;
     const WeightsSlot s = weights_slot(a, slot, cut);
     if (cut && a.err && blockIdx.x == 0 && seg == 0 && tid == 0) atomicOr(a.err, ERR_BOUNDS);
-    const int key0 = tile * WT_TILE, key1 = min(min(s.len, a.keys), key0 + WT_TILE);
+    const int key0 = group * TILES * WT_TILE, key1 = min(min(s.len, a.keys), key0 + TILES * WT_TILE);
     if (s.n == 0 || key0 >= key1) return;
-    // the tokens that see a key of the tile, `per` at a time; this segment's tiles of them
+    // the tokens that see a key of the group, `per` at a time; this segment's tiles of them
     const int2 tokens = seeing(a, s, key0, key1);
     const int per = WT_TILE / a.group, all = (tokens.y - tokens.x + per - 1) / per;
     const int u0 = (int)((long long)all * seg / a.segments), u1 = (int)((long long)all * (seg + 1) / a.segments);
+    // of those, the tiles of which some token sees a key of key tile t
+    auto range = [&](int t) {
+        const int from = key0 + t * WT_TILE, to = min(key1, from + WT_TILE);
+        if (from >= to) return make_int2(0, 0);
+        const int2 x = seeing(a, s, from, to);
+        if (x.x >= x.y) return make_int2(0, 0);
+        return make_int2(max(u0, (x.x - tokens.x) / per), min(u1, (x.y - tokens.x + per - 1) / per));
+    };
     const int lowest = a.window > 0 ? max(0, s.base - a.window + 1) : 0;  // the first key that some row sees
     const int key = key0 + tid;
-    const bool mine = tid < WT_TILE && key < key1 && key >= lowest;
+    const bool mine = tid < TILES * WT_TILE && key < key1 && key >= lowest;
     float* part = a.part + (((size_t)seg * a.slots + slot) * a.kv_heads + head) * a.width + key;
     if (u0 >= u1) {
         if (a.segments > 1 && mine) *part = 0.f;
         return;
     }
-    if (warp == WT_MMA) {
-        tmem_alloc(&tmem_base, 2 * WT_TILE);
+    if (warp == L::MMA) {
+        tmem_alloc(&tmem_base, L::TM_COLS);
         tmem_relinquish();
     }
     if (tid == 0) {
@@ -116,15 +127,16 @@ __global__ void __launch_bounds__(WT_THREADS, 2)
             mbar_init(&q_full[i], 1);
             mbar_init(&q_empty[i], 1);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 4; ++i) {
             mbar_init(&s_full[i], 1);
             mbar_init(&s_empty[i], 4);
         }
         fence_barrier_init();
     }
     // rows of a tile past the last token's are zeros
-    for (int i = tid; i < (WT_TILE - per * a.group) * 8 * (HD / 64) * ST; i += WT_THREADS) {
-        const int row = per * a.group + i / 8 % (WT_TILE - per * a.group), half = i / 8 / (WT_TILE - per * a.group);
+    const int rest = WT_TILE - per * a.group;
+    for (int i = tid; i < rest * 8 * (HD / 64) * ST; i += L::THREADS) {
+        const int row = per * a.group + i / 8 % rest, half = i / 8 / rest;
         *reinterpret_cast<uint4*>(sm + L::Q + half * WT_SUB + row * 128 + (i & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
     }
     fence_proxy_async();
@@ -133,21 +145,31 @@ __global__ void __launch_bounds__(WT_THREADS, 2)
     tc_fence_after();
     const uint32_t tmem = tmem_base;
     auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(FULL_MASK, mbar_wait(bar, parity & 1, a.err)) != 0; };
+    // the place of a key tile's c-th tile of rows: one of its own, or (one key tile) the two in turn
+    auto place = [](int t, int c) { return TILES == 1 ? c & 1 : t; };
+    auto phase = [](int c) { return TILES == 1 ? c >> 1 : c; };
 
-    if (warp == WT_COPY) {
+    if (warp == L::COPY) {
         // ---- the keys, a lane per page piece, then the rows ----
-        const int P = 1 << a.page_shift, box = min(P, WT_TILE), pieces = WT_TILE / box;
-        const int sub = lane % pieces, half = lane / pieces, at = key0 + sub * box;
-        const bool wanted = half < HD / 64 && at < key1;
-        int block = -1;  // outside the pool: zeros
-        if (wanted) {
-            const int page = a.block_table[(size_t)slot * a.bt_stride + (at >> a.page_shift)];
-            if (page >= 0 && page < a.n_pages) block = page * a.page_blocks + a.layer_block + head;
+        const int P = 1 << a.page_shift, box = min(P, WT_TILE), pieces = TILES * WT_TILE / box;
+        uint32_t bytes = 0;
+        for (int i0 = 0; i0 < pieces; i0 += 32) {
+            const bool wanted = i0 + lane < pieces && key0 + (i0 + lane) * box < key1;
+            bytes += __popc(__ballot_sync(FULL_MASK, wanted)) * box * 128 * (HD / 64);
         }
-        const unsigned have = __ballot_sync(FULL_MASK, wanted);
-        if (lane == 0) mbar_arrive_expect_tx(&k_full, __popc(have) * box * 128);
+        if (lane == 0) mbar_arrive_expect_tx(&k_full, bytes);
         __syncwarp();
-        if (wanted) tma_box(sm + L::K + half * WT_SUB + sub * box * 128, &map, half * 64, at & (P - 1), block, &k_full);
+        for (int i = lane; i < pieces; i += 32) {
+            const int at = key0 + i * box;
+            if (at >= key1) break;
+            const int page = a.block_table[(size_t)slot * a.bt_stride + (at >> a.page_shift)];
+            // (outside the pool: zeros)
+            const int block = page >= 0 && page < a.n_pages ? page * a.page_blocks + a.layer_block + head : -1;
+            const int row = i * box;  // of the group's
+            for (int h = 0; h < HD / 64; ++h)
+                tma_box(sm + L::K + (row / WT_TILE) * L::OPER + h * WT_SUB + (row % WT_TILE) * 128, &map, h * 64, at & (P - 1), block, &k_full);
+        }
+        __syncwarp();
         bool ok = true;
         int n = 0;
         for (; n < u1 - u0; ++n) {
@@ -180,22 +202,35 @@ __global__ void __launch_bounds__(WT_THREADS, 2)
             for (int i = max(0, n - ST); i < n; ++i) mbar_wait(&q_full[i % ST], (i / ST) & 1, nullptr);
         }
         __syncwarp();
-    } else if (warp == WT_MMA) {
+    } else if (warp == L::MMA) {
         if (elect_one()) {
             const uint64_t k = sw128_desc(smem_addr(sm + L::K));
+            int2 has[TILES];
+            int done[TILES];
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                has[t] = range(t);
+                done[t] = 0;
+            }
             bool ok = mbar_wait(&k_full, 0, a.err);
             for (int n = 0; ok && n < u1 - u0; ++n) {
                 const int st = n % ST, count = min(per, tokens.y - (tokens.x + (u0 + n) * per)) * a.group;
-                ok = mbar_wait(&q_full[st], (n / ST) & 1, a.err) && (n < 2 || mbar_wait(&s_empty[n & 1], (n / 2 - 1) & 1, a.err));
-                if (!ok) break;
-                tc_fence_after();
+                ok = mbar_wait(&q_full[st], (n / ST) & 1, a.err);
                 const uint64_t q = sw128_desc(smem_addr(sm + L::Q + st * L::OPER));
                 const uint32_t id = idesc<T>(count == per * a.group ? WT_TILE : (count + 15) & ~15);
 #pragma unroll
-                for (int d = 0; d < HD / 16; ++d)
-                    tc_mma(tmem + (n & 1) * WT_TILE, k + (((d >> 2) * WT_SUB + (d & 3) * 32) >> 4),
-                           q + (((d >> 2) * WT_SUB + (d & 3) * 32) >> 4), id, d != 0);
-                tc_commit(&s_full[n & 1]);
+                for (int t = 0; t < TILES; ++t) {
+                    if (!ok || u0 + n < has[t].x || u0 + n >= has[t].y) continue;
+                    const int c = done[t]++, at = place(t, c);
+                    if (phase(c) > 0) ok = mbar_wait(&s_empty[at], (phase(c) - 1) & 1, a.err);
+                    if (!ok) continue;
+                    tc_fence_after();
+#pragma unroll
+                    for (int d = 0; d < HD / 16; ++d)
+                        tc_mma(tmem + at * WT_TILE, k + ((t * L::OPER + (d >> 2) * WT_SUB + (d & 3) * 32) >> 4),
+                               q + (((d >> 2) * WT_SUB + (d & 3) * 32) >> 4), id, d != 0);
+                    tc_commit(&s_full[at]);
+                }
                 tc_commit(&q_empty[st]);
             }
             tc_commit(&drain);  // every MMA has ended before TMEM is given back
@@ -203,7 +238,9 @@ __global__ void __launch_bounds__(WT_THREADS, 2)
         }
         __syncwarp();
     } else {
-        // ---- the sums: a key per thread ----
+        // ---- the sums: a key per thread, four warps to a key tile ----
+        const int tile = warp >> 2;
+        const int2 has = range(tile);
         float* lse = reinterpret_cast<float*>(sm + L::LSE) + warp * 2 * WT_TILE;
         const int heads = a.kv_heads * a.group;
         int col_token[4], col_head[4];
@@ -215,73 +252,80 @@ __global__ void __launch_bounds__(WT_THREADS, 2)
         }
         // the negated log-sum-exps of a tile's columns, in log2 units; of columns past the rows -inf: no weight
         float l[4];
-        auto ask = [&](int n) {
-            const int token = tokens.x + (u0 + n) * per, count = min(per, tokens.y - token);
+        auto ask = [&](int u) {
+            const int token = tokens.x + u * per, count = min(per, tokens.y - token);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 l[i] = INFINITY;
                 if (col_token[i] < count) l[i] = a.lse[(long long)(s.row0 + token + col_token[i]) * heads + col_head[i]];
             }
         };
-        ask(0);
-        float sum = 0.f, rest = 0.f;  // with compensation
-        const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
+        if (has.x < has.y) ask(has.x);
+        float sum = 0.f, lost = 0.f;  // with compensation
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         bool ok = true;
-        for (int n = 0; n < u1 - u0; ++n) {
-            float* lb = lse + (n & 1) * WT_TILE;
+        for (int u = has.x; u < has.y; ++u) {
+            const int c = u - has.x, at = place(tile, c);
+            float* lb = lse + (c & 1) * WT_TILE;
 #pragma unroll
             for (int i = 0; i < 4; ++i) lb[lane + 32 * i] = -l[i] * LOG2E;
             __syncwarp();
-            if (n + 1 < u1 - u0) ask(n + 1);
-            const int token = tokens.x + (u0 + n) * per, count = min(per, tokens.y - token), cols = count * a.group;
+            if (u + 1 < has.y) ask(u + 1);
+            const int token = tokens.x + u * per, count = min(per, tokens.y - token), cols = count * a.group;
             // columns [c0, c1) see the key
             const int i0 = max(0, key - s.base - token), i1 = a.window > 0 ? min(count, key + a.window - s.base - token) : count;
             const int c0 = min(i0, count) * a.group, c1 = max(i1, 0) * a.group;
             const bool full = __all_sync(FULL_MASK, c0 == 0 && c1 == per * a.group) != 0;
-            ok = wait(&s_full[n & 1], n / 2);
+            ok = wait(&s_full[at], phase(c));
             if (!ok) break;
             tc_fence_after();
-            const uint32_t ts = lanes + (n & 1) * WT_TILE;
+            const uint32_t ts = lanes + at * WT_TILE;
             const int chunks = full ? 4 : (cols + 31) >> 5;
             float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-            float x[2][32];
-            auto add = [&](const float (&y)[32], int chunk) {
+            // (a tile's warps alone: the next columns are read while these are summed; other tiles' warps do as well)
+            constexpr int AHEAD = TILES == 1 ? 2 : 1;
+            float x[AHEAD][32];
+            auto add = [&](const float (&y)[32], int chunk, auto masked) {  // (a body of its own without masks, which are as much work again)
                 const float4* nl = reinterpret_cast<const float4*>(lb + chunk * 32);
-                const float2 c = make_float2(a.scale_log2, a.scale_log2);
+                const float2 scale = make_float2(a.scale_log2, a.scale_log2);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float4 z = nl[e];
-                    const float2 u = fma2(make_float2(y[4 * e], y[4 * e + 1]), c, make_float2(z.x, z.y));
-                    const float2 v = fma2(make_float2(y[4 * e + 2], y[4 * e + 3]), c, make_float2(z.z, z.w));
-                    float2 p = make_float2(ex2(u.x), ex2(u.y)), q = make_float2(ex2(v.x), ex2(v.y));
-                    if (!full) {
-                        const unsigned at = chunk * 32 + 4 * e - c0, width = max(c1 - c0, 0);
-                        p.x = at < width ? p.x : 0.f;
-                        p.y = at + 1 < width ? p.y : 0.f;
-                        q.x = at + 2 < width ? q.x : 0.f;
-                        q.y = at + 3 < width ? q.y : 0.f;
+                    const float2 v = fma2(make_float2(y[4 * e], y[4 * e + 1]), scale, make_float2(z.x, z.y));
+                    const float2 w = fma2(make_float2(y[4 * e + 2], y[4 * e + 3]), scale, make_float2(z.z, z.w));
+                    float2 p = make_float2(ex2(v.x), ex2(v.y)), q = make_float2(ex2(w.x), ex2(w.y));
+                    if (decltype(masked)::value) {
+                        const unsigned first = chunk * 32 + 4 * e - c0, width = max(c1 - c0, 0);
+                        p.x = first < width ? p.x : 0.f;
+                        p.y = first + 1 < width ? p.y : 0.f;
+                        q.x = first + 2 < width ? q.x : 0.f;
+                        q.y = first + 3 < width ? q.y : 0.f;
                     }
                     acc[0] = add2(acc[0], p);
                     acc[1] = add2(acc[1], q);
                 }
             };
-            tmem_ld_issue<32>(ts, x[0]);
+            if (AHEAD == 2) tmem_ld_issue<32>(ts, x[0]);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                if (c >= chunks) break;
+            for (int i = 0; i < 4; ++i) {
+                if (i >= chunks) break;
+                float(&now)[32] = x[i % AHEAD];
+                if (AHEAD == 1) tmem_ld_issue<32>(ts + i * 32, now);
                 tmem_ld_wait();
-                tmem_ld_done(x[c & 1]);
-                if (c + 1 < chunks) {
-                    tmem_ld_issue<32>(ts + (c + 1) * 32, x[(c + 1) & 1]);
-                } else {  // S is in registers
+                tmem_ld_done(now);
+                if (AHEAD == 2 && i + 1 < chunks) tmem_ld_issue<32>(ts + (i + 1) * 32, x[(i + 1) % AHEAD]);
+                if (i + 1 == chunks) {  // S is in registers
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&s_empty[n & 1]);
+                    if (lane == 0) mbar_arrive(&s_empty[at]);
                 }
-                add(x[c & 1], c);
+                if (full)
+                    add(now, i, std::false_type());
+                else
+                    add(now, i, std::true_type());
             }
-            const float y = ((acc[0].x + acc[0].y) + (acc[1].x + acc[1].y)) - rest, t = sum + y;
-            rest = (t - sum) - y;
+            const float y = ((acc[0].x + acc[0].y) + (acc[1].x + acc[1].y)) - lost, t = sum + y;
+            lost = (t - sum) - y;
             sum = t;
         }
         if (ok && mine) {
@@ -295,16 +339,20 @@ __global__ void __launch_bounds__(WT_THREADS, 2)
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == WT_MMA) tmem_dealloc(tmem, 2 * WT_TILE);
+    if (warp == L::MMA) tmem_dealloc(tmem, L::TM_COLS);
 }
 
+template <class T, int HD, int TILES>
+cudaError_t launch_tiles(const WeightsArgs& a, const CUtensorMap& map, const CUtensorMap& q_map, bool q_tma, int key_tiles, cudaStream_t s) {
+    using L = WtLayout<HD, TILES>;
+    const auto kern = key_weights_tc_kernel<T, HD, TILES>;
+    const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), L::BYTES);
+    if (e != cudaSuccess) return e;
+    return launch_ex(kern, dim3((key_tiles + TILES - 1) / TILES * a.kv_heads, a.slots, a.segments), L::THREADS, L::BYTES, s, 1, a, map, q_map, (int)q_tma);
+}
 template <class T, int HD>
 cudaError_t launch_tc(const WeightsArgs& a, const CUtensorMap& map, const CUtensorMap& q_map, bool q_tma, int key_tiles, cudaStream_t s) {
-    const auto kern = key_weights_tc_kernel<T, HD>;
-    const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(kern), WtLayout<HD>::BYTES);
-    return e == cudaSuccess ? launch_ex(kern, dim3(key_tiles * a.kv_heads, a.slots, a.segments), WT_THREADS, WtLayout<HD>::BYTES, s, 1, a, map,
-                                        q_map, (int)q_tma)
-                            : e;
+    return a.tiles == 1 ? launch_tiles<T, HD, 1>(a, map, q_map, q_tma, key_tiles, s) : launch_tiles<T, HD, 4>(a, map, q_map, q_tma, key_tiles, s);
 }
 
 }  // namespace

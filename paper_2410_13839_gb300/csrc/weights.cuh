@@ -23,6 +23,7 @@ struct WeightsArgs {
     int slots, rows, kv_heads, group, dim, page_shift, bt_stride, n_pages, width;
     int page_blocks, layer_block;  // (layer, K | V, head) blocks of a page; the layer's first
     int window, max_new, keys;     // keys: of a slot at most
+    int tiles;                     // of 128 keys that a CTA of the tensor-core kernel has: 1 or 4
     int segments;                  // row segments of the tensor-core kernel; > 1: sums into `part`
     float* part;                   // [segments][slots][kv_heads][width]
     bool q_vec;                    // rows 16-byte aligned
