@@ -11,8 +11,9 @@
 // same one by all lanes, and what a causal or window mask leaves of a tile is a range of columns.  A
 // tile's sum starts anew and is added to the key's with compensation, so that thousands of rows cost no
 // precision.
-// 512 keys: four tiles of 128, each with a place for S and four warps; while three are summed the tensor
-// cores make the fourth's.  128 keys: two places, and two CTAs an SM.
+// 512 keys: two pairs of tiles of 128, each with a place for S and eight warps, four for each half of the
+// columns; a thread has a key of both tiles, so that the log-sum-exps are read once for two.  While one pair
+// is summed the tensor cores make the other's.  128 keys: two places, four warps, and two CTAs an SM.
 #include <type_traits>
 
 #include "tcgen05.cuh"
@@ -28,11 +29,13 @@ constexpr uint32_t WT_SUB = 128 * 128;  // 128 rows of 128 bytes
 template <int HD, int TILES>
 struct WtLayout {
     static constexpr int STAGES = HD == 64 ? 4 : 2, CTAS = TILES == 1 ? 2 : 1;  // CTAS: of an SM
+    // sums: key tiles of a group of warps (they read the rows' log-sum-exps once for all), halves of the columns
+    static constexpr int KT = TILES == 1 ? 1 : 2, HALVES = TILES == 1 ? 1 : 2;
     static constexpr int MMA = 4 * TILES, COPY = MMA + 1, THREADS = (COPY + 1) * 32;
     static constexpr uint32_t TM_COLS = TILES == 1 ? 2 * WT_TILE : TILES * WT_TILE;
     static constexpr uint32_t OPER = WT_SUB * (HD / 64);
-    static constexpr uint32_t K = 0, Q = TILES * OPER, LSE = Q + STAGES * OPER;  // LSE: [4 TILES warps][2][128] floats
-    static constexpr size_t BYTES = 1024 + LSE + 4 * TILES * 2 * WT_TILE * 4;
+    static constexpr uint32_t K = 0, Q = TILES * OPER, LSE = Q + STAGES * OPER;  // LSE: [warps][2][columns of a warp] floats
+    static constexpr size_t BYTES = 1024 + LSE + 4 * TILES * 2 * (WT_TILE / HALVES) * 4;
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -109,11 +112,11 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
         return make_int2(max(u0, (x.x - tokens.x) / per), min(u1, (x.y - tokens.x + per - 1) / per));
     };
     const int lowest = a.window > 0 ? max(0, s.base - a.window + 1) : 0;  // the first key that some row sees
-    const int key = key0 + tid;
-    const bool mine = tid < TILES * WT_TILE && key < key1 && key >= lowest;
-    float* part = a.part + (((size_t)seg * a.slots + slot) * a.kv_heads + head) * a.width + key;
+    float* part = a.part + (((size_t)seg * a.slots + slot) * a.kv_heads + head) * a.width + key0;
     if (u0 >= u1) {
-        if (a.segments > 1 && mine) *part = 0.f;
+        if (a.segments > 1)
+            for (int key = key0 + tid; key < key1; key += L::THREADS)
+                if (key >= lowest) part[key - key0] = 0.f;
         return;
     }
     if (warp == L::MMA) {
@@ -129,7 +132,7 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
         }
         for (int i = 0; i < 4; ++i) {
             mbar_init(&s_full[i], 1);
-            mbar_init(&s_empty[i], 4);
+            mbar_init(&s_empty[i], 4 * L::HALVES);
         }
         fence_barrier_init();
     }
@@ -145,9 +148,18 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
     tc_fence_after();
     const uint32_t tmem = tmem_base;
     auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(FULL_MASK, mbar_wait(bar, parity & 1, a.err)) != 0; };
-    // the place of a key tile's c-th tile of rows: one of its own, or (one key tile) the two in turn
-    auto place = [](int t, int c) { return TILES == 1 ? c & 1 : t; };
+    // the place of a group of key tiles' c-th tile of rows: one of its own, or (one key tile) the two in turn
+    constexpr int KT = L::KT, H = L::HALVES;
+    auto place = [](int g, int c) { return TILES == 1 ? c & 1 : g; };
     auto phase = [](int c) { return TILES == 1 ? c >> 1 : c; };
+    auto group_range = [&](int g) {  // tiles of rows of which some token sees a key of the group's key tiles
+        int2 x = range(g * KT);
+        if (KT > 1) {
+            const int2 y = range(g * KT + 1);
+            x = x.x >= x.y ? y : y.x >= y.y ? x : make_int2(min(x.x, y.x), max(x.y, y.y));
+        }
+        return x;
+    };
 
     if (warp == L::COPY) {
         // ---- the keys, a lane per page piece, then the rows ----
@@ -205,12 +217,12 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
     } else if (warp == L::MMA) {
         if (elect_one()) {
             const uint64_t k = sw128_desc(smem_addr(sm + L::K));
-            int2 has[TILES];
-            int done[TILES];
+            int2 has[TILES / KT];
+            int done[TILES / KT];
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) {
-                has[t] = range(t);
-                done[t] = 0;
+            for (int g = 0; g < TILES / KT; ++g) {
+                has[g] = group_range(g);
+                done[g] = 0;
             }
             bool ok = mbar_wait(&k_full, 0, a.err);
             for (int n = 0; ok && n < u1 - u0; ++n) {
@@ -219,16 +231,18 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
                 const uint64_t q = sw128_desc(smem_addr(sm + L::Q + st * L::OPER));
                 const uint32_t id = idesc<T>(count == per * a.group ? WT_TILE : (count + 15) & ~15);
 #pragma unroll
-                for (int t = 0; t < TILES; ++t) {
-                    if (!ok || u0 + n < has[t].x || u0 + n >= has[t].y) continue;
-                    const int c = done[t]++, at = place(t, c);
+                for (int g = 0; g < TILES / KT; ++g) {
+                    if (!ok || u0 + n < has[g].x || u0 + n >= has[g].y) continue;
+                    const int c = done[g]++, at = place(g, c);
                     if (phase(c) > 0) ok = mbar_wait(&s_empty[at], (phase(c) - 1) & 1, a.err);
                     if (!ok) continue;
                     tc_fence_after();
 #pragma unroll
-                    for (int d = 0; d < HD / 16; ++d)
-                        tc_mma(tmem + at * WT_TILE, k + ((t * L::OPER + (d >> 2) * WT_SUB + (d & 3) * 32) >> 4),
-                               q + (((d >> 2) * WT_SUB + (d & 3) * 32) >> 4), id, d != 0);
+                    for (int t = 0; t < KT; ++t)
+#pragma unroll
+                        for (int d = 0; d < HD / 16; ++d)
+                            tc_mma(tmem + (at * KT + t) * WT_TILE, k + (((g * KT + t) * L::OPER + (d >> 2) * WT_SUB + (d & 3) * 32) >> 4),
+                                   q + (((d >> 2) * WT_SUB + (d & 3) * 32) >> 4), id, d != 0);
                     tc_commit(&s_full[at]);
                 }
                 tc_commit(&q_empty[st]);
@@ -238,104 +252,147 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
         }
         __syncwarp();
     } else {
-        // ---- the sums: a key per thread, four warps to a key tile ----
-        const int tile = warp >> 2;
-        const int2 has = range(tile);
-        float* lse = reinterpret_cast<float*>(sm + L::LSE) + warp * 2 * WT_TILE;
+        // ---- the sums: a thread has a key of each of its group's key tiles, and its half of the columns ----
+        constexpr int COLS = WT_TILE / H, W = COLS / 4;  // columns of a warp, of a step
+        const int g = warp / (4 * H), h = (warp >> 2) % H, row = tid & (WT_TILE - 1);
+        const int2 has = group_range(g);
+        float* lse = reinterpret_cast<float*>(sm + L::LSE) + warp * 2 * COLS;
         const int heads = a.kv_heads * a.group;
-        int col_token[4], col_head[4];
+        int col_token[COLS / 32], col_head[COLS / 32];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = lane + 32 * i;
+        for (int i = 0; i < COLS / 32; ++i) {
+            const int c = h * COLS + lane + 32 * i;
             col_token[i] = c / a.group;
             col_head[i] = head * a.group + c - col_token[i] * a.group;
         }
         // the negated log-sum-exps of a tile's columns, in log2 units; of columns past the rows -inf: no weight
-        float l[4];
+        float l[COLS / 32];
         auto ask = [&](int u) {
             const int token = tokens.x + u * per, count = min(per, tokens.y - token);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < COLS / 32; ++i) {
                 l[i] = INFINITY;
                 if (col_token[i] < count) l[i] = a.lse[(long long)(s.row0 + token + col_token[i]) * heads + col_head[i]];
             }
         };
         if (has.x < has.y) ask(has.x);
-        float sum = 0.f, lost = 0.f;  // with compensation
-        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        float sum[KT], lost[KT];  // with compensation
+#pragma unroll
+        for (int t = 0; t < KT; ++t) sum[t] = lost[t] = 0.f;
+        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16) + h * COLS;
         bool ok = true;
         for (int u = has.x; u < has.y; ++u) {
-            const int c = u - has.x, at = place(tile, c);
-            float* lb = lse + (c & 1) * WT_TILE;
+            const int c = u - has.x, at = place(g, c);
+            float* lb = lse + (c & 1) * COLS;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) lb[lane + 32 * i] = -l[i] * LOG2E;
+            for (int i = 0; i < COLS / 32; ++i) lb[lane + 32 * i] = -l[i] * LOG2E;
             __syncwarp();
             if (u + 1 < has.y) ask(u + 1);
             const int token = tokens.x + u * per, count = min(per, tokens.y - token), cols = count * a.group;
-            // columns [c0, c1) see the key
-            const int i0 = max(0, key - s.base - token), i1 = a.window > 0 ? min(count, key + a.window - s.base - token) : count;
-            const int c0 = min(i0, count) * a.group, c1 = max(i1, 0) * a.group;
-            const bool full = __all_sync(FULL_MASK, c0 == 0 && c1 == per * a.group) != 0;
+            // columns [c0, c1) of the warp's see the key
+            int c0[KT], c1[KT];
+            bool full = true;
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                const int key = key0 + (g * KT + t) * WT_TILE + row;
+                const int i0 = max(0, key - s.base - token), i1 = a.window > 0 ? min(count, key + a.window - s.base - token) : count;
+                c0[t] = min(i0, count) * a.group;
+                c1[t] = max(i1, 0) * a.group;
+                full = full && c0[t] == 0 && c1[t] == per * a.group;
+                c0[t] -= h * COLS;
+                c1[t] -= h * COLS;
+            }
+            full = __all_sync(FULL_MASK, full) != 0;
             ok = wait(&s_full[at], phase(c));
             if (!ok) break;
             tc_fence_after();
-            const uint32_t ts = lanes + at * WT_TILE;
-            const int chunks = full ? 4 : (cols + 31) >> 5;
-            float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-            // (a tile's warps alone: the next columns are read while these are summed; other tiles' warps do as well)
+            const uint32_t ts = lanes + at * KT * WT_TILE;
+            const int steps = full ? 4 : min(4, (max(0, cols - h * COLS) + W - 1) / W);
+            float2 acc[KT][2];
+#pragma unroll
+            for (int t = 0; t < KT; ++t) acc[t][0] = acc[t][1] = make_float2(0.f, 0.f);
+            // (one key tile: the next columns are read while these are summed; more warps do without)
             constexpr int AHEAD = TILES == 1 ? 2 : 1;
-            float x[AHEAD][32];
-            auto add = [&](const float (&y)[32], int chunk, auto masked) {  // (a body of its own without masks, which are as much work again)
-                const float4* nl = reinterpret_cast<const float4*>(lb + chunk * 32);
+            float x[AHEAD][KT][W];
+            auto read = [&](int i) {
+#pragma unroll
+                for (int t = 0; t < KT; ++t) tmem_ld_issue<W>(ts + t * WT_TILE + i * W, x[i % AHEAD][t]);
+            };
+            auto released = [&]() {  // S is in registers
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s_empty[at]);
+            };
+            auto add = [&](int i, auto masked) {  // (a body of its own without masks, which are as much work again)
+                const float4* nl = reinterpret_cast<const float4*>(lb + i * W);
                 const float2 scale = make_float2(a.scale_log2, a.scale_log2);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
+                for (int e = 0; e < W / 4; ++e) {
                     const float4 z = nl[e];
-                    const float2 v = fma2(make_float2(y[4 * e], y[4 * e + 1]), scale, make_float2(z.x, z.y));
-                    const float2 w = fma2(make_float2(y[4 * e + 2], y[4 * e + 3]), scale, make_float2(z.z, z.w));
-                    float2 p = make_float2(ex2(v.x), ex2(v.y)), q = make_float2(ex2(w.x), ex2(w.y));
-                    if (decltype(masked)::value) {
-                        const unsigned first = chunk * 32 + 4 * e - c0, width = max(c1 - c0, 0);
-                        p.x = first < width ? p.x : 0.f;
-                        p.y = first + 1 < width ? p.y : 0.f;
-                        q.x = first + 2 < width ? q.x : 0.f;
-                        q.y = first + 3 < width ? q.y : 0.f;
+#pragma unroll
+                    for (int t = 0; t < KT; ++t) {
+                        const float* y = x[i % AHEAD][t] + 4 * e;
+                        const float2 v = fma2(make_float2(y[0], y[1]), scale, make_float2(z.x, z.y));
+                        const float2 w = fma2(make_float2(y[2], y[3]), scale, make_float2(z.z, z.w));
+                        float2 p = make_float2(ex2(v.x), ex2(v.y)), q = make_float2(ex2(w.x), ex2(w.y));
+                        if (decltype(masked)::value) {
+                            const int at = i * W + 4 * e;
+                            p.x = at >= c0[t] && at < c1[t] ? p.x : 0.f;
+                            p.y = at + 1 >= c0[t] && at + 1 < c1[t] ? p.y : 0.f;
+                            q.x = at + 2 >= c0[t] && at + 2 < c1[t] ? q.x : 0.f;
+                            q.y = at + 3 >= c0[t] && at + 3 < c1[t] ? q.y : 0.f;
+                        }
+                        acc[t][0] = add2(acc[t][0], p);
+                        acc[t][1] = add2(acc[t][1], q);
                     }
-                    acc[0] = add2(acc[0], p);
-                    acc[1] = add2(acc[1], q);
                 }
             };
-            if (AHEAD == 2) tmem_ld_issue<32>(ts, x[0]);
+            if (AHEAD == 2 && steps > 0) read(0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (i >= chunks) break;
-                float(&now)[32] = x[i % AHEAD];
-                if (AHEAD == 1) tmem_ld_issue<32>(ts + i * 32, now);
+                if (i >= steps) break;
+                if (AHEAD == 1) read(i);
                 tmem_ld_wait();
-                tmem_ld_done(now);
-                if (AHEAD == 2 && i + 1 < chunks) tmem_ld_issue<32>(ts + (i + 1) * 32, x[(i + 1) % AHEAD]);
-                if (i + 1 == chunks) {  // S is in registers
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&s_empty[at]);
-                }
+#pragma unroll
+                for (int t = 0; t < KT; ++t) tmem_ld_done(x[i % AHEAD][t]);
+                if (AHEAD == 2 && i + 1 < steps) read(i + 1);
+                if (i + 1 == steps) released();
                 if (full)
-                    add(now, i, std::false_type());
+                    add(i, std::false_type());
                 else
-                    add(now, i, std::true_type());
+                    add(i, std::true_type());
             }
-            const float y = ((acc[0].x + acc[0].y) + (acc[1].x + acc[1].y)) - lost, t = sum + y;
-            lost = (t - sum) - y;
-            sum = t;
-        }
-        if (ok && mine) {
-            if (a.segments > 1) {
-                *part = sum;
-            } else {
-                float* out = a.weights + slot * a.w_slot + (long long)head * a.width + key;
-                *out = key < s.base ? *out + sum : sum;
+            if (steps == 0) released();
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                const float y = ((acc[t][0].x + acc[t][0].y) + (acc[t][1].x + acc[t][1].y)) - lost[t], v = sum[t] + y;
+                lost[t] = (v - sum[t]) - y;
+                sum[t] = v;
             }
         }
+        if constexpr (H == 2) {  // the halves' sums as one
+            float* other = reinterpret_cast<float*>(sm + L::LSE) + (warp & ~7) * 2 * COLS + row;  // (the group's log-sum-exps are done with)
+            asm volatile("bar.sync %0, 256;" ::"r"(1 + g) : "memory");
+            if (h == 1)
+#pragma unroll
+                for (int t = 0; t < KT; ++t) other[t * WT_TILE] = sum[t];
+            asm volatile("bar.sync %0, 256;" ::"r"(1 + g) : "memory");
+            if (h == 0)
+#pragma unroll
+                for (int t = 0; t < KT; ++t) sum[t] += other[t * WT_TILE];
+        }
+        if (ok && h == 0)
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                const int key = key0 + (g * KT + t) * WT_TILE + row;
+                if (key >= key1 || key < lowest) continue;
+                if (a.segments > 1) {
+                    part[key - key0] = sum[t];
+                } else {
+                    float* out = a.weights + slot * a.w_slot + (long long)head * a.width + key;
+                    *out = key < s.base ? *out + sum[t] : sum[t];
+                }
+            }
     }
     tc_fence_before();
     __syncthreads();
