@@ -257,22 +257,24 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
         const int g = warp / (4 * H), h = (warp >> 2) % H, row = tid & (WT_TILE - 1);
         const int2 has = group_range(g);
         float* lse = reinterpret_cast<float*>(sm + L::LSE) + warp * 2 * COLS;
-        const int heads = a.kv_heads * a.group;
-        int col_token[COLS / 32], col_head[COLS / 32];
+        // the log-sum-exps of the columns of the next tile of rows
+        const int heads = a.kv_heads * a.group, first = tokens.x + has.x * per;
+        int col_token[COLS / 32];
+        const float* from[COLS / 32];
 #pragma unroll
         for (int i = 0; i < COLS / 32; ++i) {
             const int c = h * COLS + lane + 32 * i;
             col_token[i] = c / a.group;
-            col_head[i] = head * a.group + c - col_token[i] * a.group;
+            from[i] = a.lse + (long long)(s.row0 + first + col_token[i]) * heads + head * a.group + c - col_token[i] * a.group;
         }
-        // the negated log-sum-exps of a tile's columns, in log2 units; of columns past the rows -inf: no weight
-        float l[COLS / 32];
+        float l[COLS / 32];  // negated, in log2 units; of columns past the rows -inf: no weight
         auto ask = [&](int u) {
-            const int token = tokens.x + u * per, count = min(per, tokens.y - token);
+            const int count = min(per, tokens.y - (tokens.x + u * per));
 #pragma unroll
             for (int i = 0; i < COLS / 32; ++i) {
                 l[i] = INFINITY;
-                if (col_token[i] < count) l[i] = a.lse[(long long)(s.row0 + token + col_token[i]) * heads + col_head[i]];
+                if (col_token[i] < count) l[i] = *from[i];
+                from[i] += per * heads;
             }
         };
         if (has.x < has.y) ask(has.x);
@@ -285,24 +287,13 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
             const int c = u - has.x, at = place(g, c);
             float* lb = lse + (c & 1) * COLS;
 #pragma unroll
-            for (int i = 0; i < COLS / 32; ++i) lb[lane + 32 * i] = -l[i] * LOG2E;
+            for (int i = 0; i < COLS / 32; ++i) lb[lane + 32 * i] = l[i] * -LOG2E;
             __syncwarp();
             if (u + 1 < has.y) ask(u + 1);
             const int token = tokens.x + u * per, count = min(per, tokens.y - token), cols = count * a.group;
-            // columns [c0, c1) of the warp's see the key
-            int c0[KT], c1[KT];
-            bool full = true;
-#pragma unroll
-            for (int t = 0; t < KT; ++t) {
-                const int key = key0 + (g * KT + t) * WT_TILE + row;
-                const int i0 = max(0, key - s.base - token), i1 = a.window > 0 ? min(count, key + a.window - s.base - token) : count;
-                c0[t] = min(i0, count) * a.group;
-                c1[t] = max(i1, 0) * a.group;
-                full = full && c0[t] == 0 && c1[t] == per * a.group;
-                c0[t] -= h * COLS;
-                c1[t] -= h * COLS;
-            }
-            full = __all_sync(FULL_MASK, full) != 0;
+            // whether every token sees every key of the group's tiles
+            const int low = key0 + g * KT * WT_TILE, high = low + KT * WT_TILE - 1, pos = s.base + token;
+            const bool full = count == per && pos >= high && (a.window <= 0 || pos + per - 1 < low + a.window);
             ok = wait(&s_full[at], phase(c));
             if (!ok) break;
             tc_fence_after();
@@ -323,6 +314,14 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&s_empty[at]);
             };
+            // columns [c0, c1) of the warp's see the thread's keys
+            int c0[KT], c1[KT];
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                const int ahead = low + t * WT_TILE + row - pos;  // the key's position less the first token's
+                c0[t] = min(max(0, ahead), count) * a.group - h * COLS;
+                c1[t] = (a.window > 0 ? max(0, min(count, ahead + a.window)) : count) * a.group - h * COLS;
+            }
             auto add = [&](int i, auto masked) {  // (a body of its own without masks, which are as much work again)
                 const float4* nl = reinterpret_cast<const float4*>(lb + i * W);
                 const float2 scale = make_float2(a.scale_log2, a.scale_log2);
