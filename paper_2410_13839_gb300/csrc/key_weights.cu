@@ -13,7 +13,6 @@
 // its 16 bytes of a query row, taken in the same order, the same two.  No shared memory, no
 // barrier; every warp has several tiles' loads in flight.
 #include <algorithm>
-#include <cstdlib>
 
 #include "weights.cuh"
 
@@ -214,7 +213,10 @@ int weights_plan(const mtp_key_weights_args* a, WeightsPlan* p) {
     p->need = 0;
     if (!p->few) {
         const long long lists = (long long)a->slots * a->n_kv_heads, row_tiles = (packed + KW_TILE - 1) / KW_TILE;
-        p->tiles = std::getenv("KW_TILES") ? atoi(std::getenv("KW_TILES")) : lists * p->key_tiles >= 4 * sms ? 4 : 1;
+        // four key tiles of a CTA read the rows from L2 a quarter as often: for long contexts that have work for all SMs.  One, four: two
+        // chunks after 6000 to 9000 keys 607, 484 us, 8 slots of 9 new tokens and up to 16000 keys 57, 44; 25 prompts of up to
+        // 578 tokens 41.5, 51.8, one chunk of 2000 tokens after 4000, one key head, 37.7, 42.9
+        p->tiles = p->key_tiles >= 16 && lists * p->key_tiles >= 8 * sms ? 4 : 1;
         // few keys and many rows: the rows are cut too, until every SM has work enough
         const long long groups = std::max(1ll, lists * ((p->key_tiles + p->tiles - 1) / p->tiles));
         p->segments = (int)std::max(1ll, std::min((row_tiles + 3) / 4, (8ll / (p->tiles == 4 ? 1 : 2) * sms + groups / 2) / groups));

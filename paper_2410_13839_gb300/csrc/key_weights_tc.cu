@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
         constexpr int COLS = WT_TILE / H, W = COLS / 4;  // columns of a warp, of a step
         const int g = warp / (4 * H), h = (warp >> 2) % H, row = tid & (WT_TILE - 1);
         const int2 has = group_range(g);
-        float* lse = reinterpret_cast<float*>(sm + L::LSE) + warp * 2 * COLS;
+        const uint32_t lse = smem_addr(sm + L::LSE) + warp * 2 * COLS * 4;
         // the log-sum-exps of the columns of the next tile of rows
         const int heads = a.kv_heads * a.group, first = tokens.x + has.x * per;
         int col_token[COLS / 32];
@@ -285,9 +285,9 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
         bool ok = true;
         for (int u = has.x; u < has.y; ++u) {
             const int c = u - has.x, at = place(g, c);
-            float* lb = lse + (c & 1) * COLS;
+            const uint32_t lb = lse + (c & 1) * COLS * 4;
 #pragma unroll
-            for (int i = 0; i < COLS / 32; ++i) lb[lane + 32 * i] = l[i] * -LOG2E;
+            for (int i = 0; i < COLS / 32; ++i) asm volatile("st.shared.f32 [%0], %1;" ::"r"(lb + (lane + 32 * i) * 4), "f"(l[i] * -LOG2E) : "memory");
             __syncwarp();
             if (u + 1 < has.y) ask(u + 1);
             const int token = tokens.x + u * per, count = min(per, tokens.y - token), cols = count * a.group;
@@ -323,11 +323,11 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
                 c1[t] = (a.window > 0 ? max(0, min(count, ahead + a.window)) : count) * a.group - h * COLS;
             }
             auto add = [&](int i, auto masked) {  // (a body of its own without masks, which are as much work again)
-                const float4* nl = reinterpret_cast<const float4*>(lb + i * W);
                 const float2 scale = make_float2(a.scale_log2, a.scale_log2);
 #pragma unroll
                 for (int e = 0; e < W / 4; ++e) {
-                    const float4 z = nl[e];
+                    float4 z;
+                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(z.x), "=f"(z.y), "=f"(z.z), "=f"(z.w) : "r"(lb + (i * W + 4 * e) * 4));
 #pragma unroll
                     for (int t = 0; t < KT; ++t) {
                         const float* y = x[i % AHEAD][t] + 4 * e;
