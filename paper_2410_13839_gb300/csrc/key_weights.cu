@@ -228,9 +228,9 @@ int weights_plan(const mtp_key_weights_args* a, WeightsPlan* p) {
 template <class T, int HD>
 cudaError_t launch_few(const WeightsArgs& a, cudaStream_t s) {
     const int packed = std::min(a.max_new, a.rows) * a.group;
-    constexpr int KT = HD == 64 ? 4 : 2;
-    // a CTA's keys: each warp a few times its tiles
-    const int chunk = KW_WARPS * 16 * KT * 2;
+    // Tiles in flight, and how often: once, twice, four and eight times two tiles 18.9, 15.9, 15.4, 18.7 us (a step of 32 slots) and 63, 52, 49, 50
+    // (4 drafts on 8 long contexts); four tiles of 64 dims 17 to 22, of 128 dims 74, one of 128 dims 52 at best.
+    constexpr int KT = 2, chunk = KW_WARPS * 16 * KT * 4;
     const dim3 grid((a.keys + chunk - 1) / chunk * a.kv_heads, a.slots);
     const auto kern = packed <= 8 ? key_weights_kernel<T, HD, 1, KT> : packed <= 16 ? key_weights_kernel<T, HD, 2, KT> : key_weights_kernel<T, HD, 4, KT>;
     return launch_ex(kern, grid, KW_THREADS, 0, s, 1, a, chunk);
