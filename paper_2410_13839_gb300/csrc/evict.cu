@@ -2,15 +2,16 @@
 // key head the keys of largest weight stay, beside the first and the last ones, move up in their
 // order, and the pages behind them become free.
 //
-// Two kernels.  The first selects: a CTA has the weights of one (slot, layer, key head) in shared memory, as
-// whole numbers in the order of the weights, and finds the m-th largest by its highest 11 bits, the 11
+// A CTA has one (slot, layer, key head).  It selects: the weights are in shared memory, as
+// whole numbers in the order of the weights, and the m-th largest is found by its highest 11 bits, the 11
 // after them and the last 10, each time by counting how many keys have each value.  Of the keys
-// equal to it the first ones stay.  Ballots and prefix sums then give each key that stays its place; its
-// row in the pool goes to a list in the workspace.
-// The second moves keys and values in place: a CTA has one (slot, layer, key head, keys | values) run and
-// goes through its list from the front, a stage of rows at a time: read, barrier, write.  Row j is
-// read from place old_j >= j, and places before a stage's are never read again, so that no copy of the
-// cache is needed; further stages are on their way into shared memory meanwhile.
+// equal to it the first ones stay.  Ballots and prefix sums then give each key that stays its place, and a list
+// of their rows in the pool takes the weights' place.
+// Then it moves keys and values in place: it goes through its list from the front, a stage of rows at a
+// time: read, barrier, write.  Row j is read from place old_j >= j, and places before a stage's are never read
+// again, so that no copy of the cache is needed; further stages are on their way into shared memory
+// meanwhile.  Memory bounds it: one CTA's selection lies behind another's moves.  A small kernel before looks at
+// the tables: no count changes before every page has been looked at.
 #include <algorithm>
 #include <climits>
 
@@ -20,14 +21,17 @@ namespace mtp {
 namespace {
 
 constexpr int EV_BINS = 2048;
-constexpr int EV_HELD = 53248;  // keys whose order shared memory holds
+constexpr int EV_HELD = 32768;  // keys whose order shared memory holds
+constexpr int EV_SMEM = 231424;  // shared memory of a CTA that has an SM to itself
+constexpr int EV_STAGES = 6;    // of rows on their way into shared memory
 
 struct EvictArgs {
     mtp_cache_evict_args a;
     int shift;      // page_size = 1 << shift
     int width;      // bt_stride * page_size: weights of a slot, layer and head
     int heads;      // layers * n_kv_heads
-    int* list;      // workspace [slots][layers][heads][width]: row of the pool (page * page_size + offset) of each key that stays
+    int smem;       // bytes of shared memory
+    int* list;      // workspace [slots][layers][heads][width], of wide tables: row of the pool (page * page_size + offset) of each key that stays
 };
 
 // A slot: keys before and after, the first and last ones that stay whatever their weight.
@@ -49,68 +53,140 @@ __device__ __forceinline__ uint32_t order_of(float w) {
     return w != w ? 0xffffffffu : (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
-// HELD: the weights' order is kept in shared memory; else (rows past EV_HELD keys) it is made again in every pass.
-template <int NT, bool HELD>
-__global__ void __launch_bounds__(NT) evict_select_kernel(const __grid_constant__ EvictArgs p) {
-    constexpr int WARPS = NT / 32, B = EV_BINS / NT;
-    extern __shared__ uint32_t ev_keys[];  // [width]
-    __shared__ __align__(16) uint32_t bins[EV_BINS];
-    __shared__ uint32_t part[WARPS], tied_of[WARPS], kept_of[WARPS];
-    __shared__ int s_bin, s_left, s_count;
+// What can be said of a slot without its weights: whether it may be changed, its table and length afterwards.  Copies the
+// counts, where they go to another array.
+constexpr int EC_THREADS = 1024;
+__global__ void __launch_bounds__(EC_THREADS) evict_check_kernel(const __grid_constant__ EvictArgs p) {
     const mtp_cache_evict_args& a = p.a;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int run = blockIdx.x, slot = run / p.heads;
-    const bool first_run = run - slot * p.heads == 0;
+    const int tid = threadIdx.x, slot = blockIdx.x, mask = (1 << p.shift) - 1;
     pdl_launch_dependents();
-    for (int i = tid; i < EV_BINS; i += NT) bins[i] = 0;
     pdl_wait();
-    const int mask = (1 << p.shift) - 1;
-    const EvictSlot s = evict_slot(a, slot);
-    const float* w = a.weights + (long long)run * p.width;
-    const int lo = s.sinks, hi = s.len - s.recent, want = s.after - s.sinks - s.recent;  // of keys [lo, hi) so many
-    bool bad = s.len < 0 || s.len > p.width || a.keep[slot] < 0;
     if (a.out_page_refs != a.page_refs)
-        for (long long i = (long long)run * NT + tid; i < a.n_pages; i += (long long)gridDim.x * NT) a.out_page_refs[i] = a.page_refs[i];
+        for (int i = slot * EC_THREADS + tid; i < a.n_pages; i += gridDim.x * EC_THREADS) a.out_page_refs[i] = a.page_refs[i];
+    if (slot >= a.slots) return;
+    const EvictSlot s = evict_slot(a, slot);
     const int* table = a.block_table + (long long)slot * a.bt_stride;
-    const bool moves = !bad && s.after < s.len;
-    auto order_at = [&](int at) { return at >= lo && at < hi ? order_of(w[at]) : 0u; };  // 0: not to be chosen
-    if (moves) {
+    bool bad = s.len < 0 || s.len > p.width || a.keep[slot] < 0;
+    const int written = (s.after + mask) >> p.shift;
+    if (!bad && s.after < s.len) {
         // every held page is one and is counted; those that are written are in no other table
-        const int held = (s.len + mask) >> p.shift, written = (s.after + mask) >> p.shift, same = s.sinks >> p.shift;
-        int page[2];
-        auto look = [&](int c) { return c < held ? table[c] : INT_MAX; };
-        page[0] = look(tid);
-        page[1] = look(tid + NT);
-        if (HELD)
-#pragma unroll 8
-            for (int i = tid; i < s.len; i += NT) ev_keys[i] = order_at(i);
-        for (int c = tid; c < held; c += 2 * NT) {
-            int n[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) n[e] = page[e] >= 0 && page[e] < a.n_pages ? a.page_refs[page[e]] : 0;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int at = c + e * NT;
-                bad |= at < held && (n[e] < 1 || (n[e] > 1 && at >= same && at < written));
-                page[e] = look(at + 2 * NT);
-            }
+        const int held = (s.len + mask) >> p.shift, same = s.sinks >> p.shift;
+#pragma unroll 4
+        for (int c = tid; c < held; c += EC_THREADS) {
+            const int page = table[c], n = page >= 0 && page < a.n_pages ? a.page_refs[page] : 0;
+            bad |= n < 1 || (n > 1 && c >= same && c < written);
         }
     }
     bad = __syncthreads_or(bad) != 0;
-    if (first_run) {
-        const int used = bad ? a.bt_stride : (s.after + mask) >> p.shift;
-        for (int c = tid; c < a.bt_stride; c += NT) a.out_block_table[(long long)slot * a.bt_stride + c] = c < used ? table[c] : -1;
-        if (tid == 0) {
-            a.out_kv_lens[slot] = bad ? s.len : s.after;
-            a.out_status[slot] = bad ? MTP_ERR_INVALID : MTP_OK;
-        }
+    const int used = bad ? a.bt_stride : written;
+    for (int c = tid; c < a.bt_stride; c += EC_THREADS) a.out_block_table[(long long)slot * a.bt_stride + c] = c < used ? table[c] : -1;
+    if (tid == 0) {
+        a.out_kv_lens[slot] = bad ? s.len : s.after;
+        a.out_status[slot] = bad ? MTP_ERR_INVALID : MTP_OK;
     }
+}
+
+__device__ __forceinline__ void copy16(void* dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
+}
+// The rows of a list (row of the pool of each key that stays, in their order) to their places, of one layer and head: keys, values or both.  A
+// thread has a fixed 16-byte piece of a row, in every UNROLL * (threads / pieces)-th row; it writes what it has read itself, so
+// that the stages need no barrier of their own.
+template <int NT, int UNROLL>
+__device__ __forceinline__ void move_rows(const EvictArgs& p, const EvictSlot& s, const int* table, const int* list, uint4* ring, int layer, int head,
+                                          int kv0, int kvs) {
+    const mtp_cache_evict_args& a = p.a;
+    const int tid = threadIdx.x, mask = (1 << p.shift) - 1;
+    const int vecs = a.head_dim / 8, pieces = vecs * kvs, rows = NT / pieces, r0 = tid / pieces, v = tid - r0 * pieces, step = rows * UNROLL;
+    const bool active = r0 < rows;
+    // a piece of row `row` (page * page_size + offset): the pool's blocks of a page apart, the head's among them
+    const int kv = kv0 + v / vecs;
+    uint4* pool = static_cast<uint4*>(a.kv_pool) + ((((long long)layer * 2 + kv) * a.n_kv_heads + head) << p.shift) * vecs + v % vecs;
+    const long long page_step = ((long long)p.heads * 2 << p.shift) * vecs;
+    auto at = [&](int page, int offset) { return pool + page * page_step + offset * vecs; };
+    int from[UNROLL];  // rows of the stage that is asked for next, on their way
+    auto look = [&](int j0) {
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int j = j0 + u * rows + r0;
+            from[u] = active && j < s.after ? list[j] : -1;
+        }
+    };
+    auto ask = [&](int stage) {
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u)
+            if (from[u] >= 0) copy16(ring + (stage * UNROLL + u) * NT + tid, at(from[u] >> p.shift, from[u] & mask));
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int next = s.sinks;  // (the first rows stay where they are)
+    look(next);
+#pragma unroll 1
+    for (int k = 0; k < EV_STAGES - 1; ++k) {
+        ask(k);
+        look(next += step);
+    }
+    int in = EV_STAGES - 1, out = 0;
+#pragma unroll 1
+    for (int j0 = s.sinks; j0 < s.after; j0 += step) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(EV_STAGES - 2) : "memory");
+        __syncthreads();  // every row of this stage and the ones before is read
+        ask(in);
+        look(next += step);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int j = j0 + u * rows + r0;
+            if (active && j < s.after) *at(table[j >> p.shift], j & mask) = ring[(out * UNROLL + u) * NT + tid];
+        }
+        in = in + 1 == EV_STAGES ? 0 : in + 1;
+        out = out + 1 == EV_STAGES ? 0 : out + 1;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+}
+// the slot's pages that become free
+template <int NT>
+__device__ __forceinline__ void free_pages(const EvictArgs& p, const EvictSlot& s, const int* table) {
+    const int mask = (1 << p.shift) - 1;
+    for (int c = ((s.after + mask) >> p.shift) + threadIdx.x; c < (s.len + mask) >> p.shift; c += NT) atomicSub(p.a.out_page_refs + table[c], 1);
+}
+
+constexpr size_t ring_bytes(int threads, int unroll) { return (size_t)EV_STAGES * unroll * threads * 16; }
+
+// Selection, and the moves: grid (run, its parts).  HELD: the weights' order is kept in shared memory, where the list takes its place, and the
+// CTA moves the rows (of keys and values, or one part's); else (rows past EV_HELD keys) the order is made again in every pass, and the list
+// goes to the workspace.
+template <int NT, bool HELD, int UNROLL>
+__global__ void __launch_bounds__(NT) evict_kernel(const __grid_constant__ EvictArgs p) {
+    constexpr int WARPS = NT / 32, B = EV_BINS / NT, BATCH = 4;
+    extern __shared__ __align__(16) unsigned char ev_sm[];  // the order of the weights, then the list; behind them the counts of a pass, then the ring
+    __shared__ uint32_t part[WARPS], tied_of[2][WARPS], kept_of[2][WARPS];
+    __shared__ int s_bin, s_left, s_count;
+    uint32_t* keys = reinterpret_cast<uint32_t*>(ev_sm);
+    uint32_t* bins = keys + (HELD ? p.width : 0);  // (widths are multiples of 16)
+    const mtp_cache_evict_args& a = p.a;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int run = blockIdx.x, sub = blockIdx.y, slot = run / p.heads, rest = run - slot * p.heads;
+    pdl_launch_dependents();
+    for (int i = tid; i < EV_BINS; i += NT) bins[i] = 0;
+    pdl_wait();
+    const EvictSlot s = evict_slot(a, slot);
+    const bool moves = a.out_status[slot] == MTP_OK && s.after < s.len;
+    const float* w = a.weights + (long long)run * p.width;
     float* out = a.out_weights + (long long)run * p.width;
-    if (bad || !moves) {
-        for (int i = tid; i < min(max(s.len, 0), p.width); i += NT) out[i] = w[i];
+    if (!moves) {
+        if (sub == 0)
+            for (int i = tid; i < min(max(s.len, 0), p.width); i += NT) out[i] = w[i];
         return;
     }
-    auto key_at = [&](int at) { return at >= s.len ? 0u : HELD ? ev_keys[at] : order_at(at); };
+    const int mask = (1 << p.shift) - 1;
+    const int* table = a.block_table + (long long)slot * a.bt_stride;
+    if (HELD && rest == 0 && sub == 0) free_pages<NT>(p, s, table);
+    const int lo = s.sinks, hi = s.len - s.recent, want = s.after - s.sinks - s.recent;  // of keys [lo, hi) so many
+    auto order_at = [&](int at) { return at >= lo && at < hi ? order_of(w[at]) : 0u; };  // 0: not to be chosen
+    if (HELD)
+#pragma unroll 8
+        for (int i = tid; i < s.len; i += NT) keys[i] = order_at(i);
+    __syncthreads();
+    auto key_at = [&](int at) { return at >= s.len ? 0u : HELD ? keys[at] : order_at(at); };
 
     // the want-th largest, from its highest bits: how many keys have each value of the next 11 bits
     uint32_t border = 0;
@@ -176,145 +252,104 @@ __global__ void __launch_bounds__(NT) evict_select_kernel(const __grid_constant_
             width = shift == 21 ? 11 : 10;
             shift -= width;
         }
-    // a warp's keys, in their order: how many stay for sure, and how many are on a border of which only the first `left` stay
-    const int per = ((s.len + NT - 1) / NT) * 32, first = warp * per, last = min(s.len, first + per);
-    const bool ties = want > 0 && !all;
+    // Keys NT * BATCH at a time, in their order, a warp's in one piece: how many of each warp stay, then their places.  A key goes to a
+    // place at or before its own, and the ones of a segment are read before any is written.
+    const bool ties = want > 0 && !all;  // of the keys on the border only the first `left` stay
     border = want > 0 ? max(border, 1u) : 0xffffffffu;
     auto sure = [&](int at, uint32_t key) {
         return at < lo || (at >= hi && at < s.len) || (want > 0 && (ties ? key > border : key >= border));
     };
-    int n_sure = 0, n_tied = 0;
-#pragma unroll 4
-    for (int i0 = first; i0 < last; i0 += 32) {
-        const int at = i0 + lane;
-        const uint32_t key = key_at(at);
-        n_sure += __popc(__ballot_sync(FULL_MASK, sure(at, key)));
-        if (ties) n_tied += __popc(__ballot_sync(FULL_MASK, key == border));
-    }
-    if (lane == 0) {
-        kept_of[warp] = n_sure;
-        tied_of[warp] = n_tied;
-    }
-    __syncthreads();
-    const int tied_before = (int)__reduce_add_sync(FULL_MASK, lane < warp ? tied_of[lane] : 0u);
-    int place = (int)__reduce_add_sync(FULL_MASK, lane < warp ? kept_of[lane] : 0u) + (ties ? min(tied_before, left) : 0);
-    left = max(0, left - tied_before);
-    int* list = p.list + (long long)run * p.width;
+    int* list = HELD ? reinterpret_cast<int*>(keys) : p.list + (long long)run * p.width;
     const unsigned below = (1u << lane) - 1;
-    constexpr int BATCH = 4;  // whose reads are on their way together
-    for (int i0 = first; i0 < last; i0 += 32 * BATCH) {
+    int place = 0;
+    for (int i0 = 0, turn = 0; i0 < s.len; i0 += NT * BATCH, turn ^= 1) {
+        const int mine = i0 + warp * 32 * BATCH + lane;
+        uint32_t key[BATCH];
+        int n_sure = 0, n_tied = 0;
+#pragma unroll
+        for (int e = 0; e < BATCH; ++e) {
+            key[e] = key_at(mine + e * 32);
+            n_sure += __popc(__ballot_sync(FULL_MASK, sure(mine + e * 32, key[e])));
+            if (ties) n_tied += __popc(__ballot_sync(FULL_MASK, key[e] == border));
+        }
+        if (lane == 0) {
+            kept_of[turn][warp] = n_sure;
+            tied_of[turn][warp] = n_tied;
+        }
+        __syncthreads();
+        const int sure_all = lane < WARPS ? (int)kept_of[turn][lane] : 0, tied_all = lane < WARPS ? (int)tied_of[turn][lane] : 0;
+        const int tied_before = __reduce_add_sync(FULL_MASK, lane < warp ? tied_all : 0), tied = __reduce_add_sync(FULL_MASK, tied_all);
+        int to = place + __reduce_add_sync(FULL_MASK, lane < warp ? sure_all : 0) + (ties ? min(tied_before, left) : 0);
+        int take = max(0, left - tied_before);
+        place += __reduce_add_sync(FULL_MASK, sure_all) + (ties ? min(tied, left) : 0);
+        left = max(0, left - tied);
         int dst[BATCH], page[BATCH];
         float weight[BATCH];
 #pragma unroll
         for (int e = 0; e < BATCH; ++e) {
-            const int at = i0 + e * 32 + lane;
-            const bool there = at < last;
-            const uint32_t key = there ? key_at(at) : 0u;
-            bool keep = there && sure(at, key);
+            const int at = mine + e * 32;
+            bool keep = sure(at, key[e]);
             if (ties) {
-                const unsigned tied = __ballot_sync(FULL_MASK, key == border);
-                keep |= key == border && __popc(tied & below) < left;
-                left = max(0, left - __popc(tied));
+                const unsigned tied = __ballot_sync(FULL_MASK, key[e] == border);
+                keep |= key[e] == border && __popc(tied & below) < take;
+                take = max(0, take - __popc(tied));
             }
             const unsigned kept = __ballot_sync(FULL_MASK, keep);
-            dst[e] = keep ? place + __popc(kept & below) : -1;
-            place += __popc(kept);
+            dst[e] = keep ? to + __popc(kept & below) : -1;
+            to += __popc(kept);
             page[e] = keep ? table[at >> p.shift] : 0;
             // the weight is in its order but for the sign of 0 and NaN's bits, and where there is none
-            const bool plain = key != 0 && key != 0x80000000u && key != 0xffffffffu;
-            weight[e] = plain ? __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key) : keep ? w[at] : 0.f;
+            const bool plain = key[e] != 0 && key[e] != 0x80000000u && key[e] != 0xffffffffu;
+            weight[e] = plain ? __uint_as_float(key[e] & 0x80000000u ? key[e] ^ 0x80000000u : ~key[e]) : keep ? w[at] : 0.f;
         }
 #pragma unroll
         for (int e = 0; e < BATCH; ++e) {
             if (dst[e] < 0) continue;
-            out[dst[e]] = weight[e];
-            list[dst[e]] = (page[e] << p.shift) + ((i0 + e * 32 + lane) & mask);
+            if (sub == 0) out[dst[e]] = weight[e];
+            list[dst[e]] = (page[e] << p.shift) + ((mine + e * 32) & mask);
         }
     }
+    if (!HELD) return;
+    __syncthreads();  // the list is there
+    const int layer = rest / a.n_kv_heads, head = rest - layer * a.n_kv_heads;
+    // the ring has what the list leaves: twice the rows a stage where that is enough
+    const int begin = (s.after * 4 + 15) & ~15, kvs = gridDim.y == 1 ? 2 : 1;
+    uint4* ring = reinterpret_cast<uint4*>(ev_sm + begin);
+    if (begin + (int)ring_bytes(NT, 2 * UNROLL) <= p.smem)
+        move_rows<NT, 2 * UNROLL>(p, s, table, list, ring, layer, head, sub, kvs);
+    else
+        move_rows<NT, UNROLL>(p, s, table, list, ring, layer, head, sub, kvs);
 }
 
-constexpr int EV_THREADS = 256, EV_STAGES = 6;
-
-__device__ __forceinline__ void copy16(void* dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
-}
-
-// Grid (run * 2 + keys | values).  A thread has a fixed 16-byte piece of a row, in every EV_UNROLL * (threads / pieces)-th row; it
-// writes what it has read itself, so that the stages need no barrier of their own.
-template <int EV_UNROLL>
-__global__ void __launch_bounds__(EV_THREADS) evict_move_kernel(const __grid_constant__ EvictArgs p) {
-    extern __shared__ uint4 ev_ring[];  // [EV_STAGES][EV_UNROLL][EV_THREADS]
+// The moves of a list in the workspace.  Grid (run * 2 + keys | values).
+constexpr int EM_THREADS = 256, EM_UNROLL = 4;
+__global__ void __launch_bounds__(EM_THREADS) evict_move_kernel(const __grid_constant__ EvictArgs p) {
+    extern __shared__ __align__(16) unsigned char ev_sm[];
     const mtp_cache_evict_args& a = p.a;
-    const int tid = threadIdx.x, run = blockIdx.x >> 1, kv = blockIdx.x & 1, slot = run / p.heads, rest = run - slot * p.heads;
+    const int run = blockIdx.x >> 1, kv = blockIdx.x & 1, slot = run / p.heads, rest = run - slot * p.heads;
     pdl_launch_dependents();
     pdl_wait();
     const EvictSlot s = evict_slot(a, slot);
     if (a.out_status[slot] != MTP_OK || s.after == s.len) return;
     const int* table = a.block_table + (long long)slot * a.bt_stride;
-    const int mask = (1 << p.shift) - 1;
-    if (rest == 0 && kv == 0)  // the slot's pages that become free
-        for (int c = ((s.after + mask) >> p.shift) + tid; c < (s.len + mask) >> p.shift; c += EV_THREADS) atomicSub(a.out_page_refs + table[c], 1);
+    if (rest == 0 && kv == 0) free_pages<EM_THREADS>(p, s, table);
     const int layer = rest / a.n_kv_heads, head = rest - layer * a.n_kv_heads;
-    const int vecs = a.head_dim / 8, rows = EV_THREADS / vecs, r0 = tid / vecs, v = tid - r0 * vecs, step = rows * EV_UNROLL;
-    const bool active = r0 < rows;
-    const int* list = p.list + (long long)run * p.width;
-    // a piece of row `row` (page * page_size + offset): the pool's blocks of a page apart, the head's among them
-    uint4* pool = static_cast<uint4*>(a.kv_pool) + ((((long long)layer * 2 + kv) * a.n_kv_heads + head) << p.shift) * vecs + v;
-    const long long page_step = ((long long)p.heads * 2 << p.shift) * vecs;
-    auto at = [&](int page, int offset) { return pool + page * page_step + offset * vecs; };
-    int from[EV_UNROLL];  // rows of the stage that is asked for next, on their way
-    auto look = [&](int j0) {
-#pragma unroll
-        for (int u = 0; u < EV_UNROLL; ++u) {
-            const int j = j0 + u * rows + r0;
-            from[u] = active && j < s.after ? list[j] : -1;
-        }
-    };
-    auto ask = [&](int stage) {
-#pragma unroll
-        for (int u = 0; u < EV_UNROLL; ++u)
-            if (from[u] >= 0) copy16(ev_ring + (stage * EV_UNROLL + u) * EV_THREADS + tid, at(from[u] >> p.shift, from[u] & mask));
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-    int next = s.sinks;  // (the first rows stay where they are)
-    look(next);
-#pragma unroll 1
-    for (int k = 0; k < EV_STAGES - 1; ++k) {
-        ask(k);
-        look(next += step);
-    }
-    int in = EV_STAGES - 1, out = 0;
-#pragma unroll 1
-    for (int j0 = s.sinks; j0 < s.after; j0 += step) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(EV_STAGES - 2) : "memory");
-        __syncthreads();  // every row of this stage and the ones before is read
-        ask(in);
-        look(next += step);
-#pragma unroll
-        for (int u = 0; u < EV_UNROLL; ++u) {
-            const int j = j0 + u * rows + r0;
-            if (active && j < s.after) *at(table[j >> p.shift], j & mask) = ev_ring[(out * EV_UNROLL + u) * EV_THREADS + tid];
-        }
-        in = in + 1 == EV_STAGES ? 0 : in + 1;
-        out = out + 1 == EV_STAGES ? 0 : out + 1;
-    }
-    asm volatile("cp.async.wait_all;" ::: "memory");
+    move_rows<EM_THREADS, EM_UNROLL>(p, s, table, p.list + (long long)run * p.width, reinterpret_cast<uint4*>(ev_sm), layer, head, kv, 1);
 }
 
-template <int UNROLL>
-cudaError_t launch_move(const EvictArgs& p, int ctas, cudaStream_t s) {
-    return launch(evict_move_kernel<UNROLL>, ctas, EV_THREADS, (size_t)EV_STAGES * UNROLL * EV_THREADS * 16, 1, s, p);
-}
-cudaError_t launch_move(const EvictArgs& p, int ctas, cudaStream_t s) {
-    int dev = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e != cudaSuccess) return e;
-    return ctas > 2 * sms ? launch_move<2>(p, ctas, s) : launch_move<4>(p, ctas, s);
+template <int NT, bool HELD, int UNROLL>
+cudaError_t launch_evict(EvictArgs p, int parts, cudaStream_t s) {
+    const int runs = p.a.slots * p.heads;
+    size_t smem = HELD ? ring_bytes(NT, UNROLL) + (size_t)p.width * 4 : EV_BINS * 4;
+    if (HELD && NT == 1024) smem = EV_SMEM;  // (one CTA an SM)
+    p.smem = (int)smem;
+    const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(evict_kernel<NT, HELD, UNROLL>), smem);
+    return e == cudaSuccess ? launch_ex(evict_kernel<NT, HELD, UNROLL>, dim3(runs, parts), NT, smem, s, 1, p) : e;
 }
 
 size_t evict_workspace(const mtp_cache_evict_args* a) {
-    return (size_t)a->slots * a->layers * a->n_kv_heads * a->bt_stride * a->page_size * sizeof(int);
+    const size_t width = (size_t)a->bt_stride * a->page_size;
+    return width <= EV_HELD ? 0 : (size_t)a->slots * a->layers * a->n_kv_heads * width * sizeof(int);
 }
 bool evict_sizes(const mtp_cache_evict_args* a) {
     return a && a->slots >= 1 && a->slots <= 8192 && a->bt_stride >= 1 && page_size_ok(a->page_size) &&
@@ -347,20 +382,30 @@ MTP_API int mtp_cache_evict(const mtp_cache_evict_args* a, void* workspace, size
             a->out_weights == a->weights)
             return invalid("cache_evict: the new lengths, tables and weights need buffers of their own");
         if (!aligned16(a->kv_pool)) return invalid("cache_evict: kv_pool must be 16-byte aligned");
-        if (!workspace || !aligned16(workspace) || workspace_bytes < evict_workspace(a))
+        if (evict_workspace(a) > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < evict_workspace(a)))
             return invalid("cache_evict: workspace %zu bytes, need %zu, 16-byte aligned", workspace_bytes, evict_workspace(a));
-        const EvictArgs p{*a, log2_of(a->page_size), a->bt_stride * a->page_size, a->layers * a->n_kv_heads, static_cast<int*>(workspace)};
+        const EvictArgs p{*a, log2_of(a->page_size), a->bt_stride * a->page_size, a->layers * a->n_kv_heads, 0, static_cast<int*>(workspace)};
         const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
         const int runs = a->slots * p.heads;
-        cudaError_t e;
-        const size_t held = p.width <= EV_HELD ? (size_t)p.width * sizeof(uint32_t) : 0;
-        if (p.width <= 4096)
-            e = launch(evict_select_kernel<256, true>, runs, 256, held, 1, s, p);
-        else if (held > 0)
-            e = launch(evict_select_kernel<1024, true>, runs, 1024, held, 1, s, p);
-        else
-            e = launch(evict_select_kernel<1024, false>, runs, 1024, 0, 1, s, p);
-        if (e == cudaSuccess) e = launch_move(p, runs * 2, s);
+        int dev = 0, sms = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+        if (e == cudaSuccess)
+            e = launch_ex(evict_check_kernel, dim3(std::max(a->slots, std::min(sms, a->n_pages / (4 * EC_THREADS)))), EC_THREADS, 0, s, 1, p);
+        if (e != cudaSuccess) return cuda_status(e, "cache_evict");
+        if (p.width <= EV_HELD) {
+            // Threads by the table's width, whose keys shared memory holds: CTAs of an SM 3, 2, 1.  Where all keys and values have room on the SMs
+            // at once, a CTA each (both make the selection).
+            if (p.width <= 4096)
+                e = runs * 2 <= 3 * sms ? launch_evict<512, true, 1>(p, 2, s) : launch_evict<256, true, 2>(p, 1, s);
+            else if (p.width <= 12288)
+                e = launch_evict<512, true, 1>(p, runs * 2 <= 2 * sms ? 2 : 1, s);
+            else
+                e = launch_evict<1024, true, 1>(p, runs * 2 <= sms ? 2 : 1, s);
+        } else {
+            e = launch_evict<1024, false, 1>(p, 1, s);
+            if (e == cudaSuccess) e = launch(evict_move_kernel, runs * 2, EM_THREADS, ring_bytes(EM_THREADS, EM_UNROLL), 1, s, p);
+        }
         return cuda_status(e, "cache_evict");
     });
 }

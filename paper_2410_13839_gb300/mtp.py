@@ -545,7 +545,7 @@ def mtp_cache_evict_workspace_bytes(args: MtpCacheEvictArgs) -> int:
     return int(lib.mtp_cache_evict_workspace_bytes(ctypes.byref(args)))
 
 
-def mtp_cache_evict(args: MtpCacheEvictArgs, workspace, workspace_bytes: int, stream=None) -> None:
+def mtp_cache_evict(args: MtpCacheEvictArgs, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
     """Every slot's keys of largest weight stay, in their order, and the pages behind them become free."""
     check(lib.mtp_cache_evict(ctypes.byref(args), _ptr(workspace), workspace_bytes, _stream_handle(stream)))
 

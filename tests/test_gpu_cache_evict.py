@@ -110,7 +110,7 @@ def _check(torch, o, want):
     ([300, 180], [64, 170], 64, 0, 32, 1, 3, 128), ([200, 130], [10, 130], 50, 50, 64, 2, 1, 8),
     ([1088], [1024], 4, 256, 64, 2, 4, 64), ([2000, 700, 701], [700] * 3, 4, 128, 64, 2, 2, 64),
     ([500, 400], [399, 1], 0, 399, 128, 1, 2, 256), ([2500, 100], [1300, 99], 3, 7, 16, 1, 2, 128),
-    ([9000], [4097], 64, 1000, 128, 1, 2, 24)])
+    ([9000], [4097], 64, 1000, 128, 1, 2, 24), ([20000, 300], [5000, 299], 64, 700, 64, 1, 2, 64)])
 def test_the_keys_of_largest_weight_stay(weights, lens, keep, sinks, recent, page, layers, kv_heads, dim):
     torch = pytest.importorskip("torch")
     mtp = lib_module()

@@ -86,10 +86,12 @@ def test_cache_evict(libpath, kw):  # noqa: F811
 
 def test_cache_evict_workspace(libpath):  # noqa: F811
     from paper_2410_13839_gb300 import mtp
-    need = mtp.mtp_cache_evict_workspace_bytes(_evict())
+    assert mtp.mtp_cache_evict_workspace_bytes(_evict()) == 0  # tables of 64 keys need none
+    wide = dict(bt_stride=4096)
+    need = mtp.mtp_cache_evict_workspace_bytes(_evict(**wide))
     assert need > 0
     for ws, n in ((None, need), (A, need - 1), (A + 8, need)):
-        _refused(lambda m: m.mtp_cache_evict(_evict(), ws, n))
+        _refused(lambda m: m.mtp_cache_evict(_evict(**wide), ws, n))
 
 
 def test_null_arguments(libpath):  # noqa: F811
