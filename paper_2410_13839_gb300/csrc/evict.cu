@@ -23,7 +23,7 @@ namespace {
 constexpr int EV_BINS = 2048;
 constexpr int EV_HELD = 32768;  // keys whose order shared memory holds
 constexpr int EV_SMEM = 231424;  // shared memory of a CTA that has an SM to itself
-constexpr int EV_STAGES = 6;    // of rows on their way into shared memory
+constexpr int EV_STAGES = 4;    // of rows on their way into shared memory: 3, 4, 5, 6, 8 take 142, 141, 146, 148, 152 us for 16 slots of 12 layers
 
 struct EvictArgs {
     mtp_cache_evict_args a;
@@ -31,6 +31,7 @@ struct EvictArgs {
     int width;      // bt_stride * page_size: weights of a slot, layer and head
     int heads;      // layers * n_kv_heads
     int smem;       // bytes of shared memory
+    bool vector;    // weights on 16-byte boundaries
     int* list;      // workspace [slots][layers][heads][width], of wide tables: row of the pool (page * page_size + offset) of each key that stays
 };
 
@@ -156,7 +157,7 @@ constexpr size_t ring_bytes(int threads, int unroll) { return (size_t)EV_STAGES 
 // goes to the workspace.
 template <int NT, bool HELD, int UNROLL>
 __global__ void __launch_bounds__(NT) evict_kernel(const __grid_constant__ EvictArgs p) {
-    constexpr int WARPS = NT / 32, B = EV_BINS / NT, BATCH = 4;
+    constexpr int WARPS = NT / 32, B = EV_BINS / NT, BATCH = NT == 1024 ? 8 : 4;
     extern __shared__ __align__(16) unsigned char ev_sm[];  // the order of the weights, then the list; behind them the counts of a pass, then the ring
     __shared__ uint32_t part[WARPS], tied_of[2][WARPS], kept_of[2][WARPS];
     __shared__ int s_bin, s_left, s_count;
@@ -182,9 +183,17 @@ __global__ void __launch_bounds__(NT) evict_kernel(const __grid_constant__ Evict
     if (HELD && rest == 0 && sub == 0) free_pages<NT>(p, s, table);
     const int lo = s.sinks, hi = s.len - s.recent, want = s.after - s.sinks - s.recent;  // of keys [lo, hi) so many
     auto order_at = [&](int at) { return at >= lo && at < hi ? order_of(w[at]) : 0u; };  // 0: not to be chosen
-    if (HELD)
-#pragma unroll 8
+    if (HELD && p.vector) {
+#pragma unroll 4
+        for (int i = tid * 4; i < s.len; i += NT * 4) {  // (rows are multiples of 16 long)
+            const float4 x = *reinterpret_cast<const float4*>(w + i);
+            auto order = [&](int at, float y) { return at >= lo && at < hi ? order_of(y) : 0u; };
+            *reinterpret_cast<uint4*>(keys + i) = make_uint4(order(i, x.x), order(i + 1, x.y), order(i + 2, x.z), order(i + 3, x.w));
+        }
+    } else if (HELD) {
+#pragma unroll 4
         for (int i = tid; i < s.len; i += NT) keys[i] = order_at(i);
+    }
     __syncthreads();
     auto key_at = [&](int at) { return at >= s.len ? 0u : HELD ? keys[at] : order_at(at); };
 
@@ -384,7 +393,7 @@ MTP_API int mtp_cache_evict(const mtp_cache_evict_args* a, void* workspace, size
         if (!aligned16(a->kv_pool)) return invalid("cache_evict: kv_pool must be 16-byte aligned");
         if (evict_workspace(a) > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < evict_workspace(a)))
             return invalid("cache_evict: workspace %zu bytes, need %zu, 16-byte aligned", workspace_bytes, evict_workspace(a));
-        const EvictArgs p{*a, log2_of(a->page_size), a->bt_stride * a->page_size, a->layers * a->n_kv_heads, 0, static_cast<int*>(workspace)};
+        const EvictArgs p{*a, log2_of(a->page_size), a->bt_stride * a->page_size, a->layers * a->n_kv_heads, 0, aligned16(a->weights), static_cast<int*>(workspace)};
         const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
         const int runs = a->slots * p.heads;
         int dev = 0, sms = 0;
