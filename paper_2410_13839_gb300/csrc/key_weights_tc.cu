@@ -92,7 +92,6 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
     unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(wt_raw) + 1023) & ~(uintptr_t)1023);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int group = blockIdx.x / a.kv_heads, head = blockIdx.x - group * a.kv_heads, slot = blockIdx.y, seg = blockIdx.z;
-    pdl_launch_dependents();
     pdl_wait();
     bool cut;
     const WeightsSlot s = weights_slot(a, slot, cut);
@@ -147,6 +146,8 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_base;
+    // (not before TMEM is there: a kernel behind this one that took it first would wait for this one, which waits for it)
+    pdl_launch_dependents();
     auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(FULL_MASK, mbar_wait(bar, parity & 1, a.err)) != 0; };
     // the place of a group of key tiles' c-th tile of rows: one of its own, or (one key tile) the two in turn
     constexpr int KT = L::KT, H = L::HALVES;

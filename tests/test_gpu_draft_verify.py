@@ -323,11 +323,12 @@ def test_pages_that_were_free_already_are_reported():
         assert int(o["err"]) == 2 and o["refs"].tolist() == refs and o["table"].tolist() == [[2, 1, -1, -1, -1]]
 
 
-def test_shared_pages_of_several_slots_and_a_graph():
+@pytest.mark.parametrize("vocab", [2000, 40000])
+def test_shared_pages_of_several_slots_and_a_graph(vocab):
     """Slots that give back the same page drop its count once each; a replay takes what the buffers hold then."""
     torch = pytest.importorskip("torch")
     mtp = lib_module()
-    c = _case(19, [4, 4, 4], 2000, "float16", True, [1.0, 0.0])
+    c = _case(19, [4, 4, 4], vocab, "float16", True, [1.0, 0.0])
     c["lens"] = [50, 50, 50]
     c["table"] = [[0, 1, 2, 3, -1], [0, 1, 4, 3, -1], [0, 1, 5, 3, -1]]
     c["refs"] = [3, 3, 1, 3, 1, 1, 0]
