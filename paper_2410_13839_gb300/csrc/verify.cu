@@ -229,11 +229,12 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
 }
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
     float2 d;
-    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
         : "=f"(d.x), "=f"(d.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
     return d;
 }
 
@@ -318,11 +319,14 @@ struct Held {
 template <int TYPE>
 __device__ __noinline__ long long hold_weights(const Row<TYPE> row, const Exponent e, uint32_t table, const Held held, int from, int to) {
     long long sum = 0;
+    int g = ((from + row.shift) >> 3) + threadIdx.x;
+    Raw<TYPE> next = row.fetch(g * 8);
 #pragma unroll 1
-    for (int g = ((from + row.shift) >> 3) + threadIdx.x; g * 8 - row.shift < to; g += VF_THREADS) {
+    for (; g * 8 - row.shift < to; g += VF_THREADS) {
         const int first = g * 8 - row.shift;
         float x[8];
-        decode<TYPE>(row.fetch(g * 8), x);
+        decode<TYPE>(next, x);
+        if (first + 8 * VF_THREADS < to) next = row.fetch((g + VF_THREADS) * 8);  // on its way
         const bool all = first >= from && first + 8 <= min(to, row.vocab);
         int su = 0, sv = 0;
 #pragma unroll
@@ -458,11 +462,12 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
                 }
             } else {
                 float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                const float low = -top * cf;  // (its rounding, 2^-24 of it, is all of the sum's: the comparison below allows for it)
 #pragma unroll
                 for (int k = 0; k < ITEM; ++k)
 #pragma unroll
                     for (int i = 0; i < 8; i += 2) {
-                        const float2 z = mul2(add2(make_float2(x[k][i], x[k][i + 1]), make_float2(-top, -top)), make_float2(cf, cf));
+                        const float2 z = fma2(make_float2(x[k][i], x[k][i + 1]), make_float2(cf, cf), make_float2(low, low));
                         sum[i >> 1 & 1] = add2(sum[i >> 1 & 1], make_float2(ex2(z.x), ex2(z.y)));
                     }
                 s.sum = fmaf(s.sum, ex2((s.top - top) * cf), (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
@@ -508,7 +513,9 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
                 const float l = unit(draft_u) * q * stat[tid].sum, r = ex2((draft_x - stat[tid].top) * cf) * q_sum;
                 keep = l < r;
                 const float big = fmaxf(l, r);
-                if (!(fabsf(l - r) > VF_NEAR * big) || big < 1e-25f) keep = 2;  // too near for 32 bits
+                const float size = fabsf(stat[tid].top) + (drafter ? fabsf(stat[n + tid].top) : 0.f);
+                // too near for 32 bits (a sum's error from its exponents: 2^-24 ln 2 of the largest, doubled)
+                if (!(fabsf(l - r) > (VF_NEAR + 0x1p-23f * size * cf) * big) || big < 1e-25f) keep = 2;
             }
         }
         state[tid] = keep;
