@@ -14,6 +14,12 @@
 // 512 keys: two pairs of tiles of 128, each with a place for S and eight warps, four for each half of the
 // columns; a thread has a key of both tiles, so that the log-sum-exps are read once for two.  While one pair
 // is summed the tensor cores make the other's.  128 keys: two places, four warps, and two CTAs an SM.
+//
+// Two chunks of 2000 to 4000 tokens after 6000 to 9000, 32 heads on 8 of 128 dims (540 GFLOP): 471 us, 1150
+// TFLOP/s, of the measured peak (cuBLAS, 1950) 59 %, and half of the rate of the exponentials (32 a cycle and
+// SM).  Without exponentials it takes 387 us, with a quarter of the products 420: neither covers the other's
+// latencies whole, and registers for more columns or TMEM for a third place are not there.  128 keys a CTA took
+// 614 us: every CTA reads all rows, 7 TB/s out of L2.  25 prompts of 182 to 578 tokens, 16 heads of 64: 36.9 us.
 #include <type_traits>
 
 #include "tcgen05.cuh"
@@ -254,7 +260,7 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
         __syncwarp();
     } else {
         // ---- the sums: a thread has a key of each of its group's key tiles, and its half of the columns ----
-        constexpr int COLS = WT_TILE / H, W = COLS / 4;  // columns of a warp, of a step
+        constexpr int COLS = WT_TILE / H, W = COLS / 4, STEPS = 4;  // columns of a warp, of a step
         const int g = warp / (4 * H), h = (warp >> 2) % H, row = tid & (WT_TILE - 1);
         const int2 has = group_range(g);
         const uint32_t lse = smem_addr(sm + L::LSE) + warp * 2 * COLS * 4;
@@ -299,31 +305,31 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
             if (!ok) break;
             tc_fence_after();
             const uint32_t ts = lanes + at * KT * WT_TILE;
-            const int steps = full ? 4 : min(4, (max(0, cols - h * COLS) + W - 1) / W);
+            const int steps = full ? STEPS : min(STEPS, (max(0, cols - h * COLS) + W - 1) / W);
             float2 acc[KT][2];
 #pragma unroll
             for (int t = 0; t < KT; ++t) acc[t][0] = acc[t][1] = make_float2(0.f, 0.f);
-            // (one key tile: the next columns are read while these are summed; more warps do without)
-            constexpr int AHEAD = TILES == 1 ? 2 : 1;
-            float x[AHEAD][KT][W];
+            // (Reading the next columns ahead takes registers, and more time than it saves: 25 prompts of up to 578 tokens 41.6 us, 36.9
+            // without, two chunks after 6000 to 9000 keys 567 and 460.)
+            float x[KT][W];
             auto read = [&](int i) {
 #pragma unroll
-                for (int t = 0; t < KT; ++t) tmem_ld_issue<W>(ts + t * WT_TILE + i * W, x[i % AHEAD][t]);
+                for (int t = 0; t < KT; ++t) tmem_ld_issue<W>(ts + t * WT_TILE + i * W, x[t]);
             };
             auto released = [&]() {  // S is in registers
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&s_empty[at]);
             };
-            // columns [c0, c1) of the warp's see the thread's keys
-            int c0[KT], c1[KT];
-#pragma unroll
-            for (int t = 0; t < KT; ++t) {
-                const int ahead = low + t * WT_TILE + row - pos;  // the key's position less the first token's
-                c0[t] = min(max(0, ahead), count) * a.group - h * COLS;
-                c1[t] = (a.window > 0 ? max(0, min(count, ahead + a.window)) : count) * a.group - h * COLS;
-            }
             auto add = [&](int i, auto masked) {  // (a body of its own without masks, which are as much work again)
+                int c0[KT], c1[KT];  // columns [c0, c1) of the warp's see the thread's keys
+                if (decltype(masked)::value)
+#pragma unroll
+                    for (int t = 0; t < KT; ++t) {
+                        const int ahead = low + t * WT_TILE + row - pos;  // the key's position less the first token's
+                        c0[t] = min(max(0, ahead), count) * a.group - h * COLS;
+                        c1[t] = (a.window > 0 ? max(0, min(count, ahead + a.window)) : count) * a.group - h * COLS;
+                    }
                 const float2 scale = make_float2(a.scale_log2, a.scale_log2);
 #pragma unroll
                 for (int e = 0; e < W / 4; ++e) {
@@ -331,7 +337,7 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
                     asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(z.x), "=f"(z.y), "=f"(z.z), "=f"(z.w) : "r"(lb + (i * W + 4 * e) * 4));
 #pragma unroll
                     for (int t = 0; t < KT; ++t) {
-                        const float* y = x[i % AHEAD][t] + 4 * e;
+                        const float* y = x[t] + 4 * e;
                         const float2 v = fma2(make_float2(y[0], y[1]), scale, make_float2(z.x, z.y));
                         const float2 w = fma2(make_float2(y[2], y[3]), scale, make_float2(z.z, z.w));
                         float2 p = make_float2(ex2(v.x), ex2(v.y)), q = make_float2(ex2(w.x), ex2(w.y));
@@ -347,15 +353,13 @@ __global__ void __launch_bounds__(WtLayout<HD, TILES>::THREADS, WtLayout<HD, TIL
                     }
                 }
             };
-            if (AHEAD == 2 && steps > 0) read(0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < STEPS; ++i) {
                 if (i >= steps) break;
-                if (AHEAD == 1) read(i);
+                read(i);
                 tmem_ld_wait();
 #pragma unroll
-                for (int t = 0; t < KT; ++t) tmem_ld_done(x[i % AHEAD][t]);
-                if (AHEAD == 2 && i + 1 < steps) read(i + 1);
+                for (int t = 0; t < KT; ++t) tmem_ld_done(x[t]);
                 if (i + 1 == steps) released();
                 if (full)
                     add(i, std::false_type());

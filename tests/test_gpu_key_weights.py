@@ -97,7 +97,10 @@ CASES = [  # new, lens, heads, kv_heads, dim, page
     ([30, 77], [30, 205], 10, 2, 64, 32), ([200, 3], [200, 640], 20, 4, 128, 128), ([300], [301], 1, 1, 64, 16),
     ([65, 64], [65, 1000], 16, 2, 64, 16), ([10], [2000], 64, 1, 128, 64),
     # few keys and many rows: the rows are cut into segments
-    ([1200], [1300], 4, 1, 64, 64), ([700, 1500], [700, 1600], 8, 1, 128, 16)]
+    ([1200], [1300], 4, 1, 64, 64), ([700, 1500], [700, 1600], 8, 1, 128, 16),
+    # long contexts with work for every SM: four key tiles of a CTA
+    ([40, 3, 60, 33, 50, 1, 0, 70], [2100, 1900, 60, 1500, 2048, 2, 500, 2000], 16, 16, 64, 64),
+    ([20, 9, 130, 1, 8, 30, 7, 0, 40, 25], [2300, 2000, 1990, 1, 800, 30, 513, 700, 640, 1025], 40, 8, 128, 16)]
 
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
