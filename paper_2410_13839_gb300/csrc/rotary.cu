@@ -9,7 +9,7 @@
 // A pair's turns per position are a 64-bit fraction of 2^64: the product with the position, modulo
 // 2^64, is the angle modulo whole turns, exactly.  What is left of the error is the fraction's last
 // place times the position, 2^-33 of a turn at most, and the rounding of the 32 highest bits to
-// fp32.  (fp32 products position * frequency are off by 0.06 radians at position 1,000,000; fp64's sine
+// fp32.  (fp32 products position * frequency are off by up to 0.03 radians at position 1,000,000; fp64's sine
 // and cosine would be most of a call.)
 //
 // Bound by memory: every element is read and written once.  A CTA takes a few rows: its threads
