@@ -213,3 +213,35 @@ def test_evicted_again_and_again():
         _check(torch, o, want)
         st = dict(st, lens=o["lens"].tolist(), table=o["table"].cpu(), refs=o["refs"].tolist(), weights=o["weights"], pool=o["pool"])
     assert sum(st["refs"]) == 0
+
+
+def test_weights_off_the_16_byte_boundary():
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    for lens, keep in (([300, 77], [100, 77]), ([5000], [1234])):
+        st = _state(torch, 70, lens, 16, 1, 2, 64, torch.float16, "special")
+        buf = torch.empty(st["weights"].numel() + 1, device="cuda")
+        moved = buf[1:].view(st["weights"].shape)
+        moved.copy_(st["weights"])
+        st["weights"] = moved
+        assert moved.data_ptr() % 16 == 4
+        _check(torch, _call(torch, mtp, st, keep, 3, 20)[0], _oracle(torch, st, keep, 3, 20))
+
+
+def test_two_streams_at_once():
+    """Calls on pools of their own, which overlap: wide tables in workspaces of their own."""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    for lens, keep in (([900, 1200], [400, 700]), ([40000], [9000])):
+        states = [_state(torch, 80 + i, lens, 64, 1, 2, 64, torch.bfloat16, "positive") for i in range(2)]
+        calls = [_call(torch, mtp, st, keep, 4, 64) for st in states]
+        streams = [torch.cuda.Stream() for _ in states]
+        torch.cuda.synchronize()
+        for (o, *_), st in zip(calls, states):
+            o["pool"].copy_(st["pool"])
+        torch.cuda.synchronize()
+        for (o, args, (ws, nbytes), _), s in zip(calls, streams):
+            mtp.mtp_cache_evict(args, ws, nbytes, s)
+        torch.cuda.synchronize()
+        for (o, *_), st in zip(calls, states):
+            _check(torch, o, _oracle(torch, st, keep, 4, 64))

@@ -366,3 +366,43 @@ def test_drawn_tokens_are_distributed_as_the_targets():
         found += q[d] * np.bincount(o["tokens"][:, 0].cpu().numpy(), minlength=4) / slots
     # acceptance p / q and the residual's borders: off by one of 64 rows or columns of the grid at most
     assert np.abs(found - p).max() <= 2 / grid
+
+
+def test_the_largest_vocabulary_of_equal_logits():
+    """2^18 tokens alike: the largest sum there is; token t's border is t / 2^18 exactly."""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    v, slots = 1 << 18, 6
+    numbers = [0.0, 0.5, 1.0 - 2.0 ** -24, 1.0, 123456.0 / v, (123457.0 - 2.0 ** -6) / v]
+    for value in (0.0, -3.0, float("-inf")):
+        c = dict(new=[1] * slots, logits=np.full((slots, v), value), draft=None, temperature=[0.7] * slots, tokens=[0] * slots,
+                 lens=[1] * slots, table=[[i] for i in range(slots)], refs=[1] * slots, page=16, max_new=1, eos=-1, dtype="float32",
+                 uniforms=[[0.0, u] for u in numbers])
+        args, o, keep = _args(torch, mtp, c)
+        mtp.mtp_draft_verify(args)
+        assert o["tokens"][:, 0].tolist() == [0, v // 2, v - 1, v - 1, 123456, 123456]
+
+
+def test_no_rows_at_all():
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    c = dict(new=[0, 0, 0], logits=np.zeros((0, 50)), draft=None, temperature=None, tokens=[], lens=[5, 0, 17],
+             table=[[0, -1], [-1, -1], [1, 2]], refs=[1, 1, 1], page=16, max_new=4, eos=3, dtype="bfloat16", uniforms=[])
+    args, o, keep = _args(torch, mtp, c)
+    mtp.mtp_draft_verify(args)
+    assert _got(o) == ([[-1] * 4] * 3, [0, 0, 0], [5, 0, 17], [0, 0, 0], c["table"], c["refs"]) and int(o["err"]) == 0
+
+
+def test_two_streams_at_once():
+    """Calls that overlap share nothing."""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    cases = [_case(60 + i, [5, 3, 7], 30000, "bfloat16", True, [1.0, 0.6]) for i in range(2)]
+    calls = [_args(torch, mtp, c) for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for (args, o, keep), s in zip(calls, streams):
+        mtp.mtp_draft_verify(args, s)
+    torch.cuda.synchronize()
+    for c, (args, o, keep) in zip(cases, calls):
+        assert _got(o) == _oracle(c)

@@ -269,3 +269,53 @@ def test_nothing_to_do():
     lse = torch.zeros(0, 2, device="cuda")
     _run(torch, mtp, c, 0, 0, lse, max_new=4)
     assert torch.equal(before, c["weights"])
+
+
+@pytest.mark.parametrize("new", [[1, 3], [90, 30], [600, 400]])
+def test_two_streams_at_once(new):
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    cases = [_case(torch, 41 + i, new, [700, 450], 4, 1, 64, 32, torch.float16) for i in range(2)]
+    lses = [_oracle(torch, c, 1, 0)[2].float() for c in cases]
+    wants = [_oracle(torch, c, 1, 0, l)[:2] for c, l in zip(cases, lses)]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    held = [_run(torch, mtp, c, 1, 0, l, stream=s) for c, l, s in zip(cases, lses, streams)]
+    torch.cuda.synchronize()
+    assert len(held) == 2
+    for c, (want, tol) in zip(cases, wants):
+        _check(torch, c, want, tol)
+
+
+def test_attention_and_weights_follow_each_other_on_one_stream():
+    """Kernels that hold tensor memory, launched behind each other without a wait of the host: each layer's weights come out
+    as alone."""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    c = _case(torch, 51, [300, 150, 70], [2100, 1500, 70], 16, 16, 64, 64, torch.bfloat16, layers=4)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    err = torch.zeros(1, **i32)
+    out, lse = torch.zeros_like(c["q"]).contiguous(), torch.zeros(c["q"].shape[0], 16, device="cuda")
+    lses = []
+    start = c["weights"].clone()
+    for rounds in range(3):
+        c["weights"].copy_(start)
+        for layer in range(4):
+            shared = dict(q=c["q"], kv_pool=c["pool"], layer=layer, block_table=c["table"], cu_rows=c["cu"], kv_lens=c["lens"],
+                          scale=c["scale"], max_new=300, max_keys=2100, err_word=err)
+            attend = mtp.chunk_attention_args(out=out, out_lse=lse, **shared)
+            n = mtp.mtp_chunk_attention_workspace_bytes(attend)
+            ws = torch.zeros(n, dtype=torch.uint8, device="cuda")
+            weigh = mtp.key_weights_args(lse=lse, weights=c["weights"], **shared)
+            m = mtp.mtp_key_weights_workspace_bytes(weigh)
+            ws2 = torch.zeros(max(m, 16), dtype=torch.uint8, device="cuda")
+            mtp.mtp_chunk_attention(attend, ws, n, torch.cuda.current_stream())
+            mtp.mtp_key_weights(weigh, ws2, m, torch.cuda.current_stream())
+            if rounds == 2:
+                lses.append(lse.clone())
+    assert int(err) == 0
+    got = c["weights"].clone()
+    c["weights"].copy_(start)
+    for layer in range(4):
+        want, tol, _ = _oracle(torch, c, layer, 0, lses[layer])
+        assert bool(((got[:, layer].double() - want[:, layer]).abs() <= tol[:, layer]).all())
