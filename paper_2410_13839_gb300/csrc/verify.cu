@@ -307,12 +307,20 @@ __device__ __noinline__ bool near_kept(float u, float x, float top, long long su
     return (double)u * q < exp2(((double)x - (double)top) * c) / ((double)sum * 0x1p-44);
 }
 
-// A window's weights of one distribution in shared memory: 45 bits each, the lowest 13 of them apart.
+// A window's weights of one distribution in shared memory, by places: 45 bits each, the lowest 13 of them apart.
 struct Held {
-    uint32_t hi, lo;  // addresses: [window] words, [window] halfwords
-    __device__ __forceinline__ void put(int i, long long w) const {
-        asm volatile("st.shared.b32 [%0], %1;" ::"r"(hi + i * 4), "r"((uint32_t)(w >> 13)) : "memory");
-        asm volatile("st.shared.b16 [%0], %1;" ::"r"(lo + i * 2), "h"((uint16_t)(w & 8191)) : "memory");
+    uint32_t hi, lo;  // addresses: words, halfwords
+    // places i .. i + 7 of the window (i a multiple of 8)
+    __device__ __forceinline__ void put(int i, const long long (&w)[8]) const {
+        uint32_t x[8], y[4];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = (uint32_t)(w[k] >> 13);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] = ((uint32_t)w[2 * k] & 8191) | ((uint32_t)w[2 * k + 1] & 8191) << 16;
+#pragma unroll
+        for (int k = 0; k < 8; k += 4)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(hi + (i + k) * 4), "r"(x[k]), "r"(x[k + 1]), "r"(x[k + 2]), "r"(x[k + 3]) : "memory");
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(lo + i * 2), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
     }
     __device__ __forceinline__ unsigned long long get(int i) const {
         uint32_t x;
@@ -327,7 +335,8 @@ struct Held {
 template <int TYPE>
 __device__ __noinline__ long long hold_weights(const Row<TYPE> row, const Exponent e, uint32_t table, const Held held, int from, int to) {
     long long sum = 0;
-    int g = ((from + row.shift) >> 3) + threadIdx.x;
+    const int g0 = (from + row.shift) >> 3;  // the window's first eight places
+    int g = g0 + threadIdx.x;
     Raw<TYPE> next = row.fetch(g * 8);
 #pragma unroll 1
     for (; g * 8 - row.shift < to; g += VF_THREADS) {
@@ -337,20 +346,20 @@ __device__ __noinline__ long long hold_weights(const Row<TYPE> row, const Expone
         if (first + 8 * VF_THREADS < to) next = row.fetch((g + VF_THREADS) * 8);  // on its way
         const bool all = first >= from && first + 8 <= min(to, row.vocab);
         int su = 0, sv = 0;
+        long long w[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             int u, v;
             ex_fixed(x[i], e, table, u, v);
             u -= EX_U;
             v -= EX_V;
-            if (!all) {
-                if (!row.in(first + i)) u = v = 0;  // (-inf, in the places of none, may count as a number)
-                if (first + i < from || first + i >= to) continue;
-            }
+            // (another window's, or none's, where -inf may count as a number)
+            if (!all && (!row.in(first + i) || first + i < from || first + i >= to)) u = v = 0;
             su += u;
             sv += v;
-            held.put(first + i - from, ((long long)u << 22) + v);
+            w[i] = ((long long)u << 22) + v;
         }
+        held.put((g - g0) * 8, w);
         sum += ((long long)su << 22) + sv;
     }
     return sum;
@@ -375,8 +384,9 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
     Stat* gather = parts + 2 * a.max_new + VF_WARPS;                // [ctas][2 max_new]
     long long* block_sum = reinterpret_cast<long long*>(gather + p.ctas * 2 * a.max_new);  // [blocks]
     const int window = min(p.blocks, VF_WINDOW) * VF_BLOCK;
-    const uint32_t table_at = smem_addr(table), held_at = smem_addr(block_sum + p.blocks);
-    const Held held_p{held_at, held_at + 8 * window}, held_q{held_at + 4 * window, held_at + 10 * window};
+    const uint32_t table_at = smem_addr(table), held_at = (smem_addr(block_sum + p.blocks) + 15) & ~15u;
+    const int room = window + 16;  // places of a window's tokens, in eights
+    const Held held_p{held_at, held_at + 8 * room}, held_q{held_at + 4 * room, held_at + 10 * room};
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, C = p.ctas, slot = blockIdx.x / C, rank = blockIdx.x - slot * C;
     constexpr int ITEM = VF_ITEM<TYPE>;
     const int V = a.vocab;
@@ -581,10 +591,13 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
             if (mode == DRAW_REST) sum[1] += hold_weights<TYPE>(d, zq, table_at, held_q, from, min(from + window, t1));
             held_from = from;
         };
-        auto weight = [&](int i) {  // of token held_from + i
-            long long w = (long long)held_p.get(i);
-            if (mode == DRAW_REST) w = max((long long)__umul64hi(w, sq) - (long long)__umul64hi(held_q.get(i), sp), 0ll);
-            if (mode == DRAW_WITHOUT && held_from + i == without) w = 0;
+        auto weight = [&](int token) {  // of the window that is held
+            long long w = (long long)held_p.get(token + t.shift - ((held_from + t.shift) & ~7));
+            if (mode == DRAW_REST) {
+                const unsigned long long q = held_q.get(token + d.shift - ((held_from + d.shift) & ~7));
+                w = max((long long)__umul64hi(w, sq) - (long long)__umul64hi(q, sp), 0ll);
+            }
+            if (mode == DRAW_WITHOUT && token == without) w = 0;
             return w;
         };
         // 0: both sums, where they are needed; 1: the weights' sums of blocks; 2: the token
@@ -601,7 +614,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
                     if (warp == 0) {
                         long long w[8], s = 0;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) s += w[i] = weight(first - from + i);
+                        for (int i = 0; i < 8; ++i) s += w[i] = weight(first + i);
                         s = warp_scan(s) + s_before - s;
                         int found = V;
 #pragma unroll
@@ -629,7 +642,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
                 for (int k = warp; k < blocks; k += VF_WARPS) {
                     long long s = 0;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) s += weight(k * VF_BLOCK + i * 32 + lane);
+                    for (int i = 0; i < 8; ++i) s += weight(from + k * VF_BLOCK + i * 32 + lane);
                     // (s < 2^48: two parts whose sums over a warp have 32 bits)
                     const uint32_t lo = __reduce_add_sync(FULL_MASK, (uint32_t)s & ((1u << 26) - 1)), hi = __reduce_add_sync(FULL_MASK, (uint32_t)(s >> 26));
                     s = ((long long)hi << 26) + lo;
@@ -724,7 +737,7 @@ cudaError_t allow_wide_cluster(const void* kernel) {  // (setting it again chang
 template <int TYPE>
 cudaError_t launch_verify(const DraftArgs& p, cudaStream_t s) {
     const size_t stats = 2 * p.a.max_new * (2 + p.ctas) + VF_WARPS, window = (size_t)std::min(p.blocks, VF_WINDOW) * VF_BLOCK;
-    const size_t smem = sizeof(ExTable) + stats * sizeof(Stat) + p.blocks * sizeof(long long) + window * 12;
+    const size_t smem = sizeof(ExTable) + stats * sizeof(Stat) + p.blocks * sizeof(long long) + 16 + (window + 16) * 12;
     if (p.ctas > 8) {
         const cudaError_t e = allow_wide_cluster(reinterpret_cast<const void*>(draft_verify_kernel<TYPE>));
         if (e != cudaSuccess) return e;
