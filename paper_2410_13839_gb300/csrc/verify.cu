@@ -20,9 +20,9 @@
 // and SM, took 15 us of a call where every thread made a logarithm.)
 //
 // Latency bounds it: three exchanges over the cluster, one after another, of about a microsecond each, and between them a
-// chain of 40 operations a weight, 8 to a thread at once.  32 slots of up to 9 rows, 48001 tokens, bf16 (29 MB): 36 us, as
-// long as its slot of 9 rows; of the chain phase 1 takes 11 to 14, the weights of both rows 13, the draw 6.
-// One slot, 5 rows of 32003: 15; 32 slots, 4 rows of 1025: 8.3.
+// chain of 40 operations a weight, 8 to a thread at once.  32 slots of up to 9 rows, 48001 tokens, bf16 (29 MB): 30 us, as
+// long as its slot of 9 rows (of 36 us, in an earlier form, phase 1 took 11 to 14, the weights of both rows 13, the draw 6).
+// One slot, 5 rows of 32003: 14; 32 slots, 4 rows of 1025: 8.3.
 // Code that is not in the instruction cache costs more than it saves: unrolled and inlined it was 128 KB.
 #include <algorithm>
 #include <climits>
@@ -34,11 +34,11 @@
 namespace mtp {
 namespace {
 
-constexpr int VF_THREADS = 256, VF_WARPS = VF_THREADS / 32;
 constexpr int VF_BLOCK = 256;      // tokens that are summed as one: 8 a lane
-constexpr int VF_WINDOW = 24;      // blocks whose weights shared memory holds
 template <int TYPE>
 constexpr int VF_ITEM = TYPE == MTP_F32 ? 2 : 4;  // blocks that a lane reads at once
+template <int NT>
+constexpr int VF_WINDOW = NT / 32 * 3;  // blocks whose weights shared memory holds: 73 KB and 148 KB
 constexpr int VF_MAX_NEW = 64, VF_MAX_VOCAB = 1 << 18, VF_MAX_CLUSTER = 16;
 constexpr float VF_HUGE = 1e38f;   // infinite logits count as this
 constexpr float VF_NEAR = 1e-4f;   // products nearer than this, relatively, are compared in 64 bits
@@ -118,7 +118,7 @@ __device__ __forceinline__ void ex_fixed(float x, const Exponent& e, uint32_t ta
     const int k = __float_as_int(kf) - e.steps;
     const float r = fmaf(kf - EX_ROUND, -1.f / EX_STEPS, p) + ((fmaf(x, e.c_lo, -e.rest) + err) + fmaf(x, e.c_hi, -p));
     ExEntry t;
-    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(t.hi), "=f"(t.lo) : "r"(table + (k & (EX_STEPS - 1)) * 8));
+    asm("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(t.hi), "=f"(t.lo) : "r"(table + (k & (EX_STEPS - 1)) * 8));
     const float scale = __int_as_float((int)((unsigned)k << (23 - EX_BITS) & 0xff800000u) + (127 << 23));
     // 2^r - 1, |r| < 2^-9: ln 2 r + (ln 2 r)^2 / 2 + (ln 2 r)^3 / 6
     const float m = r * fmaf(r, fmaf(r, 0.0555041087f, 0.2402265070f), 0.6931471806f);
@@ -332,18 +332,18 @@ struct Held {
 };
 // Weights of tokens [from, to) of a row; returns this thread's sum.  One body for all calls: inlined at each, the kernel's
 // instructions did not stay in the cache.
-template <int TYPE>
+template <int TYPE, int NT>
 __device__ __noinline__ long long hold_weights(const Row<TYPE> row, const Exponent e, uint32_t table, const Held held, int from, int to) {
     long long sum = 0;
     const int g0 = (from + row.shift) >> 3;  // the window's first eight places
     int g = g0 + threadIdx.x;
     Raw<TYPE> next = row.fetch(g * 8);
 #pragma unroll 1
-    for (; g * 8 - row.shift < to; g += VF_THREADS) {
+    for (; g * 8 - row.shift < to; g += NT) {
         const int first = g * 8 - row.shift;
         float x[8];
         decode<TYPE>(next, x);
-        if (first + 8 * VF_THREADS < to) next = row.fetch((g + VF_THREADS) * 8);  // on its way
+        if (first + 8 * NT < to) next = row.fetch((g + NT) * 8);  // on its way
         const bool all = first >= from && first + 8 <= min(to, row.vocab);
         int su = 0, sv = 0;
         long long w[8];
@@ -369,21 +369,22 @@ __device__ __noinline__ long long hold_weights(const Row<TYPE> row, const Expone
 enum DrawMode { DRAW_TARGET, DRAW_WITHOUT, DRAW_REST };  // p; p but for the drafted token; max(p - q, 0)
 
 // Grid (slots * ctas).
-template <int TYPE>
-__global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __grid_constant__ DraftArgs p) {
+template <int TYPE, int NT>
+__global__ void __launch_bounds__(NT, 512 / NT) draft_verify_kernel(const __grid_constant__ DraftArgs p) {
+    constexpr int WARPS = NT / 32, WINDOW = VF_WINDOW<NT>;
     extern __shared__ __align__(16) unsigned char vf_sm[];
     __shared__ int state[VF_MAX_NEW], fed[VF_MAX_NEW];  // of each draft: kept (2: near), the token
     __shared__ float numbers[VF_MAX_NEW];               // the rows' numbers for a draw
-    __shared__ long long warp_total[2][VF_WARPS], word[2][2][VF_MAX_CLUSTER];
+    __shared__ long long warp_total[2][WARPS], word[2][2][VF_MAX_CLUSTER];
     __shared__ int s_block;
     __shared__ long long s_before, s_at;
     const mtp_draft_verify_args& a = p.a;
     ExEntry* table = reinterpret_cast<ExEntry*>(vf_sm);
     Stat* stat = reinterpret_cast<Stat*>(vf_sm + sizeof(ExTable));  // [2 max_new], of rows
     Stat* parts = stat + 2 * a.max_new;                             // [2 max_new + warps], of the warps' parts of them
-    Stat* gather = parts + 2 * a.max_new + VF_WARPS;                // [ctas][2 max_new]
+    Stat* gather = parts + 2 * a.max_new + WARPS;                   // [ctas][2 max_new]
     long long* block_sum = reinterpret_cast<long long*>(gather + p.ctas * 2 * a.max_new);  // [blocks]
-    const int window = min(p.blocks, VF_WINDOW) * VF_BLOCK;
+    const int window = min(p.blocks, WINDOW) * VF_BLOCK;
     const uint32_t table_at = smem_addr(table), held_at = (smem_addr(block_sum + p.blocks) + 15) & ~15u;
     const int room = window + 16;  // places of a window's tokens, in eights
     const Held held_p{held_at, held_at + 8 * room}, held_q{held_at + 4 * room, held_at + 10 * room};
@@ -393,7 +394,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
     pdl_launch_dependents();
     if (C > 1) cluster_arrive_relaxed();  // (before the first push every CTA is there)
 #pragma unroll 1
-    for (int i = tid; i < EX_STEPS; i += VF_THREADS) table[i] = ex_table.e[i];
+    for (int i = tid; i < EX_STEPS; i += NT) table[i] = ex_table.e[i];
     pdl_wait();
     auto team = [&]() {
         if (C > 1) {
@@ -412,7 +413,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
         if (C > 1) cluster_wait();
         if (rank == 0) {
 #pragma unroll 1
-            for (int i = tid; i < a.max_new; i += VF_THREADS) out[i] = -1;
+            for (int i = tid; i < a.max_new; i += NT) out[i] = -1;
             if (tid == 0) {
                 a.out_counts[slot] = 0;
                 a.out_kv_lens[slot] = len;
@@ -445,7 +446,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
             if (drafter) draft_y = row_of(n + tid).at(draft);
         }
     }
-    auto first_item = [&](int w) { return (int)((long long)total * w / VF_WARPS); };
+    auto first_item = [&](int w) { return (int)((long long)total * w / WARPS); };
 #pragma unroll 1
     for (int it = first_item(warp), stop = first_item(warp + 1); it < stop;) {
         const int task = it / items, from = it, to = min(stop, (task + 1) * items);  // items [from, to) of a row
@@ -503,14 +504,14 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
     __syncthreads();
     if (C > 1) cluster_wait();
 #pragma unroll 1
-    for (int task = warp; task < tasks; task += VF_WARPS) {  // a lane per warp's part, then per CTA
-        const bool has = lane < VF_WARPS && max(first_item(lane), task * items) < min(first_item(lane + 1), (task + 1) * items);
+    for (int task = warp; task < tasks; task += WARPS) {  // a lane per warp's part, then per CTA
+        const bool has = lane < WARPS && max(first_item(lane), task * items) < min(first_item(lane + 1), (task + 1) * items);
         const Stat s = merge(has ? parts[task + lane] : Stat{-VF_HUGE, 0.f, INT_MAX, 0}, cf);
         if (lane < C) push(&gather[rank * 2 * a.max_new + task], lane, s);
     }
     team();
 #pragma unroll 1
-    for (int task = warp; task < tasks; task += VF_WARPS) {
+    for (int task = warp; task < tasks; task += WARPS) {
         Stat s = merge(lane < C ? gather[lane * 2 * a.max_new + task] : Stat{-VF_HUGE, 0.f, INT_MAX, 0}, cf);
         if (!(s.top > -VF_HUGE)) {  // nothing above what -infinity counts as: all alike
             s.sum = (float)V;
@@ -545,7 +546,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
     auto all_sums = [&](long long (&all)[2], long long& before) {
         __syncthreads();
         if (warp < 2) {
-            long long t = lane < VF_WARPS ? warp_total[warp][lane] : 0;
+            long long t = lane < WARPS ? warp_total[warp][lane] : 0;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(FULL_MASK, t, o);  // (in all lanes: up to 16 push it)
             if (lane < C) push(&word[turn][warp][rank], lane, t);
@@ -587,8 +588,8 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
         int held_from = -1;                 // first token of the window that is held
         auto hold = [&](int from, long long (&sum)[2]) {
             __syncthreads();  // (another window may still be read)
-            sum[0] += hold_weights<TYPE>(t, zp, table_at, held_p, from, min(from + window, t1));
-            if (mode == DRAW_REST) sum[1] += hold_weights<TYPE>(d, zq, table_at, held_q, from, min(from + window, t1));
+            sum[0] += hold_weights<TYPE, NT>(t, zp, table_at, held_p, from, min(from + window, t1));
+            if (mode == DRAW_REST) sum[1] += hold_weights<TYPE, NT>(d, zq, table_at, held_q, from, min(from + window, t1));
             held_from = from;
         };
         auto weight = [&](int token) {  // of the window that is held
@@ -608,7 +609,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
             if (pass == 2) {
                 const int k = s_block;
                 if (k >= 0) {  // (the whole CTA)
-                    const int from = t0 + k / VF_WINDOW * VF_WINDOW * VF_BLOCK, first = t0 + k * VF_BLOCK + lane * 8;
+                    const int from = t0 + k / WINDOW * WINDOW * VF_BLOCK, first = t0 + k * VF_BLOCK + lane * 8;
                     if (held_from != from) hold(from, again);
                     __syncthreads();
                     if (warp == 0) {
@@ -639,7 +640,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
                 const int blocks = (min(from + window, t1) - from) / VF_BLOCK;
                 long long sum = 0;
 #pragma unroll 1
-                for (int k = warp; k < blocks; k += VF_WARPS) {
+                for (int k = warp; k < blocks; k += WARPS) {
                     long long s = 0;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) s += weight(from + k * VF_BLOCK + i * 32 + lane);
@@ -708,7 +709,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
     if (rank == C - 1) {
         const int after = len - (n - 1 - kept);
 #pragma unroll 1
-        for (int i = tid; i < a.max_new; i += VF_THREADS)
+        for (int i = tid; i < a.max_new; i += NT)
             if (i != kept || cut) out[i] = i < kept ? fed[i] : -1;
         if (tid == 0) {
             a.out_counts[slot] = cut ? kept : kept + 1;
@@ -718,7 +719,7 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
         if (a.block_table) {
             const int mask = (1 << p.shift) - 1, from = (after + mask) >> p.shift, to = (len + mask) >> p.shift;
 #pragma unroll 1
-            for (int i = from + tid; i < to; i += VF_THREADS) {
+            for (int i = from + tid; i < to; i += NT) {
                 int* entry = a.block_table + (long long)slot * a.bt_stride + i;
                 const int page = *entry;
                 if (page < 0) continue;
@@ -734,15 +735,19 @@ __global__ void __launch_bounds__(VF_THREADS, 2) draft_verify_kernel(const __gri
 cudaError_t allow_wide_cluster(const void* kernel) {  // (setting it again changes nothing)
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
 }
-template <int TYPE>
-cudaError_t launch_verify(const DraftArgs& p, cudaStream_t s) {
-    const size_t stats = 2 * p.a.max_new * (2 + p.ctas) + VF_WARPS, window = (size_t)std::min(p.blocks, VF_WINDOW) * VF_BLOCK;
+template <int TYPE, int NT>
+cudaError_t launch_threads(const DraftArgs& p, cudaStream_t s) {
+    const size_t stats = 2 * p.a.max_new * (2 + p.ctas) + NT / 32, window = (size_t)std::min(p.blocks, VF_WINDOW<NT>) * VF_BLOCK;
     const size_t smem = sizeof(ExTable) + stats * sizeof(Stat) + p.blocks * sizeof(long long) + 16 + (window + 16) * 12;
     if (p.ctas > 8) {
-        const cudaError_t e = allow_wide_cluster(reinterpret_cast<const void*>(draft_verify_kernel<TYPE>));
+        const cudaError_t e = allow_wide_cluster(reinterpret_cast<const void*>(draft_verify_kernel<TYPE, NT>));
         if (e != cudaSuccess) return e;
     }
-    return launch(draft_verify_kernel<TYPE>, p.a.slots * p.ctas, VF_THREADS, smem, p.ctas, s, p);
+    return launch(draft_verify_kernel<TYPE, NT>, p.a.slots * p.ctas, NT, smem, p.ctas, s, p);
+}
+template <int TYPE>
+cudaError_t launch_verify(const DraftArgs& p, bool wide, cudaStream_t s) {
+    return wide ? launch_threads<TYPE, 512>(p, s) : launch_threads<TYPE, 256>(p, s);
 }
 
 }  // namespace
@@ -781,15 +786,22 @@ MTP_API int mtp_draft_verify(const mtp_draft_verify_args* a, void* cuda_stream) 
             cudaGetLastError();
             return cuda_status(e, "draft_verify");
         }
-        // CTAs of a slot: as long as two of them have room on an SM, and their parts of a row are a few blocks.  32 slots of 48001, us: 8 CTAs
-        // of 256 threads 36, of 512 37; 16 of 256, four or three an SM, 41 and 40; one slot: 8 CTAs 18, 16 15
+        // A slot's CTAs: as many as there are SMs for, as long as their parts of a row are a few blocks.  32 slots of 48001, us: 4 CTAs of 512
+        // threads 30; 8 of 256, two an SM, 34, of 512 40.
         int ctas = 1;
-        while (ctas < VF_MAX_CLUSTER && (long long)a->slots * ctas * 2 <= 2 * sms && a->vocab / (ctas * 2) >= VF_BLOCK * 4) ctas *= 2;
+        while (ctas < VF_MAX_CLUSTER && (long long)a->slots * ctas * 2 <= sms && a->vocab / (ctas * 2) >= VF_BLOCK * 4) ctas *= 2;
+        // CTAs of 512 threads, an SM each, if all run at once.  One slot of 32003, us: 14.1, of 256 threads 14.5; 128 slots of 9000 26.1 and 57.
+        // Wide clusters that the SMs hold side by side leave some of them over, 17 of 8 CTAs: 9000 19.0, of 256 threads, two an SM, 15.8; 8 of 16:
+        // 48001 21.3 and 19.8.  More slots than SMs: long rows want the threads (200 of 48001 170 and 262, of 9000 37 and 61), short ones the two
+        // slots an SM (200 of 4000 22.1 and 21.1, of 1025 18.1 and 14.1).
+        const bool wide = a->slots > sms ? a->vocab > 8192 : ctas < 8 || a->slots * ctas * 4 <= sms * 3;
         const int most = 16 / size - 1;  // places before a row's first token
         const int blocks = (a->vocab + most + VF_BLOCK - 1) / VF_BLOCK;
         const DraftArgs p{*a, a->block_table ? log2_of(a->page_size) : 0, ctas, (blocks + ctas - 1) / ctas};
         const cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-        e = a->logits_dtype == MTP_F32 ? launch_verify<MTP_F32>(p, s) : a->logits_dtype == MTP_BF16 ? launch_verify<MTP_BF16>(p, s) : launch_verify<MTP_F16>(p, s);
+        e = a->logits_dtype == MTP_F32    ? launch_verify<MTP_F32>(p, wide, s)
+            : a->logits_dtype == MTP_BF16 ? launch_verify<MTP_BF16>(p, wide, s)
+                                          : launch_verify<MTP_F16>(p, wide, s);
         return cuda_status(e, "draft_verify");
     });
 }

@@ -182,6 +182,13 @@ def test_many_slots_take_one_cta_each():
     _check(_case(5, [2] * 700, 300, "bfloat16", True, [1.0, 0.0]))
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("slots,new,vocab", [(160, 1, 8193), (160, 2, 8192), (153, 2, 9001), (40, 2, 9001), (17, 3, 9001), (14, 3, 9001), (9, 2, 40001),
+                                             (8, 2, 33001), (7, 3, 33001), (76, 2, 4100), (77, 2, 4100)])
+def test_slots_at_the_bounds_of_the_launches_forms(dtype, slots, new, vocab):
+    _check(_case(slots + vocab, [new] * slots, vocab, dtype, slots % 2 == 0, [0.8, 0.0, 1.2]), pad=slots % 3)
+
+
 def test_the_end_cuts():
     """eos among the drafts: kept, and nothing after it; eos drawn: done."""
     c = _case(9, [5, 5, 3, 1], 40, "float32", False, [0.0], eos=11)
