@@ -4,7 +4,8 @@
 //
 // A CTA has one (slot, layer, key head).  It selects: the weights are in shared memory, as
 // whole numbers in the order of the weights, and the m-th largest is found by its highest 11 bits, the 11
-// after them and the last 10, each time by counting how many keys have each value.  Of the keys
+// after them and the last 10, each time by counting how many keys have each value; few keys that share the
+// first bits are compared with each other instead.  Of the keys
 // equal to it the first ones stay.  Ballots and prefix sums then give each key that stays its place, and a list
 // of their rows in the pool takes the weights' place.
 // Then it moves keys and values in place: it goes through its list from the front, a stage of rows at a
@@ -12,9 +13,9 @@
 // again, so that no copy of the cache is needed; further stages are on their way into shared memory
 // meanwhile.  Memory bounds it: one CTA's selection lies behind another's moves.  A small kernel before looks at
 // the tables: no count changes before every page has been looked at.
-// 16 slots of 180 to 2000 keys cut to 700, 12 layers of 16 heads of 64 (773 MB): 140 us, 5.5 TB/s; four contexts of
-// 20,000 to 30,000 cut to 8192, 4 layers of 8 heads of 128 (1.08 GB): 220 us, of which the moves 171 and the selection, which all 128 CTAs
-// make at the same time, 35; one utterance, 1088 keys cut to 1024 (102 MB): 31 us, 9 of them before the first row moves.
+// 16 slots of 180 to 2000 keys cut to 700, 12 layers of 16 heads of 64 (773 MB): 136 us, 5.7 TB/s; four contexts of
+// 20,000 to 30,000 cut to 8192, 4 layers of 8 heads of 128 (1.08 GB): 190 us, of which the selection, which all 128 CTAs
+// make at the same time, about 25; one utterance, 1088 keys cut to 1024 (102 MB): 27 us, 8 of them before the first row moves.
 // (Found bit by bit, with 32 counts, the selections took 16, 126 and 67 us of their own; from registers, 16 to 64
 // keys a thread, the unrolled code did not stay in the instruction cache.)
 #include <algorithm>
@@ -26,9 +27,10 @@ namespace mtp {
 namespace {
 
 constexpr int EV_BINS = 2048;
-constexpr int EV_HELD = 32768;  // keys whose order shared memory holds
+constexpr int EV_HELD = 32768;   // keys whose order shared memory holds
 constexpr int EV_SMEM = 231424;  // shared memory of a CTA that has an SM to itself
-constexpr int EV_STAGES = 4;    // of rows on their way into shared memory: 3, 4, 5, 6, 8 take 142, 141, 146, 148, 152 us for 16 slots of 12 layers
+constexpr int EV_FEW = 256;      // keys of a border's bin that are compared with each other
+constexpr int EV_STAGES = 4;     // of rows on their way into shared memory: 3, 4, 6 take 140, 139, 147 us for 16 slots of 12 layers
 
 struct EvictArgs {
     mtp_cache_evict_args a;
@@ -134,15 +136,22 @@ __device__ __forceinline__ void move_rows(const EvictArgs& p, const EvictSlot& s
     int in = EV_STAGES - 1, out = 0;
 #pragma unroll 1
     for (int j0 = s.sinks; j0 < s.after; j0 += step) {
+        int to[UNROLL];  // (looked up before the stores, which might change the table for all that the compiler knows)
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int j = j0 + u * rows + r0;
+            to[u] = active && j < s.after ? table[j >> p.shift] : -1;
+        }
         asm volatile("cp.async.wait_group %0;" ::"n"(EV_STAGES - 2) : "memory");
         __syncthreads();  // every row of this stage and the ones before is read
         ask(in);
         look(next += step);
+        uint4 piece[UNROLL];
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const int j = j0 + u * rows + r0;
-            if (active && j < s.after) *at(table[j >> p.shift], j & mask) = ring[(out * UNROLL + u) * NT + tid];
-        }
+        for (int u = 0; u < UNROLL; ++u) piece[u] = ring[(out * UNROLL + u) * NT + tid];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u)
+            if (to[u] >= 0) *at(to[u], (j0 + u * rows + r0) & mask) = piece[u];
         in = in + 1 == EV_STAGES ? 0 : in + 1;
         out = out + 1 == EV_STAGES ? 0 : out + 1;
     }
@@ -160,12 +169,13 @@ constexpr size_t ring_bytes(int threads, int unroll) { return (size_t)EV_STAGES 
 // Selection, and the moves: grid (run, its parts).  HELD: the weights' order is kept in shared memory, where the list takes its place, and the
 // CTA moves the rows (of keys and values, or one part's); else (rows past EV_HELD keys) the order is made again in every pass, and the list
 // goes to the workspace.
-template <int NT, bool HELD, int UNROLL>
-__global__ void __launch_bounds__(NT) evict_kernel(const __grid_constant__ EvictArgs p) {
+template <int NT, bool HELD, int UNROLL, int CTAS>
+__global__ void __launch_bounds__(NT, CTAS) evict_kernel(const __grid_constant__ EvictArgs p) {
     constexpr int WARPS = NT / 32, B = EV_BINS / NT, BATCH = NT == 1024 ? 8 : 4;
     extern __shared__ __align__(16) unsigned char ev_sm[];  // the order of the weights, then the list; behind them the counts of a pass, then the ring
     __shared__ uint32_t part[WARPS], tied_of[2][WARPS], kept_of[2][WARPS];
-    __shared__ int s_bin, s_left, s_count;
+    __shared__ int s_bin, s_left, s_count, s_few;
+    __shared__ uint32_t s_border;
     uint32_t* keys = reinterpret_cast<uint32_t*>(ev_sm);
     uint32_t* bins = keys + (HELD ? p.width : 0);  // (widths are multiples of 16)
     const mtp_cache_evict_args& a = p.a;
@@ -173,6 +183,7 @@ __global__ void __launch_bounds__(NT) evict_kernel(const __grid_constant__ Evict
     const int run = blockIdx.x, sub = blockIdx.y, slot = run / p.heads, rest = run - slot * p.heads;
     pdl_launch_dependents();
     for (int i = tid; i < EV_BINS; i += NT) bins[i] = 0;
+    if (tid == 0) s_few = 0;
     pdl_wait();
     const EvictSlot s = evict_slot(a, slot);
     const bool moves = a.out_status[slot] == MTP_OK && s.after < s.len;
@@ -209,21 +220,15 @@ __global__ void __launch_bounds__(NT) evict_kernel(const __grid_constant__ Evict
     if (want > 0)
 #pragma unroll 1
         for (int shift = 21, width = 11; !all;) {
-#pragma unroll 4
-            for (int i0 = warp * 32; i0 < s.len; i0 += NT) {
-                const uint32_t key = key_at(i0 + lane);
-                const bool in = key != 0 && (shift == 21 || (key ^ border) >> (shift + width) == 0);
-                const unsigned who = __ballot_sync(FULL_MASK, in);
-                if (who == 0) continue;
-                // a warp's keys that are all alike are one addition (weights that are all 0, say)
-                const uint32_t digit = key >> shift & ((1u << width) - 1);
-                const int leader = __ffs(who) - 1;
-                const uint32_t first = __shfl_sync(FULL_MASK, digit, leader);
-                if (__all_sync(FULL_MASK, !in || digit == first)) {
-                    if (lane == leader) atomicAdd(&bins[digit], __popc(who));
-                } else if (in) {
-                    atomicAdd(&bins[digit], 1u);
-                }
+#pragma unroll 1
+            for (int i0 = tid; i0 < s.len; i0 += NT * 4) {
+                uint32_t key[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) key[e] = key_at(i0 + e * NT);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (key[e] != 0 && (shift == 21 || (key[e] ^ border) >> (shift + width) == 0))
+                        atomicAdd(&bins[key[e] >> shift & ((1u << width) - 1)], 1u);
             }
             __syncthreads();
             // the bin that the left-th largest is in: sums from the highest bin down, B bins a thread
@@ -263,6 +268,36 @@ __global__ void __launch_bounds__(NT) evict_kernel(const __grid_constant__ Evict
             left = s_left;
             all = s_count == left;
             if (shift == 0) break;
+            // Few: one utterance 29.8 -> 26.6 us, four long contexts 194.6 -> 190.3.  With 256 threads the code around it gets slower, the 16
+            // slots 136 -> 147.
+            if (const int n = s_count; NT > 256 && !all && n <= EV_FEW) {  // each one's place among them (the counts are 0 again)
+#pragma unroll 1
+                for (int i0 = warp * 32; i0 < s.len; i0 += NT) {
+                    const uint32_t key = key_at(i0 + lane);
+                    if (key != 0 && (key ^ border) >> shift == 0) bins[atomicAdd(&s_few, 1)] = key;
+                }
+                __syncthreads();
+                if (tid < n) {
+                    const uint32_t key = bins[tid];
+                    int above = 0, alike = 0;
+#pragma unroll 2
+                    for (int j = 0; j < n; j += 4) {
+                        const uint4 x = *reinterpret_cast<const uint4*>(bins + j);
+                        above += (x.x > key) + (x.y > key) + (x.z > key) + (x.w > key);
+                        alike += (x.x == key) + (x.y == key) + (x.z == key) + (x.w == key);
+                    }
+                    if (above < left && above + alike >= left) {
+                        s_border = key;
+                        s_left = left - above;
+                        s_count = alike;
+                    }
+                }
+                __syncthreads();
+                border = s_border;
+                left = s_left;
+                all = s_count == left;
+                break;
+            }
             width = shift == 21 ? 11 : 10;
             shift -= width;
         }
@@ -280,12 +315,14 @@ __global__ void __launch_bounds__(NT) evict_kernel(const __grid_constant__ Evict
         const int mine = i0 + warp * 32 * BATCH + lane;
         uint32_t key[BATCH];
         int n_sure = 0, n_tied = 0;
+        const bool any = i0 + warp * 32 * BATCH < s.len;  // (of the warp)
+        if (any)
 #pragma unroll
-        for (int e = 0; e < BATCH; ++e) {
-            key[e] = key_at(mine + e * 32);
-            n_sure += __popc(__ballot_sync(FULL_MASK, sure(mine + e * 32, key[e])));
-            if (ties) n_tied += __popc(__ballot_sync(FULL_MASK, key[e] == border));
-        }
+            for (int e = 0; e < BATCH; ++e) {
+                key[e] = key_at(mine + e * 32);
+                n_sure += __popc(__ballot_sync(FULL_MASK, sure(mine + e * 32, key[e])));
+                if (ties) n_tied += __popc(__ballot_sync(FULL_MASK, key[e] == border));
+            }
         if (lane == 0) {
             kept_of[turn][warp] = n_sure;
             tied_of[turn][warp] = n_tied;
@@ -297,6 +334,7 @@ __global__ void __launch_bounds__(NT) evict_kernel(const __grid_constant__ Evict
         int take = max(0, left - tied_before);
         place += __reduce_add_sync(FULL_MASK, sure_all) + (ties ? min(tied, left) : 0);
         left = max(0, left - tied);
+        if (!any) continue;
         int dst[BATCH], page[BATCH];
         float weight[BATCH];
 #pragma unroll
@@ -351,14 +389,14 @@ __global__ void __launch_bounds__(EM_THREADS) evict_move_kernel(const __grid_con
     move_rows<EM_THREADS, EM_UNROLL>(p, s, table, p.list + (long long)run * p.width, reinterpret_cast<uint4*>(ev_sm), layer, head, kv, 1);
 }
 
-template <int NT, bool HELD, int UNROLL>
+template <int NT, bool HELD, int UNROLL, int CTAS>
 cudaError_t launch_evict(EvictArgs p, int parts, cudaStream_t s) {
     const int runs = p.a.slots * p.heads;
     size_t smem = HELD ? ring_bytes(NT, UNROLL) + (size_t)p.width * 4 : EV_BINS * 4;
     if (HELD && NT == 1024) smem = EV_SMEM;  // (one CTA an SM)
     p.smem = (int)smem;
-    const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(evict_kernel<NT, HELD, UNROLL>), smem);
-    return e == cudaSuccess ? launch_ex(evict_kernel<NT, HELD, UNROLL>, dim3(runs, parts), NT, smem, s, 1, p) : e;
+    const cudaError_t e = ensure_kernel_smem(reinterpret_cast<const void*>(evict_kernel<NT, HELD, UNROLL, CTAS>), smem);
+    return e == cudaSuccess ? launch_ex(evict_kernel<NT, HELD, UNROLL, CTAS>, dim3(runs, parts), NT, smem, s, 1, p) : e;
 }
 
 size_t evict_workspace(const mtp_cache_evict_args* a) {
@@ -408,16 +446,20 @@ MTP_API int mtp_cache_evict(const mtp_cache_evict_args* a, void* workspace, size
             e = launch_ex(evict_check_kernel, dim3(std::max(a->slots, std::min(sms, a->n_pages / (4 * EC_THREADS)))), EC_THREADS, 0, s, 1, p);
         if (e != cudaSuccess) return cuda_status(e, "cache_evict");
         if (p.width <= EV_HELD) {
-            // Threads by the table's width, whose keys shared memory holds: CTAs of an SM 3, 2, 1.  Where all keys and values have room on the SMs
-            // at once, a CTA each (both make the selection).
-            if (p.width <= 4096)
-                e = runs * 2 <= 3 * sms ? launch_evict<512, true, 1>(p, 2, s) : launch_evict<256, true, 2>(p, 1, s);
+            // Threads by the table's width, whose keys shared memory holds: CTAs of an SM 5, 3, 2, 1 (and the registers that go with them: with
+            // those of 3, 8 slots of up to 10,000 keys took 249 us, with those of 2 202).  Where all keys and values have room on the SMs at
+            // once, a CTA each (both make the selection).  256 threads, 512: 16 slots of up to 2000 keys 136, 160 us, 24 of up to 2500 105, 115;
+            // 8 of up to 3000 154, 146, of up to 4000 293, 270.
+            if (p.width <= 4096 && runs * 2 <= 3 * sms)
+                e = launch_evict<512, true, 1, 3>(p, 2, s);
+            else if (p.width <= 2816)
+                e = launch_evict<256, true, 2, 5>(p, 1, s);
             else if (p.width <= 12288)
-                e = launch_evict<512, true, 1>(p, runs * 2 <= 2 * sms ? 2 : 1, s);
+                e = launch_evict<512, true, 1, 2>(p, runs * 2 <= 2 * sms ? 2 : 1, s);
             else
-                e = launch_evict<1024, true, 1>(p, runs * 2 <= sms ? 2 : 1, s);
+                e = launch_evict<1024, true, 1, 1>(p, runs * 2 <= sms ? 2 : 1, s);
         } else {
-            e = launch_evict<1024, false, 1>(p, 1, s);
+            e = launch_evict<1024, false, 1, 1>(p, 1, s);
             if (e == cudaSuccess) e = launch(evict_move_kernel, runs * 2, EM_THREADS, ring_bytes(EM_THREADS, EM_UNROLL), 1, s, p);
         }
         return cuda_status(e, "cache_evict");

@@ -119,6 +119,41 @@ def test_the_keys_of_largest_weight_stay(weights, lens, keep, sinks, recent, pag
     _check(torch, _call(torch, mtp, st, keep, sinks, recent, in_place=len(lens) > 1)[0], _oracle(torch, st, keep, sinks, recent))
 
 
+@pytest.mark.parametrize("values", [1, 3, 50, 2000])
+@pytest.mark.parametrize("alike", [2, 255, 256, 257, 600])
+@pytest.mark.parametrize("lens,page,layers,kv_heads", [
+    ([700, 701], 16, 1, 2), ([700, 701, 900, 650], 16, 4, 16), ([3000, 700], 64, 1, 2), ([4100, 2700, 650], 16, 4, 20), ([13000, 800], 128, 1, 2)])
+def test_borders_among_weights_that_are_nearly_alike(lens, page, layers, kv_heads, alike, values):
+    """A border between weights whose first bits are the same: few of them, more, and equal ones among them."""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    st = _state(torch, alike + values, lens, page, layers, kv_heads, 8, torch.bfloat16, "positive")
+    gen = torch.Generator(device="cuda").manual_seed(alike * values)
+    w = st["weights"]
+    for s, n in enumerate(lens):
+        x = 4.0 + torch.rand(w.shape[1:3] + (n,), device="cuda", generator=gen)
+        x[..., n // 2:] -= 3.0
+        where = torch.rand(x.shape, device="cuda", generator=gen).argsort(-1)[..., :alike]
+        near = 2.0 + torch.randint(0, values, where.shape, device="cuda", generator=gen) * 2.0 ** -22
+        w[s, ..., :n] = x.scatter(-1, where, near)
+    # kept: the large ones, and about half of those that are alike
+    above = int((w[0, 0, 0, : lens[0]] > 3.0).sum())
+    keep = [min(n, above * n // lens[0] + alike // 2) for n in lens]
+    _check(torch, _call(torch, mtp, st, keep, 0, 0)[0], _oracle(torch, st, keep, 0, 0))
+
+
+@pytest.mark.parametrize("weights", ["random", "ties"])
+@pytest.mark.parametrize("lens,page,layers,kv_heads", [
+    ([2816, 900, 30, 1], 16, 4, 20), ([2817, 2000, 64], 16, 4, 20), ([2800, 2000, 64], 16, 4, 20), ([4096, 300], 128, 6, 20), ([4097, 300], 16, 1, 2), ([4080, 300], 16, 1, 2),
+    ([12288], 16, 1, 200), ([12289], 16, 1, 90), ([32768], 128, 1, 3)])
+def test_widths_at_the_bounds_of_the_launches_forms(lens, page, layers, kv_heads, weights):
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    st = _state(torch, lens[0], lens, page, layers, kv_heads, 8, torch.float16, weights)
+    keep = [max(1, n * 2 // 3) for n in lens]
+    _check(torch, _call(torch, mtp, st, keep, 4, 9)[0], _oracle(torch, st, keep, 4, 9))
+
+
 @pytest.mark.parametrize("weights", ["ties", "same", "positive"])
 def test_more_keys_than_a_cta_holds(weights):
     """Rows of weights that are read again for every bit."""
