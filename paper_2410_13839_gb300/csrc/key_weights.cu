@@ -55,7 +55,7 @@ __device__ __forceinline__ void mma16<F16>(float (&d)[4], uint32_t a0, uint32_t 
 
 // Grid (chunk of keys and key head, slot).  NT: tiles of eight rows; KT: tiles of 16 keys that a warp has in flight.
 template <class T, int HD, int NT, int KT>
-__global__ void __launch_bounds__(KW_THREADS) key_weights_kernel(const __grid_constant__ WeightsArgs a, int chunk) {
+__global__ void __launch_bounds__(KW_THREADS, HD == 128 && NT == 4 ? 4 : 0) key_weights_kernel(const __grid_constant__ WeightsArgs a, int chunk) {
     constexpr int B = HD / 32;  // 16-byte pieces of a row per lane: dimensions 32 b + 8 (lane % 4) .. + 7
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = blockIdx.x / a.kv_heads, head = blockIdx.x - part * a.kv_heads, slot = blockIdx.y;
     pdl_launch_dependents();
@@ -233,9 +233,11 @@ cudaError_t launch_few(const WeightsArgs& a, cudaStream_t s) {
     const int packed = std::min(a.max_new, a.rows) * a.group;
     // Tiles in flight, and how often: once, twice, four and eight times two tiles 18.9, 15.9, 15.4, 18.7 us (a step of 32 slots) and 63, 52, 49, 50
     // (4 drafts on 8 long contexts); four tiles of 64 dims 17 to 22, of 128 dims 74, one of 128 dims 52 at best.
-    constexpr int KT = 2, chunk = KW_WARPS * 16 * KT * 4;
+    constexpr int chunk = KW_WARPS * 16 * 8;
+    // (17 to 32 rows of 128 dims: their fragments leave registers for one tile in four CTAs an SM, for two in two; 8 tokens on 8 long contexts,
+    // 4 heads a key head, 73 and 96 us, in three CTAs 75; on 32 short ones 24, 32, 29)
     const dim3 grid((a.keys + chunk - 1) / chunk * a.kv_heads, a.slots);
-    const auto kern = packed <= 8 ? key_weights_kernel<T, HD, 1, KT> : packed <= 16 ? key_weights_kernel<T, HD, 2, KT> : key_weights_kernel<T, HD, 4, KT>;
+    const auto kern = packed <= 8 ? key_weights_kernel<T, HD, 1, 2> : packed <= 16 ? key_weights_kernel<T, HD, 2, 2> : key_weights_kernel<T, HD, 4, HD == 128 ? 1 : 2>;
     return launch_ex(kern, grid, KW_THREADS, 0, s, 1, a, chunk);
 }
 
