@@ -10,11 +10,11 @@
 // Few rows: the keys are read once and memory bounds it.  A warp takes 16 keys at a time as M of
 // mma.sync (rows as N, eight at a time) straight from global memory into registers: the order of
 // the dimensions in a product is free, so a lane's 16 bytes of a key serve two steps of 16, and
-// its 16 bytes of a query row, taken in the same order, the same two.  No shared memory, no
-// barrier; every warp has several tiles' loads in flight.  A step of 32 slots (180 to 2000 keys, 16 heads of
+// its 16 bytes of a query row, taken in the same order, the same two.  Up to 16 rows (32 of 64 dims) are in registers,
+// more in shared memory, as each lane wants them; every warp has several tiles' loads in flight.  A step of 32 slots (180 to 2000 keys, 16 heads of
 // 64, 67 MB) takes 15.3 us, 9.9 of which are memory's: a CTA's chain of look-ups (slot, page, keys), about 2.5 us, comes
 // before its first byte.  4 drafts on 8 slots of 4,000 to 30,000 keys, 8 key heads of 128 dims (297 MB): 49.0 us,
-// 6.1 TB/s.
+// 6.1 TB/s.  8 drafts there (32 rows) 53, 16 (64 rows) 82.
 #include <algorithm>
 
 #include "weights.cuh"
@@ -29,7 +29,9 @@ int tc_encode_queries(CUtensorMap* map, const void* q, int dtype, int head_dim, 
 namespace {
 
 constexpr int KW_THREADS = 128, KW_WARPS = KW_THREADS / 32;
-constexpr int KW_FEW_ROWS = 32;  // packed rows up to which this file's kernel is used (their fragments are in registers)
+constexpr int KW_FEW_ROWS = 16, KW_MORE_ROWS = 64;  // packed rows up to which this file's kernel is used; on many keys
+template <int HD>
+constexpr int KW_HELD_ROWS = HD == 64 ? 32 : 16;  // and up to which their fragments are in registers, else in shared memory
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -53,9 +55,17 @@ __device__ __forceinline__ void mma16<F16>(float (&d)[4], uint32_t a0, uint32_t 
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Grid (chunk of keys and key head, slot).  NT: tiles of eight rows; KT: tiles of 16 keys that a warp has in flight.
+// A row tile's part of what the CTA's rows are, in shared memory.
+template <int HD>
+struct RowTile {
+    uint4 q[HD / 32][32];  // each lane's fragments
+    float l[8];            // log-sum-exps, times log2 e
+    int pos[8];
+};
+// Grid (chunk of keys and key head, slot).  NT: tiles of eight rows in registers, 0: as many as there are, in shared memory; KT: tiles of 16 keys
+// that a warp has in flight.
 template <class T, int HD, int NT, int KT>
-__global__ void __launch_bounds__(KW_THREADS, HD == 128 && NT == 4 ? 4 : 0) key_weights_kernel(const __grid_constant__ WeightsArgs a, int chunk) {
+__global__ void __launch_bounds__(KW_THREADS, NT == 0 ? 5 : 0) key_weights_kernel(const __grid_constant__ WeightsArgs a, int chunk) {
     constexpr int B = HD / 32;  // 16-byte pieces of a row per lane: dimensions 32 b + 8 (lane % 4) .. + 7
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = blockIdx.x / a.kv_heads, head = blockIdx.x - part * a.kv_heads, slot = blockIdx.y;
     pdl_launch_dependents();
@@ -69,38 +79,53 @@ __global__ void __launch_bounds__(KW_THREADS, HD == 128 && NT == 4 ? 4 : 0) key_
     if (last <= lowest) return;
 
     // the rows: fragments, log-sum-exps and positions of columns 2 (lane % 4), + 1 of every tile
-    uint4 q[NT][B];
-    float l[NT][2];
-    int pos[NT][2];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
+    const int tiles = NT > 0 ? NT : (rows + 7) >> 3;
+    auto fragment = [&](int t, int b) {
         const int p = t * 8 + (lane >> 2), token = p / a.group;
         const uint16_t* src = a.q + (long long)(s.row0 + token) * a.q_stride + (head * a.group + p - token * a.group) * HD + (lane & 3) * 8;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (p < rows) {
+            if (a.q_vec) {
+                v = *reinterpret_cast<const uint4*>(src + b * 32);
+            } else {
+                uint32_t w[4];
 #pragma unroll
-        for (int b = 0; b < B; ++b) {
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (p < rows) {
-                if (a.q_vec) {
-                    v = *reinterpret_cast<const uint4*>(src + b * 32);
-                } else {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = (uint32_t)src[b * 32 + 2 * e] | (uint32_t)src[b * 32 + 2 * e + 1] << 16;
-                    v = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-            }
-            q[t][b] = v;
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int c = t * 8 + (lane & 3) * 2 + e, token = c / a.group;
-            l[t][e] = 0.f;
-            pos[t][e] = -1;
-            if (c < rows) {
-                l[t][e] = a.lse[(long long)(s.row0 + token) * (a.kv_heads * a.group) + head * a.group + c - token * a.group] * LOG2E;
-                pos[t][e] = s.base + token;
+                for (int e = 0; e < 4; ++e) w[e] = (uint32_t)src[b * 32 + 2 * e] | (uint32_t)src[b * 32 + 2 * e + 1] << 16;
+                v = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
+        return v;
+    };
+    auto column = [&](int c, float& l, int& pos) {
+        const int token = c / a.group;
+        l = 0.f;
+        pos = -1;
+        if (c < rows) {
+            l = a.lse[(long long)(s.row0 + token) * (a.kv_heads * a.group) + head * a.group + c - token * a.group] * LOG2E;
+            pos = s.base + token;
+        }
+    };
+    constexpr int HELD = NT > 0 ? NT : 1;
+    uint4 q[HELD][B];
+    float l[HELD][2];
+    int pos[HELD][2];
+    extern __shared__ __align__(16) unsigned char kw_sm[];
+    RowTile<HD>* row_tiles = reinterpret_cast<RowTile<HD>*>(kw_sm);
+    if constexpr (NT > 0) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int b = 0; b < B; ++b) q[t][b] = fragment(t, b);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) column(t * 8 + (lane & 3) * 2 + e, l[t][e], pos[t][e]);
+        }
+    } else {
+        for (int t = warp; t < tiles; t += KW_WARPS) {
+#pragma unroll
+            for (int b = 0; b < B; ++b) row_tiles[t].q[b][lane] = fragment(t, b);
+            if (lane < 8) column(t * 8 + lane, row_tiles[t].l[lane], row_tiles[t].pos[lane]);
+        }
+        __syncthreads();
     }
     const int* table = a.block_table + (size_t)slot * a.bt_stride;
     float* out = a.weights + slot * a.w_slot + (long long)head * a.width;
@@ -128,13 +153,12 @@ __global__ void __launch_bounds__(KW_THREADS, HD == 128 && NT == 4 ? 4 : 0) key_
             const int key = key0 + j * 16;
             if (key >= last) break;
             float sum[2] = {0.f, 0.f};
-            const bool inner = key + 15 <= s.base && (a.window <= 0 || key > end - 1 - a.window) && rows == NT * 8;  // every row sees all
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
+            const bool seen = key + 15 <= s.base && (a.window <= 0 || key > end - 1 - a.window);  // by every row
+            auto add = [&](const uint4 (&rows_q)[B], const float (&rows_l)[2], const int (&rows_pos)[2], bool inner) {
                 float d[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int b = 0; b < B; ++b) {
-                    const uint4 x = k[j][0][b], y = k[j][1][b], z = q[t][b];
+                    const uint4 x = k[j][0][b], y = k[j][1][b], z = rows_q[b];
                     mma16<T>(d, x.x, y.x, x.y, y.y, z.x, z.y);
                     mma16<T>(d, x.z, y.z, x.w, y.w, z.z, z.w);
                 }
@@ -142,11 +166,28 @@ __global__ void __launch_bounds__(KW_THREADS, HD == 128 && NT == 4 ? 4 : 0) key_
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float w = ex2(fmaf(d[2 * h + e], a.scale_log2, -l[t][e]));
+                        float w = ex2(fmaf(d[2 * h + e], a.scale_log2, -rows_l[e]));
                         const int at = key + r + h * 8;
-                        if (!inner && (at > pos[t][e] || (a.window > 0 && at <= pos[t][e] - a.window))) w = 0.f;
+                        if (!inner && (at > rows_pos[e] || (a.window > 0 && at <= rows_pos[e] - a.window))) w = 0.f;
                         sum[h] += w;
                     }
+            };
+            if constexpr (NT > 0) {
+                const bool inner = seen && rows == NT * 8;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) add(q[t], l[t], pos[t], inner);
+            } else {
+#pragma unroll 2
+                for (int t = 0; t < tiles; ++t) {
+                    const RowTile<HD>& x = row_tiles[t];
+#pragma unroll
+                    for (int b = 0; b < B; ++b) q[0][b] = x.q[b][lane];
+                    const float2 y = *reinterpret_cast<const float2*>(x.l + (lane & 3) * 2);
+                    const int2 z = *reinterpret_cast<const int2*>(x.pos + (lane & 3) * 2);
+                    l[0][0] = y.x; l[0][1] = y.y;
+                    pos[0][0] = z.x; pos[0][1] = z.y;
+                    add(q[0], l[0], pos[0], seen && t * 8 + 8 <= rows);
+                }
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -210,16 +251,20 @@ int weights_plan(const mtp_key_weights_args* a, WeightsPlan* p) {
     }
     const long long width = (long long)a->bt_stride * a->page_size;
     const long long packed = (long long)std::min(a->max_new, a->rows) * p->group;  // rows of a slot and key head
-    p->few = packed <= KW_FEW_ROWS;
     p->key_tiles = (int)((std::min((long long)a->max_keys, width) + KW_TILE - 1) / KW_TILE);
+    const long long lists = (long long)a->slots * a->n_kv_heads, row_tiles = (packed + KW_TILE - 1) / KW_TILE;
+    const bool much = lists * p->key_tiles >= 8 * sms;  // work for all SMs
+    // This file's kernel and tcgen05, us: 24, 36, 64 rows of 128 dims on 8 contexts of 4,000 to 30,000 keys, 8 key heads, 53, 125; 65, 130; 83, 136;
+    // 32, 36, 64 rows on 32 of up to 2000 23, 40; 26, 43; 35, 44; 64 rows on 4 of up to 8000 34, 27.  Too few keys for all SMs: 32 rows on one
+    // context of 2000, 4 key heads, 12.4, 5.1
+    p->few = packed <= KW_FEW_ROWS || (packed <= KW_MORE_ROWS && much && p->key_tiles >= 8);
     p->segments = p->tiles = 1;
     p->need = 0;
     if (!p->few) {
-        const long long lists = (long long)a->slots * a->n_kv_heads, row_tiles = (packed + KW_TILE - 1) / KW_TILE;
         // four key tiles of a CTA read the rows from L2 a quarter as often: for long contexts that have work for all SMs.  One, four: two
         // chunks after 6000 to 9000 keys 607, 484 us, 8 slots of 9 new tokens and up to 16000 keys 57, 44; 25 prompts of up to
         // 578 tokens 41.5, 51.8, one chunk of 2000 tokens after 4000, one key head, 37.7, 42.9
-        p->tiles = p->key_tiles >= 16 && lists * p->key_tiles >= 8 * sms ? 4 : 1;
+        p->tiles = p->key_tiles >= 16 && much ? 4 : 1;
         // few keys and many rows: the rows are cut too, until every SM has work enough
         const long long groups = std::max(1ll, lists * ((p->key_tiles + p->tiles - 1) / p->tiles));
         p->segments = (int)std::max(1ll, std::min((row_tiles + 3) / 4, (8ll / (p->tiles == 4 ? 1 : 2) * sms + groups / 2) / groups));
@@ -234,11 +279,14 @@ cudaError_t launch_few(const WeightsArgs& a, cudaStream_t s) {
     // Tiles in flight, and how often: once, twice, four and eight times two tiles 18.9, 15.9, 15.4, 18.7 us (a step of 32 slots) and 63, 52, 49, 50
     // (4 drafts on 8 long contexts); four tiles of 64 dims 17 to 22, of 128 dims 74, one of 128 dims 52 at best.
     constexpr int chunk = KW_WARPS * 16 * 8;
-    // (17 to 32 rows of 128 dims: their fragments leave registers for one tile in four CTAs an SM, for two in two; 8 tokens on 8 long contexts,
-    // 4 heads a key head, 73 and 96 us, in three CTAs 75; on 32 short ones 24, 32, 29)
     const dim3 grid((a.keys + chunk - 1) / chunk * a.kv_heads, a.slots);
-    const auto kern = packed <= 8 ? key_weights_kernel<T, HD, 1, 2> : packed <= 16 ? key_weights_kernel<T, HD, 2, 2> : key_weights_kernel<T, HD, 4, HD == 128 ? 1 : 2>;
-    return launch_ex(kern, grid, KW_THREADS, 0, s, 1, a, chunk);
+    // Rows in shared memory: 17 to 32 of 128 dims on 8 contexts of 4,000 to 30,000 keys 53 us, in registers (two or four CTAs an SM) 96, 73; of
+    // 64 dims on 32 of up to 2000 13.0 and 11.3, on the long ones 25.5 and 27.1.
+    const bool held = packed <= KW_HELD_ROWS<HD>;
+    auto kern = packed <= 8 ? key_weights_kernel<T, HD, 1, 2> : packed <= 16 ? key_weights_kernel<T, HD, 2, 2> : key_weights_kernel<T, HD, 0, 1>;
+    if constexpr (HD == 64)
+        if (packed > 16 && held) kern = key_weights_kernel<T, HD, 4, 2>;
+    return launch_ex(kern, grid, KW_THREADS, held ? 0 : (size_t)(packed + 7) / 8 * sizeof(RowTile<HD>), s, 1, a, chunk);
 }
 
 }  // namespace

@@ -100,7 +100,10 @@ CASES = [  # new, lens, heads, kv_heads, dim, page
     ([1200], [1300], 4, 1, 64, 64), ([700, 1500], [700, 1600], 8, 1, 128, 16),
     # long contexts with work for every SM: four key tiles of a CTA
     ([40, 3, 60, 33, 50, 1, 0, 70], [2100, 1900, 60, 1500, 2048, 2, 500, 2000], 16, 16, 64, 64),
-    ([20, 9, 130, 1, 8, 30, 7, 0, 40, 25], [2300, 2000, 1990, 1, 800, 30, 513, 700, 640, 1025], 40, 8, 128, 16)]
+    ([20, 9, 130, 1, 8, 30, 7, 0, 40, 25], [2300, 2000, 1990, 1, 800, 30, 513, 700, 640, 1025], 40, 8, 128, 16),
+    # 17 to 64 rows on work for every SM: in registers, in shared memory
+    ([8, 0, 1, 5] * 5, [1100, 90, 700, 5] * 5, 32, 8, 128, 16), ([16, 9, 0, 1] * 5, [1100, 200, 640, 33] * 5, 32, 8, 128, 64),
+    ([16, 1, 13, 0] * 5, [1100, 1, 512, 600] * 5, 16, 8, 64, 128), ([31, 2, 25, 0] * 5, [1500, 2, 500, 1025] * 5, 16, 8, 64, 16)]
 
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
