@@ -696,8 +696,8 @@ typedef enum mtp_rotary_scaling {
                               of `low` and fewer are slowed down                                        */
 } mtp_rotary_scaling;
 
-/* How far each of the rot_dim / 2 pairs turns per position, as a fraction of 2^64 of a turn, for
- * mtp_rotary_append's `turns` (which stands in device memory: the caller copies them once).
+/* How far each of the rot_dim / 2 pairs turns per position, as a fraction of 2^64 of a turn, rounded to the
+ * nearest (the powers are made to about 100 bits), for mtp_rotary_append's `turns` (which stands in device memory: the caller copies them once).
  * out_turns: host memory.  rot_dim even, 2 to 256 (4 with MTP_ROTARY_BASE); base > 1; factor >= 1;
  * context > 0 and low < high with MTP_ROTARY_BANDS.  Errors: MTP_ERR_INVALID. */
 MTP_API int mtp_rotary_turns(int rot_dim, int scaling, double base, double factor, double context, double low,

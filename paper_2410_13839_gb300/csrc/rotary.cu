@@ -7,9 +7,9 @@
 // (halves) or 2 i and 2 i + 1 (pairs).  The rest of the head, and the values, are only rounded.
 //
 // A pair's turns per position are a 64-bit fraction of 2^64: the product with the position, modulo
-// 2^64, is the angle modulo whole turns, exactly.  What is left of the error is the fraction's last
-// place times the position, 2^-33 of a turn at most, and the rounding of the 32 highest bits to
-// fp32.  (fp32 products position * frequency are off by up to 0.03 radians at position 1,000,000; fp64's sine
+// 2^64, is the angle modulo whole turns, exactly.  What is left of the error is half the fraction's last
+// place times the position, 2^-34 of a turn at most (the fractions are made in twice fp64's precision: fp64's 53 bits
+// would be off by 2^-24 of a turn at position 2^31), and the rounding of the 32 highest bits to fp32.  (fp32 products position * frequency are off by up to 0.03 radians at position 1,000,000; fp64's sine
 // and cosine would be most of a call.)
 //
 // Bound by memory: every element is read and written once.  A CTA takes a few rows: its threads
@@ -272,6 +272,48 @@ cudaError_t launch_rotary(const RotaryArgs& p, bool vector, bool out_vector, cud
                                            : launch_pieces<T, SRC, PIECES_PAIRS>(p, vector, out_vector, s);
 }
 
+// ---- the turns, on the host: numbers as sums hi + lo of two fp64, about 100 bits ----
+
+struct Twice {
+    double hi, lo;
+};
+Twice joined(double hi, double lo) {  // |hi| >= |lo|
+    const double s = hi + lo;
+    return {s, lo - (s - hi)};
+}
+Twice operator+(Twice x, Twice y) {  // the rounding error of the sum of the first parts, exactly, with the second ones
+    const double s = x.hi + y.hi, t = s - x.hi;
+    return joined(s, ((x.hi - (s - t)) + (y.hi - t)) + (x.lo + y.lo));
+}
+Twice operator*(Twice x, Twice y) {
+    const double p = x.hi * y.hi;
+    return joined(p, std::fma(x.hi, y.hi, -p) + (x.hi * y.lo + x.lo * y.hi));
+}
+Twice operator-(Twice x) { return {-x.hi, -x.lo}; }
+Twice operator/(Twice x, Twice y) {
+    const double q = x.hi / y.hi;
+    return joined(q, (x + -(y * Twice{q, 0.0})).hi / y.hi);
+}
+constexpr Twice LN2{0x1.62e42fefa39efp-1, 0x1.abc9e3b39803fp-56}, TURNS{0x1.45f306dc9c883p-3, -0x1.6b01ec5417056p-57};  // TURNS: of a radian, 1 / (2 pi)
+// e^x = 2^k (1 + y)^256: y of a 256th of what x has beyond k ln 2, by its series (of at most 0.0014: 12 terms, 2^-140), squared 8 times
+Twice exp_twice(Twice x) {
+    const double k = std::nearbyint(x.hi / LN2.hi);
+    Twice r = x + -(LN2 * Twice{k, 0.0});
+    r = {r.hi / 256, r.lo / 256};
+    Twice y{0.0, 0.0};
+    for (int n = 12; n >= 1; --n) y = r * (y + Twice{1.0, 0.0}) / Twice{(double)n, 0.0};
+    for (int i = 0; i < 8; ++i) y = Twice{2 * y.hi, 2 * y.lo} + y * y;
+    y = y + Twice{1.0, 0.0};
+    return {std::ldexp(y.hi, (int)k), std::ldexp(y.lo, (int)k)};
+}
+// ln x, x > 0: one step of Newton's method from fp64's, x = 2^e m
+Twice log_twice(double x) {
+    int e = 0;
+    const double m = std::frexp(x, &e), y = std::log(m);
+    const Twice d = Twice{m, 0.0} * exp_twice({-y, 0.0}) + Twice{-1.0, 0.0};
+    return LN2 * Twice{(double)e, 0.0} + (Twice{y, 0.0} + (d + Twice{-0.5 * d.hi * d.hi, 0.0}));
+}
+
 }  // namespace
 }  // namespace mtp
 
@@ -290,20 +332,28 @@ MTP_API int mtp_rotary_turns(int rot_dim, int scaling, double base, double facto
             return invalid("rotary_turns: factor %g: 1 or more", factor);
         if (scaling == MTP_ROTARY_BASE) {
             if (rot_dim < 4) return invalid("rotary_turns: one pair alone has no base to scale");
-            base *= std::pow(factor, rot_dim / (rot_dim - 2.0));
-            if (!std::isfinite(base)) return invalid("rotary_turns: factor %g", factor);
+            if (!std::isfinite(base * std::pow(factor, rot_dim / (rot_dim - 2.0)))) return invalid("rotary_turns: factor %g", factor);
         }
         if (scaling == MTP_ROTARY_BANDS && !(context > 0.0 && std::isfinite(context) && low < high && std::isfinite(low) && std::isfinite(high)))
             return invalid("rotary_turns: context %g, bands from %g to %g turns", context, low, high);
-        const double turn = 6.283185307179586476925286766559;
+        const Twice one{1.0, 0.0}, scale{factor, 0.0};
+        Twice log_base = log_twice(base);
+        if (scaling == MTP_ROTARY_BASE) log_base = log_base + log_twice(factor) * Twice{(double)rot_dim, 0.0} / Twice{rot_dim - 2.0, 0.0};
         for (int i = 0; i < rot_dim / 2; ++i) {
-            double f = std::pow(base, -2.0 * i / rot_dim);  // radians per position
-            if (scaling == MTP_ROTARY_LINEAR) f /= factor;
+            Twice f = exp_twice(-(log_base * Twice{2.0 * i, 0.0} / Twice{(double)rot_dim, 0.0}));  // radians per position
+            if (scaling == MTP_ROTARY_LINEAR) f = f / scale;
             if (scaling == MTP_ROTARY_BANDS) {
-                const double kept = std::fmin(1.0, std::fmax(0.0, (context * f / turn - low) / (high - low)));
-                f = kept * f + (1.0 - kept) * f / factor;
+                const double about = (context * f.hi * TURNS.hi - low) / (high - low);
+                Twice kept{about > 0.5 ? 1.0 : 0.0, 0.0};
+                if (about > -0.5 && about < 1.5) {
+                    const Twice x = (Twice{context, 0.0} * f * TURNS + Twice{-low, 0.0}) / (Twice{high, 0.0} + Twice{-low, 0.0});
+                    kept = x.hi <= 0.0 ? Twice{0.0, 0.0} : x.hi < 1.0 ? x : one;
+                }
+                f = kept * f + (one + -kept) * f / scale;
             }
-            out_turns[i] = (uint64_t)std::llrint(std::ldexp(f / turn, 64));
+            const Twice turns = f * TURNS;
+            const double hi = std::ldexp(turns.hi, 64), whole = std::floor(hi);
+            out_turns[i] = (uint64_t)whole + (uint64_t)std::llrint((hi - whole) + std::ldexp(turns.lo, 64));
         }
         return MTP_OK;
     });

@@ -1,5 +1,6 @@
 """mtp_rotary_turns on the host: the pairs' turns per position against the formulas in 64 bits.  No GPU is needed."""
 import math
+from decimal import Decimal, localcontext
 
 import numpy as np
 import pytest
@@ -59,3 +60,33 @@ def test_refusals(libpath, rot, scaling, kw):  # noqa: F811
     with pytest.raises(mtp.MTPError) as e:
         _turns(rot, scaling, **kw)
     assert e.value.code == -1 and str(e.value)
+
+
+def _exact(i, rot, scaling, base, factor, context, low, high):
+    """A pair's turns per position in units of 2^-64, to 60 digits."""
+    with localcontext() as ctx:
+        ctx.prec = 60
+        base, factor, context, low, high = (Decimal(x) for x in (base, factor, context, low, high))
+        turn = 2 * Decimal("3.14159265358979323846264338327950288419716939937510582097494")
+        if scaling == "BASE":
+            base *= (factor.ln() * rot / (rot - 2)).exp()
+        f = (-2 * i * base.ln() / rot).exp()
+        if scaling == "LINEAR":
+            f /= factor
+        if scaling == "BANDS":
+            kept = min(Decimal(1), max(Decimal(0), (context * f / turn - low) / (high - low)))
+            f = kept * f + (1 - kept) * f / factor
+        return f / turn * 2 ** 64
+
+
+@pytest.mark.parametrize("scaling", ["PLAIN", "LINEAR", "BASE", "BANDS"])
+@pytest.mark.parametrize("rot,base,factor,context", [
+    (4, 10000.0, 4.0, 100.0), (64, 10000.0, 8.0, 8192.0), (64, 1.0 + 2.0 ** -40, 1.0, 30.0), (128, 500000.0, 32.0, 8192.0), (22, 1.5, 1.0, 50.0),
+    (256, 1e6, 40.0, 131072.0), (96, 1e300, 1.25, 4096.0), (128, 12345.678, 3.3, 5000.0)])
+def test_turns_are_the_formulas_to_their_last_place(libpath, scaling, rot, base, factor, context):  # noqa: F811
+    """At position 2^31 a turn's 64th place is 2^-33 of a turn: what the sines and cosines are promised at any position rests on it."""
+    from paper_2410_13839_gb300 import mtp
+    kw = dict(base=base, factor=factor, context=context, low=1.0, high=4.0)
+    for i, x in enumerate(_turns(rot, getattr(mtp, "MTP_ROTARY_" + scaling), **kw).tolist()):
+        # one rounding to a whole number; about 100 bits before it
+        assert abs(Decimal(x) - _exact(i, rot, scaling, **kw)) <= Decimal(0.5 + 2.0 ** -20), i
