@@ -835,7 +835,8 @@ MTP_API int mtp_draft_verify(const mtp_draft_verify_args* args, void* cuda_strea
  *   out_page_refs    int32 [n_pages] (may be page_refs itself)
  *   out_status       int32 [slots]: MTP_OK, or MTP_ERR_INVALID (a length outside the table, a keep below 0, a held
  *                    page outside the pool or with a count below 1, or one that would be written, from the one
- *                    behind the sinks on, that other slots hold too): such a slot stays as it is
+ *                    that the first key kept behind the sinks goes to on, that other slots hold too): such a slot
+ *                    stays as it is
  *   workspace        mtp_cache_evict_workspace_bytes(args) bytes, 16-byte aligned, of any content (0: may be NULL);
  *                    calls that overlap need workspaces of their own
  * Slots within their budgets stay as they are.  Positions turned into keys are not changed: the tokens that

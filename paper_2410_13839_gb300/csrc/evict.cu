@@ -77,8 +77,8 @@ __global__ void __launch_bounds__(EC_THREADS) evict_check_kernel(const __grid_co
     bool bad = s.len < 0 || s.len > p.width || a.keep[slot] < 0;
     const int written = (s.after + mask) >> p.shift;
     if (!bad && s.after < s.len) {
-        // every held page is one and is counted; those that are written are in no other table
-        const int held = (s.len + mask) >> p.shift, same = s.sinks >> p.shift;
+        // every held page is one and is counted; those that are written, if a key stays behind the sinks, are in no other table
+        const int held = (s.len + mask) >> p.shift, same = s.after > s.sinks ? s.sinks >> p.shift : written;
 #pragma unroll 4
         for (int c = tid; c < held; c += EC_THREADS) {
             const int page = table[c], n = page >= 0 && page < a.n_pages ? a.page_refs[page] : 0;

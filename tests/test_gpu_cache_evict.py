@@ -280,3 +280,26 @@ def test_two_streams_at_once():
         torch.cuda.synchronize()
         for (o, *_), st in zip(calls, states):
             _check(torch, o, _oracle(torch, st, keep, 4, 64))
+
+
+@pytest.mark.parametrize("sinks,keep", [(20, 20), (20, 19), (20, 17), (17, 5), (64, 33), (40, 40)])
+def test_budgets_within_the_sinks_write_nothing(sinks, keep):
+    """A budget that the sinks fill: no row moves, so shared pages are no hindrance, whole or not; the others are given back."""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    st = _state(torch, sinks * keep, [64, 70], 16, 2, 2, 64, torch.bfloat16, "positive")
+    for s in range(2):
+        for c in range(-(-st["lens"][s] // 16)):
+            st["refs"][st["table"][s, c].item()] = 1 + (c + s) % 3
+    _check(torch, _call(torch, mtp, st, [keep] * 2, sinks, 3)[0], _oracle(torch, st, [keep] * 2, sinks, 3))
+
+
+def test_one_key_behind_the_sinks_is_written():
+    """The page that the sinks end in is written where a key follows them: a shared one is refused."""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    st = _state(torch, 91, [64, 64], 16, 1, 2, 64, torch.float16)
+    for s, keep in ((0, 20), (1, 21)):
+        st["refs"][st["table"][s, 1].item()] = 2
+    o = _call(torch, mtp, st, [20, 21], 20, 0)[0]
+    assert o["status"].tolist() == [0, -1] and o["lens"].tolist() == [20, 64]
