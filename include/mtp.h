@@ -796,7 +796,7 @@ MTP_API int mtp_key_weights(const mtp_key_weights_args* args, void* workspace, s
  *   err_word     int32 on the device or NULL.  A slot without rows gets no token.  Nor does one whose rows do not lie in
  *                the buffers, or are more than max_new or than its length, or whose length is outside the
  *                table: it stays as it is, and MTP_DEVICE_ERR_BOUNDS says so, as where a page that is given back
- *                is not in the pool or has a count below 1
+ *                is not in the pool (an entry below 0, too) or has a count below 1
  * A logit of NaN or -infinity counts as -10^38, infinity as 10^38; T as 10^-30 to 10^30.  Borders between tokens are exact to 2^-36
  * or so of the sum, and the outcome is the same in every call.
  * Limits: slots <= 8192, max_new <= 64, vocab <= 2^18, bt_stride * page_size <= 2^30.

@@ -722,10 +722,10 @@ __global__ void __launch_bounds__(NT, 512 / NT) draft_verify_kernel(const __grid
             for (int i = from + tid; i < to; i += NT) {
                 int* entry = a.block_table + (long long)slot * a.bt_stride + i;
                 const int page = *entry;
-                if (page < 0) continue;
+                const bool there = page >= 0 && page < a.n_pages;
                 *entry = -1;
-                if (page < a.n_pages && atomicSub(a.page_refs + page, 1) >= 1) continue;
-                if (page < a.n_pages) atomicAdd(a.page_refs + page, 1);  // it was free already
+                if (there && atomicSub(a.page_refs + page, 1) >= 1) continue;
+                if (there) atomicAdd(a.page_refs + page, 1);  // it was free already
                 if (a.err_word) atomicOr(a.err_word, ERR_BOUNDS);
             }
         }

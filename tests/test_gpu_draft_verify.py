@@ -413,3 +413,17 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for c, (args, o, keep) in zip(cases, calls):
         assert _got(o) == _oracle(c)
+
+
+def test_places_without_a_page_are_reported():
+    """An entry below 0 where a page is to be given back is no page of the pool."""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    c = _case(18, [9], 30, "float32", False, [0.0])
+    c["lens"], c["refs"] = [50], [0, 1, 1, 1, 0, 0, 0]
+    c["tokens"] = [-1] * 9
+    for entry in (-1, -2, -2 ** 31):
+        c["table"] = [[2, 1, 3, entry, -1]]
+        args, o, keep = _args(torch, mtp, c)
+        mtp.mtp_draft_verify(args)
+        assert int(o["err"]) == 2 and o["refs"].tolist() == c["refs"] and o["table"].tolist() == [[2, 1, 3, -1, -1]]
