@@ -775,7 +775,8 @@ MTP_API int mtp_key_weights(const mtp_key_weights_args* args, void* workspace, s
  *   p = softmax(logits / T), q = softmax(draft_logits / T) of the row, or without draft_logits 1 on the draft,
  * the draft d fed at row r + 1 is kept where the ones before it are and u q(d) < p(d), u = uniforms[r][0].  A kept
  * draft that is eos_id is the last token.  Else one more is drawn: behind the last kept of all drafts from w = p,
- * behind a draft that is not kept from w = max(p - q, 0) (where that is nothing, from p): the first token t with
+ * behind a draft that is not kept from w = max(p - q, 0) (where that is nothing, or with draft_logits no more than
+ * what rounding leaves of it, 2^-32 in all, from p): the first token t with
  * w_0 + .. + w_t > v (w_0 + ..), v = uniforms[r][1] of the row r it is drawn behind.  So drawn, tokens are
  * distributed as the target's.  T <= 0 (or NaN): the likeliest token, the lowest of equal ones, is all of p;
  * a draft is kept where it is that one.
@@ -798,7 +799,8 @@ MTP_API int mtp_key_weights(const mtp_key_weights_args* args, void* workspace, s
  *                table: it stays as it is, and MTP_DEVICE_ERR_BOUNDS says so, as where a page that is given back
  *                is not in the pool (an entry below 0, too) or has a count below 1
  * A logit of NaN or -infinity counts as -10^38, infinity as 10^38; T as 10^-30 to 10^30.  Borders between tokens are exact to 2^-36
- * or so of the sum, and the outcome is the same in every call.
+ * or so of p's sum: of w's sum where w is p, and 2^-36 / D of it where w = max(p - q, 0) adds up to D.  The outcome is the
+ * same in every call.
  * Limits: slots <= 8192, max_new <= 64, vocab <= 2^18, bt_stride * page_size <= 2^30.
  * Errors: MTP_ERR_INVALID, MTP_ERR_CUDA. */
 typedef struct mtp_draft_verify_args {

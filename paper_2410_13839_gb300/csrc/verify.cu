@@ -16,7 +16,8 @@
 // than a hundredth of that, so step 3's weights are whole numbers of 2^-44 (with 1024 parts of a power of two
 // in a table and a polynomial for the rest, 2^z to about 2^-36): their sums are exact and the same in any order, so
 // the outcome depends on nothing but the inputs.  They are made once and kept in shared memory, 45 bits each; the weights of
-// max(p - q, 0) are p's times q's sum less q's times p's sum, without a division.  (64-bit operations, two a cycle
+// max(p - q, 0) are p's times q's sum less q's times p's sum, without a division; where they add up to no more than what the
+// weights' own errors leave of two that are the same, there is nothing to draw from but p.  (64-bit operations, two a cycle
 // and SM, took 15 us of a call where every thread made a logarithm.)
 //
 // Latency bounds it: three exchanges over the cluster, one after another, of about a microsecond each, and between them a
@@ -585,6 +586,7 @@ __global__ void __launch_bounds__(NT, 512 / NT) draft_verify_kernel(const __grid
         const Exponent zq = make_exponent(stat[other].top, stat[other].tamed, cf, c_lo);
         const int without = more ? fed[kept] : -1;
         unsigned long long sp = 0, sq = 0;  // sums, shifted up: weights times the other one's are in the same units
+        long long noise = 0;                // what rounding may leave of p - q, where they are the same
         int held_from = -1;                 // first token of the window that is held
         auto hold = [&](int from, long long (&sum)[2]) {
             __syncthreads();  // (another window may still be read)
@@ -674,8 +676,10 @@ __global__ void __launch_bounds__(NT, 512 / NT) draft_verify_kernel(const __grid
                 const int up = __clzll(max(all[0], all[1]));
                 sp = (unsigned long long)all[0] << up;
                 sq = (unsigned long long)all[1] << up;
+                // (a weight errs by 2^-33 of itself at most, a share by twice that; half of what two shares differ by is above 0)
+                noise = (long long)(__umul64hi(all[0], sq) >> 32);
                 pass = 1;
-            } else if (all[0] == 0 && mode != DRAW_TARGET) {  // nothing is left of p: p
+            } else if (all[0] <= noise && mode != DRAW_TARGET) {  // nothing is left of p: p
                 mode = DRAW_TARGET;
             } else {
                 // the token's weight covers this place

@@ -427,3 +427,73 @@ def test_places_without_a_page_are_reported():
         args, o, keep = _args(torch, mtp, c)
         mtp.mtp_draft_verify(args)
         assert int(o["err"]) == 2 and o["refs"].tolist() == c["refs"] and o["table"].tolist() == [[2, 1, 3, -1, -1]]
+
+
+def _without_draft(c):
+    """Every slot's draft outside the vocabulary: a token is drawn behind its first row."""
+    for s in range(len(c["new"])):
+        c["tokens"][2 * s + 1] = -1 - s
+    return c
+
+
+@pytest.mark.parametrize("vocab,scale", [(50, 2.0), (1025, 2.0), (9000, 0.0), (9000, 5.0), (48001, 1.0), (48001, 8.0)])
+def test_a_drafter_that_is_the_target_leaves_only_rounding(vocab, scale):
+    """q = p, its logits a constant away: nothing is left of p - q but the rounding of both, and the token is drawn from p."""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    slots = 24
+    c = _without_draft(_case(vocab, [2] * slots, vocab, "float32", True, [1.0, 0.7, 1.3]))
+    rng = np.random.default_rng(vocab)
+    # multiples of 2^-10, and sums that fp32 holds
+    c["logits"] = np.round(rng.normal(0, scale, c["logits"].shape) * 1024) / 1024
+    c["draft"] = c["logits"] + np.array([3.0, -1.0, 0.625, 17.5])[np.arange(2 * slots) % 4][:, None]
+    args, o, keep = _args(torch, mtp, c)
+    mtp.mtp_draft_verify(args)
+    want = []
+    for s in range(slots):
+        cum = np.cumsum(_shares(c["logits"][2 * s], c["temperature"][s]))
+        want.append(int(np.searchsorted(cum, c["uniforms"][2 * s][1] * cum[-1], side="right")))
+    assert o["counts"].tolist() == [1] * slots and o["tokens"][:, 0].tolist() == want
+
+
+@pytest.mark.parametrize("vocab,near", [(1025, 1e-3), (9000, 1e-4), (48001, 1e-3), (48001, 1e-5)])
+def test_a_drafter_very_near_the_target(vocab, near):
+    """What is left of p - q is small: the borders of its draw are as exact as p and q are.  A weight errs by 2^-32 of itself at
+    most (its exponent's rest, below 2^-10, and the power of that are in fp32: three sums, three roundings each of 2^-35),
+    a share by twice that, p - q by four times, a border and the whole so much each; and every weight by 3 units of 2^-44 of the
+    row's largest."""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    slots = 48
+    c = _case(vocab, [2] * slots, vocab, "float32", True, [1.0, 0.8], near=near)
+    rng = np.random.default_rng(vocab)
+    for s in range(slots):
+        t = c["temperature"][s]
+        p, q = _shares(c["logits"][2 * s], t), _shares(c["draft"][2 * s], t)
+        c["tokens"][2 * s + 1] = int(rng.choice(np.flatnonzero(p < q * (1 - near / 8))))  # not kept by the largest number
+        c["uniforms"][2 * s][0] = 1.0 - 2.0 ** -24
+    args, o, keep = _args(torch, mtp, c)
+    mtp.mtp_draft_verify(args)
+    assert o["counts"].tolist() == [1] * slots
+    for s, token in enumerate(o["tokens"][:, 0].tolist()):
+        t = c["temperature"][s]
+        p = _shares(c["logits"][2 * s], t)
+        w = np.maximum(p - _shares(c["draft"][2 * s], t), 0)
+        cum, v = np.cumsum(w) / w.sum(), c["uniforms"][2 * s][1]
+        tol = (2.0 ** -29 + 6 * vocab * 2.0 ** -44 * p.max()) / w.sum()
+        assert (token == 0 or cum[token - 1] <= v + tol) and v < cum[token] + tol and tol < 1e-2, (s, token)
+
+
+def test_a_small_rest_of_a_sharp_target_is_drawn_from():
+    """Two rare tokens changed about, 2^-25 of the whole: the rest is the one that the target likes better."""
+    slots = 8
+    c = _case(3, [2] * slots, 3000, "float32", True, [1.0])
+    for r in range(2 * slots):
+        c["logits"][r], c["draft"][r] = -60.0, -60.0
+        c["logits"][r, 100] = c["draft"][r, 100] = 0.0
+        c["logits"][r, 7], c["draft"][r, 7] = -17.0, -18.0
+        c["logits"][r, 2000 + r], c["draft"][r, 2000 + r] = -18.0, -17.0
+    for s in range(slots):
+        c["tokens"][2 * s + 1] = 2000 + 2 * s
+        c["uniforms"][2 * s] = [0.9, (s + 0.5) / slots]
+    assert [t[0] for t in _check(c)[0]] == [7] * slots
