@@ -79,13 +79,13 @@ struct Exponent {
     bool wide;
 };
 constexpr float EX_ROUND = 12582912.f;  // 1.5 * 2^23
-__device__ __forceinline__ Exponent make_exponent(float top, bool tamed, float c_hi, float c_lo) {
+__device__ __forceinline__ Exponent make_exponent(float top, float c_hi, float c_lo) {
     Exponent e;
     e.c_hi = c_hi;
     e.c_lo = c_lo;
     e.top = top;
     const float p = top * c_hi;
-    e.wide = tamed || !(fabsf(p) < 2000.f);  // (2^21 steps)
+    e.wide = !(fabsf(p) < 2000.f);  // (2^21 steps; what infinite logits count as passes it at every temperature)
     e.low = (e.wide ? 0.f : top) - 100.f / c_hi;
     const float kf = fmaf(p, (float)EX_STEPS, EX_ROUND);
     e.steps = __float_as_int(EX_ROUND);
@@ -249,7 +249,7 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
 
 struct alignas(16) Stat {  // of a row's logits: the largest, sum of 2^((x - top) c), lowest token of the largest
     float top, sum;
-    int arg, tamed;  // tamed: some logit is not finite, or as large
+    int arg;
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -263,7 +263,7 @@ __device__ __forceinline__ void push(long long* p, int rank, long long v) {
 }
 __device__ __forceinline__ void push(Stat* p, int rank, const Stat& s) {
     const uint32_t at = dsmem_addr(p, rank);
-    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(__float_as_uint(s.top)), "r"(__float_as_uint(s.sum)), "r"(s.arg), "r"(s.tamed)
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(__float_as_uint(s.top)), "r"(__float_as_uint(s.sum)), "r"(s.arg), "r"(0)
                  : "memory");
 }
 // Of the lanes' rows one: c as Exponent's.
@@ -272,7 +272,6 @@ __device__ __forceinline__ Stat merge(const Stat& s, float c) {
     all.top = warp_max(s.top);
     all.sum = mtp::warp_sum(s.sum * ex2((s.top - all.top) * c));
     all.arg = __reduce_min_sync(FULL_MASK, s.top == all.top ? s.arg : INT_MAX);
-    all.tamed = __any_sync(FULL_MASK, s.tamed);
     return all;
 }
 __device__ __forceinline__ long long warp_scan(long long x) {  // inclusive
@@ -288,7 +287,7 @@ __device__ __forceinline__ long long warp_scan(long long x) {  // inclusive
 // A lane's part of the places [from, to) of a row, with what values that are not finite count as.
 template <int TYPE>
 __device__ __noinline__ Stat tame_stat(const Row<TYPE>& row, int from, int to, float c) {
-    Stat s{-VF_HUGE, 0.f, INT_MAX, 1};
+    Stat s{-VF_HUGE, 0.f, INT_MAX};
 #pragma unroll 1
     for (int j = from + (threadIdx.x & 31); j < to; j += 32) {
         const int token = j - row.shift;
@@ -452,7 +451,7 @@ __global__ void __launch_bounds__(NT, 512 / NT) draft_verify_kernel(const __grid
     for (int it = first_item(warp), stop = first_item(warp + 1); it < stop;) {
         const int task = it / items, from = it, to = min(stop, (task + 1) * items);  // items [from, to) of a row
         const Row<TYPE> row = row_of(task);
-        Stat s{-VF_HUGE, 0.f, INT_MAX, 0};
+        Stat s{-VF_HUGE, 0.f, INT_MAX};
         Raw<TYPE> raw[ITEM], next[ITEM];
 #pragma unroll 1
         for (int at = from - 1; at < to; ++at) {
@@ -495,10 +494,15 @@ __global__ void __launch_bounds__(NT, 512 / NT) draft_verify_kernel(const __grid
             s.top = top;
         }
         it = to;
-        // values that are not finite show in the sum or the largest (or in that there is none): the row's part once more, with care
         const float most = warp_max(s.top);
-        if (!__all_sync(FULL_MASK, s.sum >= 0.f) || !(most < VF_HUGE && most > -VF_HUGE))
-            s = tame_stat<TYPE>(row, (b0 + (from - task * items) * ITEM) * VF_BLOCK, min(b0 + p.blocks, b0 + (to - task * items) * ITEM) * VF_BLOCK, cf);
+        const int first = (b0 + (from - task * items) * ITEM) * VF_BLOCK, past = min(b0 + p.blocks, b0 + (to - task * items) * ITEM) * VF_BLOCK;
+        if (most == -VF_HUGE) {  // nothing above what -infinity counts as: its tokens, if there are any, alike
+            const int token = max(0, first - row.shift), tokens = max(0, min(V, past - row.shift) - token);
+            s = Stat{-VF_HUGE, lane == 0 ? (float)tokens : 0.f, tokens > 0 ? token : INT_MAX};
+        } else if (!__all_sync(FULL_MASK, s.sum >= 0.f) || !(most < VF_HUGE)) {
+            // values that are not finite show in the sum or the largest: the row's part once more, with care
+            s = tame_stat<TYPE>(row, first, past, cf);
+        }
         s = merge(s, cf);
         if (lane == 0) parts[task + warp] = s;
     }
@@ -507,17 +511,14 @@ __global__ void __launch_bounds__(NT, 512 / NT) draft_verify_kernel(const __grid
 #pragma unroll 1
     for (int task = warp; task < tasks; task += WARPS) {  // a lane per warp's part, then per CTA
         const bool has = lane < WARPS && max(first_item(lane), task * items) < min(first_item(lane + 1), (task + 1) * items);
-        const Stat s = merge(has ? parts[task + lane] : Stat{-VF_HUGE, 0.f, INT_MAX, 0}, cf);
+        const Stat s = merge(has ? parts[task + lane] : Stat{-VF_HUGE, 0.f, INT_MAX}, cf);
         if (lane < C) push(&gather[rank * 2 * a.max_new + task], lane, s);
     }
     team();
 #pragma unroll 1
     for (int task = warp; task < tasks; task += WARPS) {
-        Stat s = merge(lane < C ? gather[lane * 2 * a.max_new + task] : Stat{-VF_HUGE, 0.f, INT_MAX, 0}, cf);
-        if (!(s.top > -VF_HUGE)) {  // nothing above what -infinity counts as: all alike
-            s.sum = (float)V;
-            s.tamed = 1;
-        }
+        Stat s = merge(lane < C ? gather[lane * 2 * a.max_new + task] : Stat{-VF_HUGE, 0.f, INT_MAX}, cf);
+        if (!(s.top > -VF_HUGE)) s.sum = (float)V;  // nothing above what -infinity counts as: all alike
         if (lane == 0) stat[task] = s;
     }
     __syncthreads();
@@ -582,8 +583,8 @@ __global__ void __launch_bounds__(NT, 512 / NT) draft_verify_kernel(const __grid
         const int other = more && drafter ? n + kept : kept;
         DrawMode mode = !more ? DRAW_TARGET : drafter ? DRAW_REST : DRAW_WITHOUT;
         const Row<TYPE> t = row_of(kept), d = row_of(other);
-        const Exponent zp = make_exponent(stat[kept].top, stat[kept].tamed, cf, c_lo);
-        const Exponent zq = make_exponent(stat[other].top, stat[other].tamed, cf, c_lo);
+        const Exponent zp = make_exponent(stat[kept].top, cf, c_lo);
+        const Exponent zq = make_exponent(stat[other].top, cf, c_lo);
         const int without = more ? fed[kept] : -1;
         unsigned long long sp = 0, sq = 0;  // sums, shifted up: weights times the other one's are in the same units
         long long noise = 0;                // what rounding may leave of p - q, where they are the same

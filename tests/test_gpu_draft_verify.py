@@ -497,3 +497,57 @@ def test_a_small_rest_of_a_sharp_target_is_drawn_from():
         c["tokens"][2 * s + 1] = 2000 + 2 * s
         c["uniforms"][2 * s] = [0.9, (s + 0.5) / slots]
     assert [t[0] for t in _check(c)[0]] == [7] * slots
+
+
+def _nearest_numbers(x):
+    """Of each row the number in fp32 that is nearest to a border between tokens, relative to it."""
+    e = np.exp(x - x.max(-1, keepdims=True))
+    borders = np.cumsum(e, -1)[:, :-1] / e.sum(-1, keepdims=True)
+    near = borders.astype(np.float32)
+    best = np.argmin(np.abs(near.astype(np.float64) / borders - 1.0), -1)[:, None]
+    return np.take_along_axis(near, best, -1)[:, 0]
+
+
+@pytest.mark.parametrize("slots,padded", [(3000, 2048), (3000, 2560), (150, 4096), (40, 16385), (10, 50257), (1, 32768)])
+def test_masked_tokens_behind_a_row_change_nothing(slots, padded):
+    """Tokens of -infinity have no part in a draw, to the last bit of its borders, wherever the row is cut: the numbers are
+    the ones next to a border."""
+    torch = pytest.importorskip("torch")
+    mtp = lib_module()
+    vocab, many = 1025, 3000
+    x = np.random.default_rng(padded).normal(0, 2, (many, vocab)).astype(np.float32).astype(np.float64)
+    numbers = _nearest_numbers(x)
+
+    def drawn(first, logits):
+        n = len(logits)
+        c = dict(new=[1] * n, logits=logits, draft=None, temperature=None, tokens=[0] * n, lens=[1] * n, table=[[0]] * n,
+                 refs=[n], page=16, max_new=1, eos=-1, dtype="float32", uniforms=[[0.0, float(u)] for u in numbers[first:first + n]])
+        args, o, keep = _args(torch, mtp, c)
+        mtp.mtp_draft_verify(args)
+        return o["tokens"][:, 0].tolist()
+    want = drawn(0, x)
+    for first in range(0, min(many, 60 * slots), slots):
+        masked = np.full((slots, padded), -np.inf)
+        masked[:, :vocab] = x[first:first + slots]
+        assert drawn(first, masked) == want[first:first + slots]
+
+
+@pytest.mark.parametrize("slots,vocab", [(2, 1024), (32, 1024), (1, 4096), (32, 4096), (3, 16384), (1, 16385), (32, 16384), (1, 32768),
+                                         (2, 50257), (32, 50257), (1, 128256)])
+def test_vocabularies_that_leave_parts_without_tokens(slots, vocab):
+    c = _case(slots + vocab, [2 + slots % 2] * slots, vocab, "bfloat16", slots < 3, [0.8, 1.2, 0.0])
+    if slots > 2:
+        c["logits"][::2, vocab // 3:vocab // 2] = -np.inf
+        c["logits"][1::4, 7] = np.inf
+    _check(c)
+
+
+@pytest.mark.parametrize("vocab", [1024, 16385, 50257])
+def test_parts_without_tokens_at_extreme_temperatures(vocab):
+    """Temperatures whose exponents overflow where a part has no token, and where it has only -infinity."""
+    for dtype in ("float32", "float16"):
+        c = _case(vocab, [2] * 6, vocab, dtype, True, [1e-38, 0.01, 0.3, 1e30, float("inf"), 2.0])
+        c["logits"][1::2, 600:] = -np.inf
+        for s in range(6):  # no draft is a matter of 64 bits
+            c["uniforms"][2 * s][0] = 0.5
+        _check(c)
