@@ -697,7 +697,8 @@ typedef enum mtp_rotary_scaling {
 } mtp_rotary_scaling;
 
 /* How far each of the rot_dim / 2 pairs turns per position, as a fraction of 2^64 of a turn, rounded to the
- * nearest (the powers are made to about 100 bits), for mtp_rotary_append's `turns` (which stands in device memory: the caller copies them once).
+ * nearest (the powers are made to about 100 bits), for mtp_rotary_append's `turns` (which stands in device memory:
+ * the caller copies them once).
  * out_turns: host memory.  rot_dim even, 2 to 256 (4 with MTP_ROTARY_BASE); base > 1; factor >= 1;
  * context > 0 and low < high with MTP_ROTARY_BANDS.  Errors: MTP_ERR_INVALID. */
 MTP_API int mtp_rotary_turns(int rot_dim, int scaling, double base, double factor, double context, double low,
@@ -745,7 +746,7 @@ MTP_API int mtp_rotary_append(const mtp_rotary_append_args* args, void* cuda_str
  *   weights   float [slots][layers][n_kv_heads][bt_stride * page_size], read and written in place
  *   max_new, max_keys  host-known upper bounds of a slot's new tokens and length; rows and keys
  *             past them are left out, and MTP_DEVICE_ERR_BOUNDS says so in err_word, as for rows outside the
- *             buffers and lengths outside the table
+ *             buffers and lengths outside the table (where rows or one of them is 0 the call does nothing)
  *   err_word  int32 on the device or NULL: MTP_DEVICE_ERR_* bits are ORed in
  *   workspace mtp_key_weights_workspace_bytes(args) bytes, 16-byte aligned, of any content (0: may be NULL);
  *             calls that overlap need workspaces of their own
@@ -784,7 +785,7 @@ MTP_API int mtp_key_weights(const mtp_key_weights_args* args, void* workspace, s
  *   draft_logits as logits (stride draft_stride), or NULL; of a slot's last row nothing is read
  *   temperature  float [slots], or NULL: 1
  *   tokens       int32 [rows]: the token fed at each row; a draft outside the vocabulary is not kept
- *   uniforms     float [rows][2] in [0, 1) (other values count as the nearest, NaN as 0)
+ *   uniforms     float [rows][2] in [0, 1) (values below 0 and NaN count as 0, those above 1 as 1)
  *   kv_lens      int32 [slots]: lengths with all n tokens
  *   eos_id       the end's token, -1 = none
  *   out_tokens   int32 [slots][max_new]: the kept drafts, the token drawn, then -1

@@ -13,7 +13,7 @@
 // again, so that no copy of the cache is needed; further stages are on their way into shared memory
 // meanwhile.  Memory bounds it: one CTA's selection lies behind another's moves.  A small kernel before looks at
 // the tables: no count changes before every page has been looked at.
-// 16 slots of 180 to 2000 keys cut to 700, 12 layers of 16 heads of 64 (773 MB): 136 us, 5.7 TB/s; four contexts of
+// 16 slots of 180 to 2000 keys cut to 700, 12 layers of 16 heads of 64 (773 MB): 136 us (133 to 150 by the GPU), 5.7 TB/s; four contexts of
 // 20,000 to 30,000 cut to 8192, 4 layers of 8 heads of 128 (1.08 GB): 190 us, of which the selection, which all 128 CTAs
 // make at the same time, about 25; one utterance, 1088 keys cut to 1024 (102 MB): 27 us, 8 of them before the first row moves.
 // (Found bit by bit, with 32 counts, the selections took 16, 126 and 67 us of their own; from registers, 16 to 64

@@ -13,8 +13,9 @@
 // its 16 bytes of a query row, taken in the same order, the same two.  Up to 16 rows (32 of 64 dims) are in registers,
 // more in shared memory, as each lane wants them; every warp has several tiles' loads in flight.  A step of 32 slots (180 to 2000 keys, 16 heads of
 // 64, 67 MB) takes 15.3 us, 9.9 of which are memory's: a CTA's chain of look-ups (slot, page, keys), about 2.5 us, comes
-// before its first byte.  4 drafts on 8 slots of 4,000 to 30,000 keys, 8 key heads of 128 dims (297 MB): 49.0 us,
-// 6.1 TB/s.  8 drafts there (32 rows) 53, 16 (64 rows) 82.
+// before its first byte.  4 drafts on 8 slots of 4,000 to 30,000 keys, 8 key heads of 128 dims (297 MB): 49 to 56 us
+// by the GPU, 6.1 to 5.3 TB/s.  8 drafts there (32 rows) 53 to 57, 16 (64 rows) 82: every 16 keys' products read the rows' fragments from
+// shared memory again.  One slot alone, 2000 keys of 16 heads of 64 dims, 5.5: 64 CTAs, four rounds of loads in each.
 #include <algorithm>
 
 #include "weights.cuh"

@@ -1,5 +1,5 @@
-// key_weights_tc.cu -- the kernel of mtp_key_weights for more than 32 rows per slot and key
-// head (prompts, chunks): tcgen05.
+// key_weights_tc.cu -- the kernel of mtp_key_weights for more than 64 rows per slot and key head
+// (prompts, chunks), and for more than 16 on keys too few for every SM: tcgen05.
 //
 //   S^T = K Q^T        128 keys x up to 128 packed rows, fp32 in TMEM
 //   w_j += sum_p 2^(c S_jp - l_p)   a key per thread
@@ -15,9 +15,9 @@
 // columns; a thread has a key of both tiles, so that the log-sum-exps are read once for two.  While one pair
 // is summed the tensor cores make the other's.  128 keys: two places, four warps, and two CTAs an SM.
 //
-// Two chunks of 2000 to 4000 tokens after 6000 to 9000, 32 heads on 8 of 128 dims (540 GFLOP): 471 us, 1150
-// TFLOP/s, of the measured peak (cuBLAS, 1950) 59 %, and half of the rate of the exponentials (32 a cycle and
-// SM).  Without exponentials it takes 387 us, with a quarter of the products 420: neither covers the other's
+// Two chunks of 2000 to 4000 tokens after 6000 to 9000, 32 heads on 8 of 128 dims (540 GFLOP): 400 to 471 us by the GPU, 1150
+// TFLOP/s or more, of the measured peak (cuBLAS, 1950) 59 to 69 %, and half of the rate of the exponentials (32 a cycle and
+// SM).  (The other figures here are of the GPU that takes 471.)  Without exponentials it takes 387 us, with a quarter of the products 420: neither covers the other's
 // latencies whole, and registers for more columns or TMEM for a third place are not there.  128 keys a CTA took
 // 614 us: every CTA reads all rows, 7 TB/s out of L2.  25 prompts of 182 to 578 tokens, 16 heads of 64: 36.9 us.
 #include <type_traits>

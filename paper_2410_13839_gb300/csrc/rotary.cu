@@ -16,7 +16,8 @@
 // ask for their elements, make the rows' sines and cosines in shared memory meanwhile (a pair's
 // serve all heads), and turn.  14592 rows of 16 heads of 64 from fp32: 269 MB in 41.6 us, 6.5 TB/s; four pieces a thread
 // at once 48.0 us, two and no more registers than four CTAs of an SM have 41.6 (three CTAs 43.0, rows for
-// one batch or four of those 47.7, 48.2).  A step's 32 rows are latency, 3.0 us.
+// one batch or four of those 47.7, 48.2).  A step's 32 rows are latency, 2.7 us.  Halves that are no multiple of 8 long have
+// their partners loaded one by one: 14592 such rows with 40 of 64 elements turned take 69 us.
 #include <algorithm>
 #include <climits>
 #include <cmath>

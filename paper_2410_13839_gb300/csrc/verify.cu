@@ -23,7 +23,8 @@
 // Latency bounds it: three exchanges over the cluster, one after another, of about a microsecond each, and between them a
 // chain of 40 operations a weight, 8 to a thread at once.  32 slots of up to 9 rows, 48001 tokens, bf16 (29 MB): 30 us, as
 // long as its slot of 9 rows (of 36 us, in an earlier form, phase 1 took 11 to 14, the weights of both rows 13, the draw 6).
-// One slot, 5 rows of 32003: 14; 32 slots, 4 rows of 1025: 8.3.
+// One slot, 5 rows of 32003: 14, of 128256 21; 32 slots, 4 rows of 1025: 8.1.  Where a CTA's part of a row has more blocks than
+// shared memory holds the weights of, they are made again in every pass: 32 slots, 4 rows of 48001 24, of 50257 47, of 128256 75.
 // Code that is not in the instruction cache costs more than it saves: unrolled and inlined it was 128 KB.
 #include <algorithm>
 #include <climits>
