@@ -436,7 +436,7 @@ def _without_draft(c):
     return c
 
 
-@pytest.mark.parametrize("vocab,scale", [(50, 2.0), (1025, 2.0), (9000, 0.0), (9000, 5.0), (48001, 1.0), (48001, 8.0)])
+@pytest.mark.parametrize("vocab,scale", [(50, 2.0), (1025, 2.0), (9000, 0.0), (9000, 5.0), (48001, 1.0), (48001, 8.0), (70001, 2.0)])
 def test_a_drafter_that_is_the_target_leaves_only_rounding(vocab, scale):
     """q = p, its logits a constant away: nothing is left of p - q but the rounding of both, and the token is drawn from p."""
     torch = pytest.importorskip("torch")
